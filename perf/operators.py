@@ -275,8 +275,9 @@ def _own(s, case):
                              grad_gamma=s["grad_gamma"])
         return {"grad_x": s["grad_x"], "grad_gamma": s["grad_gamma"]}
     if case["op"] == "linear" and not case["back"]:
+        # 8-bit inference lets the 8-bit matrix instruction add: its sums are a hundred times closer than the bf16 output
         hb.heta_linear(s["g"], s["in"], s["W"], s["out"], bias=s["bias"], act=s["act"], residual=s["residual"],
-                       in_scale=s.get("in_scale"), w_scale=s.get("w_scale"))
+                       in_scale=s.get("in_scale"), w_scale=s.get("w_scale"), coarse_sums=case["dtype"] == "e4m3")
         return {"out": s["out"]}
     if case["op"] == "linear":
         hb.heta_linear_bwd(s["g"], s["in"], s["W"], s["grad_out"], act=s["act"], pre=s["pre"], grad_pre=s["grad_pre"],
