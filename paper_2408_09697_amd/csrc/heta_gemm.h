@@ -94,6 +94,89 @@ template <> __device__ __forceinline__ float convert<float, float>(float v) { re
 template <> __device__ __forceinline__ bf16_t convert<float, bf16_t>(float v) { return to_bf16(v); }
 template <> __device__ __forceinline__ bf16_t convert<bf16_t, bf16_t>(bf16_t v) { return v; }
 
+// ---- memory straight into LDS -----------------------------------------------------------------------
+typedef __attribute__((address_space(3))) void *lds_ptr_t;
+
+// s_waitcnt: at most N vector-memory operations outstanding and, optionally, no LDS operation
+// (gfx9 encoding: vmcnt[3:0] in bits 3:0, vmcnt[5:4] in bits 15:14, lgkmcnt in bits 11:8; expcnt
+// left at "no wait").
+template <int N, bool LDS_DONE> __device__ __forceinline__ void wait_counters()
+{
+    static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((LDS_DONE ? 0 : 15) << 8) | ((N >> 4) << 14));
+}
+
+// One 16-byte chunk per lane from global memory into LDS: lane l reads base + offset_l and its
+// chunk lands at lds_byte_addr + 16*l (base and lds_byte_addr are wavefront-uniform and travel in
+// scalar registers / M0, so advancing a tile costs no vector instruction).  Written as inline
+// assembly so that the compiler's wait-count insertion does not treat every later LDS read as
+// dependent on it (which would drain the whole prefetch ring); the kernel orders these loads
+// against their readers itself, with wait_counters() and the workgroup barrier.
+__device__ __forceinline__ void load_chunk_to_lds(const void *base, uint32_t offset, uint32_t lds_byte_addr)
+{
+    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "{m0}"(lds_byte_addr) : "memory");
+}
+
+// Workgroup barrier that the compiler may not move memory operations across, without the
+// "wait for every outstanding load" a fence would add.
+__device__ __forceinline__ void barrier_no_drain() { asm volatile("s_barrier" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t lds_address(const void *p)
+{
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)p));
+}
+
+// Chunk permutation of a k-contiguous LDS row: chunk c of row r sits at position c ^ swz(r).
+// Chosen so that 8 (32 banks) as well as 16 (64 banks) consecutive rows reading the same chunk
+// index cover every 16-byte bank group once.
+template <int CPR> __device__ __forceinline__ int swz(int r)
+{
+    if (CPR == 8) return ((r >> 1) + 4 * (r & 1)) & 7;
+    if (CPR == 4) return ((r >> 1) + (r >> 3)) & 3;
+    if (CPR == 2) return (r >> 2) & 1;
+    return 0;
+}
+
+// Place of chunk c (16 bytes, 8 values) in row k of an r-contiguous bf16 tile, and the chunk at place p: a transposing read
+// takes 64 bytes of four rows at a time, which have to fall on distinct banks (256 bytes of them).
+template <int CPR> __device__ __forceinline__ int rc_place(int c, int k)
+{
+    if (CPR % 16 == 0) return c ^ (4 * (k & 3));
+    const int s = 4 * ((k >> 1) & 1); // rows of an odd number of 128 bytes: the next row lies on the other half of the banks
+    if ((CPR & (CPR - 1)) == 0) return c ^ s;
+    return c + s >= CPR ? c + s - CPR : c + s;
+}
+template <int CPR> __device__ __forceinline__ int rc_chunk(int p, int k)
+{
+    if ((CPR & (CPR - 1)) == 0 || CPR % 16 == 0) return rc_place<CPR>(p, k);
+    const int s = 4 * ((k >> 1) & 1);
+    return p < s ? p - s + CPR : p - s;
+}
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float floatx2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const floatx2_t f = {lo, hi};
+    const bf16x2_t h = __builtin_convertvector(f, bf16x2_t);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// fp32 products on the bf16 matrix pipe.  x = h + m + l with three bf16 terms (h = bf16(x), m = bf16(x - h),
+// l = bf16(x - h - m); both differences are exact in fp32) is exact: eight bits each, a remainder's sign its ninth.
+// Only below 2^-110, where l leaves bf16's range, does x lose bits.  A product a b
+// is fed as the six terms ah bh, ah bm, am bh, am bm, ah bl, al bh (each a product of two 8-bit significands,
+// exact in the fp32 accumulator's input); |m| <= 2^-8 |x|, |l| <= 2^-17 |x|, so the three terms left out are at most
+// 2^-24 |a b|, the rounding of one fp32 multiplication (over random significands 2^-27.5 rms).  Six bf16 MFMAs of
+// 16 k-values cost 6 x 8 passes where the fp32 MFMA needs 8 x 16 for the same 16 k-values.
+__device__ __forceinline__ void split3_pair(float x0, float x1, uint32_t &h, uint32_t &m, uint32_t &l)
+{
+    h = pack_bf16(x0, x1);
+    const float r0 = x0 - __uint_as_float(h << 16), r1 = x1 - __uint_as_float(h & 0xffff0000u);
+    m = pack_bf16(r0, r1);
+    const float s0 = r0 - __uint_as_float(m << 16), s1 = r1 - __uint_as_float(m & 0xffff0000u);
+    l = pack_bf16(s0, s1);
+}
+
 // ---- LDS tile layouts ------------------------------------------------------------------------------
 // A k-contiguous operand (element (r,k) at base[r*ld + k]) is kept r-major in LDS, rows of one
 // tile's k-values (128 bytes) padded by 16 bytes: copied with 128-bit stores, fragments read with one 128-bit load
