@@ -50,9 +50,12 @@ typedef enum {
     HETA_ERR_DEVICE = 6       /* a HIP call failed; heta_last_error() carries the HIP message */
 } heta_status;
 
-typedef enum { HETA_F32 = 0, HETA_BF16 = 1 } heta_dtype;
+/* HETA_E4M3: 8 bits, 4 of exponent and 3 of significand (largest value 448, no infinities); only where a call names it */
+typedef enum { HETA_F32 = 0, HETA_BF16 = 1, HETA_E4M3 = 2 } heta_dtype;
 typedef enum { HETA_SUM = 0, HETA_MEAN = 1 } heta_reduce;
-typedef enum { HETA_ACT_NONE = 0, HETA_ACT_RELU = 1 } heta_act;
+/* GELU in its tanh form, x / (1 + exp(-2 sqrt(2 / pi) (x + 0.044715 x^3))), and SILU, x / (1 + exp(-x)), are activations of
+ * heta_linear and heta_linear_bwd; the other calls know NONE and RELU */
+typedef enum { HETA_ACT_NONE = 0, HETA_ACT_RELU = 1, HETA_ACT_GELU = 2, HETA_ACT_SILU = 3 } heta_act;
 
 /* flags of heta_graph_create */
 #define HETA_PTRS_ON_DEVICE 1u /* the index arrays of every heta_relation are device pointers */
@@ -603,6 +606,116 @@ typedef struct heta_adam_item {
 } heta_adam_item;
 heta_status heta_sparse_adam_multi(int32_t n_items, const heta_adam_item *items, float lr, float beta1, float beta2, float eps,
                                    int64_t step, void *hip_stream);
+
+/* ---- residual feed-forward blocks over node embeddings --------------------------------------------
+ * A deep model follows the relation aggregation of a node type with a block  h <- h + act(norm(h + agg) W1 + b1) W2 + b2.
+ * These calls are its norm, its products and the update of its matrices (and of the relations').
+ *
+ * heta_rms_norm: s = x + residual, rounded to x_dt;  rstd_i = 1 / sqrt(sum_j s_ij^2 / d + eps);  out = s rstd gamma.
+ *   x, residual (NULL: none), sum (NULL: not stored): device [n_rows, d] of x_dt; gamma: device fp32 [d] (NULL: ones);
+ *   rstd: device fp32 [n_rows] (NULL: not stored).  sum may be x or residual (same rows).
+ *   out: x_dt, or bf16, or HETA_E4M3: then scale (device fp32 [n_rows], otherwise NULL) receives
+ *   max_j |out_ij| / 448 and out holds the nearest 8-bit values of out / scale (a row of zeros: zeros, scale 0).
+ *   bf16 rows have no fp32 output. */
+heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, const void *residual, int64_t ld_res,
+                          const float *gamma, float eps, void *sum, int64_t ld_sum, void *out, heta_dtype out_dt, int64_t ld_out,
+                          float *scale, float *rstd, void *hip_stream);
+/* Its backward, x being the s that was normalised and rstd what the forward stored; with h = x rstd and w = grad_out gamma:
+ *   grad_x = rstd (w - h sum_j(w h) / d) + grad_sum;   grad_gamma = sum over the rows of grad_out h (fixed order; overwritten).
+ * grad_sum (NULL: none; what reaches s past the norm) and grad_x are of x_dt, grad_out of x_dt or bf16; grad_x may be grad_sum.
+ * grad_gamma: device fp32 [d] or NULL.  Uses the handle's workspace (may grow it). */
+heta_status heta_rms_norm_bwd(heta_graph *g, int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, const float *gamma,
+                              const float *rstd, const void *grad_out, heta_dtype go_dt, int64_t ld_go, const void *grad_sum, int64_t ld_gs,
+                              void *grad_x, int64_t ld_gx, float *grad_gamma, void *hip_stream);
+
+/* heta_linear: pre = in . W + bias;  out = act(pre) + residual  (the sums in fp32, out rounded once).
+ *   fp32 and bf16: in [n_rows, d_in], W [d_in, d_out] of one type; fp32 operands have an fp32 output, bf16 ones a bf16 or fp32 one.
+ *   HETA_E4M3: W is [d_out, d_in] (heta_linear_pack_e4m3), in_scale [n_rows] and w_scale [d_out] (device fp32) belong to the rows
+ *   of in and of W, pre = in_scale_i w_scale_j (in . W^T) + bias; out is bf16 or fp32.  Scales are NULL otherwise.  Its products
+ *   are added as exactly as those of the other types (bf16 matrix instruction), or, with coarse_sums != 0, by the 8-bit matrix
+ *   instruction: twice the rate, and sums that may miss 2^-12 of sum_k |in_ik W_kj| (1.5e-5 of the result over 1,024 random
+ *   products, a hundredth of a bf16 output's rounding).
+ *   bias: device fp32 [d_out] or NULL; residual: out_dt [n_rows, ld_res] or NULL, may be out; pre (NULL: not stored) receives
+ *   the pre-activation in out_dt, which heta_linear_bwd reads.
+ * g: handle whose workspace the call may use (and grow). */
+typedef struct heta_linear_args {
+    int64_t n_rows;
+    int32_t d_in, d_out;
+    const void *in;
+    int64_t ld_in;
+    const float *in_scale;
+    const void *W;
+    int64_t ld_w;
+    const float *w_scale;
+    const float *bias;
+    const void *residual;
+    int64_t ld_res;
+    void *pre;
+    int64_t ld_pre;
+    void *out;
+    int64_t ld_out;
+    heta_dtype in_dt, w_dt, out_dt;
+    heta_act act;
+    int32_t coarse_sums;
+} heta_linear_args;
+heta_status heta_linear(heta_graph *g, const heta_linear_args *args, void *hip_stream);
+/* Its backward; in, W, the rows' gradients and pre are of one type dt (fp32 or bf16):
+ *   grad_pre = grad_out * act'(pre)     (act = NONE: grad_pre is grad_out itself, and pre and grad_pre are not used)
+ *   dbias[j] = sum_i grad_pre[i, j]     (fp32, from the unrounded products; NULL: not computed)
+ *   grad_in  = (grad_pre . W^T) * in_act'(in_pre)   (NULL: not computed; in_act = NONE: no factor.  With the activation that made
+ *              `in`, grad_in is the gradient at its pre-activation in_pre [n_rows, d_in], what the product before takes as grad_out)
+ *   dW       = in^T . grad_pre          (dw_dt: fp32, or bf16 for bf16 operands; NULL: not computed), rows added in a fixed order
+ * The gradient of the residual is grad_out.  grad_pre may be grad_out or pre, grad_in may be in_pre; all outputs are
+ * overwritten.  Uses the handle's workspace (may grow it). */
+typedef struct heta_linear_bwd_args {
+    int64_t n_rows;
+    int32_t d_in, d_out;
+    heta_dtype dt, dw_dt;
+    heta_act act, in_act;
+    const void *in;
+    int64_t ld_in;
+    const void *W;
+    int64_t ld_w;
+    const void *grad_out;
+    int64_t ld_go;
+    const void *pre;
+    int64_t ld_pre;
+    void *grad_pre;
+    int64_t ld_gp;
+    void *grad_in;
+    int64_t ld_gi;
+    const void *in_pre;
+    int64_t ld_ip;
+    void *dW;
+    int64_t ld_dw;
+    float *dbias;
+} heta_linear_bwd_args;
+heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args *args, void *hip_stream);
+/* Weights W [d_in, d_out] (fp32 or bf16) as 8-bit rows: packed [d_out, ld_packed >= d_in] of HETA_E4M3, scale [d_out] =
+ * max_k |W[k, j]| / 448.  Once per set of weights. */
+heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int64_t ld_w, int32_t d_in, int32_t d_out, void *packed, int64_t ld_packed,
+                                  float *scale, void *hip_stream);
+
+/* heta_muon_multi: orthogonalised momentum (Muon, Jordan et al. 2024) on n_items weight matrices [rows, cols] of products in . W:
+ *   m <- momentum m + grad;   u = nesterov ? grad + momentum m : m;   X = u / (|u|_F + eps);
+ *   `steps` times  X <- 3.4445 X + (-4.7750 A + 2.0315 A A) X  with  A = X X^T  (of the shorter side);
+ *   W <- (1 - lr weight_decay) W - lr sqrt(max(1, cols / rows)) X.
+ * W: fp32 (products to 2^-24) or bf16 (X kept to 16 bits, W updated in fp32 and rounded back); m: fp32; grad: fp32 or bf16.  All
+ * arrays are device memory, items a HOST array; no array of an item may overlap what another item writes.  A zero gradient
+ * and momentum leave X = 0.  Uses the handle's workspace (may grow it: about 8 rows * cols * 2 bytes an item).  n_items = 0
+ * is a no-op. */
+typedef struct heta_muon_item {
+    void *W;
+    int64_t ld_w;
+    float *m;
+    int64_t ld_m;
+    const void *grad;
+    int64_t ld_grad;
+    int32_t rows, cols;
+    heta_dtype dt, grad_dt;
+} heta_muon_item;
+heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t nesterov,
+                            float weight_decay, float eps, int32_t steps, void *hip_stream);
 
 /* ---- meta-partitioning (Section 5, Algorithm 2): which relations a GPU (or machine) holds ---------
  * Host-only: works on the weighted metagraph, touches no device.  All pointers are HOST arrays.

@@ -19,9 +19,9 @@ LIB_PATH = os.path.join(_PKG, "lib", "libheta.so")
 HETA_OK = 0
 HETA_ERR_INVALID_ARG, HETA_ERR_BAD_CSR, HETA_ERR_SHAPE = 1, 2, 3
 HETA_ERR_UNSUPPORTED, HETA_ERR_OOM, HETA_ERR_DEVICE = 4, 5, 6
-HETA_F32, HETA_BF16 = 0, 1
+HETA_F32, HETA_BF16, HETA_E4M3 = 0, 1, 2
 HETA_SUM, HETA_MEAN = 0, 1
-HETA_ACT_NONE, HETA_ACT_RELU = 0, 1
+HETA_ACT_NONE, HETA_ACT_RELU, HETA_ACT_GELU, HETA_ACT_SILU = 0, 1, 2, 3
 HETA_PTRS_ON_DEVICE = 1
 
 EXPORTS = ["heta_graph_create", "heta_graph_create_batch", "heta_graph_destroy", "heta_scratch_release", "heta_graph_get_csc", "heta_graph_get_degrees",
@@ -38,7 +38,7 @@ EXPORTS = ["heta_graph_create", "heta_graph_create_batch", "heta_graph_destroy",
            "heta_sample_neighbors", "heta_unique_relabel",
            "heta_cross_rel_aggregate_project", "heta_meta_partition", "heta_sample_neighbors_batch",
            "heta_unique_relabel_batch", "heta_sample_hop", "heta_rel_aggregate_fwd_noalloc", "heta_attn_fold", "heta_attn_fold_bwd",
-           "heta_graph_index_bytes"]
+           "heta_graph_index_bytes", "heta_rms_norm", "heta_rms_norm_bwd", "heta_linear", "heta_linear_bwd", "heta_linear_pack_e4m3", "heta_muon_multi"]
 # process-wide switches for tests and measurements, declared in csrc/heta_test_hooks.h (not in the public header)
 TEST_HOOKS = ["heta_projection_force_staged", "heta_ingest_force", "heta_projection_f32_native"]
 HETA_NOALLOC_SCRATCH_BYTES = 32 << 20
@@ -65,6 +65,24 @@ class _AdamItem(ctypes.Structure):
     _fields_ = [("table", ctypes.c_void_p), ("dt", ctypes.c_int32), ("ld_table", ctypes.c_int64), ("d", ctypes.c_int32),
                 ("n_table_rows", ctypes.c_int64), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("ld_state", ctypes.c_int64),
                 ("ids", ctypes.c_void_p), ("n", ctypes.c_int64), ("grad", ctypes.c_void_p), ("ld_grad", ctypes.c_int64)]
+
+
+class _LinearArgs(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int64), ("d_in", ctypes.c_int32), ("d_out", ctypes.c_int32), ("inp", ctypes.c_void_p), ("ld_in", ctypes.c_int64),
+                ("in_scale", ctypes.c_void_p), ("W", ctypes.c_void_p), ("ld_w", ctypes.c_int64), ("w_scale", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p), ("ld_res", ctypes.c_int64), ("pre", ctypes.c_void_p), ("ld_pre", ctypes.c_int64), ("out", ctypes.c_void_p),
+                ("ld_out", ctypes.c_int64), ("in_dt", ctypes.c_int32), ("w_dt", ctypes.c_int32), ("out_dt", ctypes.c_int32), ("act", ctypes.c_int32), ("coarse_sums", ctypes.c_int32)]
+
+
+class _LinearBwdArgs(ctypes.Structure):
+    _fields_ = ([("n_rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("d_in", "d_out", "dt", "dw_dt", "act", "in_act")] +
+                [f for n in ("inp", "W", "grad_out", "pre", "grad_pre", "grad_in", "in_pre", "dW") for f in ((n, ctypes.c_void_p), ("ld_" + n, ctypes.c_int64))] +
+                [("dbias", ctypes.c_void_p)])
+
+
+class _MuonItem(ctypes.Structure):
+    _fields_ = [("W", ctypes.c_void_p), ("ld_w", ctypes.c_int64), ("m", ctypes.c_void_p), ("ld_m", ctypes.c_int64), ("grad", ctypes.c_void_p),
+                ("ld_grad", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("dt", ctypes.c_int32), ("grad_dt", ctypes.c_int32)]
 
 
 class _AggItem(ctypes.Structure):
@@ -127,6 +145,12 @@ def load_library() -> ctypes.CDLL:
     L.heta_sparse_adam_multi.argtypes = [i32, vp, f32, f32, f32, f32, i64, vp]
     L.heta_sample_hop.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.heta_graph_create_batch.argtypes = [i32, vp, vp, vp, vp, u32, vp]
+    L.heta_rms_norm.argtypes = [i64, i32, vp, i32, i64, vp, i64, vp, f32, vp, i64, vp, i32, i64, vp, vp, vp]
+    L.heta_rms_norm_bwd.argtypes = [vp, i64, i32, vp, i32, i64, vp, vp, vp, i32, i64, vp, i64, vp, i64, vp, vp]
+    L.heta_linear.argtypes = [vp, vp, vp]
+    L.heta_linear_bwd.argtypes = [vp, vp, vp]
+    L.heta_linear_pack_e4m3.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp]
+    L.heta_muon_multi.argtypes = [vp, i32, vp, f32, f32, i32, f32, f32, i32, vp]
     for name in EXPORTS + TEST_HOOKS:
         getattr(L, name).restype = ctypes.c_int
     L.heta_last_error.restype = ctypes.c_char_p
@@ -258,6 +282,10 @@ assert _NT_PACK.size == ctypes.sizeof(_NType) and _REL_PACK.size == ctypes.sizeo
 
 _AGG_PACK = struct.Struct("=iiQqqQQqf4x")    # heta_agg_item
 _ADAM_PACK = struct.Struct("=Qi4xqi4xqQQqQqQq")  # heta_adam_item
+_LINEAR_PACK = struct.Struct("=qiiQqQQqQQQqQqQqiiiii4x")       # heta_linear_args
+_LINEAR_BWD_PACK = struct.Struct("=qiiiiii" + "Qq" * 8 + "Q")  # heta_linear_bwd_args
+_MUON_PACK = struct.Struct("=QqQqQqiiii")                      # heta_muon_item
+assert _LINEAR_PACK.size == ctypes.sizeof(_LinearArgs) and _LINEAR_BWD_PACK.size == ctypes.sizeof(_LinearBwdArgs) and _MUON_PACK.size == ctypes.sizeof(_MuonItem)
 assert _AGG_PACK.size == ctypes.sizeof(_AggItem) and _ADAM_PACK.size == ctypes.sizeof(_AdamItem)
 
 
@@ -882,6 +910,135 @@ def heta_sparse_adam_multi(items: Sequence[Sequence], lr: float = 1e-3, beta1: f
             raise HetaError(HETA_ERR_SHAPE, "optimizer states have fewer rows than the table")
         arr.append(_ADAM_PACK.pack(pt, _dt(table), lt, d, rt, pm, pv, lm, _dev(ids, "ids", torch.int64) or 0, rows, pg, lg))
     _check(load_library().heta_sparse_adam_multi(n, b"".join(arr), lr, beta1, beta2, eps, int(step), _stream(stream)))
+
+
+def _rows_of(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, rows: int, cols: int):
+    """(address, leading dimension) of a device matrix of exactly rows x cols elements; (0, cols) for None."""
+    if t is None:
+        return 0, cols
+    p, ld, r, c = _mat(t, name, dtype)
+    if r != rows or c != cols:
+        raise HetaError(HETA_ERR_SHAPE, f"{name} must be [{rows}, {cols}], got [{r}, {c}]")
+    return p, (ld if r > 1 else max(ld, c))
+
+
+def _floats_of(t: Optional[torch.Tensor], name: str, n: int) -> int:
+    """Address of a contiguous fp32 device vector of n elements; 0 for None."""
+    if t is None:
+        return 0
+    p, got = _vec(t, name, torch.float32)
+    if got != n:
+        raise HetaError(HETA_ERR_SHAPE, f"{name} must have {n} elements, got {got}")
+    return p
+
+
+_DT8 = {torch.float32: HETA_F32, torch.bfloat16: HETA_BF16, torch.float8_e4m3fn: HETA_E4M3}
+
+
+def _dt8(t: torch.Tensor) -> int:
+    dt = _DT8.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"unsupported tensor dtype {t.dtype}")
+    return dt
+
+
+def heta_rms_norm(x: torch.Tensor, out: torch.Tensor, residual: Optional[torch.Tensor] = None, sum: Optional[torch.Tensor] = None,
+                  gamma: Optional[torch.Tensor] = None, eps: float = 1e-6, scale: Optional[torch.Tensor] = None,
+                  rstd: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """sum = x + residual; out = sum * rstd * gamma with rstd = 1 / sqrt(mean(sum^2) + eps), per row.  out: x's type, bf16, or
+    torch.float8_e4m3fn with `scale` (one per row)."""
+    t = x.dtype
+    n, d = x.shape
+    px, lx = _rows_of(x, "x", t, n, d)
+    pr, lr = _rows_of(residual, "residual", t, n, d)
+    ps, ls = _rows_of(sum, "sum", t, n, d)
+    po, lo = _rows_of(out, "out", out.dtype, n, d)
+    _check(load_library().heta_rms_norm(n, d, px, _dt8(x), lx, pr, lr, _floats_of(gamma, "gamma", d), eps, ps, ls, po, _dt8(out), lo,
+                                        _floats_of(scale, "scale", n), _floats_of(rstd, "rstd", n), _stream(stream)))
+    return out
+
+
+def heta_rms_norm_bwd(g: Graph, x: torch.Tensor, rstd: torch.Tensor, grad_out: torch.Tensor, grad_x: torch.Tensor,
+                      gamma: Optional[torch.Tensor] = None, grad_sum: Optional[torch.Tensor] = None,
+                      grad_gamma: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """grad_x (+ grad_sum, what reaches the sum past the norm) and grad_gamma of heta_rms_norm; x: the sum that was normalised."""
+    t = x.dtype
+    n, d = x.shape
+    px, lx = _rows_of(x, "x", t, n, d)
+    po, lo = _rows_of(grad_out, "grad_out", grad_out.dtype, n, d)
+    ps, ls = _rows_of(grad_sum, "grad_sum", t, n, d)
+    pg, lg = _rows_of(grad_x, "grad_x", t, n, d)
+    _check(load_library().heta_rms_norm_bwd(g.handle, n, d, px, _dt8(x), lx, _floats_of(gamma, "gamma", d), _floats_of(rstd, "rstd", n), po, _dt8(grad_out), lo,
+                                            ps, ls, pg, lg, _floats_of(grad_gamma, "grad_gamma", d), _stream(stream)))
+    return grad_x
+
+
+def heta_linear(g: Graph, inp: torch.Tensor, W: torch.Tensor, out: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = HETA_ACT_NONE,
+                residual: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, in_scale: Optional[torch.Tensor] = None,
+                w_scale: Optional[torch.Tensor] = None, coarse_sums: bool = False, stream=None) -> torch.Tensor:
+    """pre = inp @ W + bias; out = act(pre) + residual.  W is [d_in, d_out]; for 8-bit operands [d_out, d_in] with in_scale [n_rows]
+    and w_scale [d_out], and coarse_sums lets the 8-bit matrix instruction add their products."""
+    n, d_in = inp.shape
+    d_out = out.shape[1]
+    t = out.dtype
+    dt = _dt8(inp)
+    pi, li = _rows_of(inp, "in", inp.dtype, n, d_in)
+    pw, lw = _rows_of(W, "W", W.dtype, d_out, d_in) if dt == HETA_E4M3 else _rows_of(W, "W", W.dtype, d_in, d_out)
+    po, lo = _rows_of(out, "out", t, n, d_out)
+    pr, lr = _rows_of(residual, "residual", t, n, d_out)
+    pp, lp = _rows_of(pre, "pre", t, n, d_out)
+    args = _LINEAR_PACK.pack(n, d_in, d_out, pi, li, _floats_of(in_scale, "in_scale", n), pw, lw, _floats_of(w_scale, "w_scale", d_out),
+                             _floats_of(bias, "bias", d_out), pr, lr, pp, lp, po, lo, dt, _dt8(W), _dt8(out), act, int(coarse_sums))
+    _check(load_library().heta_linear(g.handle, args, _stream(stream)))
+    return out
+
+
+def heta_linear_bwd(g: Graph, inp: Optional[torch.Tensor], W: Optional[torch.Tensor], grad_out: torch.Tensor, act: int = HETA_ACT_NONE,
+                    pre: Optional[torch.Tensor] = None, grad_pre: Optional[torch.Tensor] = None, grad_in: Optional[torch.Tensor] = None,
+                    in_act: int = HETA_ACT_NONE, in_pre: Optional[torch.Tensor] = None, grad_W: Optional[torch.Tensor] = None,
+                    grad_bias: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Backward of heta_linear.  grad_pre (needed with an activation) = grad_out * act'(pre); then, each if given, grad_in =
+    (grad_pre @ W^T) * in_act'(in_pre), grad_W = inp^T @ grad_pre and grad_bias = grad_pre.sum(0).  inp may be None without grad_W,
+    W without grad_in."""
+    n, d_out = grad_out.shape
+    t = grad_out.dtype
+    d_in = next((x.shape[1] for x in (inp, grad_in) if x is not None), None)
+    if d_in is None:
+        d_in = W.shape[0] if W is not None else 1
+    pi, li = _rows_of(inp, "in", t, n, d_in)
+    pw, lw = _rows_of(W, "W", t, d_in, d_out)
+    pg, lg = _rows_of(grad_out, "grad_out", t, n, d_out)
+    pp, lp = _rows_of(pre, "pre", t, n, d_out)
+    pq, lq = _rows_of(grad_pre, "grad_pre", t, n, d_out)
+    px, lx = _rows_of(grad_in, "grad_in", t, n, d_in)
+    py, ly = _rows_of(in_pre, "in_pre", t, n, d_in)
+    pd, ld = (0, d_out) if grad_W is None else _rows_of(grad_W, "grad_W", grad_W.dtype, d_in, d_out)
+    args = _LINEAR_BWD_PACK.pack(n, d_in, d_out, _dt8(grad_out), HETA_F32 if grad_W is None else _dt8(grad_W), act, in_act, pi, li, pw, lw, pg, lg,
+                                 pp, lp, pq, lq, px, lx, py, ly, pd, ld, _floats_of(grad_bias, "grad_bias", d_out))
+    _check(load_library().heta_linear_bwd(g.handle, args, _stream(stream)))
+
+
+def heta_linear_pack_e4m3(W: torch.Tensor, packed: torch.Tensor, scale: torch.Tensor, stream=None) -> torch.Tensor:
+    """Weights [d_in, d_out] as 8-bit rows [d_out, d_in] (torch.float8_e4m3fn) with a scale each, for heta_linear."""
+    d_in, d_out = W.shape
+    pw, lw = _rows_of(W, "W", W.dtype, d_in, d_out)
+    pp, lp = _rows_of(packed, "packed", torch.float8_e4m3fn, d_out, d_in)
+    _check(load_library().heta_linear_pack_e4m3(pw, _dt8(W), lw, d_in, d_out, pp, lp, _floats_of(scale, "scale", d_out), _stream(stream)))
+    return packed
+
+
+def heta_muon_multi(g: Graph, items: Sequence[Sequence], lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
+                    weight_decay: float = 0.0, eps: float = 1e-7, steps: int = 5, stream=None) -> None:
+    """One step of orthogonalised momentum on several weight matrices: items[i] = (W, m, grad), all [rows, cols]; W fp32 or bf16,
+    m fp32, grad fp32 or bf16; W and m are updated in place."""
+    arr = []
+    for W, m, grad in items:
+        rows, cols = W.shape
+        pw, lw = _rows_of(W, "W", W.dtype, rows, cols)
+        pm, lm = _rows_of(m, "m", torch.float32, rows, cols)
+        pg, lg = _rows_of(grad, "grad", grad.dtype, rows, cols)
+        arr.append(_MUON_PACK.pack(pw, lw, pm, lm, pg, lg, rows, cols, _dt8(W), _dt8(grad)))
+    _check(load_library().heta_muon_multi(g.handle, len(arr), b"".join(arr), lr, momentum, int(bool(nesterov)), weight_decay, eps, int(steps), _stream(stream)))
 
 
 def _scores(t: torch.Tensor, name: str, rows: int, heads: int) -> int:

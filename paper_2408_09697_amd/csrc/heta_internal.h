@@ -33,6 +33,12 @@ heta_status fail(heta_status st, const char *fmt, ...) __attribute__((format(pri
             return ::heta::fail(HETA_ERR_DEVICE, "launch of %s failed: %s", name, hipGetErrorString(e_)); \
     } while (0)
 
+#define HETA_TRY(call)                                                                               \
+    do {                                                                                             \
+        const heta_status e_ = (call);                                                               \
+        if (e_ != HETA_OK) return e_;                                                                \
+    } while (0)
+
 // A grid dimension holds at most 2^32 - 1 threads; a longer grid is cut off without an error.
 constexpr int64_t max_blocks(int threads) { return ((int64_t(1) << 32) - 1) / threads; }
 // Calls launch(first workgroup, number of workgroups) for the pieces that `blocks` workgroups of `threads` threads are

@@ -1,0 +1,476 @@
+// Products with a fused epilogue (bias, activation, residual) over rows of node embeddings, and their backward pass: the two
+// matrices of a feed-forward block that follows a layer's relation aggregation.
+//
+//     pre = s_i w_j (in . W) + bias,  out = act(pre) + residual          s, w: scales of 8-bit rows / columns, else 1
+//     grad_pre = grad_out * act'(pre),  grad_bias = sum of its rows,  grad_in = (grad_pre . W^T) * act_in'(pre_in),
+//     grad_W = in^T . grad_pre
+//
+// All three products are the tile kernel of heta_tiles.h: bf16 operands straight into LDS; e4m3 operands too, widened to
+// bf16 behind LDS or, where the caller allows coarser sums, on the 8-bit matrix instruction at twice the rate (block scales 1;
+// the scales of rows and columns come in the epilogue); fp32 operands as three bf16 terms.  grad_W is split over the rows; the partial products are added in a fixed order.
+#include <algorithm>
+#include <cmath>
+
+#include "heta_rows.h"
+#include "heta_tiles.h"
+
+namespace heta {
+
+// ---- activations: x * sigmoid(z(x)); GELU in its tanh form, 0.5 (1 + tanh(u)) = sigmoid(2 u) --------------------
+constexpr float kGelu2 = 1.5957691216057308f; // 2 sqrt(2 / pi)
+constexpr float kGeluCubic = 0.044715f;
+
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+
+__device__ __forceinline__ float activate(float x, int act)
+{
+    if (act == HETA_ACT_RELU) return x > 0.f ? x : (x != x ? x : 0.f);
+    const float s = sigmoid(act == HETA_ACT_GELU ? kGelu2 * (x + kGeluCubic * x * x * x) : x);
+    return x < -200.f ? -0.f : x * s; // below, the product is zero in fp32, and -inf * 0 would be NaN
+}
+
+__device__ __forceinline__ float activation_slope(float x, int act)
+{
+    if (act == HETA_ACT_RELU) return x > 0.f ? 1.f : (x != x ? x : 0.f);
+    x = x > 60.f ? 60.f : (x < -60.f ? -60.f : x); // the slope is 1 or 0 there; NaN stays
+    if (act == HETA_ACT_GELU) {
+        const float s = sigmoid(kGelu2 * (x + kGeluCubic * x * x * x));
+        return s + x * s * (1.f - s) * kGelu2 * (1.f + 3.f * kGeluCubic * x * x);
+    }
+    const float s = sigmoid(x);
+    return s + x * s * (1.f - s);
+}
+
+// ---- epilogues ---------------------------------------------------------------------------------------
+struct LinearExtra {
+    const float *bias, *in_scale, *w_scale; // nullable
+    const void *residual, *slope_at;        // nullable; slope_at: the producer's pre-activation, whose slope multiplies
+    void *pre, *out;                        // pre nullable
+    int64_t ld_res, ld_slope, ld_pre, ld_out;
+    int act, slope_act;
+    int vec; // every array that is there can be moved 16 bytes at a time
+};
+template <typename O> struct LinearEpi {
+    static constexpr int kItems = 1;
+    using Extra = LinearExtra;
+    struct Cols {
+        float bias[8], scale[8];
+        __device__ __forceinline__ Cols(const Extra &x, int64_t n, int valid)
+        {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                bias[e] = x.bias && e < valid ? x.bias[n + e] : 0.f;
+                scale[e] = x.w_scale && e < valid ? x.w_scale[n + e] : 1.f;
+            }
+        }
+    };
+    __device__ __forceinline__ static void put(const Extra &x, const TileItem &, const Cols &c, int64_t m, int64_t n, int valid, const float (&v)[8], int)
+    {
+        float y[8], t[8];
+        if (x.in_scale) {
+            const float s = x.in_scale[m];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = v[e] * s * c.scale[e] + c.bias[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = v[e] + c.bias[e];
+        }
+        if (x.pre) store8(static_cast<O *>(x.pre) + m * x.ld_pre + n, valid, x.vec, y);
+        if (x.act != HETA_ACT_NONE) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = activate(y[e], x.act);
+        }
+        if (x.slope_at) {
+            load8(static_cast<const O *>(x.slope_at) + m * x.ld_slope + n, valid, x.vec, t);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= activation_slope(t[e], x.slope_act);
+        }
+        if (x.residual) {
+            load8(static_cast<const O *>(x.residual) + m * x.ld_res + n, valid, x.vec, t);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] += t[e];
+        }
+        store8(static_cast<O *>(x.out) + m * x.ld_out + n, valid, x.vec, y);
+    }
+};
+
+// partial products of a contraction that is split over its rows: [split][M][N] fp32
+struct PartialEpi {
+    static constexpr int kItems = 1;
+    struct Extra {
+        float *part;
+        int vec;
+    };
+    struct Cols {
+        __device__ __forceinline__ Cols(const Extra &, int64_t, int) {}
+    };
+    __device__ __forceinline__ static void put(const Extra &x, const TileItem &it, const Cols &, int64_t m, int64_t n, int valid, const float (&v)[8], int split)
+    {
+        store8(x.part + (split * it.M + m) * it.N + n, valid, x.vec, v);
+    }
+};
+
+// ---- sums of partials --------------------------------------------------------------------------------
+// 256 threads: 256 / CH column groups of four, CH chains over the partials each, joined through LDS in order.
+template <int CH, typename O> __global__ void __launch_bounds__(256) fold_partials_kernel(const float *part, int64_t n_part, int64_t total, O *out, int32_t width, int64_t ld)
+{
+    constexpr int G = 256 / CH;
+    __shared__ float sums[CH][G][4];
+    const int gq = threadIdx.x % G, ch = threadIdx.x / G;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x) * G + gq) * 4;
+    const int valid = static_cast<int>(min(total - c, static_cast<int64_t>(4)));
+    const bool vec = (total & 3) == 0;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (valid > 0) {
+        // chain ch takes a contiguous range of partials
+        const int64_t each = (n_part + CH - 1) / CH, lo = ch * each, hi = min(n_part, lo + each);
+#pragma unroll 8
+        for (int64_t i = lo; i < hi; ++i) {
+            const float *p = part + i * total + c;
+            if (vec) {
+                const float4 x = *reinterpret_cast<const float4 *>(p);
+                s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < valid) s[e] += p[e];
+            }
+        }
+    }
+    if constexpr (CH > 1) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[ch][gq][e] = s[e];
+        __syncthreads();
+        if (ch != 0) return;
+#pragma unroll
+        for (int i = 1; i < CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += sums[i][gq][e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < valid) {
+            const int64_t row = (c + e) / width, col = (c + e) - row * width;
+            if constexpr (sizeof(O) == 2) out[row * ld + col] = to_bf16(s[e]);
+            else out[row * ld + col] = s[e];
+        }
+}
+
+template <typename O> static void fold_launch(const float *part, int64_t n_part, int64_t total, O *out, int32_t width, int64_t ld, hipStream_t st)
+{
+    const int64_t groups = (total + 3) / 4;
+    // few columns: the chains are what keeps loads in flight
+    if (groups < 16384 && n_part >= 16)
+        hipLaunchKernelGGL((fold_partials_kernel<32, O>), dim3((unsigned)((groups + 7) / 8)), dim3(256), 0, st, part, n_part, total, out, width, ld);
+    else
+        hipLaunchKernelGGL((fold_partials_kernel<4, O>), dim3((unsigned)((groups + 63) / 64)), dim3(256), 0, st, part, n_part, total, out, width, ld);
+}
+
+heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void *out, heta_dtype out_dt, int32_t width, int64_t ld, hipStream_t st)
+{
+    if ((total + 3) / 4 / 8 >= max_blocks(256)) return fail(HETA_ERR_UNSUPPORTED, "sum of partials: too many columns for one launch");
+    ProfScope prof("fold_partials_kernel", st, static_cast<double>(total) * (4.0 * n_part + dtype_size(out_dt)), static_cast<double>(total) * n_part);
+    if (out_dt == HETA_F32) fold_launch(part, n_part, total, static_cast<float *>(out), width, ld, st);
+    else fold_launch(part, n_part, total, static_cast<bf16_t *>(out), width, ld, st);
+    HETA_LAUNCH_CHECK("fold_partials_kernel");
+    return HETA_OK;
+}
+
+// ---- gradient through the activation, and the bias's ---------------------------------------------------
+// A workgroup takes a slab of rows of 256 columns: 32 lanes of eight columns, 8 rows at a time; every lane keeps the sums of
+// its columns, which are joined through LDS into the slab's row of the partials.
+template <typename E> __global__ void __launch_bounds__(256) act_grad_kernel(const E *go, int64_t ld_go, const E *pre, int64_t ld_pre, E *gp, int64_t ld_gp, int act,
+                                                                            int64_t n_rows, int32_t d, int64_t rows_each, float *part, int vec, uint32_t first)
+{
+    __shared__ float sums[8][256 + 8];
+    const int lx = threadIdx.x & 31, ly = threadIdx.x >> 5;
+    const uint32_t strips = (d + 255) / 256, b = first + blockIdx.x;
+    const int64_t slab = b / strips;
+    const int c = static_cast<int>(b % strips) * 256 + lx * 8, valid = min(d - c, 8);
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (valid > 0) {
+        const int64_t end = min(n_rows, (slab + 1) * rows_each);
+#pragma unroll 4
+        for (int64_t r = slab * rows_each + ly; r < end; r += 8) {
+            float g[8];
+            load8(go + r * ld_go + c, valid, vec, g);
+            if (gp) {
+                float x[8];
+                load8(pre + r * ld_pre + c, valid, vec, x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] *= activation_slope(x[e], act);
+                store8(gp + r * ld_gp + c, valid, vec, g);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] += g[e];
+        }
+    }
+    if (!part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[ly][lx * 8 + e] = s[e];
+    __syncthreads();
+    const int col = static_cast<int>(b % strips) * 256 + threadIdx.x;
+    if (col >= d) return;
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t += sums[i][threadIdx.x];
+    part[slab * d + col] = t;
+}
+
+// ---- weights in 8 bits -------------------------------------------------------------------------------
+// Column j of W [d_in, d_out] becomes row j of the packed matrix [d_out, d_in], e4m3 with the scale max|W[:, j]| / 448.  Once per
+// set of weights: one wavefront per column.
+template <typename E> __global__ void __launch_bounds__(256) pack_e4m3_kernel(const E *W, int64_t ld_w, int32_t d_in, int32_t d_out, uint8_t *out, int64_t ld_out, float *scale)
+{
+    const int64_t j = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (j >= d_out) return;
+    float amax = 0.f;
+    for (int k = lane; k < d_in; k += 64) {
+        const float x = fabsf(widen(W[k * ld_w + j]));
+        amax = x > amax || x != x ? x : amax;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const float x = __shfl_xor(amax, o);
+        amax = x > amax || x != x ? x : amax;
+    }
+    const float inv = amax > 0.f ? fminf(448.f / amax, 3.402823466e38f) : (amax != amax ? amax : 0.f);
+    for (int k = lane; k < d_in; k += 64) {
+        const float x = widen(W[k * ld_w + j]) * inv;
+        out[j * ld_out + k] = static_cast<uint8_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
+    }
+    if (lane == 0) scale[j] = amax / 448.f;
+}
+
+// ---- host side ---------------------------------------------------------------------------------------
+// shapes: BM x BN, k-values per stage, stages
+template <typename S, bool A_RC, bool B_RC> using Bf16Large = TileShape<S, 2, 1, A_RC, B_RC, kDirect, 2, 4, 4, 2, 64, 2, 1>;
+template <typename S, bool A_RC, bool B_RC> using Bf16Small = TileShape<S, 2, 1, A_RC, B_RC, kDirect, 2, 2, 1, 1, 64, 3, 2>;
+template <bool A_RC, bool B_RC> using Bf16Elements = TileShape<bf16_t, 2, 1, A_RC, B_RC, kElements, 2, 2, 2, 2, 32, 2, 1>;
+template <bool A_RC, bool B_RC> using F32Large = TileShape<float, 2, 3, A_RC, B_RC, kStaged, 4, 2, 2, 2, 32, 2, 1>;
+template <bool A_RC, bool B_RC> using F32Small = TileShape<float, 2, 3, A_RC, B_RC, kStaged, 2, 2, 1, 1, 32, 2, 2>;
+template <bool A_RC, bool B_RC> using F32Elements = TileShape<float, 2, 3, A_RC, B_RC, kElements, 2, 2, 1, 1, 32, 2, 2>;
+template <bool WIDEN> using E4m3Large = TileShape<uint8_t, 1, 1, false, false, kDirect, 2, 4, 4, 2, 128, 2, 1, WIDEN>;
+template <bool WIDEN> using E4m3Small = TileShape<uint8_t, 1, 1, false, false, kDirect, 2, 2, 1, 1, 128, 3, 2, WIDEN>;
+template <bool WIDEN> using E4m3Elements = TileShape<uint8_t, 1, 1, false, false, kElements, 2, 2, 2, 2, 64, 2, 1, WIDEN>;
+
+// rows that can go straight into LDS: 16-byte aligned, and a tile's rows within 32-bit offsets
+static bool direct_rows(const void *p, int64_t ld, size_t elt) { return aligned16(p) && (ld * static_cast<int64_t>(elt)) % 16 == 0 && ld * static_cast<int64_t>(elt) < (int64_t(1) << 23); }
+
+static int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return (M + bm - 1) / bm * ((N + bn - 1) / bn); }
+
+template <bool A_RC, bool B_RC, typename Epi>
+static heta_status launch_product(const char *who, const char *name, heta_dtype dt, TileArgs<Epi> &p, double bytes, double flops, hipStream_t st, bool coarse = false)
+{
+    TileItem &it = p.item[0];
+    const size_t esz = dt == HETA_F32 ? 4 : dt == HETA_BF16 ? 2 : 1;
+    const bool direct = direct_rows(it.A, it.lda, esz) && direct_rows(it.B, it.ldb, esz);
+    const bool large = tiles_of(it.M, it.N, 256, 256) * it.n_split >= 128;
+    if (dt == HETA_F32) {
+        if (!direct) return launch_tiles<F32Elements<A_RC, B_RC>>(who, name, p, bytes, flops, st);
+        if (large) return launch_tiles<F32Large<A_RC, B_RC>>(who, name, p, bytes, flops, st);
+        return launch_tiles<F32Small<A_RC, B_RC>>(who, name, p, bytes, flops, st);
+    }
+    if (dt == HETA_BF16) {
+        if (!direct) return launch_tiles<Bf16Elements<A_RC, B_RC>>(who, name, p, bytes, flops, st);
+        if (large) return launch_tiles<Bf16Large<bf16_t, A_RC, B_RC>>(who, name, p, bytes, flops, st);
+        return launch_tiles<Bf16Small<bf16_t, A_RC, B_RC>>(who, name, p, bytes, flops, st);
+    }
+    if constexpr (!A_RC && !B_RC) {
+        auto go = [&](auto widen) {
+            constexpr bool W = decltype(widen)::value;
+            if (!direct) return launch_tiles<E4m3Elements<W>>(who, name, p, bytes, flops, st);
+            if (large) return launch_tiles<E4m3Large<W>>(who, name, p, bytes, flops, st);
+            return launch_tiles<E4m3Small<W>>(who, name, p, bytes, flops, st);
+        };
+        return coarse ? go(std::false_type{}) : go(std::true_type{});
+    }
+    return fail(HETA_ERR_UNSUPPORTED, "%s: no such product of 8-bit operands", who);
+}
+
+static bool valid_act(int a) { return a >= HETA_ACT_NONE && a <= HETA_ACT_SILU; }
+
+static heta_status check_matrix(const char *who, const char *what, const void *p, int64_t rows, int64_t ld, int64_t d, size_t elt)
+{
+    if (!p && rows > 0) return fail(HETA_ERR_INVALID_ARG, "%s: null %s", who, what);
+    if (ld < d) return fail(HETA_ERR_SHAPE, "%s: leading dimension of %s is below its width", who, what);
+    if (reinterpret_cast<uintptr_t>(p) % elt) return fail(HETA_ERR_INVALID_ARG, "%s: %s is not aligned to its element size", who, what);
+    return HETA_OK;
+}
+} // namespace heta
+
+using namespace heta;
+
+extern "C" heta_status heta_linear(heta_graph *, const heta_linear_args *a, void *hip_stream)
+{
+    const char *who = "heta_linear";
+    if (!a) return fail(HETA_ERR_INVALID_ARG, "%s: null arguments", who);
+    if (a->n_rows < 0 || a->d_in <= 0 || a->d_out <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and widths > 0", who);
+    if (!valid_act(a->act)) return fail(HETA_ERR_INVALID_ARG, "%s: bad act", who);
+    const bool q = a->in_dt == HETA_E4M3;
+    if (!q && !valid_dtype(a->in_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (!valid_dtype(a->out_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: outputs are fp32 or bf16", who);
+    if (a->w_dt != a->in_dt || (a->in_dt == HETA_F32 && a->out_dt != HETA_F32))
+        return fail(HETA_ERR_UNSUPPORTED, "%s: in and W have one type, and fp32 operands an fp32 output", who);
+    if (q != (a->in_scale != nullptr) || q != (a->w_scale != nullptr))
+        return fail(HETA_ERR_INVALID_ARG, "%s: scales belong to 8-bit operands, and those need them", who);
+    if (!q && a->coarse_sums) return fail(HETA_ERR_INVALID_ARG, "%s: coarse sums are those of 8-bit operands", who);
+    const size_t esz = q ? 1 : dtype_size(a->in_dt), osz = dtype_size(a->out_dt);
+    HETA_TRY(check_matrix(who, "in", a->in, a->n_rows, a->ld_in, a->d_in, esz));
+    HETA_TRY(check_matrix(who, "W", a->W, 1, a->ld_w, q ? a->d_in : a->d_out, esz));
+    HETA_TRY(check_matrix(who, "out", a->out, a->n_rows, a->ld_out, a->d_out, osz));
+    if (a->residual) HETA_TRY(check_matrix(who, "residual", a->residual, a->n_rows, a->ld_res, a->d_out, osz));
+    if (a->pre) HETA_TRY(check_matrix(who, "pre", a->pre, a->n_rows, a->ld_pre, a->d_out, osz));
+    for (const float *v : {a->bias, a->in_scale, a->w_scale})
+        if (reinterpret_cast<uintptr_t>(v) & 3u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
+    const RowRange out(a->out, a->n_rows, a->ld_out, a->d_out, osz), pre(a->pre, a->n_rows, a->ld_pre, a->d_out, osz);
+    const RowRange in(a->in, a->n_rows, a->ld_in, a->d_in, esz), w(a->W, q ? a->d_out : a->d_in, a->ld_w, q ? a->d_in : a->d_out, esz);
+    const RowRange res(a->residual, a->n_rows, a->ld_res, a->d_out, osz);
+    const bool same_rows = a->residual == a->out && a->ld_res == a->ld_out; // read and written by the same lane
+    if (out.overlaps(in) || out.overlaps(w) || out.overlaps(pre) || pre.overlaps(in) || pre.overlaps(w) || pre.overlaps(res) || (out.overlaps(res) && !same_rows))
+        return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);
+    if (a->n_rows == 0) return HETA_OK;
+    const LinearExtra x{a->bias, a->in_scale, a->w_scale, a->residual, nullptr, a->pre, a->out, a->ld_res, 0, a->ld_pre, a->ld_out, a->act, HETA_ACT_NONE,
+                        vec_rows(a->out, a->ld_out, osz) && vec_rows(a->residual, a->ld_res, osz) && vec_rows(a->pre, a->ld_pre, osz)};
+    const TileItem it{a->in, a->W, a->ld_in, a->ld_w, 0, 0, a->n_rows, a->d_out, a->d_in, a->d_in, 1, 0, 0, 0};
+    const double bytes = static_cast<double>(a->n_rows) * (a->d_in * esz + a->d_out * osz * (1.0 + !!a->residual + !!a->pre)) + static_cast<double>(a->d_in) * a->d_out * esz;
+    const double flops = 2.0 * a->n_rows * a->d_in * a->d_out;
+    hipStream_t st = as_stream(hip_stream);
+    auto go = [&](auto tag) {
+        using O = decltype(tag);
+        TileArgs<LinearEpi<O>> p{1, {it}, {x}};
+        return q ? launch_product<false, false>(who, "linear_kernel", a->in_dt, p, bytes, flops, st, a->coarse_sums != 0)
+                 : launch_product<false, true>(who, "linear_kernel", a->in_dt, p, bytes, flops, st);
+    };
+    return a->out_dt == HETA_F32 ? go(float{}) : go(bf16_t{});
+}
+
+extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args *a, void *hip_stream)
+{
+    const char *who = "heta_linear_bwd";
+    if (!g || !a) return fail(HETA_ERR_INVALID_ARG, "%s: null arguments", who);
+    if (a->n_rows < 0 || a->d_in <= 0 || a->d_out <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and widths > 0", who);
+    if (!valid_act(a->act) || !valid_act(a->in_act)) return fail(HETA_ERR_INVALID_ARG, "%s: bad act", who);
+    if (!valid_dtype(a->dt) || (a->dW && !valid_dtype(a->dw_dt))) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (a->dt == HETA_F32 && a->dW && a->dw_dt != HETA_F32) return fail(HETA_ERR_UNSUPPORTED, "%s: fp32 operands have an fp32 weight gradient", who);
+    const bool acts = a->act != HETA_ACT_NONE, fused = a->in_act != HETA_ACT_NONE;
+    const size_t esz = dtype_size(a->dt);
+    const int64_t n = a->n_rows;
+    HETA_TRY(check_matrix(who, "grad_out", a->grad_out, n, a->ld_go, a->d_out, esz));
+    if (acts) {
+        HETA_TRY(check_matrix(who, "pre", a->pre, n, a->ld_pre, a->d_out, esz));
+        HETA_TRY(check_matrix(who, "grad_pre", a->grad_pre, n, a->ld_gp, a->d_out, esz));
+    }
+    if (a->grad_in) {
+        HETA_TRY(check_matrix(who, "grad_in", a->grad_in, n, a->ld_gi, a->d_in, esz));
+        HETA_TRY(check_matrix(who, "W", a->W, 1, a->ld_w, a->d_out, esz));
+        if (fused) HETA_TRY(check_matrix(who, "in_pre", a->in_pre, n, a->ld_ip, a->d_in, esz));
+    }
+    if (a->dW) {
+        HETA_TRY(check_matrix(who, "in", a->in, n, a->ld_in, a->d_in, esz));
+        HETA_TRY(check_matrix(who, "dW", a->dW, 1, a->ld_dw, a->d_out, dtype_size(a->dw_dt)));
+    }
+    if (reinterpret_cast<uintptr_t>(a->dbias) & 3u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
+    const RowRange go(a->grad_out, n, a->ld_go, a->d_out, esz), pre(acts ? a->pre : nullptr, n, a->ld_pre, a->d_out, esz);
+    const RowRange gp(acts ? a->grad_pre : nullptr, n, a->ld_gp, a->d_out, esz), gi(a->grad_in, n, a->ld_gi, a->d_in, esz);
+    const RowRange w(a->grad_in ? a->W : nullptr, a->d_in, a->ld_w, a->d_out, esz), in(a->dW ? a->in : nullptr, n, a->ld_in, a->d_in, esz);
+    const RowRange ip(a->grad_in && fused ? a->in_pre : nullptr, n, a->ld_ip, a->d_in, esz);
+    const RowRange dw(a->dW, a->d_in, a->ld_dw, a->d_out, a->dW ? dtype_size(a->dw_dt) : 4), db(a->dbias, 1, a->d_out, a->d_out, 4);
+    const bool over_go = a->grad_pre == a->grad_out && a->ld_gp == a->ld_go, over_pre = a->grad_pre == a->pre && a->ld_gp == a->ld_pre;
+    const bool over_ip = a->grad_in == a->in_pre && a->ld_gi == a->ld_ip; // each read and written by the same lane
+    const RowRange outs[4] = {gp, gi, dw, db}, ins[5] = {go, pre, w, in, ip};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (outs[i].overlaps(outs[j])) return fail(HETA_ERR_INVALID_ARG, "%s: two outputs overlap", who);
+        for (int j = 0; j < 5; ++j)
+            if (outs[i].overlaps(ins[j]) && !(i == 0 && ((j == 0 && over_go) || (j == 1 && over_pre))) && !(i == 1 && j == 4 && over_ip))
+                return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand", who);
+    }
+    hipStream_t st = as_stream(hip_stream);
+
+    // workspace: partial sums of the bias gradient and partial products of the weight gradient
+    const int64_t strips = (a->d_out + 255) / 256;
+    const int64_t slabs = std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, 2048 / strips));
+    const int64_t rows_each = std::max<int64_t>(1, (n + slabs - 1) / slabs);
+    const int64_t bias_elems = a->dbias ? slabs * a->d_out : 0;
+    const int64_t bias_off = (bias_elems + 3) / 4 * 4;
+    const int64_t w_tiles = tiles_of(a->d_in, a->d_out, 256, 256);
+    int64_t n_split = 0, k_per_split = 0;
+    if (a->dW && n > 0) {
+        const int64_t most = std::max<int64_t>(1, 256 / w_tiles); // one workgroup per CU
+        k_per_split = (std::max<int64_t>((n + most - 1) / most, 256) + 63) / 64 * 64;
+        n_split = (n + k_per_split - 1) / k_per_split;
+    }
+    const int64_t w_elems = n_split * a->d_in * a->d_out;
+    if (bias_off + w_elems > 0) HETA_TRY(ensure_workspace(g, static_cast<size_t>(bias_off + w_elems) * sizeof(float)));
+    float *ws = static_cast<float *>(g->d_ws);
+
+    // gradient at the pre-activation
+    const void *gpre = acts ? a->grad_pre : a->grad_out;
+    const int64_t ld_gpre = acts ? a->ld_gp : a->ld_go;
+    if (n > 0 && (acts || a->dbias)) {
+        const int vec = vec_rows(a->grad_out, a->ld_go, esz) && (!acts || (vec_rows(a->pre, a->ld_pre, esz) && vec_rows(a->grad_pre, a->ld_gp, esz)));
+        ProfScope prof("act_grad_kernel", st, static_cast<double>(n) * a->d_out * esz * (acts ? 3 : 1), static_cast<double>(n) * a->d_out);
+        launch_pieces(slabs * strips, 256, [&](unsigned first, unsigned count) {
+            if (a->dt == HETA_F32)
+                hipLaunchKernelGGL(act_grad_kernel<float>, dim3(count), dim3(256), 0, st, static_cast<const float *>(a->grad_out), a->ld_go,
+                                   static_cast<const float *>(a->pre), a->ld_pre, acts ? static_cast<float *>(a->grad_pre) : nullptr, a->ld_gp, a->act, n,
+                                   a->d_out, rows_each, a->dbias ? ws : nullptr, vec, first);
+            else
+                hipLaunchKernelGGL(act_grad_kernel<bf16_t>, dim3(count), dim3(256), 0, st, static_cast<const bf16_t *>(a->grad_out), a->ld_go,
+                                   static_cast<const bf16_t *>(a->pre), a->ld_pre, acts ? static_cast<bf16_t *>(a->grad_pre) : nullptr, a->ld_gp, a->act, n,
+                                   a->d_out, rows_each, a->dbias ? ws : nullptr, vec, first);
+        });
+        HETA_LAUNCH_CHECK("act_grad_kernel");
+    }
+    if (a->dbias) HETA_TRY(fold_partials(ws, n > 0 ? slabs : 0, a->d_out, a->dbias, HETA_F32, a->d_out, a->d_out, st));
+
+    const double flops = 2.0 * n * a->d_in * a->d_out;
+    if (a->grad_in && n > 0) {
+        const LinearExtra x{nullptr, nullptr, nullptr, nullptr, fused ? a->in_pre : nullptr, nullptr, a->grad_in, 0, a->ld_ip, 0, a->ld_gi, HETA_ACT_NONE, a->in_act,
+                            vec_rows(a->grad_in, a->ld_gi, esz) && (!fused || vec_rows(a->in_pre, a->ld_ip, esz))};
+        const TileItem it{gpre, a->W, ld_gpre, a->ld_w, 0, 0, n, a->d_in, a->d_out, a->d_out, 1, 0, 0, 0};
+        const double bytes = (static_cast<double>(n) * (a->d_in * (fused ? 2 : 1) + a->d_out) + static_cast<double>(a->d_in) * a->d_out) * esz;
+        if (a->dt == HETA_F32) {
+            TileArgs<LinearEpi<float>> p{1, {it}, {x}};
+            HETA_TRY((launch_product<false, false>(who, "linear_grad_in_kernel", a->dt, p, bytes, flops, st)));
+        } else {
+            TileArgs<LinearEpi<bf16_t>> p{1, {it}, {x}};
+            HETA_TRY((launch_product<false, false>(who, "linear_grad_in_kernel", a->dt, p, bytes, flops, st)));
+        }
+    }
+    if (a->dW) {
+        float *part = ws + bias_off;
+        if (n > 0) {
+            TileArgs<PartialEpi> p{1, {TileItem{a->in, gpre, a->ld_in, ld_gpre, 0, 0, a->d_in, a->d_out, n, k_per_split, static_cast<int32_t>(n_split), 0, 0, 0}},
+                                   {PartialEpi::Extra{part, a->d_out % 4 == 0}}};
+            const double bytes = static_cast<double>(n) * (a->d_in + a->d_out) * esz + 4.0 * w_elems;
+            HETA_TRY((launch_product<true, true>(who, "linear_grad_w_kernel", a->dt, p, bytes, flops, st)));
+        }
+        HETA_TRY(fold_partials(part, n_split, static_cast<int64_t>(a->d_in) * a->d_out, a->dW, a->dw_dt, a->d_out, a->ld_dw, st));
+    }
+    return HETA_OK;
+}
+
+extern "C" heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int64_t ld_w, int32_t d_in, int32_t d_out, void *packed, int64_t ld_packed, float *scale, void *hip_stream)
+{
+    const char *who = "heta_linear_pack_e4m3";
+    if (!valid_dtype(w_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (d_in <= 0 || d_out <= 0) return fail(HETA_ERR_SHAPE, "%s: need widths > 0", who);
+    HETA_TRY(check_matrix(who, "W", W, 1, ld_w, d_out, dtype_size(w_dt)));
+    HETA_TRY(check_matrix(who, "packed", packed, 1, ld_packed, d_in, 1));
+    if (!scale || (reinterpret_cast<uintptr_t>(scale) & 3u)) return fail(HETA_ERR_INVALID_ARG, "%s: bad scale", who);
+    const RowRange w(W, d_in, ld_w, d_out, dtype_size(w_dt)), o(packed, d_out, ld_packed, d_in, 1), s(scale, 1, d_out, d_out, 4);
+    if (o.overlaps(w) || s.overlaps(w) || s.overlaps(o)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);
+    hipStream_t st = as_stream(hip_stream);
+    ProfScope prof("pack_e4m3_kernel", st, static_cast<double>(d_in) * d_out * (2.0 * dtype_size(w_dt) + 1.0), 0);
+    if (w_dt == HETA_F32)
+        hipLaunchKernelGGL(pack_e4m3_kernel<float>, dim3((d_out + 3) / 4), dim3(256), 0, st, static_cast<const float *>(W), ld_w, d_in, d_out,
+                           static_cast<uint8_t *>(packed), ld_packed, scale);
+    else
+        hipLaunchKernelGGL(pack_e4m3_kernel<bf16_t>, dim3((d_out + 3) / 4), dim3(256), 0, st, static_cast<const bf16_t *>(W), ld_w, d_in, d_out,
+                           static_cast<uint8_t *>(packed), ld_packed, scale);
+    HETA_LAUNCH_CHECK("pack_e4m3_kernel");
+    return HETA_OK;
+}

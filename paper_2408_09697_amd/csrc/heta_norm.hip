@@ -1,0 +1,457 @@
+// Root-mean-square norm of embedding rows with the residual's addition in front, its backward pass, and an 8-bit output
+// with a scale a row for products of 8-bit operands.
+//
+//     s = round(x + residual) (stored if asked for),  rstd = (sum_j s_j^2 / d + eps)^(-1/2),  out = s rstd gamma
+//     8-bit: scale = max_j |out_j| / 448,  q = e4m3(out / scale); a row of zeros has scale 0
+//     h = s rstd, w = grad_out gamma:  grad_x = rstd (w - h sum_j(w_j h_j) / d) + grad_sum,  grad_gamma = sum over rows of grad_out h
+//
+// HBM-bound: six to nine operations per element that is read.  One pass: a row lives in the registers of 8 to 64 lanes
+// from its load to its last store (LANES x NV chunks of eight elements; rows of more than 2,048 columns are walked by a
+// workgroup, up to three times through the caches).  Statistics and all sums are fp32.  Rows that are not 16-byte aligned
+// are dealt to the lanes element by element, so that a load instruction still covers consecutive memory.
+// grad_gamma: every lane adds up its columns over the rows it visits, a workgroup joins its groups of lanes through LDS in
+// order, and the workgroups' partial sums are added in a fixed order: no atomics.
+#include <algorithm>
+
+#include "heta_rows.h"
+
+namespace heta {
+
+struct NormFwd {
+    const void *x, *residual; // residual nullable
+    void *sum, *out;          // sum nullable
+    const float *gamma;       // nullable: ones
+    float *scale, *rstd;      // scale with 8-bit output, rstd nullable
+    int64_t ld_x, ld_res, ld_sum, ld_out, n_rows;
+    int32_t d;
+    float eps;
+};
+
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
+{
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+template <int LANES> __device__ __forceinline__ float lanes_max(float v)
+{
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+// Element e of chunk v of lane l: with VEC eight consecutive columns of the row, else columns LANES apart.
+template <int LANES, bool VEC> __device__ __forceinline__ int column(int v, int e, int l) { return VEC ? (v * LANES + l) * 8 + e : (v * 8 + e) * LANES + l; }
+
+template <int LANES, int NV, bool VEC, typename T> __device__ __forceinline__ void load_row(const T *row, int d, int l, float (&x)[NV][8])
+{
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        if constexpr (VEC) {
+            const int c = column<LANES, true>(v, 0, l);
+            load8(row + c, d - c, true, x[v]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int c = column<LANES, false>(v, e, l);
+                x[v][e] = c < d ? widen(row[c]) : 0.f;
+            }
+        }
+    }
+}
+template <int LANES, int NV, bool VEC, typename T> __device__ __forceinline__ void store_row(T *row, int d, int l, const float (&x)[NV][8])
+{
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        if constexpr (VEC) {
+            const int c = column<LANES, true>(v, 0, l);
+            store8(row + c, d - c, true, x[v]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int c = column<LANES, false>(v, e, l);
+                if (c < d) {
+                    if constexpr (sizeof(T) == 2) row[c] = to_bf16(x[v][e]);
+                    else row[c] = x[v][e];
+                }
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d)
+{
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
+}
+// 8-bit scale of a row whose largest magnitude is amax: the factor (0 for a row of zeros); amax / 448 may be subnormal
+__device__ __forceinline__ float e4m3_factor(float amax) { return amax > 0.f ? fminf(448.f / amax, 3.402823466e38f) : 0.f; }
+
+template <int LANES, int NV, bool VEC> __device__ __forceinline__ void store_row_e4m3(uint8_t *row, int d, int l, const float (&x)[NV][8], float f)
+{
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const uint32_t lo = four_e4m3(x[v][0] * f, x[v][1] * f, x[v][2] * f, x[v][3] * f), hi = four_e4m3(x[v][4] * f, x[v][5] * f, x[v][6] * f, x[v][7] * f);
+        const int c = column<LANES, VEC>(v, 0, l);
+        if (VEC && c + 8 <= d) {
+            *reinterpret_cast<uint2 *>(row + c) = make_uint2(lo, hi);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int ce = column<LANES, VEC>(v, e, l);
+                if (ce < d) row[ce] = static_cast<uint8_t>((e < 4 ? lo >> (8 * e) : hi >> (8 * (e - 4))) & 0xff);
+            }
+        }
+    }
+}
+
+template <typename T> __device__ __forceinline__ float rounded(float v)
+{
+    if constexpr (sizeof(T) == 2) return widen(to_bf16(v));
+    else return v;
+}
+
+// T: type of x, residual and sum; O: of the output (uint8_t: e4m3)
+template <typename T, typename O, int LANES, int NV, bool VEC> __global__ void __launch_bounds__(256) rms_norm_kernel(NormFwd p)
+{
+    constexpr int GROUPS = 256 / LANES;
+    const int l = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+    float gamma[NV][8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = column<LANES, VEC>(v, e, l);
+            gamma[v][e] = p.gamma && c < p.d ? p.gamma[c] : 1.f;
+        }
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * GROUPS + grp; r < p.n_rows; r += static_cast<int64_t>(gridDim.x) * GROUPS) {
+        float x[NV][8];
+        load_row<LANES, NV, VEC>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, x);
+        if (p.residual) {
+            float y[NV][8];
+            load_row<LANES, NV, VEC>(static_cast<const T *>(p.residual) + r * p.ld_res, p.d, l, y);
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[v][e] = rounded<T>(x[v][e] + y[v][e]);
+        }
+        if (p.sum) store_row<LANES, NV, VEC>(static_cast<T *>(p.sum) + r * p.ld_sum, p.d, l, x);
+        float ss = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss += x[v][e] * x[v][e];
+        const float rstd = 1.f / sqrtf(lanes_sum<LANES>(ss) / static_cast<float>(p.d) + p.eps);
+        if (p.rstd && l == 0) p.rstd[r] = rstd;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[v][e] = x[v][e] * rstd * gamma[v][e];
+        if constexpr (sizeof(O) == 1) {
+            float amax = 0.f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[v][e]));
+            amax = lanes_max<LANES>(amax);
+            if (l == 0) p.scale[r] = amax / 448.f;
+            store_row_e4m3<LANES, NV, VEC>(static_cast<uint8_t *>(p.out) + r * p.ld_out, p.d, l, x, e4m3_factor(amax));
+        } else {
+            store_row<LANES, NV, VEC>(static_cast<O *>(p.out) + r * p.ld_out, p.d, l, x);
+        }
+    }
+}
+
+// Sum (or maximum) over the 256 threads of a workgroup, in every thread.
+template <bool MAX> __device__ __forceinline__ float group_reduce(float v, float *lds)
+{
+    v = MAX ? lanes_max<64>(v) : lanes_sum<64>(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return MAX ? fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3])) : (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+// Rows too wide for one wavefront's registers: a workgroup per row.  `sum` may alias x or residual: a thread reads its
+// columns before it writes them, and later passes read the sum.
+template <typename T, typename O> __global__ void __launch_bounds__(256) rms_norm_wide_kernel(NormFwd p)
+{
+    __shared__ float lds[4];
+    for (int64_t r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
+        const T *x = static_cast<const T *>(p.x) + r * p.ld_x, *y = p.residual ? static_cast<const T *>(p.residual) + r * p.ld_res : nullptr;
+        T *sum = p.sum ? static_cast<T *>(p.sum) + r * p.ld_sum : nullptr;
+        float ss = 0.f;
+        for (int c = threadIdx.x; c < p.d; c += 256) {
+            const float s = y ? rounded<T>(widen(x[c]) + widen(y[c])) : widen(x[c]);
+            if (sum) {
+                if constexpr (sizeof(T) == 2) sum[c] = to_bf16(s);
+                else sum[c] = s;
+            }
+            ss += s * s;
+        }
+        const float rstd = 1.f / sqrtf(group_reduce<false>(ss, lds) / static_cast<float>(p.d) + p.eps);
+        if (p.rstd && threadIdx.x == 0) p.rstd[r] = rstd;
+        auto value = [&](int c) {
+            const float s = sum ? widen(sum[c]) : (y ? rounded<T>(widen(x[c]) + widen(y[c])) : widen(x[c]));
+            return s * rstd * (p.gamma ? p.gamma[c] : 1.f);
+        };
+        if constexpr (sizeof(O) == 1) {
+            float amax = 0.f;
+            for (int c = threadIdx.x; c < p.d; c += 256) amax = fmaxf(amax, fabsf(value(c)));
+            amax = group_reduce<true>(amax, lds);
+            if (threadIdx.x == 0) p.scale[r] = amax / 448.f;
+            const float f = e4m3_factor(amax);
+            for (int c = threadIdx.x; c < p.d; c += 256) {
+                const float v = value(c) * f;
+                (static_cast<uint8_t *>(p.out) + r * p.ld_out)[c] = static_cast<uint8_t>(__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false) & 0xff);
+            }
+        } else {
+            O *out = static_cast<O *>(p.out) + r * p.ld_out;
+            for (int c = threadIdx.x; c < p.d; c += 256) {
+                if constexpr (sizeof(O) == 2) out[c] = to_bf16(value(c));
+                else out[c] = value(c);
+            }
+        }
+    }
+}
+
+struct NormBwd {
+    const void *x, *grad_out, *grad_sum; // grad_sum nullable
+    void *grad_x;
+    const float *gamma, *rstd;           // gamma nullable
+    float *part;                         // [workgroups][d], nullable
+    int64_t ld_x, ld_go, ld_gs, ld_gx, n_rows;
+    int32_t d;
+};
+
+template <typename T, typename G, int LANES, int NV, bool VEC> __global__ void __launch_bounds__(256) rms_norm_bwd_kernel(NormBwd p)
+{
+    constexpr int GROUPS = 256 / LANES;
+    __shared__ float joined[GROUPS * LANES * NV * 8];
+    const int l = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+    float gamma[NV][8], dg[NV][8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = column<LANES, VEC>(v, e, l);
+            gamma[v][e] = p.gamma && c < p.d ? p.gamma[c] : 1.f;
+            dg[v][e] = 0.f;
+        }
+    const float inv_d = 1.f / static_cast<float>(p.d);
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * GROUPS + grp; r < p.n_rows; r += static_cast<int64_t>(gridDim.x) * GROUPS) {
+        float h[NV][8], w[NV][8];
+        load_row<LANES, NV, VEC>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, h);
+        load_row<LANES, NV, VEC>(static_cast<const G *>(p.grad_out) + r * p.ld_go, p.d, l, w);
+        const float rstd = p.rstd[r];
+        float dot = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[v][e] *= rstd;
+                dg[v][e] += w[v][e] * h[v][e];
+                w[v][e] *= gamma[v][e];
+                dot += w[v][e] * h[v][e];
+            }
+        dot = lanes_sum<LANES>(dot) * inv_d;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[v][e] = rstd * (w[v][e] - h[v][e] * dot);
+        if (p.grad_sum) {
+            load_row<LANES, NV, VEC>(static_cast<const T *>(p.grad_sum) + r * p.ld_gs, p.d, l, h);
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[v][e] += h[v][e];
+        }
+        store_row<LANES, NV, VEC>(static_cast<T *>(p.grad_x) + r * p.ld_gx, p.d, l, w);
+    }
+    if (!p.part) return;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) joined[(grp * NV * 8 + v * 8 + e) * LANES + l] = dg[v][e];
+    __syncthreads();
+    for (int q = threadIdx.x; q < LANES * NV * 8; q += 256) {
+        float s = 0.f;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) s += joined[g * NV * 8 * LANES + q];
+        const int c = column<LANES, VEC>(q / LANES / 8, q / LANES % 8, q % LANES);
+        if (c < p.d) p.part[static_cast<int64_t>(blockIdx.x) * p.d + c] = s;
+    }
+}
+
+// Rows too wide for one wavefront's registers: a workgroup per row; grad_gamma by a kernel of its own over slabs of rows.
+template <typename T, typename G> __global__ void __launch_bounds__(256) rms_norm_bwd_wide_kernel(NormBwd p)
+{
+    __shared__ float lds[4];
+    for (int64_t r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
+        const T *x = static_cast<const T *>(p.x) + r * p.ld_x, *gs = p.grad_sum ? static_cast<const T *>(p.grad_sum) + r * p.ld_gs : nullptr;
+        const G *go = static_cast<const G *>(p.grad_out) + r * p.ld_go;
+        T *gx = static_cast<T *>(p.grad_x) + r * p.ld_gx;
+        const float rstd = p.rstd[r];
+        float dot = 0.f;
+        for (int c = threadIdx.x; c < p.d; c += 256) dot += widen(go[c]) * (p.gamma ? p.gamma[c] : 1.f) * (widen(x[c]) * rstd);
+        dot = group_reduce<false>(dot, lds) / static_cast<float>(p.d);
+        for (int c = threadIdx.x; c < p.d; c += 256) {
+            float v = rstd * (widen(go[c]) * (p.gamma ? p.gamma[c] : 1.f) - widen(x[c]) * rstd * dot);
+            if (gs) v += widen(gs[c]);
+            if constexpr (sizeof(T) == 2) gx[c] = to_bf16(v);
+            else gx[c] = v;
+        }
+    }
+}
+template <typename T, typename G> __global__ void __launch_bounds__(256) rms_norm_gamma_kernel(NormBwd p, int64_t rows_each)
+{
+    const uint32_t strips = (p.d + 255) / 256;
+    const int64_t slab = blockIdx.x / strips;
+    const int c = static_cast<int>(blockIdx.x % strips) * 256 + threadIdx.x;
+    if (c >= p.d) return;
+    const int64_t end = min(p.n_rows, (slab + 1) * rows_each);
+    float s = 0.f;
+#pragma unroll 4
+    for (int64_t r = slab * rows_each; r < end; ++r)
+        s += widen(static_cast<const G *>(p.grad_out)[r * p.ld_go + c]) * (widen(static_cast<const T *>(p.x)[r * p.ld_x + c]) * p.rstd[r]);
+    p.part[slab * p.d + c] = s;
+}
+
+// ---- host side ---------------------------------------------------------------------------------------
+// Lanes and chunks per row by width, so that as few lanes as possible lie idle: f(lanes, chunks) or, above, wide().
+template <typename F, typename W> static void by_width(int32_t d, F f, W wide)
+{
+    using std::integral_constant;
+    if (d <= 64) f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    else if (d <= 128) f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (d <= 256) f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    else if (d <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (d <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    else if (d <= 2048) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else wide();
+}
+static unsigned row_blocks(int64_t n_rows, int groups, int64_t most) { return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n_rows + groups - 1) / groups, most))); }
+
+template <typename T, typename O> static void launch_norm(const NormFwd &p, bool vec, hipStream_t st)
+{
+    by_width(
+        p.d,
+        [&](auto lanes, auto nv) {
+            constexpr int L = decltype(lanes)::value, V = decltype(nv)::value;
+            const dim3 grid(row_blocks(p.n_rows, 256 / L, 4096));
+            if (vec) hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, true>), grid, dim3(256), 0, st, p);
+            else hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, false>), grid, dim3(256), 0, st, p);
+        },
+        [&] { hipLaunchKernelGGL((rms_norm_wide_kernel<T, O>), dim3(row_blocks(p.n_rows, 1, 8192)), dim3(256), 0, st, p); });
+}
+
+constexpr int64_t kNormBwdBlocks = 2048;
+
+template <typename T, typename G> static void launch_norm_bwd(const NormBwd &p, bool vec, int64_t n_part, hipStream_t st)
+{
+    by_width(
+        p.d,
+        [&](auto lanes, auto nv) {
+            constexpr int L = decltype(lanes)::value, V = decltype(nv)::value;
+            const dim3 grid(static_cast<unsigned>(n_part));
+            if (vec) hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, true>), grid, dim3(256), 0, st, p);
+            else hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, false>), grid, dim3(256), 0, st, p);
+        },
+        [&] {
+            hipLaunchKernelGGL((rms_norm_bwd_wide_kernel<T, G>), dim3(row_blocks(p.n_rows, 1, 8192)), dim3(256), 0, st, p);
+            if (p.part)
+                hipLaunchKernelGGL((rms_norm_gamma_kernel<T, G>), dim3(static_cast<unsigned>(n_part * ((p.d + 255) / 256))), dim3(256), 0, st, p,
+                                   (p.n_rows + n_part - 1) / n_part);
+        });
+}
+
+static heta_status check_rows(const char *who, const char *what, const void *p, int64_t n_rows, int64_t ld, int32_t d, size_t elt)
+{
+    if (!p && n_rows > 0) return fail(HETA_ERR_INVALID_ARG, "%s: null %s", who, what);
+    if (ld < d) return fail(HETA_ERR_SHAPE, "%s: leading dimension of %s is below its width", who, what);
+    if (reinterpret_cast<uintptr_t>(p) % elt) return fail(HETA_ERR_INVALID_ARG, "%s: %s is not aligned to its element size", who, what);
+    return HETA_OK;
+}
+
+} // namespace heta
+
+using namespace heta;
+
+extern "C" heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, const void *residual, int64_t ld_res, const float *gamma,
+                                     float eps, void *sum, int64_t ld_sum, void *out, heta_dtype out_dt, int64_t ld_out, float *scale, float *rstd, void *hip_stream)
+{
+    const char *who = "heta_rms_norm";
+    if (n_rows < 0 || d <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and d > 0", who);
+    if (!valid_dtype(x_dt) || (!valid_dtype(out_dt) && out_dt != HETA_E4M3)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (!(eps >= 0.f)) return fail(HETA_ERR_INVALID_ARG, "%s: need eps >= 0", who);
+    const bool q = out_dt == HETA_E4M3;
+    if (x_dt == HETA_BF16 && out_dt == HETA_F32) return fail(HETA_ERR_UNSUPPORTED, "%s: bf16 rows have a bf16 or an 8-bit output", who);
+    if (q != (scale != nullptr) && !(q && n_rows == 0)) return fail(HETA_ERR_INVALID_ARG, "%s: scales belong to an 8-bit output, and that needs them", who);
+    const size_t esz = dtype_size(x_dt), osz = q ? 1 : dtype_size(out_dt);
+    HETA_TRY(check_rows(who, "x", x, n_rows, ld_x, d, esz));
+    HETA_TRY(check_rows(who, "out", out, n_rows, ld_out, d, osz));
+    if (residual) HETA_TRY(check_rows(who, "residual", residual, n_rows, ld_res, d, esz));
+    if (sum) HETA_TRY(check_rows(who, "sum", sum, n_rows, ld_sum, d, esz));
+    for (const float *v : {gamma, static_cast<const float *>(scale), static_cast<const float *>(rstd)})
+        if (reinterpret_cast<uintptr_t>(v) & 3u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
+    // every array is read and written row by row by the lanes that hold the row: outputs may lie on inputs, in the same rows
+    const RowRange rx(x, n_rows, ld_x, d, esz), rr(residual, n_rows, ld_res, d, esz), rs(sum, n_rows, ld_sum, d, esz), ro(out, n_rows, ld_out, d, osz);
+    const bool sum_on_x = sum == x && ld_sum == ld_x, sum_on_res = sum == residual && ld_sum == ld_res;
+    if ((rs.overlaps(rx) && !sum_on_x) || (rs.overlaps(rr) && !sum_on_res) || ro.overlaps(rx) || ro.overlaps(rr) || ro.overlaps(rs))
+        return fail(HETA_ERR_INVALID_ARG, "%s: out overlaps another array, or sum one in other rows", who);
+    if (n_rows == 0) return HETA_OK;
+    const NormFwd p{x, residual, sum, out, gamma, scale, rstd, ld_x, ld_res, ld_sum, ld_out, n_rows, d, eps};
+    const bool vec = vec_rows(x, ld_x, esz) && vec_rows(residual, ld_res, esz) && vec_rows(sum, ld_sum, esz) &&
+                     (q ? ld_out % 8 == 0 && reinterpret_cast<uintptr_t>(out) % 8 == 0 : vec_rows(out, ld_out, osz));
+    hipStream_t st = as_stream(hip_stream);
+    ProfScope prof("rms_norm_kernel", st, static_cast<double>(n_rows) * d * (esz * (1.0 + !!residual + !!sum) + osz), 6.0 * n_rows * d);
+    if (x_dt == HETA_F32) {
+        if (q) launch_norm<float, uint8_t>(p, vec, st);
+        else if (out_dt == HETA_F32) launch_norm<float, float>(p, vec, st);
+        else launch_norm<float, bf16_t>(p, vec, st);
+    } else {
+        if (q) launch_norm<bf16_t, uint8_t>(p, vec, st);
+        else launch_norm<bf16_t, bf16_t>(p, vec, st);
+    }
+    HETA_LAUNCH_CHECK("rms_norm_kernel");
+    return HETA_OK;
+}
+
+extern "C" heta_status heta_rms_norm_bwd(heta_graph *g, int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, const float *gamma, const float *rstd,
+                                         const void *grad_out, heta_dtype go_dt, int64_t ld_go, const void *grad_sum, int64_t ld_gs, void *grad_x, int64_t ld_gx,
+                                         float *grad_gamma, void *hip_stream)
+{
+    const char *who = "heta_rms_norm_bwd";
+    if (!g) return fail(HETA_ERR_INVALID_ARG, "%s: null handle", who);
+    if (n_rows < 0 || d <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and d > 0", who);
+    if (!valid_dtype(x_dt) || !valid_dtype(go_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (x_dt == HETA_BF16 && go_dt == HETA_F32) return fail(HETA_ERR_UNSUPPORTED, "%s: bf16 rows have a bf16 gradient", who);
+    const size_t esz = dtype_size(x_dt), gsz = dtype_size(go_dt);
+    HETA_TRY(check_rows(who, "x", x, n_rows, ld_x, d, esz));
+    HETA_TRY(check_rows(who, "grad_out", grad_out, n_rows, ld_go, d, gsz));
+    HETA_TRY(check_rows(who, "grad_x", grad_x, n_rows, ld_gx, d, esz));
+    if (grad_sum) HETA_TRY(check_rows(who, "grad_sum", grad_sum, n_rows, ld_gs, d, esz));
+    if (!rstd && n_rows > 0) return fail(HETA_ERR_INVALID_ARG, "%s: null rstd", who);
+    for (const float *v : {gamma, rstd, static_cast<const float *>(grad_gamma)})
+        if (reinterpret_cast<uintptr_t>(v) & 3u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
+    const RowRange rx(x, n_rows, ld_x, d, esz), rg(grad_out, n_rows, ld_go, d, gsz), rs(grad_sum, n_rows, ld_gs, d, esz), ro(grad_x, n_rows, ld_gx, d, esz);
+    // grad_x may be grad_sum (the same lane reads and writes); rows of more than 2,048 columns read x and grad_out twice
+    if (ro.overlaps(rx) || ro.overlaps(rg) || (ro.overlaps(rs) && !(grad_x == grad_sum && ld_gx == ld_gs)))
+        return fail(HETA_ERR_INVALID_ARG, "%s: grad_x overlaps an operand", who);
+    int64_t n_part = 0;
+    by_width(d, [&](auto lanes, auto) { n_part = row_blocks(n_rows, 256 / decltype(lanes)::value, kNormBwdBlocks); }, [&] { n_part = row_blocks(n_rows, 32, 256); });
+    if (n_rows == 0) n_part = 0;
+    if (grad_gamma) HETA_TRY(ensure_workspace(g, static_cast<size_t>(std::max<int64_t>(n_part, 1)) * d * sizeof(float)));
+    float *part = grad_gamma ? static_cast<float *>(g->d_ws) : nullptr;
+    hipStream_t st = as_stream(hip_stream);
+    if (n_rows > 0) {
+        const NormBwd p{x, grad_out, grad_sum, grad_x, gamma, rstd, part, ld_x, ld_go, ld_gs, ld_gx, n_rows, d};
+        const bool vec = vec_rows(x, ld_x, esz) && vec_rows(grad_out, ld_go, gsz) && vec_rows(grad_sum, ld_gs, esz) && vec_rows(grad_x, ld_gx, esz);
+        ProfScope prof("rms_norm_bwd_kernel", st, static_cast<double>(n_rows) * d * (esz * (2.0 + !!grad_sum) + gsz), 9.0 * n_rows * d);
+        if (x_dt == HETA_BF16) launch_norm_bwd<bf16_t, bf16_t>(p, vec, n_part, st);
+        else if (go_dt == HETA_F32) launch_norm_bwd<float, float>(p, vec, n_part, st);
+        else launch_norm_bwd<float, bf16_t>(p, vec, n_part, st);
+        HETA_LAUNCH_CHECK("rms_norm_bwd_kernel");
+    }
+    return grad_gamma ? fold_partials(part, n_part, d, grad_gamma, HETA_F32, d, d, st) : HETA_OK;
+}

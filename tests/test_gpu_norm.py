@@ -1,0 +1,220 @@
+"""heta_rms_norm and heta_rms_norm_bwd against the definition in 64 bits.
+
+Tolerances, u = 2^-24 (one fp32 rounding).  A row's sum of squares has positive terms, added at most 48 deep (32 per lane or
+d / 256 per thread, then a tree), so it is off by at most 48 u relative, rstd by 24 u + 3 u (root, quotient, division by d)
+and an output by two products more: 32 u |out|.  A bf16 output is rounded once more, by 2^-8 of its value; an 8-bit one by 2^-4
+of its value or half the smallest step, 2^-10 of its scale (448 at the row's largest).
+grad_x = rstd (w - h mean(w h)): every term is off by at most 64 u of its magnitude, and so is the sum by that of the magnitudes
+added up.  grad_gamma adds n terms in chains: (n / lanes groups + 160) u of the magnitudes added up is an upper bound.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2408_09697_amd as heta
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+HALF = {torch.float32: U, torch.bfloat16: 2.0 ** -8}
+F32, BF16, E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def handle():
+    g = heta.heta_graph_create([(1, 1, 0)], [])
+    yield g
+    g.destroy()
+
+
+def rows(n, d, dtype, seed, pad=0, scale=1.0):
+    """[n, d] rows in a buffer whose leading dimension is d + pad."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    buf = torch.full((n, d + pad), float("nan"), device="cuda", dtype=dtype)
+    buf[:, :d] = (torch.randn(n, d, generator=g, device="cuda") * scale).to(dtype)
+    return buf[:, :d]
+
+
+def gammas(d, seed=5):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return 1.0 + 0.2 * torch.randn(d, generator=g, device="cuda")
+
+
+def reference(x, residual, gamma, eps):
+    s = x.double() if residual is None else (x.double() + residual.double()).to(x.dtype).double()
+    rstd = 1.0 / torch.sqrt((s * s).mean(1) + eps)
+    y = s * rstd[:, None]
+    return s, rstd, y if gamma is None else y * gamma.double()
+
+
+def within(got, ref, bound, what):
+    off = (got.double() - ref).abs()
+    assert torch.isfinite(got.double()).all(), what
+    assert (off <= bound).all(), f"{what}: {float((off - bound).max()):.3e} over its bound, worst {float(off.max()):.3e}"
+
+
+SHAPES = [(1, 1), (1, 7), (3, 16), (5, 64), (64, 256), (129, 100), (1000, 300), (77, 789), (17, 1000), (33, 2048), (9, 2049), (4, 5003), (70000, 24)]
+
+
+@pytest.mark.parametrize("n,d", SHAPES)
+@pytest.mark.parametrize("dtype,out_dtype", [(F32, F32), (F32, BF16), (F32, E4M3), (BF16, BF16), (BF16, E4M3)])
+@pytest.mark.parametrize("pad", [0, 5, 16])
+def test_forward(n, d, dtype, out_dtype, pad):
+    x, res = rows(n, d, dtype, 1, pad), rows(n, d, dtype, 2, pad) if d % 3 else None
+    gamma = gammas(d) if d != 64 else None
+    out = rows(n, d, F32, 3, pad).to(out_dtype) if pad == 0 else torch.empty(n, d + pad, device="cuda", dtype=out_dtype)[:, :d]
+    total = rows(n, d, dtype, 4, pad) if res is not None else None
+    scale = torch.empty(n, device="cuda") if out_dtype is E4M3 else None
+    rstd = torch.empty(n, device="cuda")
+    heta.heta_rms_norm(x, out, residual=res, sum=total, gamma=gamma, eps=1e-5, scale=scale, rstd=rstd)
+    s, r, y = reference(x, res, gamma, 1e-5)
+    if total is not None:
+        assert torch.equal(total.double(), s)
+    within(rstd, r, 32 * U * r, "rstd")
+    if out_dtype is E4M3:
+        top = y.abs().amax(1)
+        within(scale, top / 448, 40 * U * top / 448 + 2.0 ** -149, "scale")
+        got = out.float().double() * scale.double()[:, None]
+        within(got, y, (2.0 ** -4 + 128 * U) * y.abs() + 2.0 ** -10 * (1 + 128 * U) * scale.double()[:, None], "8-bit rows")
+    else:
+        within(out, y, (32 * U + (HALF[BF16] if out_dtype is BF16 else 0)) * y.abs(), "out")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [24, 256, 1000, 2500])
+def test_sum_may_be_its_own_operand(dtype, d):
+    x, res = rows(70, d, dtype, 1), rows(70, d, dtype, 2)
+    want, out0 = torch.empty_like(x), torch.empty_like(x)
+    heta.heta_rms_norm(x, out0, residual=res, sum=want)
+    for which in ("x", "residual"):
+        a, b, out = x.clone(), res.clone(), torch.empty_like(x)
+        heta.heta_rms_norm(a, out, residual=b, sum=a if which == "x" else b)
+        assert torch.equal(a if which == "x" else b, want) and torch.equal(out, out0)
+
+
+def test_rows_of_zeros_and_of_infinities_keep_to_themselves():
+    x = rows(40, 200, F32, 1)
+    clean = x.clone()
+    x[3] = 0.0
+    x[7, 11] = float("inf")
+    x[9, 0] = float("nan")
+    x[12] = 3.0e38  # the sum of squares overflows: rstd = 0
+    for out_dtype in (F32, BF16, E4M3):
+        out, ref = torch.empty(40, 200, device="cuda", dtype=out_dtype), torch.empty(40, 200, device="cuda", dtype=out_dtype)
+        scale, scale0 = (torch.empty(40, device="cuda") if out_dtype is E4M3 else None for _ in range(2))
+        heta.heta_rms_norm(x, out, eps=0.0 if out_dtype is F32 else 1e-6, scale=scale)
+        heta.heta_rms_norm(clean, ref, eps=0.0 if out_dtype is F32 else 1e-6, scale=scale0)
+        keep = [i for i in range(40) if i not in (3, 7, 9, 12)]
+        assert torch.equal(out[keep].float(), ref[keep].float())
+        assert out[9].float().isnan().all()
+        if out_dtype is not F32:
+            assert (out[3].float() == 0).all() and (out[12].float() == 0).all()
+            if scale is not None:
+                assert float(scale[3]) == 0.0 and float(scale[12]) == 0.0
+
+
+def test_no_rows(handle):
+    x, gamma = torch.empty(0, 32, device="cuda"), gammas(32)
+    heta.heta_rms_norm(x, torch.empty_like(x), gamma=gamma)
+    gg = torch.full((32,), 7.0, device="cuda")
+    heta.heta_rms_norm_bwd(handle, x, torch.empty(0, device="cuda"), x.clone(), torch.empty_like(x), gamma=gamma, grad_gamma=gg)
+    assert (gg == 0).all()
+
+
+def backward_reference(x, rstd, go, gs, gamma):
+    xd, god, r = x.double(), go.double(), rstd.double()[:, None]
+    w = god if gamma is None else god * gamma.double()
+    h = xd * r
+    dot = (w * h).mean(1, keepdim=True)
+    gx = r * (w - h * dot)
+    size = r * (w.abs() + h.abs() * (w * h).abs().mean(1, keepdim=True))
+    if gs is not None:
+        gx, size = gx + gs.double(), size + gs.double().abs()
+    return gx, size, (god * h).sum(0), (god * h).abs().sum(0)
+
+
+@pytest.mark.parametrize("n,d", SHAPES)
+@pytest.mark.parametrize("dtype,go_dtype", [(F32, F32), (F32, BF16), (BF16, BF16)])
+@pytest.mark.parametrize("pad", [0, 5, 16])
+def test_backward(handle, n, d, dtype, go_dtype, pad):
+    x, go = rows(n, d, dtype, 1, pad), rows(n, d, go_dtype, 2, pad)
+    gs = rows(n, d, dtype, 3, pad) if d % 3 else None
+    gamma = gammas(d) if d != 64 else None
+    rstd = 1.0 / torch.sqrt((x.float() ** 2).mean(1) + 1e-5)
+    gx, gg = rows(n, d, dtype, 4, pad), torch.empty(d, device="cuda")
+    heta.heta_rms_norm_bwd(handle, x, rstd, go, gx, gamma=gamma, grad_sum=gs, grad_gamma=gg)
+    ref, size, gref, gsize = backward_reference(x, rstd, go, gs, gamma)
+    within(gx, ref, 64 * U * size + (HALF[BF16] * ref.abs() if dtype is BF16 else 0), "grad_x")
+    within(gg, gref, (n / 64 + 160) * U * gsize, "grad_gamma")
+    # the gradient that passes the norm by may be overwritten by the sum, and grad_gamma left out
+    if gs is not None:
+        same = gs.clone()
+        heta.heta_rms_norm_bwd(handle, x, rstd, go, same, gamma=gamma, grad_sum=same)
+        assert torch.equal(same, gx)
+
+
+def test_backward_agrees_with_differences(handle):
+    """(f(x + t v) - f(x - t v)) / 2t of f = <norm(x), c> in 64 bits; t = 1e-5: truncation ~1e-10, rounding ~1e-11."""
+    n, d, eps = 6, 50, 1e-3
+    x, c, gamma, v = rows(n, d, F32, 1), rows(n, d, F32, 2), gammas(d), rows(n, d, F32, 3).double()
+    rstd = 1.0 / torch.sqrt((x.double() ** 2).mean(1) + eps)
+    gx, gg = torch.empty_like(x), torch.empty(d, device="cuda")
+    heta.heta_rms_norm_bwd(handle, x, rstd.float(), c, gx, gamma=gamma, grad_gamma=gg)
+
+    def f(xx, gm):
+        return (xx / torch.sqrt((xx * xx).mean(1, keepdim=True) + eps) * gm * c.double()).sum()
+
+    t, dg = 1e-5, rows(1, d, F32, 4).double()[0]
+    by_x = (f(x.double() + t * v, gamma.double()) - f(x.double() - t * v, gamma.double())) / (2 * t)
+    by_gamma = (f(x.double(), gamma.double() + t * dg) - f(x.double(), gamma.double() - t * dg)) / (2 * t)
+    size_x, size_g = (gx.double() * v).abs().sum(), (gg.double() * dg).abs().sum()
+    assert abs(float((gx.double() * v).sum() - by_x)) <= 1e-5 * float(size_x)
+    assert abs(float((gg.double() * dg).sum() - by_gamma)) <= 1e-5 * float(size_g)
+
+
+def test_same_bits_again_and_on_another_stream(handle):
+    x, go, gamma = rows(5000, 256, BF16, 1), rows(5000, 256, BF16, 2), gammas(256)
+    rstd = 1.0 / torch.sqrt((x.float() ** 2).mean(1) + 1e-5)
+    got = []
+    side = torch.cuda.Stream()
+    for stream in (None, None, side):
+        gx, gg, out = torch.empty_like(x), torch.empty(256, device="cuda"), torch.empty_like(x)
+        torch.cuda.synchronize()
+        heta.heta_rms_norm(x, out, gamma=gamma, stream=stream)
+        heta.heta_rms_norm_bwd(handle, x, rstd, go, gx, gamma=gamma, grad_gamma=gg, stream=stream)
+        torch.cuda.synchronize()
+        got.append((out, gx, gg))
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+def test_backward_in_a_graph(handle):
+    """Captured after a first eager call, replayed several times with eager calls between the replays."""
+    x, go, gamma = rows(3000, 256, F32, 1), rows(3000, 256, F32, 2), gammas(256)
+    rstd = 1.0 / torch.sqrt((x ** 2).mean(1) + 1e-5)
+    want_x, want_g = torch.empty_like(x), torch.empty(256, device="cuda")
+    heta.heta_rms_norm_bwd(handle, x, rstd, go, want_x, gamma=gamma, grad_gamma=want_g)
+    gx, gg = torch.empty_like(x), torch.empty(256, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        heta.heta_rms_norm_bwd(handle, x, rstd, go, gx, gamma=gamma, grad_gamma=gg)
+    for _ in range(3):
+        gx.fill_(float("nan")), gg.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(gx, want_x) and torch.equal(gg, want_g)
+        heta.heta_rms_norm_bwd(handle, x, rstd, go, torch.empty_like(x), gamma=gamma, grad_gamma=torch.empty(256, device="cuda"))
+
+
+def test_offsets_past_32_bits():
+    """Rows whose elements lie more than 2^31 elements apart: 200 rows 12,000,000 elements apart in a bf16 buffer of 4.8 GB."""
+    n, d, ld = 200, 40, 12_000_000
+    buf = torch.empty(n * ld, device="cuda", dtype=BF16)
+    x = buf.as_strided((n, d), (ld, 1))
+    src = rows(n, d, BF16, 1)
+    x.copy_(src)
+    out, want = torch.empty_like(src), torch.empty_like(src)
+    heta.heta_rms_norm(x, out)
+    heta.heta_rms_norm(src, want)
+    assert torch.equal(out, want)
