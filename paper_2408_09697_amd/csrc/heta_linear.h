@@ -1,0 +1,231 @@
+// Epilogues and launches of heta_linear and heta_linear_bwd, shared by the translation units that hold the kernels of one
+// operand type each (not part of the ABI).
+#pragma once
+
+#include <algorithm>
+
+#include "heta_rows.h"
+#include "heta_tiles.h"
+
+namespace heta {
+
+// ---- activations: x * sigmoid(z(x)); GELU in its tanh form, 0.5 (1 + tanh(u)) = sigmoid(2 u) --------------------
+constexpr float kGelu2 = 1.5957691216057308f; // 2 sqrt(2 / pi)
+constexpr float kGeluCubic = 0.044715f;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 1 / (1 + exp(-z)) by the hardware's 2^x and reciprocal (one unit in the last place each)
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z)); }
+
+// -inf takes the value of the lowest finite number, -0, where -inf * 0 would be NaN; NaN stays, by the sigmoid.
+template <int ACT> __device__ __forceinline__ float activate(float x)
+{
+    if constexpr (ACT == HETA_ACT_RELU) return x > 0.f ? x : (x != x ? x : 0.f);
+    const float s = sigmoid(ACT == HETA_ACT_GELU ? x * fmaf(kGelu2 * kGeluCubic, x * x, kGelu2) : x);
+    return fmaxf(x, -3.402823466e38f) * s;
+}
+template <int ACT> __device__ __forceinline__ float activation_slope(float x)
+{
+    if constexpr (ACT == HETA_ACT_RELU) return x > 0.f ? 1.f : (x != x ? x : 0.f);
+    x = x > 60.f ? 60.f : (x < -60.f ? -60.f : x); // the slope is 1 or 0 there; NaN stays
+    if constexpr (ACT == HETA_ACT_GELU) {
+        const float s = sigmoid(x * fmaf(kGelu2 * kGeluCubic, x * x, kGelu2));
+        return fmaf(x * s * (1.f - s), fmaf(3.f * kGelu2 * kGeluCubic, x * x, kGelu2), s);
+    }
+    const float s = sigmoid(x);
+    return fmaf(x * s, 1.f - s, s);
+}
+// Several elements per (uniform) branch: chosen element by element, the choice costs more than the function.
+template <int N> __device__ __forceinline__ void activate_all(float (&y)[N], int act)
+{
+    if (act == HETA_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = activate<HETA_ACT_SILU>(y[e]);
+    } else if (act == HETA_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = activate<HETA_ACT_GELU>(y[e]);
+    } else if (act == HETA_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = activate<HETA_ACT_RELU>(y[e]);
+    }
+}
+template <int N> __device__ __forceinline__ void times_slopes(float (&y)[N], const float (&x)[N], int act)
+{
+    if (act == HETA_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] *= activation_slope<HETA_ACT_SILU>(x[e]);
+    } else if (act == HETA_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] *= activation_slope<HETA_ACT_GELU>(x[e]);
+    } else if (act == HETA_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] *= activation_slope<HETA_ACT_RELU>(x[e]);
+    }
+}
+
+// ---- epilogues ---------------------------------------------------------------------------------------
+struct LinearExtra {
+    const float *bias, *in_scale, *w_scale; // nullable
+    const void *other;                      // nullable: the residual, or the producer's pre-activation whose slope multiplies
+    void *pre, *out_p;                      // pre nullable
+    int64_t ld_other, ld_pre, ld_out;
+    int act, slope_act;                     // slope_act != NONE: other is a pre-activation
+    int vec; // every array in the output's shape can be moved 16 bytes at a time
+};
+// O: type of the outputs and of what is read in their shape.  WHOLE: their rows are whole 16-byte pieces (aligned, a multiple
+// of eight columns) and pass through strips.  SCALED: 8-bit operands.  ACT, SLOPE: which activation, and whose slope, or
+// kAnyAct for a choice at run time (tiles with one block per wavefront): with everything left to run time the epilogue of a
+// large tile is 11,000 instructions long and takes longer than the product.  READS: whether `other` may be there.
+constexpr int kAnyAct = -1;
+template <typename O, bool WHOLE, bool SCALED, int ACT = kAnyAct, int SLOPE = kAnyAct, bool READS = true> struct LinearEpi {
+    static constexpr int kItems = 1;
+    static constexpr bool kStrip = WHOLE, kReads = READS, kPre = SLOPE <= 0;
+    using Out = O;
+    using Extra = LinearExtra;
+    static constexpr int W = 16 / (int)sizeof(O);
+    struct Cols {
+        float bias[W], scale[SCALED ? W : 1];
+        __device__ __forceinline__ void load(const Extra &x, int64_t n, int64_t N)
+        {
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                bias[e] = 0.f;
+                if constexpr (SCALED) scale[e] = 0.f;
+            }
+            if (n >= N) return;
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                if (x.bias) bias[e] = x.bias[n + e];
+                if constexpr (SCALED) scale[e] = x.w_scale[n + e];
+            }
+        }
+    };
+    struct Row {
+        float scale;
+        __device__ __forceinline__ void load(const Extra &x, int64_t m, int64_t M)
+        {
+            if constexpr (SCALED) scale = m < M ? x.in_scale[m] : 0.f;
+        }
+    };
+    __device__ __forceinline__ static O *out(const Extra &x, const TileItem &, int) { return static_cast<O *>(x.out_p); }
+    __device__ __forceinline__ static void first(const Cols &c, const Row &r, float (&y)[W])
+    {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            if constexpr (SCALED) y[e] = fmaf(y[e], r.scale * c.scale[e], c.bias[e]);
+            else y[e] += c.bias[e];
+        }
+    }
+    template <int N> __device__ __forceinline__ static void second(const Extra &x, float (&y)[N], const float (&t)[N])
+    {
+        activate_all(y, ACT == kAnyAct ? x.act : ACT);
+        const int slope = SLOPE == kAnyAct ? x.slope_act : SLOPE;
+        if (slope != HETA_ACT_NONE) {
+            times_slopes(y, t, slope);
+        } else if (READS && x.other) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] += t[e];
+        }
+    }
+    __device__ __forceinline__ static void put(const Extra &x, const TileItem &, int64_t m, int64_t n, int valid, float (&y)[8], int)
+    {
+        float t[8] = {}, s[8];
+        if constexpr (SCALED) {
+            load8(x.w_scale + n, valid, false, s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= x.in_scale[m] * s[e];
+        }
+        if (x.bias) {
+            load8(x.bias + n, valid, false, s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] += s[e];
+        }
+        if (x.pre) store8(static_cast<O *>(x.pre) + m * x.ld_pre + n, valid, x.vec, y);
+        if (x.other) load8(static_cast<const O *>(x.other) + m * x.ld_other + n, valid, x.vec, t);
+        second(x, y, t);
+        store8(static_cast<O *>(x.out_p) + m * x.ld_out + n, valid, x.vec, y);
+    }
+};
+
+// partial products of a contraction that is split over its rows: [split][M][N] fp32.  WHOLE: N is a multiple of four
+template <bool WHOLE> struct PartialEpi {
+    static constexpr int kItems = 1;
+    static constexpr bool kStrip = WHOLE, kReads = false, kPre = false;
+    using Out = float;
+    struct Extra {
+        float *part;
+        int64_t ld_out; // N
+    };
+    struct Cols {
+        __device__ __forceinline__ void load(const Extra &, int64_t, int64_t) {}
+    };
+    using Row = Cols;
+    __device__ __forceinline__ static float *out(const Extra &x, const TileItem &it, int split) { return x.part + split * it.M * it.N; }
+    __device__ __forceinline__ static void first(const Cols &, const Row &, float (&)[4]) {}
+    __device__ __forceinline__ static void second(const Extra &, float (&)[4], const float (&)[4]) {}
+    __device__ __forceinline__ static void put(const Extra &x, const TileItem &it, int64_t m, int64_t n, int valid, const float (&v)[8], int split)
+    {
+        store8(x.part + (split * it.M + m) * it.N + n, valid, false, v);
+    }
+};
+
+// rows that can go straight into LDS: 16-byte aligned, and a tile's rows within 32-bit offsets
+inline bool direct_rows(const void *p, int64_t ld, size_t elt) { return aligned16(p) && (ld * static_cast<int64_t>(elt)) % 16 == 0 && ld * static_cast<int64_t>(elt) < (int64_t(1) << 23); }
+
+inline int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return (M + bm - 1) / bm * ((N + bn - 1) / bn); }
+
+// One product; large tiles where they give every second CU one.
+struct Launch {
+    const char *who, *name;
+    TileItem it;
+    double bytes, flops;
+    hipStream_t st;
+    template <typename C, typename Epi> heta_status go(const typename Epi::Extra &x) const
+    {
+        TileArgs<Epi> p{1, 0, {it}, {x}};
+        return launch_tiles<C>(who, name, p, bytes, flops, st);
+    }
+    bool direct(size_t elt) const { return direct_rows(it.A, it.lda, elt) && direct_rows(it.B, it.ldb, elt); }
+    bool large() const { return tiles_of(it.M, it.N, 256, 256) * it.n_split >= 128; }
+};
+// f(std::integral_constant<int, a>) for activation a
+template <typename F> inline heta_status with_act(int a, F f)
+{
+    if (a == HETA_ACT_RELU) return f(std::integral_constant<int, HETA_ACT_RELU>{});
+    if (a == HETA_ACT_GELU) return f(std::integral_constant<int, HETA_ACT_GELU>{});
+    if (a == HETA_ACT_SILU) return f(std::integral_constant<int, HETA_ACT_SILU>{});
+    return f(std::integral_constant<int, HETA_ACT_NONE>{});
+}
+// in . W (B_RC = true; the output's activation) or grad . W^T (the slope's activation), and the split in^T . grad
+heta_status launch_linear_f32(const Launch &l, bool input_gradient, const LinearExtra &x);
+heta_status launch_linear_bf16(const Launch &l, bool input_gradient, heta_dtype out_dt, const LinearExtra &x);
+heta_status launch_linear_e4m3(const Launch &l, heta_dtype out_dt, bool coarse, const LinearExtra &x);
+heta_status launch_grad_w_f32(const Launch &l, float *part);
+heta_status launch_grad_w_bf16(const Launch &l, float *part);
+
+// one type's launches from its tile shapes: large tiles, small ones, and those for rows that cannot go straight into LDS
+template <typename Large, typename Small, typename Elements, typename O, bool SLOPES> inline heta_status launch_linear(const Launch &l, size_t elt, const LinearExtra &x)
+{
+    const bool whole = x.vec && l.it.N % 8 == 0;
+    constexpr bool SCALED = Large::EB == 1;
+    if (!l.direct(elt)) return l.go<Elements, LinearEpi<O, false, SCALED>>(x);
+    if (!whole) return l.go<Small, LinearEpi<O, false, SCALED>>(x);
+    if (!l.large()) return l.go<Small, LinearEpi<O, true, SCALED>>(x);
+    return with_act(SLOPES ? x.slope_act : x.act, [&](auto a) {
+        constexpr int A = decltype(a)::value;
+        if constexpr (SLOPES) return l.go<Large, LinearEpi<O, true, SCALED, HETA_ACT_NONE, A, A != HETA_ACT_NONE>>(x);
+        else return x.other ? l.go<Large, LinearEpi<O, true, SCALED, A, HETA_ACT_NONE, true>>(x) : l.go<Large, LinearEpi<O, true, SCALED, A, HETA_ACT_NONE, false>>(x);
+    });
+}
+template <typename Large, typename Small, typename Elements> inline heta_status launch_grad_w(const Launch &l, size_t elt, float *part)
+{
+    auto with = [&](auto whole) {
+        using Epi = PartialEpi<decltype(whole)::value>;
+        const typename Epi::Extra x{part, l.it.N};
+        if (!l.direct(elt)) return l.go<Elements, Epi>(x);
+        return l.large() ? l.go<Large, Epi>(x) : l.go<Small, Epi>(x);
+    };
+    return l.it.N % 4 == 0 ? with(std::true_type{}) : with(std::false_type{});
+}
+
+} // namespace heta

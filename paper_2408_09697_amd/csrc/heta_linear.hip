@@ -9,106 +9,10 @@
 // bf16 behind LDS or, where the caller allows coarser sums, on the 8-bit matrix instruction at twice the rate (block scales 1;
 // the scales of rows and columns come in the epilogue); fp32 operands as three bf16 terms.  grad_W is split over the rows; the partial products are added in a fixed order.
 #include <algorithm>
-#include <cmath>
 
-#include "heta_rows.h"
-#include "heta_tiles.h"
+#include "heta_linear.h"
 
 namespace heta {
-
-// ---- activations: x * sigmoid(z(x)); GELU in its tanh form, 0.5 (1 + tanh(u)) = sigmoid(2 u) --------------------
-constexpr float kGelu2 = 1.5957691216057308f; // 2 sqrt(2 / pi)
-constexpr float kGeluCubic = 0.044715f;
-
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
-
-__device__ __forceinline__ float activate(float x, int act)
-{
-    if (act == HETA_ACT_RELU) return x > 0.f ? x : (x != x ? x : 0.f);
-    const float s = sigmoid(act == HETA_ACT_GELU ? kGelu2 * (x + kGeluCubic * x * x * x) : x);
-    return x < -200.f ? -0.f : x * s; // below, the product is zero in fp32, and -inf * 0 would be NaN
-}
-
-__device__ __forceinline__ float activation_slope(float x, int act)
-{
-    if (act == HETA_ACT_RELU) return x > 0.f ? 1.f : (x != x ? x : 0.f);
-    x = x > 60.f ? 60.f : (x < -60.f ? -60.f : x); // the slope is 1 or 0 there; NaN stays
-    if (act == HETA_ACT_GELU) {
-        const float s = sigmoid(kGelu2 * (x + kGeluCubic * x * x * x));
-        return s + x * s * (1.f - s) * kGelu2 * (1.f + 3.f * kGeluCubic * x * x);
-    }
-    const float s = sigmoid(x);
-    return s + x * s * (1.f - s);
-}
-
-// ---- epilogues ---------------------------------------------------------------------------------------
-struct LinearExtra {
-    const float *bias, *in_scale, *w_scale; // nullable
-    const void *residual, *slope_at;        // nullable; slope_at: the producer's pre-activation, whose slope multiplies
-    void *pre, *out;                        // pre nullable
-    int64_t ld_res, ld_slope, ld_pre, ld_out;
-    int act, slope_act;
-    int vec; // every array that is there can be moved 16 bytes at a time
-};
-template <typename O> struct LinearEpi {
-    static constexpr int kItems = 1;
-    using Extra = LinearExtra;
-    struct Cols {
-        float bias[8], scale[8];
-        __device__ __forceinline__ Cols(const Extra &x, int64_t n, int valid)
-        {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                bias[e] = x.bias && e < valid ? x.bias[n + e] : 0.f;
-                scale[e] = x.w_scale && e < valid ? x.w_scale[n + e] : 1.f;
-            }
-        }
-    };
-    __device__ __forceinline__ static void put(const Extra &x, const TileItem &, const Cols &c, int64_t m, int64_t n, int valid, const float (&v)[8], int)
-    {
-        float y[8], t[8];
-        if (x.in_scale) {
-            const float s = x.in_scale[m];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = v[e] * s * c.scale[e] + c.bias[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = v[e] + c.bias[e];
-        }
-        if (x.pre) store8(static_cast<O *>(x.pre) + m * x.ld_pre + n, valid, x.vec, y);
-        if (x.act != HETA_ACT_NONE) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = activate(y[e], x.act);
-        }
-        if (x.slope_at) {
-            load8(static_cast<const O *>(x.slope_at) + m * x.ld_slope + n, valid, x.vec, t);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] *= activation_slope(t[e], x.slope_act);
-        }
-        if (x.residual) {
-            load8(static_cast<const O *>(x.residual) + m * x.ld_res + n, valid, x.vec, t);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] += t[e];
-        }
-        store8(static_cast<O *>(x.out) + m * x.ld_out + n, valid, x.vec, y);
-    }
-};
-
-// partial products of a contraction that is split over its rows: [split][M][N] fp32
-struct PartialEpi {
-    static constexpr int kItems = 1;
-    struct Extra {
-        float *part;
-        int vec;
-    };
-    struct Cols {
-        __device__ __forceinline__ Cols(const Extra &, int64_t, int) {}
-    };
-    __device__ __forceinline__ static void put(const Extra &x, const TileItem &it, const Cols &, int64_t m, int64_t n, int valid, const float (&v)[8], int split)
-    {
-        store8(x.part + (split * it.M + m) * it.N + n, valid, x.vec, v);
-    }
-};
 
 // ---- sums of partials --------------------------------------------------------------------------------
 // 256 threads: 256 / CH column groups of four, CH chains over the partials each, joined through LDS in order.
@@ -197,8 +101,7 @@ template <typename E> __global__ void __launch_bounds__(256) act_grad_kernel(con
             if (gp) {
                 float x[8];
                 load8(pre + r * ld_pre + c, valid, vec, x);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] *= activation_slope(x[e], act);
+                times_slopes(g, x, act);
                 store8(gp + r * ld_gp + c, valid, vec, g);
             }
 #pragma unroll
@@ -244,51 +147,6 @@ template <typename E> __global__ void __launch_bounds__(256) pack_e4m3_kernel(co
 }
 
 // ---- host side ---------------------------------------------------------------------------------------
-// shapes: BM x BN, k-values per stage, stages
-template <typename S, bool A_RC, bool B_RC> using Bf16Large = TileShape<S, 2, 1, A_RC, B_RC, kDirect, 2, 4, 4, 2, 64, 2, 1>;
-template <typename S, bool A_RC, bool B_RC> using Bf16Small = TileShape<S, 2, 1, A_RC, B_RC, kDirect, 2, 2, 1, 1, 64, 3, 2>;
-template <bool A_RC, bool B_RC> using Bf16Elements = TileShape<bf16_t, 2, 1, A_RC, B_RC, kElements, 2, 2, 2, 2, 32, 2, 1>;
-template <bool A_RC, bool B_RC> using F32Large = TileShape<float, 2, 3, A_RC, B_RC, kStaged, 4, 2, 2, 2, 32, 2, 1>;
-template <bool A_RC, bool B_RC> using F32Small = TileShape<float, 2, 3, A_RC, B_RC, kStaged, 2, 2, 1, 1, 32, 2, 2>;
-template <bool A_RC, bool B_RC> using F32Elements = TileShape<float, 2, 3, A_RC, B_RC, kElements, 2, 2, 1, 1, 32, 2, 2>;
-template <bool WIDEN> using E4m3Large = TileShape<uint8_t, 1, 1, false, false, kDirect, 2, 4, 4, 2, 128, 2, 1, WIDEN>;
-template <bool WIDEN> using E4m3Small = TileShape<uint8_t, 1, 1, false, false, kDirect, 2, 2, 1, 1, 128, 3, 2, WIDEN>;
-template <bool WIDEN> using E4m3Elements = TileShape<uint8_t, 1, 1, false, false, kElements, 2, 2, 2, 2, 64, 2, 1, WIDEN>;
-
-// rows that can go straight into LDS: 16-byte aligned, and a tile's rows within 32-bit offsets
-static bool direct_rows(const void *p, int64_t ld, size_t elt) { return aligned16(p) && (ld * static_cast<int64_t>(elt)) % 16 == 0 && ld * static_cast<int64_t>(elt) < (int64_t(1) << 23); }
-
-static int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return (M + bm - 1) / bm * ((N + bn - 1) / bn); }
-
-template <bool A_RC, bool B_RC, typename Epi>
-static heta_status launch_product(const char *who, const char *name, heta_dtype dt, TileArgs<Epi> &p, double bytes, double flops, hipStream_t st, bool coarse = false)
-{
-    TileItem &it = p.item[0];
-    const size_t esz = dt == HETA_F32 ? 4 : dt == HETA_BF16 ? 2 : 1;
-    const bool direct = direct_rows(it.A, it.lda, esz) && direct_rows(it.B, it.ldb, esz);
-    const bool large = tiles_of(it.M, it.N, 256, 256) * it.n_split >= 128;
-    if (dt == HETA_F32) {
-        if (!direct) return launch_tiles<F32Elements<A_RC, B_RC>>(who, name, p, bytes, flops, st);
-        if (large) return launch_tiles<F32Large<A_RC, B_RC>>(who, name, p, bytes, flops, st);
-        return launch_tiles<F32Small<A_RC, B_RC>>(who, name, p, bytes, flops, st);
-    }
-    if (dt == HETA_BF16) {
-        if (!direct) return launch_tiles<Bf16Elements<A_RC, B_RC>>(who, name, p, bytes, flops, st);
-        if (large) return launch_tiles<Bf16Large<bf16_t, A_RC, B_RC>>(who, name, p, bytes, flops, st);
-        return launch_tiles<Bf16Small<bf16_t, A_RC, B_RC>>(who, name, p, bytes, flops, st);
-    }
-    if constexpr (!A_RC && !B_RC) {
-        auto go = [&](auto widen) {
-            constexpr bool W = decltype(widen)::value;
-            if (!direct) return launch_tiles<E4m3Elements<W>>(who, name, p, bytes, flops, st);
-            if (large) return launch_tiles<E4m3Large<W>>(who, name, p, bytes, flops, st);
-            return launch_tiles<E4m3Small<W>>(who, name, p, bytes, flops, st);
-        };
-        return coarse ? go(std::false_type{}) : go(std::true_type{});
-    }
-    return fail(HETA_ERR_UNSUPPORTED, "%s: no such product of 8-bit operands", who);
-}
-
 static bool valid_act(int a) { return a >= HETA_ACT_NONE && a <= HETA_ACT_SILU; }
 
 static heta_status check_matrix(const char *who, const char *what, const void *p, int64_t rows, int64_t ld, int64_t d, size_t elt)
@@ -331,19 +189,13 @@ extern "C" heta_status heta_linear(heta_graph *, const heta_linear_args *a, void
     if (out.overlaps(in) || out.overlaps(w) || out.overlaps(pre) || pre.overlaps(in) || pre.overlaps(w) || pre.overlaps(res) || (out.overlaps(res) && !same_rows))
         return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);
     if (a->n_rows == 0) return HETA_OK;
-    const LinearExtra x{a->bias, a->in_scale, a->w_scale, a->residual, nullptr, a->pre, a->out, a->ld_res, 0, a->ld_pre, a->ld_out, a->act, HETA_ACT_NONE,
+    const LinearExtra x{a->bias, a->in_scale, a->w_scale, a->residual, a->pre, a->out, a->ld_res, a->ld_pre, a->ld_out, a->act, HETA_ACT_NONE,
                         vec_rows(a->out, a->ld_out, osz) && vec_rows(a->residual, a->ld_res, osz) && vec_rows(a->pre, a->ld_pre, osz)};
-    const TileItem it{a->in, a->W, a->ld_in, a->ld_w, 0, 0, a->n_rows, a->d_out, a->d_in, a->d_in, 1, 0, 0, 0};
     const double bytes = static_cast<double>(a->n_rows) * (a->d_in * esz + a->d_out * osz * (1.0 + !!a->residual + !!a->pre)) + static_cast<double>(a->d_in) * a->d_out * esz;
-    const double flops = 2.0 * a->n_rows * a->d_in * a->d_out;
-    hipStream_t st = as_stream(hip_stream);
-    auto go = [&](auto tag) {
-        using O = decltype(tag);
-        TileArgs<LinearEpi<O>> p{1, {it}, {x}};
-        return q ? launch_product<false, false>(who, "linear_kernel", a->in_dt, p, bytes, flops, st, a->coarse_sums != 0)
-                 : launch_product<false, true>(who, "linear_kernel", a->in_dt, p, bytes, flops, st);
-    };
-    return a->out_dt == HETA_F32 ? go(float{}) : go(bf16_t{});
+    const Launch l{who, "linear_kernel", TileItem{a->in, a->W, a->ld_in, a->ld_w, 0, 0, a->n_rows, a->d_out, a->d_in, a->d_in, 1, 0, 0, 0, 0}, bytes,
+                   2.0 * a->n_rows * a->d_in * a->d_out, as_stream(hip_stream)};
+    if (q) return launch_linear_e4m3(l, a->out_dt, a->coarse_sums != 0, x);
+    return a->in_dt == HETA_F32 ? launch_linear_f32(l, false, x) : launch_linear_bf16(l, false, a->out_dt, x);
 }
 
 extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args *a, void *hip_stream)
@@ -428,25 +280,19 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
 
     const double flops = 2.0 * n * a->d_in * a->d_out;
     if (a->grad_in && n > 0) {
-        const LinearExtra x{nullptr, nullptr, nullptr, nullptr, fused ? a->in_pre : nullptr, nullptr, a->grad_in, 0, a->ld_ip, 0, a->ld_gi, HETA_ACT_NONE, a->in_act,
+        const LinearExtra x{nullptr, nullptr, nullptr, fused ? a->in_pre : nullptr, nullptr, a->grad_in, a->ld_ip, 0, a->ld_gi, HETA_ACT_NONE, a->in_act,
                             vec_rows(a->grad_in, a->ld_gi, esz) && (!fused || vec_rows(a->in_pre, a->ld_ip, esz))};
-        const TileItem it{gpre, a->W, ld_gpre, a->ld_w, 0, 0, n, a->d_in, a->d_out, a->d_out, 1, 0, 0, 0};
         const double bytes = (static_cast<double>(n) * (a->d_in * (fused ? 2 : 1) + a->d_out) + static_cast<double>(a->d_in) * a->d_out) * esz;
-        if (a->dt == HETA_F32) {
-            TileArgs<LinearEpi<float>> p{1, {it}, {x}};
-            HETA_TRY((launch_product<false, false>(who, "linear_grad_in_kernel", a->dt, p, bytes, flops, st)));
-        } else {
-            TileArgs<LinearEpi<bf16_t>> p{1, {it}, {x}};
-            HETA_TRY((launch_product<false, false>(who, "linear_grad_in_kernel", a->dt, p, bytes, flops, st)));
-        }
+        const Launch l{who, "linear_grad_in_kernel", TileItem{gpre, a->W, ld_gpre, a->ld_w, 0, 0, n, a->d_in, a->d_out, a->d_out, 1, 0, 0, 0, 0}, bytes, flops, st};
+        HETA_TRY(a->dt == HETA_F32 ? launch_linear_f32(l, true, x) : launch_linear_bf16(l, true, HETA_BF16, x));
     }
     if (a->dW) {
         float *part = ws + bias_off;
         if (n > 0) {
-            TileArgs<PartialEpi> p{1, {TileItem{a->in, gpre, a->ld_in, ld_gpre, 0, 0, a->d_in, a->d_out, n, k_per_split, static_cast<int32_t>(n_split), 0, 0, 0}},
-                                   {PartialEpi::Extra{part, a->d_out % 4 == 0}}};
-            const double bytes = static_cast<double>(n) * (a->d_in + a->d_out) * esz + 4.0 * w_elems;
-            HETA_TRY((launch_product<true, true>(who, "linear_grad_w_kernel", a->dt, p, bytes, flops, st)));
+            const Launch l{who, "linear_grad_w_kernel",
+                           TileItem{a->in, gpre, a->ld_in, ld_gpre, 0, 0, a->d_in, a->d_out, n, k_per_split, static_cast<int32_t>(n_split), 0, 0, 0, 0},
+                           static_cast<double>(n) * (a->d_in + a->d_out) * esz + 4.0 * w_elems, flops, st};
+            HETA_TRY(a->dt == HETA_F32 ? launch_grad_w_f32(l, part) : launch_grad_w_bf16(l, part));
         }
         HETA_TRY(fold_partials(part, n_split, static_cast<int64_t>(a->d_in) * a->d_out, a->dW, a->dw_dt, a->d_out, a->ld_dw, st));
     }

@@ -162,13 +162,12 @@ struct TermsExtra {
 };
 template <int T> struct TermsEpi {
     static constexpr int kItems = kMuonItems;
+    static constexpr bool kStrip = false;
+    using Out = bf16_t;
     struct Extra : TermsExtra {
         float alpha, beta;
     };
-    struct Cols {
-        __device__ __forceinline__ Cols(const Extra &, int64_t, int) {}
-    };
-    __device__ __forceinline__ static void put(const Extra &x, const TileItem &, const Cols &, int64_t m, int64_t n, int valid, const float (&v)[8], int)
+    __device__ __forceinline__ static void put(const Extra &x, const TileItem &, int64_t m, int64_t n, int valid, const float (&v)[8], int)
     {
         float y[8];
 #pragma unroll
@@ -295,9 +294,9 @@ static heta_status muon_group(const char *who, heta_graph *g, const std::vector<
             const MuonPlan &pl = plan[i];
             char *x = ws + pl.x[s & 1], *y = ws + pl.x[(s & 1) ^ 1], *A = ws + pl.gram, *P = ws + pl.poly;
             auto terms = [](char *p) { return reinterpret_cast<bf16_t *>(p); };
-            gram.item[i] = TileItem{x, x, pl.ld_x, pl.ld_x, pl.x_plane * 2, pl.x_plane * 2, pl.k, pl.k, pl.l, pl.l, 1, 0, 0, 0};
-            poly.item[i] = TileItem{A, A, pl.ld_g, pl.ld_g, pl.g_plane * 2, pl.g_plane * 2, pl.k, pl.k, pl.k, pl.k, 1, 0, 0, 0};
-            apply.item[i] = TileItem{P, x, pl.ld_g, pl.ld_x, pl.g_plane * 2, pl.x_plane * 2, pl.k, pl.l, pl.k, pl.k, 1, 0, 0, 0};
+            gram.item[i] = TileItem{x, x, pl.ld_x, pl.ld_x, pl.x_plane * 2, pl.x_plane * 2, pl.k, pl.k, pl.l, pl.l, 1, 0, 0, 0, 0};
+            poly.item[i] = TileItem{A, A, pl.ld_g, pl.ld_g, pl.g_plane * 2, pl.g_plane * 2, pl.k, pl.k, pl.k, pl.k, 1, 0, 0, 0, 0};
+            apply.item[i] = TileItem{P, x, pl.ld_g, pl.ld_x, pl.g_plane * 2, pl.x_plane * 2, pl.k, pl.l, pl.k, pl.k, 1, 0, 0, 0, 0};
             gram.extra[i] = {{nullptr, terms(A), 0, 0, pl.ld_g, pl.g_plane}, 1.f, 0.f};
             poly.extra[i] = {{terms(A), terms(P), pl.ld_g, pl.g_plane, pl.ld_g, pl.g_plane}, kNsC, kNsB};
             apply.extra[i] = {{terms(x), terms(y), pl.ld_x, pl.x_plane, pl.ld_x, pl.x_plane}, 1.f, kNsA};

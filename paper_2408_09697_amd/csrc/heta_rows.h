@@ -53,7 +53,7 @@ __device__ __forceinline__ void store8(bf16_t *p, int valid, bool vec, const flo
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        if (e < valid) p[e] = to_bf16(v[e]);
+        if (e < valid) p[e] = static_cast<bf16_t>(pack2_bf16(v[e], v[e]) & 0xffffu);
 }
 
 // rows of `ld` elements from p on that can be moved 16 bytes at a time (a null pointer can: it is not read)

@@ -8,14 +8,17 @@
 //   transposing LDS read, so neither operand of any product is ever transposed in memory.
 // It gets there straight from memory (kDirect: 16-byte aligned rows of the image's own type, T planes side by side in
 // memory) or through registers (kStaged / kElements: any storage type and alignment; fp32 is split into its three terms
-// there, once per workgroup, not by every wavefront that reads the tile).  A last tile with fewer k-values always takes
-// the way through registers, which fills up with zeros: the loop itself knows no ragged tile.
+// there, once per workgroup, not by every wavefront that reads the tile).  A last k-tile with fewer k-values is filled up
+// with zeros in LDS: fragments and products know no ragged tile.
 //
-// The product is formed as (B^T A^T): a lane's accumulator registers then hold consecutive COLUMNS of C, four at a time,
-// and the epilogue's pass through LDS takes 128-bit stores; it reads the strip back with eight consecutive columns per
-// lane, so that bias, residual and output move 16 bytes (bf16) or 32 (fp32) per lane and whole cache lines per row.
+// The product is formed as (B^T A^T): a lane's accumulator registers then hold consecutive COLUMNS of C, four at a time, and go
+// through a strip of LDS, one 32 x 32 block per wavefront at a time, in 128-bit accesses; read back by rows, a lane has 16
+// bytes of consecutive outputs, and memory sees 64 or 128 bytes of a row at a time, also for what the epilogue reads in the
+// output's shape.  Stored from the registers as they lie, 32 bytes of 32 rows, products of 700,000 x 1,024 x 256 and 700,000 x 256 x 1,024
+// took 477 and 622 us, with the columns in the outer loop 593 and 738, against 435 and 564 through strips.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "heta_gemm.h"
@@ -84,6 +87,43 @@ template <bool RC, int ROWS, int BK, int EB, int NW, int T> struct PlaneLoader {
 #pragma unroll
             for (int i = 0; i < NI; ++i) load_chunk_to_lds(tile + t * plane, off[i], lds + t * Img::BYTES + slot(i, wave) * 1024);
         tile += step;
+    }
+    // the last k-tile of a contraction, with only kv of its k-values: nothing beyond them is read (chunks or rows are clamped
+    // to the last that holds one), and clear_tail() has to follow when the tile is there
+    __device__ __forceinline__ void issue_tail(uint32_t lds, int wave, int lane, int kv, int64_t ld, int64_t r0, int64_t r_total)
+    {
+        const uint32_t ld_bytes = static_cast<uint32_t>(ld * EB);
+        const int64_t room = RC ? (r_total - r0 + Img::E - 1) / Img::E : r_total - r0;
+        const int last = static_cast<int>(min(room, static_cast<int64_t>(RC ? Img::CPR : ROWS))) - 1;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int q = slot(i, wave) * 64 + lane, row = q / Img::CPR, chunk = Img::chunk_at(q);
+            const uint32_t o = RC ? static_cast<uint32_t>(min(row, kv - 1)) * ld_bytes + static_cast<uint32_t>(min(chunk, last)) * 16u
+                                  : static_cast<uint32_t>(min(row, last)) * ld_bytes + static_cast<uint32_t>(min(chunk, (kv - 1) / Img::E)) * 16u;
+#pragma unroll
+            for (int t = 0; t < T; ++t) load_chunk_to_lds(tile + t * plane, o, lds + t * Img::BYTES + slot(i, wave) * 1024);
+        }
+    }
+    // zeroes what lies in the k-values from kv on
+    __device__ __forceinline__ static void clear_tail(char *lds, int tid, int kv)
+    {
+        for (int q = tid; q < T * Img::CHUNKS; q += 64 * NW) {
+            const int in = q % Img::CHUNKS, k = RC ? in / Img::CPR : Img::chunk_at(in) * Img::E; // its (first) k-value
+            uint4 *p = reinterpret_cast<uint4 *>(lds) + q;
+            if (k >= kv) {
+                *p = make_uint4(0u, 0u, 0u, 0u);
+            } else if (!RC && k + Img::E > kv) {
+                uint4 u = *p;
+                uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                const int bytes = (kv - k) * EB; // valid bytes of the chunk
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int b = bytes - 4 * j;
+                    w[j] = b >= 4 ? w[j] : b <= 0 ? 0u : w[j] & ((1u << (8 * b)) - 1u);
+                }
+                *p = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
     }
 };
 
@@ -188,24 +228,80 @@ __device__ __forceinline__ bf16x8 widen_e4m3(uint32_t lo, uint32_t hi)
     return f.v;
 }
 
+template <int EB, int T, int MI, int NJ> struct Fragments { // of one step
+    using F = std::conditional_t<EB == 1, Frag8, Frag16>;
+    F a[MI][T], b[NJ][T];
+};
+
+// 16 bytes of outputs from fp32, and back
+template <typename O> __device__ __forceinline__ uint4 pack16(const float (&y)[16 / sizeof(O)])
+{
+    if constexpr (sizeof(O) == 2) return make_uint4(pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3]), pack2_bf16(y[4], y[5]), pack2_bf16(y[6], y[7]));
+    else return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+}
+template <typename O> __device__ __forceinline__ void unpack16(uint4 raw, float (&y)[16 / sizeof(O)])
+{
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(O) == 2) {
+            y[2 * j] = __uint_as_float(w[j] << 16);
+            y[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        } else {
+            y[j] = __uint_as_float(w[j]);
+        }
+    }
+}
+
 // ---- items of a launch ------------------------------------------------------------------------------
-struct TileItem {
+struct TileItem { // M, N, K > 0
     const void *A, *B;
     int64_t lda, ldb;          // elements
     int64_t a_plane, b_plane;  // bytes from term to term (kDirect, T > 1)
     int64_t M, N, K;
     int64_t k_per_split;       // multiple of BK; n_split * k_per_split >= K
-    int32_t n_split;
+    int32_t n_split;           // every split has k-values
     int32_t mt, nt;            // tiles
-    uint32_t block0;           // first workgroup (multiple of 8)
+    uint32_t block0, places;   // first workgroup (multiple of 8), places of the item's tiles
 };
 
-// Epi: struct with `static constexpr int kItems`, `Extra` (what an item's epilogue needs) and
-//   struct Cols { __device__ Cols(const Extra &x, int64_t n, int valid); }    what a lane keeps of its eight columns n, n + 1, ...
-//   __device__ static void put(const Extra &x, const TileItem &it, const Cols &c, int64_t m, int64_t n, int valid, const float (&v)[8], int split)
-// for those columns (valid: as many of them as the matrix has) of row m < M.
+// A place in the order of an item's output tiles, and the tile there.  Place -> (XCD, position in its queue) -> tile:
+// workgroups go round-robin to the 8 XCDs, and the tiles that share operand rows (the column tiles of a row block, all tiles
+// of a split) follow one another on one of them.
+struct TilePlace {
+    uint32_t at;
+    int64_t m0, n0, k0;
+    int kn, split;
+    // the first place from `at` on, `stride` apart, that has a tile
+    __device__ __forceinline__ bool seek(const TileItem &it, uint32_t stride, int bm, int bn)
+    {
+        const bool splits = it.n_split > 1;
+        const uint32_t inner = splits ? static_cast<uint32_t>(it.nt) * it.mt : static_cast<uint32_t>(it.nt), n_outer = static_cast<uint32_t>(splits ? it.n_split : it.mt);
+        for (; at < it.places; at += stride) {
+            const uint32_t j = at / 8, in = j % inner, outer = j / inner * 8 + at % 8;
+            if (outer >= n_outer) continue;
+            split = splits ? static_cast<int>(outer) : 0;
+            m0 = static_cast<int64_t>(splits ? in / it.nt : outer) * bm;
+            n0 = static_cast<int64_t>(splits ? in % it.nt : in) * bn;
+            k0 = split * it.k_per_split;
+            kn = static_cast<int>(min(it.K - k0, it.k_per_split));
+            return true;
+        }
+        return false;
+    }
+};
+
+// Epi: what becomes of the product; all functions are device functions.
+//   kItems, Extra: items of a launch at most, and what an item's epilogue needs
+//   kStrip = false: put(x, it, m, n, valid, v, split) takes eight columns n, n + 1, ... of row m < M (valid: as many as there are)
+//   kStrip = true (Out rows of whole, aligned 16-byte pieces): with W = 16 bytes of columns, first(cols, row, y) makes
+//     pre-activations of W sums and second(x, y, t) results, t being W elements of x.other (if kReads; zeros or nothing where it
+//     is null); x.pre (if kPre and not null) and out(x, it, split) receive them, rows x.ld_pre and x.ld_out apart.
+//     struct Cols, Row { void load(const Extra &x, int64_t n, int64_t N); } are what a lane keeps of W columns and of a row (which
+//     may lie beyond the matrix).
 template <typename Epi> struct TileArgs {
     int n_items;
+    uint32_t stride; // from one tile of a workgroup to its next
     TileItem item[Epi::kItems];
     typename Epi::Extra extra[Epi::kItems];
 };
@@ -231,83 +327,82 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
     using ImgA = TileImage<C::A_RC, BM, BK, EB>;
     using ImgB = TileImage<C::B_RC, BN, BK, EB>;
     constexpr int A_STAGE = ImgA::BYTES * T, STAGE = A_STAGE + ImgB::BYTES * T;
-    constexpr int EW = 32 * NJ, PITCH = EW + 4; // epilogue strip: 32 rows of a wavefront's columns; rows 16 bytes further on the banks
-    constexpr int STRIPS = NW * 32 * PITCH * 4;
-    __shared__ __attribute__((aligned(1024))) char ring[ST * STAGE > STRIPS ? ST * STAGE : STRIPS];
+    // epilogue strips: one 32 x 32 block of sums per wavefront, its own; behind the ring where that is filled during the epilogue
+    constexpr int STRIPS = Epi::kStrip ? NW * 4096 : 0, STRIPS_AT = DIRECT ? ST * STAGE : 0;
+    __shared__ __attribute__((aligned(1024))) char ring[std::max(ST * STAGE, STRIPS_AT + STRIPS)];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = (wave / C::WN) * (32 * MI), wn = (wave % C::WN) * (32 * NJ);
 
-    // workgroup -> item -> (XCD, position in its queue) -> tile: workgroups go round-robin to the 8 XCDs, and the tiles that
-    // share operand rows (the column tiles of a row block, all tiles of a split) follow one another on one of them
     int c = 0;
-    while (c + 1 < p.n_items && blockIdx.x >= p.item[c + 1].block0) ++c; // uniform
-    const TileItem &it = p.item[c];
-    const uint32_t b = blockIdx.x - it.block0, xcd = b % 8, j = b / 8;
-    const uint32_t inner = it.n_split > 1 ? static_cast<uint32_t>(it.nt) * it.mt : static_cast<uint32_t>(it.nt);
-    const uint32_t in = j % inner, outer = j / inner * 8 + xcd;
-    if (outer >= static_cast<uint32_t>(it.n_split > 1 ? it.n_split : it.mt)) return;
-    const int split = it.n_split > 1 ? static_cast<int>(outer) : 0;
-    const int64_t m0 = static_cast<int64_t>(it.n_split > 1 ? in / it.nt : outer) * BM, n0 = static_cast<int64_t>(it.n_split > 1 ? in % it.nt : in) * BN;
-    const int64_t k0 = split * it.k_per_split, k_end = min(it.K, k0 + it.k_per_split);
-    const int kn = static_cast<int>(max(k_end - k0, static_cast<int64_t>(0)));
+    if constexpr (Epi::kItems > 1)
+        while (c + 1 < p.n_items && blockIdx.x >= p.item[c + 1].block0) ++c; // uniform
+    const TileItem it = p.item[c];
+    const typename Epi::Extra extra = p.extra[c];
+    TilePlace now;
+    now.at = blockIdx.x - it.block0;
+    if (!now.seek(it, p.stride, BM, BN)) return;
 
     floatx16 acc[MI][NJ];
+    auto clear = [&] {
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int jj = 0; jj < NJ; ++jj)
+            for (int jj = 0; jj < NJ; ++jj)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][jj][v] = 0.f;
+                for (int v = 0; v < 16; ++v) acc[i][jj][v] = 0.f;
+    };
 
+    // One k-tile.  The fragments of a step are read before the products of the step in front of it, and scheduling barriers
+    // keep them there: left to itself the compiler reads a fragment just before its first product, and every step waits for LDS.
     auto compute = [&](const char *stage) {
         const char *At = stage, *Bt = stage + A_STAGE;
-        if constexpr (EB == 1) {
-#pragma unroll
-            for (int kk = 0; kk < BK; kk += 64) {
+        constexpr int KS = EB == 1 ? 64 : 16, STEPS = BK / KS;
+        constexpr int SETS = EB == 1 ? 1 : 2; // two sets of 8-bit fragments do not fit beside the accumulators
+        Fragments<EB, T, MI, NJ> f[SETS];
+        auto read = [&](Fragments<EB, T, MI, NJ> &to, int kk) {
+            if constexpr (EB == 1) {
                 // which 32 (or 8) of the k-values a lane feeds to an instruction does not matter as long as both operands agree
-                Frag8 fa[MI], fb[NJ];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                    for (int jj = 0; jj < NJ; ++jj) fb[jj].u[h] = tile_chunk8<BN, BK>(Bt, wn + 32 * jj, kk + 32 * h, lane);
+                    for (int jj = 0; jj < NJ; ++jj) to.b[jj][0].u[h] = tile_chunk8<BN, BK>(Bt, wn + 32 * jj, kk + 32 * h, lane);
 #pragma unroll
-                    for (int i = 0; i < MI; ++i) fa[i].u[h] = tile_chunk8<BM, BK>(At, wm + 32 * i, kk + 32 * h, lane);
+                    for (int i = 0; i < MI; ++i) to.a[i][0].u[h] = tile_chunk8<BM, BK>(At, wm + 32 * i, kk + 32 * h, lane);
                 }
-                if constexpr (C::WIDEN) {
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        bf16x8 wb[NJ];
-#pragma unroll
-                        for (int jj = 0; jj < NJ; ++jj) wb[jj] = widen_e4m3(fb[jj].v[2 * h], fb[jj].v[2 * h + 1]);
-#pragma unroll
-                        for (int i = 0; i < MI; ++i) {
-                            const bf16x8 wa = widen_e4m3(fa[i].v[2 * h], fa[i].v[2 * h + 1]);
-#pragma unroll
-                            for (int jj = 0; jj < NJ; ++jj) acc[i][jj] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[jj], wa, acc[i][jj], 0, 0, 0);
-                        }
-                    }
-                } else {
-                    constexpr int kOne = 0x7f7f7f7f; // block scales of 2^0
-#pragma unroll
-                    for (int i = 0; i < MI; ++i)
-#pragma unroll
-                        for (int jj = 0; jj < NJ; ++jj)
-                            acc[i][jj] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[jj].v, fa[i].v, acc[i][jj], 0, 0, 0, kOne, 0, kOne);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int kk = 0; kk < BK; kk += 16) {
-                Frag16 fa[MI][T], fb[NJ][T];
+            } else {
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
 #pragma unroll
-                    for (int jj = 0; jj < NJ; ++jj) fb[jj][t].u = tile_frag16<C::B_RC, BN, BK>(Bt + t * ImgB::BYTES, wn + 32 * jj, kk, lane);
+                    for (int jj = 0; jj < NJ; ++jj) to.b[jj][t].u = tile_frag16<C::B_RC, BN, BK>(Bt + t * ImgB::BYTES, wn + 32 * jj, kk, lane);
 #pragma unroll
-                    for (int i = 0; i < MI; ++i) fa[i][t].u = tile_frag16<C::A_RC, BM, BK>(At + t * ImgA::BYTES, wm + 32 * i, kk, lane);
+                    for (int i = 0; i < MI; ++i) to.a[i][t].u = tile_frag16<C::A_RC, BM, BK>(At + t * ImgA::BYTES, wm + 32 * i, kk, lane);
                 }
+            }
+        };
+        auto multiply = [&](const Fragments<EB, T, MI, NJ> &x) {
+            if constexpr (EB == 1 && C::WIDEN) {
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    bf16x8 wb[NJ];
+#pragma unroll
+                    for (int jj = 0; jj < NJ; ++jj) wb[jj] = widen_e4m3(x.b[jj][0].v[2 * h], x.b[jj][0].v[2 * h + 1]);
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) {
+                        const bf16x8 wa = widen_e4m3(x.a[i][0].v[2 * h], x.a[i][0].v[2 * h + 1]);
+#pragma unroll
+                        for (int jj = 0; jj < NJ; ++jj) acc[i][jj] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[jj], wa, acc[i][jj], 0, 0, 0);
+                    }
+                }
+            } else if constexpr (EB == 1) {
+                constexpr int kOne = 0x7f7f7f7f; // block scales of 2^0
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int jj = 0; jj < NJ; ++jj)
+                        acc[i][jj] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x.b[jj][0].v, x.a[i][0].v, acc[i][jj], 0, 0, 0, kOne, 0, kOne);
+            } else {
                 // leading terms first; those whose weights add up to less than the third term's are left out
 #pragma unroll
                 for (int order = 0; order < T; ++order)
@@ -320,118 +415,231 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
                             for (int i = 0; i < MI; ++i)
 #pragma unroll
                                 for (int jj = 0; jj < NJ; ++jj)
-                                    acc[i][jj] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[jj][tb].v, fa[i][ta].v, acc[i][jj], 0, 0, 0);
+                                    acc[i][jj] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.b[jj][tb].v, x.a[i][ta].v, acc[i][jj], 0, 0, 0);
                         }
+            }
+        };
+        read(f[0], 0);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            if (SETS == 2 && s + 1 < STEPS) read(f[(s + 1) % SETS], (s + 1) * KS);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            multiply(f[s % SETS]);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (SETS == 1 && s + 1 < STEPS) read(f[0], (s + 1) * KS);
+        }
+    };
+
+    // register 4 q + e of block (i, jj) is column 8 q + 4 (lane / 32) + e of row lane % 32
+    const int half = lane >> 5, l32 = lane & 31;
+    auto epilogue = [&] {
+        if constexpr (Epi::kStrip) {
+            using O = typename Epi::Out;
+            constexpr int W = 16 / (int)sizeof(O);                        // columns of a lane: 16 bytes of the output
+            constexpr int LPR = 32 / W, RPP = 64 / LPR, ROUNDS = 32 / RPP; // lanes per row of a block, rows per access, accesses
+            float *strip = reinterpret_cast<float *>(ring + STRIPS_AT + wave * 4096);
+            auto at = [&](int row, int chunk) { return reinterpret_cast<float4 *>(strip + row * 32 + ((chunk ^ (row & 7)) * 4)); };
+            const int sr = lane / LPR, sc = lane % LPR;
+            const int64_t rm = now.m0 + wm + sr, rn = now.n0 + wn + sc * W;
+            // What the epilogue reads in the output's shape comes a row of blocks ahead, and what belongs to columns and rows before all of it:
+            // a load waits for every store that was issued before it.
+            uint4 other[Epi::kReads ? 2 : 1][NJ][ROUNDS];
+            auto fetch = [&](int i) {
+                if constexpr (Epi::kReads)
+                    if (extra.other) {
+#pragma unroll
+                        for (int jj = 0; jj < NJ; ++jj)
+#pragma unroll
+                            for (int r = 0; r < ROUNDS; ++r) {
+                                const int64_t m = rm + 32 * i + RPP * r, n = rn + 32 * jj;
+                                other[i & 1][jj][r] = make_uint4(0u, 0u, 0u, 0u);
+                                if (m < it.M && n < it.N) other[i & 1][jj][r] = *reinterpret_cast<const uint4 *>(static_cast<const O *>(extra.other) + m * extra.ld_other + n);
+                            }
+                    }
+            };
+            typename Epi::Cols cols[NJ];
+#pragma unroll
+            for (int jj = 0; jj < NJ; ++jj) cols[jj].load(extra, rn + 32 * jj, it.N);
+            typename Epi::Row rows[MI][ROUNDS];
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int r = 0; r < ROUNDS; ++r) rows[i][r].load(extra, rm + 32 * i + RPP * r, it.M);
+            fetch(0);
+            O *const out = Epi::out(extra, it, now.split);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                if (i + 1 < MI) fetch(i + 1);
+#pragma unroll
+                for (int jj = 0; jj < NJ; ++jj) {
+                    const int64_t n = rn + 32 * jj;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *at(l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
+#pragma unroll
+                    for (int r = 0; r < ROUNDS; ++r) {
+                        const int64_t m = rm + 32 * i + RPP * r;
+                        float y[W];
+#pragma unroll
+                        for (int h = 0; h < W / 4; ++h) {
+                            const float4 f = *at(RPP * r + sr, sc * (W / 4) + h);
+                            y[4 * h] = f.x; y[4 * h + 1] = f.y; y[4 * h + 2] = f.z; y[4 * h + 3] = f.w;
+                        }
+                        if (m >= it.M || n >= it.N) continue;
+                        Epi::first(cols[jj], rows[i][r], y);
+                        if constexpr (Epi::kPre)
+                            if (extra.pre) *reinterpret_cast<uint4 *>(static_cast<O *>(extra.pre) + m * extra.ld_pre + n) = pack16<O>(y);
+                        float t[W];
+                        if constexpr (Epi::kReads) unpack16<O>(other[i & 1][jj][r], t);
+                        Epi::second(extra, y, t);
+                        *reinterpret_cast<uint4 *>(out + m * extra.ld_out + n) = pack16<O>(y);
+                    }
+                }
+            }
+        } else {
+            // Exchanging the upper half of the lanes of register group q with the lower half of group q + 1 leaves a lane with
+            // eight consecutive columns: 16 u + 8 (lane / 32) + 0..7 of the wavefront's part
+            const int64_t nb = now.n0 + wn + 8 * half;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int64_t m = now.m0 + wm + 32 * i + l32;
+#pragma unroll
+                for (int u = 0; u < 2 * NJ; ++u) {
+                    const int64_t n = nb + 16 * u;
+                    const int valid = static_cast<int>(min(it.N - n, static_cast<int64_t>(8)));
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][u / 2][8 * (u & 1) + e]), __float_as_uint(acc[i][u / 2][8 * (u & 1) + 4 + e]), false, false);
+                        v[e] = __uint_as_float(r[0]);
+                        v[4 + e] = __uint_as_float(r[1]);
+                    }
+                    if (m < it.M && valid > 0) Epi::put(extra, it, m, n, valid, v, now.split);
+                }
             }
         }
     };
 
     if constexpr (DIRECT) {
+        // One stream of k-tiles through the ring over all output tiles of the workgroup: the first k-tiles of the next output
+        // tile are on their way while this one's epilogue runs.
         using LA = PlaneLoader<C::A_RC, BM, BK, EB, NW, T>;
         using LB = PlaneLoader<C::B_RC, BN, BK, EB, NW, T>;
         constexpr int LOADS = LA::LOADS + LB::LOADS;
         static_assert((ST - 2) * LOADS < 64, "the wait counter has 6 bits");
         LA la;
         LB lb;
-        la.init(it.A, it.lda, it.a_plane, m0, it.M, k0, wave, lane);
-        lb.init(it.B, it.ldb, it.b_plane, n0, it.N, k0, wave, lane);
-        const int full = kn / BK, tail = kn % BK, tiles = full + (tail ? 1 : 0);
         const uint32_t lds0 = lds_address(ring);
-#pragma unroll
-        for (int s = 0; s < ST - 1; ++s)
-            if (s < full) {
+        TilePlace ahead = now; // the output tile whose k-tiles are being loaded
+        int left = 0;          // k-values of it that are still to be loaded
+        bool more = true;
+        int known = 0, flying = 0; // k-tiles ahead of the current one: those known to be there, those issued
+        auto aim = [&] {
+            la.init(it.A, it.lda, it.a_plane, ahead.m0, it.M, ahead.k0, wave, lane);
+            lb.init(it.B, it.ldb, it.b_plane, ahead.n0, it.N, ahead.k0, wave, lane);
+            left = ahead.kn;
+        };
+        auto issue = [&](int s) { // the next k-tile of the stream, if there is one, into stage s
+            if (left <= 0) {
+                if (!more) return;
+                ahead.at += p.stride;
+                more = ahead.seek(it, p.stride, BM, BN);
+                if (!more) return;
+                aim();
+            }
+            if (left >= BK) {
                 la.issue(lds0 + s * STAGE, wave);
                 lb.issue(lds0 + s * STAGE + A_STAGE, wave);
+            } else {
+                la.issue_tail(lds0 + s * STAGE, wave, lane, left, it.lda, ahead.m0, it.M);
+                lb.issue_tail(lds0 + s * STAGE + A_STAGE, wave, lane, left, it.ldb, ahead.n0, it.N);
             }
+            left -= BK;
+            ++flying;
+        };
+        aim();
+#pragma unroll
+        for (int s = 0; s < ST - 1; ++s) issue(s);
         int cur = 0;
-        for (int t = 0; t < tiles; ++t) {
-            if (t + ST - 2 < full) wait_counters<(ST - 2) * LOADS, true>(); // tile t is there; this wavefront's reads of tile t - 1 too
-            else wait_counters<0, true>();
-            if (t >= full) { // the last, shorter tile
-                StagedLoader<S, C::A_RC, BM, BK, EB, NT, 1, true> sa;
-                StagedLoader<S, C::B_RC, BN, BK, EB, NT, 1, true> sb;
-#pragma unroll
-                for (int q = 0; q < T; ++q) {
-                    sa.load(reinterpret_cast<const S *>(static_cast<const char *>(it.A) + q * it.a_plane), it.lda, m0, it.M, k0 + full * BK, k_end, tid);
-                    sb.load(reinterpret_cast<const S *>(static_cast<const char *>(it.B) + q * it.b_plane), it.ldb, n0, it.N, k0 + full * BK, k_end, tid);
-                    sa.store(ring + cur * STAGE + q * ImgA::BYTES, tid);
-                    sb.store(ring + cur * STAGE + A_STAGE + q * ImgB::BYTES, tid);
+        while (true) {
+            clear();
+            for (int kv = now.kn; kv > 0; kv -= BK) {
+                // this wavefront's part of the k-tile is there, and its fragment reads of the last one are done
+                if (known > 0) {
+                    --known;
+                    wait_counters<63, true>();
+                } else if (flying >= ST - 1) {
+                    wait_counters<(ST - 2) * LOADS, true>();
+                } else {
+                    wait_counters<0, true>();
                 }
-                wait_counters<0, true>();
+                --flying;
+                barrier_no_drain();
+                if (kv < BK) {
+                    LA::clear_tail(ring + cur * STAGE, tid, kv);
+                    LB::clear_tail(ring + cur * STAGE + A_STAGE, tid, kv);
+                    wait_counters<63, true>();
+                    barrier_no_drain();
+                }
+                issue(cur == 0 ? ST - 1 : cur - 1); // every wavefront is done with the stage of the k-tile before this one
+                compute(ring + cur * STAGE);
+                cur = cur + 1 == ST ? 0 : cur + 1;
             }
-            barrier_no_drain();
-            if (t + ST - 1 < full) {
-                const int s = cur == 0 ? ST - 1 : cur - 1; // (t + ST - 1) % ST
-                la.issue(lds0 + s * STAGE, wave);
-                lb.issue(lds0 + s * STAGE + A_STAGE, wave);
+            // The k-tiles ahead are awaited here, not behind the epilogue's stores (the counter runs in order): they were
+            // issued before the last k-tile's products.
+            TilePlace next = now;
+            next.at += p.stride;
+            const bool again = next.seek(it, p.stride, BM, BN);
+            if (again) {
+                wait_counters<0, false>();
+                known = flying;
             }
-            compute(ring + cur * STAGE);
-            cur = cur + 1 == ST ? 0 : cur + 1;
+            epilogue();
+            if (!again) break;
+            now = next;
         }
     } else {
         StagedLoader<S, C::A_RC, BM, BK, EB, NT, T, VEC> sa;
         StagedLoader<S, C::B_RC, BN, BK, EB, NT, T, VEC> sb;
         const S *A = static_cast<const S *>(it.A), *B = static_cast<const S *>(it.B);
-        const int tiles = (kn + BK - 1) / BK;
-        if (tiles > 0) {
-            sa.load(A, it.lda, m0, it.M, k0, k_end, tid);
-            sb.load(B, it.ldb, n0, it.N, k0, k_end, tid);
+        do {
+            const int64_t k_end = now.k0 + now.kn;
+            const int tiles = (now.kn + BK - 1) / BK;
+            clear();
+            sa.load(A, it.lda, now.m0, it.M, now.k0, k_end, tid);
+            sb.load(B, it.ldb, now.n0, it.N, now.k0, k_end, tid);
             sa.store(ring, tid);
             sb.store(ring + A_STAGE, tid);
-        }
-        wait_counters<0, true>();
-        barrier_no_drain();
-        for (int t = 0; t < tiles; ++t) {
-            const bool more = t + 1 < tiles;
-            if (more) {
-                sa.load(A, it.lda, m0, it.M, k0 + static_cast<int64_t>(t + 1) * BK, k_end, tid);
-                sb.load(B, it.ldb, n0, it.N, k0 + static_cast<int64_t>(t + 1) * BK, k_end, tid);
-            }
-            compute(ring + (t & 1) * STAGE);
-            if (more) {
-                char *next = ring + ((t + 1) & 1) * STAGE;
-                sa.store(next, tid);
-                sb.store(next + A_STAGE, tid);
-            }
             wait_counters<63, true>();
             barrier_no_drain();
-        }
-    }
-    wait_counters<0, true>();
-    barrier_no_drain(); // every wavefront's last fragment reads are done: the strips overlay the ring
-
-    // epilogue: register 4 q + e of a lane is column 8 q + 4 (lane / 32) + e of row lane % 32
-    float *strip = reinterpret_cast<float *>(ring) + wave * 32 * PITCH;
-    const int half = lane >> 5, l32 = lane & 31;
-    constexpr int LPR = EW / 8, RPP = 64 / LPR; // lanes per row, rows per pass
-    const int lr = lane / LPR, lc = (lane % LPR) * 8;
-    const int64_t n = n0 + wn + lc;
-    const int valid = static_cast<int>(min(it.N - n, static_cast<int64_t>(8)));
-    const typename Epi::Cols cols(p.extra[c], n, valid);
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-#pragma unroll
-        for (int jj = 0; jj < NJ; ++jj)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<float4 *>(strip + l32 * PITCH + 32 * jj + 8 * q + 4 * half) =
-                    make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
-        // the strip is the wavefront's own, and LDS operations of one wavefront complete in order: what keeps the compiler
-        // from moving the reads up is that they alias
-#pragma unroll
-        for (int r = 0; r < 32; r += RPP) {
-            const float4 lo = *reinterpret_cast<const float4 *>(strip + (r + lr) * PITCH + lc);
-            const float4 hi = *reinterpret_cast<const float4 *>(strip + (r + lr) * PITCH + lc + 4);
-            const int64_t m = m0 + wm + 32 * i + r + lr;
-            if (m < it.M && valid > 0) {
-                const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                Epi::put(p.extra[c], it, cols, m, n, valid, v, split);
+            for (int t = 0; t < tiles; ++t) {
+                const bool more = t + 1 < tiles;
+                if (more) {
+                    sa.load(A, it.lda, now.m0, it.M, now.k0 + static_cast<int64_t>(t + 1) * BK, k_end, tid);
+                    sb.load(B, it.ldb, now.n0, it.N, now.k0 + static_cast<int64_t>(t + 1) * BK, k_end, tid);
+                }
+                compute(ring + (t & 1) * STAGE);
+                if (more) {
+                    char *next = ring + ((t + 1) & 1) * STAGE;
+                    sa.store(next, tid);
+                    sb.store(next + A_STAGE, tid);
+                }
+                wait_counters<63, true>();
+                barrier_no_drain();
             }
-        }
+            epilogue();
+            if constexpr (STRIPS > 0) {
+                wait_counters<63, true>();
+                barrier_no_drain(); // the next tile's first k-tile overlays the strips
+            }
+            now.at += p.stride;
+        } while (now.seek(it, p.stride, BM, BN));
     }
 }
 
-// Tile counts and workgroups of the items; false where a grid cannot hold them.
+// Tiles and workgroups of the items; false where a grid cannot hold them.
 template <typename C, typename Epi> inline bool plan_tiles(TileArgs<Epi> &p, uint32_t *blocks)
 {
     int64_t at = 0;
@@ -440,15 +648,28 @@ template <typename C, typename Epi> inline bool plan_tiles(TileArgs<Epi> &p, uin
         const int64_t mt = (it.M + C::BM - 1) / C::BM, nt = (it.N + C::BN - 1) / C::BN;
         const int64_t outer = it.n_split > 1 ? it.n_split : mt, inner = it.n_split > 1 ? mt * nt : nt;
         if (mt >= (int64_t(1) << 31) || nt >= (int64_t(1) << 31) || inner >= (int64_t(1) << 31) || it.K >= (int64_t(1) << 31)) return false;
+        if (outer > (int64_t(1) << 31) / inner) return false;
         it.mt = static_cast<int32_t>(mt);
         it.nt = static_cast<int32_t>(nt);
         it.block0 = static_cast<uint32_t>(at);
-        if (inner > 0 && outer > max_blocks(C::NT) / inner) return false;
-        at += (outer + 7) / 8 * 8 * inner;
-        if (at > max_blocks(C::NT)) return false;
+        it.places = static_cast<uint32_t>((outer + 7) / 8 * 8 * inner);
+        at += it.places;
+        if (p.n_items > 1 && at > max_blocks(C::NT)) return false;
     }
     *blocks = static_cast<uint32_t>(at);
     return true;
+}
+
+// workgroups of a kernel that are resident at a time
+template <typename C, typename Epi> inline uint32_t resident_tiles()
+{
+    static const uint32_t n = [] {
+        int dev = 0, cus = 0, each = 0;
+        if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) cus = 256;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&each, tile_gemm_kernel<C, Epi>, C::NT, 0) != hipSuccess || each <= 0) each = 1;
+        return static_cast<uint32_t>(cus / 8 * 8 * each);
+    }();
+    return n;
 }
 
 template <typename C, typename Epi> inline heta_status launch_tiles(const char *who, const char *name, TileArgs<Epi> &p, double bytes, double flops, hipStream_t st)
@@ -457,6 +678,9 @@ template <typename C, typename Epi> inline heta_status launch_tiles(const char *
     uint32_t blocks = 0;
     if (!plan_tiles<C>(p, &blocks)) return fail(HETA_ERR_UNSUPPORTED, "%s: matrix too large for one launch", who);
     if (blocks == 0) return HETA_OK;
+    // one item's tiles are walked by the workgroups that fit the chip; several items' get one each
+    if (p.n_items == 1) blocks = std::min(blocks, resident_tiles<C, Epi>());
+    p.stride = p.n_items == 1 ? blocks : 0x80000000u;
     ProfScope prof(name, st, bytes, flops);
     hipLaunchKernelGGL((tile_gemm_kernel<C, Epi>), dim3(blocks), dim3(C::NT), 0, st, p);
     HETA_LAUNCH_CHECK("tile_gemm_kernel");
