@@ -700,10 +700,10 @@ heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int64_t ld_w, 
  *   m <- momentum m + grad;   u = nesterov ? grad + momentum m : m;   X = u / (|u|_F + eps);
  *   `steps` times  X <- 3.4445 X + (-4.7750 A + 2.0315 A A) X  with  A = X X^T  (of the shorter side);
  *   W <- (1 - lr weight_decay) W - lr sqrt(max(1, cols / rows)) X.
- * W: fp32 (products to 2^-24) or bf16 (X kept to 16 bits, W updated in fp32 and rounded back); m: fp32; grad: fp32 or bf16.  All
- * arrays are device memory, items a HOST array; no array of an item may overlap what another item writes.  A zero gradient
- * and momentum leave X = 0.  Uses the handle's workspace (may grow it: about 8 rows * cols * 2 bytes an item).  n_items = 0
- * is a no-op. */
+ * W: fp32 or bf16 (updated in fp32 and rounded back); m: fp32; grad: fp32 or bf16.  X is kept to 16 significant bits between the
+ * steps' products (sums are fp32), which puts it 2.5e-5 of its norm off exact arithmetic.  All arrays are device memory, items
+ * a HOST array; no array of an item may overlap what another item writes.  A zero gradient and momentum leave X = 0.  Uses the
+ * handle's workspace (may grow it: 8 rows * cols + 8 min(rows, cols)^2 bytes an item).  n_items = 0 is a no-op. */
 typedef struct heta_muon_item {
     void *W;
     int64_t ld_w;

@@ -79,7 +79,7 @@ struct LinearExtra {
 constexpr int kAnyAct = -1;
 template <typename O, bool WHOLE, bool SCALED, int ACT = kAnyAct, int SLOPE = kAnyAct, bool READS = true> struct LinearEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kStrip = WHOLE, kReads = READS, kPre = SLOPE <= 0;
+    static constexpr bool kBlocks = false, kStrip = WHOLE, kReads = READS, kPre = SLOPE <= 0;
     using Out = O;
     using Extra = LinearExtra;
     static constexpr int W = 16 / (int)sizeof(O);
@@ -150,7 +150,7 @@ template <typename O, bool WHOLE, bool SCALED, int ACT = kAnyAct, int SLOPE = kA
 // partial products of a contraction that is split over its rows: [split][M][N] fp32.  WHOLE: N is a multiple of four
 template <bool WHOLE> struct PartialEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kStrip = WHOLE, kReads = false, kPre = false;
+    static constexpr bool kBlocks = false, kStrip = WHOLE, kReads = false, kPre = false;
     using Out = float;
     struct Extra {
         float *part;
@@ -182,7 +182,7 @@ struct Launch {
     hipStream_t st;
     template <typename C, typename Epi> heta_status go(const typename Epi::Extra &x) const
     {
-        TileArgs<Epi> p{1, 0, {it}, {x}};
+        TileArgs<Epi> p{1, 0, 0, {it}, {x}};
         return launch_tiles<C>(who, name, p, bytes, flops, st);
     }
     bool direct(size_t elt) const { return direct_rows(it.A, it.lda, elt) && direct_rows(it.B, it.ldb, elt); }

@@ -7,10 +7,9 @@
 // The matrices [rows, cols] are those of a product in . W.  X lies with its shorter side k as rows (a tall matrix is
 // transposed on its way in and out, by the element-wise kernels), so a step is three products for every item: k x k Gram
 // matrix, k x k polynomial, k x l update.  They are the tile kernel of heta_tiles.h on the bf16 matrix pipe with every
-// matrix held as bf16 terms, three for fp32 weights (24 bits, the rounding of fp32: a state of 32 bits or more), two for
-// bf16 weights (16 bits: the update is lr times X and the weight it is subtracted from keeps 8); the epilogue that makes
-// a matrix writes it as terms, so that the next product loads them straight into LDS.
-// |u| is summed per 64 x 64 tile, then over the tiles in a fixed order by every workgroup that needs it.
+// matrix held as two bf16 terms (kTerms); the epilogue that makes a matrix writes it as terms, so that the next product loads
+// them straight into LDS.  Gram matrix and polynomial are symmetric: only the tiles on and above the diagonal are formed.
+// |u| is summed per part of 32 x 64, then over the parts in a fixed order by every workgroup that needs it.
 #include <algorithm>
 #include <cmath>
 
@@ -20,6 +19,9 @@
 namespace heta {
 
 constexpr int kMuonItems = 12; // per launch
+// bf16 terms of a matrix.  Two hold 16 bits; the update then misses the one of exact products by 2.5e-5 of its norm (three: 2.3e-7,
+// at twice the products; one: 1.3e-2).  The polynomial itself leaves singular values 20 to 30 % away from 1.
+constexpr int kTerms = 2;
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 
 struct MuonItem {
@@ -29,11 +31,11 @@ struct MuonItem {
     int64_t ld_w, ld_m, ld_grad;
     int32_t rows, cols;
     int32_t tall;      // rows > cols: X is the transpose
-    int32_t grad_bf16;
+    int32_t grad_bf16, w_bf16;
     bf16_t *x;         // terms of X
     int64_t ld_x, plane; // elements
-    float *part;       // sums of squares, one per tile
-    uint32_t block0, tiles;
+    float *part;       // sums of squares, one per part
+    uint32_t block0, parts; // first workgroup and number of its 32 x 64 parts
 };
 struct MuonArgs {
     int n;
@@ -54,137 +56,147 @@ __device__ __forceinline__ float muon_grad(const MuonItem &it, int64_t r, int64_
     return it.grad_bf16 ? widen(static_cast<const bf16_t *>(it.grad)[r * it.ld_grad + c]) : static_cast<const float *>(it.grad)[r * it.ld_grad + c];
 }
 
-// One workgroup per 64 x 64 tile: momentum, and the sum of squares of u.
+// Momentum, and the sum of squares of u: one workgroup per part of 32 x 64.  Every load comes before the first store: a
+// small matrix has one workgroup's latency to wait for.
 __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonArgs p)
 {
     __shared__ float sums[4];
     const MuonItem &it = p.item[muon_item(p)];
     const uint32_t b = blockIdx.x - it.block0, tc = (it.cols + 63) / 64;
-    const int64_t r0 = static_cast<int64_t>(b / tc) * 64, c = static_cast<int64_t>(b % tc) * 64 + (threadIdx.x & 63);
-    float ss = 0.f;
-    if (c < it.cols) {
-#pragma unroll 4
-        for (int64_t r = r0 + (threadIdx.x >> 6); r < min(r0 + 64, static_cast<int64_t>(it.rows)); r += 4) {
-            const float g = muon_grad(it, r, c);
-            const float m = fmaf(p.mu, it.m[r * it.ld_m + c], g);
-            it.m[r * it.ld_m + c] = m;
-            const float u = p.nesterov ? fmaf(p.mu, m, g) : m;
-            ss += u * u;
-        }
+    const int lx = threadIdx.x & 63, ly = threadIdx.x >> 6;
+    const int64_t r0 = static_cast<int64_t>(b / tc) * 32 + ly, c = static_cast<int64_t>(b % tc) * 64 + lx;
+    float g[8], m[8], ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + 4 * i;
+        const bool in = r < it.rows && c < it.cols;
+        g[i] = in ? muon_grad(it, r, c) : 0.f;
+        m[i] = in ? it.m[r * it.ld_m + c] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + 4 * i;
+        m[i] = fmaf(p.mu, m[i], g[i]);
+        const float u = p.nesterov ? fmaf(p.mu, m[i], g[i]) : m[i];
+        ss += u * u;
+        if (r < it.rows && c < it.cols) it.m[r * it.ld_m + c] = m[i];
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
+    if (lx == 0) sums[ly] = ss;
     __syncthreads();
     if (threadIdx.x == 0) it.part[b] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-template <int T> __device__ __forceinline__ void store_terms(bf16_t *p, int64_t plane, float v)
+__device__ __forceinline__ void store_terms(bf16_t *p, int64_t plane, float v)
 {
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
+    for (int t = 0; t < kTerms; ++t) {
         const bf16_t h = to_bf16(v);
         p[t * plane] = h;
         v -= widen(h);
     }
 }
 
-// X_0 as terms; a tall matrix goes through LDS so that both its reads and its writes are along rows.
-template <int T> __global__ void __launch_bounds__(256) muon_start_kernel(MuonArgs p)
+// X_0 as terms; a tall matrix goes through LDS so that both its reads and its writes are along
+// rows.  The sums of squares come in while the part does.
+__global__ void __launch_bounds__(256) muon_start_kernel(MuonArgs p)
 {
-    __shared__ float tile[64][65];
+    __shared__ float tile[32][65];
     __shared__ float sums[4];
     const MuonItem &it = p.item[muon_item(p)];
+    const uint32_t b = blockIdx.x - it.block0, tc = (it.cols + 63) / 64;
+    const int64_t r0 = static_cast<int64_t>(b / tc) * 32, c0 = static_cast<int64_t>(b % tc) * 64;
+    const int lx = threadIdx.x & 63, ly = threadIdx.x >> 6;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + 4 * i + ly, c = c0 + lx;
+        x[i] = 0.f;
+        if (r < it.rows && c < it.cols) {
+            x[i] = it.m[r * it.ld_m + c];
+            if (p.nesterov) x[i] = fmaf(p.mu, x[i], muon_grad(it, r, c));
+        }
+    }
     float ss = 0.f;
-    for (uint32_t i = threadIdx.x; i < it.tiles; i += 256) ss += it.part[i];
+    for (uint32_t i = threadIdx.x; i < it.parts; i += 256) ss += it.part[i];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
+    if (lx == 0) sums[ly] = ss;
     __syncthreads();
     const float inv = 1.f / (sqrtf((sums[0] + sums[1]) + (sums[2] + sums[3])) + p.eps);
-    const uint32_t b = blockIdx.x - it.block0, tc = (it.cols + 63) / 64;
-    const int64_t r0 = static_cast<int64_t>(b / tc) * 64, c0 = static_cast<int64_t>(b % tc) * 64;
-    const int lx = threadIdx.x & 63, ly = threadIdx.x >> 6;
-#pragma unroll 4
-    for (int i = ly; i < 64; i += 4) {
-        const int64_t r = r0 + i, c = c0 + lx;
-        if (r >= it.rows || c >= it.cols) continue;
-        const float m = it.m[r * it.ld_m + c];
-        const float x = (p.nesterov ? fmaf(p.mu, m, muon_grad(it, r, c)) : m) * inv;
-        if (it.tall) tile[i][lx] = x;
-        else store_terms<T>(it.x + r * it.ld_x + c, it.plane, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + 4 * i + ly, c = c0 + lx;
+        if (it.tall) tile[4 * i + ly][lx] = x[i] * inv;
+        else if (r < it.rows && c < it.cols) store_terms(it.x + r * it.ld_x + c, it.plane, x[i] * inv);
     }
     if (!it.tall) return; // uniform
     __syncthreads();
-#pragma unroll 4
-    for (int i = ly; i < 64; i += 4)
-        if (c0 + i < it.cols && r0 + lx < it.rows) store_terms<T>(it.x + (c0 + i) * it.ld_x + r0 + lx, it.plane, tile[lx][i]);
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c0 + 8 * i + ty < it.cols && r0 + tx < it.rows) store_terms(it.x + (c0 + 8 * i + ty) * it.ld_x + r0 + tx, it.plane, tile[tx][8 * i + ty]);
 }
 
 // W <- keep W - step X
-template <int T, typename E> __global__ void __launch_bounds__(256) muon_update_kernel(MuonArgs p)
+__global__ void __launch_bounds__(256) muon_update_kernel(MuonArgs p)
 {
-    __shared__ float tile[64][65];
+    __shared__ float tile[32][65];
     const MuonItem &it = p.item[muon_item(p)];
     const uint32_t b = blockIdx.x - it.block0, tc = (it.cols + 63) / 64;
-    const int64_t r0 = static_cast<int64_t>(b / tc) * 64, c0 = static_cast<int64_t>(b % tc) * 64;
-    const int lx = threadIdx.x & 63, ly = threadIdx.x >> 6;
+    const int64_t r0 = static_cast<int64_t>(b / tc) * 32, c0 = static_cast<int64_t>(b % tc) * 64;
+    const int lx = threadIdx.x & 63, ly = threadIdx.x >> 6, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
     auto value = [&](int64_t at) {
         float v = widen(it.x[at]);
 #pragma unroll
-        for (int t = 1; t < T; ++t) v += widen(it.x[at + t * it.plane]);
+        for (int t = 1; t < kTerms; ++t) v += widen(it.x[at + t * it.plane]);
         return v;
     };
-    if (it.tall) {
-#pragma unroll 4
-        for (int i = ly; i < 64; i += 4)
-            if (c0 + i < it.cols && r0 + lx < it.rows) tile[lx][i] = value((c0 + i) * it.ld_x + r0 + lx);
+    float w[8], x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + 4 * i + ly, c = c0 + lx, at = r * it.ld_w + c;
+        const bool in = r < it.rows && c < it.cols;
+        w[i] = in ? (it.w_bf16 ? widen(static_cast<const bf16_t *>(it.W)[at]) : static_cast<const float *>(it.W)[at]) : 0.f;
+        if (it.tall) x[i] = c0 + 8 * i + ty < it.cols && r0 + tx < it.rows ? value((c0 + 8 * i + ty) * it.ld_x + r0 + tx) : 0.f;
+        else x[i] = in ? value(r * it.ld_x + c) : 0.f;
+    }
+    if (it.tall) { // uniform
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tile[tx][8 * i + ty] = x[i];
         __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = tile[4 * i + ly][lx];
     }
     const float step = p.step_size * sqrtf(fmaxf(1.f, static_cast<float>(it.cols) / static_cast<float>(it.rows)));
-    E *W = static_cast<E *>(it.W);
-#pragma unroll 4
-    for (int i = ly; i < 64; i += 4) {
-        const int64_t r = r0 + i, c = c0 + lx;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + 4 * i + ly, c = c0 + lx, at = r * it.ld_w + c;
         if (r >= it.rows || c >= it.cols) continue;
-        const float x = it.tall ? tile[i][lx] : value(r * it.ld_x + c);
-        const float w = fmaf(-step, x, p.keep * widen(W[r * it.ld_w + c]));
-        if constexpr (sizeof(E) == 2) W[r * it.ld_w + c] = to_bf16(w);
-        else W[r * it.ld_w + c] = w;
+        const float v = fmaf(-step, x[i], p.keep * w[i]);
+        if (it.w_bf16) static_cast<bf16_t *>(it.W)[at] = to_bf16(v);
+        else static_cast<float *>(it.W)[at] = v;
     }
 }
 
-// out = beta old + alpha A B, as terms
+// out = beta old + alpha A B, as terms.  A symmetric product's tiles beside the diagonal are written twice, the second time
+// with rows and columns exchanged.
 struct TermsExtra {
     const bf16_t *old; // nullable
     bf16_t *out;
     int64_t ld_old, old_plane, ld_out, out_plane; // elements
+    float alpha, beta;
 };
-template <int T> struct TermsEpi {
+struct TermsEpi {
     static constexpr int kItems = kMuonItems;
-    static constexpr bool kStrip = false;
-    using Out = bf16_t;
-    struct Extra : TermsExtra {
-        float alpha, beta;
-    };
-    __device__ __forceinline__ static void put(const Extra &x, const TileItem &, int64_t m, int64_t n, int valid, const float (&v)[8], int)
+    static constexpr bool kBlocks = true, kStrip = false;
+    using Extra = TermsExtra;
+    // eight results of row r, columns c, c + 1, ... (valid of them there; rows of the terms are 16-byte aligned)
+    __device__ __forceinline__ static void put(const Extra &x, int64_t r, int64_t c, int valid, float (&y)[8])
     {
-        float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = x.alpha * v[e];
-        if (x.old) {
-            float o[8], s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int t = T - 1; t >= 0; --t) { // smallest first
-                load8(x.old + t * x.old_plane + m * x.ld_old + n, valid, true, o);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[e] += o[e];
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = fmaf(x.beta, s[e], y[e]);
-        }
-#pragma unroll
-        for (int t = 0; t < T; ++t) {
+        for (int t = 0; t < kTerms; ++t) {
             uint32_t w[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -192,7 +204,7 @@ template <int T> struct TermsEpi {
                 y[2 * j] -= __uint_as_float(w[j] << 16);
                 y[2 * j + 1] -= __uint_as_float(w[j] & 0xffff0000u);
             }
-            bf16_t *to = x.out + t * x.out_plane + m * x.ld_out + n;
+            bf16_t *to = x.out + t * x.out_plane + r * x.ld_out + c;
             if (valid >= 8) {
                 *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
             } else {
@@ -202,61 +214,115 @@ template <int T> struct TermsEpi {
             }
         }
     }
+    __device__ __forceinline__ static void block(const Extra &x, const TileItem &it, float *strip, int64_t m0, int64_t n0, bool off_diagonal, int lane)
+    {
+        const int sr = lane / 4, sc = lane % 4;
+        const bool mirror = it.symmetric && off_diagonal;
+        const int64_t n = n0 + 8 * sc;
+        const int valid = static_cast<int>(min(it.N - n, static_cast<int64_t>(8)));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = 16 * h + sr;
+            const int64_t m = m0 + row;
+            const float4 lo = *strip_at(strip, row, 2 * sc), hi = *strip_at(strip, row, 2 * sc + 1);
+            float y[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= x.alpha;
+            if (x.old && m < it.M && valid > 0) {
+                float o[8], s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = kTerms - 1; t >= 0; --t) { // smallest first
+                    load8(x.old + t * x.old_plane + m * x.ld_old + n, valid, true, o);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e] += o[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = fmaf(x.beta, s[e], y[e]);
+            }
+            if (mirror) { // back into the strip, to be read by columns
+                *strip_at(strip, row, 2 * sc) = make_float4(y[0], y[1], y[2], y[3]);
+                *strip_at(strip, row, 2 * sc + 1) = make_float4(y[4], y[5], y[6], y[7]);
+            }
+            if (m < it.M && valid > 0) put(x, m, n, valid, y);
+        }
+        if (!mirror) return;
+        const int64_t c = m0 + 8 * sc; // column of the mirrored block
+        const int there = static_cast<int>(min(it.M - c, static_cast<int64_t>(8)));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int col = 16 * h + sr;
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int row = 8 * sc + e;
+                y[e] = reinterpret_cast<const float *>(strip_at(strip, row, col / 4))[col % 4];
+            }
+            if (n0 + col < it.N && there > 0) put(x, n0 + col, c, there, y);
+        }
+    }
 };
 
 // ---- host side ---------------------------------------------------------------------------------------
-template <int T, bool B_RC> using NsSmall = TileShape<bf16_t, 2, T, false, B_RC, kDirect, 2, 2, 1, 1, 32, 3, 2>;
-template <int T, bool B_RC> using NsLarge = TileShape<bf16_t, 2, T, false, B_RC, kDirect, 2, 2, 2, 2, 32, 2, 1>;
+template <bool B_RC> using NsDeep = TileShape<bf16_t, 2, kTerms, false, B_RC, kDirect, 2, 2, 1, 1, 64, 4, 1>;   // 64 x 64, one per CU
+template <bool B_RC> using NsSmall = TileShape<bf16_t, 2, kTerms, false, B_RC, kDirect, 2, 2, 1, 1, 64, 2, 1>;  // 64 x 64, two per CU
+template <bool B_RC> using NsLarge = TileShape<bf16_t, 2, kTerms, false, B_RC, kDirect, 2, 4, 2, 1, 64, 2, 1>;  // 128 x 128
 
-template <int T, bool B_RC> static heta_status launch_terms(const char *who, TileArgs<TermsEpi<T>> &p, hipStream_t st)
+template <bool B_RC> static heta_status launch_terms(const char *who, TileArgs<TermsEpi> &p, hipStream_t st)
 {
     double bytes = 0, flops = 0;
-    int64_t tiles = 0;
+    int64_t large = 0, small = 0;
     for (int i = 0; i < p.n_items; ++i) {
         const TileItem &it = p.item[i];
-        bytes += 2.0 * T * (static_cast<double>(it.M) * it.K + static_cast<double>(it.K) * it.N + static_cast<double>(it.M) * it.N);
-        flops += 2.0 * it.M * it.N * it.K;
-        tiles += (it.M + 127) / 128 * ((it.N + 127) / 128);
+        bytes += 2.0 * kTerms * (static_cast<double>(it.M) * it.K + static_cast<double>(it.K) * it.N + static_cast<double>(it.M) * it.N);
+        flops += (it.symmetric ? 1.0 : 2.0) * it.M * it.N * it.K;
+        auto tiles = [&](int64_t b) {
+            const int64_t mt = (it.M + b - 1) / b, nt = (it.N + b - 1) / b;
+            return it.symmetric ? mt * (mt + 1) / 2 : mt * nt;
+        };
+        large += tiles(128);
+        small += tiles(64);
     }
-    if (tiles >= 256) return launch_tiles<NsLarge<T, B_RC>>(who, "muon_product_kernel", p, bytes, flops, st);
-    return launch_tiles<NsSmall<T, B_RC>>(who, "muon_product_kernel", p, bytes, flops, st);
+    // Large tiles once they occupy a good third of the chip.  Below, 64 x 64: with a workgroup per CU at most, the ring takes the CU's
+    // whole LDS and the first 256 k-values are on their way at once (7 matrices of 128 x 256: 138 -> 121 us); with more of
+    // them, two share a CU (2 matrices of 1,024 x 4,096: 709 us, 871 with the deep ring).
+    if (large >= 96) return launch_tiles<NsLarge<B_RC>>(who, "muon_product_kernel", p, bytes, flops, st);
+    if (small <= 256) return launch_tiles<NsDeep<B_RC>>(who, "muon_product_kernel", p, bytes, flops, st);
+    return launch_tiles<NsSmall<B_RC>>(who, "muon_product_kernel", p, bytes, flops, st);
 }
 
 static int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
 struct MuonPlan { // places in the workspace, in bytes, of one item
-    int64_t k, l, tiles;
+    int64_t k, l, parts;
     int64_t ld_x, ld_g, x_plane, g_plane; // elements
     int64_t x[2], gram, poly, part, end;
-    MuonPlan(int32_t rows, int32_t cols, int terms, int64_t at)
-        : k(std::min(rows, cols)), l(std::max(rows, cols)), tiles(int64_t((rows + 63) / 64) * ((cols + 63) / 64)), ld_x(pad8(l)), ld_g(pad8(k)), x_plane(k * ld_x), g_plane(k * ld_g)
+    MuonPlan(int32_t rows, int32_t cols, int64_t at)
+        : k(std::min(rows, cols)), l(std::max(rows, cols)), parts(int64_t((rows + 31) / 32) * ((cols + 63) / 64)), ld_x(pad8(l)), ld_g(pad8(k)), x_plane(k * ld_x), g_plane(k * ld_g)
     {
         auto take = [&](int64_t bytes) {
             const int64_t p = at;
             at += (bytes + 255) / 256 * 256;
             return p;
         };
-        x[0] = take(x_plane * terms * 2);
-        x[1] = take(x_plane * terms * 2);
-        gram = take(g_plane * terms * 2);
-        poly = take(g_plane * terms * 2);
-        part = take(tiles * 4);
+        x[0] = take(x_plane * kTerms * 2);
+        x[1] = take(x_plane * kTerms * 2);
+        gram = take(g_plane * kTerms * 2);
+        poly = take(g_plane * kTerms * 2);
+        part = take(parts * 4);
         end = at;
     }
 };
 
-template <int T, typename E>
-static heta_status muon_group(const char *who, heta_graph *g, const std::vector<const heta_muon_item *> &items, float lr, float mu, int nesterov, float wd, float eps, int steps,
+static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_item *items, int n, float lr, float mu, int nesterov, float wd, float eps, int steps,
                               hipStream_t st)
 {
     int64_t at = 0;
     std::vector<MuonPlan> plan;
-    for (const heta_muon_item *it : items) {
-        plan.emplace_back(it->rows, it->cols, T, at);
+    for (int i = 0; i < n; ++i) {
+        plan.emplace_back(items[i].rows, items[i].cols, at);
         at = plan.back().end;
     }
     HETA_TRY(ensure_workspace(g, static_cast<size_t>(at)));
     char *ws = static_cast<char *>(g->d_ws);
-    const int n = static_cast<int>(items.size());
     MuonArgs a{};
     a.n = n;
     a.mu = mu;
@@ -267,11 +333,11 @@ static heta_status muon_group(const char *who, heta_graph *g, const std::vector<
     int64_t blocks = 0;
     double elems = 0, esz = 0;
     for (int i = 0; i < n; ++i) {
-        const heta_muon_item &q = *items[i];
+        const heta_muon_item &q = items[i];
         const MuonPlan &pl = plan[i];
-        a.item[i] = MuonItem{q.W, q.m, q.grad, q.ld_w, q.ld_m, q.ld_grad, q.rows, q.cols, q.rows > q.cols, q.grad_dt == HETA_BF16, reinterpret_cast<bf16_t *>(ws + pl.x[0]), pl.ld_x,
-                             pl.x_plane, reinterpret_cast<float *>(ws + pl.part), static_cast<uint32_t>(blocks), static_cast<uint32_t>(pl.tiles)};
-        blocks += pl.tiles;
+        a.item[i] = MuonItem{q.W, q.m, q.grad, q.ld_w, q.ld_m, q.ld_grad, q.rows, q.cols, q.rows > q.cols, q.grad_dt == HETA_BF16, q.dt == HETA_BF16, reinterpret_cast<bf16_t *>(ws + pl.x[0]), pl.ld_x,
+                             pl.x_plane, reinterpret_cast<float *>(ws + pl.part), static_cast<uint32_t>(blocks), static_cast<uint32_t>(pl.parts)};
+        blocks += pl.parts;
         elems += static_cast<double>(q.rows) * q.cols;
         esz = static_cast<double>(dtype_size(q.grad_dt));
         if (blocks > max_blocks(256)) return fail(HETA_ERR_UNSUPPORTED, "%s: too many elements for one launch", who);
@@ -283,31 +349,31 @@ static heta_status muon_group(const char *who, heta_graph *g, const std::vector<
         HETA_LAUNCH_CHECK("muon_momentum_kernel");
     }
     {
-        ProfScope prof("muon_start_kernel", st, elems * (4 + esz + 2 * T), 0);
-        hipLaunchKernelGGL(muon_start_kernel<T>, grid, dim3(256), 0, st, a);
+        ProfScope prof("muon_start_kernel", st, elems * (4 + esz + 2 * kTerms), 0);
+        hipLaunchKernelGGL(muon_start_kernel, grid, dim3(256), 0, st, a);
         HETA_LAUNCH_CHECK("muon_start_kernel");
     }
     for (int s = 0; s < steps; ++s) {
-        TileArgs<TermsEpi<T>> gram{}, poly{}, apply{};
+        TileArgs<TermsEpi> gram{}, poly{}, apply{};
         gram.n_items = poly.n_items = apply.n_items = n;
         for (int i = 0; i < n; ++i) {
             const MuonPlan &pl = plan[i];
             char *x = ws + pl.x[s & 1], *y = ws + pl.x[(s & 1) ^ 1], *A = ws + pl.gram, *P = ws + pl.poly;
             auto terms = [](char *p) { return reinterpret_cast<bf16_t *>(p); };
-            gram.item[i] = TileItem{x, x, pl.ld_x, pl.ld_x, pl.x_plane * 2, pl.x_plane * 2, pl.k, pl.k, pl.l, pl.l, 1, 0, 0, 0, 0};
-            poly.item[i] = TileItem{A, A, pl.ld_g, pl.ld_g, pl.g_plane * 2, pl.g_plane * 2, pl.k, pl.k, pl.k, pl.k, 1, 0, 0, 0, 0};
-            apply.item[i] = TileItem{P, x, pl.ld_g, pl.ld_x, pl.g_plane * 2, pl.x_plane * 2, pl.k, pl.l, pl.k, pl.k, 1, 0, 0, 0, 0};
-            gram.extra[i] = {{nullptr, terms(A), 0, 0, pl.ld_g, pl.g_plane}, 1.f, 0.f};
-            poly.extra[i] = {{terms(A), terms(P), pl.ld_g, pl.g_plane, pl.ld_g, pl.g_plane}, kNsC, kNsB};
-            apply.extra[i] = {{terms(x), terms(y), pl.ld_x, pl.x_plane, pl.ld_x, pl.x_plane}, 1.f, kNsA};
+            gram.item[i] = TileItem{x, x, pl.ld_x, pl.ld_x, pl.x_plane * 2, pl.x_plane * 2, pl.k, pl.k, pl.l, pl.l, 1, 0, 0, 1, 0, 0};
+            poly.item[i] = TileItem{A, A, pl.ld_g, pl.ld_g, pl.g_plane * 2, pl.g_plane * 2, pl.k, pl.k, pl.k, pl.k, 1, 0, 0, 1, 0, 0};
+            apply.item[i] = TileItem{P, x, pl.ld_g, pl.ld_x, pl.g_plane * 2, pl.x_plane * 2, pl.k, pl.l, pl.k, pl.k, 1, 0, 0, 0, 0, 0};
+            gram.extra[i] = {nullptr, terms(A), 0, 0, pl.ld_g, pl.g_plane, 1.f, 0.f};
+            poly.extra[i] = {terms(A), terms(P), pl.ld_g, pl.g_plane, pl.ld_g, pl.g_plane, kNsC, kNsB};
+            apply.extra[i] = {terms(x), terms(y), pl.ld_x, pl.x_plane, pl.ld_x, pl.x_plane, 1.f, kNsA};
         }
-        HETA_TRY((launch_terms<T, false>(who, gram, st)));
-        HETA_TRY((launch_terms<T, false>(who, poly, st)));
-        HETA_TRY((launch_terms<T, true>(who, apply, st)));
+        HETA_TRY((launch_terms<false>(who, gram, st)));
+        HETA_TRY((launch_terms<false>(who, poly, st)));
+        HETA_TRY((launch_terms<true>(who, apply, st)));
     }
     for (int i = 0; i < n; ++i) a.item[i].x = reinterpret_cast<bf16_t *>(ws + plan[i].x[steps & 1]);
-    ProfScope prof("muon_update_kernel", st, elems * (2 * T + 2 * sizeof(E)), 0);
-    hipLaunchKernelGGL((muon_update_kernel<T, E>), grid, dim3(256), 0, st, a);
+    ProfScope prof("muon_update_kernel", st, elems * (2 * kTerms + 2 * esz), 0);
+    hipLaunchKernelGGL(muon_update_kernel, grid, dim3(256), 0, st, a);
     HETA_LAUNCH_CHECK("muon_update_kernel");
     return HETA_OK;
 }
@@ -333,7 +399,7 @@ extern "C" heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const het
         const size_t esz = dtype_size(q.dt), gsz = dtype_size(q.grad_dt);
         if (reinterpret_cast<uintptr_t>(q.W) % esz || reinterpret_cast<uintptr_t>(q.m) % 4 || reinterpret_cast<uintptr_t>(q.grad) % gsz)
             return fail(HETA_ERR_INVALID_ARG, "%s: item %d: pointer not aligned to its element size", who, i);
-        if (static_cast<int64_t>((q.rows + 63) / 64) * ((q.cols + 63) / 64) > (1 << 22)) return fail(HETA_ERR_UNSUPPORTED, "%s: item %d: matrix too large", who, i);
+        if (static_cast<int64_t>((q.rows + 31) / 32) * ((q.cols + 63) / 64) > (1 << 22)) return fail(HETA_ERR_UNSUPPORTED, "%s: item %d: matrix too large", who, i);
         const RowRange w(q.W, q.rows, q.ld_w, q.cols, esz), m(q.m, q.rows, q.ld_m, q.cols, 4), gr(q.grad, q.rows, q.ld_grad, q.cols, gsz);
         if (gr.overlaps(w) || gr.overlaps(m)) return fail(HETA_ERR_INVALID_ARG, "%s: item %d: the gradient overlaps an output", who, i);
         outs.emplace_back(i, w);
@@ -342,15 +408,7 @@ extern "C" heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const het
     }
     if (items_collide(outs, ins)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps another item's arrays", who);
     hipStream_t st = as_stream(hip_stream);
-    for (const heta_dtype dt : {HETA_F32, HETA_BF16}) {
-        std::vector<const heta_muon_item *> some;
-        for (int32_t i = 0; i <= n_items; ++i) {
-            if (i < n_items && items[i].dt == dt) some.push_back(&items[i]);
-            if (some.empty() || (i < n_items && some.size() < static_cast<size_t>(kMuonItems))) continue;
-            HETA_TRY((dt == HETA_F32 ? muon_group<3, float>(who, g, some, lr, momentum, nesterov != 0, weight_decay, eps, steps, st)
-                                     : muon_group<2, bf16_t>(who, g, some, lr, momentum, nesterov != 0, weight_decay, eps, steps, st)));
-            some.clear();
-        }
-    }
+    for (int32_t i = 0; i < n_items; i += kMuonItems)
+        HETA_TRY(muon_group(who, g, items + i, std::min<int32_t>(kMuonItems, n_items - i), lr, momentum, nesterov != 0, weight_decay, eps, steps, st));
     return HETA_OK;
 }

@@ -253,6 +253,9 @@ template <typename O> __device__ __forceinline__ void unpack16(uint4 raw, float 
     }
 }
 
+// four columns (chunk 0..7) of a row of a 32 x 32 fp32 strip
+__device__ __forceinline__ float4 *strip_at(float *strip, int row, int chunk) { return reinterpret_cast<float4 *>(strip + row * 32 + ((chunk ^ (row & 7)) * 4)); }
+
 // ---- items of a launch ------------------------------------------------------------------------------
 struct TileItem { // M, N, K > 0
     const void *A, *B;
@@ -262,17 +265,26 @@ struct TileItem { // M, N, K > 0
     int64_t k_per_split;       // multiple of BK; n_split * k_per_split >= K
     int32_t n_split;           // every split has k-values
     int32_t mt, nt;            // tiles
-    uint32_t block0, places;   // first workgroup (multiple of 8), places of the item's tiles
+    int32_t symmetric;         // C is: the tiles below the diagonal are not formed (several items, one tile size along both sides)
+    uint32_t block0, places;   // one item: places of its tiles; several: the tiles before it, its tiles
 };
 
-// A place in the order of an item's output tiles, and the tile there.  Place -> (XCD, position in its queue) -> tile:
-// workgroups go round-robin to the 8 XCDs, and the tiles that share operand rows (the column tiles of a row block, all tiles
-// of a split) follow one another on one of them.
+// An output tile and the part of the contraction that goes into it.
 struct TilePlace {
     uint32_t at;
     int64_t m0, n0, k0;
     int kn, split;
-    // the first place from `at` on, `stride` apart, that has a tile
+    __device__ __forceinline__ void set(const TileItem &it, uint32_t row, uint32_t col, int s, int bm, int bn)
+    {
+        split = s;
+        m0 = static_cast<int64_t>(row) * bm;
+        n0 = static_cast<int64_t>(col) * bn;
+        k0 = s * it.k_per_split;
+        kn = static_cast<int>(min(it.K - k0, it.k_per_split));
+    }
+    // One item: the first place from `at` on, `stride` apart, that has a tile.  Place -> (XCD, position in its queue) -> tile:
+    // workgroups go round-robin to the 8 XCDs, and the tiles that share operand rows (the column tiles of a row block, all
+    // tiles of a split) follow one another on one of them.
     __device__ __forceinline__ bool seek(const TileItem &it, uint32_t stride, int bm, int bn)
     {
         const bool splits = it.n_split > 1;
@@ -280,19 +292,28 @@ struct TilePlace {
         for (; at < it.places; at += stride) {
             const uint32_t j = at / 8, in = j % inner, outer = j / inner * 8 + at % 8;
             if (outer >= n_outer) continue;
-            split = splits ? static_cast<int>(outer) : 0;
-            m0 = static_cast<int64_t>(splits ? in / it.nt : outer) * bm;
-            n0 = static_cast<int64_t>(splits ? in % it.nt : in) * bn;
-            k0 = split * it.k_per_split;
-            kn = static_cast<int>(min(it.K - k0, it.k_per_split));
+            if (splits) set(it, in / it.nt, in % it.nt, static_cast<int>(outer), bm, bn);
+            else set(it, outer, in, 0, bm, bn);
             return true;
         }
         return false;
+    }
+    // Several items: tile `in` of an item, row block by row block (a symmetric one's from the diagonal on).
+    __device__ __forceinline__ void pick(const TileItem &it, uint32_t in, int bm, int bn)
+    {
+        uint32_t row = 0;
+        if (it.symmetric) {
+            while (in >= static_cast<uint32_t>(it.nt) - row) in -= static_cast<uint32_t>(it.nt) - row++;
+            set(it, row, row + in, 0, bm, bn);
+        } else {
+            set(it, in / it.nt, in % it.nt, 0, bm, bn);
+        }
     }
 };
 
 // Epi: what becomes of the product; all functions are device functions.
 //   kItems, Extra: items of a launch at most, and what an item's epilogue needs
+//   kBlocks = true: block(x, it, strip, m, n, off_diagonal, lane) takes 32 x 32 sums at row m, column n from the strip (strip_at)
 //   kStrip = false: put(x, it, m, n, valid, v, split) takes eight columns n, n + 1, ... of row m < M (valid: as many as there are)
 //   kStrip = true (Out rows of whole, aligned 16-byte pieces): with W = 16 bytes of columns, first(cols, row, y) makes
 //     pre-activations of W sums and second(x, y, t) results, t being W elements of x.other (if kReads; zeros or nothing where it
@@ -301,7 +322,8 @@ struct TilePlace {
 //     may lie beyond the matrix).
 template <typename Epi> struct TileArgs {
     int n_items;
-    uint32_t stride; // from one tile of a workgroup to its next
+    uint32_t stride; // one item: from one tile of a workgroup to its next; several: tiles of an XCD
+    uint32_t total;  // several items: tiles
     TileItem item[Epi::kItems];
     typename Epi::Extra extra[Epi::kItems];
 };
@@ -328,7 +350,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
     using ImgB = TileImage<C::B_RC, BN, BK, EB>;
     constexpr int A_STAGE = ImgA::BYTES * T, STAGE = A_STAGE + ImgB::BYTES * T;
     // epilogue strips: one 32 x 32 block of sums per wavefront, its own; behind the ring where that is filled during the epilogue
-    constexpr int STRIPS = Epi::kStrip ? NW * 4096 : 0, STRIPS_AT = DIRECT ? ST * STAGE : 0;
+    constexpr int STRIPS = Epi::kStrip || Epi::kBlocks ? NW * 4096 : 0, STRIPS_AT = DIRECT ? ST * STAGE : 0;
     __shared__ __attribute__((aligned(1024))) char ring[std::max(ST * STAGE, STRIPS_AT + STRIPS)];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -336,13 +358,25 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
     const int wm = (wave / C::WN) * (32 * MI), wn = (wave % C::WN) * (32 * NJ);
 
     int c = 0;
-    if constexpr (Epi::kItems > 1)
-        while (c + 1 < p.n_items && blockIdx.x >= p.item[c + 1].block0) ++c; // uniform
+    TilePlace now;
+    if constexpr (Epi::kItems > 1) {
+        // a workgroup per tile; an XCD's are consecutive ones, so that an item's operands meet in one or two L2s
+        const uint32_t tile = blockIdx.x % 8 * p.stride + blockIdx.x / 8;
+        if (tile >= p.total) return;
+        while (c + 1 < p.n_items && tile >= p.item[c + 1].block0) ++c; // uniform
+        now.pick(p.item[c], tile - p.item[c].block0, BM, BN);
+    } else {
+        now.at = blockIdx.x;
+        if (!now.seek(p.item[0], p.stride, BM, BN)) return;
+    }
     const TileItem it = p.item[c];
     const typename Epi::Extra extra = p.extra[c];
-    TilePlace now;
-    now.at = blockIdx.x - it.block0;
-    if (!now.seek(it, p.stride, BM, BN)) return;
+
+    auto further = [&](TilePlace &t) { // the workgroup's next tile
+        if constexpr (Epi::kItems > 1) return false;
+        t.at += p.stride;
+        return t.seek(it, p.stride, BM, BN);
+    };
 
     floatx16 acc[MI][NJ];
     auto clear = [&] {
@@ -435,12 +469,23 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
     // register 4 q + e of block (i, jj) is column 8 q + 4 (lane / 32) + e of row lane % 32
     const int half = lane >> 5, l32 = lane & 31;
     auto epilogue = [&] {
-        if constexpr (Epi::kStrip) {
+        if constexpr (Epi::kBlocks) {
+            float *strip = reinterpret_cast<float *>(ring + STRIPS_AT + wave * 4096);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int jj = 0; jj < NJ; ++jj) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
+                    Epi::block(extra, it, strip, now.m0 + wm + 32 * i, now.n0 + wn + 32 * jj, now.m0 != now.n0, lane);
+                }
+        } else if constexpr (Epi::kStrip) {
             using O = typename Epi::Out;
             constexpr int W = 16 / (int)sizeof(O);                        // columns of a lane: 16 bytes of the output
             constexpr int LPR = 32 / W, RPP = 64 / LPR, ROUNDS = 32 / RPP; // lanes per row of a block, rows per access, accesses
             float *strip = reinterpret_cast<float *>(ring + STRIPS_AT + wave * 4096);
-            auto at = [&](int row, int chunk) { return reinterpret_cast<float4 *>(strip + row * 32 + ((chunk ^ (row & 7)) * 4)); };
+            auto at = [&](int row, int chunk) { return strip_at(strip, row, chunk); };
             const int sr = lane / LPR, sc = lane % LPR;
             const int64_t rm = now.m0 + wm + sr, rn = now.n0 + wn + sc * W;
             // What the epilogue reads in the output's shape comes a row of blocks ahead, and what belongs to columns and rows before all of it:
@@ -544,8 +589,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
         auto issue = [&](int s) { // the next k-tile of the stream, if there is one, into stage s
             if (left <= 0) {
                 if (!more) return;
-                ahead.at += p.stride;
-                more = ahead.seek(it, p.stride, BM, BN);
+                more = further(ahead);
                 if (!more) return;
                 aim();
             }
@@ -590,8 +634,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
             // The k-tiles ahead are awaited here, not behind the epilogue's stores (the counter runs in order): they were
             // issued before the last k-tile's products.
             TilePlace next = now;
-            next.at += p.stride;
-            const bool again = next.seek(it, p.stride, BM, BN);
+            const bool again = further(next);
             if (again) {
                 wait_counters<0, false>();
                 known = flying;
@@ -634,12 +677,11 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
                 wait_counters<63, true>();
                 barrier_no_drain(); // the next tile's first k-tile overlays the strips
             }
-            now.at += p.stride;
-        } while (now.seek(it, p.stride, BM, BN));
+        } while (further(now));
     }
 }
 
-// Tiles and workgroups of the items; false where a grid cannot hold them.
+// Tiles of the items and workgroups; false where a grid cannot hold them.
 template <typename C, typename Epi> inline bool plan_tiles(TileArgs<Epi> &p, uint32_t *blocks)
 {
     int64_t at = 0;
@@ -648,15 +690,22 @@ template <typename C, typename Epi> inline bool plan_tiles(TileArgs<Epi> &p, uin
         const int64_t mt = (it.M + C::BM - 1) / C::BM, nt = (it.N + C::BN - 1) / C::BN;
         const int64_t outer = it.n_split > 1 ? it.n_split : mt, inner = it.n_split > 1 ? mt * nt : nt;
         if (mt >= (int64_t(1) << 31) || nt >= (int64_t(1) << 31) || inner >= (int64_t(1) << 31) || it.K >= (int64_t(1) << 31)) return false;
-        if (outer > (int64_t(1) << 31) / inner) return false;
+        if (outer > (int64_t(1) << 31) / inner - 8) return false;
         it.mt = static_cast<int32_t>(mt);
         it.nt = static_cast<int32_t>(nt);
         it.block0 = static_cast<uint32_t>(at);
-        it.places = static_cast<uint32_t>((outer + 7) / 8 * 8 * inner);
+        if (Epi::kItems > 1) it.places = static_cast<uint32_t>(it.symmetric ? mt * (mt + 1) / 2 : mt * nt);
+        else it.places = static_cast<uint32_t>((outer + 7) / 8 * 8 * inner);
         at += it.places;
-        if (p.n_items > 1 && at > max_blocks(C::NT)) return false;
+        if (Epi::kItems > 1 && (it.n_split > 1 || (it.symmetric && C::BM != C::BN) || at > max_blocks(C::NT) - 8)) return false;
     }
-    *blocks = static_cast<uint32_t>(at);
+    if (Epi::kItems > 1) {
+        p.total = static_cast<uint32_t>(at);
+        p.stride = (p.total + 7) / 8;
+        *blocks = 8 * p.stride;
+    } else {
+        *blocks = static_cast<uint32_t>(at);
+    }
     return true;
 }
 
@@ -678,9 +727,7 @@ template <typename C, typename Epi> inline heta_status launch_tiles(const char *
     uint32_t blocks = 0;
     if (!plan_tiles<C>(p, &blocks)) return fail(HETA_ERR_UNSUPPORTED, "%s: matrix too large for one launch", who);
     if (blocks == 0) return HETA_OK;
-    // one item's tiles are walked by the workgroups that fit the chip; several items' get one each
-    if (p.n_items == 1) blocks = std::min(blocks, resident_tiles<C, Epi>());
-    p.stride = p.n_items == 1 ? blocks : 0x80000000u;
+    if (Epi::kItems == 1) p.stride = blocks = std::min(blocks, resident_tiles<C, Epi>()); // walked by the workgroups that fit the chip
     ProfScope prof(name, st, bytes, flops);
     hipLaunchKernelGGL((tile_gemm_kernel<C, Epi>), dim3(blocks), dim3(C::NT), 0, st, p);
     HETA_LAUNCH_CHECK("tile_gemm_kernel");
