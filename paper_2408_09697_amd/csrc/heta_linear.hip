@@ -100,7 +100,7 @@ heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void
 // ---- gradient through the activation, and the bias's ---------------------------------------------------
 // A workgroup takes a slab of rows of 256 columns: 32 lanes of eight columns, 8 rows at a time; every lane keeps the sums of
 // its columns, which are joined through LDS into the slab's row of the partials.
-template <typename E> __global__ void __launch_bounds__(256) act_grad_kernel(const E *go, int64_t ld_go, const E *pre, int64_t ld_pre, E *gp, int64_t ld_gp, int act,
+template <typename E, bool STREAM> __global__ void __launch_bounds__(256) act_grad_kernel(const E *go, int64_t ld_go, const E *pre, int64_t ld_pre, E *gp, int64_t ld_gp, int act,
                                                                             int64_t n_rows, int32_t d, int64_t rows_each, float *part, int vec, uint32_t first)
 {
     __shared__ float sums[8][256 + 8];
@@ -114,12 +114,12 @@ template <typename E> __global__ void __launch_bounds__(256) act_grad_kernel(con
 #pragma unroll 4
         for (int64_t r = slab * rows_each + ly; r < end; r += 8) {
             float g[8];
-            load8(go + r * ld_go + c, valid, vec, g);
+            load8<STREAM>(go + r * ld_go + c, valid, vec, g);
             if (gp) {
                 float x[8];
-                load8(pre + r * ld_pre + c, valid, vec, x);
+                load8<STREAM>(pre + r * ld_pre + c, valid, vec, x);
                 times_slopes(g, x, act);
-                store8(gp + r * ld_gp + c, valid, vec, g);
+                store8<STREAM>(gp + r * ld_gp + c, valid, vec, g);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[e] += g[e];
@@ -280,17 +280,18 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
     const int64_t ld_gpre = acts ? a->ld_gp : a->ld_go;
     if (n > 0 && (acts || a->dbias)) {
         const int vec = vec_rows(a->grad_out, a->ld_go, esz) && (!acts || (vec_rows(a->pre, a->ld_pre, esz) && vec_rows(a->grad_pre, a->ld_gp, esz)));
-        ProfScope prof("act_grad_kernel", st, static_cast<double>(n) * a->d_out * esz * (acts ? 3 : 1), static_cast<double>(n) * a->d_out);
-        launch_pieces(slabs * strips, 256, [&](unsigned first, unsigned count) {
-            if (a->dt == HETA_F32)
-                hipLaunchKernelGGL(act_grad_kernel<float>, dim3(count), dim3(256), 0, st, static_cast<const float *>(a->grad_out), a->ld_go,
-                                   static_cast<const float *>(a->pre), a->ld_pre, acts ? static_cast<float *>(a->grad_pre) : nullptr, a->ld_gp, a->act, n,
-                                   a->d_out, rows_each, a->dbias ? ws : nullptr, vec, first);
-            else
-                hipLaunchKernelGGL(act_grad_kernel<bf16_t>, dim3(count), dim3(256), 0, st, static_cast<const bf16_t *>(a->grad_out), a->ld_go,
-                                   static_cast<const bf16_t *>(a->pre), a->ld_pre, acts ? static_cast<bf16_t *>(a->grad_pre) : nullptr, a->ld_gp, a->act, n,
-                                   a->d_out, rows_each, a->dbias ? ws : nullptr, vec, first);
-        });
+        const double bytes = static_cast<double>(n) * a->d_out * esz * (acts ? 3 : 1);
+        ProfScope prof("act_grad_kernel", st, bytes, static_cast<double>(n) * a->d_out);
+        auto go = [&](auto tag, auto stream) {
+            using E = decltype(tag);
+            launch_pieces(slabs * strips, 256, [&](unsigned first, unsigned count) {
+                hipLaunchKernelGGL((act_grad_kernel<E, decltype(stream)::value>), dim3(count), dim3(256), 0, st, static_cast<const E *>(a->grad_out), a->ld_go,
+                                   static_cast<const E *>(a->pre), a->ld_pre, acts ? static_cast<E *>(a->grad_pre) : nullptr, a->ld_gp, a->act, n, a->d_out, rows_each,
+                                   a->dbias ? ws : nullptr, vec, first);
+            });
+        };
+        auto with = [&](auto tag) { streams(bytes) ? go(tag, std::true_type{}) : go(tag, std::false_type{}); };
+        a->dt == HETA_F32 ? with(float{}) : with(bf16_t{});
         HETA_LAUNCH_CHECK("act_grad_kernel");
     }
     if (a->dbias) HETA_TRY(fold_partials(ws, n > 0 ? slabs : 0, a->d_out, a->dbias, HETA_F32, a->d_out, a->d_out, st));

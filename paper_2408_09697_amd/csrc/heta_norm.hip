@@ -43,13 +43,16 @@ template <int LANES> __device__ __forceinline__ float lanes_max(float v)
 // Element e of chunk v of lane l: with VEC eight consecutive columns of the row, else columns LANES apart.
 template <int LANES, bool VEC> __device__ __forceinline__ int column(int v, int e, int l) { return VEC ? (v * LANES + l) * 8 + e : (v * 8 + e) * LANES + l; }
 
-template <int LANES, int NV, bool VEC, typename T> __device__ __forceinline__ void load_row(const T *row, int d, int l, float (&x)[NV][8])
+// How rows are accessed: kVec 16 bytes at a time (kStream: with the streaming hint), kSingle element by element.
+enum RowAccess { kSingle, kVec, kStream };
+
+template <int LANES, int NV, int ACC, typename T> __device__ __forceinline__ void load_row(const T *row, int d, int l, float (&x)[NV][8])
 {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        if constexpr (VEC) {
+        if constexpr (ACC != kSingle) {
             const int c = column<LANES, true>(v, 0, l);
-            load8(row + c, d - c, true, x[v]);
+            load8<ACC == kStream>(row + c, d - c, true, x[v]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -59,13 +62,13 @@ template <int LANES, int NV, bool VEC, typename T> __device__ __forceinline__ vo
         }
     }
 }
-template <int LANES, int NV, bool VEC, typename T> __device__ __forceinline__ void store_row(T *row, int d, int l, const float (&x)[NV][8])
+template <int LANES, int NV, int ACC, typename T> __device__ __forceinline__ void store_row(T *row, int d, int l, const float (&x)[NV][8])
 {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        if constexpr (VEC) {
+        if constexpr (ACC != kSingle) {
             const int c = column<LANES, true>(v, 0, l);
-            store8(row + c, d - c, true, x[v]);
+            store8<ACC == kStream>(row + c, d - c, true, x[v]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -112,8 +115,9 @@ template <typename T> __device__ __forceinline__ float rounded(float v)
 }
 
 // T: type of x, residual and sum; O: of the output (uint8_t: e4m3)
-template <typename T, typename O, int LANES, int NV, bool VEC> __global__ void __launch_bounds__(256) rms_norm_kernel(NormFwd p)
+template <typename T, typename O, int LANES, int NV, int ACC> __global__ void __launch_bounds__(256) rms_norm_kernel(NormFwd p)
 {
+    constexpr bool VEC = ACC != kSingle;
     constexpr int GROUPS = 256 / LANES;
     const int l = threadIdx.x % LANES, grp = threadIdx.x / LANES;
     float gamma[NV][8];
@@ -126,16 +130,16 @@ template <typename T, typename O, int LANES, int NV, bool VEC> __global__ void _
         }
     for (int64_t r = static_cast<int64_t>(blockIdx.x) * GROUPS + grp; r < p.n_rows; r += static_cast<int64_t>(gridDim.x) * GROUPS) {
         float x[NV][8];
-        load_row<LANES, NV, VEC>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, x);
+        load_row<LANES, NV, ACC>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, x);
         if (p.residual) {
             float y[NV][8];
-            load_row<LANES, NV, VEC>(static_cast<const T *>(p.residual) + r * p.ld_res, p.d, l, y);
+            load_row<LANES, NV, ACC>(static_cast<const T *>(p.residual) + r * p.ld_res, p.d, l, y);
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[v][e] = rounded<T>(x[v][e] + y[v][e]);
         }
-        if (p.sum) store_row<LANES, NV, VEC>(static_cast<T *>(p.sum) + r * p.ld_sum, p.d, l, x);
+        if (p.sum) store_row<LANES, NV, ACC>(static_cast<T *>(p.sum) + r * p.ld_sum, p.d, l, x);
         float ss = 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
@@ -157,7 +161,7 @@ template <typename T, typename O, int LANES, int NV, bool VEC> __global__ void _
             if (l == 0) p.scale[r] = amax / 448.f;
             store_row_e4m3<LANES, NV, VEC>(static_cast<uint8_t *>(p.out) + r * p.ld_out, p.d, l, x, e4m3_factor(amax));
         } else {
-            store_row<LANES, NV, VEC>(static_cast<O *>(p.out) + r * p.ld_out, p.d, l, x);
+            store_row<LANES, NV, ACC>(static_cast<O *>(p.out) + r * p.ld_out, p.d, l, x);
         }
     }
 }
@@ -224,8 +228,9 @@ struct NormBwd {
     int32_t d;
 };
 
-template <typename T, typename G, int LANES, int NV, bool VEC> __global__ void __launch_bounds__(256) rms_norm_bwd_kernel(NormBwd p)
+template <typename T, typename G, int LANES, int NV, int ACC> __global__ void __launch_bounds__(256) rms_norm_bwd_kernel(NormBwd p)
 {
+    constexpr bool VEC = ACC != kSingle;
     constexpr int GROUPS = 256 / LANES;
     __shared__ float joined[GROUPS * LANES * NV * 8];
     const int l = threadIdx.x % LANES, grp = threadIdx.x / LANES;
@@ -241,8 +246,8 @@ template <typename T, typename G, int LANES, int NV, bool VEC> __global__ void _
     const float inv_d = 1.f / static_cast<float>(p.d);
     for (int64_t r = static_cast<int64_t>(blockIdx.x) * GROUPS + grp; r < p.n_rows; r += static_cast<int64_t>(gridDim.x) * GROUPS) {
         float h[NV][8], w[NV][8];
-        load_row<LANES, NV, VEC>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, h);
-        load_row<LANES, NV, VEC>(static_cast<const G *>(p.grad_out) + r * p.ld_go, p.d, l, w);
+        load_row<LANES, NV, ACC>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, h);
+        load_row<LANES, NV, ACC>(static_cast<const G *>(p.grad_out) + r * p.ld_go, p.d, l, w);
         const float rstd = p.rstd[r];
         float dot = 0.f;
 #pragma unroll
@@ -260,13 +265,13 @@ template <typename T, typename G, int LANES, int NV, bool VEC> __global__ void _
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[v][e] = rstd * (w[v][e] - h[v][e] * dot);
         if (p.grad_sum) {
-            load_row<LANES, NV, VEC>(static_cast<const T *>(p.grad_sum) + r * p.ld_gs, p.d, l, h);
+            load_row<LANES, NV, ACC>(static_cast<const T *>(p.grad_sum) + r * p.ld_gs, p.d, l, h);
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[v][e] += h[v][e];
         }
-        store_row<LANES, NV, VEC>(static_cast<T *>(p.grad_x) + r * p.ld_gx, p.d, l, w);
+        store_row<LANES, NV, ACC>(static_cast<T *>(p.grad_x) + r * p.ld_gx, p.d, l, w);
     }
     if (!p.part) return;
 #pragma unroll
@@ -330,32 +335,37 @@ template <typename F, typename W> static void by_width(int32_t d, F f, W wide)
     else if (d <= 2048) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
     else wide();
 }
+// Workgroups at most, each walking over rows.  1.1 M rows of 256 bf16 columns to 8 bits, with 2,048 / 4,096 / 16,384 workgroups and one per 8
+// rows: 483 / 427 / 391 / 590 us, and 366 with 16,384 and the streaming hint; to bf16 434 / 450 / 469 / 542 and 402.  Backward of
+// 700,000 rows with 1,024 / 2,048 / 4,096 / 8,192: 290 / 320 / 284 / 301 us, and 259 with 4,096 and the hint.
+constexpr int64_t kNormBlocks = 16384, kNormBwdBlocks = 4096;
 static unsigned row_blocks(int64_t n_rows, int groups, int64_t most) { return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n_rows + groups - 1) / groups, most))); }
 
-template <typename T, typename O> static void launch_norm(const NormFwd &p, bool vec, hipStream_t st)
+template <typename T, typename O> static void launch_norm(const NormFwd &p, RowAccess acc, hipStream_t st)
 {
     by_width(
         p.d,
         [&](auto lanes, auto nv) {
             constexpr int L = decltype(lanes)::value, V = decltype(nv)::value;
-            const dim3 grid(row_blocks(p.n_rows, 256 / L, 4096));
-            if (vec) hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, true>), grid, dim3(256), 0, st, p);
-            else hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, false>), grid, dim3(256), 0, st, p);
+            const dim3 grid(row_blocks(p.n_rows, 256 / L, kNormBlocks));
+            if (acc == kStream) hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, kStream>), grid, dim3(256), 0, st, p);
+            else if (acc == kVec) hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, kVec>), grid, dim3(256), 0, st, p);
+            else hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, kSingle>), grid, dim3(256), 0, st, p);
         },
         [&] { hipLaunchKernelGGL((rms_norm_wide_kernel<T, O>), dim3(row_blocks(p.n_rows, 1, 8192)), dim3(256), 0, st, p); });
 }
 
-constexpr int64_t kNormBwdBlocks = 2048;
 
-template <typename T, typename G> static void launch_norm_bwd(const NormBwd &p, bool vec, int64_t n_part, hipStream_t st)
+template <typename T, typename G> static void launch_norm_bwd(const NormBwd &p, RowAccess acc, int64_t n_part, hipStream_t st)
 {
     by_width(
         p.d,
         [&](auto lanes, auto nv) {
             constexpr int L = decltype(lanes)::value, V = decltype(nv)::value;
             const dim3 grid(static_cast<unsigned>(n_part));
-            if (vec) hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, true>), grid, dim3(256), 0, st, p);
-            else hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, false>), grid, dim3(256), 0, st, p);
+            if (acc == kStream) hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, kStream>), grid, dim3(256), 0, st, p);
+            else if (acc == kVec) hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, kVec>), grid, dim3(256), 0, st, p);
+            else hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, kSingle>), grid, dim3(256), 0, st, p);
         },
         [&] {
             hipLaunchKernelGGL((rms_norm_bwd_wide_kernel<T, G>), dim3(row_blocks(p.n_rows, 1, 8192)), dim3(256), 0, st, p);
@@ -404,14 +414,16 @@ extern "C" heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, h
     const bool vec = vec_rows(x, ld_x, esz) && vec_rows(residual, ld_res, esz) && vec_rows(sum, ld_sum, esz) &&
                      (q ? ld_out % 8 == 0 && reinterpret_cast<uintptr_t>(out) % 8 == 0 : vec_rows(out, ld_out, osz));
     hipStream_t st = as_stream(hip_stream);
-    ProfScope prof("rms_norm_kernel", st, static_cast<double>(n_rows) * d * (esz * (1.0 + !!residual + !!sum) + osz), 6.0 * n_rows * d);
+    const double bytes = static_cast<double>(n_rows) * d * (esz * (1.0 + !!residual + !!sum) + osz);
+    const RowAccess acc = !vec ? kSingle : streams(bytes) ? kStream : kVec;
+    ProfScope prof("rms_norm_kernel", st, bytes, 6.0 * n_rows * d);
     if (x_dt == HETA_F32) {
-        if (q) launch_norm<float, uint8_t>(p, vec, st);
-        else if (out_dt == HETA_F32) launch_norm<float, float>(p, vec, st);
-        else launch_norm<float, bf16_t>(p, vec, st);
+        if (q) launch_norm<float, uint8_t>(p, acc, st);
+        else if (out_dt == HETA_F32) launch_norm<float, float>(p, acc, st);
+        else launch_norm<float, bf16_t>(p, acc, st);
     } else {
-        if (q) launch_norm<bf16_t, uint8_t>(p, vec, st);
-        else launch_norm<bf16_t, bf16_t>(p, vec, st);
+        if (q) launch_norm<bf16_t, uint8_t>(p, acc, st);
+        else launch_norm<bf16_t, bf16_t>(p, acc, st);
     }
     HETA_LAUNCH_CHECK("rms_norm_kernel");
     return HETA_OK;
@@ -447,10 +459,12 @@ extern "C" heta_status heta_rms_norm_bwd(heta_graph *g, int64_t n_rows, int32_t 
     if (n_rows > 0) {
         const NormBwd p{x, grad_out, grad_sum, grad_x, gamma, rstd, part, ld_x, ld_go, ld_gs, ld_gx, n_rows, d};
         const bool vec = vec_rows(x, ld_x, esz) && vec_rows(grad_out, ld_go, gsz) && vec_rows(grad_sum, ld_gs, esz) && vec_rows(grad_x, ld_gx, esz);
-        ProfScope prof("rms_norm_bwd_kernel", st, static_cast<double>(n_rows) * d * (esz * (2.0 + !!grad_sum) + gsz), 9.0 * n_rows * d);
-        if (x_dt == HETA_BF16) launch_norm_bwd<bf16_t, bf16_t>(p, vec, n_part, st);
-        else if (go_dt == HETA_F32) launch_norm_bwd<float, float>(p, vec, n_part, st);
-        else launch_norm_bwd<float, bf16_t>(p, vec, n_part, st);
+        const double bytes = static_cast<double>(n_rows) * d * (esz * (2.0 + !!grad_sum) + gsz);
+        const RowAccess acc = !vec ? kSingle : streams(bytes) ? kStream : kVec;
+        ProfScope prof("rms_norm_bwd_kernel", st, bytes, 9.0 * n_rows * d);
+        if (x_dt == HETA_BF16) launch_norm_bwd<bf16_t, bf16_t>(p, acc, n_part, st);
+        else if (go_dt == HETA_F32) launch_norm_bwd<float, float>(p, acc, n_part, st);
+        else launch_norm_bwd<float, bf16_t>(p, acc, n_part, st);
         HETA_LAUNCH_CHECK("rms_norm_bwd_kernel");
     }
     return grad_gamma ? fold_partials(part, n_part, d, grad_gamma, HETA_F32, d, d, st) : HETA_OK;

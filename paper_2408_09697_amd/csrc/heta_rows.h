@@ -9,52 +9,75 @@ namespace heta {
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(bf16_t x) { return __uint_as_float(static_cast<uint32_t>(x) << 16); }
 
-__device__ __forceinline__ void load8(const float *p, int valid, bool vec, float (&v)[8])
+// 16 bytes; STREAM: with the hint that they will not be needed again soon
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+template <bool STREAM> __device__ __forceinline__ uintx4 load16(const void *p)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const uintx4 *>(p));
+    else return *static_cast<const uintx4 *>(p);
+}
+template <bool STREAM> __device__ __forceinline__ void store16(void *p, uintx4 v)
+{
+    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<uintx4 *>(p));
+    else *static_cast<uintx4 *>(p) = v;
+}
+
+template <bool STREAM = false> __device__ __forceinline__ void load8(const float *p, int valid, bool vec, float (&v)[8])
 {
     if (vec && valid >= 8) {
-        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        const uintx4 a = load16<STREAM>(p), b = load16<STREAM>(p + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = __uint_as_float(a[j]);
+            v[4 + j] = __uint_as_float(b[j]);
+        }
         return;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < valid ? p[e] : 0.f;
 }
-__device__ __forceinline__ void load8(const bf16_t *p, int valid, bool vec, float (&v)[8])
+template <bool STREAM = false> __device__ __forceinline__ void load8(const bf16_t *p, int valid, bool vec, float (&v)[8])
 {
     if (vec && valid >= 8) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+        const uintx4 a = load16<STREAM>(p);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            v[2 * j] = __uint_as_float(w[j] << 16);
-            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            v[2 * j] = __uint_as_float(a[j] << 16);
+            v[2 * j + 1] = __uint_as_float(a[j] & 0xffff0000u);
         }
         return;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < valid ? widen(p[e]) : 0.f;
 }
-__device__ __forceinline__ void store8(float *p, int valid, bool vec, const float (&v)[8])
+template <bool STREAM = false> __device__ __forceinline__ void store8(float *p, int valid, bool vec, const float (&v)[8])
 {
     if (vec && valid >= 8) {
-        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        const uintx4 a = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        const uintx4 b = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+        store16<STREAM>(p, a);
+        store16<STREAM>(p + 4, b);
         return;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (e < valid) p[e] = v[e];
 }
-__device__ __forceinline__ void store8(bf16_t *p, int valid, bool vec, const float (&v)[8])
+template <bool STREAM = false> __device__ __forceinline__ void store8(bf16_t *p, int valid, bool vec, const float (&v)[8])
 {
     if (vec && valid >= 8) {
-        *reinterpret_cast<uint4 *>(p) = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
+        const uintx4 a = {pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+        store16<STREAM>(p, a);
         return;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (e < valid) p[e] = static_cast<bf16_t>(pack2_bf16(v[e], v[e]) & 0xffffu);
 }
+
+// Calls that move more than the chip's 256 MB last-level cache holds read and write with the streaming hint; below, what a
+// call writes is still cached when the next one reads it.
+inline bool streams(double bytes) { return bytes > 256e6; }
 
 // rows of `ld` elements from p on that can be moved 16 bytes at a time (a null pointer can: it is not read)
 inline bool vec_rows(const void *p, int64_t ld, size_t elt) { return !p || (aligned16(p) && (ld * static_cast<int64_t>(elt)) % 16 == 0); }
