@@ -99,11 +99,13 @@ heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void
 
 // ---- gradient through the activation, and the bias's ---------------------------------------------------
 // A workgroup takes a slab of rows of 256 columns: 32 lanes of eight columns, 8 rows at a time; every lane keeps the sums of
-// its columns, which are joined through LDS into the slab's row of the partials.
-template <typename E, bool STREAM> __global__ void __launch_bounds__(256) act_grad_kernel(const E *go, int64_t ld_go, const E *pre, int64_t ld_pre, E *gp, int64_t ld_gp, int act,
-                                                                            int64_t n_rows, int32_t d, int64_t rows_each, float *part, int vec, uint32_t first)
+// its columns, which are joined through LDS into the slab's row of the partials.  Four rows are read before the first is
+// worked on.  ACT = NONE: sums alone.
+template <typename E, int ACT, bool STREAM> __global__ void __launch_bounds__(256) act_grad_kernel(const E *go, int64_t ld_go, const E *pre, int64_t ld_pre, E *gp, int64_t ld_gp,
+                                                                                                  int64_t n_rows, int32_t d, int64_t rows_each, float *part, int vec, uint32_t first)
 {
     __shared__ float sums[8][256 + 8];
+    constexpr bool ACTS = ACT != HETA_ACT_NONE;
     const int lx = threadIdx.x & 31, ly = threadIdx.x >> 5;
     const uint32_t strips = (d + 255) / 256, b = first + blockIdx.x;
     const int64_t slab = b / strips;
@@ -111,19 +113,27 @@ template <typename E, bool STREAM> __global__ void __launch_bounds__(256) act_gr
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (valid > 0) {
         const int64_t end = min(n_rows, (slab + 1) * rows_each);
-#pragma unroll 4
-        for (int64_t r = slab * rows_each + ly; r < end; r += 8) {
-            float g[8];
-            load8<STREAM>(go + r * ld_go + c, valid, vec, g);
-            if (gp) {
-                float x[8];
-                load8<STREAM>(pre + r * ld_pre + c, valid, vec, x);
-                times_slopes(g, x, act);
-                store8<STREAM>(gp + r * ld_gp + c, valid, vec, g);
+        auto rows = [&](int64_t r, auto count) {
+            constexpr int N = decltype(count)::value;
+            float g[N][8], x[ACTS ? N : 1][8];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                load8<STREAM>(go + (r + 8 * i) * ld_go + c, valid, vec, g[i]);
+                if constexpr (ACTS) load8<STREAM>(pre + (r + 8 * i) * ld_pre + c, valid, vec, x[i]);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += g[e];
-        }
+            for (int i = 0; i < N; ++i) {
+                if constexpr (ACTS) {
+                    times_slopes(g[i], x[i], ACT);
+                    store8<STREAM>(gp + (r + 8 * i) * ld_gp + c, valid, vec, g[i]);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e] += g[i][e];
+            }
+        };
+        int64_t r = slab * rows_each + ly;
+        for (; r + 24 < end; r += 32) rows(r, std::integral_constant<int, 4>{});
+        for (; r < end; r += 8) rows(r, std::integral_constant<int, 1>{});
     }
     if (!part) return;
 #pragma unroll
@@ -282,16 +292,16 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
         const int vec = vec_rows(a->grad_out, a->ld_go, esz) && (!acts || (vec_rows(a->pre, a->ld_pre, esz) && vec_rows(a->grad_pre, a->ld_gp, esz)));
         const double bytes = static_cast<double>(n) * a->d_out * esz * (acts ? 3 : 1);
         ProfScope prof("act_grad_kernel", st, bytes, static_cast<double>(n) * a->d_out);
-        auto go = [&](auto tag, auto stream) {
+        auto go = [&](auto tag, auto act, auto stream) {
             using E = decltype(tag);
             launch_pieces(slabs * strips, 256, [&](unsigned first, unsigned count) {
-                hipLaunchKernelGGL((act_grad_kernel<E, decltype(stream)::value>), dim3(count), dim3(256), 0, st, static_cast<const E *>(a->grad_out), a->ld_go,
-                                   static_cast<const E *>(a->pre), a->ld_pre, acts ? static_cast<E *>(a->grad_pre) : nullptr, a->ld_gp, a->act, n, a->d_out, rows_each,
-                                   a->dbias ? ws : nullptr, vec, first);
+                hipLaunchKernelGGL((act_grad_kernel<E, decltype(act)::value, decltype(stream)::value>), dim3(count), dim3(256), 0, st, static_cast<const E *>(a->grad_out), a->ld_go,
+                                   static_cast<const E *>(a->pre), a->ld_pre, static_cast<E *>(a->grad_pre), a->ld_gp, n, a->d_out, rows_each, a->dbias ? ws : nullptr, vec, first);
             });
+            return HETA_OK;
         };
-        auto with = [&](auto tag) { streams(bytes) ? go(tag, std::true_type{}) : go(tag, std::false_type{}); };
-        a->dt == HETA_F32 ? with(float{}) : with(bf16_t{});
+        auto with = [&](auto tag) { return with_act(a->act, [&](auto act) { return streams(bytes) ? go(tag, act, std::true_type{}) : go(tag, act, std::false_type{}); }); };
+        (void)(a->dt == HETA_F32 ? with(float{}) : with(bf16_t{}));
         HETA_LAUNCH_CHECK("act_grad_kernel");
     }
     if (a->dbias) HETA_TRY(fold_partials(ws, n > 0 ? slabs : 0, a->d_out, a->dbias, HETA_F32, a->d_out, a->d_out, st));

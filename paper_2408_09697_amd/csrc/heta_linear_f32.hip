@@ -9,8 +9,8 @@ template <bool A_RC, bool B_RC> using Elements = TileShape<float, 2, 3, A_RC, B_
 
 heta_status launch_linear_f32(const Launch &l, bool input_gradient, const LinearExtra &x)
 {
-    if (input_gradient) return launch_linear<Large<false, false>, Small<false, false>, Elements<false, false>, float, true>(l, 4, x);
-    return launch_linear<Large<false, true>, Small<false, true>, Elements<false, true>, float, false>(l, 4, x);
+    if (input_gradient) return launch_linear<Large<false, false>, Large<false, false>, Small<false, false>, Elements<false, false>, float, true>(l, 4, x);
+    return launch_linear<Large<false, true>, Large<false, true>, Small<false, true>, Elements<false, true>, float, false>(l, 4, x);
 }
 heta_status launch_grad_w_f32(const Launch &l, float *part) { return launch_grad_w<Large<true, true>, Small<true, true>, Elements<true, true>>(l, 4, part); }
 

@@ -253,6 +253,13 @@ template <typename O> __device__ __forceinline__ void unpack16(uint4 raw, float 
     }
 }
 
+template <bool STREAM> __device__ __forceinline__ void store_chunk(void *p, uint4 v)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    if constexpr (STREAM) __builtin_nontemporal_store(words{v.x, v.y, v.z, v.w}, static_cast<words *>(p));
+    else *static_cast<uint4 *>(p) = v;
+}
+
 // four columns (chunk 0..7) of a row of a 32 x 32 fp32 strip
 __device__ __forceinline__ float4 *strip_at(float *strip, int row, int chunk) { return reinterpret_cast<float4 *>(strip + row * 32 + ((chunk ^ (row & 7)) * 4)); }
 
@@ -318,6 +325,7 @@ struct TilePlace {
 //   kStrip = true (Out rows of whole, aligned 16-byte pieces): with W = 16 bytes of columns, first(cols, row, y) makes
 //     pre-activations of W sums and second(x, y, t) results, t being W elements of x.other (if kReads; zeros or nothing where it
 //     is null); x.pre (if kPre and not null) and out(x, it, split) receive them, rows x.ld_pre and x.ld_out apart.
+//     kStream: with the streaming hint.
 //     struct Cols, Row { void load(const Extra &x, int64_t n, int64_t N); } are what a lane keeps of W columns and of a row (which
 //     may lie beyond the matrix).
 template <typename Epi> struct TileArgs {
@@ -539,7 +547,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
                         float t[W];
                         if constexpr (Epi::kReads) unpack16<O>(other[i & 1][jj][r], t);
                         Epi::second(extra, y, t);
-                        *reinterpret_cast<uint4 *>(out + m * extra.ld_out + n) = pack16<O>(y);
+                        store_chunk<Epi::kStream>(out + m * extra.ld_out + n, pack16<O>(y));
                     }
                 }
             }
