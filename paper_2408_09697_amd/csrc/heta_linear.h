@@ -4,7 +4,6 @@
 
 #include <algorithm>
 
-#include "heta_rows.h"
 #include "heta_tiles.h"
 
 namespace heta {
@@ -70,16 +69,15 @@ struct LinearExtra {
     void *pre, *out_p;                      // pre nullable
     int64_t ld_other, ld_pre, ld_out;
     int act, slope_act;                     // slope_act != NONE: other is a pre-activation
-    int vec; // every array in the output's shape can be moved 16 bytes at a time
 };
-// O: type of the outputs and of what is read in their shape.  WHOLE: their rows are whole 16-byte pieces (aligned, a multiple
-// of eight columns) and pass through strips.  SCALED: 8-bit operands.  ACT, SLOPE: which activation, and whose slope, or
-// kAnyAct for a choice at run time (tiles with one block per wavefront): with everything left to run time the epilogue of a
-// large tile is 11,000 instructions long and takes longer than the product.  READS: whether `other` may be there.
+// O: type of the outputs and of what is read in their shape.  SCALED: 8-bit operands.  ACT, SLOPE: which activation, and whose
+// slope, or kAnyAct for a choice at run time (small tiles): with it the epilogue of a large tile is 11,000 instructions long
+// and takes longer than the product.  READS: whether `other` may be there.  WHOLE: the output is whole 16-byte pieces wide (without
+// it the epilogues of large tiles cost 5 to 14 % of a product).
 constexpr int kAnyAct = -1;
-template <typename O, bool WHOLE, bool SCALED, int ACT = kAnyAct, int SLOPE = kAnyAct, bool READS = true> struct LinearEpi {
+template <typename O, bool SCALED, int ACT = kAnyAct, int SLOPE = kAnyAct, bool READS = true, bool WHOLE = false> struct LinearEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kBlocks = false, kStrip = WHOLE, kReads = READS, kPre = SLOPE <= 0;
+    static constexpr bool kBlocks = false, kReads = READS, kPre = SLOPE <= 0, kWhole = WHOLE;
     // large tiles of 8-bit operands store with the streaming hint: their weights then stay in the L2s (200,000 x 1,024 x 4,096:
     // 1,294 -> 1,103 us; products of bf16 operands are as fast without)
     static constexpr bool kStream = SCALED && ACT != kAnyAct;
@@ -95,9 +93,10 @@ template <typename O, bool WHOLE, bool SCALED, int ACT = kAnyAct, int SLOPE = kA
                 bias[e] = 0.f;
                 if constexpr (SCALED) scale[e] = 0.f;
             }
-            if (n >= N) return;
+            if (WHOLE && n >= N) return;
 #pragma unroll
             for (int e = 0; e < W; ++e) {
+                if (!WHOLE && n + e >= N) continue;
                 if (x.bias) bias[e] = x.bias[n + e];
                 if constexpr (SCALED) scale[e] = x.w_scale[n + e];
             }
@@ -130,30 +129,12 @@ template <typename O, bool WHOLE, bool SCALED, int ACT = kAnyAct, int SLOPE = kA
             for (int e = 0; e < N; ++e) y[e] += t[e];
         }
     }
-    __device__ __forceinline__ static void put(const Extra &x, const TileItem &, int64_t m, int64_t n, int valid, float (&y)[8], int)
-    {
-        float t[8] = {}, s[8];
-        if constexpr (SCALED) {
-            load8(x.w_scale + n, valid, false, s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] *= x.in_scale[m] * s[e];
-        }
-        if (x.bias) {
-            load8(x.bias + n, valid, false, s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] += s[e];
-        }
-        if (x.pre) store8(static_cast<O *>(x.pre) + m * x.ld_pre + n, valid, x.vec, y);
-        if (x.other) load8(static_cast<const O *>(x.other) + m * x.ld_other + n, valid, x.vec, t);
-        second(x, y, t);
-        store8(static_cast<O *>(x.out_p) + m * x.ld_out + n, valid, x.vec, y);
-    }
 };
 
-// partial products of a contraction that is split over its rows: [split][M][N] fp32.  WHOLE: N is a multiple of four
-template <bool WHOLE> struct PartialEpi {
+// partial products of a contraction that is split over its rows: [split][M][N] fp32
+struct PartialEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kBlocks = false, kStrip = WHOLE, kReads = false, kPre = false, kStream = false;
+    static constexpr bool kBlocks = false, kReads = false, kPre = false, kStream = false, kWhole = false;
     using Out = float;
     struct Extra {
         float *part;
@@ -166,11 +147,37 @@ template <bool WHOLE> struct PartialEpi {
     __device__ __forceinline__ static float *out(const Extra &x, const TileItem &it, int split) { return x.part + split * it.M * it.N; }
     __device__ __forceinline__ static void first(const Cols &, const Row &, float (&)[4]) {}
     __device__ __forceinline__ static void second(const Extra &, float (&)[4], const float (&)[4]) {}
-    __device__ __forceinline__ static void put(const Extra &x, const TileItem &it, int64_t m, int64_t n, int valid, const float (&v)[8], int split)
-    {
-        store8(x.part + (split * it.M + m) * it.N + n, valid, false, v);
-    }
 };
+
+// The rest of a product whose contraction was split: the partial products of 16 bytes of outputs added in order, and the epilogue.
+template <typename O, bool SCALED> __global__ void __launch_bounds__(256) linear_finish_kernel(LinearExtra x, const float *part, int n_split, int64_t M, int64_t N)
+{
+    using Epi = LinearEpi<O, SCALED>;
+    constexpr int W = Epi::W;
+    const int64_t per_row = (N + W - 1) / W, at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, m = at / per_row, n = (at - m * per_row) * W;
+    if (m >= M) return;
+    const int valid = static_cast<int>(min(N - n, static_cast<int64_t>(W)));
+    typename Epi::Cols cols;
+    typename Epi::Row row;
+    cols.load(x, n, N);
+    row.load(x, m, M);
+    float y[W], t[W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) y[e] = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < n_split; ++s)
+#pragma unroll
+        for (int h = 0; h < W; h += 4) {
+            const uintx4 q = load_piece(part + (s * M + m) * N + n + h, valid - h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[h + e] += __uint_as_float(q[e]);
+        }
+    unpack16<O>(x.other ? load_piece(static_cast<const O *>(x.other) + m * x.ld_other + n, valid) : uintx4{0u, 0u, 0u, 0u}, t);
+    Epi::first(cols, row, y);
+    if (x.pre) store_piece(static_cast<O *>(x.pre) + m * x.ld_pre + n, valid, pack16<O>(y));
+    Epi::second(x, y, t);
+    store_piece(static_cast<O *>(x.out_p) + m * x.ld_out + n, valid, pack16<O>(y));
+}
 
 // rows that can go straight into LDS: 16-byte aligned, and a tile's rows within 32-bit offsets
 inline bool direct_rows(const void *p, int64_t ld, size_t elt) { return aligned16(p) && (ld * static_cast<int64_t>(elt)) % 16 == 0 && ld * static_cast<int64_t>(elt) < (int64_t(1) << 23); }
@@ -179,6 +186,7 @@ inline int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return (M + bm -
 
 // One product; large tiles where they give every second CU one.
 struct Launch {
+    heta_graph *g;
     const char *who, *name;
     TileItem it;
     double bytes, flops;
@@ -207,29 +215,47 @@ heta_status launch_grad_w_f32(const Launch &l, float *part);
 heta_status launch_grad_w_bf16(const Launch &l, float *part);
 
 // one type's launches from its tile shapes: large tiles (Reading: where the epilogue reads in the output's shape), small ones, and
-// those for rows that cannot go straight into LDS
-template <typename Large, typename Reading, typename Small, typename Elements, typename O, bool SLOPES> inline heta_status launch_linear(const Launch &l, size_t elt, const LinearExtra &x)
+// both for rows that cannot go straight into LDS
+template <typename Large, typename Reading, typename Small, typename StagedLarge, typename StagedSmall, typename O, bool SLOPES>
+inline heta_status launch_linear(const Launch &l, size_t elt, const LinearExtra &x)
 {
-    const bool whole = x.vec && l.it.N % 8 == 0;
     constexpr bool SCALED = Large::EB == 1;
-    if (!l.direct(elt)) return l.go<Elements, LinearEpi<O, false, SCALED>>(x);
-    if (!whole) return l.go<Small, LinearEpi<O, false, SCALED>>(x);
-    if (!l.large()) return l.go<Small, LinearEpi<O, true, SCALED>>(x);
+    const bool direct = l.direct(elt);
+    if (!l.large()) {
+        // Few tiles and a long contraction: it is split so that a workgroup has about eight k-tiles and most of the chip one
+        // workgroup; a second launch adds the parts up and does the epilogue (114 x 1,611 x 7: 114 -> 15 us).
+        const int64_t tiles = tiles_of(l.it.M, l.it.N, Small::BM, Small::BN), k_tiles = (l.it.K + Small::BK - 1) / Small::BK;
+        const int64_t splits = std::min(k_tiles / 8, 256 / tiles);
+        if (splits >= 2) {
+            Launch part = l;
+            part.it.k_per_split = (k_tiles + splits - 1) / splits * Small::BK;
+            part.it.n_split = static_cast<int32_t>((l.it.K + part.it.k_per_split - 1) / part.it.k_per_split);
+            HETA_TRY(ensure_workspace(l.g, static_cast<size_t>(part.it.n_split) * l.it.M * l.it.N * sizeof(float)));
+            float *ws = static_cast<float *>(l.g->d_ws);
+            const PartialEpi::Extra px{ws, l.it.N};
+            HETA_TRY((direct ? part.go<Small, PartialEpi>(px) : part.go<StagedSmall, PartialEpi>(px)));
+            constexpr int W = 16 / (int)sizeof(O);
+            const int64_t blocks = (l.it.M * ((l.it.N + W - 1) / W) + 255) / 256;
+            ProfScope prof("linear_finish_kernel", l.st, static_cast<double>(l.it.M) * l.it.N * (4.0 * part.it.n_split + sizeof(O)), 0);
+            hipLaunchKernelGGL((linear_finish_kernel<O, SCALED>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, l.st, x, ws, part.it.n_split, l.it.M, l.it.N);
+            HETA_LAUNCH_CHECK("linear_finish_kernel");
+            return HETA_OK;
+        }
+        return direct ? l.go<Small, LinearEpi<O, SCALED>>(x) : l.go<StagedSmall, LinearEpi<O, SCALED>>(x);
+    }
+    if (!direct && !std::is_same<StagedLarge, Large>::value) return l.go<StagedLarge, LinearEpi<O, SCALED>>(x);
+    if (l.it.N % (16 / (int)sizeof(O)) != 0) return l.go<Reading, LinearEpi<O, SCALED>>(x);
     return with_act(SLOPES ? x.slope_act : x.act, [&](auto a) {
         constexpr int A = decltype(a)::value;
-        if constexpr (SLOPES) return l.go<Large, LinearEpi<O, true, SCALED, HETA_ACT_NONE, A, A != HETA_ACT_NONE>>(x);
-        else return x.other ? l.go<Reading, LinearEpi<O, true, SCALED, A, HETA_ACT_NONE, true>>(x) : l.go<Large, LinearEpi<O, true, SCALED, A, HETA_ACT_NONE, false>>(x);
+        if constexpr (SLOPES) return l.go<Large, LinearEpi<O, SCALED, HETA_ACT_NONE, A, A != HETA_ACT_NONE, true>>(x);
+        else return x.other ? l.go<Reading, LinearEpi<O, SCALED, A, HETA_ACT_NONE, true, true>>(x) : l.go<Large, LinearEpi<O, SCALED, A, HETA_ACT_NONE, false, true>>(x);
     });
 }
-template <typename Large, typename Small, typename Elements> inline heta_status launch_grad_w(const Launch &l, size_t elt, float *part)
+template <typename Large, typename Small, typename StagedLarge, typename StagedSmall> inline heta_status launch_grad_w(const Launch &l, size_t elt, float *part)
 {
-    auto with = [&](auto whole) {
-        using Epi = PartialEpi<decltype(whole)::value>;
-        const typename Epi::Extra x{part, l.it.N};
-        if (!l.direct(elt)) return l.go<Elements, Epi>(x);
-        return l.large() ? l.go<Large, Epi>(x) : l.go<Small, Epi>(x);
-    };
-    return l.it.N % 4 == 0 ? with(std::true_type{}) : with(std::false_type{});
+    const PartialEpi::Extra x{part, l.it.N};
+    if (l.direct(elt)) return l.large() ? l.go<Large, PartialEpi>(x) : l.go<Small, PartialEpi>(x);
+    return l.large() ? l.go<StagedLarge, PartialEpi>(x) : l.go<StagedSmall, PartialEpi>(x);
 }
 
 } // namespace heta

@@ -102,7 +102,7 @@ heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void
 // its columns, which are joined through LDS into the slab's row of the partials.  Four rows are read before the first is
 // worked on.  ACT = NONE: sums alone.
 template <typename E, int ACT, bool STREAM> __global__ void __launch_bounds__(256) act_grad_kernel(const E *go, int64_t ld_go, const E *pre, int64_t ld_pre, E *gp, int64_t ld_gp,
-                                                                                                  int64_t n_rows, int32_t d, int64_t rows_each, float *part, int vec, uint32_t first)
+                                                                                                  int64_t n_rows, int32_t d, int64_t rows_each, float *part, uint32_t first)
 {
     __shared__ float sums[8][256 + 8];
     constexpr bool ACTS = ACT != HETA_ACT_NONE;
@@ -118,14 +118,14 @@ template <typename E, int ACT, bool STREAM> __global__ void __launch_bounds__(25
             float g[N][8], x[ACTS ? N : 1][8];
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                load8<STREAM>(go + (r + 8 * i) * ld_go + c, valid, vec, g[i]);
-                if constexpr (ACTS) load8<STREAM>(pre + (r + 8 * i) * ld_pre + c, valid, vec, x[i]);
+                load8<STREAM>(go + (r + 8 * i) * ld_go + c, valid, g[i]);
+                if constexpr (ACTS) load8<STREAM>(pre + (r + 8 * i) * ld_pre + c, valid, x[i]);
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 if constexpr (ACTS) {
                     times_slopes(g[i], x[i], ACT);
-                    store8<STREAM>(gp + (r + 8 * i) * ld_gp + c, valid, vec, g[i]);
+                    store8<STREAM>(gp + (r + 8 * i) * ld_gp + c, valid, g[i]);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s[e] += g[i][e];
@@ -187,10 +187,10 @@ static heta_status check_matrix(const char *who, const char *what, const void *p
 
 using namespace heta;
 
-extern "C" heta_status heta_linear(heta_graph *, const heta_linear_args *a, void *hip_stream)
+extern "C" heta_status heta_linear(heta_graph *g, const heta_linear_args *a, void *hip_stream)
 {
     const char *who = "heta_linear";
-    if (!a) return fail(HETA_ERR_INVALID_ARG, "%s: null arguments", who);
+    if (!g || !a) return fail(HETA_ERR_INVALID_ARG, "%s: null arguments", who);
     if (a->n_rows < 0 || a->d_in <= 0 || a->d_out <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and widths > 0", who);
     if (!valid_act(a->act)) return fail(HETA_ERR_INVALID_ARG, "%s: bad act", who);
     const bool q = a->in_dt == HETA_E4M3;
@@ -216,10 +216,9 @@ extern "C" heta_status heta_linear(heta_graph *, const heta_linear_args *a, void
     if (out.overlaps(in) || out.overlaps(w) || out.overlaps(pre) || pre.overlaps(in) || pre.overlaps(w) || pre.overlaps(res) || (out.overlaps(res) && !same_rows))
         return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);
     if (a->n_rows == 0) return HETA_OK;
-    const LinearExtra x{a->bias, a->in_scale, a->w_scale, a->residual, a->pre, a->out, a->ld_res, a->ld_pre, a->ld_out, a->act, HETA_ACT_NONE,
-                        vec_rows(a->out, a->ld_out, osz) && vec_rows(a->residual, a->ld_res, osz) && vec_rows(a->pre, a->ld_pre, osz)};
+    const LinearExtra x{a->bias, a->in_scale, a->w_scale, a->residual, a->pre, a->out, a->ld_res, a->ld_pre, a->ld_out, a->act, HETA_ACT_NONE};
     const double bytes = static_cast<double>(a->n_rows) * (a->d_in * esz + a->d_out * osz * (1.0 + !!a->residual + !!a->pre)) + static_cast<double>(a->d_in) * a->d_out * esz;
-    const Launch l{who, "linear_kernel", TileItem{a->in, a->W, a->ld_in, a->ld_w, 0, 0, a->n_rows, a->d_out, a->d_in, a->d_in, 1, 0, 0, 0, 0, 0}, bytes,
+    const Launch l{g, who, "linear_kernel", TileItem{a->in, a->W, a->ld_in, a->ld_w, 0, 0, a->n_rows, a->d_out, a->d_in, a->d_in, 1, 0, 0, 0, 0, 0}, bytes,
                    2.0 * a->n_rows * a->d_in * a->d_out, as_stream(hip_stream)};
     if (q) return launch_linear_e4m3(l, a->out_dt, a->coarse_sums != 0, x);
     return a->in_dt == HETA_F32 ? launch_linear_f32(l, false, x) : launch_linear_bf16(l, false, a->out_dt, x);
@@ -289,14 +288,13 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
     const void *gpre = acts ? a->grad_pre : a->grad_out;
     const int64_t ld_gpre = acts ? a->ld_gp : a->ld_go;
     if (n > 0 && (acts || a->dbias)) {
-        const int vec = vec_rows(a->grad_out, a->ld_go, esz) && (!acts || (vec_rows(a->pre, a->ld_pre, esz) && vec_rows(a->grad_pre, a->ld_gp, esz)));
         const double bytes = static_cast<double>(n) * a->d_out * esz * (acts ? 3 : 1);
         ProfScope prof("act_grad_kernel", st, bytes, static_cast<double>(n) * a->d_out);
         auto go = [&](auto tag, auto act, auto stream) {
             using E = decltype(tag);
             launch_pieces(slabs * strips, 256, [&](unsigned first, unsigned count) {
                 hipLaunchKernelGGL((act_grad_kernel<E, decltype(act)::value, decltype(stream)::value>), dim3(count), dim3(256), 0, st, static_cast<const E *>(a->grad_out), a->ld_go,
-                                   static_cast<const E *>(a->pre), a->ld_pre, static_cast<E *>(a->grad_pre), a->ld_gp, n, a->d_out, rows_each, a->dbias ? ws : nullptr, vec, first);
+                                   static_cast<const E *>(a->pre), a->ld_pre, static_cast<E *>(a->grad_pre), a->ld_gp, n, a->d_out, rows_each, a->dbias ? ws : nullptr, first);
             });
             return HETA_OK;
         };
@@ -308,16 +306,15 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
 
     const double flops = 2.0 * n * a->d_in * a->d_out;
     if (a->grad_in && n > 0) {
-        const LinearExtra x{nullptr, nullptr, nullptr, fused ? a->in_pre : nullptr, nullptr, a->grad_in, a->ld_ip, 0, a->ld_gi, HETA_ACT_NONE, a->in_act,
-                            vec_rows(a->grad_in, a->ld_gi, esz) && (!fused || vec_rows(a->in_pre, a->ld_ip, esz))};
+        const LinearExtra x{nullptr, nullptr, nullptr, fused ? a->in_pre : nullptr, nullptr, a->grad_in, a->ld_ip, 0, a->ld_gi, HETA_ACT_NONE, a->in_act};
         const double bytes = (static_cast<double>(n) * (a->d_in * (fused ? 2 : 1) + a->d_out) + static_cast<double>(a->d_in) * a->d_out) * esz;
-        const Launch l{who, "linear_grad_in_kernel", TileItem{gpre, a->W, ld_gpre, a->ld_w, 0, 0, n, a->d_in, a->d_out, a->d_out, 1, 0, 0, 0, 0, 0}, bytes, flops, st};
+        const Launch l{g, who, "linear_grad_in_kernel", TileItem{gpre, a->W, ld_gpre, a->ld_w, 0, 0, n, a->d_in, a->d_out, a->d_out, 1, 0, 0, 0, 0, 0}, bytes, flops, st};
         HETA_TRY(a->dt == HETA_F32 ? launch_linear_f32(l, true, x) : launch_linear_bf16(l, true, HETA_BF16, x));
     }
     if (a->dW) {
-        float *part = ws + bias_off;
+        float *part = static_cast<float *>(g->d_ws) + bias_off; // the input gradient may have grown the workspace
         if (n > 0) {
-            const Launch l{who, "linear_grad_w_kernel",
+            const Launch l{g, who, "linear_grad_w_kernel",
                            TileItem{a->in, gpre, a->ld_in, ld_gpre, 0, 0, a->d_in, a->d_out, n, k_per_split, static_cast<int32_t>(n_split), 0, 0, 0, 0, 0},
                            static_cast<double>(n) * (a->d_in + a->d_out) * esz + 4.0 * w_elems, flops, st};
             HETA_TRY(a->dt == HETA_F32 ? launch_grad_w_f32(l, part) : launch_grad_w_bf16(l, part));

@@ -7,15 +7,16 @@ namespace heta {
 // an epilogue that reads, or for a longer one of fp32 outputs.
 template <bool WIDEN> using Wide = TileShape<uint8_t, 1, 1, false, false, kDirect, 4, 2, 2, 4, 128, 2, 1, WIDEN>;
 template <bool WIDEN> using Tall = TileShape<uint8_t, 1, 1, false, false, kDirect, 2, 4, 4, 2, 128, 2, 1, WIDEN>;
-template <bool WIDEN> using Small = TileShape<uint8_t, 1, 1, false, false, kDirect, 2, 2, 1, 1, 128, 3, 2, WIDEN>;      // 64 x 64
-template <bool WIDEN> using Elements = TileShape<uint8_t, 1, 1, false, false, kElements, 2, 2, 2, 2, 64, 2, 1, WIDEN>;  // 128 x 128
+template <bool WIDEN> using Small = TileShape<uint8_t, 1, 1, false, false, kDirect, 2, 2, 1, 1, 128, 3, 2, WIDEN>;       // 64 x 64
+template <bool WIDEN> using StagedLarge = TileShape<uint8_t, 1, 1, false, false, kStaged, 4, 2, 2, 2, 128, 2, 1, WIDEN>; // 256 x 128
+template <bool WIDEN> using StagedSmall = TileShape<uint8_t, 1, 1, false, false, kStaged, 2, 2, 1, 1, 128, 2, 2, WIDEN>; // 64 x 64
 
 heta_status launch_linear_e4m3(const Launch &l, heta_dtype out_dt, bool coarse, const LinearExtra &x)
 {
     auto with = [&](auto tag, auto widen) {
         using O = decltype(tag);
         constexpr bool W = decltype(widen)::value;
-        return launch_linear<std::conditional_t<sizeof(O) == 2, Wide<W>, Tall<W>>, Tall<W>, Small<W>, Elements<W>, O, false>(l, 1, x);
+        return launch_linear<std::conditional_t<sizeof(O) == 2, Wide<W>, Tall<W>>, Tall<W>, Small<W>, StagedLarge<W>, StagedSmall<W>, O, false>(l, 1, x);
     };
     if (out_dt == HETA_F32) return coarse ? with(float{}, std::false_type{}) : with(float{}, std::true_type{});
     return coarse ? with(bf16_t{}, std::false_type{}) : with(bf16_t{}, std::true_type{});

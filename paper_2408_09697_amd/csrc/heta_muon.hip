@@ -13,7 +13,6 @@
 #include <algorithm>
 #include <cmath>
 
-#include "heta_rows.h"
 #include "heta_tiles.h"
 
 namespace heta {
@@ -190,7 +189,7 @@ struct TermsExtra {
 };
 struct TermsEpi {
     static constexpr int kItems = kMuonItems;
-    static constexpr bool kBlocks = true, kStrip = false;
+    static constexpr bool kBlocks = true;
     using Extra = TermsExtra;
     // eight results of row r, columns c, c + 1, ... (valid of them there; rows of the terms are 16-byte aligned)
     __device__ __forceinline__ static void put(const Extra &x, int64_t r, int64_t c, int valid, float (&y)[8])
@@ -232,7 +231,7 @@ struct TermsEpi {
                 float o[8], s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int t = kTerms - 1; t >= 0; --t) { // smallest first
-                    load8(x.old + t * x.old_plane + m * x.ld_old + n, valid, true, o);
+                    load8(x.old + t * x.old_plane + m * x.ld_old + n, valid, o);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[e] += o[e];
                 }

@@ -1,5 +1,5 @@
-// Eight consecutive elements of a row as fp32, for kernels that read and write rows of either element type (not part of
-// the ABI).  `vec`: the rows are 16-byte aligned; `valid`: elements of the eight that exist (others read as 0).
+// Consecutive elements of a row as fp32, for kernels that read and write rows of either element type (not part of the ABI).
+// Rows need no alignment beyond their elements': global memory takes 16-byte accesses at any address.
 #pragma once
 
 #include "heta_gemm.h"
@@ -9,22 +9,24 @@ namespace heta {
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(bf16_t x) { return __uint_as_float(static_cast<uint32_t>(x) << 16); }
 
-// 16 bytes; STREAM: with the hint that they will not be needed again soon
+// 16 bytes at any address; STREAM: with the hint that they will not be needed again soon
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
-template <bool STREAM> __device__ __forceinline__ uintx4 load16(const void *p)
+typedef uint32_t uintx4_any __attribute__((ext_vector_type(4), aligned(1)));
+template <bool STREAM = false> __device__ __forceinline__ uintx4 load16(const void *p)
 {
-    if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const uintx4 *>(p));
-    else return *static_cast<const uintx4 *>(p);
+    if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const uintx4_any *>(p));
+    else return *static_cast<const uintx4_any *>(p);
 }
-template <bool STREAM> __device__ __forceinline__ void store16(void *p, uintx4 v)
+template <bool STREAM = false> __device__ __forceinline__ void store16(void *p, uintx4 v)
 {
-    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<uintx4 *>(p));
-    else *static_cast<uintx4 *>(p) = v;
+    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<uintx4_any *>(p));
+    else *static_cast<uintx4_any *>(p) = v;
 }
 
-template <bool STREAM = false> __device__ __forceinline__ void load8(const float *p, int valid, bool vec, float (&v)[8])
+// eight elements, `valid` of which exist (others read as 0)
+template <bool STREAM = false> __device__ __forceinline__ void load8(const float *p, int valid, float (&v)[8])
 {
-    if (vec && valid >= 8) {
+    if (valid >= 8) {
         const uintx4 a = load16<STREAM>(p), b = load16<STREAM>(p + 4);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -36,9 +38,9 @@ template <bool STREAM = false> __device__ __forceinline__ void load8(const float
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < valid ? p[e] : 0.f;
 }
-template <bool STREAM = false> __device__ __forceinline__ void load8(const bf16_t *p, int valid, bool vec, float (&v)[8])
+template <bool STREAM = false> __device__ __forceinline__ void load8(const bf16_t *p, int valid, float (&v)[8])
 {
-    if (vec && valid >= 8) {
+    if (valid >= 8) {
         const uintx4 a = load16<STREAM>(p);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -50,9 +52,9 @@ template <bool STREAM = false> __device__ __forceinline__ void load8(const bf16_
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < valid ? widen(p[e]) : 0.f;
 }
-template <bool STREAM = false> __device__ __forceinline__ void store8(float *p, int valid, bool vec, const float (&v)[8])
+template <bool STREAM = false> __device__ __forceinline__ void store8(float *p, int valid, const float (&v)[8])
 {
-    if (vec && valid >= 8) {
+    if (valid >= 8) {
         const uintx4 a = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
         const uintx4 b = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
         store16<STREAM>(p, a);
@@ -63,9 +65,9 @@ template <bool STREAM = false> __device__ __forceinline__ void store8(float *p, 
     for (int e = 0; e < 8; ++e)
         if (e < valid) p[e] = v[e];
 }
-template <bool STREAM = false> __device__ __forceinline__ void store8(bf16_t *p, int valid, bool vec, const float (&v)[8])
+template <bool STREAM = false> __device__ __forceinline__ void store8(bf16_t *p, int valid, const float (&v)[8])
 {
-    if (vec && valid >= 8) {
+    if (valid >= 8) {
         const uintx4 a = {pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
         store16<STREAM>(p, a);
         return;
@@ -75,12 +77,55 @@ template <bool STREAM = false> __device__ __forceinline__ void store8(bf16_t *p,
         if (e < valid) p[e] = static_cast<bf16_t>(pack2_bf16(v[e], v[e]) & 0xffffu);
 }
 
+// 16 bytes of outputs (valid of their elements exist) from fp32, and as they lie in memory
+template <typename O> __device__ __forceinline__ uintx4 pack16(const float (&y)[16 / sizeof(O)])
+{
+    if constexpr (sizeof(O) == 2) return uintx4{pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3]), pack2_bf16(y[4], y[5]), pack2_bf16(y[6], y[7])};
+    else return uintx4{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
+}
+template <typename O> __device__ __forceinline__ void unpack16(uintx4 w, float (&y)[16 / sizeof(O)])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(O) == 2) {
+            y[2 * j] = __uint_as_float(w[j] << 16);
+            y[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        } else {
+            y[j] = __uint_as_float(w[j]);
+        }
+    }
+}
+template <typename O, bool STREAM = false> __device__ __forceinline__ void store_piece(O *p, int valid, uintx4 w)
+{
+    constexpr int W = 16 / (int)sizeof(O);
+    if (valid >= W) {
+        store16<STREAM>(p, w);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < W; ++e)
+        if (e < valid) {
+            if constexpr (sizeof(O) == 2) p[e] = static_cast<O>(w[e / 2] >> (16 * (e & 1)));
+            else p[e] = __uint_as_float(w[e]);
+        }
+}
+template <typename O> __device__ __forceinline__ uintx4 load_piece(const O *p, int valid)
+{
+    constexpr int W = 16 / (int)sizeof(O);
+    if (valid >= W) return load16(p);
+    uintx4 w = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < W; ++e)
+        if (e < valid) {
+            if constexpr (sizeof(O) == 2) w[e / 2] |= static_cast<uint32_t>(p[e]) << (16 * (e & 1));
+            else w[e] = __float_as_uint(p[e]);
+        }
+    return w;
+}
+
 // Calls that move more than the chip's 256 MB last-level cache holds read and write with the streaming hint; below, what a
 // call writes is still cached when the next one reads it.
 inline bool streams(double bytes) { return bytes > 256e6; }
-
-// rows of `ld` elements from p on that can be moved 16 bytes at a time (a null pointer can: it is not read)
-inline bool vec_rows(const void *p, int64_t ld, size_t elt) { return !p || (aligned16(p) && (ld * static_cast<int64_t>(elt)) % 16 == 0); }
 
 // out[c] (or, for rows of `width`, out[(c / width) * ld + c % width]) = sum over s < n_part of part[s * total + c], c < total,
 // in a fixed order; out is fp32 or bf16.  Deterministic second half of sums over rows that many workgroups share.

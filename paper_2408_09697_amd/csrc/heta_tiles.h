@@ -7,7 +7,7 @@
 //   r-contiguous (element (r, k) at base[k * ld + r]): LDS row k, chunks at rc_place; fragments are read with the
 //   transposing LDS read, so neither operand of any product is ever transposed in memory.
 // It gets there straight from memory (kDirect: 16-byte aligned rows of the image's own type, T planes side by side in
-// memory) or through registers (kStaged / kElements: any storage type and alignment; fp32 is split into its three terms
+// memory) or through registers (kStaged: any storage type and alignment; fp32 is split into its three terms
 // there, once per workgroup, not by every wavefront that reads the tile).  A last k-tile with fewer k-values is filled up
 // with zeros in LDS: fragments and products know no ragged tile.
 //
@@ -21,11 +21,11 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "heta_gemm.h"
+#include "heta_rows.h"
 
 namespace heta {
 
-enum TileLoad { kDirect = 0, kStaged = 1, kElements = 2 };
+enum TileLoad { kDirect = 0, kStaged = 1 };
 
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef short shortx4_tr __attribute__((ext_vector_type(4)));
@@ -130,7 +130,7 @@ template <bool RC, int ROWS, int BK, int EB, int NW, int T> struct PlaneLoader {
 // ---- memory -> registers -> LDS ---------------------------------------------------------------------
 // An item is one 16-byte chunk of the image: E consecutive elements, converted to the planes of their type.  Elements
 // beyond the matrix count as zero.
-template <typename S, bool RC, int ROWS, int BK, int EB, int NT, int T, bool VEC> struct StagedLoader {
+template <typename S, bool RC, int ROWS, int BK, int EB, int NT, int T> struct StagedLoader {
     using Img = TileImage<RC, ROWS, BK, EB>;
     static constexpr int E = Img::E, NI = (Img::CHUNKS + NT - 1) / NT, W = E * (int)sizeof(S) / 16; // 16-byte words per item
     static_assert(W >= 1 && (T == 1 || sizeof(S) == 4), "planes are split from fp32");
@@ -147,9 +147,12 @@ template <typename S, bool RC, int ROWS, int BK, int EB, int NT, int T, bool VEC
             for (int w = 0; w < W; ++w) raw[i][w] = make_uint4(0u, 0u, 0u, 0u);
             if (!in) continue;
             const S *src = base + (RC ? k * ld + r : r * ld + k);
-            if (VEC && left >= E) {
+            if (left >= E) {
 #pragma unroll
-                for (int w = 0; w < W; ++w) raw[i][w] = reinterpret_cast<const uint4 *>(src)[w];
+                for (int w = 0; w < W; ++w) {
+                    const uintx4 q = load16(reinterpret_cast<const char *>(src) + 16 * w);
+                    raw[i][w] = make_uint4(q[0], q[1], q[2], q[3]);
+                }
             } else {
                 union { uint4 u[W]; S s[E]; } t;
 #pragma unroll
@@ -233,33 +236,6 @@ template <int EB, int T, int MI, int NJ> struct Fragments { // of one step
     F a[MI][T], b[NJ][T];
 };
 
-// 16 bytes of outputs from fp32, and back
-template <typename O> __device__ __forceinline__ uint4 pack16(const float (&y)[16 / sizeof(O)])
-{
-    if constexpr (sizeof(O) == 2) return make_uint4(pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3]), pack2_bf16(y[4], y[5]), pack2_bf16(y[6], y[7]));
-    else return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
-}
-template <typename O> __device__ __forceinline__ void unpack16(uint4 raw, float (&y)[16 / sizeof(O)])
-{
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if constexpr (sizeof(O) == 2) {
-            y[2 * j] = __uint_as_float(w[j] << 16);
-            y[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        } else {
-            y[j] = __uint_as_float(w[j]);
-        }
-    }
-}
-
-template <bool STREAM> __device__ __forceinline__ void store_chunk(void *p, uint4 v)
-{
-    typedef uint32_t words __attribute__((ext_vector_type(4)));
-    if constexpr (STREAM) __builtin_nontemporal_store(words{v.x, v.y, v.z, v.w}, static_cast<words *>(p));
-    else *static_cast<uint4 *>(p) = v;
-}
-
 // four columns (chunk 0..7) of a row of a 32 x 32 fp32 strip
 __device__ __forceinline__ float4 *strip_at(float *strip, int row, int chunk) { return reinterpret_cast<float4 *>(strip + row * 32 + ((chunk ^ (row & 7)) * 4)); }
 
@@ -321,13 +297,10 @@ struct TilePlace {
 // Epi: what becomes of the product; all functions are device functions.
 //   kItems, Extra: items of a launch at most, and what an item's epilogue needs
 //   kBlocks = true: block(x, it, strip, m, n, off_diagonal, lane) takes 32 x 32 sums at row m, column n from the strip (strip_at)
-//   kStrip = false: put(x, it, m, n, valid, v, split) takes eight columns n, n + 1, ... of row m < M (valid: as many as there are)
-//   kStrip = true (Out rows of whole, aligned 16-byte pieces): with W = 16 bytes of columns, first(cols, row, y) makes
-//     pre-activations of W sums and second(x, y, t) results, t being W elements of x.other (if kReads; zeros or nothing where it
-//     is null); x.pre (if kPre and not null) and out(x, it, split) receive them, rows x.ld_pre and x.ld_out apart.
-//     kStream: with the streaming hint.
-//     struct Cols, Row { void load(const Extra &x, int64_t n, int64_t N); } are what a lane keeps of W columns and of a row (which
-//     may lie beyond the matrix).
+//   kBlocks = false: with W = 16 bytes of columns of Out, first(cols, row, y) makes pre-activations of W sums and second(x, y, t)
+//     results, t being W elements of x.other (if kReads; zeros or nothing where it is null); x.pre (if kPre and not null) and
+//     out(x, it, split) receive them, rows x.ld_pre and x.ld_out apart, kStream: with the streaming hint; kWhole: N is a multiple of W.  struct Cols, Row { void
+//     load(const Extra &x, int64_t n, int64_t N); } are what a lane keeps of W columns and of a row (which may lie beyond the matrix).
 template <typename Epi> struct TileArgs {
     int n_items;
     uint32_t stride; // one item: from one tile of a workgroup to its next; several: tiles of an XCD
@@ -353,12 +326,12 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
 {
     using S = typename C::S;
     constexpr int EB = C::EB, T = C::T, MI = C::MI, NJ = C::NJ, BK = C::BK, ST = C::ST, NW = C::NW, NT = C::NT, BM = C::BM, BN = C::BN;
-    constexpr bool DIRECT = C::LOAD == kDirect, VEC = C::LOAD != kElements;
+    constexpr bool DIRECT = C::LOAD == kDirect;
     using ImgA = TileImage<C::A_RC, BM, BK, EB>;
     using ImgB = TileImage<C::B_RC, BN, BK, EB>;
     constexpr int A_STAGE = ImgA::BYTES * T, STAGE = A_STAGE + ImgB::BYTES * T;
     // epilogue strips: one 32 x 32 block of sums per wavefront, its own; behind the ring where that is filled during the epilogue
-    constexpr int STRIPS = Epi::kStrip || Epi::kBlocks ? NW * 4096 : 0, STRIPS_AT = DIRECT ? ST * STAGE : 0;
+    constexpr int STRIPS = NW * 4096, STRIPS_AT = DIRECT ? ST * STAGE : 0;
     __shared__ __attribute__((aligned(1024))) char ring[std::max(ST * STAGE, STRIPS_AT + STRIPS)];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -488,28 +461,34 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
                         *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
                     Epi::block(extra, it, strip, now.m0 + wm + 32 * i, now.n0 + wn + 32 * jj, now.m0 != now.n0, lane);
                 }
-        } else if constexpr (Epi::kStrip) {
+        } else {
             using O = typename Epi::Out;
             constexpr int W = 16 / (int)sizeof(O);                        // columns of a lane: 16 bytes of the output
             constexpr int LPR = 32 / W, RPP = 64 / LPR, ROUNDS = 32 / RPP; // lanes per row of a block, rows per access, accesses
             float *strip = reinterpret_cast<float *>(ring + STRIPS_AT + wave * 4096);
-            auto at = [&](int row, int chunk) { return strip_at(strip, row, chunk); };
             const int sr = lane / LPR, sc = lane % LPR;
             const int64_t rm = now.m0 + wm + sr, rn = now.n0 + wn + sc * W;
-            // What the epilogue reads in the output's shape comes a row of blocks ahead, and what belongs to columns and rows before all of it:
-            // a load waits for every store that was issued before it.
-            uint4 other[Epi::kReads ? 2 : 1][NJ][ROUNDS];
-            auto fetch = [&](int i) {
+            auto valid = [&](int64_t n) { return Epi::kWhole ? W : static_cast<int>(min(it.N - n, static_cast<int64_t>(W))); };
+            // What the epilogue reads in the output's shape comes for as many rows of blocks at a time as 32 registers hold, and is
+            // awaited at once, in front of their stores: a load waits for every store that was issued before it, and one
+            // left to the compiler, across the branches below, for every store so far at each of its uses (700,000 x 1,024 x 256 with
+            // a residual: 495 to 556 us that way, 485 this way; with 64 registers accumulators spill, 556).
+            constexpr int BATCH = std::max(1, std::min(MI, 8 / (NJ * ROUNDS)));
+            uintx4 other[Epi::kReads ? BATCH : 1][NJ][ROUNDS];
+            auto fetch = [&](int i0) {
                 if constexpr (Epi::kReads)
                     if (extra.other) {
 #pragma unroll
-                        for (int jj = 0; jj < NJ; ++jj)
+                        for (int i = i0; i < i0 + BATCH && i < MI; ++i)
 #pragma unroll
-                            for (int r = 0; r < ROUNDS; ++r) {
-                                const int64_t m = rm + 32 * i + RPP * r, n = rn + 32 * jj;
-                                other[i & 1][jj][r] = make_uint4(0u, 0u, 0u, 0u);
-                                if (m < it.M && n < it.N) other[i & 1][jj][r] = *reinterpret_cast<const uint4 *>(static_cast<const O *>(extra.other) + m * extra.ld_other + n);
-                            }
+                            for (int jj = 0; jj < NJ; ++jj)
+#pragma unroll
+                                for (int r = 0; r < ROUNDS; ++r) {
+                                    const int64_t m = rm + 32 * i + RPP * r, n = rn + 32 * jj;
+                                    other[i % BATCH][jj][r] = uintx4{0u, 0u, 0u, 0u};
+                                    if (m < it.M && n < it.N) other[i % BATCH][jj][r] = load_piece(static_cast<const O *>(extra.other) + m * extra.ld_other + n, valid(n));
+                                }
+                        wait_counters<0, false>();
                     }
             };
             typename Epi::Cols cols[NJ];
@@ -520,56 +499,34 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
             for (int i = 0; i < MI; ++i)
 #pragma unroll
                 for (int r = 0; r < ROUNDS; ++r) rows[i][r].load(extra, rm + 32 * i + RPP * r, it.M);
-            fetch(0);
             O *const out = Epi::out(extra, it, now.split);
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
-                if (i + 1 < MI) fetch(i + 1);
+                if (i % BATCH == 0) fetch(i);
 #pragma unroll
                 for (int jj = 0; jj < NJ; ++jj) {
                     const int64_t n = rn + 32 * jj;
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        *at(l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
+                        *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
 #pragma unroll
                     for (int r = 0; r < ROUNDS; ++r) {
                         const int64_t m = rm + 32 * i + RPP * r;
                         float y[W];
 #pragma unroll
                         for (int h = 0; h < W / 4; ++h) {
-                            const float4 f = *at(RPP * r + sr, sc * (W / 4) + h);
+                            const float4 f = *strip_at(strip, RPP * r + sr, sc * (W / 4) + h);
                             y[4 * h] = f.x; y[4 * h + 1] = f.y; y[4 * h + 2] = f.z; y[4 * h + 3] = f.w;
                         }
                         if (m >= it.M || n >= it.N) continue;
                         Epi::first(cols[jj], rows[i][r], y);
                         if constexpr (Epi::kPre)
-                            if (extra.pre) *reinterpret_cast<uint4 *>(static_cast<O *>(extra.pre) + m * extra.ld_pre + n) = pack16<O>(y);
+                            if (extra.pre) store_piece(static_cast<O *>(extra.pre) + m * extra.ld_pre + n, valid(n), pack16<O>(y));
                         float t[W];
-                        if constexpr (Epi::kReads) unpack16<O>(other[i & 1][jj][r], t);
+                        if constexpr (Epi::kReads) unpack16<O>(other[i % BATCH][jj][r], t);
                         Epi::second(extra, y, t);
-                        store_chunk<Epi::kStream>(out + m * extra.ld_out + n, pack16<O>(y));
+                        store_piece<O, Epi::kStream>(out + m * extra.ld_out + n, valid(n), pack16<O>(y));
                     }
-                }
-            }
-        } else {
-            // Exchanging the upper half of the lanes of register group q with the lower half of group q + 1 leaves a lane with
-            // eight consecutive columns: 16 u + 8 (lane / 32) + 0..7 of the wavefront's part
-            const int64_t nb = now.n0 + wn + 8 * half;
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const int64_t m = now.m0 + wm + 32 * i + l32;
-#pragma unroll
-                for (int u = 0; u < 2 * NJ; ++u) {
-                    const int64_t n = nb + 16 * u;
-                    const int valid = static_cast<int>(min(it.N - n, static_cast<int64_t>(8)));
-                    float v[8];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][u / 2][8 * (u & 1) + e]), __float_as_uint(acc[i][u / 2][8 * (u & 1) + 4 + e]), false, false);
-                        v[e] = __uint_as_float(r[0]);
-                        v[4 + e] = __uint_as_float(r[1]);
-                    }
-                    if (m < it.M && valid > 0) Epi::put(extra, it, m, n, valid, v, now.split);
                 }
             }
         }
@@ -652,8 +609,8 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
             now = next;
         }
     } else {
-        StagedLoader<S, C::A_RC, BM, BK, EB, NT, T, VEC> sa;
-        StagedLoader<S, C::B_RC, BN, BK, EB, NT, T, VEC> sb;
+        StagedLoader<S, C::A_RC, BM, BK, EB, NT, T> sa;
+        StagedLoader<S, C::B_RC, BN, BK, EB, NT, T> sb;
         const S *A = static_cast<const S *>(it.A), *B = static_cast<const S *>(it.B);
         do {
             const int64_t k_end = now.k0 + now.kn;
@@ -681,10 +638,8 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
                 barrier_no_drain();
             }
             epilogue();
-            if constexpr (STRIPS > 0) {
-                wait_counters<63, true>();
-                barrier_no_drain(); // the next tile's first k-tile overlays the strips
-            }
+            wait_counters<63, true>();
+            barrier_no_drain(); // the next tile's first k-tile overlays the strips
         } while (further(now));
     }
 }
