@@ -95,6 +95,13 @@ def test_forward(handle, n, d_in, d_out, dtype, out_dtype, pad, kind):
     check_forward(handle, n, d_in, d_out, dtype, out_dtype, kind, pad, kind in (NONE, GELU), kind in (RELU, GELU))
 
 
+@pytest.mark.parametrize("dtype,out_dtype", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("kind", [NONE, RELU, GELU, SILU])
+@pytest.mark.parametrize("n,d_in,d_out,pad", [(40000, 252, 260, 4), (20011, 256, 514, 6), (24000, 1100, 516, 12)])
+def test_large_products_with_tails_in_aligned_rows(handle, n, d_in, d_out, pad, dtype, out_dtype, kind):
+    check_forward(handle, n, d_in, d_out, dtype, out_dtype, kind, pad, True, True)
+
+
 @pytest.mark.parametrize("n,d_in,d_out", SHAPES)
 @pytest.mark.parametrize("out_dtype", [BF16, F32])
 @pytest.mark.parametrize("pad", [0, 16, 3])

@@ -3,8 +3,9 @@
 Tolerances.  m is one fused multiply-add: 2^-24 of its value.  The polynomial p(s) = 3.4445 s - 4.7750 s^3 + 2.0315 s^5 has |p(s) / s| and |p'(s)|
 of at most 3.4445 where singular values stay (below 1.21), so what one step rounds off, relative to |X|_F, reaches the end of the
 following j steps multiplied by at most 3.4445^j: 683 altogether after five steps.  A step rounds X, its Gram matrix and the
-polynomial and forms three products; eight roundings of u = 2^-24 each (three bf16 terms hold 24 bits) give 683 * 8 u = 3.3e-4 of
-|X|_F, with two terms (bf16 weights; 2^-17) 683 * 8 * 2^-17 = 4.2e-2.  W is off by lr scale times that and its own rounding.
+polynomial and forms three products; eight roundings of u = 2^-24 each would give 683 * 8 u = 3.3e-4 of |X|_F, and ones of 2^-17 (two
+bf16 terms) 683 * 8 * 2^-17 = 4.2e-2.  The kernels keep two terms; the bound for fp32 weights is the tighter one all the same: the
+roundings of a matrix's elements are independent, and what they add up to stays well below their worst case.  W is off by lr scale times that and its own rounding.
 """
 import math
 
