@@ -16,7 +16,9 @@ namespace heta {
 
 // ---- sums of partials --------------------------------------------------------------------------------
 // 256 threads: 256 / CH groups of four columns, CH chains over the partials each, joined through LDS in order.  A chain keeps
-// sixteen loads in flight: with eight, and 32 chains for 256 columns of 2,048 partials, the sum took 36 us of a norm's 340.
+// sixteen loads in flight: with eight, and 32 chains for 256 columns of 2,048 partials, the sum took 36 us of a norm's 340.  Four columns
+// come by one load at whatever place they start (a width that is no multiple of four shifts them from partial to partial).
+typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
 template <int CH, typename O> __global__ void __launch_bounds__(256) fold_partials_kernel(const float *part, int64_t n_part, int64_t total, O *out, int32_t width, int64_t ld)
 {
     constexpr int G = 256 / CH;
@@ -24,18 +26,17 @@ template <int CH, typename O> __global__ void __launch_bounds__(256) fold_partia
     const int gq = threadIdx.x % G, ch = threadIdx.x / G;
     const int64_t c = (static_cast<int64_t>(blockIdx.x) * G + gq) * 4;
     const int valid = static_cast<int>(min(total - c, static_cast<int64_t>(4)));
-    const bool vec = (total & 3) == 0;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (valid > 0) {
         // chain ch takes every CH-th partial
-        if (vec) {
+        if (valid == 4) {
             const float *p = part + c + ch * total;
             const int64_t n = ch < n_part ? (n_part - ch + CH - 1) / CH : 0, step = CH * total;
             int64_t i = 0;
             for (; i + 16 <= n; i += 16, p += 16 * step) {
-                float4 x[16];
+                float4_any x[16];
 #pragma unroll
-                for (int q = 0; q < 16; ++q) x[q] = *reinterpret_cast<const float4 *>(p + q * step);
+                for (int q = 0; q < 16; ++q) x[q] = *reinterpret_cast<const float4_any *>(p + q * step);
 #pragma unroll
                 for (int q = 0; q < 16; ++q) {
                     s[0] += x[q].x; s[1] += x[q].y; s[2] += x[q].z; s[3] += x[q].w;
@@ -43,7 +44,7 @@ template <int CH, typename O> __global__ void __launch_bounds__(256) fold_partia
             }
 #pragma unroll 4
             for (; i < n; ++i, p += step) {
-                const float4 x = *reinterpret_cast<const float4 *>(p);
+                const float4_any x = *reinterpret_cast<const float4_any *>(p);
                 s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
             }
         } else {
