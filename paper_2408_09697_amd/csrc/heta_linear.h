@@ -212,6 +212,8 @@ heta_status launch_linear_f32(const Launch &l, bool input_gradient, const Linear
 heta_status launch_linear_bf16(const Launch &l, bool input_gradient, heta_dtype out_dt, const LinearExtra &x);
 heta_status launch_linear_e4m3(const Launch &l, heta_dtype out_dt, bool coarse, const LinearExtra &x);
 heta_status launch_grad_w_f32(const Launch &l, float *part);
+// Copies operands of a large weight gradient whose rows start anywhere to aligned rows, in the workspace from byte `offset` on.
+heta_status align_grad_w_bf16(Launch &l, size_t offset);
 heta_status launch_grad_w_bf16(const Launch &l, float *part);
 
 // one type's launches from its tile shapes: large tiles (Reading: where the epilogue reads in the output's shape), small ones, and

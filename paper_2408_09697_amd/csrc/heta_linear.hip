@@ -7,7 +7,8 @@
 //
 // All three products are the tile kernel of heta_tiles.h: bf16 operands straight into LDS; e4m3 operands too, widened to
 // bf16 behind LDS or, where the caller allows coarser sums, on the 8-bit matrix instruction at twice the rate (block scales 1;
-// the scales of rows and columns come in the epilogue); fp32 operands as three bf16 terms.  grad_W is split over the rows; the partial products are added in a fixed order.
+// the scales of rows and columns come in the epilogue); fp32 operands as three bf16 terms.  grad_W is split over the rows (long
+// unaligned bf16 operands of it are copied to aligned rows first); the partial products are added in a fixed order.
 #include <algorithm>
 
 #include "heta_linear.h"
@@ -313,13 +314,12 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
         HETA_TRY(a->dt == HETA_F32 ? launch_linear_f32(l, true, x) : launch_linear_bf16(l, true, HETA_BF16, x));
     }
     if (a->dW) {
-        float *part = static_cast<float *>(g->d_ws) + bias_off; // the input gradient may have grown the workspace
-        if (n > 0) {
-            const Launch l{g, who, "linear_grad_w_kernel",
-                           TileItem{a->in, gpre, a->ld_in, ld_gpre, 0, 0, a->d_in, a->d_out, n, k_per_split, static_cast<int32_t>(n_split), 0, 0, 0, 0, 0},
-                           static_cast<double>(n) * (a->d_in + a->d_out) * esz + 4.0 * w_elems, flops, st};
-            HETA_TRY(a->dt == HETA_F32 ? launch_grad_w_f32(l, part) : launch_grad_w_bf16(l, part));
-        }
+        Launch l{g, who, "linear_grad_w_kernel",
+                 TileItem{a->in, gpre, a->ld_in, ld_gpre, 0, 0, a->d_in, a->d_out, n, k_per_split, static_cast<int32_t>(n_split), 0, 0, 0, 0, 0},
+                 static_cast<double>(n) * (a->d_in + a->d_out) * esz + 4.0 * w_elems, flops, st};
+        if (n > 0 && a->dt == HETA_BF16) HETA_TRY(align_grad_w_bf16(l, static_cast<size_t>(bias_off + w_elems) * sizeof(float)));
+        float *part = static_cast<float *>(g->d_ws) + bias_off; // the workspace may have grown since its first use
+        if (n > 0) HETA_TRY(a->dt == HETA_F32 ? launch_grad_w_f32(l, part) : launch_grad_w_bf16(l, part));
         HETA_TRY(fold_partials(part, n_split, static_cast<int64_t>(a->d_in) * a->d_out, a->dW, a->dw_dt, a->d_out, a->ld_dw, st));
     }
     return HETA_OK;

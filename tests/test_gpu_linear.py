@@ -235,6 +235,19 @@ def test_backward_agrees_with_differences(handle):
             assert abs(float((g.double() * v).sum()) - diff) <= 2e-5 * float((g.double() * v).abs().sum())
 
 
+@pytest.mark.parametrize("n,d_in,d_out,pad", [(20011, 301, 517, 0), (40011, 301, 517, 3), (70000, 264, 512, 3), (40000, 512, 789, 0), (90000, 256, 189, 0)])
+@pytest.mark.parametrize("kind", [NONE, GELU])
+def test_large_products_of_unaligned_rows(handle, n, d_in, d_out, pad, kind):
+    check_forward(handle, n, d_in, d_out, BF16, BF16, kind, pad, True, True)
+    test_backward(handle, n, d_in, d_out, BF16, BF16, pad, kind)
+
+
+def test_a_workspace_that_grows_between_the_gradients():
+    g = heta.heta_graph_create([(1, 1, 0)], [])
+    test_backward(g, 40011, 301, 517, BF16, F32, 3, SILU)
+    g.destroy()
+
+
 def test_gradients_in_the_place_of_their_operands(handle):
     go, pre, x, W, ip = rows(500, 72, BF16, 1), rows(500, 72, BF16, 2), rows(500, 40, BF16, 3), rows(40, 72, BF16, 4), rows(500, 40, BF16, 5)
     gp, gi = torch.empty_like(go), torch.empty_like(x)
