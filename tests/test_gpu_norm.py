@@ -218,3 +218,21 @@ def test_offsets_past_32_bits():
     heta.heta_rms_norm(x, out)
     heta.heta_rms_norm(src, want)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("d", [201, 202, 203, 204, 205, 206, 207, 2, 3, 5, 6])
+@pytest.mark.parametrize("pad", [0, 5])
+def test_rows_that_end_inside_eight_columns(handle, d, pad):
+    test_forward(70, d, BF16, BF16, pad)
+    test_forward(70, d, BF16, E4M3, pad)
+    test_backward(handle, 70, d, BF16, BF16, pad)
+
+
+@pytest.mark.parametrize("d", [201, 202, 203, 204, 205, 206, 207])
+def test_columns_beyond_a_row_stay(handle, d):
+    buf = [torch.full((40, d + 9), 7.0, device="cuda", dtype=BF16) for _ in range(3)]
+    x, rstd = torch.randn(40, d, device="cuda").to(BF16), torch.ones(40, device="cuda")
+    heta.heta_rms_norm(x, buf[0][:, :d], residual=x, sum=buf[1][:, :d])
+    heta.heta_rms_norm_bwd(handle, x, rstd, x, buf[2][:, :d], grad_sum=x)
+    for b in buf:
+        assert (b[:, d:] == 7.0).all()
