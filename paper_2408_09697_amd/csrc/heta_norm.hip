@@ -42,7 +42,8 @@ template <int LANES> __device__ __forceinline__ float lanes_max(float v)
 // A lane's eight values of chunk v are 8 / P pieces of P consecutive columns; the pieces of a group of lanes lie side by side, so
 // that an access of the widest type among the row's arrays is 16 bytes of consecutive memory per lane (P = 4 where fp32 is among
 // them, else 8).  100,000 unaligned rows of 789 fp32 columns, backward: 328 us with eight consecutive columns per lane; of bf16
-// rows, 274 with pieces of four, 229 with pieces of eight whose last is taken apart (300,000 x 300: 270 / 259; 10^6 x 100: 241 / 200).
+// rows, 274 with pieces of four, 229 with pieces of eight whose last is taken apart (300,000 x 300: 270 / 259; 10^6 x 100: 241 / 200); the
+// code for that piece alone takes 4 % of the time of widths that have none (700,000 x 256, backward: 267 / 257).
 template <int LANES, int P> __device__ __forceinline__ int column(int v, int e, int l) { return ((v * (8 / P) + e / P) * LANES + l) * P + e % P; }
 
 // N words at any address
@@ -110,7 +111,9 @@ __device__ __forceinline__ void store_tail(bf16_t *p, int rest, const uint32_t (
     if (rest & 1) *p = static_cast<bf16_t>(rest == 1 ? w[0] : rest == 3 ? w[1] : rest == 5 ? w[2] : w[3]);
 }
 
-template <int LANES, int NV, int P, bool STREAM, typename T> __device__ __forceinline__ void load_row(const T *row, int d, int l, float (&x)[NV][8])
+// TAIL: the width may be no multiple of P.  Without it lanes beyond the width still go through the branch for single elements, which reads
+// none; with plain zeros there, the compiler's order of the loads costs 6 % (700,000 x 256, backward: 273 us for 257).
+template <int LANES, int NV, int P, bool TAIL, bool STREAM, typename T> __device__ __forceinline__ void load_row(const T *row, int d, int l, float (&x)[NV][8])
 {
     constexpr int N = P * (int)sizeof(T) / 4;
 #pragma unroll
@@ -126,7 +129,7 @@ template <int LANES, int NV, int P, bool STREAM, typename T> __device__ __forcei
                     if constexpr (sizeof(T) == 4) x[v][h + e] = __uint_as_float(w[e]);
                     else x[v][h + e] = __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
                 }
-            } else if constexpr (P == 8 && sizeof(T) == 2) {
+            } else if constexpr (TAIL && P == 8 && sizeof(T) == 2) {
                 uint32_t w[4] = {0u, 0u, 0u, 0u};
                 if (c < d) load_tail(row + c, d & 7, w);
 #pragma unroll
@@ -137,7 +140,7 @@ template <int LANES, int NV, int P, bool STREAM, typename T> __device__ __forcei
             }
         }
 }
-template <int LANES, int NV, int P, bool STREAM, typename T> __device__ __forceinline__ void store_row(T *row, int d, int l, const float (&x)[NV][8])
+template <int LANES, int NV, int P, bool TAIL, bool STREAM, typename T> __device__ __forceinline__ void store_row(T *row, int d, int l, const float (&x)[NV][8])
 {
     constexpr int N = P * (int)sizeof(T) / 4;
 #pragma unroll
@@ -153,7 +156,7 @@ template <int LANES, int NV, int P, bool STREAM, typename T> __device__ __forcei
             }
             if (c + P <= d) {
                 store_words<N, STREAM>(row + c, w);
-            } else if constexpr (P == 8 && sizeof(T) == 2) {
+            } else if constexpr (TAIL && P == 8 && sizeof(T) == 2) {
                 if (c < d) store_tail(row + c, d & 7, w);
             } else {
 #pragma unroll
@@ -201,7 +204,7 @@ template <typename T> __device__ __forceinline__ float rounded(float v)
 }
 
 // T: type of x, residual and sum; O: of the output (uint8_t: e4m3)
-template <typename T, typename O, int LANES, int NV, int P, bool STREAM> __global__ void __launch_bounds__(256) rms_norm_kernel(NormFwd p)
+template <typename T, typename O, int LANES, int NV, int P, bool TAIL, bool STREAM> __global__ void __launch_bounds__(256) rms_norm_kernel(NormFwd p)
 {
     constexpr int GROUPS = 256 / LANES;
     const int l = threadIdx.x % LANES, grp = threadIdx.x / LANES;
@@ -215,16 +218,16 @@ template <typename T, typename O, int LANES, int NV, int P, bool STREAM> __globa
         }
     for (int64_t r = static_cast<int64_t>(blockIdx.x) * GROUPS + grp; r < p.n_rows; r += static_cast<int64_t>(gridDim.x) * GROUPS) {
         float x[NV][8];
-        load_row<LANES, NV, P, STREAM>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, x);
+        load_row<LANES, NV, P, TAIL, STREAM>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, x);
         if (p.residual) {
             float y[NV][8];
-            load_row<LANES, NV, P, STREAM>(static_cast<const T *>(p.residual) + r * p.ld_res, p.d, l, y);
+            load_row<LANES, NV, P, TAIL, STREAM>(static_cast<const T *>(p.residual) + r * p.ld_res, p.d, l, y);
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[v][e] = rounded<T>(x[v][e] + y[v][e]);
         }
-        if (p.sum) store_row<LANES, NV, P, STREAM>(static_cast<T *>(p.sum) + r * p.ld_sum, p.d, l, x);
+        if (p.sum) store_row<LANES, NV, P, TAIL, STREAM>(static_cast<T *>(p.sum) + r * p.ld_sum, p.d, l, x);
         float ss = 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
@@ -246,7 +249,7 @@ template <typename T, typename O, int LANES, int NV, int P, bool STREAM> __globa
             if (l == 0) p.scale[r] = amax / 448.f;
             store_row_e4m3<LANES, NV, P>(static_cast<uint8_t *>(p.out) + r * p.ld_out, p.d, l, x, e4m3_factor(amax));
         } else {
-            store_row<LANES, NV, P, STREAM>(static_cast<O *>(p.out) + r * p.ld_out, p.d, l, x);
+            store_row<LANES, NV, P, TAIL, STREAM>(static_cast<O *>(p.out) + r * p.ld_out, p.d, l, x);
         }
     }
 }
@@ -313,7 +316,7 @@ struct NormBwd {
     int32_t d;
 };
 
-template <typename T, typename G, int LANES, int NV, int P, bool STREAM> __global__ void __launch_bounds__(256) rms_norm_bwd_kernel(NormBwd p)
+template <typename T, typename G, int LANES, int NV, int P, bool TAIL, bool STREAM> __global__ void __launch_bounds__(256) rms_norm_bwd_kernel(NormBwd p)
 {
     constexpr int GROUPS = 256 / LANES;
     __shared__ float joined[GROUPS * LANES * NV * 8];
@@ -330,8 +333,8 @@ template <typename T, typename G, int LANES, int NV, int P, bool STREAM> __globa
     const float inv_d = 1.f / static_cast<float>(p.d);
     for (int64_t r = static_cast<int64_t>(blockIdx.x) * GROUPS + grp; r < p.n_rows; r += static_cast<int64_t>(gridDim.x) * GROUPS) {
         float h[NV][8], w[NV][8];
-        load_row<LANES, NV, P, STREAM>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, h);
-        load_row<LANES, NV, P, STREAM>(static_cast<const G *>(p.grad_out) + r * p.ld_go, p.d, l, w);
+        load_row<LANES, NV, P, TAIL, STREAM>(static_cast<const T *>(p.x) + r * p.ld_x, p.d, l, h);
+        load_row<LANES, NV, P, TAIL, STREAM>(static_cast<const G *>(p.grad_out) + r * p.ld_go, p.d, l, w);
         const float rstd = p.rstd[r];
         float dot = 0.f;
 #pragma unroll
@@ -349,13 +352,13 @@ template <typename T, typename G, int LANES, int NV, int P, bool STREAM> __globa
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[v][e] = rstd * (w[v][e] - h[v][e] * dot);
         if (p.grad_sum) {
-            load_row<LANES, NV, P, STREAM>(static_cast<const T *>(p.grad_sum) + r * p.ld_gs, p.d, l, h);
+            load_row<LANES, NV, P, TAIL, STREAM>(static_cast<const T *>(p.grad_sum) + r * p.ld_gs, p.d, l, h);
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[v][e] += h[v][e];
         }
-        store_row<LANES, NV, P, STREAM>(static_cast<T *>(p.grad_x) + r * p.ld_gx, p.d, l, w);
+        store_row<LANES, NV, P, TAIL, STREAM>(static_cast<T *>(p.grad_x) + r * p.ld_gx, p.d, l, w);
     }
     if (!p.part) return;
 #pragma unroll
@@ -433,14 +436,15 @@ template <typename T, typename O> static void launch_norm(const NormFwd &p, bool
         [&](auto lanes, auto nv) {
             constexpr int L = decltype(lanes)::value, V = decltype(nv)::value;
             const dim3 grid(row_blocks(p.n_rows, 256 / L, kNormBlocks));
-            auto go = [&](auto piece) {
+            auto go = [&](auto piece, auto tail) {
                 constexpr int P = decltype(piece)::value;
-                if (stream) hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, P, true>), grid, dim3(256), 0, st, p);
-                else hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, P, false>), grid, dim3(256), 0, st, p);
+                constexpr bool TAIL = decltype(tail)::value;
+                if (stream) hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, P, TAIL, true>), grid, dim3(256), 0, st, p);
+                else hipLaunchKernelGGL((rms_norm_kernel<T, O, L, V, P, TAIL, false>), grid, dim3(256), 0, st, p);
             };
-            if constexpr (sizeof(T) == 2 && sizeof(O) == 2) go(integral_constant<int, 8>{});
-            else if (sizeof(T) == 2 && sizeof(O) == 1 && p.d % 8 == 0) go(integral_constant<int, 8>{});
-            else go(integral_constant<int, 4>{});
+            if constexpr (sizeof(T) == 2 && sizeof(O) <= 2)
+                if (p.d % 8 == 0) return go(integral_constant<int, 8>{}, std::false_type{});
+            go(integral_constant<int, sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4>{}, std::true_type{});
         },
         [&] { hipLaunchKernelGGL((rms_norm_wide_kernel<T, O>), dim3(row_blocks(p.n_rows, 1, 8192)), dim3(256), 0, st, p); });
 }
@@ -453,12 +457,18 @@ template <typename T, typename G> static void launch_norm_bwd(const NormBwd &p, 
         [&](auto lanes, auto nv) {
             constexpr int L = decltype(lanes)::value, V = decltype(nv)::value;
             const dim3 grid(static_cast<unsigned>(n_part));
-            auto go = [&](auto piece) {
+            auto go = [&](auto piece, auto tail) {
                 constexpr int P = decltype(piece)::value;
-                if (stream) hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, P, true>), grid, dim3(256), 0, st, p);
-                else hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, P, false>), grid, dim3(256), 0, st, p);
+                constexpr bool TAIL = decltype(tail)::value;
+                if (stream) hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, P, TAIL, true>), grid, dim3(256), 0, st, p);
+                else hipLaunchKernelGGL((rms_norm_bwd_kernel<T, G, L, V, P, TAIL, false>), grid, dim3(256), 0, st, p);
             };
-            go(integral_constant<int, sizeof(T) == 2 && sizeof(G) == 2 ? 8 : 4>{});
+            if constexpr (sizeof(T) == 2 && sizeof(G) == 2) {
+                if (p.d % 8 == 0) go(integral_constant<int, 8>{}, std::false_type{});
+                else go(integral_constant<int, 8>{}, std::true_type{});
+            } else {
+                go(integral_constant<int, 4>{}, std::true_type{});
+            }
         },
         [&] {
             hipLaunchKernelGGL((rms_norm_bwd_wide_kernel<T, G>), dim3(row_blocks(p.n_rows, 1, 8192)), dim3(256), 0, st, p);
