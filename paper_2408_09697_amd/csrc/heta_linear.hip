@@ -200,7 +200,8 @@ extern "C" heta_status heta_linear(heta_graph *g, const heta_linear_args *a, voi
     if (!valid_dtype(a->out_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: outputs are fp32 or bf16", who);
     if (a->w_dt != a->in_dt || (a->in_dt == HETA_F32 && a->out_dt != HETA_F32))
         return fail(HETA_ERR_UNSUPPORTED, "%s: in and W have one type, and fp32 operands an fp32 output", who);
-    if (q != (a->in_scale != nullptr) || q != (a->w_scale != nullptr))
+    // no rows, no scales of theirs: an empty array's address may be null
+    if ((q ? !a->in_scale && a->n_rows > 0 : a->in_scale != nullptr) || q != (a->w_scale != nullptr))
         return fail(HETA_ERR_INVALID_ARG, "%s: scales belong to 8-bit operands, and those need them", who);
     if (!q && a->coarse_sums) return fail(HETA_ERR_INVALID_ARG, "%s: coarse sums are those of 8-bit operands", who);
     const size_t esz = q ? 1 : dtype_size(a->in_dt), osz = dtype_size(a->out_dt);

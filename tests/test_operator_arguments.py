@@ -1,0 +1,38 @@
+"""What heta_rms_norm, heta_linear, heta_muon_multi and their backward calls accept and refuse on the host, beyond what a single
+spoiled argument shows: no device call is made here, the addresses belong to nothing."""
+import ctypes
+
+import pytest
+
+from paper_2408_09697_amd import binding as hb
+
+BAD, SHAPE, UNSUPPORTED = hb.HETA_ERR_INVALID_ARG, hb.HETA_ERR_SHAPE, hb.HETA_ERR_UNSUPPORTED
+F32, BF16, E4M3 = hb.HETA_F32, hb.HETA_BF16, hb.HETA_E4M3
+AT = {name: 0x10000000 * (i + 1) for i, name in enumerate("abcdefghijkl")}  # 256 MB apart
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return hb.load_library()
+
+
+@pytest.fixture(scope="module")
+def handle():
+    return ctypes.addressof(ctypes.create_string_buffer(4096))
+
+
+def refused(lib, status, expect, needle=""):
+    assert status == expect, (status, lib.heta_last_error())
+    assert needle in lib.heta_last_error().decode()
+
+
+@pytest.mark.parametrize("coarse", [0, 1])
+def test_no_rows_of_8_bit_operands(lib, handle, coarse):
+    """An empty tensor's address is null: 8-bit rows and their scales may be, where there are none."""
+    a = dict(n_rows=0, d_in=64, d_out=48, inp=None, ld_in=64, in_scale=None, W=AT["b"], ld_w=64, w_scale=AT["h"], bias=AT["c"], out=None, ld_out=48,
+             in_dt=E4M3, w_dt=E4M3, out_dt=BF16, act=hb.HETA_ACT_GELU, coarse_sums=coarse)
+    assert lib.heta_linear(handle, ctypes.byref(hb._LinearArgs(**a)), None) == hb.HETA_OK
+    refused(lib, lib.heta_linear(handle, ctypes.byref(hb._LinearArgs(**{**a, "w_scale": None})), None), BAD, "scales")
+    refused(lib, lib.heta_linear(handle, ctypes.byref(hb._LinearArgs(**{**a, "n_rows": 1, "inp": AT["a"], "out": AT["d"]})), None), BAD, "scales")
+    f = {**a, "in_dt": F32, "w_dt": F32, "out_dt": F32, "coarse_sums": 0, "w_scale": None}
+    refused(lib, lib.heta_linear(handle, ctypes.byref(hb._LinearArgs(**{**f, "in_scale": AT["g"]})), None), BAD, "scales")
