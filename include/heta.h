@@ -703,7 +703,8 @@ heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int64_t ld_w, 
  * W: fp32 or bf16 (updated in fp32 and rounded back); m: fp32; grad: fp32 or bf16.  X is kept to 16 significant bits between the
  * steps' products (sums are fp32), which puts it 2.5e-5 of its norm off exact arithmetic.  All arrays are device memory, items
  * a HOST array; no array of an item may overlap what another item writes.  A zero gradient and momentum leave X = 0.  Uses the
- * handle's workspace (may grow it: 8 rows * cols + 8 min(rows, cols)^2 bytes an item).  n_items = 0 is a no-op. */
+ * handle's workspace (may grow it: 8 rows * cols + 8 min(rows, cols)^2 bytes an item).  HETA_ERR_UNSUPPORTED beyond 2^33 elements an
+ * item or, with k = min(rows, cols, 128) > 1, a longer side of 2^31 / (k - 1).  n_items = 0 is a no-op. */
 typedef struct heta_muon_item {
     void *W;
     int64_t ld_w;

@@ -266,6 +266,9 @@ template <bool B_RC> using NsDeep = TileShape<bf16_t, 2, kTerms, false, B_RC, kD
 template <bool B_RC> using NsSmall = TileShape<bf16_t, 2, kTerms, false, B_RC, kDirect, 2, 2, 1, 1, 64, 2, 1>;  // 64 x 64, two per CU
 template <bool B_RC> using NsLarge = TileShape<bf16_t, 2, kTerms, false, B_RC, kDirect, 2, 4, 2, 1, 64, 2, 1>;  // 128 x 128
 
+constexpr int64_t kTileRows = 128; // of an operand of any of them, at most
+static_assert(NsLarge<false>::BM <= kTileRows && NsLarge<false>::BN <= kTileRows, "the size check of heta_muon_multi counts rows of a tile");
+
 template <bool B_RC> static heta_status launch_terms(const char *who, TileArgs<TermsEpi> &p, hipStream_t st)
 {
     double bytes = 0, flops = 0;
@@ -398,7 +401,10 @@ extern "C" heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const het
         const size_t esz = dtype_size(q.dt), gsz = dtype_size(q.grad_dt);
         if (reinterpret_cast<uintptr_t>(q.W) % esz || reinterpret_cast<uintptr_t>(q.m) % 4 || reinterpret_cast<uintptr_t>(q.grad) % gsz)
             return fail(HETA_ERR_INVALID_ARG, "%s: item %d: pointer not aligned to its element size", who, i);
-        if (static_cast<int64_t>((q.rows + 31) / 32) * ((q.cols + 63) / 64) > (1 << 22)) return fail(HETA_ERR_UNSUPPORTED, "%s: item %d: matrix too large", who, i);
+        // a tile's rows (of the shorter side, 128 at most) are loaded by 32-bit offsets from its first one
+        const int64_t k = std::min(q.rows, q.cols), row_bytes = pad8(std::max(q.rows, q.cols)) * 2;
+        if ((int64_t(q.rows) + 31) / 32 * ((int64_t(q.cols) + 63) / 64) > (1 << 22) || (std::min<int64_t>(k, kTileRows) - 1) * row_bytes > (int64_t(1) << 32) - 1024)
+            return fail(HETA_ERR_UNSUPPORTED, "%s: item %d: matrix too large", who, i);
         const RowRange w(q.W, q.rows, q.ld_w, q.cols, esz), m(q.m, q.rows, q.ld_m, q.cols, 4), gr(q.grad, q.rows, q.ld_grad, q.cols, gsz);
         if (gr.overlaps(w) || gr.overlaps(m)) return fail(HETA_ERR_INVALID_ARG, "%s: item %d: the gradient overlaps an output", who, i);
         outs.emplace_back(i, w);

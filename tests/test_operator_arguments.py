@@ -36,3 +36,16 @@ def test_no_rows_of_8_bit_operands(lib, handle, coarse):
     refused(lib, lib.heta_linear(handle, ctypes.byref(hb._LinearArgs(**{**a, "n_rows": 1, "inp": AT["a"], "out": AT["d"]})), None), BAD, "scales")
     f = {**a, "in_dt": F32, "w_dt": F32, "out_dt": F32, "coarse_sums": 0, "w_scale": None}
     refused(lib, lib.heta_linear(handle, ctypes.byref(hb._LinearArgs(**{**f, "in_scale": AT["g"]})), None), BAD, "scales")
+
+
+HYPER = (0.02, 0.9, 1, 0.0, 1e-7, 5)
+
+
+def muon_item(rows, cols, **change):
+    return hb._MuonItem(**{**dict(W=AT["a"], ld_w=cols, m=AT["b"], ld_m=cols, grad=AT["c"], ld_grad=cols, rows=rows, cols=cols, dt=F32, grad_dt=F32), **change})
+
+
+@pytest.mark.parametrize("rows,cols", [(128, 17_000_000), (17_000_000, 128), (300, 17_000_000), (65, 2 ** 26 // 2 + 2 ** 20), (2, 2 ** 31 - 1), (1, 2 ** 31 - 1), (2 ** 31 - 1, 1)])
+def test_momentum_of_rows_whose_offsets_pass_32_bits(lib, handle, rows, cols):
+    """Offsets from a tile's first row count in 32 bits: longer rows are refused."""
+    refused(lib, lib.heta_muon_multi(handle, 1, ctypes.byref(muon_item(rows, cols)), *HYPER, None), UNSUPPORTED, "large")
