@@ -40,7 +40,7 @@ EXPORTS = ["heta_graph_create", "heta_graph_create_batch", "heta_graph_destroy",
            "heta_unique_relabel_batch", "heta_sample_hop", "heta_rel_aggregate_fwd_noalloc", "heta_attn_fold", "heta_attn_fold_bwd",
            "heta_graph_index_bytes", "heta_rms_norm", "heta_rms_norm_bwd", "heta_linear", "heta_linear_bwd", "heta_linear_pack_e4m3", "heta_muon_multi"]
 # process-wide switches for tests and measurements, declared in csrc/heta_test_hooks.h (not in the public header)
-TEST_HOOKS = ["heta_projection_force_staged", "heta_ingest_force", "heta_projection_f32_native"]
+TEST_HOOKS = ["heta_projection_force_staged", "heta_ingest_force", "heta_projection_f32_native", "heta_workspace_limit"]
 HETA_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 
@@ -1734,6 +1734,12 @@ def heta_projection_f32_native(on: bool) -> None:
     L = load_library()
     L.heta_projection_f32_native.argtypes = [ctypes.c_int32]
     _check(L.heta_projection_f32_native(1 if on else 0))
+
+
+def heta_workspace_limit(n_bytes: int) -> None:
+    L = load_library()
+    L.heta_workspace_limit.argtypes = [ctypes.c_int64]
+    _check(L.heta_workspace_limit(int(n_bytes)))
 
 
 def heta_calibration_copy(dst: torch.Tensor, src: torch.Tensor, stream=None) -> None:

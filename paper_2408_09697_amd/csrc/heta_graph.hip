@@ -162,6 +162,8 @@ void scratch_free(void *p)
     for (void *q : back) (void)hipFree(q);
 }
 
+static size_t g_ws_limit = 0; // test switch, see heta_test_hooks.h
+
 heta_status ensure_workspace(heta_graph *g, size_t bytes)
 {
     if (bytes <= g->ws_bytes)
@@ -175,7 +177,14 @@ heta_status ensure_workspace(heta_graph *g, size_t bytes)
         g->ws_bytes = 0;
     }
     size_t want = bytes + bytes / 4;
-    HETA_HIP(scratch_alloc(&g->d_ws, want));
+    if (g_ws_limit > 0 && bytes > g_ws_limit)
+        return fail(HETA_ERR_OOM, "workspace of %zu bytes: beyond the limit set for tests", bytes);
+    const hipError_t e = scratch_alloc(&g->d_ws, want);
+    if (e != hipSuccess) {
+        g->d_ws = nullptr;
+        (void)hipGetLastError(); // reported here, not by the next launch's check
+        return fail(e == hipErrorOutOfMemory ? HETA_ERR_OOM : HETA_ERR_DEVICE, "workspace of %zu bytes: %s", want, hipGetErrorString(e));
+    }
     g->ws_bytes = want;
     return HETA_OK;
 }
@@ -1129,6 +1138,13 @@ heta_status heta_ingest_force(int32_t mode)
 {
     if (mode < 0 || mode > 3) return fail(HETA_ERR_INVALID_ARG, "heta_ingest_force: mode must be 0, 1, 2 or 3");
     g_ingest_mode = mode;
+    return HETA_OK;
+}
+
+heta_status heta_workspace_limit(int64_t bytes)
+{
+    if (bytes < 0) return fail(HETA_ERR_INVALID_ARG, "heta_workspace_limit: negative size");
+    g_ws_limit = static_cast<size_t>(bytes);
     return HETA_OK;
 }
 

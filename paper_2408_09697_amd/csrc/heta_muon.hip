@@ -298,7 +298,7 @@ struct MuonPlan { // places in the workspace, in bytes, of one item
     int64_t ld_x, ld_g, x_plane, g_plane; // elements
     int64_t x[2], gram, poly, part, end;
     MuonPlan(int32_t rows, int32_t cols, int64_t at)
-        : k(std::min(rows, cols)), l(std::max(rows, cols)), parts(int64_t((rows + 31) / 32) * ((cols + 63) / 64)), ld_x(pad8(l)), ld_g(pad8(k)), x_plane(k * ld_x), g_plane(k * ld_g)
+        : k(std::min(rows, cols)), l(std::max(rows, cols)), parts((int64_t(rows) + 31) / 32 * ((int64_t(cols) + 63) / 64)), ld_x(pad8(l)), ld_g(pad8(k)), x_plane(k * ld_x), g_plane(k * ld_g)
     {
         auto take = [&](int64_t bytes) {
             const int64_t p = at;
@@ -314,16 +314,28 @@ struct MuonPlan { // places in the workspace, in bytes, of one item
     }
 };
 
-static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_item *items, int n, float lr, float mu, int nesterov, float wd, float eps, int steps,
+// Items that share their launches, as many as fit: kMuonItems, and the parts of a grid.
+struct MuonGroup {
+    std::vector<MuonPlan> plan;
+    int64_t bytes = 0, parts = 0; // of workspace, and workgroups of the element-wise kernels
+    MuonGroup(const heta_muon_item *items, int32_t left)
+    {
+        for (int32_t i = 0; i < left && i < kMuonItems; ++i) {
+            const MuonPlan p(items[i].rows, items[i].cols, bytes);
+            if (parts + p.parts > max_blocks(256)) break; // never the first: heta_muon_multi bounds an item's
+            plan.push_back(p);
+            bytes = p.end;
+            parts += p.parts;
+        }
+    }
+};
+
+// Launches alone: what it needs has been checked, and the workspace is there.
+static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_item *items, const MuonGroup &group, float lr, float mu, int nesterov, float wd, float eps, int steps,
                               hipStream_t st)
 {
-    int64_t at = 0;
-    std::vector<MuonPlan> plan;
-    for (int i = 0; i < n; ++i) {
-        plan.emplace_back(items[i].rows, items[i].cols, at);
-        at = plan.back().end;
-    }
-    HETA_TRY(ensure_workspace(g, static_cast<size_t>(at)));
+    const std::vector<MuonPlan> &plan = group.plan;
+    const int n = static_cast<int>(plan.size());
     char *ws = static_cast<char *>(g->d_ws);
     MuonArgs a{};
     a.n = n;
@@ -342,7 +354,6 @@ static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_it
         blocks += pl.parts;
         elems += static_cast<double>(q.rows) * q.cols;
         esz = static_cast<double>(dtype_size(q.grad_dt));
-        if (blocks > max_blocks(256)) return fail(HETA_ERR_UNSUPPORTED, "%s: too many elements for one launch", who);
     }
     const dim3 grid(static_cast<unsigned>(blocks));
     {
@@ -412,8 +423,18 @@ extern "C" heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const het
         ins.emplace_back(i, gr);
     }
     if (items_collide(outs, ins)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps another item's arrays", who);
+    // every group's workspace before the first group's launches: a call that fails has updated nothing
+    std::vector<MuonGroup> groups;
+    int64_t need = 0;
+    for (int32_t i = 0; i < n_items; i += static_cast<int32_t>(groups.back().plan.size())) {
+        groups.emplace_back(items + i, n_items - i);
+        need = std::max(need, groups.back().bytes);
+    }
+    if (n_items > 0) HETA_TRY(ensure_workspace(g, static_cast<size_t>(need)));
     hipStream_t st = as_stream(hip_stream);
-    for (int32_t i = 0; i < n_items; i += kMuonItems)
-        HETA_TRY(muon_group(who, g, items + i, std::min<int32_t>(kMuonItems, n_items - i), lr, momentum, nesterov != 0, weight_decay, eps, steps, st));
+    for (const MuonGroup &group : groups) {
+        HETA_TRY(muon_group(who, g, items, group, lr, momentum, nesterov != 0, weight_decay, eps, steps, st));
+        items += group.plan.size();
+    }
     return HETA_OK;
 }

@@ -25,6 +25,10 @@ heta_status heta_projection_force_staged(int32_t on);
  * instead: the same results to rounding order at about 2.5 times the matrix-pipe time. */
 heta_status heta_projection_f32_native(int32_t on);
 
+/* Workspaces of handles that are to grow beyond `bytes` fail to (HETA_ERR_OOM), as with a device that is full; what a handle
+ * holds already stays usable.  0 (the default): no limit. */
+heta_status heta_workspace_limit(int64_t bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,3 +35,31 @@ def test_a_block_of_no_rows(handle, agg):
     assert block.forward(x, x.clone() if agg else None).shape == (0, 32)
     assert block.backward(x).shape == (0, 32)
     assert all((v == 0).all() for v in block.grads.values() if v is not None)
+
+
+@pytest.fixture
+def workspace_limit():
+    """Sets what a handle's workspace may grow to, as if the device were full beyond it."""
+    yield heta.binding.heta_workspace_limit
+    heta.binding.heta_workspace_limit(0)
+
+
+def test_momentum_that_cannot_have_its_workspace_updates_nothing(workspace_limit):
+    """More matrices than share launches, the last of them large: the call fails before the first ones are touched, and can be repeated."""
+    g = heta.heta_graph_create([(1, 1, 0)], [])
+    make = lambda: [(randn(i, 24, 40), randn(50 + i, 24, 40), randn(90 + i, 24, 40)) for i in range(12)] + [(randn(40, 300, 500), randn(41, 300, 500), randn(42, 300, 500))]  # noqa: E731
+    items, start, want = make(), make(), make()
+    heta.heta_muon_multi(g, want)
+    g.destroy()
+    g = heta.heta_graph_create([(1, 1, 0)], [])
+    workspace_limit(1 << 20)
+    with pytest.raises(heta.HetaError) as e:
+        heta.heta_muon_multi(g, items)
+    assert e.value.args and "workspace" in str(e.value)
+    for a, b in zip(items, start):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    workspace_limit(0)
+    heta.heta_muon_multi(g, items)
+    for a, b in zip(items, want):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    g.destroy()
