@@ -12,6 +12,7 @@
 // |u| is summed per part of 32 x 64, then over the parts in a fixed order by every workgroup that needs it.
 #include <algorithm>
 #include <cmath>
+#include <new>
 
 #include "heta_tiles.h"
 
@@ -395,8 +396,8 @@ static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_it
 
 using namespace heta;
 
-extern "C" heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t nesterov, float weight_decay, float eps,
-                                       int32_t steps, void *hip_stream)
+static heta_status muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t nesterov, float weight_decay, float eps, int32_t steps,
+                              void *hip_stream)
 {
     const char *who = "heta_muon_multi";
     if (!g || n_items < 0 || (n_items > 0 && !items)) return fail(HETA_ERR_INVALID_ARG, "%s: bad handle or item list", who);
@@ -437,4 +438,15 @@ extern "C" heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const het
         items += group.plan.size();
     }
     return HETA_OK;
+}
+
+// No exception crosses the boundary: host containers may throw std::bad_alloc.
+extern "C" heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t nesterov, float weight_decay, float eps,
+                                       int32_t steps, void *hip_stream)
+{
+    try {
+        return muon_multi(g, n_items, items, lr, momentum, nesterov, weight_decay, eps, steps, hip_stream);
+    } catch (const std::bad_alloc &) {
+        return fail(HETA_ERR_OOM, "heta_muon_multi: host allocation failed");
+    }
 }

@@ -1,6 +1,9 @@
 """What heta_rms_norm, heta_linear, heta_muon_multi and their backward calls accept and refuse on the host, beyond what a single
 spoiled argument shows: no device call is made here, the addresses belong to nothing."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -49,3 +52,26 @@ def muon_item(rows, cols, **change):
 def test_momentum_of_rows_whose_offsets_pass_32_bits(lib, handle, rows, cols):
     """Offsets from a tile's first row count in 32 bits: longer rows are refused."""
     refused(lib, lib.heta_muon_multi(handle, 1, ctypes.byref(muon_item(rows, cols)), *HYPER, None), UNSUPPORTED, "large")
+
+
+OUT_OF_MEMORY = """
+import ctypes, resource
+from paper_2408_09697_amd import binding as hb
+lib = hb.load_library()
+n = 3_000_000
+item = bytes(hb._MuonItem(W=0x10000000, ld_w=48, m=0x20000000, ld_m=48, grad=0x30000000, ld_grad=48, rows=64, cols=48, dt=hb.HETA_F32, grad_dt=hb.HETA_F32))
+items = item * n
+handle = ctypes.create_string_buffer(4096)
+with open("/proc/self/statm") as f:
+    size = int(f.read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (size + (64 << 20), resource.RLIM_INFINITY))
+status = lib.heta_muon_multi(ctypes.addressof(handle), n, items, 0.02, 0.9, 1, 0.0, 1e-7, 5, None)
+print(status, lib.heta_last_error().decode())
+"""
+
+
+def test_momentum_without_host_memory_for_its_lists():
+    """An exception of the host's containers becomes a status (in a process of its own, whose address space ends 64 MB ahead)."""
+    r = subprocess.run([sys.executable, "-c", OUT_OF_MEMORY], capture_output=True, text=True, timeout=100, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, r.stderr[-500:]
+    assert r.stdout.startswith(f"{hb.HETA_ERR_OOM} ") and "host allocation" in r.stdout, r.stdout
