@@ -91,7 +91,7 @@ template <typename O> static void fold_launch(const float *part, int64_t n_part,
 
 heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void *out, heta_dtype out_dt, int32_t width, int64_t ld, hipStream_t st)
 {
-    if ((total + 3) / 4 / 2 >= max_blocks(256)) return fail(HETA_ERR_UNSUPPORTED, "sum of partials: too many columns for one launch");
+    if (total > kFoldMost) return fail(HETA_ERR_UNSUPPORTED, "sum of partials: too many columns for one launch");
     ProfScope prof("fold_partials_kernel", st, static_cast<double>(total) * (4.0 * n_part + dtype_size(out_dt)), static_cast<double>(total) * n_part);
     if (out_dt == HETA_F32) fold_launch(part, n_part, total, static_cast<float *>(out), width, ld, st);
     else fold_launch(part, n_part, total, static_cast<bf16_t *>(out), width, ld, st);

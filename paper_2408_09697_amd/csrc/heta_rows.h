@@ -129,6 +129,7 @@ inline bool streams(double bytes) { return bytes > 256e6; }
 
 // out[c] (or, for rows of `width`, out[(c / width) * ld + c % width]) = sum over s < n_part of part[s * total + c], c < total,
 // in a fixed order; out is fp32 or bf16.  Deterministic second half of sums over rows that many workgroups share.
+constexpr int64_t kFoldMost = int64_t(256) * (max_blocks(256) - 1); // columns
 heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void *out, heta_dtype out_dt, int32_t width, int64_t ld, hipStream_t st);
 
 } // namespace heta

@@ -63,3 +63,18 @@ def test_momentum_that_cannot_have_its_workspace_updates_nothing(workspace_limit
     for a, b in zip(items, want):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
     g.destroy()
+
+
+def integers(seed, r, c, dtype, most=2, pad=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    buf = torch.full((r, c + pad), float("nan"), device="cuda").to(dtype)
+    buf[:, :c] = torch.randint(-most, most + 1, (r, c), generator=g, device="cuda").to(dtype)
+    return buf[:, :c]
+
+
+def test_weight_gradient_of_many_elements(handle):
+    """16,384 x 8,200: more columns than a launch of one workgroup per eight of them would hold."""
+    x, go = integers(1, 70, 16384, BF16), integers(2, 70, 8200, BF16)
+    gw = torch.full((16384, 8200), 7.0, device="cuda")
+    heta.heta_linear_bwd(handle, x, None, go, grad_W=gw)
+    assert torch.equal(gw, x.float().t() @ go.float())
