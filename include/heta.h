@@ -665,8 +665,10 @@ heta_status heta_linear(heta_graph *g, const heta_linear_args *args, void *hip_s
  *   grad_in  = (grad_pre . W^T) * in_act'(in_pre)   (NULL: not computed; in_act = NONE: no factor.  With the activation that made
  *              `in`, grad_in is the gradient at its pre-activation in_pre [n_rows, d_in], what the product before takes as grad_out)
  *   dW       = in^T . grad_pre          (dw_dt: fp32, or bf16 for bf16 operands; NULL: not computed), rows added in a fixed order
- * The gradient of the residual is grad_out.  grad_pre may be grad_out or pre, grad_in may be in_pre; all outputs are
- * overwritten.  Uses the handle's workspace (may grow it). */
+ * The products read grad_pre as it is stored (rounded to dt).  The gradient of the residual is grad_out.  grad_pre may be grad_out or
+ * pre, grad_in may be in_pre; all outputs are overwritten.  HETA_ERR_UNSUPPORTED: dW from 2^31 rows or some 2^32 elements on.
+ * Uses the handle's workspace (may grow it: by partial sums of dW, 64 MB at most or one dW where that is more, and, for long bf16 operands whose rows are not
+ * 16-byte aligned, by copies of them of up to 1 GiB; without memory for these the call runs on the operands as they are). */
 typedef struct heta_linear_bwd_args {
     int64_t n_rows;
     int32_t d_in, d_out;

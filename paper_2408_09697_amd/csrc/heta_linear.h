@@ -199,6 +199,24 @@ struct Launch {
     bool direct(size_t elt) const { return direct_rows(it.A, it.lda, elt) && direct_rows(it.B, it.ldb, elt); }
     bool large() const { return tiles_of(it.M, it.N, 256, 256) * it.n_split >= 128; }
 };
+// How a product of few tiles and a long contraction is split: so that a workgroup has about eight k-tiles and most of the chip one
+// workgroup; a second launch adds the parts up and does the epilogue (114 x 1,611 x 7: 114 -> 15 us).  Small tiles are 64 x 64 of 128 bytes of k-values.
+struct SplitPlan {
+    int64_t k_per_split = 0;
+    int32_t n_split = 1; // 1: not split
+    size_t bytes = 0;    // of partial products
+};
+inline SplitPlan plan_split(const Launch &l, size_t elt)
+{
+    SplitPlan s;
+    const int64_t bk = 128 / static_cast<int64_t>(elt), tiles = tiles_of(l.it.M, l.it.N, 64, 64), k_tiles = (l.it.K + bk - 1) / bk;
+    const int64_t splits = l.large() ? 0 : std::min(k_tiles / 8, 256 / tiles);
+    if (splits < 2) return s;
+    s.k_per_split = (k_tiles + splits - 1) / splits * bk;
+    s.n_split = static_cast<int32_t>((l.it.K + s.k_per_split - 1) / s.k_per_split);
+    s.bytes = static_cast<size_t>(s.n_split) * l.it.M * l.it.N * sizeof(float);
+    return s;
+}
 // f(std::integral_constant<int, a>) for activation a
 template <typename F> inline heta_status with_act(int a, F f)
 {
@@ -212,8 +230,10 @@ heta_status launch_linear_f32(const Launch &l, bool input_gradient, const Linear
 heta_status launch_linear_bf16(const Launch &l, bool input_gradient, heta_dtype out_dt, const LinearExtra &x);
 heta_status launch_linear_e4m3(const Launch &l, heta_dtype out_dt, bool coarse, const LinearExtra &x);
 heta_status launch_grad_w_f32(const Launch &l, float *part);
-// Copies operands of a large weight gradient whose rows start anywhere to aligned rows, in the workspace from byte `offset` on.
-heta_status align_grad_w_bf16(Launch &l, size_t offset);
+// Bytes of the copies, in aligned rows, of the operands of a large weight gradient whose rows start anywhere (0: none are worth it), and
+// the copies themselves, `to` (256-byte aligned) that many bytes of the workspace.
+size_t align_grad_w_bytes(const Launch &l);
+heta_status align_grad_w_bf16(Launch &l, char *to);
 heta_status launch_grad_w_bf16(const Launch &l, float *part);
 
 // one type's launches from its tile shapes: large tiles (Reading: where the epilogue reads in the output's shape), small ones, and
@@ -224,15 +244,13 @@ inline heta_status launch_linear(const Launch &l, size_t elt, const LinearExtra 
     constexpr bool SCALED = Large::EB == 1;
     const bool direct = l.direct(elt);
     if (!l.large()) {
-        // Few tiles and a long contraction: it is split so that a workgroup has about eight k-tiles and most of the chip one
-        // workgroup; a second launch adds the parts up and does the epilogue (114 x 1,611 x 7: 114 -> 15 us).
-        const int64_t tiles = tiles_of(l.it.M, l.it.N, Small::BM, Small::BN), k_tiles = (l.it.K + Small::BK - 1) / Small::BK;
-        const int64_t splits = std::min(k_tiles / 8, 256 / tiles);
-        if (splits >= 2) {
+        static_assert(Small::BM == 64 && Small::BN == 64 && Small::BK * sizeof(typename Small::S) == 128, "plan_split() counts such tiles");
+        const SplitPlan split = plan_split(l, elt);
+        if (split.n_split > 1) {
             Launch part = l;
-            part.it.k_per_split = (k_tiles + splits - 1) / splits * Small::BK;
-            part.it.n_split = static_cast<int32_t>((l.it.K + part.it.k_per_split - 1) / part.it.k_per_split);
-            HETA_TRY(ensure_workspace(l.g, static_cast<size_t>(part.it.n_split) * l.it.M * l.it.N * sizeof(float)));
+            part.it.k_per_split = split.k_per_split;
+            part.it.n_split = split.n_split;
+            HETA_TRY(ensure_workspace(l.g, split.bytes));
             float *ws = static_cast<float *>(l.g->d_ws);
             const PartialEpi::Extra px{ws, l.it.N};
             HETA_TRY((direct ? part.go<Small, PartialEpi>(px) : part.go<StagedSmall, PartialEpi>(px)));

@@ -284,12 +284,27 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
         n_split = (n + k_per_split - 1) / k_per_split;
     }
     const int64_t w_elems = n_split * a->d_in * a->d_out;
-    if (bias_off + w_elems > 0) HETA_TRY(ensure_workspace(g, static_cast<size_t>(bias_off + w_elems) * sizeof(float)));
+    const void *gpre = acts ? a->grad_pre : a->grad_out;
+    const int64_t ld_gpre = acts ? a->ld_gp : a->ld_go;
+    const double flops = 2.0 * n * a->d_in * a->d_out;
+    const double in_bytes = (static_cast<double>(n) * (a->d_in * (fused ? 2 : 1) + a->d_out) + static_cast<double>(a->d_in) * a->d_out) * esz;
+    const Launch in_l{g, who, "linear_grad_in_kernel", TileItem{gpre, a->W, ld_gpre, a->ld_w, 0, 0, n, a->d_in, a->d_out, a->d_out, 1, 0, 0, 0, 0, 0}, in_bytes, flops, st};
+    Launch w_l{g, who, "linear_grad_w_kernel", TileItem{a->in, gpre, a->ld_in, ld_gpre, 0, 0, a->d_in, a->d_out, n, k_per_split, static_cast<int32_t>(n_split), 0, 0, 0, 0, 0},
+               static_cast<double>(n) * (a->d_in + a->d_out) * esz + 4.0 * w_elems, flops, st};
+
+    // Everything that can fail comes before the first launch.  The copies to aligned rows are only faster: without room for them the
+    // operands are read as they are.
+    if (a->dW && (n >= (int64_t(1) << 31) || static_cast<int64_t>(a->d_in) * a->d_out > kFoldMost))
+        return fail(HETA_ERR_UNSUPPORTED, "%s: weight gradient of too many rows or elements", who);
+    size_t need = static_cast<size_t>(bias_off + w_elems) * sizeof(float);
+    const size_t copies_at = (need + 255) / 256 * 256;
+    size_t copies = a->dW && n > 0 && a->dt == HETA_BF16 ? align_grad_w_bytes(w_l) : 0;
+    if (a->grad_in && n > 0) need = std::max(need, plan_split(in_l, esz).bytes);
+    if (copies > 0 && ensure_workspace(g, std::max(need, copies_at + copies)) != HETA_OK) copies = 0;
+    if (need > 0) HETA_TRY(ensure_workspace(g, need));
     float *ws = static_cast<float *>(g->d_ws);
 
     // gradient at the pre-activation
-    const void *gpre = acts ? a->grad_pre : a->grad_out;
-    const int64_t ld_gpre = acts ? a->ld_gp : a->ld_go;
     if (n > 0 && (acts || a->dbias)) {
         const double bytes = static_cast<double>(n) * a->d_out * esz * (acts ? 3 : 1);
         ProfScope prof("act_grad_kernel", st, bytes, static_cast<double>(n) * a->d_out);
@@ -307,20 +322,14 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
     }
     if (a->dbias) HETA_TRY(fold_partials(ws, n > 0 ? slabs : 0, a->d_out, a->dbias, HETA_F32, a->d_out, a->d_out, st));
 
-    const double flops = 2.0 * n * a->d_in * a->d_out;
     if (a->grad_in && n > 0) {
         const LinearExtra x{nullptr, nullptr, nullptr, fused ? a->in_pre : nullptr, nullptr, a->grad_in, a->ld_ip, 0, a->ld_gi, HETA_ACT_NONE, a->in_act};
-        const double bytes = (static_cast<double>(n) * (a->d_in * (fused ? 2 : 1) + a->d_out) + static_cast<double>(a->d_in) * a->d_out) * esz;
-        const Launch l{g, who, "linear_grad_in_kernel", TileItem{gpre, a->W, ld_gpre, a->ld_w, 0, 0, n, a->d_in, a->d_out, a->d_out, 1, 0, 0, 0, 0, 0}, bytes, flops, st};
-        HETA_TRY(a->dt == HETA_F32 ? launch_linear_f32(l, true, x) : launch_linear_bf16(l, true, HETA_BF16, x));
+        HETA_TRY(a->dt == HETA_F32 ? launch_linear_f32(in_l, true, x) : launch_linear_bf16(in_l, true, HETA_BF16, x));
     }
     if (a->dW) {
-        Launch l{g, who, "linear_grad_w_kernel",
-                 TileItem{a->in, gpre, a->ld_in, ld_gpre, 0, 0, a->d_in, a->d_out, n, k_per_split, static_cast<int32_t>(n_split), 0, 0, 0, 0, 0},
-                 static_cast<double>(n) * (a->d_in + a->d_out) * esz + 4.0 * w_elems, flops, st};
-        if (n > 0 && a->dt == HETA_BF16) HETA_TRY(align_grad_w_bf16(l, static_cast<size_t>(bias_off + w_elems) * sizeof(float)));
-        float *part = static_cast<float *>(g->d_ws) + bias_off; // the workspace may have grown since its first use
-        if (n > 0) HETA_TRY(a->dt == HETA_F32 ? launch_grad_w_f32(l, part) : launch_grad_w_bf16(l, part));
+        float *part = ws + bias_off;
+        if (copies > 0) HETA_TRY(align_grad_w_bf16(w_l, static_cast<char *>(g->d_ws) + copies_at));
+        if (n > 0) HETA_TRY(a->dt == HETA_F32 ? launch_grad_w_f32(w_l, part) : launch_grad_w_bf16(w_l, part));
         HETA_TRY(fold_partials(part, n_split, static_cast<int64_t>(a->d_in) * a->d_out, a->dW, a->dw_dt, a->d_out, a->ld_dw, st));
     }
     return HETA_OK;

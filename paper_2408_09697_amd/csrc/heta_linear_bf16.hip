@@ -52,18 +52,23 @@ static __global__ void __launch_bounds__(256) align_rows_kernel(const bf16_t *sr
 //   both: 300,000 x 301 x 301 612 / 285, 10^6 x 101 x 103 497 / 323;  below 32 MB: 9,000 x 257 x 259 25 / 38, 4,000 x 1,030 x 1,030 67 / 74
 //   one, read by one tile: 100,000 x 789 x 64 89 / 114, 100,000 x 256 x 789 116 / 129
 // At most 1 GiB is copied.
-heta_status align_grad_w_bf16(Launch &l, size_t offset)
+size_t align_grad_w_bytes(const Launch &l)
+{
+    const TileItem &it = l.it;
+    const bool a_in = direct_rows(it.A, it.lda, 2), b_in = direct_rows(it.B, it.ldb, 2);
+    const int64_t a_ld = (it.M + 7) / 8 * 8, b_ld = (it.N + 7) / 8 * 8;
+    const size_t bytes = static_cast<size_t>(it.K) * ((a_in ? 0 : a_ld) + (b_in ? 0 : b_ld)) * 2;
+    if (!l.large() || bytes < (size_t(32) << 20) || bytes > (size_t(1) << 30)) return 0;
+    if ((a_in && it.M <= 256) || (b_in && it.N <= 128)) return 0;
+    if (a_ld * 2 >= (int64_t(1) << 23) || b_ld * 2 >= (int64_t(1) << 23)) return 0; // the copies could not go straight into LDS either
+    return bytes;
+}
+
+heta_status align_grad_w_bf16(Launch &l, char *to)
 {
     TileItem &it = l.it;
     const bool a_in = direct_rows(it.A, it.lda, 2), b_in = direct_rows(it.B, it.ldb, 2);
     const int64_t a_ld = (it.M + 7) / 8 * 8, b_ld = (it.N + 7) / 8 * 8;
-    const size_t a_bytes = a_in ? 0 : static_cast<size_t>(it.K) * a_ld * 2, b_bytes = b_in ? 0 : static_cast<size_t>(it.K) * b_ld * 2;
-    if (!l.large() || a_bytes + b_bytes < (size_t(32) << 20) || a_bytes + b_bytes > (size_t(1) << 30)) return HETA_OK;
-    if ((a_in && it.M <= 256) || (b_in && it.N <= 128)) return HETA_OK;
-    if (a_ld * 2 >= (int64_t(1) << 23) || b_ld * 2 >= (int64_t(1) << 23)) return HETA_OK; // the copies could not go straight into LDS either
-    offset = (offset + 255) / 256 * 256;
-    HETA_TRY(ensure_workspace(l.g, offset + a_bytes + b_bytes));
-    char *to = static_cast<char *>(l.g->d_ws) + offset;
     const int64_t rows = it.K;
     auto copy = [&](const void *&p, int64_t &ld, int64_t cols, int64_t ld_to) {
         ProfScope prof("align_rows_kernel", l.st, 4.0 * rows * cols, 0);

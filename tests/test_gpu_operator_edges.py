@@ -72,6 +72,27 @@ def integers(seed, r, c, dtype, most=2, pad=0):
     return buf[:, :c]
 
 
+def test_linear_backward_in_little_memory(workspace_limit):
+    """Copies of unaligned operands are left out where there is no room for them (the same result), and where there is none for the partial sums
+    the call fails with its outputs untouched."""
+    n, d_in, d_out = 100_000, 301, 517  # copies of 165 MB, partial sums of 26 MB
+    x, W, go = integers(1, n, d_in, BF16), integers(2, d_in, d_out, BF16), integers(3, n, d_out, BF16)
+    outs = lambda: (torch.full((n, d_in), 7.0, device="cuda", dtype=BF16), torch.full((d_in, d_out), 7.0, device="cuda"), torch.full((d_out,), 7.0, device="cuda"))  # noqa: E731
+    want = (go.float() @ W.float().t()).to(BF16), x.float().t() @ go.float(), go.float().sum(0)
+    for limit in (0, 64 << 20, 1 << 20):
+        g, (gi, gw, gb) = heta.heta_graph_create([(1, 1, 0)], []), outs()
+        workspace_limit(limit)
+        if limit == 1 << 20:
+            with pytest.raises(heta.HetaError):
+                heta.heta_linear_bwd(g, x, W, go, grad_in=gi, grad_W=gw, grad_bias=gb)
+            assert all((t == 7.0).all() for t in (gi, gw, gb))
+            workspace_limit(0)
+        heta.heta_linear_bwd(g, x, W, go, grad_in=gi, grad_W=gw, grad_bias=gb)
+        for got, ref in zip((gi, gw, gb), want):
+            assert torch.equal(got, ref), limit
+        g.destroy()
+
+
 def test_weight_gradient_of_many_elements(handle):
     """16,384 x 8,200: more columns than a launch of one workgroup per eight of them would hold."""
     x, go = integers(1, 70, 16384, BF16), integers(2, 70, 8200, BF16)

@@ -75,3 +75,12 @@ def test_momentum_without_host_memory_for_its_lists():
     r = subprocess.run([sys.executable, "-c", OUT_OF_MEMORY], capture_output=True, text=True, timeout=100, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert r.returncode == 0, r.stderr[-500:]
     assert r.stdout.startswith(f"{hb.HETA_ERR_OOM} ") and "host allocation" in r.stdout, r.stdout
+
+
+@pytest.mark.parametrize("change", [{"d_in": 70000, "d_out": 70000}, {"n_rows": 2 ** 31}])
+def test_weight_gradients_too_large_are_refused_before_anything_else(lib, handle, change):
+    a = dict(n_rows=100, d_in=64, d_out=48, dt=BF16, dw_dt=F32, act=hb.HETA_ACT_SILU, in_act=0)
+    a.update(change)
+    at = {name: 1 << 44 | i << 40 for i, name in enumerate(("inp", "W", "grad_out", "pre", "grad_pre", "grad_in", "dW", "dbias"))}  # 1 TB apart
+    lds = dict(ld_inp=a["d_in"], ld_W=a["d_out"], ld_grad_out=a["d_out"], ld_pre=a["d_out"], ld_grad_pre=a["d_out"], ld_grad_in=a["d_in"], ld_dW=a["d_out"])
+    refused(lib, lib.heta_linear_bwd(handle, ctypes.byref(hb._LinearBwdArgs(**a, **at, **lds)), None), UNSUPPORTED, "weight gradient")
