@@ -615,7 +615,8 @@ heta_status heta_sparse_adam_multi(int32_t n_items, const heta_adam_item *items,
  *   x, residual (NULL: none), sum (NULL: not stored): device [n_rows, d] of x_dt; gamma: device fp32 [d] (NULL: ones);
  *   rstd: device fp32 [n_rows] (NULL: not stored).  sum may be x or residual (same rows).
  *   out: x_dt, or bf16, or HETA_E4M3: then scale (device fp32 [n_rows], otherwise NULL) receives
- *   max_j |out_ij| / 448 and out holds the nearest 8-bit values of out / scale (a row of zeros: zeros, scale 0).
+ *   max_j |out_ij| / 448 and out holds the nearest 8-bit values of out / scale (a row of zeros: zeros, scale 0; a row with a NaN
+ *   among its outputs: NaN throughout, scale too).
  *   bf16 rows have no fp32 output. */
 heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, const void *residual, int64_t ld_res,
                           const float *gamma, float eps, void *sum, int64_t ld_sum, void *out, heta_dtype out_dt, int64_t ld_out,

@@ -157,17 +157,11 @@ template <typename E> __global__ void __launch_bounds__(256) pack_e4m3_kernel(co
     const int64_t j = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (j >= d_out) return;
-    float amax = 0.f;
-    for (int k = lane; k < d_in; k += 64) {
-        const float x = fabsf(widen(W[k * ld_w + j]));
-        amax = x > amax || x != x ? x : amax;
-    }
+    uint32_t top = 0;
+    for (int k = lane; k < d_in; k += 64) top = max(top, magnitude(widen(W[k * ld_w + j])));
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const float x = __shfl_xor(amax, o);
-        amax = x > amax || x != x ? x : amax;
-    }
-    const float inv = amax > 0.f ? fminf(448.f / amax, 3.402823466e38f) : (amax != amax ? amax : 0.f);
+    for (int o = 32; o > 0; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o)));
+    const float amax = __uint_as_float(top), inv = e4m3_factor(amax);
     for (int k = lane; k < d_in; k += 64) {
         const float x = widen(W[k * ld_w + j]) * inv;
         out[j * ld_out + k] = static_cast<uint8_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);

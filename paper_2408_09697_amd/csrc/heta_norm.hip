@@ -32,10 +32,10 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
     for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
-template <int LANES> __device__ __forceinline__ float lanes_max(float v)
+template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
 {
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    for (int o = LANES / 2; o > 0; o >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), o)));
     return v;
 }
 
@@ -174,9 +174,6 @@ __device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d
     const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
 }
-// 8-bit scale of a row whose largest magnitude is amax: the factor (0 for a row of zeros); amax / 448 may be subnormal
-__device__ __forceinline__ float e4m3_factor(float amax) { return amax > 0.f ? fminf(448.f / amax, 3.402823466e38f) : 0.f; }
-
 template <int LANES, int NV, int P> __device__ __forceinline__ void store_row_e4m3(uint8_t *row, int d, int l, const float (&x)[NV][8], float f)
 {
 #pragma unroll
@@ -240,12 +237,12 @@ template <typename T, typename O, int LANES, int NV, int P, bool TAIL, bool STRE
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[v][e] = x[v][e] * rstd * gamma[v][e];
         if constexpr (sizeof(O) == 1) {
-            float amax = 0.f;
+            uint32_t top = 0;
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[v][e]));
-            amax = lanes_max<LANES>(amax);
+                for (int e = 0; e < 8; ++e) top = max(top, magnitude(x[v][e]));
+            const float amax = __uint_as_float(lanes_max<LANES>(top));
             if (l == 0) p.scale[r] = amax / 448.f;
             store_row_e4m3<LANES, NV, P>(static_cast<uint8_t *>(p.out) + r * p.ld_out, p.d, l, x, e4m3_factor(amax));
         } else {
@@ -254,14 +251,22 @@ template <typename T, typename O, int LANES, int NV, int P, bool TAIL, bool STRE
     }
 }
 
-// Sum (or maximum) over the 256 threads of a workgroup, in every thread.
-template <bool MAX> __device__ __forceinline__ float group_reduce(float v, float *lds)
+// Sum, and largest magnitude, over the 256 threads of a workgroup, in every thread.
+__device__ __forceinline__ float group_sum(float v, float *lds)
 {
-    v = MAX ? lanes_max<64>(v) : lanes_sum<64>(v);
+    v = lanes_sum<64>(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return MAX ? fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3])) : (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+__device__ __forceinline__ float group_max(uint32_t v, float *lds)
+{
+    v = lanes_max<64>(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = __uint_as_float(v);
+    __syncthreads();
+    return __uint_as_float(max(max(__float_as_uint(lds[0]), __float_as_uint(lds[1])), max(__float_as_uint(lds[2]), __float_as_uint(lds[3]))));
 }
 
 // Rows too wide for one wavefront's registers: a workgroup per row.  `sum` may alias x or residual: a thread reads its
@@ -281,16 +286,16 @@ template <typename T, typename O> __global__ void __launch_bounds__(256) rms_nor
             }
             ss += s * s;
         }
-        const float rstd = 1.f / sqrtf(group_reduce<false>(ss, lds) / static_cast<float>(p.d) + p.eps);
+        const float rstd = 1.f / sqrtf(group_sum(ss, lds) / static_cast<float>(p.d) + p.eps);
         if (p.rstd && threadIdx.x == 0) p.rstd[r] = rstd;
         auto value = [&](int c) {
             const float s = sum ? widen(sum[c]) : (y ? rounded<T>(widen(x[c]) + widen(y[c])) : widen(x[c]));
             return s * rstd * (p.gamma ? p.gamma[c] : 1.f);
         };
         if constexpr (sizeof(O) == 1) {
-            float amax = 0.f;
-            for (int c = threadIdx.x; c < p.d; c += 256) amax = fmaxf(amax, fabsf(value(c)));
-            amax = group_reduce<true>(amax, lds);
+            uint32_t top = 0;
+            for (int c = threadIdx.x; c < p.d; c += 256) top = max(top, magnitude(value(c)));
+            const float amax = group_max(top, lds);
             if (threadIdx.x == 0) p.scale[r] = amax / 448.f;
             const float f = e4m3_factor(amax);
             for (int c = threadIdx.x; c < p.d; c += 256) {
@@ -386,7 +391,7 @@ template <typename T, typename G> __global__ void __launch_bounds__(256) rms_nor
         const float rstd = p.rstd[r];
         float dot = 0.f;
         for (int c = threadIdx.x; c < p.d; c += 256) dot += widen(go[c]) * (p.gamma ? p.gamma[c] : 1.f) * (widen(x[c]) * rstd);
-        dot = group_reduce<false>(dot, lds) / static_cast<float>(p.d);
+        dot = group_sum(dot, lds) / static_cast<float>(p.d);
         for (int c = threadIdx.x; c < p.d; c += 256) {
             float v = rstd * (widen(go[c]) * (p.gamma ? p.gamma[c] : 1.f) - widen(x[c]) * rstd * dot);
             if (gs) v += widen(gs[c]);

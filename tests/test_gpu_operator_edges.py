@@ -99,3 +99,23 @@ def test_weight_gradient_of_many_elements(handle):
     gw = torch.full((16384, 8200), 7.0, device="cuda")
     heta.heta_linear_bwd(handle, x, None, go, grad_W=gw)
     assert torch.equal(gw, x.float().t() @ go.float())
+
+
+@pytest.mark.parametrize("d", [24, 200, 789, 2048, 2500])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_8_bit_rows_with_nan_and_infinities(d, dtype):
+    """A NaN among a row's outputs makes its scale and values NaN, as in packed weights; an infinity times the reciprocal root of an infinite sum is one."""
+    x = randn(1, 20, d).to(dtype)
+    clean = x.clone()
+    x[2, d - 1], x[5, 0], x[9, d // 2], x[12] = float("nan"), float("inf"), -float("inf"), float("nan")
+    out, ref, scale, scale0 = torch.empty(20, d, device="cuda", dtype=E4M3), torch.empty(20, d, device="cuda", dtype=E4M3), torch.empty(20, device="cuda"), torch.empty(20, device="cuda")
+    heta.heta_rms_norm(x, out, scale=scale)
+    heta.heta_rms_norm(clean, ref, scale=scale0)
+    bad = [2, 5, 9, 12]
+    keep = [i for i in range(20) if i not in bad]
+    assert scale[bad].isnan().all() and out.float()[bad].isnan().all()
+    assert torch.equal(scale[keep], scale0[keep]) and torch.equal(out.float()[keep], ref.float()[keep])
+    W = x.t().contiguous()
+    packed, ws = torch.empty(20, d, device="cuda", dtype=E4M3), torch.empty(20, device="cuda")
+    heta.heta_linear_pack_e4m3(W, packed, ws)
+    assert ws[[2, 12]].isnan().all() and packed.float()[[2, 12]].isnan().all() and torch.isfinite(ws[keep]).all()
