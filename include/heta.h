@@ -615,8 +615,8 @@ heta_status heta_sparse_adam_multi(int32_t n_items, const heta_adam_item *items,
  *   x, residual (NULL: none), sum (NULL: not stored): device [n_rows, d] of x_dt; gamma: device fp32 [d] (NULL: ones);
  *   rstd: device fp32 [n_rows] (NULL: not stored).  sum may be x or residual (same rows).
  *   out: x_dt, or bf16, or HETA_E4M3: then scale (device fp32 [n_rows], otherwise NULL) receives
- *   max_j |out_ij| / 448 and out holds the nearest 8-bit values of out / scale (a row of zeros: zeros, scale 0; a row with a NaN
- *   among its outputs: NaN throughout, scale too).
+ *   max_j |out_ij| / 448 and out holds the nearest 8-bit values of out / scale (a row of zeros, or of nothing from 2^-119 on:
+ *   zeros, scale 0; a row with a NaN among its outputs: NaN throughout, scale too).
  *   bf16 rows have no fp32 output. */
 heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, const void *residual, int64_t ld_res,
                           const float *gamma, float eps, void *sum, int64_t ld_sum, void *out, heta_dtype out_dt, int64_t ld_out,
@@ -695,7 +695,7 @@ typedef struct heta_linear_bwd_args {
 } heta_linear_bwd_args;
 heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args *args, void *hip_stream);
 /* Weights W [d_in, d_out] (fp32 or bf16) as 8-bit rows: packed [d_out, ld_packed >= d_in] of HETA_E4M3, scale [d_out] =
- * max_k |W[k, j]| / 448.  Once per set of weights. */
+ * max_k |W[k, j]| / 448 (columns of zeros and with NaN as in heta_rms_norm).  Once per set of weights. */
 heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int64_t ld_w, int32_t d_in, int32_t d_out, void *packed, int64_t ld_packed,
                                   float *scale, void *hip_stream);
 

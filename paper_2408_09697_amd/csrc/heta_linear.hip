@@ -166,7 +166,7 @@ template <typename E> __global__ void __launch_bounds__(256) pack_e4m3_kernel(co
         const float x = widen(W[k * ld_w + j]) * inv;
         out[j * ld_out + k] = static_cast<uint8_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
     }
-    if (lane == 0) scale[j] = amax / 448.f;
+    if (lane == 0) scale[j] = e4m3_scale(amax);
 }
 
 // ---- host side ---------------------------------------------------------------------------------------

@@ -243,7 +243,7 @@ template <typename T, typename O, int LANES, int NV, int P, bool TAIL, bool STRE
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = max(top, magnitude(x[v][e]));
             const float amax = __uint_as_float(lanes_max<LANES>(top));
-            if (l == 0) p.scale[r] = amax / 448.f;
+            if (l == 0) p.scale[r] = e4m3_scale(amax);
             store_row_e4m3<LANES, NV, P>(static_cast<uint8_t *>(p.out) + r * p.ld_out, p.d, l, x, e4m3_factor(amax));
         } else {
             store_row<LANES, NV, P, TAIL, STREAM>(static_cast<O *>(p.out) + r * p.ld_out, p.d, l, x);
@@ -296,7 +296,7 @@ template <typename T, typename O> __global__ void __launch_bounds__(256) rms_nor
             uint32_t top = 0;
             for (int c = threadIdx.x; c < p.d; c += 256) top = max(top, magnitude(value(c)));
             const float amax = group_max(top, lds);
-            if (threadIdx.x == 0) p.scale[r] = amax / 448.f;
+            if (threadIdx.x == 0) p.scale[r] = e4m3_scale(amax);
             const float f = e4m3_factor(amax);
             for (int c = threadIdx.x; c < p.d; c += 256) {
                 const float v = value(c) * f;

@@ -126,9 +126,11 @@ template <typename O> __device__ __forceinline__ uintx4 load_piece(const O *p, i
 // 8-bit rows.  |v| as an integer: ordered like the magnitudes, infinity above the numbers and NaN above infinity, so that the largest of a
 // row with a NaN is NaN (fmaxf drops it).
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-// What the values of a row (or column) whose largest magnitude is amax are multiplied by; its scale is amax / 448, which may be subnormal.
-// 0 for zeros; NaN makes scale and values NaN.
-__device__ __forceinline__ float e4m3_factor(float amax) { return amax > 0.f ? fminf(448.f / amax, 3.402823466e38f) : amax; }
+// What the values of a row (or column) whose largest magnitude is amax are multiplied by, and its scale, which may be subnormal.  Below 2^-119
+// the factor 448 / amax leaves fp32's range: such rows count as zeros.  NaN makes scale and values NaN.
+constexpr float kE4m3Least = 1.504632769052528e-36f; // 2^-119
+__device__ __forceinline__ float e4m3_factor(float amax) { return amax >= kE4m3Least ? 448.f / amax : amax != amax ? amax : 0.f; }
+__device__ __forceinline__ float e4m3_scale(float amax) { return amax < kE4m3Least ? 0.f : amax / 448.f; }
 
 // Calls that move more than the chip's 256 MB last-level cache holds read and write with the streaming hint; below, what a
 // call writes is still cached when the next one reads it.

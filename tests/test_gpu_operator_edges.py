@@ -119,3 +119,24 @@ def test_8_bit_rows_with_nan_and_infinities(d, dtype):
     packed, ws = torch.empty(20, d, device="cuda", dtype=E4M3), torch.empty(20, device="cuda")
     heta.heta_linear_pack_e4m3(W, packed, ws)
     assert ws[[2, 12]].isnan().all() and packed.float()[[2, 12]].isnan().all() and torch.isfinite(ws[keep]).all()
+
+
+@pytest.mark.parametrize("d", [16, 200, 2500])
+def test_8_bit_rows_near_the_smallest_numbers(d):
+    """Rows x whose largest value is m, with eps = 1: their reciprocal roots are 1, and out = x.  A value is off by half a step of e4m3 (2^-4 of it, or 2^-10 of the scale),
+    the factor and the scale by three roundings and by half a subnormal step of the scale; from 2^-119 down rows are zeros with scale 0."""
+    tops = [1e-30, 6e-36, 5e-36, 2e-36, 1.6e-36, 1.4e-36, 1e-37, 1e-38, 1e-42]
+    x = torch.rand(len(tops), d, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda", dtype=torch.float64) * 2 - 1
+    x[:, d // 3] = 1.0
+    x = (x * torch.tensor(tops, device="cuda", dtype=torch.float64)[:, None]).float()
+    q, scale = torch.empty(len(tops), d, device="cuda", dtype=E4M3), torch.empty(len(tops), device="cuda")
+    w8, ws = torch.empty_like(q), torch.empty_like(scale)
+    heta.heta_rms_norm(x, q, eps=1.0, scale=scale)
+    heta.heta_linear_pack_e4m3(x.t().contiguous(), w8, ws)
+    assert torch.equal(ws, scale) and torch.equal(w8.float(), q.float())
+    kept = [i for i, t in enumerate(tops) if t >= 2.0 ** -119]
+    gone = [i for i, t in enumerate(tops) if t < 2.0 ** -119]
+    assert (scale[gone] == 0).all() and (q[gone].float() == 0).all()
+    s, y = scale[kept].double()[:, None], x[kept].double()
+    off = (q[kept].float().double() * s - y).abs()
+    assert (off <= (2.0 ** -4 + 4 * U) * y.abs() + 2.0 ** -10 * (1 + 4 * U) * s + 448 * 2.0 ** -150).all()
