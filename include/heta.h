@@ -617,7 +617,8 @@ heta_status heta_sparse_adam_multi(int32_t n_items, const heta_adam_item *items,
  *   out: x_dt, or bf16, or HETA_E4M3: then scale (device fp32 [n_rows], otherwise NULL) receives
  *   max_j |out_ij| / 448 and out holds the nearest 8-bit values of out / scale (a row of zeros, or of nothing from 2^-119 on:
  *   zeros, scale 0; a row with a NaN among its outputs: NaN throughout, scale too).
- *   bf16 rows have no fp32 output. */
+ *   bf16 rows have no fp32 output.  Sums are fp32: with eps = 0 a row whose squares add up to 0 there has rstd 0 and zeros as outputs; one
+ *   whose squares pass 3.4e38 has rstd 0, too. */
 heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, const void *residual, int64_t ld_res,
                           const float *gamma, float eps, void *sum, int64_t ld_sum, void *out, heta_dtype out_dt, int64_t ld_out,
                           float *scale, float *rstd, void *hip_stream);

@@ -39,6 +39,9 @@ template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
     return v;
 }
 
+// Without eps, a row whose squares add up to nothing has no reciprocal root; 0 makes its outputs zeros, and so its share of the gradients.
+__device__ __forceinline__ float reciprocal_root(float mean_sq) { return mean_sq == 0.f ? 0.f : 1.f / sqrtf(mean_sq); }
+
 // A lane's eight values of chunk v are 8 / P pieces of P consecutive columns; the pieces of a group of lanes lie side by side, so
 // that an access of the widest type among the row's arrays is 16 bytes of consecutive memory per lane (P = 4 where fp32 is among
 // them, else 8).  100,000 unaligned rows of 789 fp32 columns, backward: 328 us with eight consecutive columns per lane; of bf16
@@ -230,7 +233,7 @@ template <typename T, typename O, int LANES, int NV, int P, bool TAIL, bool STRE
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int e = 0; e < 8; ++e) ss += x[v][e] * x[v][e];
-        const float rstd = 1.f / sqrtf(lanes_sum<LANES>(ss) / static_cast<float>(p.d) + p.eps);
+        const float rstd = reciprocal_root(lanes_sum<LANES>(ss) / static_cast<float>(p.d) + p.eps);
         if (p.rstd && l == 0) p.rstd[r] = rstd;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
@@ -286,7 +289,7 @@ template <typename T, typename O> __global__ void __launch_bounds__(256) rms_nor
             }
             ss += s * s;
         }
-        const float rstd = 1.f / sqrtf(group_sum(ss, lds) / static_cast<float>(p.d) + p.eps);
+        const float rstd = reciprocal_root(group_sum(ss, lds) / static_cast<float>(p.d) + p.eps);
         if (p.rstd && threadIdx.x == 0) p.rstd[r] = rstd;
         auto value = [&](int c) {
             const float s = sum ? widen(sum[c]) : (y ? rounded<T>(widen(x[c]) + widen(y[c])) : widen(x[c]));

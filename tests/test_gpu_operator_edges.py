@@ -140,3 +140,26 @@ def test_8_bit_rows_near_the_smallest_numbers(d):
     s, y = scale[kept].double()[:, None], x[kept].double()
     off = (q[kept].float().double() * s - y).abs()
     assert (off <= (2.0 ** -4 + 4 * U) * y.abs() + 2.0 ** -10 * (1 + 4 * U) * s + 448 * 2.0 ** -150).all()
+
+
+@pytest.mark.parametrize("d", [24, 256, 789, 2500])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_of_zeros_without_eps(handle, d, dtype):
+    """No reciprocal root of 0: such rows give zeros, and gradients that pass the norm by alone; their neighbours are those of other calls."""
+    x, go, gs = randn(1, 9, d).to(dtype), randn(2, 9, d).to(dtype), randn(3, 9, d).to(dtype)
+    clean = x.clone()
+    x[2], x[6] = 0.0, 0.0
+    keep = [i for i in range(9) if i not in (2, 6)]
+    for out_dtype in (dtype, E4M3):
+        out, ref = torch.empty(9, d, device="cuda", dtype=out_dtype), torch.empty(9, d, device="cuda", dtype=out_dtype)
+        scale = torch.empty(9, device="cuda") if out_dtype is E4M3 else None
+        rstd, rstd0 = torch.empty(9, device="cuda"), torch.empty(9, device="cuda")
+        heta.heta_rms_norm(x, out, eps=0.0, scale=scale, rstd=rstd)
+        heta.heta_rms_norm(clean, ref, eps=0.0, scale=None if scale is None else torch.empty(9, device="cuda"), rstd=rstd0)
+        assert (out[[2, 6]].float() == 0).all() and (rstd[[2, 6]] == 0).all() and (scale is None or (scale[[2, 6]] == 0).all())
+        assert torch.equal(out[keep].float(), ref[keep].float()) and torch.equal(rstd[keep], rstd0[keep])
+    gx, gg, gg0 = torch.empty_like(x), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    heta.heta_rms_norm_bwd(handle, x, rstd, go, gx, grad_sum=gs, grad_gamma=gg)
+    assert torch.equal(gx[[2, 6]], gs[[2, 6]]) and torch.isfinite(gx.float()).all()
+    heta.heta_rms_norm_bwd(handle, x[keep], rstd[keep].contiguous(), go[keep], torch.empty_like(x[keep]), grad_gamma=gg0)
+    assert float((gg - gg0).abs().max()) <= 160 * U * float((go.double() * x.double() * rstd.double()[:, None]).abs().sum(0).max())
