@@ -518,6 +518,13 @@ extern "C" heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, h
     // every array is read and written row by row by the lanes that hold the row: outputs may lie on inputs, in the same rows
     const RowRange rx(x, n_rows, ld_x, d, esz), rr(residual, n_rows, ld_res, d, esz), rs(sum, n_rows, ld_sum, d, esz), ro(out, n_rows, ld_out, d, osz);
     const bool sum_on_x = sum == x && ld_sum == ld_x, sum_on_res = sum == residual && ld_sum == ld_res;
+    const RowRange rg(gamma, 1, d, d, 4), rscale(scale, 1, n_rows, n_rows, 4), rrstd(rstd, 1, n_rows, n_rows, 4);
+    for (const RowRange &o : {rs, ro})
+        for (const RowRange &v : {rg, rscale, rrstd})
+            if (o.overlaps(v)) return fail(HETA_ERR_INVALID_ARG, "%s: gamma, scale or rstd overlaps out or sum", who);
+    for (const RowRange &v : {rx, rr, rg})
+        if (rscale.overlaps(v) || rrstd.overlaps(v)) return fail(HETA_ERR_INVALID_ARG, "%s: scale or rstd overlaps an operand", who);
+    if (rscale.overlaps(rrstd)) return fail(HETA_ERR_INVALID_ARG, "%s: scale overlaps rstd", who);
     if ((rs.overlaps(rx) && !sum_on_x) || (rs.overlaps(rr) && !sum_on_res) || ro.overlaps(rx) || ro.overlaps(rr) || ro.overlaps(rs))
         return fail(HETA_ERR_INVALID_ARG, "%s: out overlaps another array, or sum one in other rows", who);
     if (n_rows == 0) return HETA_OK;
@@ -559,6 +566,10 @@ extern "C" heta_status heta_rms_norm_bwd(heta_graph *g, int64_t n_rows, int32_t 
     // grad_x may be grad_sum (the same lane reads and writes); rows of more than 2,048 columns read x and grad_out twice
     if (ro.overlaps(rx) || ro.overlaps(rg) || (ro.overlaps(rs) && !(grad_x == grad_sum && ld_gx == ld_gs)))
         return fail(HETA_ERR_INVALID_ARG, "%s: grad_x overlaps an operand", who);
+    const RowRange rgamma(gamma, 1, d, d, 4), rrstd(rstd, 1, n_rows, n_rows, 4), rgg(grad_gamma, 1, d, d, 4);
+    if (ro.overlaps(rgamma) || ro.overlaps(rrstd)) return fail(HETA_ERR_INVALID_ARG, "%s: grad_x overlaps an operand", who);
+    for (const RowRange &v : {rx, rg, rs, ro, rgamma, rrstd})
+        if (rgg.overlaps(v)) return fail(HETA_ERR_INVALID_ARG, "%s: grad_gamma overlaps an operand or grad_x", who);
     int64_t n_part = 0;
     by_width(d, [&](auto lanes, auto) { n_part = row_blocks(n_rows, 256 / decltype(lanes)::value, kNormBwdBlocks); }, [&] { n_part = row_blocks(n_rows, 32, 256); });
     if (n_rows == 0) n_part = 0;

@@ -84,3 +84,26 @@ def test_weight_gradients_too_large_are_refused_before_anything_else(lib, handle
     at = {name: 1 << 44 | i << 40 for i, name in enumerate(("inp", "W", "grad_out", "pre", "grad_pre", "grad_in", "dW", "dbias"))}  # 1 TB apart
     lds = dict(ld_inp=a["d_in"], ld_W=a["d_out"], ld_grad_out=a["d_out"], ld_pre=a["d_out"], ld_grad_pre=a["d_out"], ld_grad_in=a["d_in"], ld_dW=a["d_out"])
     refused(lib, lib.heta_linear_bwd(handle, ctypes.byref(hb._LinearBwdArgs(**a, **at, **lds)), None), UNSUPPORTED, "weight gradient")
+
+
+NORM = dict(n=100, d=64, x=AT["a"], x_dt=F32, ld_x=64, res=AT["b"], ld_res=64, gamma=AT["c"], eps=1e-6, sum=AT["d"], ld_sum=64, out=AT["e"], out_dt=F32, ld_out=64,
+            scale=None, rstd=AT["f"], stream=None)
+NORM8 = dict(NORM, out_dt=E4M3, scale=AT["g"])
+
+
+@pytest.mark.parametrize("base,change", [
+    (NORM, {"gamma": AT["d"] + 64}), (NORM, {"gamma": AT["e"] + 99 * 256}), (NORM, {"rstd": AT["a"] + 256}), (NORM, {"rstd": AT["b"]}), (NORM, {"rstd": AT["c"] + 128}),
+    (NORM, {"rstd": AT["d"] + 512}), (NORM, {"rstd": AT["e"] + 512}), (NORM8, {"scale": AT["a"]}), (NORM8, {"scale": AT["c"] + 252}), (NORM8, {"scale": AT["e"] + 64}),
+    (NORM8, {"scale": AT["d"]}), (NORM8, {"scale": AT["f"] + 396})])
+def test_norm_vectors_that_overlap(lib, base, change):
+    refused(lib, lib.heta_rms_norm(*{**base, **change}.values()), BAD, "overlaps")
+
+
+NORM_BWD = dict(g=1, n=100, d=64, x=AT["a"], x_dt=F32, ld_x=64, gamma=AT["c"], rstd=AT["d"], go=AT["e"], go_dt=F32, ld_go=64, gs=AT["f"], ld_gs=64, gx=AT["g"], ld_gx=64,
+                gg=AT["h"], stream=None)
+
+
+@pytest.mark.parametrize("change", [{"gg": AT["a"]}, {"gg": AT["c"] + 16}, {"gg": AT["d"] + 396}, {"gg": AT["e"] + 256}, {"gg": AT["f"]}, {"gg": AT["g"] + 99 * 256 + 252},
+                                    {"gamma": AT["g"] + 64}, {"rstd": AT["g"] + 99 * 256}])
+def test_norm_backward_vectors_that_overlap(lib, handle, change):
+    refused(lib, lib.heta_rms_norm_bwd(*{**NORM_BWD, **change, "g": handle}.values()), BAD, "overlaps")
