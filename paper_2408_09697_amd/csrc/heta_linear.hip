@@ -212,6 +212,8 @@ extern "C" heta_status heta_linear(heta_graph *g, const heta_linear_args *a, voi
     const bool same_rows = a->residual == a->out && a->ld_res == a->ld_out; // read and written by the same lane
     if (out.overlaps(in) || out.overlaps(w) || out.overlaps(pre) || pre.overlaps(in) || pre.overlaps(w) || pre.overlaps(res) || (out.overlaps(res) && !same_rows))
         return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);
+    for (const RowRange &v : {RowRange(a->bias, 1, a->d_out, a->d_out, 4), RowRange(a->in_scale, 1, a->n_rows, a->n_rows, 4), RowRange(a->w_scale, 1, a->d_out, a->d_out, 4)})
+        if (out.overlaps(v) || pre.overlaps(v)) return fail(HETA_ERR_INVALID_ARG, "%s: bias or a scale overlaps an output", who);
     if (a->n_rows == 0) return HETA_OK;
     const LinearExtra x{a->bias, a->in_scale, a->w_scale, a->residual, a->pre, a->out, a->ld_res, a->ld_pre, a->ld_out, a->act, HETA_ACT_NONE};
     const double bytes = static_cast<double>(a->n_rows) * (a->d_in * esz + a->d_out * osz * (1.0 + !!a->residual + !!a->pre)) + static_cast<double>(a->d_in) * a->d_out * esz;

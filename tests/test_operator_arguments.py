@@ -107,3 +107,15 @@ NORM_BWD = dict(g=1, n=100, d=64, x=AT["a"], x_dt=F32, ld_x=64, gamma=AT["c"], r
                                     {"gamma": AT["g"] + 64}, {"rstd": AT["g"] + 99 * 256}])
 def test_norm_backward_vectors_that_overlap(lib, handle, change):
     refused(lib, lib.heta_rms_norm_bwd(*{**NORM_BWD, **change, "g": handle}.values()), BAD, "overlaps")
+
+
+LINEAR = dict(n_rows=100, d_in=64, d_out=48, inp=AT["a"], ld_in=64, W=AT["b"], ld_w=48, bias=AT["c"], residual=AT["d"], ld_res=48, pre=AT["e"], ld_pre=48, out=AT["f"], ld_out=48,
+              in_dt=F32, w_dt=F32, out_dt=F32, act=hb.HETA_ACT_GELU)
+LINEAR8 = dict(LINEAR, in_dt=E4M3, w_dt=E4M3, ld_w=64, in_scale=AT["g"], w_scale=AT["h"])
+
+
+@pytest.mark.parametrize("base,change", [
+    (LINEAR, {"bias": AT["f"] + 192}), (LINEAR, {"bias": AT["e"] + 99 * 192}), (LINEAR8, {"in_scale": AT["f"]}), (LINEAR8, {"in_scale": AT["e"] + 1920}),
+    (LINEAR8, {"w_scale": AT["f"] + 4}), (LINEAR8, {"w_scale": AT["e"]}), (LINEAR8, {"bias": AT["f"]})])
+def test_linear_vectors_that_overlap(lib, handle, base, change):
+    refused(lib, lib.heta_linear(handle, ctypes.byref(hb._LinearArgs(**{**base, **change})), None), BAD, "overlaps")
