@@ -127,6 +127,30 @@ template <bool RC, int ROWS, int BK, int EB, int NW, int T> struct PlaneLoader {
     }
 };
 
+// Three terms of eight values (split3_pair), also of those beyond bf16's range, whose first term would be infinite and the others NaN:
+//   from 2^128 - 2^119 on: the largest bf16 number, and what is left of the value;
+//   infinity: +-1, 0, +-infinity.  A product then has an infinite term only where the factor against it is the other operand's first
+//   term, which is 0 for 0 alone: infinity times 0 is NaN, times anything else infinity of their signs, infinity too.
+constexpr float kBeyondBf16 = 3.3961775292304957e38f; // 2^128 - 2^119
+template <bool CAREFUL> __device__ __forceinline__ void split3_chunk(const float (&x)[8], uint32_t (&h)[4], uint32_t (&m)[4], uint32_t (&l)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) split3_pair(x[2 * j], x[2 * j + 1], h[j], m[j], l[j]);
+    if constexpr (!CAREFUL) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (!(fabsf(x[e]) >= kBeyondBf16)) continue; // NaN has NaN terms already
+        const bool inf = fabsf(x[e]) > 3.402823466e38f;
+        const float first = copysignf(inf ? 1.f : 3.3895313892515355e38f, x[e]), rest = inf ? 0.f : x[e] - first;
+        const bf16_t mid = to_bf16(rest);
+        const uint32_t t[3] = {to_bf16(first), mid, to_bf16(inf ? x[e] : rest - widen(mid))};
+        const int at = 16 * (e & 1);
+        h[e / 2] = (h[e / 2] & ~(0xffffu << at)) | t[0] << at;
+        m[e / 2] = (m[e / 2] & ~(0xffffu << at)) | t[1] << at;
+        l[e / 2] = (l[e / 2] & ~(0xffffu << at)) | t[2] << at;
+    }
+}
+
 // ---- memory -> registers -> LDS ---------------------------------------------------------------------
 // An item is one 16-byte chunk of the image: E consecutive elements, converted to the planes of their type.  Elements
 // beyond the matrix count as zero.
@@ -167,6 +191,23 @@ template <typename S, bool RC, int ROWS, int BK, int EB, int NT, int T> struct S
     }
     __device__ __forceinline__ void store(char *lds, int tid) const
     {
+        if constexpr (T == 1) {
+            put<false>(lds, tid);
+        } else {
+            // a wavefront with a value beyond bf16's range takes the longer way
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int w = 0; w < W; ++w)
+                    top = fmaxf(fmaxf(fmaxf(top, fabsf(__uint_as_float(raw[i][w].x))), fmaxf(fabsf(__uint_as_float(raw[i][w].y)), fabsf(__uint_as_float(raw[i][w].z)))),
+                                fabsf(__uint_as_float(raw[i][w].w)));
+            if (__builtin_expect(__any(top >= kBeyondBf16), 0)) put<true>(lds, tid);
+            else put<false>(lds, tid);
+        }
+    }
+    template <bool CAREFUL> __device__ __forceinline__ void put(char *lds, int tid) const
+    {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int q = tid + NT * i;
@@ -175,15 +216,15 @@ template <typename S, bool RC, int ROWS, int BK, int EB, int NT, int T> struct S
             if constexpr (T == 1) {
                 *reinterpret_cast<uint4 *>(to) = raw[i][0];
             } else {
+                static_assert(E == 8 && T == 3, "the splitting of a chunk");
                 union { uint4 u[W]; float f[E]; } x;
 #pragma unroll
                 for (int w = 0; w < W; ++w) x.u[w] = raw[i][w];
                 uint32_t h[4], m[4], l[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) split3_pair(x.f[2 * j], x.f[2 * j + 1], h[j], m[j], l[j]);
+                split3_chunk<CAREFUL>(x.f, h, m, l);
                 *reinterpret_cast<uint4 *>(to) = make_uint4(h[0], h[1], h[2], h[3]);
                 *reinterpret_cast<uint4 *>(to + Img::BYTES) = make_uint4(m[0], m[1], m[2], m[3]);
-                if constexpr (T == 3) *reinterpret_cast<uint4 *>(to + 2 * Img::BYTES) = make_uint4(l[0], l[1], l[2], l[3]);
+                *reinterpret_cast<uint4 *>(to + 2 * Img::BYTES) = make_uint4(l[0], l[1], l[2], l[3]);
             }
         }
     }

@@ -163,3 +163,37 @@ def test_rows_of_zeros_without_eps(handle, d, dtype):
     assert torch.equal(gx[[2, 6]], gs[[2, 6]]) and torch.isfinite(gx.float()).all()
     heta.heta_rms_norm_bwd(handle, x[keep], rstd[keep].contiguous(), go[keep], torch.empty_like(x[keep]), grad_gamma=gg0)
     assert float((gg - gg0).abs().max()) <= 160 * U * float((go.double() * x.double() * rstd.double()[:, None]).abs().sum(0).max())
+
+
+def same_with_infinities(got, ref, bound, what):
+    got = got.double()
+    assert torch.equal(got.isnan(), ref.isnan()), what
+    inf = ref.isinf()
+    assert torch.equal(got[inf], ref[inf]), what
+    fine = torch.isfinite(ref)
+    assert ((got - ref).abs()[fine] <= bound[fine]).all(), what
+
+
+@pytest.mark.parametrize("n,d_in,d_out", [(40, 24, 56), (300, 203, 136), (40000, 64, 264), (257, 2050, 40)])
+def test_fp32_products_of_infinities_and_of_the_largest_numbers(handle, n, d_in, d_out):
+    """The definition's results: infinity times 0 is NaN, times anything else infinity of their signs.  Other sums are those of the values: at most (2 k + 16) u of sum |a||b| off,
+    also where a value is beyond bf16's largest."""
+    x, W = integers(1, n, d_in, F32, 3), integers(2, d_in, d_out, F32, 3) / 16
+    go = integers(3, n, d_out, F32, 3)
+    x[3, 5], x[7, 1], x[7, 2], x[11, d_in - 1], x[12, 4] = float("inf"), float("inf"), -float("inf"), -float("inf"), float("nan")
+    x[15, 3], x[16, 4], x[16, 7], x[17, 0] = 3.4028234e38, -3.4e38, 3.3961775e38, 3.39e38
+    W[2, 9], W[8, 11] = -float("inf"), float("inf")
+    go[n - 1, 2], go[n - 2, 3], go[5, 4] = float("inf"), -float("inf"), -3.402e38
+    a, b, c = x.cpu().double(), W.cpu().double(), go.cpu().double()
+    out = torch.empty(n, d_out, device="cuda")
+    heta.heta_linear(handle, x, W, out)
+    fin = lambda t: torch.where(torch.isfinite(t), t, torch.zeros_like(t)).abs()  # noqa: E731
+    same_with_infinities(out.cpu(), a @ b, (2 * d_in + 16) * U * (fin(a) @ fin(b)), "out")
+    gi, gw = torch.empty_like(x), torch.empty_like(W)
+    heta.heta_linear_bwd(handle, x, W, go, grad_in=gi, grad_W=gw)
+    same_with_infinities(gi.cpu(), c @ b.t(), (2 * d_out + 16) * U * (fin(c) @ fin(b).t()), "grad_in")
+    x = integers(4, n, d_in, F32, 1) / 64
+    x[3, 5], x[7, 1], x[12, 4], x[15, 3] = float("inf"), -float("inf"), float("nan"), 3.4028234e38
+    a, c = x.cpu().double(), torch.where(c.abs() > 1e30, torch.ones_like(c), c) / 4
+    heta.heta_linear_bwd(handle, x, None, c.float().cuda(), grad_W=gw)
+    same_with_infinities(gw.cpu(), a.t() @ c, (2 * n + 600) * U * (fin(a).t() @ fin(c)), "grad_W")
