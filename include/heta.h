@@ -701,14 +701,18 @@ heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int64_t ld_w, 
                                   float *scale, void *hip_stream);
 
 /* heta_muon_multi: orthogonalised momentum (Muon, Jordan et al. 2024) on n_items weight matrices [rows, cols] of products in . W:
- *   m <- momentum m + grad;   u = nesterov ? grad + momentum m : m;   X = u / (|u|_F + eps);
+ *   m <- momentum m + grad;   u = grad + momentum m with HETA_MUON_NESTEROV among the flags, else m;   X = u / (|u|_F + eps);
  *   `steps` times  X <- 3.4445 X + (-4.7750 A + 2.0315 A A) X  with  A = X X^T  (of the shorter side);
  *   W <- (1 - lr weight_decay) W - lr sqrt(max(1, cols / rows)) X.
- * W: fp32 or bf16 (updated in fp32 and rounded back); m: fp32; grad: fp32 or bf16.  X is kept to 16 significant bits between the
- * steps' products (sums are fp32), which puts it 2.5e-5 of its norm off exact arithmetic.  All arrays are device memory, items
- * a HOST array; no array of an item may overlap what another item writes.  A zero gradient and momentum leave X = 0.  Uses the
- * handle's workspace (may grow it: 8 rows * cols + 8 min(rows, cols)^2 bytes an item).  HETA_ERR_UNSUPPORTED beyond 2^33 elements an
+ * W: fp32 or bf16 (updated in fp32 and rounded back); m: fp32; grad: fp32 or bf16.  Between the steps' products X is kept to fp32 for fp32
+ * weights (the update is 2.3e-7 of its norm off exact arithmetic) and to 16 significant bits for bf16 ones and with HETA_MUON_COARSE
+ * (2.5e-5, at half the products); sums are fp32, that of the
+ * squares of u too (|u| below 1.8e19).  All arrays are device memory, items a HOST array; no array of an item may overlap what
+ * another item writes.  A zero gradient and momentum leave X = 0.  Uses the handle's workspace (may grow it: for the up to 12 matrices of one
+ * kind that share launches, 12 rows * cols + 12 min(rows, cols)^2 bytes each, 8 where X has 16 bits).  HETA_ERR_UNSUPPORTED beyond 2^33 elements an
  * item or, with k = min(rows, cols, 128) > 1, a longer side of 2^31 / (k - 1).  n_items = 0 is a no-op. */
+#define HETA_MUON_NESTEROV 1
+#define HETA_MUON_COARSE 2
 typedef struct heta_muon_item {
     void *W;
     int64_t ld_w;
@@ -719,7 +723,7 @@ typedef struct heta_muon_item {
     int32_t rows, cols;
     heta_dtype dt, grad_dt;
 } heta_muon_item;
-heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t nesterov,
+heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t flags,
                             float weight_decay, float eps, int32_t steps, void *hip_stream);
 
 /* ---- meta-partitioning (Section 5, Algorithm 2): which relations a GPU (or machine) holds ---------

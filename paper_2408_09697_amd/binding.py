@@ -23,6 +23,7 @@ HETA_F32, HETA_BF16, HETA_E4M3 = 0, 1, 2
 HETA_SUM, HETA_MEAN = 0, 1
 HETA_ACT_NONE, HETA_ACT_RELU, HETA_ACT_GELU, HETA_ACT_SILU = 0, 1, 2, 3
 HETA_PTRS_ON_DEVICE = 1
+HETA_MUON_NESTEROV, HETA_MUON_COARSE = 1, 2
 
 EXPORTS = ["heta_graph_create", "heta_graph_create_batch", "heta_graph_destroy", "heta_scratch_release", "heta_graph_get_csc", "heta_graph_get_degrees",
            "heta_feature_gather", "heta_check_ids", "heta_rel_aggregate_fwd", "heta_rel_aggregate_bwd",
@@ -1028,9 +1029,9 @@ def heta_linear_pack_e4m3(W: torch.Tensor, packed: torch.Tensor, scale: torch.Te
 
 
 def heta_muon_multi(g: Graph, items: Sequence[Sequence], lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
-                    weight_decay: float = 0.0, eps: float = 1e-7, steps: int = 5, stream=None) -> None:
+                    weight_decay: float = 0.0, eps: float = 1e-7, steps: int = 5, stream=None, coarse: bool = False) -> None:
     """One step of orthogonalised momentum on several weight matrices: items[i] = (W, m, grad), all [rows, cols]; W fp32 or bf16,
-    m fp32, grad fp32 or bf16; W and m are updated in place."""
+    m fp32, grad fp32 or bf16; W and m are updated in place.  coarse: 16 bits between the steps' products for fp32 weights too."""
     arr = []
     for W, m, grad in items:
         rows, cols = W.shape
@@ -1038,7 +1039,7 @@ def heta_muon_multi(g: Graph, items: Sequence[Sequence], lr: float = 0.02, momen
         pm, lm = _rows_of(m, "m", torch.float32, rows, cols)
         pg, lg = _rows_of(grad, "grad", grad.dtype, rows, cols)
         arr.append(_MUON_PACK.pack(pw, lw, pm, lm, pg, lg, rows, cols, _dt8(W), _dt8(grad)))
-    _check(load_library().heta_muon_multi(g.handle, len(arr), b"".join(arr), lr, momentum, int(bool(nesterov)), weight_decay, eps, int(steps), _stream(stream)))
+    _check(load_library().heta_muon_multi(g.handle, len(arr), b"".join(arr), lr, momentum, int(bool(nesterov)) | (HETA_MUON_COARSE if coarse else 0), weight_decay, eps, int(steps), _stream(stream)))
 
 
 def _scores(t: torch.Tensor, name: str, rows: int, heads: int) -> int:

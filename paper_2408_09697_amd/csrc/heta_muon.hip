@@ -7,8 +7,8 @@
 // The matrices [rows, cols] are those of a product in . W.  X lies with its shorter side k as rows (a tall matrix is
 // transposed on its way in and out, by the element-wise kernels), so a step is three products for every item: k x k Gram
 // matrix, k x k polynomial, k x l update.  They are the tile kernel of heta_tiles.h on the bf16 matrix pipe with every
-// matrix held as two bf16 terms (kTerms); the epilogue that makes a matrix writes it as terms, so that the next product loads
-// them straight into LDS.  Gram matrix and polynomial are symmetric: only the tiles on and above the diagonal are formed.
+// matrix held as bf16 terms, three for fp32 weights and two for bf16 ones; the epilogue that makes a matrix writes it as terms, so that
+// the next product loads them straight into LDS.  Gram matrix and polynomial are symmetric: only the tiles on and above the diagonal are formed.
 // |u| is summed per part of 32 x 64, then over the parts in a fixed order by every workgroup that needs it.
 #include <algorithm>
 #include <cmath>
@@ -19,9 +19,10 @@
 namespace heta {
 
 constexpr int kMuonItems = 12; // per launch
-// bf16 terms of a matrix.  Two hold 16 bits; the update then misses the one of exact products by 2.5e-5 of its norm (three: 2.3e-7,
-// at twice the products; one: 1.3e-2).  The polynomial itself leaves singular values 20 to 30 % away from 1.
-constexpr int kTerms = 2;
+// T, bf16 terms of a matrix.  Three hold fp32 (the update misses the one of exact products by 2.3e-7 of its norm), two 16 bits (2.5e-5) at half
+// the products: enough for weights that are rounded to 8 bits behind the update, 2^-9 of their own, and for a caller who asks for it.
+// One: 1.3e-2.
+static int muon_terms(int dt, int flags) { return dt == HETA_F32 && !(flags & HETA_MUON_COARSE) ? 3 : 2; }
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 
 struct MuonItem {
@@ -88,10 +89,10 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonArgs p)
     if (threadIdx.x == 0) it.part[b] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-__device__ __forceinline__ void store_terms(bf16_t *p, int64_t plane, float v)
+template <int T> __device__ __forceinline__ void store_terms(bf16_t *p, int64_t plane, float v)
 {
 #pragma unroll
-    for (int t = 0; t < kTerms; ++t) {
+    for (int t = 0; t < T; ++t) {
         const bf16_t h = to_bf16(v);
         p[t * plane] = h;
         v -= widen(h);
@@ -100,7 +101,7 @@ __device__ __forceinline__ void store_terms(bf16_t *p, int64_t plane, float v)
 
 // X_0 as terms; a tall matrix goes through LDS so that both its reads and its writes are along
 // rows.  The sums of squares come in while the part does.
-__global__ void __launch_bounds__(256) muon_start_kernel(MuonArgs p)
+template <int T> __global__ void __launch_bounds__(256) muon_start_kernel(MuonArgs p)
 {
     __shared__ float tile[32][65];
     __shared__ float sums[4];
@@ -129,18 +130,18 @@ __global__ void __launch_bounds__(256) muon_start_kernel(MuonArgs p)
     for (int i = 0; i < 8; ++i) {
         const int64_t r = r0 + 4 * i + ly, c = c0 + lx;
         if (it.tall) tile[4 * i + ly][lx] = x[i] * inv;
-        else if (r < it.rows && c < it.cols) store_terms(it.x + r * it.ld_x + c, it.plane, x[i] * inv);
+        else if (r < it.rows && c < it.cols) store_terms<T>(it.x + r * it.ld_x + c, it.plane, x[i] * inv);
     }
     if (!it.tall) return; // uniform
     __syncthreads();
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (c0 + 8 * i + ty < it.cols && r0 + tx < it.rows) store_terms(it.x + (c0 + 8 * i + ty) * it.ld_x + r0 + tx, it.plane, tile[tx][8 * i + ty]);
+        if (c0 + 8 * i + ty < it.cols && r0 + tx < it.rows) store_terms<T>(it.x + (c0 + 8 * i + ty) * it.ld_x + r0 + tx, it.plane, tile[tx][8 * i + ty]);
 }
 
 // W <- keep W - step X
-__global__ void __launch_bounds__(256) muon_update_kernel(MuonArgs p)
+template <int T> __global__ void __launch_bounds__(256) muon_update_kernel(MuonArgs p)
 {
     __shared__ float tile[32][65];
     const MuonItem &it = p.item[muon_item(p)];
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(256) muon_update_kernel(MuonArgs p)
     auto value = [&](int64_t at) {
         float v = widen(it.x[at]);
 #pragma unroll
-        for (int t = 1; t < kTerms; ++t) v += widen(it.x[at + t * it.plane]);
+        for (int t = 1; t < T; ++t) v += widen(it.x[at + t * it.plane]);
         return v;
     };
     float w[8], x[8];
@@ -188,7 +189,7 @@ struct TermsExtra {
     int64_t ld_old, old_plane, ld_out, out_plane; // elements
     float alpha, beta;
 };
-struct TermsEpi {
+template <int T> struct TermsEpi {
     static constexpr int kItems = kMuonItems;
     static constexpr bool kBlocks = true;
     using Extra = TermsExtra;
@@ -196,7 +197,7 @@ struct TermsEpi {
     __device__ __forceinline__ static void put(const Extra &x, int64_t r, int64_t c, int valid, float (&y)[8])
     {
 #pragma unroll
-        for (int t = 0; t < kTerms; ++t) {
+        for (int t = 0; t < T; ++t) {
             uint32_t w[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -231,7 +232,7 @@ struct TermsEpi {
             if (x.old && m < it.M && valid > 0) {
                 float o[8], s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int t = kTerms - 1; t >= 0; --t) { // smallest first
+                for (int t = T - 1; t >= 0; --t) { // smallest first
                     load8(x.old + t * x.old_plane + m * x.ld_old + n, valid, o);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[e] += o[e];
@@ -263,20 +264,28 @@ struct TermsEpi {
 };
 
 // ---- host side ---------------------------------------------------------------------------------------
-template <bool B_RC> using NsDeep = TileShape<bf16_t, 2, kTerms, false, B_RC, kDirect, 2, 2, 1, 1, 64, 4, 1>;   // 64 x 64, one per CU
-template <bool B_RC> using NsSmall = TileShape<bf16_t, 2, kTerms, false, B_RC, kDirect, 2, 2, 1, 1, 64, 2, 1>;  // 64 x 64, two per CU
-template <bool B_RC> using NsLarge = TileShape<bf16_t, 2, kTerms, false, B_RC, kDirect, 2, 4, 2, 1, 64, 2, 1>;  // 128 x 128
-
+// Tiles by how much LDS the terms' stages take.
+template <int T, bool B_RC> struct Ns;
+template <bool B_RC> struct Ns<2, B_RC> {
+    using Deep = TileShape<bf16_t, 2, 2, false, B_RC, kDirect, 2, 2, 1, 1, 64, 4, 1>;  // 64 x 64, one per CU
+    using Small = TileShape<bf16_t, 2, 2, false, B_RC, kDirect, 2, 2, 1, 1, 64, 2, 1>; // 64 x 64, two per CU
+    using Large = TileShape<bf16_t, 2, 2, false, B_RC, kDirect, 2, 4, 2, 1, 64, 2, 1>; // 128 x 128
+};
+template <bool B_RC> struct Ns<3, B_RC> {
+    using Deep = TileShape<bf16_t, 2, 3, false, B_RC, kDirect, 2, 2, 1, 1, 64, 3, 1>;
+    using Small = TileShape<bf16_t, 2, 3, false, B_RC, kDirect, 2, 2, 1, 1, 32, 2, 1>;
+    using Large = TileShape<bf16_t, 2, 3, false, B_RC, kDirect, 2, 4, 2, 1, 32, 2, 1>;
+};
 constexpr int64_t kTileRows = 128; // of an operand of any of them, at most
-static_assert(NsLarge<false>::BM <= kTileRows && NsLarge<false>::BN <= kTileRows, "the size check of heta_muon_multi counts rows of a tile");
+static_assert(Ns<2, false>::Large::BM <= kTileRows && Ns<3, false>::Large::BM <= kTileRows, "the size check of heta_muon_multi counts rows of a tile");
 
-template <bool B_RC> static heta_status launch_terms(const char *who, TileArgs<TermsEpi> &p, hipStream_t st)
+template <int T, bool B_RC> static heta_status launch_terms(const char *who, TileArgs<TermsEpi<T>> &p, hipStream_t st)
 {
     double bytes = 0, flops = 0;
     int64_t large = 0, small = 0;
     for (int i = 0; i < p.n_items; ++i) {
         const TileItem &it = p.item[i];
-        bytes += 2.0 * kTerms * (static_cast<double>(it.M) * it.K + static_cast<double>(it.K) * it.N + static_cast<double>(it.M) * it.N);
+        bytes += 2.0 * T * (static_cast<double>(it.M) * it.K + static_cast<double>(it.K) * it.N + static_cast<double>(it.M) * it.N);
         flops += (it.symmetric ? 1.0 : 2.0) * it.M * it.N * it.K;
         auto tiles = [&](int64_t b) {
             const int64_t mt = (it.M + b - 1) / b, nt = (it.N + b - 1) / b;
@@ -286,11 +295,11 @@ template <bool B_RC> static heta_status launch_terms(const char *who, TileArgs<T
         small += tiles(64);
     }
     // Large tiles once they occupy a good third of the chip.  Below, 64 x 64: with a workgroup per CU at most, the ring takes the CU's
-    // whole LDS and the first 256 k-values are on their way at once (7 matrices of 128 x 256: 138 -> 121 us); with more of
-    // them, two share a CU (2 matrices of 1,024 x 4,096: 709 us, 871 with the deep ring).
-    if (large >= 96) return launch_tiles<NsLarge<B_RC>>(who, "muon_product_kernel", p, bytes, flops, st);
-    if (small <= 256) return launch_tiles<NsDeep<B_RC>>(who, "muon_product_kernel", p, bytes, flops, st);
-    return launch_tiles<NsSmall<B_RC>>(who, "muon_product_kernel", p, bytes, flops, st);
+    // whole LDS and the first 256 k-values are on their way at once (7 matrices of 128 x 256, two terms: 138 -> 121 us); with more of
+    // them, two share a CU (2 matrices of 1,024 x 4,096, two terms: 709 us, 871 with the deep ring).
+    if (large >= 96) return launch_tiles<typename Ns<T, B_RC>::Large>(who, "muon_product_kernel", p, bytes, flops, st);
+    if (small <= 256) return launch_tiles<typename Ns<T, B_RC>::Deep>(who, "muon_product_kernel", p, bytes, flops, st);
+    return launch_tiles<typename Ns<T, B_RC>::Small>(who, "muon_product_kernel", p, bytes, flops, st);
 }
 
 static int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -298,7 +307,7 @@ struct MuonPlan { // places in the workspace, in bytes, of one item
     int64_t k, l, parts;
     int64_t ld_x, ld_g, x_plane, g_plane; // elements
     int64_t x[2], gram, poly, part, end;
-    MuonPlan(int32_t rows, int32_t cols, int64_t at)
+    MuonPlan(int32_t rows, int32_t cols, int terms, int64_t at)
         : k(std::min(rows, cols)), l(std::max(rows, cols)), parts((int64_t(rows) + 31) / 32 * ((int64_t(cols) + 63) / 64)), ld_x(pad8(l)), ld_g(pad8(k)), x_plane(k * ld_x), g_plane(k * ld_g)
     {
         auto take = [&](int64_t bytes) {
@@ -306,34 +315,36 @@ struct MuonPlan { // places in the workspace, in bytes, of one item
             at += (bytes + 255) / 256 * 256;
             return p;
         };
-        x[0] = take(x_plane * kTerms * 2);
-        x[1] = take(x_plane * kTerms * 2);
-        gram = take(g_plane * kTerms * 2);
-        poly = take(g_plane * kTerms * 2);
+        x[0] = take(x_plane * terms * 2);
+        x[1] = take(x_plane * terms * 2);
+        gram = take(g_plane * terms * 2);
+        poly = take(g_plane * terms * 2);
         part = take(parts * 4);
         end = at;
     }
 };
 
-// Items that share their launches, as many as fit: kMuonItems, and the parts of a grid.
+// Items that share their launches: those of a list with as many terms, as many as fit kMuonItems and the parts of a grid.
 struct MuonGroup {
+    std::vector<const heta_muon_item *> items;
     std::vector<MuonPlan> plan;
     int64_t bytes = 0, parts = 0; // of workspace, and workgroups of the element-wise kernels
-    MuonGroup(const heta_muon_item *items, int32_t left)
+    int terms;
+    bool add(const heta_muon_item &q)
     {
-        for (int32_t i = 0; i < left && i < kMuonItems; ++i) {
-            const MuonPlan p(items[i].rows, items[i].cols, bytes);
-            if (parts + p.parts > max_blocks(256)) break; // never the first: heta_muon_multi bounds an item's
-            plan.push_back(p);
-            bytes = p.end;
-            parts += p.parts;
-        }
+        const MuonPlan p(q.rows, q.cols, terms, bytes);
+        if (static_cast<int>(items.size()) == kMuonItems || parts + p.parts > max_blocks(256)) return false; // never the first: an item's parts are bounded
+        items.push_back(&q);
+        plan.push_back(p);
+        bytes = p.end;
+        parts += p.parts;
+        return true;
     }
 };
 
 // Launches alone: what it needs has been checked, and the workspace is there.
-static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_item *items, const MuonGroup &group, float lr, float mu, int nesterov, float wd, float eps, int steps,
-                              hipStream_t st)
+template <int T>
+static heta_status muon_group(const char *who, heta_graph *g, const MuonGroup &group, float lr, float mu, int nesterov, float wd, float eps, int steps, hipStream_t st)
 {
     const std::vector<MuonPlan> &plan = group.plan;
     const int n = static_cast<int>(plan.size());
@@ -348,7 +359,7 @@ static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_it
     int64_t blocks = 0;
     double elems = 0, esz = 0;
     for (int i = 0; i < n; ++i) {
-        const heta_muon_item &q = items[i];
+        const heta_muon_item &q = *group.items[i];
         const MuonPlan &pl = plan[i];
         a.item[i] = MuonItem{q.W, q.m, q.grad, q.ld_w, q.ld_m, q.ld_grad, q.rows, q.cols, q.rows > q.cols, q.grad_dt == HETA_BF16, q.dt == HETA_BF16, reinterpret_cast<bf16_t *>(ws + pl.x[0]), pl.ld_x,
                              pl.x_plane, reinterpret_cast<float *>(ws + pl.part), static_cast<uint32_t>(blocks), static_cast<uint32_t>(pl.parts)};
@@ -363,12 +374,12 @@ static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_it
         HETA_LAUNCH_CHECK("muon_momentum_kernel");
     }
     {
-        ProfScope prof("muon_start_kernel", st, elems * (4 + esz + 2 * kTerms), 0);
-        hipLaunchKernelGGL(muon_start_kernel, grid, dim3(256), 0, st, a);
+        ProfScope prof("muon_start_kernel", st, elems * (4 + esz + 2 * T), 0);
+        hipLaunchKernelGGL(muon_start_kernel<T>, grid, dim3(256), 0, st, a);
         HETA_LAUNCH_CHECK("muon_start_kernel");
     }
     for (int s = 0; s < steps; ++s) {
-        TileArgs<TermsEpi> gram{}, poly{}, apply{};
+        TileArgs<TermsEpi<T>> gram{}, poly{}, apply{};
         gram.n_items = poly.n_items = apply.n_items = n;
         for (int i = 0; i < n; ++i) {
             const MuonPlan &pl = plan[i];
@@ -381,13 +392,13 @@ static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_it
             poly.extra[i] = {terms(A), terms(P), pl.ld_g, pl.g_plane, pl.ld_g, pl.g_plane, kNsC, kNsB};
             apply.extra[i] = {terms(x), terms(y), pl.ld_x, pl.x_plane, pl.ld_x, pl.x_plane, 1.f, kNsA};
         }
-        HETA_TRY((launch_terms<false>(who, gram, st)));
-        HETA_TRY((launch_terms<false>(who, poly, st)));
-        HETA_TRY((launch_terms<true>(who, apply, st)));
+        HETA_TRY((launch_terms<T, false>(who, gram, st)));
+        HETA_TRY((launch_terms<T, false>(who, poly, st)));
+        HETA_TRY((launch_terms<T, true>(who, apply, st)));
     }
     for (int i = 0; i < n; ++i) a.item[i].x = reinterpret_cast<bf16_t *>(ws + plan[i].x[steps & 1]);
-    ProfScope prof("muon_update_kernel", st, elems * (2 * kTerms + 2 * esz), 0);
-    hipLaunchKernelGGL(muon_update_kernel, grid, dim3(256), 0, st, a);
+    ProfScope prof("muon_update_kernel", st, elems * (2 * T + 2 * esz), 0);
+    hipLaunchKernelGGL(muon_update_kernel<T>, grid, dim3(256), 0, st, a);
     HETA_LAUNCH_CHECK("muon_update_kernel");
     return HETA_OK;
 }
@@ -396,13 +407,14 @@ static heta_status muon_group(const char *who, heta_graph *g, const heta_muon_it
 
 using namespace heta;
 
-static heta_status muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t nesterov, float weight_decay, float eps, int32_t steps,
+static heta_status muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t flags, float weight_decay, float eps, int32_t steps,
                               void *hip_stream)
 {
     const char *who = "heta_muon_multi";
     if (!g || n_items < 0 || (n_items > 0 && !items)) return fail(HETA_ERR_INVALID_ARG, "%s: bad handle or item list", who);
     if (!(momentum >= 0.f && momentum < 1.f) || !(eps > 0.f) || steps < 0 || steps > 64 || !(weight_decay >= 0.f) || !std::isfinite(lr))
         return fail(HETA_ERR_INVALID_ARG, "%s: need 0 <= momentum < 1, eps > 0, weight_decay >= 0, 0 <= steps <= 64 and a finite lr", who);
+    if (flags & ~(HETA_MUON_NESTEROV | HETA_MUON_COARSE)) return fail(HETA_ERR_INVALID_ARG, "%s: unknown flags", who);
     std::vector<ItemRange> outs, ins;
     for (int32_t i = 0; i < n_items; ++i) {
         const heta_muon_item &q = items[i];
@@ -427,25 +439,34 @@ static heta_status muon_multi(heta_graph *g, int32_t n_items, const heta_muon_it
     // every group's workspace before the first group's launches: a call that fails has updated nothing
     std::vector<MuonGroup> groups;
     int64_t need = 0;
-    for (int32_t i = 0; i < n_items; i += static_cast<int32_t>(groups.back().plan.size())) {
-        groups.emplace_back(items + i, n_items - i);
-        need = std::max(need, groups.back().bytes);
+    for (const int terms : {3, 2}) {
+        bool open = false;
+        for (int32_t i = 0; i < n_items; ++i) {
+            if (muon_terms(items[i].dt, flags) != terms) continue;
+            if (!open || !groups.back().add(items[i])) {
+                groups.emplace_back();
+                groups.back().terms = terms;
+                groups.back().add(items[i]);
+                open = true;
+            }
+        }
     }
-    if (n_items > 0) HETA_TRY(ensure_workspace(g, static_cast<size_t>(need)));
+    for (const MuonGroup &group : groups) need = std::max(need, group.bytes);
+    if (need > 0) HETA_TRY(ensure_workspace(g, static_cast<size_t>(need)));
     hipStream_t st = as_stream(hip_stream);
     for (const MuonGroup &group : groups) {
-        HETA_TRY(muon_group(who, g, items, group, lr, momentum, nesterov != 0, weight_decay, eps, steps, st));
-        items += group.plan.size();
+        const auto run = group.terms == 3 ? muon_group<3> : muon_group<2>;
+        HETA_TRY(run(who, g, group, lr, momentum, flags & HETA_MUON_NESTEROV, weight_decay, eps, steps, st));
     }
     return HETA_OK;
 }
 
 // No exception crosses the boundary: host containers may throw std::bad_alloc.
-extern "C" heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t nesterov, float weight_decay, float eps,
+extern "C" heta_status heta_muon_multi(heta_graph *g, int32_t n_items, const heta_muon_item *items, float lr, float momentum, int32_t flags, float weight_decay, float eps,
                                        int32_t steps, void *hip_stream)
 {
     try {
-        return muon_multi(g, n_items, items, lr, momentum, nesterov, weight_decay, eps, steps, hip_stream);
+        return muon_multi(g, n_items, items, lr, momentum, flags, weight_decay, eps, steps, hip_stream);
     } catch (const std::bad_alloc &) {
         return fail(HETA_ERR_OOM, "heta_muon_multi: host allocation failed");
     }

@@ -197,3 +197,55 @@ def test_fp32_products_of_infinities_and_of_the_largest_numbers(handle, n, d_in,
     a, c = x.cpu().double(), torch.where(c.abs() > 1e30, torch.ones_like(c), c) / 4
     heta.heta_linear_bwd(handle, x, None, c.float().cuda(), grad_W=gw)
     same_with_infinities(gw.cpu(), a.t() @ c, (2 * n + 600) * U * (fin(a).t() @ fin(c)), "grad_W")
+
+
+@pytest.mark.parametrize("r,c", [(16, 16), (16, 48), (60, 16), (130, 16)])
+@pytest.mark.parametrize("grad_dtype", [F32, BF16])
+def test_momentum_of_fp32_weights_keeps_fp32(handle, r, c, grad_dtype):
+    """Update of zero weights: -X scale.  Without steps X is u over its norm: a sum of r c squares whose terms add up in chains of at most 48, root, quotient and product, 48 u of
+    every element in all.  One step on a matrix whose singular values are all 1 / 4 rounds X, its Gram matrix and the polynomial and forms three products over 16
+    terms or the long side's, each off by a few u of the result in root mean square and multiplied by at most p(s) / s = 3.2 behind: 24 u of the norm.  (16 bits would be off by
+    2^-17 = 128 u of the largest elements and 2^-18 = 64 u in root mean square at every rounding.)"""
+    g = randn(1, r, c).to(grad_dtype)
+    W, m = torch.zeros(r, c, device="cuda"), torch.zeros(r, c, device="cuda")
+    scale = math.sqrt(max(1.0, c / r))
+    heta.heta_muon_multi(handle, [(W, m, g)], lr=1.0, momentum=0.0, nesterov=False, steps=0)
+    want = -scale * g.double() / (g.double().norm() + 1e-7)
+    assert ((W.double() - want).abs() <= 48 * U * want.abs()).all()
+    k = min(r, c)
+    q = torch.linalg.qr(randn(2, max(r, c), k).double())[0]
+    g = (q if r > c else q.t()).contiguous().float()
+    W, m = torch.zeros(r, c, device="cuda"), torch.zeros(r, c, device="cuda")
+    heta.heta_muon_multi(handle, [(W, m, g)], lr=1.0, momentum=0.0, nesterov=False, steps=1)
+    x = g.double() / (g.double().norm() + 1e-7)
+    x = x.t() if r > c else x
+    a = x @ x.t()
+    x = 3.4445 * x + (-4.7750 * a + 2.0315 * a @ a) @ x
+    want = -scale * (x.t() if r > c else x)
+    assert float((W.double() - want).norm()) <= 24 * U * float(want.norm())
+
+
+def test_momentum_of_mixed_types_is_that_of_calls_of_their_own(handle):
+    """Bits do not depend on what else is in the list, in whatever order."""
+    shapes = [(64, 200, F32), (200, 64, BF16), (40, 40, BF16), (300, 128, F32), (16, 16, F32), (128, 128, BF16)] * 3
+    make = lambda: [(randn(i, r, c, scale=0.1).to(t), randn(50 + i, r, c, scale=0.01), randn(90 + i, r, c)) for i, (r, c, t) in enumerate(shapes)]  # noqa: E731
+    together, apart = make(), make()
+    heta.heta_muon_multi(handle, together)
+    for t in (F32, BF16):
+        mine = [it for it in apart if it[0].dtype is t]
+        for i in range(0, len(mine), 12):
+            heta.heta_muon_multi(handle, mine[i:i + 12])
+    for a, b in zip(together, apart):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_momentum_in_16_bits_on_request(handle):
+    """The same for bf16 weights; fp32 ones then differ by what the header says, 2.5e-5 of the update's norm, here with four times as much room."""
+    make = lambda t: [(randn(1, 100, 300, scale=0.1).to(t), randn(2, 100, 300, scale=0.01), randn(3, 100, 300))]  # noqa: E731
+    for t in (F32, BF16):
+        a, b, c = make(t), make(t), make(t)
+        heta.heta_muon_multi(handle, a, lr=1.0)
+        heta.heta_muon_multi(handle, b, lr=1.0, coarse=True)
+        off, size = float((a[0][0].double() - b[0][0].double()).norm()), float((a[0][0].double() - c[0][0].double()).norm())
+        assert off == 0.0 if t is BF16 else 0.0 < off <= 1e-4 * size
+        assert torch.equal(a[0][1], b[0][1])

@@ -119,3 +119,8 @@ LINEAR8 = dict(LINEAR, in_dt=E4M3, w_dt=E4M3, ld_w=64, in_scale=AT["g"], w_scale
     (LINEAR8, {"w_scale": AT["f"] + 4}), (LINEAR8, {"w_scale": AT["e"]}), (LINEAR8, {"bias": AT["f"]})])
 def test_linear_vectors_that_overlap(lib, handle, base, change):
     refused(lib, lib.heta_linear(handle, ctypes.byref(hb._LinearArgs(**{**base, **change})), None), BAD, "overlaps")
+
+
+@pytest.mark.parametrize("flags", [4, 7, -1])
+def test_momentum_flags(lib, handle, flags):
+    refused(lib, lib.heta_muon_multi(handle, 1, ctypes.byref(muon_item(64, 48)), 0.02, 0.9, flags, 0.0, 1e-7, 5, None), BAD, "flags")
