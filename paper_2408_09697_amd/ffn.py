@@ -75,9 +75,9 @@ class FeedForwardBlock:
         return packed, scale
 
     def infer(self, x: torch.Tensor, agg: Optional[torch.Tensor] = None, packed: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
-              coarse_sums: bool = True) -> torch.Tensor:
+              coarse_sums: bool = False) -> torch.Tensor:
         """The output alone.  With `packed` (what `pack` gave; bf16 embeddings) the norm writes its rows in 8 bits and the first product
-        reads them and the weights that way."""
+        reads them and the weights that way; with `coarse_sums` the 8-bit matrix instruction adds, at up to twice the rate (heta_linear)."""
         n, d = x.shape
         dev, t, d_hidden = x.device, x.dtype, self.W1.shape[1]
         h = x if agg is None else torch.empty_like(x)

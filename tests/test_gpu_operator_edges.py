@@ -249,3 +249,11 @@ def test_momentum_in_16_bits_on_request(handle):
         off, size = float((a[0][0].double() - b[0][0].double()).norm()), float((a[0][0].double() - c[0][0].double()).norm())
         assert off == 0.0 if t is BF16 else 0.0 < off <= 1e-4 * size
         assert torch.equal(a[0][1], b[0][1])
+
+
+def test_8_bit_inference_adds_exactly_unless_asked(handle):
+    block = heta.FeedForwardBlock(handle, randn(1, 256, 1024, scale=1 / 16).to(BF16), randn(2, 1024, 256, scale=1 / 32).to(BF16))
+    x, packed = randn(3, 2000, 256).to(BF16), block.pack()
+    exact, coarse = block.infer(x, packed=packed, coarse_sums=False), block.infer(x, packed=packed, coarse_sums=True)
+    assert not torch.equal(exact, coarse)
+    assert torch.equal(block.infer(x, packed=packed), exact)
