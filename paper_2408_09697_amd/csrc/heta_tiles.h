@@ -290,7 +290,7 @@ struct TileItem { // M, N, K > 0
     int32_t n_split;           // every split has k-values
     int32_t mt, nt;            // tiles
     int32_t symmetric;         // C is: the tiles below the diagonal are not formed (several items, one tile size along both sides)
-    uint32_t block0, places;   // one item: places of its tiles; several: the tiles before it, its tiles
+    uint32_t block0, places;   // one item: its tiles, places of them (a multiple of 8); several: the tiles before it, its tiles
 };
 
 // An output tile and the part of the contraction that goes into it.
@@ -307,15 +307,17 @@ struct TilePlace {
         kn = static_cast<int>(min(it.K - k0, it.k_per_split));
     }
     // One item: the first place from `at` on, `stride` apart, that has a tile.  Place -> (XCD, position in its queue) -> tile:
-    // workgroups go round-robin to the 8 XCDs, and the tiles that share operand rows (the column tiles of a row block, all
-    // tiles of a split) follow one another on one of them.
+    // workgroups go round-robin to the 8 XCDs, each of which takes an eighth of the tiles, consecutive ones: those that share operand rows (the
+    // column tiles of a row block, all tiles of a split) follow one another, and no XCD has more than one tile above the others, however
+    // few row blocks or splits there are.
     __device__ __forceinline__ bool seek(const TileItem &it, uint32_t stride, int bm, int bn)
     {
         const bool splits = it.n_split > 1;
-        const uint32_t inner = splits ? static_cast<uint32_t>(it.nt) * it.mt : static_cast<uint32_t>(it.nt), n_outer = static_cast<uint32_t>(splits ? it.n_split : it.mt);
+        const uint32_t inner = splits ? static_cast<uint32_t>(it.nt) * it.mt : static_cast<uint32_t>(it.nt), each = it.places / 8;
         for (; at < it.places; at += stride) {
-            const uint32_t j = at / 8, in = j % inner, outer = j / inner * 8 + at % 8;
-            if (outer >= n_outer) continue;
+            const uint32_t tile = at % 8 * each + at / 8;
+            if (tile >= it.block0) continue;
+            const uint32_t outer = tile / inner, in = tile - outer * inner;
             if (splits) set(it, in / it.nt, in % it.nt, static_cast<int>(outer), bm, bn);
             else set(it, outer, in, 0, bm, bn);
             return true;
@@ -697,9 +699,9 @@ template <typename C, typename Epi> inline bool plan_tiles(TileArgs<Epi> &p, uin
         if (outer > (int64_t(1) << 31) / inner - 8) return false;
         it.mt = static_cast<int32_t>(mt);
         it.nt = static_cast<int32_t>(nt);
-        it.block0 = static_cast<uint32_t>(at);
+        it.block0 = static_cast<uint32_t>(Epi::kItems > 1 ? at : outer * inner);
         if (Epi::kItems > 1) it.places = static_cast<uint32_t>(it.symmetric ? mt * (mt + 1) / 2 : mt * nt);
-        else it.places = static_cast<uint32_t>((outer + 7) / 8 * 8 * inner);
+        else it.places = static_cast<uint32_t>((outer * inner + 7) / 8 * 8);
         at += it.places;
         if (Epi::kItems > 1 && (it.n_split > 1 || (it.symmetric && C::BM != C::BN) || at > max_blocks(C::NT) - 8)) return false;
     }

@@ -257,3 +257,15 @@ def test_8_bit_inference_adds_exactly_unless_asked(handle):
     exact, coarse = block.infer(x, packed=packed, coarse_sums=False), block.infer(x, packed=packed, coarse_sums=True)
     assert not torch.equal(exact, coarse)
     assert torch.equal(block.infer(x, packed=packed), exact)
+
+
+@pytest.mark.parametrize("n,d_in,d_out", [(300, 1024, 4096), (2304, 256, 1000), (3000, 1024, 4096), (2400, 1792, 1024), (5000, 2048, 4096), (64, 300, 1100)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_few_row_blocks_and_splits(handle, n, d_in, d_out, dtype):
+    """Counts of row blocks and of splits that eight does not divide: every tile is formed, by exact sums."""
+    x, W, go = integers(1, n, d_in, dtype), integers(2, d_in, d_out, dtype), integers(3, n, d_out, dtype)
+    out, gi, gw, gb = torch.empty(n, d_out, device="cuda"), torch.empty(n, d_in, device="cuda", dtype=dtype), torch.empty(d_in, d_out, device="cuda"), torch.empty(d_out, device="cuda")
+    heta.heta_linear(handle, x, W, out)
+    assert torch.equal(out, x.float() @ W.float())
+    heta.heta_linear_bwd(handle, x, W, go, grad_in=gi, grad_W=gw, grad_bias=gb)
+    assert torch.equal(gi, (go.float() @ W.float().t()).to(dtype)) and torch.equal(gw, x.float().t() @ go.float()) and torch.equal(gb, go.float().sum(0))
