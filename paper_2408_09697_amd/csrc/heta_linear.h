@@ -78,9 +78,6 @@ constexpr int kAnyAct = -1;
 template <typename O, bool SCALED, int ACT = kAnyAct, int SLOPE = kAnyAct, bool READS = true, bool WHOLE = false> struct LinearEpi {
     static constexpr int kItems = 1;
     static constexpr bool kBlocks = false, kReads = READS, kPre = SLOPE <= 0, kWhole = WHOLE;
-    // large tiles of 8-bit operands store with the streaming hint: their weights then stay in the L2s (200,000 x 1,024 x 4,096:
-    // 1,294 -> 1,103 us; products of bf16 operands are as fast without)
-    static constexpr bool kStream = SCALED && ACT != kAnyAct;
     using Out = O;
     using Extra = LinearExtra;
     static constexpr int W = 16 / (int)sizeof(O);
@@ -134,7 +131,7 @@ template <typename O, bool SCALED, int ACT = kAnyAct, int SLOPE = kAnyAct, bool 
 // partial products of a contraction that is split over its rows: [split][M][N] fp32
 struct PartialEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kBlocks = false, kReads = false, kPre = false, kStream = false, kWhole = false;
+    static constexpr bool kBlocks = false, kReads = false, kPre = false, kWhole = false;
     using Out = float;
     struct Extra {
         float *part;

@@ -3,7 +3,7 @@
 
 namespace heta {
 
-// 256 x 256.  64 x 128 per wavefront took 1,294 us where 128 x 64 took 1,354 (200,000 x 1,024 x 4,096), but leaves no registers for
+// 256 x 256.  64 x 128 per wavefront took 1,286 us where 128 x 64 took 1,331 (200,000 x 1,024 x 4,096), but leaves no registers for
 // an epilogue that reads, or for a longer one of fp32 outputs.
 template <bool WIDEN> using Wide = TileShape<uint8_t, 1, 1, false, false, kDirect, 4, 2, 2, 4, 128, 2, 1, WIDEN>;
 template <bool WIDEN> using Tall = TileShape<uint8_t, 1, 1, false, false, kDirect, 2, 4, 4, 2, 128, 2, 1, WIDEN>;

@@ -430,9 +430,9 @@ template <typename F, typename W> static void by_width(int32_t d, F f, W wide)
     else if (d <= 2048) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
     else wide();
 }
-// Workgroups at most, each walking over rows.  1.1 M rows of 256 bf16 columns to 8 bits, with 2,048 / 4,096 / 16,384 workgroups and one per 8
-// rows: 483 / 427 / 391 / 590 us, and 366 with 16,384 and the streaming hint; to bf16 434 / 450 / 469 / 542 and 402.  Backward of
-// 700,000 rows with 1,024 / 2,048 / 4,096 / 8,192: 290 / 320 / 284 / 301 us, and 259 with 4,096 and the hint.
+// Workgroups at most, each walking over rows (us on three sets of inputs in turn).  1.1 M rows of 256 bf16 columns with 2,048 / 4,096 / 16,384 workgroups and
+// one per 8 rows: to 8 bits 380 / 376 / 378 / 537, to bf16 409 / 405 / 402 / 537; without the streaming hint 381 and 440 with 16,384.  Backward of 700,000 rows with 1,024 /
+// 2,048 / 4,096 / 8,192: 275 / 295 / 259 / 276, 285 without the hint; of 100,000 fp32 rows of 789 238 / 240 / 246 / 263, and 264.
 constexpr int64_t kNormBlocks = 16384, kNormBwdBlocks = 4096;
 static unsigned row_blocks(int64_t n_rows, int groups, int64_t most) { return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n_rows + groups - 1) / groups, most))); }
 

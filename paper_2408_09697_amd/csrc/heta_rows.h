@@ -95,11 +95,11 @@ template <typename O> __device__ __forceinline__ void unpack16(uintx4 w, float (
         }
     }
 }
-template <typename O, bool STREAM = false> __device__ __forceinline__ void store_piece(O *p, int valid, uintx4 w)
+template <typename O> __device__ __forceinline__ void store_piece(O *p, int valid, uintx4 w)
 {
     constexpr int W = 16 / (int)sizeof(O);
     if (valid >= W) {
-        store16<STREAM>(p, w);
+        store16(p, w);
         return;
     }
 #pragma unroll

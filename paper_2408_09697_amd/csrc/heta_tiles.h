@@ -16,6 +16,8 @@
 // bytes of consecutive outputs, and memory sees 64 or 128 bytes of a row at a time, also for what the epilogue reads in the
 // output's shape.  Stored from the registers as they lie, 32 bytes of 32 rows, products of 700,000 x 1,024 x 256 and 700,000 x 256 x 1,024
 // took 477 and 622 us, with the columns in the outer loop 593 and 738, against 435 and 564 through strips.
+// Outputs carry no streaming hint: with it 8-bit products of 200,000 x 1,024 x 4,096 and 700,000 x 256 x 1,024 took 1,347 and 808 us for 1,290 and
+// 702, and where the output stays in the cache (20,000 x 1,024 x 4,096: 117 for 137 us) the product that reads it next loses more (351 for 335 us, both).
 #pragma once
 
 #include <algorithm>
@@ -342,7 +344,7 @@ struct TilePlace {
 //   kBlocks = true: block(x, it, strip, m, n, off_diagonal, lane) takes 32 x 32 sums at row m, column n from the strip (strip_at)
 //   kBlocks = false: with W = 16 bytes of columns of Out, first(cols, row, y) makes pre-activations of W sums and second(x, y, t)
 //     results, t being W elements of x.other (if kReads; zeros or nothing where it is null); x.pre (if kPre and not null) and
-//     out(x, it, split) receive them, rows x.ld_pre and x.ld_out apart, kStream: with the streaming hint; kWhole: N is a multiple of W.  struct Cols, Row { void
+//     out(x, it, split) receive them, rows x.ld_pre and x.ld_out apart; kWhole: N is a multiple of W.  struct Cols, Row { void
 //     load(const Extra &x, int64_t n, int64_t N); } are what a lane keeps of W columns and of a row (which may lie beyond the matrix).
 template <typename Epi> struct TileArgs {
     int n_items;
@@ -568,7 +570,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
                         float t[W];
                         if constexpr (Epi::kReads) unpack16<O>(other[i % BATCH][jj][r], t);
                         Epi::second(extra, y, t);
-                        store_piece<O, Epi::kStream>(out + m * extra.ld_out + n, valid(n), pack16<O>(y));
+                        store_piece(out + m * extra.ld_out + n, valid(n), pack16<O>(y));
                     }
                 }
             }
