@@ -81,29 +81,39 @@ template <typename O, bool SCALED, int ACT = kAnyAct, int SLOPE = kAnyAct, bool 
     using Out = O;
     using Extra = LinearExtra;
     static constexpr int W = 16 / (int)sizeof(O);
+    // Columns and rows beyond the matrix take the values of its last ones (they are not stored): no lane is masked here, see heta_tiles.h.
     struct Cols {
         float bias[W], scale[SCALED ? W : 1];
-        __device__ __forceinline__ void load(const Extra &x, int64_t n, int64_t N)
+        __device__ __forceinline__ static void floats(const float *v, int64_t n, int64_t N, float (&y)[W])
         {
 #pragma unroll
-            for (int e = 0; e < W; ++e) {
-                bias[e] = 0.f;
-                if constexpr (SCALED) scale[e] = 0.f;
-            }
-            if (WHOLE && n >= N) return;
+            for (int h = 0; h < W; h += 4) {
+                if constexpr (WHOLE) {
+                    const uintx4 q = load16(v + min(n, N - W) + h);
 #pragma unroll
-            for (int e = 0; e < W; ++e) {
-                if (!WHOLE && n + e >= N) continue;
-                if (x.bias) bias[e] = x.bias[n + e];
-                if constexpr (SCALED) scale[e] = x.w_scale[n + e];
+                    for (int e = 0; e < 4; ++e) y[h + e] = __uint_as_float(q[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[h + e] = v[min(n + h + e, N - 1)];
+                }
             }
+        }
+        __device__ __forceinline__ void load(const Extra &x, int64_t n, int64_t N)
+        {
+            if (x.bias) {
+                floats(x.bias, n, N, bias);
+            } else {
+#pragma unroll
+                for (int e = 0; e < W; ++e) bias[e] = 0.f;
+            }
+            if constexpr (SCALED) floats(x.w_scale, n, N, scale);
         }
     };
     struct Row {
         float scale;
         __device__ __forceinline__ void load(const Extra &x, int64_t m, int64_t M)
         {
-            if constexpr (SCALED) scale = m < M ? x.in_scale[m] : 0.f;
+            if constexpr (SCALED) scale = x.in_scale[min(m, M - 1)];
         }
     };
     __device__ __forceinline__ static O *out(const Extra &x, const TileItem &, int) { return static_cast<O *>(x.out_p); }
@@ -233,9 +243,9 @@ size_t align_grad_w_bytes(const Launch &l);
 heta_status align_grad_w_bf16(Launch &l, char *to);
 heta_status launch_grad_w_bf16(const Launch &l, float *part);
 
-// one type's launches from its tile shapes: large tiles (Reading: where the epilogue reads in the output's shape), small ones, and
-// both for rows that cannot go straight into LDS
-template <typename Large, typename Reading, typename Small, typename StagedLarge, typename StagedSmall, typename O, bool SLOPES>
+// one type's launches from its tile shapes: large tiles (Reading: where the epilogue reads in the output's shape; Ragged: where its rows are not whole
+// 16-byte pieces), small ones, and both for rows that cannot go straight into LDS
+template <typename Large, typename Reading, typename Ragged, typename Small, typename StagedLarge, typename StagedSmall, typename O, bool SLOPES>
 inline heta_status launch_linear(const Launch &l, size_t elt, const LinearExtra &x)
 {
     constexpr bool SCALED = Large::EB == 1;
@@ -261,7 +271,7 @@ inline heta_status launch_linear(const Launch &l, size_t elt, const LinearExtra 
         return direct ? l.go<Small, LinearEpi<O, SCALED>>(x) : l.go<StagedSmall, LinearEpi<O, SCALED>>(x);
     }
     if (!direct && !std::is_same<StagedLarge, Large>::value) return l.go<StagedLarge, LinearEpi<O, SCALED>>(x);
-    if (l.it.N % (16 / (int)sizeof(O)) != 0) return l.go<Reading, LinearEpi<O, SCALED>>(x);
+    if (l.it.N % (16 / (int)sizeof(O)) != 0) return l.go<Ragged, LinearEpi<O, SCALED>>(x);
     return with_act(SLOPES ? x.slope_act : x.act, [&](auto a) {
         constexpr int A = decltype(a)::value;
         if constexpr (SLOPES) return l.go<Large, LinearEpi<O, SCALED, HETA_ACT_NONE, A, A != HETA_ACT_NONE, true>>(x);

@@ -4,13 +4,14 @@
 namespace heta {
 
 template <bool A_RC, bool B_RC> using Large = TileShape<bf16_t, 2, 1, A_RC, B_RC, kDirect, 2, 4, 4, 2, 64, 2, 1>;       // 256 x 256
+template <bool A_RC, bool B_RC> using Ragged = TileShape<bf16_t, 2, 1, A_RC, B_RC, kDirect, 4, 2, 2, 2, 64, 2, 1>;      // 256 x 128: for epilogues of any width
 template <bool A_RC, bool B_RC> using Small = TileShape<bf16_t, 2, 1, A_RC, B_RC, kDirect, 2, 2, 1, 1, 64, 3, 2>;       // 64 x 64
 template <bool A_RC, bool B_RC> using StagedLarge = TileShape<bf16_t, 2, 1, A_RC, B_RC, kStaged, 4, 2, 2, 2, 64, 2, 1>; // 256 x 128
 template <bool A_RC, bool B_RC> using StagedSmall = TileShape<bf16_t, 2, 1, A_RC, B_RC, kStaged, 2, 2, 1, 1, 64, 2, 2>; // 64 x 64
 
 template <bool B_RC, typename O, bool SLOPES> static heta_status launch(const Launch &l, const LinearExtra &x)
 {
-    return launch_linear<Large<false, B_RC>, Large<false, B_RC>, Small<false, B_RC>, StagedLarge<false, B_RC>, StagedSmall<false, B_RC>, O, SLOPES>(l, 2, x);
+    return launch_linear<Large<false, B_RC>, Large<false, B_RC>, Ragged<false, B_RC>, Small<false, B_RC>, StagedLarge<false, B_RC>, StagedSmall<false, B_RC>, O, SLOPES>(l, 2, x);
 }
 heta_status launch_linear_bf16(const Launch &l, bool input_gradient, heta_dtype out_dt, const LinearExtra &x)
 {
