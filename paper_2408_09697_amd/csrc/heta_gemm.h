@@ -111,10 +111,11 @@ template <int N, bool LDS_DONE> __device__ __forceinline__ void wait_counters()
 // scalar registers / M0, so advancing a tile costs no vector instruction).  Written as inline
 // assembly so that the compiler's wait-count insertion does not treat every later LDS read as
 // dependent on it (which would drain the whole prefetch ring); the kernel orders these loads
-// against their readers itself, with wait_counters() and the workgroup barrier.
+// against their readers itself, with wait_counters() and the workgroup barrier.  A scalar write of M0 needs one wait state in front
+// of a load into LDS, which the compiler puts in front of its own builtins but cannot put into this block.
 __device__ __forceinline__ void load_chunk_to_lds(const void *base, uint32_t offset, uint32_t lds_byte_addr)
 {
-    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "{m0}"(lds_byte_addr) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "{m0}"(lds_byte_addr) : "memory");
 }
 
 // Workgroup barrier that the compiler may not move memory operations across, without the

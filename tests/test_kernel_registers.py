@@ -46,3 +46,27 @@ def test_products_do_not_spill(tmp_path):
             if int(re.search(r"\.vgpr_spill_count:\s+(\d+)", kernel).group(1)) or int(re.search(r"\.private_segment_fixed_size:\s+(\d+)", kernel).group(1)):
                 spilled.append(name)
     assert seen >= 40 and not spilled, spilled
+
+
+OBJDUMP = os.path.join(os.path.dirname(READELF), "llvm-objdump")
+
+
+@pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="llvm-objdump is not installed")
+def test_m0_is_written_a_wait_state_before_loads_into_lds(tmp_path):
+    """gfx9 wants one between a scalar write of M0 and a load that takes its LDS address from there."""
+    loads = 0
+    for i, image in enumerate(device_images(hb.LIB_PATH)):
+        if b"gemm" not in image:
+            continue
+        f = tmp_path / f"{i}.co"
+        f.write_bytes(image)
+        before = ""
+        with subprocess.Popen([OBJDUMP, "-d", "--no-show-raw-insn", "--no-leading-addr", str(f)], stdout=subprocess.PIPE, text=True) as p:
+            for line in p.stdout:
+                op = line.split("//")[0].strip()
+                if op.startswith("global_load_lds"):
+                    loads += 1
+                    assert not re.match(r"s_\S+ m0,", before), f"{before}; {op}"
+                if op:
+                    before = op
+    assert loads > 1000
