@@ -172,13 +172,6 @@ template <typename E> __global__ void __launch_bounds__(256) pack_e4m3_kernel(co
 // ---- host side ---------------------------------------------------------------------------------------
 static bool valid_act(int a) { return a >= HETA_ACT_NONE && a <= HETA_ACT_SILU; }
 
-static heta_status check_matrix(const char *who, const char *what, const void *p, int64_t rows, int64_t ld, int64_t d, size_t elt)
-{
-    if (!p && rows > 0) return fail(HETA_ERR_INVALID_ARG, "%s: null %s", who, what);
-    if (ld < d) return fail(HETA_ERR_SHAPE, "%s: leading dimension of %s is below its width", who, what);
-    if (reinterpret_cast<uintptr_t>(p) % elt) return fail(HETA_ERR_INVALID_ARG, "%s: %s is not aligned to its element size", who, what);
-    return HETA_OK;
-}
 } // namespace heta
 
 using namespace heta;
@@ -188,6 +181,7 @@ extern "C" heta_status heta_linear(heta_graph *g, const heta_linear_args *a, voi
     const char *who = "heta_linear";
     if (!g || !a) return fail(HETA_ERR_INVALID_ARG, "%s: null arguments", who);
     if (a->n_rows < 0 || a->d_in <= 0 || a->d_out <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and widths > 0", who);
+    if (std::max(a->d_in, a->d_out) > kWidest) return fail(HETA_ERR_UNSUPPORTED, "%s: rows too wide", who);
     if (!valid_act(a->act)) return fail(HETA_ERR_INVALID_ARG, "%s: bad act", who);
     const bool q = a->in_dt == HETA_E4M3;
     if (!q && !valid_dtype(a->in_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
@@ -199,11 +193,11 @@ extern "C" heta_status heta_linear(heta_graph *g, const heta_linear_args *a, voi
         return fail(HETA_ERR_INVALID_ARG, "%s: scales belong to 8-bit operands, and those need them", who);
     if (!q && a->coarse_sums) return fail(HETA_ERR_INVALID_ARG, "%s: coarse sums are those of 8-bit operands", who);
     const size_t esz = q ? 1 : dtype_size(a->in_dt), osz = dtype_size(a->out_dt);
-    HETA_TRY(check_matrix(who, "in", a->in, a->n_rows, a->ld_in, a->d_in, esz));
-    HETA_TRY(check_matrix(who, "W", a->W, 1, a->ld_w, q ? a->d_in : a->d_out, esz));
-    HETA_TRY(check_matrix(who, "out", a->out, a->n_rows, a->ld_out, a->d_out, osz));
-    if (a->residual) HETA_TRY(check_matrix(who, "residual", a->residual, a->n_rows, a->ld_res, a->d_out, osz));
-    if (a->pre) HETA_TRY(check_matrix(who, "pre", a->pre, a->n_rows, a->ld_pre, a->d_out, osz));
+    HETA_TRY(check_rows(who, "in", a->in, a->n_rows, a->ld_in, a->d_in, esz));
+    HETA_TRY(check_rows(who, "W", a->W, 1, a->ld_w, q ? a->d_in : a->d_out, esz));
+    HETA_TRY(check_rows(who, "out", a->out, a->n_rows, a->ld_out, a->d_out, osz));
+    if (a->residual) HETA_TRY(check_rows(who, "residual", a->residual, a->n_rows, a->ld_res, a->d_out, osz));
+    if (a->pre) HETA_TRY(check_rows(who, "pre", a->pre, a->n_rows, a->ld_pre, a->d_out, osz));
     for (const float *v : {a->bias, a->in_scale, a->w_scale})
         if (reinterpret_cast<uintptr_t>(v) & 3u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
     const RowRange out(a->out, a->n_rows, a->ld_out, a->d_out, osz), pre(a->pre, a->n_rows, a->ld_pre, a->d_out, osz);
@@ -228,25 +222,26 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
     const char *who = "heta_linear_bwd";
     if (!g || !a) return fail(HETA_ERR_INVALID_ARG, "%s: null arguments", who);
     if (a->n_rows < 0 || a->d_in <= 0 || a->d_out <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and widths > 0", who);
+    if (std::max(a->d_in, a->d_out) > kWidest) return fail(HETA_ERR_UNSUPPORTED, "%s: rows too wide", who);
     if (!valid_act(a->act) || !valid_act(a->in_act)) return fail(HETA_ERR_INVALID_ARG, "%s: bad act", who);
     if (!valid_dtype(a->dt) || (a->dW && !valid_dtype(a->dw_dt))) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
     if (a->dt == HETA_F32 && a->dW && a->dw_dt != HETA_F32) return fail(HETA_ERR_UNSUPPORTED, "%s: fp32 operands have an fp32 weight gradient", who);
     const bool acts = a->act != HETA_ACT_NONE, fused = a->in_act != HETA_ACT_NONE;
     const size_t esz = dtype_size(a->dt);
     const int64_t n = a->n_rows;
-    HETA_TRY(check_matrix(who, "grad_out", a->grad_out, n, a->ld_go, a->d_out, esz));
+    HETA_TRY(check_rows(who, "grad_out", a->grad_out, n, a->ld_go, a->d_out, esz));
     if (acts) {
-        HETA_TRY(check_matrix(who, "pre", a->pre, n, a->ld_pre, a->d_out, esz));
-        HETA_TRY(check_matrix(who, "grad_pre", a->grad_pre, n, a->ld_gp, a->d_out, esz));
+        HETA_TRY(check_rows(who, "pre", a->pre, n, a->ld_pre, a->d_out, esz));
+        HETA_TRY(check_rows(who, "grad_pre", a->grad_pre, n, a->ld_gp, a->d_out, esz));
     }
     if (a->grad_in) {
-        HETA_TRY(check_matrix(who, "grad_in", a->grad_in, n, a->ld_gi, a->d_in, esz));
-        HETA_TRY(check_matrix(who, "W", a->W, 1, a->ld_w, a->d_out, esz));
-        if (fused) HETA_TRY(check_matrix(who, "in_pre", a->in_pre, n, a->ld_ip, a->d_in, esz));
+        HETA_TRY(check_rows(who, "grad_in", a->grad_in, n, a->ld_gi, a->d_in, esz));
+        HETA_TRY(check_rows(who, "W", a->W, 1, a->ld_w, a->d_out, esz));
+        if (fused) HETA_TRY(check_rows(who, "in_pre", a->in_pre, n, a->ld_ip, a->d_in, esz));
     }
     if (a->dW) {
-        HETA_TRY(check_matrix(who, "in", a->in, n, a->ld_in, a->d_in, esz));
-        HETA_TRY(check_matrix(who, "dW", a->dW, 1, a->ld_dw, a->d_out, dtype_size(a->dw_dt)));
+        HETA_TRY(check_rows(who, "in", a->in, n, a->ld_in, a->d_in, esz));
+        HETA_TRY(check_rows(who, "dW", a->dW, 1, a->ld_dw, a->d_out, dtype_size(a->dw_dt)));
     }
     if (reinterpret_cast<uintptr_t>(a->dbias) & 3u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
     const RowRange go(a->grad_out, n, a->ld_go, a->d_out, esz), pre(acts ? a->pre : nullptr, n, a->ld_pre, a->d_out, esz);
@@ -336,8 +331,9 @@ extern "C" heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int
     const char *who = "heta_linear_pack_e4m3";
     if (!valid_dtype(w_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
     if (d_in <= 0 || d_out <= 0) return fail(HETA_ERR_SHAPE, "%s: need widths > 0", who);
-    HETA_TRY(check_matrix(who, "W", W, 1, ld_w, d_out, dtype_size(w_dt)));
-    HETA_TRY(check_matrix(who, "packed", packed, 1, ld_packed, d_in, 1));
+    if (std::max(d_in, d_out) > kWidest) return fail(HETA_ERR_UNSUPPORTED, "%s: rows too wide", who);
+    HETA_TRY(check_rows(who, "W", W, 1, ld_w, d_out, dtype_size(w_dt)));
+    HETA_TRY(check_rows(who, "packed", packed, 1, ld_packed, d_in, 1));
     if (!scale || (reinterpret_cast<uintptr_t>(scale) & 3u)) return fail(HETA_ERR_INVALID_ARG, "%s: bad scale", who);
     const RowRange w(W, d_in, ld_w, d_out, dtype_size(w_dt)), o(packed, d_out, ld_packed, d_in, 1), s(scale, 1, d_out, d_out, 4);
     if (o.overlaps(w) || s.overlaps(w) || s.overlaps(o)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);

@@ -486,14 +486,6 @@ template <typename T, typename G> static void launch_norm_bwd(const NormBwd &p, 
         });
 }
 
-static heta_status check_rows(const char *who, const char *what, const void *p, int64_t n_rows, int64_t ld, int32_t d, size_t elt)
-{
-    if (!p && n_rows > 0) return fail(HETA_ERR_INVALID_ARG, "%s: null %s", who, what);
-    if (ld < d) return fail(HETA_ERR_SHAPE, "%s: leading dimension of %s is below its width", who, what);
-    if (reinterpret_cast<uintptr_t>(p) % elt) return fail(HETA_ERR_INVALID_ARG, "%s: %s is not aligned to its element size", who, what);
-    return HETA_OK;
-}
-
 } // namespace heta
 
 using namespace heta;
@@ -503,6 +495,7 @@ extern "C" heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, h
 {
     const char *who = "heta_rms_norm";
     if (n_rows < 0 || d <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and d > 0", who);
+    if (d > kWidest) return fail(HETA_ERR_UNSUPPORTED, "%s: rows too wide", who);
     if (!valid_dtype(x_dt) || (!valid_dtype(out_dt) && out_dt != HETA_E4M3)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
     if (!(eps >= 0.f)) return fail(HETA_ERR_INVALID_ARG, "%s: need eps >= 0", who);
     const bool q = out_dt == HETA_E4M3;
@@ -552,6 +545,7 @@ extern "C" heta_status heta_rms_norm_bwd(heta_graph *g, int64_t n_rows, int32_t 
     const char *who = "heta_rms_norm_bwd";
     if (!g) return fail(HETA_ERR_INVALID_ARG, "%s: null handle", who);
     if (n_rows < 0 || d <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and d > 0", who);
+    if (d > kWidest) return fail(HETA_ERR_UNSUPPORTED, "%s: rows too wide", who);
     if (!valid_dtype(x_dt) || !valid_dtype(go_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
     if (x_dt == HETA_BF16 && go_dt == HETA_F32) return fail(HETA_ERR_UNSUPPORTED, "%s: bf16 rows have a bf16 gradient", who);
     const size_t esz = dtype_size(x_dt), gsz = dtype_size(go_dt);

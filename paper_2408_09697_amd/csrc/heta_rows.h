@@ -132,6 +132,16 @@ constexpr float kE4m3Least = 1.504632769052528e-36f; // 2^-119
 __device__ __forceinline__ float e4m3_factor(float amax) { return amax >= kE4m3Least ? 448.f / amax : amax != amax ? amax : 0.f; }
 __device__ __forceinline__ float e4m3_scale(float amax) { return amax < kE4m3Least ? 0.f : amax / 448.f; }
 
+// Argument checks of the calls on such rows (host).  Widths stay a little below 2^31: kernels count columns in 32 bits, a workgroup's at a time.
+constexpr int32_t kWidest = INT32_MAX - 1023;
+inline heta_status check_rows(const char *who, const char *what, const void *p, int64_t n_rows, int64_t ld, int64_t d, size_t elt)
+{
+    if (!p && n_rows > 0) return fail(HETA_ERR_INVALID_ARG, "%s: null %s", who, what);
+    if (ld < d) return fail(HETA_ERR_SHAPE, "%s: leading dimension of %s is below its width", who, what);
+    if (reinterpret_cast<uintptr_t>(p) % elt) return fail(HETA_ERR_INVALID_ARG, "%s: %s is not aligned to its element size", who, what);
+    return HETA_OK;
+}
+
 // Calls that move more than the chip's 256 MB last-level cache holds read and write with the streaming hint; below, what a
 // call writes is still cached when the next one reads it.
 inline bool streams(double bytes) { return bytes > 256e6; }

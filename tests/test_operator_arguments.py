@@ -124,3 +124,20 @@ def test_linear_vectors_that_overlap(lib, handle, base, change):
 @pytest.mark.parametrize("flags", [4, 7, -1])
 def test_momentum_flags(lib, handle, flags):
     refused(lib, lib.heta_muon_multi(handle, 1, ctypes.byref(muon_item(64, 48)), 0.02, 0.9, flags, 0.0, 1e-7, 5, None), BAD, "flags")
+
+
+WIDE = 2 ** 31 - 1
+
+
+def test_widths_near_2_to_the_31(lib, handle):
+    """Column counters step by a workgroup's width and would pass 2^31."""
+    far = {name: 1 << 44 | i << 40 for i, name in enumerate("abcdefgh")}  # 1 TB apart
+    refused(lib, lib.heta_rms_norm(1, WIDE, far["a"], F32, WIDE, None, 0, None, 1e-6, None, 0, far["b"], F32, WIDE, None, None, None), UNSUPPORTED, "wide")
+    refused(lib, lib.heta_rms_norm_bwd(handle, 1, WIDE, far["a"], F32, WIDE, None, far["b"], far["c"], F32, WIDE, None, 0, far["d"], WIDE, far["e"], None), UNSUPPORTED, "wide")
+    for d_in, d_out in ((1, WIDE), (WIDE, 1)):
+        a = dict(n_rows=1, d_in=d_in, d_out=d_out, inp=far["a"], ld_in=d_in, W=far["b"], ld_w=d_out, out=far["c"], ld_out=d_out, in_dt=BF16, w_dt=BF16, out_dt=BF16)
+        refused(lib, lib.heta_linear(handle, ctypes.byref(hb._LinearArgs(**a)), None), UNSUPPORTED, "wide")
+        a = dict(n_rows=1, d_in=d_in, d_out=d_out, dt=BF16, dw_dt=BF16, inp=far["a"], ld_inp=d_in, W=far["b"], ld_W=d_out, grad_out=far["c"], ld_grad_out=d_out, grad_in=far["d"],
+                 ld_grad_in=d_in, dW=far["e"], ld_dW=d_out, dbias=far["f"])
+        refused(lib, lib.heta_linear_bwd(handle, ctypes.byref(hb._LinearBwdArgs(**a)), None), UNSUPPORTED, "wide")
+        refused(lib, lib.heta_linear_pack_e4m3(far["a"], F32, d_out, d_in, d_out, far["b"], d_in, far["c"], None), UNSUPPORTED, "wide")
