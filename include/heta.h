@@ -609,7 +609,10 @@ heta_status heta_sparse_adam_multi(int32_t n_items, const heta_adam_item *items,
 
 /* ---- residual feed-forward blocks over node embeddings --------------------------------------------
  * A deep model follows the relation aggregation of a node type with a block  h <- h + act(norm(h + agg) W1 + b1) W2 + b2.
- * These calls are its norm, its products and the update of its matrices (and of the relations').
+ * These calls are its norm, its products and the update of its matrices (and of the relations').  Where a call uses the handle's
+ * workspace (heta_linear does for products of few tiles and a long contraction), it has to be stream-ordered with the handle's other calls that do: one
+ * handle per stream that runs them.  heta_project and its relatives are the products of a layer's relations (accumulation into an output, several relations
+ * per launch, row scales); heta_linear that of a dense layer (bias, activation, residual, its pre-activation, 8-bit operands).
  *
  * heta_rms_norm: s = x + residual, rounded to x_dt;  rstd_i = 1 / sqrt(sum_j s_ij^2 / d + eps);  out = s rstd gamma.
  *   x, residual (NULL: none), sum (NULL: not stored): device [n_rows, d] of x_dt; gamma: device fp32 [d] (NULL: ones);
@@ -639,7 +642,8 @@ heta_status heta_rms_norm_bwd(heta_graph *g, int64_t n_rows, int32_t d, const vo
  *   products, a hundredth of a bf16 output's rounding).
  *   bias: device fp32 [d_out] or NULL; residual: out_dt [n_rows, ld_res] or NULL, may be out; pre (NULL: not stored) receives
  *   the pre-activation in out_dt, which heta_linear_bwd reads.
- * g: handle whose workspace the call may use (and grow). */
+ * Infinite fp32 operands give what the definition gives (infinity times 0 is NaN).
+ * g: handle whose workspace the call may use (and grow, by up to 4 MB). */
 typedef struct heta_linear_args {
     int64_t n_rows;
     int32_t d_in, d_out;

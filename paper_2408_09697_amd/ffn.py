@@ -18,8 +18,8 @@ from . import binding as hb
 
 
 class FeedForwardBlock:
-    """g: any handle whose workspace the calls may use.  W1 [d, d_hidden], W2 [d_hidden, d] (fp32 or bf16, like the embeddings);
-    gamma, b1, b2: fp32 vectors or None."""
+    """g: any handle whose workspace the calls may use; blocks that run on streams of their own have handles of their own.
+    W1 [d, d_hidden], W2 [d_hidden, d] (fp32 or bf16, like the embeddings); gamma, b1, b2: fp32 vectors or None."""
 
     def __init__(self, g: hb.Graph, W1: torch.Tensor, W2: torch.Tensor, gamma: Optional[torch.Tensor] = None, b1: Optional[torch.Tensor] = None,
                  b2: Optional[torch.Tensor] = None, act: int = hb.HETA_ACT_GELU, eps: float = 1e-6):
