@@ -71,7 +71,7 @@ struct LinearExtra {
     int act, slope_act;                     // slope_act != NONE: other is a pre-activation
 };
 // O: type of the outputs and of what is read in their shape.  SCALED: 8-bit operands.  ACT, SLOPE: which activation, and whose
-// slope, or kAnyAct for a choice at run time (small tiles): with it the epilogue of a large tile is 11,000 instructions long
+// slope, or kAnyAct for a choice at run time (small tiles, and outputs of any width): with it the epilogue of a large tile is 11,000 instructions long
 // and takes longer than the product.  READS: whether `other` may be there.  WHOLE: the output is whole 16-byte pieces wide (without
 // it the epilogues of large tiles cost 5 to 14 % of a product).
 constexpr int kAnyAct = -1;
