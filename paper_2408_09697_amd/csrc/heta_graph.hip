@@ -177,11 +177,15 @@ heta_status ensure_workspace(heta_graph *g, size_t bytes)
         g->ws_bytes = 0;
     }
     size_t want = bytes + bytes / 4;
-    if (g_ws_limit > 0 && bytes > g_ws_limit)
+    auto refused = [&] { g->ws_refused = g->ws_refused > 0 ? std::min(g->ws_refused, bytes) : bytes; };
+    if (g_ws_limit > 0 && bytes > g_ws_limit) {
+        refused();
         return fail(HETA_ERR_OOM, "workspace of %zu bytes: beyond the limit set for tests", bytes);
+    }
     const hipError_t e = scratch_alloc(&g->d_ws, want);
     if (e != hipSuccess) {
         g->d_ws = nullptr;
+        refused();
         (void)hipGetLastError(); // reported here, not by the next launch's check
         return fail(e == hipErrorOutOfMemory ? HETA_ERR_OOM : HETA_ERR_DEVICE, "workspace of %zu bytes: %s", want, hipGetErrorString(e));
     }

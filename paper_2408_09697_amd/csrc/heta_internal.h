@@ -147,6 +147,7 @@ struct heta_graph {
     // workspace for hub-row partials and split weight-gradient partials; grown on demand
     void *d_ws = nullptr;
     size_t ws_bytes = 0;
+    size_t ws_refused = 0; // smallest size that there was no room for (0: none), not tried again where a call can do with less
     // k-contiguous copies of the bf16 weight matrices of the projection in flight; grown on demand
     void *d_pack = nullptr;
     size_t pack_bytes = 0;

@@ -291,7 +291,8 @@ extern "C" heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args
     const size_t copies_at = (need + 255) / 256 * 256;
     size_t copies = a->dW && n > 0 && a->dt == HETA_BF16 ? align_grad_w_bytes(w_l) : 0;
     if (a->grad_in && n > 0) need = std::max(need, plan_split(in_l, esz).bytes);
-    if (copies > 0 && ensure_workspace(g, std::max(need, copies_at + copies)) != HETA_OK) copies = 0;
+    const size_t most = std::max(need, copies_at + copies);
+    if (copies > 0 && ((g->ws_refused > 0 && most >= g->ws_refused) || ensure_workspace(g, most) != HETA_OK)) copies = 0;
     if (need > 0) HETA_TRY(ensure_workspace(g, need));
     float *ws = static_cast<float *>(g->d_ws);
 

@@ -269,3 +269,25 @@ def test_few_row_blocks_and_splits(handle, n, d_in, d_out, dtype):
     assert torch.equal(out, x.float() @ W.float())
     heta.heta_linear_bwd(handle, x, W, go, grad_in=gi, grad_W=gw, grad_bias=gb)
     assert torch.equal(gi, (go.float() @ W.float().t()).to(dtype)) and torch.equal(gw, x.float().t() @ go.float()) and torch.equal(gb, go.float().sum(0))
+
+
+def test_copies_without_room_are_not_tried_again(workspace_limit):
+    """A second call leaves the workspace alone, so that it can be captured into a graph like any warmed-up call."""
+    n, d_in, d_out = 100_000, 301, 517
+    x, go = integers(1, n, d_in, BF16), integers(3, n, d_out, BF16)
+    want = x.float().t() @ go.float()
+    g, gw = heta.heta_graph_create([(1, 1, 0)], []), torch.empty(d_in, d_out, device="cuda")
+    workspace_limit(64 << 20)
+    heta.heta_linear_bwd(g, x, None, go, grad_W=gw)
+    workspace_limit(0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        heta.heta_linear_bwd(g, x, None, go, grad_W=gw)
+    for _ in range(3):
+        gw.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(gw, want)
+    del graph
+    g.destroy()
