@@ -50,8 +50,9 @@ typedef enum {
     HETA_ERR_DEVICE = 6       /* a HIP call failed; heta_last_error() carries the HIP message */
 } heta_status;
 
-/* HETA_E4M3: 8 bits, 4 of exponent and 3 of significand (largest value 448, no infinities); only where a call names it */
-typedef enum { HETA_F32 = 0, HETA_BF16 = 1, HETA_E4M3 = 2 } heta_dtype;
+/* HETA_E4M3: 8 bits, 4 of exponent and 3 of significand (largest value 448, no infinities); HETA_I8: whole numbers of 8 bits; only where a call
+ * names them */
+typedef enum { HETA_F32 = 0, HETA_BF16 = 1, HETA_E4M3 = 2, HETA_I8 = 3 } heta_dtype;
 typedef enum { HETA_SUM = 0, HETA_MEAN = 1 } heta_reduce;
 /* GELU in its tanh form, x / (1 + exp(-2 sqrt(2 / pi) (x + 0.044715 x^3))), and SILU, x / (1 + exp(-x)), are activations of
  * heta_linear and heta_linear_bwd; the other calls know NONE and RELU */
@@ -640,6 +641,8 @@ heta_status heta_rms_norm_bwd(heta_graph *g, int64_t n_rows, int32_t d, const vo
  *   are added as exactly as those of the other types (bf16 matrix instruction), or, with coarse_sums != 0, by the 8-bit matrix
  *   instruction: twice the rate, and sums that may miss 2^-12 of sum_k |in_ik W_kj| (1.5e-5 of the result over 1,024 random
  *   products, a hundredth of a bf16 output's rounding).
+ *   HETA_I8: W is [d_out, d_in] (heta_linear_pack_i8) and the rows are those of heta_linear_rows_i8, scales as above; the products are added as
+ *   32-bit integers, exactly, at the 8-bit rate.  d_in below 2^17 (HETA_ERR_UNSUPPORTED otherwise).
  *   bias: device fp32 [d_out] or NULL; residual: out_dt [n_rows, ld_res] or NULL, may be out; pre (NULL: not stored) receives
  *   the pre-activation in out_dt, which heta_linear_bwd reads.
  * Infinite fp32 operands give what the definition gives (infinity times 0 is NaN).
@@ -703,6 +706,96 @@ heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args *args, voi
  * max_k |W[k, j]| / 448 (columns of zeros and with NaN as in heta_rms_norm).  Once per set of weights. */
 heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int64_t ld_w, int32_t d_in, int32_t d_out, void *packed, int64_t ld_packed,
                                   float *scale, void *hip_stream);
+
+/* Rows in 8-bit whole numbers, for heta_linear: out_ij = the nearest whole number (ties to even) to 127 x_ij / max_j |x_ij|, scale_i = max_j |x_ij| / 127
+ * (device fp32 [n_rows]); rows of nothing from 2^-119 on are zeros with scale 0, those with a NaN or an infinity have it as their scale.  x: fp32 or bf16
+ * [n_rows, ld_x]; out: device [n_rows, ld_out] of HETA_I8. */
+heta_status heta_linear_rows_i8(int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, void *out, int64_t ld_out, float *scale, void *hip_stream);
+/* Weights W [d_in, d_out] (fp32 or bf16) as such rows: packed [d_out, ld_packed >= d_in] of HETA_I8, scale [d_out] = max_k |W[k, j]| / 127.  Once per set
+ * of weights. */
+heta_status heta_linear_pack_i8(const void *W, heta_dtype w_dt, int64_t ld_w, int32_t d_in, int32_t d_out, void *packed, int64_t ld_packed, float *scale,
+                                void *hip_stream);
+
+/* ---- the loss behind an output product, without its logits in memory -------------------------------
+ * heta_linear_xent: softmax cross entropy of n_rows rows over n_classes classes,
+ *   z = in . W + bias;  lse_i = log sum_j exp z_ij;  loss_i = lse_i - z_i,labels[i]
+ * in, W: fp32 or bf16, [n_rows, d] and [d, n_classes]; bias: device fp32 [n_classes] or NULL; labels: device int64 [n_rows].  A row whose label is outside
+ * [0, n_classes) (-1 by custom) has none: its loss is 0, its gradients are zeros, and nothing else depends on what the row holds, NaN included.
+ * loss (NULL: not stored), lse: device fp32 [n_rows].  mean (device fp32 [2], NULL: not computed): the mean of the losses of the rows with a label (0
+ * without any) and how many these are.  Logits are fp32 sums; they are at no time in memory.
+ * Uses the handle's workspace (may grow it: by 8 bytes for 32 to 64 logits, and, from 512 rows on, by copies of bf16 operands whose rows are not
+ * 16-byte aligned). */
+typedef struct heta_linear_xent_args {
+    int64_t n_rows;
+    int32_t d, n_classes;
+    const void *in;
+    int64_t ld_in;
+    const void *W;
+    int64_t ld_w;
+    const float *bias;
+    const int64_t *labels;
+    float *loss, *lse, *mean;
+    heta_dtype dt;
+} heta_linear_xent_args;
+heta_status heta_linear_xent(heta_graph *g, const heta_linear_xent_args *args, void *hip_stream);
+/* Its gradients, lse being what the forward stored, with f_i = scale * (grad_loss ? grad_loss[i] : 1) / (mean ? mean[1] : 1) and D_ij = f_i (exp(z_ij -
+ * lse_i) - [j = labels[i]]), zero for rows without a label:
+ *   grad_in = D . W^T (dt);   dW = in^T . D (dw_dt: fp32, or bf16 for bf16 operands);   dbias[j] = sum_i D_ij (fp32)      each NULL: not computed
+ * grad_loss: device fp32 [n_rows] or NULL; mean: what the forward wrote (gradients of the mean) or NULL (of the sum).  All outputs are overwritten; sums
+ * are added in a fixed order.  The products read D rounded to dt.  The logits are formed again.
+ * Uses the handle's workspace (may grow it: by 192 MB of D or D itself where that is less, a copy of the rows, partial sums of the gradients, and copies as
+ * above). */
+typedef struct heta_linear_xent_bwd_args {
+    int64_t n_rows;
+    int32_t d, n_classes;
+    const void *in;
+    int64_t ld_in;
+    const void *W;
+    int64_t ld_w;
+    const float *bias;
+    const int64_t *labels;
+    const float *lse, *grad_loss, *mean;
+    void *grad_in;
+    int64_t ld_gi;
+    void *dW;
+    int64_t ld_dw;
+    float *dbias;
+    float scale;
+    heta_dtype dt, dw_dt;
+} heta_linear_xent_bwd_args;
+heta_status heta_linear_xent_bwd(heta_graph *g, const heta_linear_xent_bwd_args *args, void *hip_stream);
+
+/* ---- the update of a model's tensors ---------------------------------------------------------------
+ * heta_adamw_multi: one step of Adam with decoupled weight decay on n_items tensors [rows, d], for the listed rows r = ids ? ids[i] : i, i < n, g = grad[i]:
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2;
+ *   W = (1 - lr weight_decay) W - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * W: fp32 or bf16 (updated in fp32 and rounded back); grad: fp32 or bf16; ids as for heta_sparse_adam (distinct; those outside [0, rows) are skipped).
+ * state_dt HETA_F32: m, v device fp32 [rows, ld_state], scales NULL.
+ * state_dt HETA_E4M3: m holds m and v holds sqrt(v), 8 bits an element, with a scale for each 128 columns of a row (m_scale, v_scale: device fp32 [rows,
+ *   ld_scale >= ceil(d / 128)]); a value is its code times its scale.  The scale is the largest new magnitude of the block / 448 (0, and the codes too, below 2^-119),
+ *   and a value goes to one of its two neighbours among the codes, up with probability (value - lower) / (upper - lower), by 16 bits that are a function of
+ *   seed, step and the element's place alone; a sqrt(v) above 0 keeps a code above 0.  Zeros (codes and scales) are the state before the first step.  A NaN or
+ *   an infinity among a block's new values makes the block NaN.  W's step is taken from the new values before they are rounded.
+ * seed: of its own for each tensor with 8-bit states.  weight_decay: per item (0 for gains and biases, by custom).
+ * All arrays are device memory, items a HOST array; no array that is written may overlap another one of the call.  All items are checked before the first
+ * launch.  Items share launches: up to 64 that are contiguous with fp32 states, up to 24 others of the same types.  n_items = 0 is a no-op. */
+typedef struct heta_adamw_item {
+    void *W;
+    int64_t ld_w;
+    const void *grad;
+    int64_t ld_grad;
+    void *m, *v;
+    int64_t ld_state;
+    float *m_scale, *v_scale;
+    int64_t ld_scale;
+    const int64_t *ids;
+    int64_t n, rows;
+    int32_t d;
+    heta_dtype dt, grad_dt, state_dt;
+    float weight_decay;
+    uint32_t seed;
+} heta_adamw_item;
+heta_status heta_adamw_multi(int32_t n_items, const heta_adamw_item *items, float lr, float beta1, float beta2, float eps, int64_t step, void *hip_stream);
 
 /* heta_muon_multi: orthogonalised momentum (Muon, Jordan et al. 2024) on n_items weight matrices [rows, cols] of products in . W:
  *   m <- momentum m + grad;   u = grad + momentum m with HETA_MUON_NESTEROV among the flags, else m;   X = u / (|u|_F + eps);

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_PKG, "lib", "libheta.so")
 HETA_OK = 0
 HETA_ERR_INVALID_ARG, HETA_ERR_BAD_CSR, HETA_ERR_SHAPE = 1, 2, 3
 HETA_ERR_UNSUPPORTED, HETA_ERR_OOM, HETA_ERR_DEVICE = 4, 5, 6
-HETA_F32, HETA_BF16, HETA_E4M3 = 0, 1, 2
+HETA_F32, HETA_BF16, HETA_E4M3, HETA_I8 = 0, 1, 2, 3
 HETA_SUM, HETA_MEAN = 0, 1
 HETA_ACT_NONE, HETA_ACT_RELU, HETA_ACT_GELU, HETA_ACT_SILU = 0, 1, 2, 3
 HETA_PTRS_ON_DEVICE = 1
@@ -39,7 +39,8 @@ EXPORTS = ["heta_graph_create", "heta_graph_create_batch", "heta_graph_destroy",
            "heta_sample_neighbors", "heta_unique_relabel",
            "heta_cross_rel_aggregate_project", "heta_meta_partition", "heta_sample_neighbors_batch",
            "heta_unique_relabel_batch", "heta_sample_hop", "heta_rel_aggregate_fwd_noalloc", "heta_attn_fold", "heta_attn_fold_bwd",
-           "heta_graph_index_bytes", "heta_rms_norm", "heta_rms_norm_bwd", "heta_linear", "heta_linear_bwd", "heta_linear_pack_e4m3", "heta_muon_multi"]
+           "heta_graph_index_bytes", "heta_rms_norm", "heta_rms_norm_bwd", "heta_linear", "heta_linear_bwd", "heta_linear_pack_e4m3", "heta_muon_multi",
+           "heta_linear_rows_i8", "heta_linear_pack_i8", "heta_linear_xent", "heta_linear_xent_bwd", "heta_adamw_multi"]
 # process-wide switches for tests and measurements, declared in csrc/heta_test_hooks.h (not in the public header)
 TEST_HOOKS = ["heta_projection_force_staged", "heta_ingest_force", "heta_projection_f32_native", "heta_workspace_limit"]
 HETA_NOALLOC_SCRATCH_BYTES = 32 << 20
@@ -84,6 +85,25 @@ class _LinearBwdArgs(ctypes.Structure):
 class _MuonItem(ctypes.Structure):
     _fields_ = [("W", ctypes.c_void_p), ("ld_w", ctypes.c_int64), ("m", ctypes.c_void_p), ("ld_m", ctypes.c_int64), ("grad", ctypes.c_void_p),
                 ("ld_grad", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("dt", ctypes.c_int32), ("grad_dt", ctypes.c_int32)]
+
+
+class _XentArgs(ctypes.Structure):
+    _fields_ = ([("n_rows", ctypes.c_int64), ("d", ctypes.c_int32), ("n_classes", ctypes.c_int32), ("inp", ctypes.c_void_p), ("ld_in", ctypes.c_int64), ("W", ctypes.c_void_p),
+                 ("ld_w", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("bias", "labels", "loss", "lse", "mean")] + [("dt", ctypes.c_int32)])
+
+
+class _XentBwdArgs(ctypes.Structure):
+    _fields_ = ([("n_rows", ctypes.c_int64), ("d", ctypes.c_int32), ("n_classes", ctypes.c_int32), ("inp", ctypes.c_void_p), ("ld_in", ctypes.c_int64), ("W", ctypes.c_void_p),
+                 ("ld_w", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("bias", "labels", "lse", "grad_loss", "mean", "grad_in")] +
+                [("ld_gi", ctypes.c_int64), ("dW", ctypes.c_void_p), ("ld_dw", ctypes.c_int64), ("dbias", ctypes.c_void_p), ("scale", ctypes.c_float), ("dt", ctypes.c_int32),
+                 ("dw_dt", ctypes.c_int32)])
+
+
+class _AdamwItem(ctypes.Structure):
+    _fields_ = [("W", ctypes.c_void_p), ("ld_w", ctypes.c_int64), ("grad", ctypes.c_void_p), ("ld_grad", ctypes.c_int64), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("ld_state", ctypes.c_int64), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64), ("ids", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("rows", ctypes.c_int64), ("d", ctypes.c_int32), ("dt", ctypes.c_int32), ("grad_dt", ctypes.c_int32), ("state_dt", ctypes.c_int32),
+                ("weight_decay", ctypes.c_float), ("seed", ctypes.c_uint32)]
 
 
 class _AggItem(ctypes.Structure):
@@ -151,6 +171,11 @@ def load_library() -> ctypes.CDLL:
     L.heta_linear.argtypes = [vp, vp, vp]
     L.heta_linear_bwd.argtypes = [vp, vp, vp]
     L.heta_linear_pack_e4m3.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp]
+    L.heta_linear_rows_i8.argtypes = [i64, i32, vp, i32, i64, vp, i64, vp, vp]
+    L.heta_linear_pack_i8.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp]
+    L.heta_linear_xent.argtypes = [vp, vp, vp]
+    L.heta_linear_xent_bwd.argtypes = [vp, vp, vp]
+    L.heta_adamw_multi.argtypes = [i32, vp, f32, f32, f32, f32, i64, vp]
     L.heta_muon_multi.argtypes = [vp, i32, vp, f32, f32, i32, f32, f32, i32, vp]
     for name in EXPORTS + TEST_HOOKS:
         getattr(L, name).restype = ctypes.c_int
@@ -285,6 +310,10 @@ _AGG_PACK = struct.Struct("=iiQqqQQqf4x")    # heta_agg_item
 _ADAM_PACK = struct.Struct("=Qi4xqi4xqQQqQqQq")  # heta_adam_item
 _LINEAR_PACK = struct.Struct("=qiiQqQQqQQQqQqQqiiiii4x")       # heta_linear_args
 _LINEAR_BWD_PACK = struct.Struct("=qiiiiii" + "Qq" * 8 + "Q")  # heta_linear_bwd_args
+_XENT_PACK = struct.Struct("=qiiQqQqQQQQQi4x")                  # heta_linear_xent_args
+_XENT_BWD_PACK = struct.Struct("=qiiQqQqQQQQQQqQqQfii4x")      # heta_linear_xent_bwd_args
+_ADAMW_PACK = struct.Struct("=QqQqQQqQQqQqqiiiifI")            # heta_adamw_item
+assert _XENT_PACK.size == ctypes.sizeof(_XentArgs) and _XENT_BWD_PACK.size == ctypes.sizeof(_XentBwdArgs) and _ADAMW_PACK.size == ctypes.sizeof(_AdamwItem)
 _MUON_PACK = struct.Struct("=QqQqQqiiii")                      # heta_muon_item
 assert _LINEAR_PACK.size == ctypes.sizeof(_LinearArgs) and _LINEAR_BWD_PACK.size == ctypes.sizeof(_LinearBwdArgs) and _MUON_PACK.size == ctypes.sizeof(_MuonItem)
 assert _AGG_PACK.size == ctypes.sizeof(_AggItem) and _ADAM_PACK.size == ctypes.sizeof(_AdamItem)
@@ -933,7 +962,7 @@ def _floats_of(t: Optional[torch.Tensor], name: str, n: int) -> int:
     return p
 
 
-_DT8 = {torch.float32: HETA_F32, torch.bfloat16: HETA_BF16, torch.float8_e4m3fn: HETA_E4M3}
+_DT8 = {torch.float32: HETA_F32, torch.bfloat16: HETA_BF16, torch.float8_e4m3fn: HETA_E4M3, torch.int8: HETA_I8}
 
 
 def _dt8(t: torch.Tensor) -> int:
@@ -977,14 +1006,14 @@ def heta_rms_norm_bwd(g: Graph, x: torch.Tensor, rstd: torch.Tensor, grad_out: t
 def heta_linear(g: Graph, inp: torch.Tensor, W: torch.Tensor, out: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = HETA_ACT_NONE,
                 residual: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, in_scale: Optional[torch.Tensor] = None,
                 w_scale: Optional[torch.Tensor] = None, coarse_sums: bool = False, stream=None) -> torch.Tensor:
-    """pre = inp @ W + bias; out = act(pre) + residual.  W is [d_in, d_out]; for 8-bit operands [d_out, d_in] with in_scale [n_rows]
-    and w_scale [d_out], and coarse_sums lets the 8-bit matrix instruction add their products."""
+    """pre = inp @ W + bias; out = act(pre) + residual.  W is [d_in, d_out]; for 8-bit operands (torch.float8_e4m3fn, torch.int8) [d_out, d_in] with in_scale
+    [n_rows] and w_scale [d_out]; for torch.float8_e4m3fn coarse_sums lets the 8-bit matrix instruction add the products."""
     n, d_in = inp.shape
     d_out = out.shape[1]
     t = out.dtype
     dt = _dt8(inp)
     pi, li = _rows_of(inp, "in", inp.dtype, n, d_in)
-    pw, lw = _rows_of(W, "W", W.dtype, d_out, d_in) if dt == HETA_E4M3 else _rows_of(W, "W", W.dtype, d_in, d_out)
+    pw, lw = _rows_of(W, "W", W.dtype, d_out, d_in) if dt in (HETA_E4M3, HETA_I8) else _rows_of(W, "W", W.dtype, d_in, d_out)
     po, lo = _rows_of(out, "out", t, n, d_out)
     pr, lr = _rows_of(residual, "residual", t, n, d_out)
     pp, lp = _rows_of(pre, "pre", t, n, d_out)
@@ -1026,6 +1055,127 @@ def heta_linear_pack_e4m3(W: torch.Tensor, packed: torch.Tensor, scale: torch.Te
     pp, lp = _rows_of(packed, "packed", torch.float8_e4m3fn, d_out, d_in)
     _check(load_library().heta_linear_pack_e4m3(pw, _dt8(W), lw, d_in, d_out, pp, lp, _floats_of(scale, "scale", d_out), _stream(stream)))
     return packed
+
+
+def heta_linear_rows_i8(x: torch.Tensor, out: torch.Tensor, scale: torch.Tensor, stream=None) -> torch.Tensor:
+    """Rows as 8-bit whole numbers (torch.int8) with a scale each, for heta_linear."""
+    n, d = x.shape
+    px, lx = _rows_of(x, "x", x.dtype, n, d)
+    po, lo = _rows_of(out, "out", torch.int8, n, d)
+    _check(load_library().heta_linear_rows_i8(n, d, px, _dt8(x), lx, po, lo, _floats_of(scale, "scale", n), _stream(stream)))
+    return out
+
+
+def heta_linear_pack_i8(W: torch.Tensor, packed: torch.Tensor, scale: torch.Tensor, stream=None) -> torch.Tensor:
+    """Weights [d_in, d_out] as rows [d_out, d_in] of 8-bit whole numbers (torch.int8) with a scale each, for heta_linear."""
+    d_in, d_out = W.shape
+    pw, lw = _rows_of(W, "W", W.dtype, d_in, d_out)
+    pp, lp = _rows_of(packed, "packed", torch.int8, d_out, d_in)
+    _check(load_library().heta_linear_pack_i8(pw, _dt8(W), lw, d_in, d_out, pp, lp, _floats_of(scale, "scale", d_out), _stream(stream)))
+    return packed
+
+
+def _labels_of(t: torch.Tensor, n: int) -> int:
+    p, got = _vec(t, "labels", torch.int64)
+    if got != n:
+        raise HetaError(HETA_ERR_SHAPE, f"labels must have {n} elements, got {got}")
+    return p
+
+
+def heta_linear_xent(g: Graph, inp: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, loss: Optional[torch.Tensor], lse: torch.Tensor,
+                     bias: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Softmax cross entropy of the rows of inp @ W + bias (W [d, n_classes]) against labels (int64; outside the classes: none, loss 0): loss and lse [n] and
+    mean [2] (the mean over the rows with a label, and their number), fp32.  The logits are not kept."""
+    n, d = inp.shape
+    classes = W.shape[1]
+    pi, li = _rows_of(inp, "in", inp.dtype, n, d)
+    pw, lw = _rows_of(W, "W", inp.dtype, d, classes)
+    args = _XENT_PACK.pack(n, d, classes, pi, li, pw, lw, _floats_of(bias, "bias", classes), _labels_of(labels, n), _floats_of(loss, "loss", n),
+                           _floats_of(lse, "lse", n), _floats_of(mean, "mean", 2), _dt8(inp))
+    _check(load_library().heta_linear_xent(g.handle, args, _stream(stream)))
+    return loss
+
+
+def heta_linear_xent_bwd(g: Graph, inp: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                         grad_loss: Optional[torch.Tensor] = None, scale: float = 1.0, mean: Optional[torch.Tensor] = None, grad_in: Optional[torch.Tensor] = None,
+                         grad_W: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients (each if given) of heta_linear_xent's losses times scale * grad_loss (ones if not given), or, with the forward's mean, of their mean."""
+    n, d = inp.shape
+    classes = W.shape[1]
+    t = inp.dtype
+    pi, li = _rows_of(inp, "in", t, n, d)
+    pw, lw = _rows_of(W, "W", t, d, classes)
+    px, lx = _rows_of(grad_in, "grad_in", t, n, d)
+    pd, ld = (0, classes) if grad_W is None else _rows_of(grad_W, "grad_W", grad_W.dtype, d, classes)
+    args = _XENT_BWD_PACK.pack(n, d, classes, pi, li, pw, lw, _floats_of(bias, "bias", classes), _labels_of(labels, n), _floats_of(lse, "lse", n),
+                               _floats_of(grad_loss, "grad_loss", n), _floats_of(mean, "mean", 2), px, lx, pd, ld, _floats_of(grad_bias, "grad_bias", classes),
+                               scale, _dt8(inp), HETA_F32 if grad_W is None else _dt8(grad_W))
+    _check(load_library().heta_linear_xent_bwd(g.handle, args, _stream(stream)))
+
+
+def heta_adamw_state(W: torch.Tensor, bits: int = 32):
+    """The states of a tensor [rows, d] (or [d]) before heta_adamw_multi's first step: (m, v) in fp32, or for bits = 8 (m, m_scale, r, r_scale), r = sqrt(v)."""
+    if bits not in (8, 32):
+        raise ValueError("states have 8 or 32 bits")
+    if bits == 32:
+        return tuple(torch.zeros(W.shape, dtype=torch.float32, device=W.device) for _ in range(2))
+    rows, d = W.shape if W.dim() == 2 else (1, W.shape[0])
+    codes = lambda: torch.zeros(W.shape, dtype=torch.uint8, device=W.device).view(torch.float8_e4m3fn)  # noqa: E731
+    scales = lambda: torch.zeros((rows, (d + 127) // 128), device=W.device)  # noqa: E731
+    return codes(), scales(), codes(), scales()
+
+
+class AdamwPlan:
+    """The tensors of heta_adamw_multi calls, checked and listed once; holds on to them."""
+
+    def __init__(self, items: Sequence[Sequence]):
+        self.items = list(items)
+        self.packed = b"".join(_adamw_item(*it) for it in self.items)
+
+
+def _adamw_item(W, state, grad, weight_decay=0.0, ids=None, seed=0) -> bytes:
+    as_rows = lambda t: t.unsqueeze(0) if t is not None and t.dim() == 1 else t  # noqa: E731
+    W, grad = as_rows(W), as_rows(grad)
+    pw, lw, rows, d = _mat(W, "W", W.dtype)
+    pg, lg, n, dg = _mat(grad, "grad", grad.dtype)
+    if dg != d:
+        raise HetaError(HETA_ERR_SHAPE, f"grad must be {d} wide, got {dg}")
+    if ids is None and n != rows:
+        raise HetaError(HETA_ERR_SHAPE, f"grad must have {rows} rows without ids, got {n}")
+    pi = 0
+    if ids is not None:
+        pi, got = _vec(ids, "ids", torch.int64)
+        if got != n:
+            raise HetaError(HETA_ERR_SHAPE, f"ids must have {n} elements, got {got}")
+    if len(state) == 2:
+        m, v = as_rows(state[0]), as_rows(state[1])
+        sm = sv = None
+        t, st = torch.float32, HETA_F32
+    else:
+        m, sm, v, sv = (as_rows(x) for x in state)
+        t, st = torch.float8_e4m3fn, HETA_E4M3
+    pm, lm = _rows_of(m, "m", t, rows, d)
+    pv, lv = _rows_of(v, "v", t, rows, d)
+    if lm != lv:
+        raise HetaError(HETA_ERR_SHAPE, "m and v must have one leading dimension")
+    blocks = (d + 127) // 128
+    ps, ls = _rows_of(sm, "m_scale", torch.float32, rows, blocks)
+    pr, lr = _rows_of(sv, "v_scale", torch.float32, rows, blocks)
+    if ls != lr:
+        raise HetaError(HETA_ERR_SHAPE, "the scales of m and v must have one leading dimension")
+    return _ADAMW_PACK.pack(pw, lw, pg, lg, pm, pv, lm, ps, pr, ls, pi, n, rows, d, _dt8(W), _dt8(grad), st, weight_decay, int(seed) & 0xffffffff)
+
+
+def heta_adamw_plan(items: Sequence[Sequence]) -> AdamwPlan:
+    """items[i] = (W, state, grad[, weight_decay[, ids[, seed]]]): W and grad fp32 or bf16, [rows, d] (or [d]); state: heta_adamw_state's; ids: the rows of W that
+    grad's belong to (distinct), or None; seed: of its own for each tensor with 8-bit states."""
+    return AdamwPlan(items)
+
+
+def heta_adamw_multi(items, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 1, stream=None) -> None:
+    """One AdamW step (step = 1, 2, ...) on several tensors, in place; items: a heta_adamw_plan, or what makes one."""
+    plan = items if isinstance(items, AdamwPlan) else AdamwPlan(items)
+    _check(load_library().heta_adamw_multi(len(plan.items), plan.packed, lr, beta1, beta2, eps, int(step), _stream(stream)))
 
 
 def heta_muon_multi(g: Graph, items: Sequence[Sequence], lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,

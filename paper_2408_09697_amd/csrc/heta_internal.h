@@ -155,6 +155,7 @@ struct heta_graph {
     // attention aggregation; grown on demand
     void *d_attn = nullptr;
     size_t attn_bytes = 0;
+    uint32_t xent_calls = 0; // heta_linear_xent_bwd's calls: each has a number of its own
 };
 
 namespace heta {

@@ -7,7 +7,7 @@
 //
 // All three products are the tile kernel of heta_tiles.h: bf16 operands straight into LDS; e4m3 operands too, widened to
 // bf16 behind LDS or, where the caller allows coarser sums, on the 8-bit matrix instruction at twice the rate (block scales 1;
-// the scales of rows and columns come in the epilogue); fp32 operands as three bf16 terms.  grad_W is split over the rows (long
+// the scales of rows and columns come in the epilogue); 8-bit integers on the integer instruction; fp32 operands as three bf16 terms.  grad_W is split over the rows (long
 // unaligned bf16 operands of it are copied to aligned rows first); the partial products are added in a fixed order.
 #include <algorithm>
 
@@ -20,7 +20,7 @@ namespace heta {
 // sixteen loads in flight: with eight, and 32 chains for 256 columns of 2,048 partials, the sum took 36 us of a norm's 340.  Four columns
 // come by one load at whatever place they start (a width that is no multiple of four shifts them from partial to partial).
 typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
-template <int CH, typename O> __global__ void __launch_bounds__(256) fold_partials_kernel(const float *part, int64_t n_part, int64_t total, O *out, int32_t width, int64_t ld)
+template <int CH, typename O> __global__ void __launch_bounds__(256) fold_partials_kernel(const float *part, int64_t n_part, int64_t total, O *out, int32_t width, int64_t ld, const float *factor)
 {
     constexpr int G = 256 / CH;
     __shared__ float sums[CH][G][4];
@@ -68,6 +68,11 @@ template <int CH, typename O> __global__ void __launch_bounds__(256) fold_partia
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[e] += sums[i][gq][e];
     }
+    if (factor) {
+        const float f = *factor;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] *= f;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (e < valid) {
@@ -77,24 +82,24 @@ template <int CH, typename O> __global__ void __launch_bounds__(256) fold_partia
         }
 }
 
-template <typename O> static void fold_launch(const float *part, int64_t n_part, int64_t total, O *out, int32_t width, int64_t ld, hipStream_t st)
+template <typename O> static void fold_launch(const float *part, int64_t n_part, int64_t total, O *out, int32_t width, int64_t ld, hipStream_t st, const float *factor)
 {
     const int64_t groups = (total + 3) / 4;
     // few columns: the chains are what keeps loads in flight
     if (groups < 2048 && n_part >= 64)
-        hipLaunchKernelGGL((fold_partials_kernel<128, O>), dim3((unsigned)((groups + 1) / 2)), dim3(256), 0, st, part, n_part, total, out, width, ld);
+        hipLaunchKernelGGL((fold_partials_kernel<128, O>), dim3((unsigned)((groups + 1) / 2)), dim3(256), 0, st, part, n_part, total, out, width, ld, factor);
     else if (groups < 16384 && n_part >= 16)
-        hipLaunchKernelGGL((fold_partials_kernel<16, O>), dim3((unsigned)((groups + 15) / 16)), dim3(256), 0, st, part, n_part, total, out, width, ld);
+        hipLaunchKernelGGL((fold_partials_kernel<16, O>), dim3((unsigned)((groups + 15) / 16)), dim3(256), 0, st, part, n_part, total, out, width, ld, factor);
     else
-        hipLaunchKernelGGL((fold_partials_kernel<4, O>), dim3((unsigned)((groups + 63) / 64)), dim3(256), 0, st, part, n_part, total, out, width, ld);
+        hipLaunchKernelGGL((fold_partials_kernel<4, O>), dim3((unsigned)((groups + 63) / 64)), dim3(256), 0, st, part, n_part, total, out, width, ld, factor);
 }
 
-heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void *out, heta_dtype out_dt, int32_t width, int64_t ld, hipStream_t st)
+heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void *out, heta_dtype out_dt, int32_t width, int64_t ld, hipStream_t st, const float *factor)
 {
     if (total > kFoldMost) return fail(HETA_ERR_UNSUPPORTED, "sum of partials: too many columns for one launch");
     ProfScope prof("fold_partials_kernel", st, static_cast<double>(total) * (4.0 * n_part + dtype_size(out_dt)), static_cast<double>(total) * n_part);
-    if (out_dt == HETA_F32) fold_launch(part, n_part, total, static_cast<float *>(out), width, ld, st);
-    else fold_launch(part, n_part, total, static_cast<bf16_t *>(out), width, ld, st);
+    if (out_dt == HETA_F32) fold_launch(part, n_part, total, static_cast<float *>(out), width, ld, st, factor);
+    else fold_launch(part, n_part, total, static_cast<bf16_t *>(out), width, ld, st, factor);
     HETA_LAUNCH_CHECK("fold_partials_kernel");
     return HETA_OK;
 }
@@ -183,7 +188,7 @@ extern "C" heta_status heta_linear(heta_graph *g, const heta_linear_args *a, voi
     if (a->n_rows < 0 || a->d_in <= 0 || a->d_out <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and widths > 0", who);
     if (std::max(a->d_in, a->d_out) > kWidest) return fail(HETA_ERR_UNSUPPORTED, "%s: rows too wide", who);
     if (!valid_act(a->act)) return fail(HETA_ERR_INVALID_ARG, "%s: bad act", who);
-    const bool q = a->in_dt == HETA_E4M3;
+    const bool whole = a->in_dt == HETA_I8, q = a->in_dt == HETA_E4M3 || whole;
     if (!q && !valid_dtype(a->in_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
     if (!valid_dtype(a->out_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: outputs are fp32 or bf16", who);
     if (a->w_dt != a->in_dt || (a->in_dt == HETA_F32 && a->out_dt != HETA_F32))
@@ -191,7 +196,8 @@ extern "C" heta_status heta_linear(heta_graph *g, const heta_linear_args *a, voi
     // no rows, no scales of theirs: an empty array's address may be null
     if ((q ? !a->in_scale && a->n_rows > 0 : a->in_scale != nullptr) || q != (a->w_scale != nullptr))
         return fail(HETA_ERR_INVALID_ARG, "%s: scales belong to 8-bit operands, and those need them", who);
-    if (!q && a->coarse_sums) return fail(HETA_ERR_INVALID_ARG, "%s: coarse sums are those of 8-bit operands", who);
+    if ((!q || whole) && a->coarse_sums) return fail(HETA_ERR_INVALID_ARG, "%s: coarse sums are those of HETA_E4M3 operands", who);
+    if (whole && a->d_in >= 1 << 17) return fail(HETA_ERR_UNSUPPORTED, "%s: 2^17 products of 8-bit integers and more may pass 32 bits", who);
     const size_t esz = q ? 1 : dtype_size(a->in_dt), osz = dtype_size(a->out_dt);
     HETA_TRY(check_rows(who, "in", a->in, a->n_rows, a->ld_in, a->d_in, esz));
     HETA_TRY(check_rows(who, "W", a->W, 1, a->ld_w, q ? a->d_in : a->d_out, esz));
@@ -213,6 +219,7 @@ extern "C" heta_status heta_linear(heta_graph *g, const heta_linear_args *a, voi
     const double bytes = static_cast<double>(a->n_rows) * (a->d_in * esz + a->d_out * osz * (1.0 + !!a->residual + !!a->pre)) + static_cast<double>(a->d_in) * a->d_out * esz;
     const Launch l{g, who, "linear_kernel", TileItem{a->in, a->W, a->ld_in, a->ld_w, 0, 0, a->n_rows, a->d_out, a->d_in, a->d_in, 1, 0, 0, 0, 0, 0}, bytes,
                    2.0 * a->n_rows * a->d_in * a->d_out, as_stream(hip_stream)};
+    if (whole) return launch_linear_i8(l, a->out_dt, x);
     if (q) return launch_linear_e4m3(l, a->out_dt, a->coarse_sums != 0, x);
     return a->in_dt == HETA_F32 ? launch_linear_f32(l, false, x) : launch_linear_bf16(l, false, a->out_dt, x);
 }

@@ -1,0 +1,155 @@
+// heta_linear on rows and weights of 8-bit whole numbers, and how both are made.
+//
+//     q_ij = round(127 x_ij / max_j |x_ij|), scale_i = max_j |x_ij| / 127      (rows; weights: the columns of W)
+//     pre_ij = scale_i w_scale_j sum_k q_ik p_jk + bias_j
+//
+// The integer matrix instruction adds exactly and takes 32 k-values in the time of 16 in bf16: the products are those of the e4m3 kernels with coarse
+// sums in rate, and of those with exact ones in their sums.
+#include "heta_linear.h"
+
+namespace heta {
+
+template <int WM, int WN, int MI, int NJ, int LOAD, int ST, int OCC> using Shape = TileShape<uint8_t, 1, 1, false, false, LOAD, WM, WN, MI, NJ, 128, ST, OCC, false, true>;
+using Large = Shape<2, 4, 4, 2, kDirect, 2, 1>;       // 256 x 256
+using Half = Shape<4, 2, 2, 2, kDirect, 2, 1>;        // 256 x 128: for epilogues that read or take any width
+using Small = Shape<2, 2, 1, 1, kDirect, 3, 2>;       // 64 x 64
+using StagedLarge = Shape<4, 2, 2, 2, kStaged, 2, 1>; // 256 x 128
+using StagedSmall = Shape<2, 2, 1, 1, kStaged, 2, 2>; // 64 x 64
+
+heta_status launch_linear_i8(const Launch &l, heta_dtype out_dt, const LinearExtra &x)
+{
+    if (out_dt == HETA_F32) return launch_linear<Large, Half, Half, Small, StagedLarge, StagedSmall, float, false>(l, 1, x);
+    return launch_linear<Large, Half, Half, Small, StagedLarge, StagedSmall, bf16_t, false>(l, 1, x);
+}
+
+// ---- rows ----------------------------------------------------------------------------------------------
+// A row lies in the registers of 8 to 64 lanes, eight consecutive columns a lane and chunk; longer ones are walked twice by a workgroup.
+template <typename T, int LANES, int NV> __global__ void __launch_bounds__(256) rows_i8_kernel(const T *x, int64_t ld_x, int64_t n_rows, int32_t d, int8_t *out, int64_t ld_out, float *scale)
+{
+    constexpr int GROUPS = 256 / LANES;
+    const int l = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * GROUPS + grp; r < n_rows; r += static_cast<int64_t>(gridDim.x) * GROUPS) {
+        float v[NV][8];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) load8(x + r * ld_x + (i * LANES + l) * 8, d - (i * LANES + l) * 8, v[i]);
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[i][e]));
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o)));
+        const float amax = __uint_as_float(top), f = i8_factor(amax);
+        if (l == 0) scale[r] = i8_scale(amax);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * LANES + l) * 8;
+            store_codes(reinterpret_cast<uint8_t *>(out) + r * ld_out + c, d - c,
+                        Codes8{{four_i8(v[i][0] * f, v[i][1] * f, v[i][2] * f, v[i][3] * f), four_i8(v[i][4] * f, v[i][5] * f, v[i][6] * f, v[i][7] * f)}});
+        }
+    }
+}
+template <typename T> __global__ void __launch_bounds__(256) rows_i8_wide_kernel(const T *x, int64_t ld_x, int64_t n_rows, int32_t d, int8_t *out, int64_t ld_out, float *scale)
+{
+    __shared__ uint32_t tops[4];
+    for (int64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
+        const T *row = x + r * ld_x;
+        uint32_t top = 0;
+        for (int c = threadIdx.x * 8; c < d; c += 2048) {
+            float v[8];
+            load8(row + c, d - c, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o)));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+        __syncthreads();
+        const float amax = __uint_as_float(max(max(tops[0], tops[1]), max(tops[2], tops[3]))), f = i8_factor(amax);
+        if (threadIdx.x == 0) scale[r] = i8_scale(amax);
+        for (int c = threadIdx.x * 8; c < d; c += 2048) {
+            float v[8];
+            load8(row + c, d - c, v);
+            store_codes(reinterpret_cast<uint8_t *>(out) + r * ld_out + c, d - c, Codes8{{four_i8(v[0] * f, v[1] * f, v[2] * f, v[3] * f), four_i8(v[4] * f, v[5] * f, v[6] * f, v[7] * f)}});
+        }
+    }
+}
+
+// ---- weights -------------------------------------------------------------------------------------------
+// Column j of W [d_in, d_out] becomes row j of the packed matrix.  Once per set of weights: one wavefront per column.
+template <typename T> __global__ void __launch_bounds__(256) pack_i8_kernel(const T *W, int64_t ld_w, int32_t d_in, int32_t d_out, int8_t *out, int64_t ld_out, float *scale)
+{
+    const int64_t j = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (j >= d_out) return;
+    uint32_t top = 0;
+    for (int k = lane; k < d_in; k += 64) top = max(top, magnitude(widen(W[k * ld_w + j])));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o)));
+    const float amax = __uint_as_float(top), f = i8_factor(amax);
+    for (int k = lane; k < d_in; k += 64) out[j * ld_out + k] = static_cast<int8_t>(one_i8(widen(W[k * ld_w + j]) * f));
+    if (lane == 0) scale[j] = i8_scale(amax);
+}
+
+template <typename T> static void launch_rows(const T *x, int64_t ld_x, int64_t n, int32_t d, int8_t *out, int64_t ld_out, float *scale, hipStream_t st)
+{
+    auto go = [&](auto lanes, auto nv) {
+        constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
+        const int64_t blocks = (n + 256 / L - 1) / (256 / L);
+        hipLaunchKernelGGL((rows_i8_kernel<T, L, NV>), dim3(static_cast<unsigned>(std::min<int64_t>(blocks, 1 << 20))), dim3(256), 0, st, x, ld_x, n, d, out, ld_out, scale);
+    };
+    using std::integral_constant;
+    if (d <= 64) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    else if (d <= 128) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (d <= 256) go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    else if (d <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (d <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    else if (d <= 2048) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else hipLaunchKernelGGL(rows_i8_wide_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(n, 1 << 20))), dim3(256), 0, st, x, ld_x, n, d, out, ld_out, scale);
+}
+
+} // namespace heta
+
+using namespace heta;
+
+extern "C" heta_status heta_linear_rows_i8(int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, void *out, int64_t ld_out, float *scale, void *hip_stream)
+{
+    const char *who = "heta_linear_rows_i8";
+    if (n_rows < 0 || d <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and d > 0", who);
+    if (d > kWidest) return fail(HETA_ERR_UNSUPPORTED, "%s: rows too wide", who);
+    if (!valid_dtype(x_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    HETA_TRY(check_rows(who, "x", x, n_rows, ld_x, d, dtype_size(x_dt)));
+    HETA_TRY(check_rows(who, "out", out, n_rows, ld_out, d, 1));
+    if ((!scale && n_rows > 0) || (reinterpret_cast<uintptr_t>(scale) & 3u)) return fail(HETA_ERR_INVALID_ARG, "%s: bad scale", who);
+    const RowRange rx(x, n_rows, ld_x, d, dtype_size(x_dt)), ro(out, n_rows, ld_out, d, 1), rs(scale, 1, n_rows, n_rows, 4);
+    if (ro.overlaps(rx) || rs.overlaps(rx) || rs.overlaps(ro)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);
+    if (n_rows == 0) return HETA_OK;
+    hipStream_t st = as_stream(hip_stream);
+    ProfScope prof("rows_i8_kernel", st, static_cast<double>(n_rows) * (d * (dtype_size(x_dt) + 1.0) + 4), 0);
+    if (x_dt == HETA_F32) launch_rows(static_cast<const float *>(x), ld_x, n_rows, d, static_cast<int8_t *>(out), ld_out, scale, st);
+    else launch_rows(static_cast<const bf16_t *>(x), ld_x, n_rows, d, static_cast<int8_t *>(out), ld_out, scale, st);
+    HETA_LAUNCH_CHECK("rows_i8_kernel");
+    return HETA_OK;
+}
+
+extern "C" heta_status heta_linear_pack_i8(const void *W, heta_dtype w_dt, int64_t ld_w, int32_t d_in, int32_t d_out, void *packed, int64_t ld_packed, float *scale, void *hip_stream)
+{
+    const char *who = "heta_linear_pack_i8";
+    if (!valid_dtype(w_dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (d_in <= 0 || d_out <= 0) return fail(HETA_ERR_SHAPE, "%s: need widths > 0", who);
+    if (std::max(d_in, d_out) > kWidest) return fail(HETA_ERR_UNSUPPORTED, "%s: rows too wide", who);
+    HETA_TRY(check_rows(who, "W", W, 1, ld_w, d_out, dtype_size(w_dt)));
+    HETA_TRY(check_rows(who, "packed", packed, 1, ld_packed, d_in, 1));
+    if (!scale || (reinterpret_cast<uintptr_t>(scale) & 3u)) return fail(HETA_ERR_INVALID_ARG, "%s: bad scale", who);
+    const RowRange w(W, d_in, ld_w, d_out, dtype_size(w_dt)), o(packed, d_out, ld_packed, d_in, 1), s(scale, 1, d_out, d_out, 4);
+    if (o.overlaps(w) || s.overlaps(w) || s.overlaps(o)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);
+    hipStream_t st = as_stream(hip_stream);
+    ProfScope prof("pack_i8_kernel", st, static_cast<double>(d_in) * d_out * (2.0 * dtype_size(w_dt) + 1.0), 0);
+    if (w_dt == HETA_F32)
+        hipLaunchKernelGGL(pack_i8_kernel<float>, dim3((d_out + 3) / 4), dim3(256), 0, st, static_cast<const float *>(W), ld_w, d_in, d_out, static_cast<int8_t *>(packed), ld_packed, scale);
+    else
+        hipLaunchKernelGGL(pack_i8_kernel<bf16_t>, dim3((d_out + 3) / 4), dim3(256), 0, st, static_cast<const bf16_t *>(W), ld_w, d_in, d_out, static_cast<int8_t *>(packed), ld_packed, scale);
+    HETA_LAUNCH_CHECK("pack_i8_kernel");
+    return HETA_OK;
+}

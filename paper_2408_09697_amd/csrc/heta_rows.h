@@ -132,6 +132,42 @@ constexpr float kE4m3Least = 1.504632769052528e-36f; // 2^-119
 __device__ __forceinline__ float e4m3_factor(float amax) { return amax >= kE4m3Least ? 448.f / amax : amax != amax ? amax : 0.f; }
 __device__ __forceinline__ float e4m3_scale(float amax) { return amax < kE4m3Least ? 0.f : amax / 448.f; }
 
+// Whole numbers of 8 bits: the largest magnitude of a row (or column) is 127.  As above below 2^-119; a row with a NaN has a NaN scale (and zeros), one with an
+// infinity the scale infinity (and zeros): its products are NaN.
+__device__ __forceinline__ float i8_factor(float amax) { return amax >= kE4m3Least ? 1.f / amax * 127.f : 0.f; }
+__device__ __forceinline__ float i8_scale(float amax) { return amax < kE4m3Least ? 0.f : amax * (1.f / 127.f); }
+// |y| <= 127 (or NaN: 0), nearest, ties to even
+__device__ __forceinline__ uint32_t one_i8(float y) { return static_cast<uint32_t>(static_cast<int>(rintf(y))) & 0xffu; }
+__device__ __forceinline__ uint32_t four_i8(float a, float b, float c, float d) { return one_i8(a) | one_i8(b) << 8 | one_i8(c) << 16 | one_i8(d) << 24; }
+
+// eight 8-bit values, `valid` of which exist
+typedef uint32_t uintx2_any __attribute__((ext_vector_type(2), aligned(1)));
+struct Codes8 {
+    uint32_t w[2];
+};
+__device__ __forceinline__ Codes8 load_codes(const uint8_t *p, int valid)
+{
+    Codes8 q{{0u, 0u}};
+    if (valid >= 8) {
+        const uintx2_any v = *reinterpret_cast<const uintx2_any *>(p);
+        return Codes8{{v[0], v[1]}};
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < valid) q.w[e / 4] |= static_cast<uint32_t>(p[e]) << (8 * (e & 3));
+    return q;
+}
+__device__ __forceinline__ void store_codes(uint8_t *p, int valid, const Codes8 &q)
+{
+    if (valid >= 8) {
+        *reinterpret_cast<uintx2_any *>(p) = uintx2_any{q.w[0], q.w[1]};
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < valid) p[e] = static_cast<uint8_t>(q.w[e / 4] >> (8 * (e & 3)));
+}
+
 // Argument checks of the calls on such rows (host).  Widths stay a little below 2^31: kernels count columns in 32 bits, a workgroup's at a time.
 constexpr int32_t kWidest = INT32_MAX - 1023;
 inline heta_status check_rows(const char *who, const char *what, const void *p, int64_t n_rows, int64_t ld, int64_t d, size_t elt)
@@ -149,6 +185,7 @@ inline bool streams(double bytes) { return bytes > 256e6; }
 // out[c] (or, for rows of `width`, out[(c / width) * ld + c % width]) = sum over s < n_part of part[s * total + c], c < total,
 // in a fixed order; out is fp32 or bf16.  Deterministic second half of sums over rows that many workgroups share.
 constexpr int64_t kFoldMost = int64_t(256) * (max_blocks(256) - 1); // columns
-heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void *out, heta_dtype out_dt, int32_t width, int64_t ld, hipStream_t st);
+// factor: device, multiplies the sums (NULL: 1).
+heta_status fold_partials(const float *part, int64_t n_part, int64_t total, void *out, heta_dtype out_dt, int32_t width, int64_t ld, hipStream_t st, const float *factor = nullptr);
 
 } // namespace heta

@@ -29,7 +29,9 @@ namespace heta {
 
 enum TileLoad { kDirect = 0, kStaged = 1 };
 
+typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef int intx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4_tr __attribute__((ext_vector_type(4)));
 
 // ---- LDS image of one operand tile ------------------------------------------------------------------
@@ -233,7 +235,7 @@ template <typename S, bool RC, int ROWS, int BK, int EB, int NT, int T> struct S
 };
 
 // ---- LDS -> fragments -------------------------------------------------------------------------------
-union Frag16 { uint4 u; bf16x8 v; };
+union Frag16 { uint4 u; bf16x8 v; intx4 i; };
 union Frag8 { uint4 u[2]; intx8 v; };
 
 // the eight k-values kk + 8 * (lane / 32) + 0..7 of row r + lane % 32 (r and kk multiples of 32 and 16)
@@ -274,8 +276,8 @@ __device__ __forceinline__ bf16x8 widen_e4m3(uint32_t lo, uint32_t hi)
     return f.v;
 }
 
-template <int EB, int T, int MI, int NJ> struct Fragments { // of one step
-    using F = std::conditional_t<EB == 1, Frag8, Frag16>;
+template <int EB, int T, int MI, int NJ, bool INT> struct Fragments { // of one step
+    using F = std::conditional_t<EB == 1 && !INT, Frag8, Frag16>;
     F a[MI][T], b[NJ][T];
 };
 
@@ -346,6 +348,10 @@ struct TilePlace {
 //     results, t being W elements of x.other (if kReads; zeros or nothing where it is null); x.pre (if kPre and not null) and
 //     out(x, it, split) receive them, rows x.ld_pre and x.ld_out apart; kWhole: N is a multiple of W.  struct Cols, Row { void
 //     load(const Extra &x, int64_t n, int64_t N); } are what a lane keeps of W columns and of a row (which may lie beyond the matrix).
+//   Instead, kTile = true: tile<C>(x, it, acc, strip, place, wave, lane) takes a wavefront's sums as they lie in the registers, and choose(x, it) may
+//     change the item's addresses by what is in memory when the kernel runs.
+template <typename Epi, typename = void> struct takes_tile : std::false_type {};
+template <typename Epi> struct takes_tile<Epi, std::enable_if_t<Epi::kTile>> : std::true_type {};
 template <typename Epi> struct TileArgs {
     int n_items;
     uint32_t stride; // one item: from one tile of a workgroup to its next; several: tiles of an XCD
@@ -359,10 +365,13 @@ template <typename Epi> struct TileArgs {
 // their way from LDS to the bf16 matrix instruction, whose sums are exact to fp32; the 8-bit instruction takes half the time,
 // but aligns its products to the largest with about 14 bits below (sums of 1,024 products of random values: 1.5e-5 off
 // relative to the result, against 2e-7).
-template <typename S_, int EB_, int T_, bool A_RC_, bool B_RC_, int LOAD_, int WM_, int WN_, int MI_, int NJ_, int BK_, int ST_, int OCC_, bool WIDEN_ = false> struct TileShape {
+// INT: the 8-bit values are whole numbers, their products are added as 32-bit integers, at the 8-bit rate and exactly (|sum| < 2^31: fewer than 2^17
+// products), and rounded to fp32 in front of the epilogue.
+template <typename S_, int EB_, int T_, bool A_RC_, bool B_RC_, int LOAD_, int WM_, int WN_, int MI_, int NJ_, int BK_, int ST_, int OCC_, bool WIDEN_ = false, bool INT_ = false> struct TileShape {
     using S = S_;
     static constexpr int EB = EB_, T = T_, LOAD = LOAD_, WM = WM_, WN = WN_, MI = MI_, NJ = NJ_, BK = BK_, ST = LOAD_ == kDirect ? ST_ : 2, OCC = OCC_;
-    static constexpr bool A_RC = A_RC_, B_RC = B_RC_, WIDEN = WIDEN_;
+    static constexpr bool A_RC = A_RC_, B_RC = B_RC_, WIDEN = WIDEN_, INT = INT_;
+    using Sum = std::conditional_t<INT_, intx16, floatx16>;
     static constexpr int NW = WM * WN, NT = 64 * NW, BM = 32 * MI * WM, BN = 32 * NJ * WN;
 };
 
@@ -399,8 +408,9 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
         now.at = blockIdx.x;
         if (!now.seek(p.item[0], p.stride, BM, BN)) return;
     }
-    const TileItem it = p.item[c];
+    TileItem it = p.item[c];
     const typename Epi::Extra extra = p.extra[c];
+    if constexpr (takes_tile<Epi>::value) Epi::choose(extra, it);
 
     auto further = [&](TilePlace &t) { // the workgroup's next tile
         if constexpr (Epi::kItems > 1) return false;
@@ -408,25 +418,32 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
         return t.seek(it, p.stride, BM, BN);
     };
 
-    floatx16 acc[MI][NJ];
+    typename C::Sum acc[MI][NJ];
     auto clear = [&] {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int jj = 0; jj < NJ; ++jj)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][jj][v] = 0.f;
+                for (int v = 0; v < 16; ++v) acc[i][jj][v] = 0;
     };
+    auto four = [&](int i, int jj, int q) { return make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]); };
 
     // One k-tile.  The fragments of a step are read before the products of the step in front of it, and scheduling barriers
     // keep them there: left to itself the compiler reads a fragment just before its first product, and every step waits for LDS.
     auto compute = [&](const char *stage) {
         const char *At = stage, *Bt = stage + A_STAGE;
-        constexpr int KS = EB == 1 ? 64 : 16, STEPS = BK / KS;
-        constexpr int SETS = EB == 1 ? 1 : 2; // two sets of 8-bit fragments do not fit beside the accumulators
-        Fragments<EB, T, MI, NJ> f[SETS];
-        auto read = [&](Fragments<EB, T, MI, NJ> &to, int kk) {
-            if constexpr (EB == 1) {
+        constexpr int KS = C::INT ? 32 : EB == 1 ? 64 : 16, STEPS = BK / KS;
+        constexpr int SETS = EB == 1 && !C::INT ? 1 : 2; // two sets of 8-bit fragments of 64 k-values do not fit beside the accumulators
+        using Step = Fragments<EB, T, MI, NJ, C::INT>;
+        Step f[SETS];
+        auto read = [&](Step &to, int kk) {
+            if constexpr (C::INT) {
+#pragma unroll
+                for (int jj = 0; jj < NJ; ++jj) to.b[jj][0].u = tile_chunk8<BN, BK>(Bt, wn + 32 * jj, kk, lane);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) to.a[i][0].u = tile_chunk8<BM, BK>(At, wm + 32 * i, kk, lane);
+            } else if constexpr (EB == 1) {
                 // which 32 (or 8) of the k-values a lane feeds to an instruction does not matter as long as both operands agree
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -445,8 +462,13 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
                 }
             }
         };
-        auto multiply = [&](const Fragments<EB, T, MI, NJ> &x) {
-            if constexpr (EB == 1 && C::WIDEN) {
+        auto multiply = [&](const Step &x) {
+            if constexpr (C::INT) {
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int jj = 0; jj < NJ; ++jj) acc[i][jj] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x.b[jj][0].i, x.a[i][0].i, acc[i][jj], 0, 0, 0);
+            } else if constexpr (EB == 1 && C::WIDEN) {
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
                     bf16x8 wb[NJ];
@@ -498,7 +520,9 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
 
     // register 4 q + e of block (i, jj) is column 8 q + 4 (lane / 32) + e of row lane % 32
     auto epilogue = [&] {
-        if constexpr (Epi::kBlocks) {
+        if constexpr (takes_tile<Epi>::value) {
+            Epi::template tile<C>(extra, it, acc, reinterpret_cast<float *>(ring + STRIPS_AT + wave * 4096), now, wave, lane);
+        } else if constexpr (Epi::kBlocks) {
             const int half = lane >> 5, l32 = lane & 31;
             float *strip = reinterpret_cast<float *>(ring + STRIPS_AT + wave * 4096);
 #pragma unroll
@@ -507,7 +531,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
                 for (int jj = 0; jj < NJ; ++jj) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
+                        *strip_at(strip, l32, 2 * q + half) = four(i, jj, q);
                     Epi::block(extra, it, strip, now.m0 + wm + 32 * i, now.n0 + wn + 32 * jj, now.m0 != now.n0, lane);
                 }
         } else {
@@ -561,7 +585,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
                     const int64_t n = rn + 32 * jj;
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
+                        *strip_at(strip, l32, 2 * q + half) = four(i, jj, q);
 #pragma unroll
                     for (int r = 0; r < ROUNDS; ++r) {
                         const int64_t m = rm + 32 * i + RPP * r;

@@ -1,0 +1,700 @@
+// Softmax cross entropy of rows through an output product, and its gradients, without the logits in memory.
+//
+//     z = in . W + bias,  lse_i = log sum_j exp z_ij,  loss_i = lse_i - z_i,label(i)   (0 for a row without a label)
+//     D_ij = g_i (exp(z_ij - lse_i) - [j = label(i)]),  grad_in = F D W^T,  grad_W = F in^T D,  grad_bias = F sum_i D_i
+//
+// Forward: the product of heta_tiles.h with an epilogue that leaves, of a row's logits in a wavefront's columns, their largest and the sum of
+// the exponentials below it, 8 bytes for 64 logits; a second kernel joins a row's.  The label's logit is taken from the registers it is in.
+// Backward: the logits are formed again (2 d operations each; kept in 4 bytes they would cost as long to write and read at d = 1,024 and
+// longer below), their epilogue makes D of them, and two products read D.  D is made in pieces that the last-level cache holds:
+// Rows x Classes of about a square, since every further piece along the classes adds n d partial sums of grad_in, and every one along the rows d V of grad_W.
+// D is stored in the operands' type: the matrix instruction reads 16 bits, and its rounding (2^-9 of each D, to and fro) is below that of a gradient
+// in 16 bits.  F, which all rows share (scale, over the number of labelled rows), multiplies the sums: in D, its rounding would be the same for all labels' elements
+// (8,192 x 512 x 131,072: gradients 3.7e-3 of their norm off, 1.7e-3 this way, their own rounding).  grad_bias is added up from the unrounded D in the epilogue's registers.
+// Logits are held in units of log 2, z log2(e), from one fused operation with the bias, so that exponentials are the hardware's 2^x.
+//
+// A row without a label has D = 0 whatever it holds; where it holds NaN or infinities (a padded batch), 0 times those would reach grad_W, which then reads
+// a copy of the rows with zeros in their place.  Such rows have an lse that is not finite, which is how they are found.
+#include <algorithm>
+#include <cmath>
+
+#include "heta_linear.h"
+
+namespace heta {
+
+constexpr float kLn2 = 0.6931471805599453f;
+// In the place of a largest logit of -infinity or infinity: beyond every other, and its difference to any is finite.
+constexpr float kBeyond = 1e30f, kNothing = -kBeyond;
+
+// ---- forward: a tile's logits ----------------------------------------------------------------------------
+struct XentPart {
+    float top, sum; // in units of log 2; sum over j of 2^(z_j - top)
+};
+// top is kept finite; with a logit of +infinity the sum is infinite, whatever it is joined with
+__device__ __forceinline__ float finite_top(float t) { return __builtin_amdgcn_fmed3f(t, kNothing, kBeyond); }
+__device__ __forceinline__ XentPart join(XentPart a, XentPart b)
+{
+    const float t = fmaxf(a.top, b.top);
+    return {t, a.sum * __builtin_amdgcn_exp2f(a.top - t) + b.sum * __builtin_amdgcn_exp2f(b.top - t)};
+}
+
+struct XentForward {
+    const float *bias;     // nullable
+    const int64_t *labels;
+    XentPart *part;        // [strips of columns][n]
+    float *target;         // [n]: the label's logit
+};
+struct XentForwardEpi {
+    static constexpr int kItems = 1;
+    static constexpr bool kTile = true;
+    using Extra = XentForward;
+    __device__ __forceinline__ static void choose(const Extra &, TileItem &) {}
+    template <typename C, typename Acc>
+    __device__ __forceinline__ static void tile(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], float *, const TilePlace &now, int wave, int lane)
+    {
+        constexpr int MI = C::MI, NJ = C::NJ;
+        int here = lane;
+        asm volatile("" : "+v"(here)); // not kept through the products
+        const int half = here >> 5, l32 = here & 31;
+        const int64_t m0 = now.m0 + (wave / C::WN) * (32 * MI) + l32, n0 = now.n0 + (wave % C::WN) * (32 * NJ);
+        if (n0 >= it.N) return;
+        const int n_here = static_cast<int>(min(it.N - n0, static_cast<int64_t>(32 * NJ))); // columns of this strip
+        // columns 32 jj + 8 q + 4 half + e of the strip are a lane's; edge: some are beyond the last class, where acc may hold anything
+        auto strip_part = [&](auto edge) {
+            constexpr bool EDGE = decltype(edge)::value;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int64_t m = m0 + 32 * i, label = x.labels[min(m, it.M - 1)] - n0;
+                const int at = label >= 0 && label < n_here ? static_cast<int>(label) - 4 * half : -64; // the label's column
+                XentPart p;
+#pragma unroll
+                for (int jj = 0; jj < NJ; ++jj) {
+                    __builtin_amdgcn_sched_barrier(0); // one block at a time: the registers hold no more beside the sums
+                    int beyond = n_here - 4 * half - 32 * jj;
+                    asm volatile("" : "+v"(beyond)); // compared here, not once for all rows: that takes two scalar registers a column
+                    float z[16], top = -INFINITY, sum = 0.f;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int c = 32 * jj + 8 * (v / 4) + 4 * half + v % 4;
+                        const float bias = x.bias ? x.bias[n0 + (EDGE ? min(c, n_here - 1) : c)] * kLog2e : 0.f;
+                        z[v] = fmaf(acc[i][jj][v], kLog2e, bias);
+                        if constexpr (EDGE) z[v] = 8 * (v / 4) + v % 4 < beyond ? z[v] : -INFINITY;
+                        top = fmaxf(top, z[v]);
+                    }
+                    top = finite_top(top);
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(z[v] - top);
+                    p = jj == 0 ? XentPart{top, sum} : join(p, {top, sum});
+                    const int c = at - 32 * jj;
+                    if (__any(c >= 0 && c < 32 && (c & 4) == 0)) {
+                        float t = 0.f;
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) t = c == 8 * (v / 4) + v % 4 ? z[v] : t;
+                        if (c >= 0 && c < 32 && (c & 4) == 0 && m < it.M) x.target[m] = t;
+                    }
+                }
+                p = join(p, {__shfl_xor(p.top, 32), __shfl_xor(p.sum, 32)});
+                if (half == 0 && m < it.M) x.part[n0 / (32 * NJ) * it.M + m] = p;
+            }
+        };
+        if (n_here == 32 * NJ) strip_part(std::false_type{});
+        else strip_part(std::true_type{});
+    }
+};
+
+// ---- forward: a row's parts joined -------------------------------------------------------------------------
+// R rows a workgroup, 256 / R threads a row.  sums: of the workgroup's losses, and how many rows have a label; a single workgroup writes the mean at once.
+struct XentSum {
+    double loss, rows;
+};
+__device__ __forceinline__ void mean_of(XentSum s, float *mean)
+{
+    mean[0] = s.rows > 0 ? static_cast<float>(s.loss / s.rows) : 0.f;
+    mean[1] = static_cast<float>(s.rows);
+}
+template <int R> __global__ void __launch_bounds__(256) xent_rows_kernel(const XentPart *part, int64_t strips, const float *target, const int64_t *labels, int64_t n, int64_t n_classes,
+                                                                        float *loss, float *lse, XentSum *sums, float *mean)
+{
+    constexpr int G = 256 / R;
+    __shared__ XentPart parts[G][R];
+    __shared__ XentSum rows[R];
+    const int r = threadIdx.x % R, g = threadIdx.x / R;
+    const int64_t m = static_cast<int64_t>(blockIdx.x) * R + r;
+    XentPart p{kNothing, 0.f};
+    if (m < n) {
+#pragma unroll 4
+        for (int64_t s = g; s < strips; s += G) p = join(p, part[s * n + m]);
+    }
+    parts[g][r] = p;
+    __syncthreads();
+    for (int h = G / 2; h > 0; h /= 2) {
+        if (g < h) parts[g][r] = join(parts[g][r], parts[g + h][r]);
+        __syncthreads();
+    }
+    if (g == 0) {
+        XentSum s{0., 0.};
+        if (m < n) {
+            p = parts[0][r];
+            const float l2 = p.top + __builtin_amdgcn_logf(p.sum);
+            const int64_t label = labels[m];
+            const bool has = label >= 0 && label < n_classes;
+            const float mine = has ? (l2 - target[m]) * kLn2 : 0.f;
+            lse[m] = l2 * kLn2;
+            if (loss) loss[m] = mine;
+            s = {mine, has ? 1. : 0.};
+        }
+        rows[r] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && (sums || mean)) {
+        XentSum s{0., 0.};
+        for (int i = 0; i < R; ++i) s = {s.loss + rows[i].loss, s.rows + rows[i].rows};
+        if (sums) sums[blockIdx.x] = s;
+        else mean_of(s, mean);
+    }
+}
+__global__ void __launch_bounds__(256) xent_mean_kernel(const XentSum *sums, int64_t n, float *mean)
+{
+    __shared__ XentSum all[256];
+    XentSum s{0., 0.};
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < n; i += 256) s = {s.loss + sums[i].loss, s.rows + sums[i].rows};
+    all[threadIdx.x] = s;
+    __syncthreads();
+    for (int h = 128; h > 0; h /= 2) {
+        if (threadIdx.x < static_cast<unsigned>(h)) all[threadIdx.x] = {all[threadIdx.x].loss + all[threadIdx.x + h].loss, all[threadIdx.x].rows + all[threadIdx.x + h].rows};
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) mean_of(all[0], mean);
+}
+
+// ---- backward: what a row's D needs ------------------------------------------------------------------------
+struct XentRow {
+    float lse;  // in units of log 2
+    float f;    // the row's grad_loss; 0: its D is 0
+    int64_t label;
+};
+// call: this call's number.  *poison becomes it where a row without a gradient holds something that 0 does not clear.
+__global__ void __launch_bounds__(256) xent_prepare_kernel(const int64_t *labels, const float *lse, const float *grad_loss, const float *mean, float scale, int64_t n, int64_t n_classes,
+                                                           XentRow *rows, float *factor, uint32_t *poison, uint32_t call)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i == 0) *factor = !mean ? scale : mean[1] > 0.f ? scale / mean[1] : 0.f;
+    if (i >= n) return;
+    const int64_t label = labels[i];
+    const bool has = label >= 0 && label < n_classes;
+    const float f = grad_loss ? grad_loss[i] : 1.f, l = lse[i];
+    rows[i] = {l * kLog2e, has ? f : 0.f, has ? label : -1};
+    if (!(has && f != 0.f) && !(fabsf(l) < INFINITY)) *poison = call; // all that write write the same
+}
+// The rows for grad_W: with zeros in those without a gradient.  Unless always, only where *poison says that there is need.
+template <typename E> __global__ void __launch_bounds__(256) xent_clean_kernel(const E *in, int64_t ld, int64_t n, int32_t d, const XentRow *rows, E *out, int64_t ld_out, bool always,
+                                                                               const uint32_t *poison, uint32_t call)
+{
+    if (!always && *poison != call) return;
+    const int chunks = static_cast<int>(ld_out / 8);
+    const int64_t total = n * chunks;
+    for (int64_t q = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; q < total; q += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t r = q / chunks;
+        const int c = static_cast<int>(q - r * chunks) * 8;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (rows[r].f != 0.f) load8(in + r * ld + c, d - c, v);
+        store8(out + r * ld_out + c, 8, v);
+    }
+}
+
+// ---- backward: a tile of D -----------------------------------------------------------------------------------
+struct XentBackward {
+    const float *bias;   // nullable
+    const XentRow *rows; // of the piece
+    void *D;
+    int64_t ld;
+    float *sums;         // [strips of rows][N]: D's sums over them; nullable
+    int64_t first;       // the piece's first class
+};
+template <typename O> struct XentBackwardEpi {
+    static constexpr int kItems = 1;
+    static constexpr bool kTile = true;
+    using Extra = XentBackward;
+    __device__ __forceinline__ static void choose(const Extra &, TileItem &) {}
+    template <typename C, typename Acc>
+    __device__ __forceinline__ static void tile(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], float *strip, const TilePlace &now, int wave, int lane)
+    {
+        constexpr int MI = C::MI, NJ = C::NJ, W = 16 / (int)sizeof(O), LPR = 32 / W, RPP = 64 / LPR, ROUNDS = 32 / RPP;
+        int here = lane;
+        asm volatile("" : "+v"(here)); // not kept through the products
+        const int sr = here / LPR, sc = here % LPR, half = here >> 5, l32 = here & 31;
+        const int64_t m0 = now.m0 + (wave / C::WN) * (32 * MI) + sr, n0 = now.n0 + (wave % C::WN) * (32 * NJ) + sc * W;
+        float bias[NJ][W], sum[NJ][W];
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj)
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                bias[jj][e] = x.bias ? x.bias[min(n0 + 32 * jj + e, it.N - 1)] * kLog2e : 0.f;
+                sum[jj][e] = 0.f;
+            }
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            XentRow row[ROUNDS];
+#pragma unroll
+            for (int r = 0; r < ROUNDS; ++r) row[r] = x.rows[min(m0 + 32 * i + RPP * r, it.M - 1)];
+#pragma unroll
+            for (int jj = 0; jj < NJ; ++jj) {
+                const int64_t n = n0 + 32 * jj;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
+#pragma unroll
+                for (int r = 0; r < ROUNDS; ++r) {
+                    const int64_t m = m0 + 32 * i + RPP * r;
+                    float y[W];
+#pragma unroll
+                    for (int h = 0; h < W / 4; ++h) {
+                        const float4 f = *strip_at(strip, RPP * r + sr, sc * (W / 4) + h);
+                        y[4 * h] = f.x; y[4 * h + 1] = f.y; y[4 * h + 2] = f.z; y[4 * h + 3] = f.w;
+                    }
+                    const float f = m < it.M ? row[r].f : 0.f;
+                    const int64_t label = row[r].label - x.first - n;
+                    const int at = label >= 0 && label < W ? static_cast<int>(label) : -1; // its column among this lane's
+                    int valid = static_cast<int>(min(max(it.N - n, static_cast<int64_t>(0)), static_cast<int64_t>(W)));
+                    asm volatile("" : "+v"(valid)); // compared here, not once for all rows: that takes two scalar registers a column
+#pragma unroll
+                    for (int e = 0; e < W; ++e) {
+                        float p = __builtin_amdgcn_exp2f(fmaf(y[e], kLog2e, bias[jj][e]) - row[r].lse);
+                        if (at == e) p -= 1.f;
+                        y[e] = f != 0.f && e < valid ? p * f : 0.f;
+                        sum[jj][e] += y[e];
+                    }
+                    // D's rows are padded to whole pieces; what lies behind the classes is zero
+                    if (m < it.M && n < x.ld) store16(static_cast<O *>(x.D) + m * x.ld + n, pack16<O>(y));
+                }
+            }
+        }
+        if (!x.sums || now.m0 + (wave / C::WN) * (32 * MI) >= it.M) return;
+        const int64_t slot = now.m0 / (32 * MI) + wave / C::WN;
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj)
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                float s = sum[jj][e];
+#pragma unroll
+                for (int o = LPR; o < 64; o <<= 1) s += __shfl_xor(s, o);
+                if (sr == 0 && n0 + 32 * jj + e < it.N) x.sums[slot * it.N + n0 + 32 * jj + e] = s;
+            }
+    }
+};
+
+// grad_W's partial products, the rows read from their clean copy where there is need of it
+struct XentWeights {
+    float *part;
+    int64_t ld_out;
+    const void *clean; // nullable
+    int64_t ld_clean;
+    const uint32_t *poison;
+    uint32_t call;
+};
+struct XentWeightsEpi {
+    static constexpr int kItems = 1;
+    static constexpr bool kTile = true;
+    using Extra = XentWeights;
+    __device__ __forceinline__ static void choose(const Extra &x, TileItem &it)
+    {
+        if (*x.poison != x.call) return;
+        it.A = x.clean;
+        it.lda = x.ld_clean;
+    }
+    template <typename C, typename Acc>
+    __device__ __forceinline__ static void tile(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], float *strip, const TilePlace &now, int wave, int lane)
+    {
+        constexpr int MI = C::MI, NJ = C::NJ;
+        int here = lane;
+        asm volatile("" : "+v"(here));
+        const int sr = here / 8, sc = here % 8, half = here >> 5, l32 = here & 31;
+        const int64_t m0 = now.m0 + (wave / C::WN) * (32 * MI) + sr, n0 = now.n0 + (wave % C::WN) * (32 * NJ) + sc * 4;
+        float *out = x.part + now.split * it.M * it.N;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int jj = 0; jj < NJ; ++jj) {
+                const int64_t n = n0 + 32 * jj;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t m = m0 + 32 * i + 8 * r;
+                    const float4 f = *strip_at(strip, 8 * r + sr, sc);
+                    if (m < it.M && n < it.N)
+                        store_piece(out + m * it.N + n, static_cast<int>(min(it.N - n, static_cast<int64_t>(4))),
+                                    uintx4{__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(f.z), __float_as_uint(f.w)});
+                }
+            }
+    }
+};
+
+// ---- host side ---------------------------------------------------------------------------------------------
+template <typename E, bool A_RC, bool B_RC, bool LARGE, bool STAGED> struct XentShape;
+template <bool A_RC, bool B_RC> struct XentShape<bf16_t, A_RC, B_RC, true, false> { using type = TileShape<bf16_t, 2, 1, A_RC, B_RC, kDirect, 2, 4, 4, 2, 64, 2, 1>; };   // 256 x 256
+template <> struct XentShape<bf16_t, false, true, true, false> { using type = TileShape<bf16_t, 2, 1, false, true, kDirect, 4, 2, 2, 2, 64, 2, 1>; };                     // 256 x 128: the logits'
+template <bool A_RC, bool B_RC> struct XentShape<bf16_t, A_RC, B_RC, false, false> { using type = TileShape<bf16_t, 2, 1, A_RC, B_RC, kDirect, 2, 2, 1, 1, 64, 3, 2>; };  // 64 x 64
+template <bool A_RC, bool B_RC, bool LARGE> struct XentShape<bf16_t, A_RC, B_RC, LARGE, true> { using type = TileShape<bf16_t, 2, 1, A_RC, B_RC, kStaged, 2, 2, 1, 1, 64, 2, 2>; };
+template <bool A_RC, bool B_RC, bool STAGED> struct XentShape<float, A_RC, B_RC, true, STAGED> { using type = TileShape<float, 2, 3, A_RC, B_RC, kStaged, 4, 2, 2, 2, 32, 2, 1>; };  // 256 x 128
+template <bool A_RC, bool B_RC, bool STAGED> struct XentShape<float, A_RC, B_RC, false, STAGED> { using type = TileShape<float, 2, 3, A_RC, B_RC, kStaged, 2, 2, 1, 1, 32, 2, 2>; }; // 64 x 64
+
+static int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// Regions of the workspace, 256 bytes apart.
+struct Regions {
+    size_t bytes = 0;
+    size_t take(size_t b)
+    {
+        const size_t at = bytes;
+        bytes += (b + 255) / 256 * 256;
+        return at;
+    }
+};
+
+// What a row operand or the weights are read from: themselves, or a copy of them with aligned rows.
+struct Operand {
+    const void *p;
+    int64_t ld;
+};
+
+template <typename E> __global__ void __launch_bounds__(256) xent_align_kernel(const E *in, int64_t ld, int64_t n, int32_t d, E *out, int64_t ld_out)
+{
+    const int chunks = static_cast<int>(ld_out / 8);
+    const int64_t total = n * chunks;
+    for (int64_t q = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; q < total; q += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t r = q / chunks;
+        const int c = static_cast<int>(q - r * chunks) * 8;
+        float v[8];
+        load8(in + r * ld + c, d - c, v);
+        store8(out + r * ld_out + c, 8, v);
+    }
+}
+static unsigned walk(int64_t items) { return static_cast<unsigned>(std::min<int64_t>((items + 255) / 256, 16384)); }
+
+enum XentTiles { kTilesLarge, kTilesSmall, kTilesStaged };
+// The tiles of a product M x N of `splits` parts: staged where bf16 rows are not aligned, large where they give every second CU one and are not mostly
+// beyond the last row.
+template <typename E> static XentTiles tiles_for(bool direct, int64_t M, int64_t N, int64_t splits)
+{
+    if (sizeof(E) == 2 && !direct) return kTilesStaged;
+    return M > 64 && tiles_of(M, N, 256, 256) * splits >= 128 ? kTilesLarge : kTilesSmall;
+}
+// f(shape)
+template <typename E, bool A_RC, bool B_RC, typename F> static heta_status with_tiles(XentTiles t, F f)
+{
+    if (t == kTilesStaged) return f(XentShape<E, A_RC, B_RC, false, true>{});
+    return t == kTilesLarge ? f(XentShape<E, A_RC, B_RC, true, false>{}) : f(XentShape<E, A_RC, B_RC, false, false>{});
+}
+template <typename E, bool A_RC, bool B_RC, typename Epi> static heta_status go_tiles(const Launch &l, XentTiles t, const typename Epi::Extra &x)
+{
+    return with_tiles<E, A_RC, B_RC>(t, [&](auto shape) { return l.go<typename decltype(shape)::type, Epi>(x); });
+}
+// rows and columns of a wavefront's sums
+template <typename E> static void strip_of(XentTiles t, int64_t *rows, int64_t *cols)
+{
+    (void)with_tiles<E, false, true>(t, [&](auto shape) {
+        using C = typename decltype(shape)::type;
+        *rows = 32 * C::MI;
+        *cols = 32 * C::NJ;
+        return HETA_OK;
+    });
+}
+
+// Whether the product is worth aligned copies of its operands: where the weights are read by several tiles.
+static bool copies_pay(int64_t n) { return n >= 512; }
+
+// Sums over the parts of a contraction, after those of earlier pieces (nullable): out[i / width][i % width] for i < total, in a fixed order.
+template <typename O> __global__ void __launch_bounds__(256) xent_add_kernel(const float *so_far, const float *part, int splits, int64_t total, O *out, int32_t width, int64_t ld, const float *factor)
+{
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (i >= total) return;
+    const int valid = static_cast<int>(min(total - i, static_cast<int64_t>(4)));
+    float y[4] = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](const float *p) {
+        const uintx4 q = load_piece(p + i, valid);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] += __uint_as_float(q[e]);
+    };
+    if (so_far) add(so_far);
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) add(part + s * total);
+    if (factor) {
+        const float f = *factor;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] *= f;
+    }
+    const int64_t row = i / width;
+    int32_t c = static_cast<int32_t>(i - row * width);
+    O *to = out + row * ld;
+    if (c + 4 <= width && valid == 4) {
+        if constexpr (sizeof(O) == 4) store16(to + c, uintx4{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])});
+        else __builtin_memcpy(to + c, (const uint32_t[2]){pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3])}, 8);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (e >= valid) continue;
+        if constexpr (sizeof(O) == 4) to[c] = y[e];
+        else to[c] = to_bf16(y[e]);
+        if (++c == width) {
+            c = 0;
+            to += ld;
+        }
+    }
+}
+static heta_status xent_add(const float *so_far, const float *part, int splits, int64_t total, void *out, heta_dtype dt, int32_t width, int64_t ld, const float *factor, hipStream_t st)
+{
+    const int64_t blocks = (total + 1023) / 1024;
+    if (blocks > max_blocks(256)) return fail(HETA_ERR_UNSUPPORTED, "heta_linear_xent_bwd: input gradient too large for one launch");
+    ProfScope prof("xent_add_kernel", st, static_cast<double>(total) * (4.0 * (splits + !!so_far) + dtype_size(dt)), 0);
+    if (dt == HETA_F32) hipLaunchKernelGGL(xent_add_kernel<float>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, so_far, part, splits, total, static_cast<float *>(out), width, ld, factor);
+    else hipLaunchKernelGGL(xent_add_kernel<bf16_t>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, so_far, part, splits, total, static_cast<bf16_t *>(out), width, ld, factor);
+    HETA_LAUNCH_CHECK("xent_add_kernel");
+    return HETA_OK;
+}
+
+template <typename E> static heta_status xent_forward(heta_graph *g, const heta_linear_xent_args &a, hipStream_t st)
+{
+    const char *who = "heta_linear_xent";
+    const int64_t n = a.n_rows, d = a.d, V = a.n_classes;
+    const double flops = 2.0 * n * d * V;
+    Regions ws;
+    const bool bf16 = sizeof(E) == 2;
+    const bool copy_w = bf16 && copies_pay(n) && !direct_rows(a.W, a.ld_w, 2), copy_in = bf16 && copies_pay(n) && !direct_rows(a.in, a.ld_in, 2);
+    const int64_t ld_wc = round_up(V, 8), ld_ic = round_up(d, 8);
+    const size_t w_at = ws.take(copy_w ? static_cast<size_t>(d) * ld_wc * 2 : 0), in_at = ws.take(copy_in ? static_cast<size_t>(n) * ld_ic * 2 : 0);
+    const size_t target_at = ws.take(static_cast<size_t>(n) * 4);
+    const XentTiles tiles = tiles_for<E>((copy_w || direct_rows(a.W, a.ld_w, 2)) && (copy_in || direct_rows(a.in, a.ld_in, 2)), n, V, 1);
+    int64_t strip_rows = 0, strip_cols = 0;
+    strip_of<E>(tiles, &strip_rows, &strip_cols);
+    const int64_t strips = (V + strip_cols - 1) / strip_cols;
+    const size_t part_at = ws.take(static_cast<size_t>(strips) * n * sizeof(XentPart));
+    const bool wide = n >= 4096 || V <= 4096;
+    const int64_t groups = (n + (wide ? 31 : 3)) / (wide ? 32 : 4);
+    const size_t sums_at = ws.take(a.mean && groups > 1 ? static_cast<size_t>(groups) * sizeof(XentSum) : 0);
+    HETA_TRY(ensure_workspace(g, ws.bytes));
+    char *base = static_cast<char *>(g->d_ws);
+    Operand W{a.W, a.ld_w}, in{a.in, a.ld_in};
+    if (copy_w) {
+        hipLaunchKernelGGL(xent_align_kernel<bf16_t>, dim3(walk(d * ld_wc / 8)), dim3(256), 0, st, static_cast<const bf16_t *>(a.W), a.ld_w, d, a.n_classes, reinterpret_cast<bf16_t *>(base + w_at), ld_wc);
+        W = {base + w_at, ld_wc};
+    }
+    if (copy_in) {
+        hipLaunchKernelGGL(xent_align_kernel<bf16_t>, dim3(walk(n * ld_ic / 8)), dim3(256), 0, st, static_cast<const bf16_t *>(a.in), a.ld_in, n, a.d, reinterpret_cast<bf16_t *>(base + in_at), ld_ic);
+        in = {base + in_at, ld_ic};
+    }
+    HETA_LAUNCH_CHECK("xent_align_kernel");
+    const Launch l{g, who, "xent_kernel", TileItem{in.p, W.p, in.ld, W.ld, 0, 0, n, V, d, d, 1, 0, 0, 0, 0, 0}, (static_cast<double>(n) * d + static_cast<double>(d) * V) * sizeof(E), flops, st};
+    const XentForward x{a.bias, a.labels, reinterpret_cast<XentPart *>(base + part_at), reinterpret_cast<float *>(base + target_at)};
+    HETA_TRY((go_tiles<E, false, true, XentForwardEpi>(l, tiles, x)));
+    XentSum *sums = a.mean && groups > 1 ? reinterpret_cast<XentSum *>(base + sums_at) : nullptr;
+    {
+        ProfScope prof("xent_rows_kernel", st, static_cast<double>(n) * (8.0 * strips + 20), 0);
+        if (wide) hipLaunchKernelGGL(xent_rows_kernel<32>, dim3(static_cast<unsigned>(groups)), dim3(256), 0, st, x.part, strips, x.target, a.labels, n, V, a.loss, a.lse, sums, a.mean);
+        else hipLaunchKernelGGL(xent_rows_kernel<4>, dim3(static_cast<unsigned>(groups)), dim3(256), 0, st, x.part, strips, x.target, a.labels, n, V, a.loss, a.lse, sums, a.mean);
+        HETA_LAUNCH_CHECK("xent_rows_kernel");
+    }
+    if (sums) hipLaunchKernelGGL(xent_mean_kernel, dim3(1), dim3(256), 0, st, sums, groups, a.mean);
+    HETA_LAUNCH_CHECK("xent_mean_kernel");
+    return HETA_OK;
+}
+
+constexpr int64_t kXentPiece = int64_t(192) << 20; // bytes of D at a time
+
+// splits of a contraction over K for tiles of M x N outputs: one workgroup per CU
+static void split_for(int64_t M, int64_t N, int64_t K, int64_t least, int32_t *n_split, int64_t *k_per_split)
+{
+    const int64_t tiles = tiles_of(M, N, 256, 256), most = std::max<int64_t>(1, 256 / tiles);
+    *k_per_split = round_up(std::max((K + most - 1) / most, least), 64);
+    *n_split = static_cast<int32_t>((K + *k_per_split - 1) / *k_per_split);
+}
+
+template <typename E> static heta_status xent_backward(heta_graph *g, const heta_linear_xent_bwd_args &a, hipStream_t st)
+{
+    const char *who = "heta_linear_xent_bwd";
+    const int64_t n = a.n_rows, d = a.d, V = a.n_classes;
+    const bool bf16 = sizeof(E) == 2;
+    const heta_dtype dt = bf16 ? HETA_BF16 : HETA_F32;
+    const int64_t room = kXentPiece / static_cast<int64_t>(sizeof(E));
+    int64_t R = n, Vc = V; // a piece of D
+    if (n * round_up(V, 8) > room) {
+        const int64_t side = static_cast<int64_t>(std::sqrt(static_cast<double>(room)));
+        R = std::min(n, std::max(side, room / round_up(V, 8)));
+        R = round_up((n + (n + R - 1) / R - 1) / ((n + R - 1) / R), 256); // pieces of one size
+        const int64_t most = std::max<int64_t>(256, room / R);
+        Vc = round_up((V + (V + most - 1) / most - 1) / ((V + most - 1) / most), 256);
+        R = std::min(R, n);
+        Vc = std::min(Vc, V);
+    }
+    const int64_t n_r = (n + R - 1) / R, n_v = (V + Vc - 1) / Vc, ld_d = round_up(Vc, 8);
+    const bool copy_w = bf16 && copies_pay(n) && !direct_rows(a.W, a.ld_w, 2), copy_in = bf16 && copies_pay(n) && !direct_rows(a.in, a.ld_in, 2);
+    const int64_t ld_wc = round_up(V, 8), ld_ic = round_up(d, 8);
+    int32_t in_splits = 1, w_splits = 1;
+    int64_t in_k = Vc, w_k = R;
+    split_for(R, d, Vc, 512, &in_splits, &in_k);
+    split_for(d, Vc, R, 256, &w_splits, &w_k);
+    const bool direct_w = copy_w || direct_rows(a.W, a.ld_w, 2), direct_in = copy_in || direct_rows(a.in, a.ld_in, 2);
+    Regions ws;
+    const size_t poison_at = ws.take(8), rows_at = ws.take(static_cast<size_t>(n) * sizeof(XentRow));
+    const size_t w_at = ws.take(copy_w ? static_cast<size_t>(d) * ld_wc * 2 : 0), in_at = ws.take(a.dW ? static_cast<size_t>(n) * ld_ic * sizeof(E) : copy_in ? static_cast<size_t>(n) * ld_ic * 2 : 0);
+    const size_t d_at = ws.take(static_cast<size_t>(R) * ld_d * sizeof(E));
+    const size_t sums_at = ws.take(a.dbias ? static_cast<size_t>((R + 31) / 32 * n_r) * Vc * 4 : 0);
+    const size_t dw_at = ws.take(a.dW ? static_cast<size_t>(w_splits) * n_r * d * Vc * 4 : 0);
+    // grad_in's sums over the classes so far, and in front of each piece's partial products
+    const size_t di_at = ws.take(a.grad_in ? static_cast<size_t>(in_splits + (n_v > 1 ? n_r : 0)) * R * d * 4 : 0);
+    HETA_TRY(ensure_workspace(g, ws.bytes));
+    char *base = static_cast<char *>(g->d_ws);
+    uint32_t *poison = reinterpret_cast<uint32_t *>(base + poison_at);
+    float *factor = reinterpret_cast<float *>(poison) + 1;
+    XentRow *rows = reinterpret_cast<XentRow *>(base + rows_at);
+    const uint32_t call = ++g->xent_calls;
+    {
+        ProfScope prof("xent_prepare_kernel", st, 32.0 * n, 0);
+        hipLaunchKernelGGL(xent_prepare_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, a.labels, a.lse, a.grad_loss, a.mean, a.scale, n, V, rows, factor, poison, call);
+        HETA_LAUNCH_CHECK("xent_prepare_kernel");
+    }
+    Operand W{a.W, a.ld_w}, in{a.in, a.ld_in};
+    if (copy_w) {
+        hipLaunchKernelGGL(xent_align_kernel<bf16_t>, dim3(walk(d * ld_wc / 8)), dim3(256), 0, st, static_cast<const bf16_t *>(a.W), a.ld_w, d, a.n_classes, reinterpret_cast<bf16_t *>(base + w_at), ld_wc);
+        W = {base + w_at, ld_wc};
+    }
+    E *clean = reinterpret_cast<E *>(base + in_at);
+    if (copy_in || a.dW)
+        hipLaunchKernelGGL(xent_clean_kernel<E>, dim3(walk(n * ld_ic / 8)), dim3(256), 0, st, static_cast<const E *>(a.in), a.ld_in, n, a.d, rows, clean, ld_ic, copy_in, poison, call);
+    if (copy_in) in = {clean, ld_ic};
+    HETA_LAUNCH_CHECK("xent_align_kernel");
+
+    float *sums = a.dbias ? reinterpret_cast<float *>(base + sums_at) : nullptr;
+    for (int64_t v = 0; v < n_v; ++v) {
+        const int64_t v0 = v * Vc, cols = std::min(Vc, V - v0);
+        const E *Wv = static_cast<const E *>(W.p) + v0;
+        float *dw = reinterpret_cast<float *>(base + dw_at);
+        int64_t bias_slots = 0, dw_parts = 0;
+        for (int64_t r = 0; r < n_r; ++r) {
+            const int64_t r0 = r * R, rn = std::min(R, n - r0);
+            const E *in_r = static_cast<const E *>(in.p) + r0 * in.ld;
+            const double product = 2.0 * rn * d * cols;
+            {
+                const Launch l{g, who, "xent_logit_grad_kernel", TileItem{in_r, Wv, in.ld, W.ld, 0, 0, rn, cols, d, d, 1, 0, 0, 0, 0, 0},
+                               (static_cast<double>(rn) * (d + cols) + static_cast<double>(d) * cols) * sizeof(E), product, st};
+                const XentTiles tiles = tiles_for<E>(direct_w && direct_in, rn, cols, 1);
+                int64_t strip_rows = 0, strip_cols = 0;
+                strip_of<E>(tiles, &strip_rows, &strip_cols);
+                const XentBackward x{a.bias ? a.bias + v0 : nullptr, rows + r0, base + d_at, ld_d, sums ? sums + bias_slots * cols : nullptr, v0};
+                HETA_TRY((go_tiles<E, false, true, XentBackwardEpi<E>>(l, tiles, x)));
+                bias_slots += (rn + strip_rows - 1) / strip_rows;
+            }
+            if (a.grad_in) {
+                int32_t splits = 1;
+                int64_t k_each = cols;
+                split_for(rn, d, cols, 512, &splits, &k_each);
+                splits = std::min(splits, in_splits);
+                if (static_cast<int64_t>(splits) * k_each < cols) k_each = round_up((cols + splits - 1) / splits, 64), splits = static_cast<int32_t>((cols + k_each - 1) / k_each);
+                const Launch l{g, who, "xent_grad_in_kernel", TileItem{base + d_at, Wv, ld_d, W.ld, 0, 0, rn, d, cols, k_each, splits, 0, 0, 0, 0, 0},
+                               (static_cast<double>(rn) * (d + cols) + static_cast<double>(d) * cols) * sizeof(E), product, st};
+                float *so_far = reinterpret_cast<float *>(base + di_at) + (n_v > 1 ? r * R * d : 0), *part = reinterpret_cast<float *>(base + di_at) + (n_v > 1 ? n_r * R * d : 0);
+                const PartialEpi::Extra x{part, d};
+                HETA_TRY((go_tiles<E, false, false, PartialEpi>(l, tiles_for<E>(direct_w, rn, d, splits), x)));
+                E *out = static_cast<E *>(a.grad_in) + r0 * a.ld_gi;
+                const bool last = v + 1 == n_v;
+                HETA_TRY(xent_add(v > 0 ? so_far : nullptr, part, splits, rn * d, last ? static_cast<void *>(out) : so_far, last ? dt : HETA_F32, a.d, last ? a.ld_gi : d, last ? factor : nullptr, st));
+            }
+            if (a.dW) {
+                int32_t splits = 1;
+                int64_t k_each = rn;
+                split_for(d, cols, rn, 256, &splits, &k_each);
+                splits = std::min(splits, w_splits);
+                if (static_cast<int64_t>(splits) * k_each < rn) k_each = round_up((rn + splits - 1) / splits, 64), splits = static_cast<int32_t>((rn + k_each - 1) / k_each);
+                const Launch l{g, who, "xent_grad_w_kernel", TileItem{in_r, base + d_at, in.ld, ld_d, 0, 0, d, cols, rn, k_each, splits, 0, 0, 0, 0, 0},
+                               (static_cast<double>(rn) * (d + cols)) * sizeof(E) + 4.0 * splits * d * cols, product, st};
+                const XentWeights x{dw + dw_parts * d * cols, cols, clean + r0 * ld_ic, ld_ic, poison, call};
+                HETA_TRY((go_tiles<E, true, true, XentWeightsEpi>(l, tiles_for<E>(direct_in, d, cols, splits), x)));
+                dw_parts += splits;
+            }
+        }
+        if (a.dbias) HETA_TRY(fold_partials(sums, bias_slots, cols, a.dbias + v0, HETA_F32, static_cast<int32_t>(cols), cols, st, factor));
+        if (a.dW) {
+            char *to = static_cast<char *>(a.dW) + v0 * dtype_size(a.dw_dt);
+            HETA_TRY(fold_partials(dw, dw_parts, d * cols, to, a.dw_dt, static_cast<int32_t>(cols), a.ld_dw, st, factor));
+        }
+    }
+    return HETA_OK;
+}
+
+} // namespace heta
+
+using namespace heta;
+
+extern "C" heta_status heta_linear_xent(heta_graph *g, const heta_linear_xent_args *a, void *hip_stream)
+{
+    const char *who = "heta_linear_xent";
+    if (!g || !a) return fail(HETA_ERR_INVALID_ARG, "%s: null arguments", who);
+    if (a->n_rows < 0 || a->d <= 0 || a->n_classes <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0, a width and classes", who);
+    if (std::max(a->d, a->n_classes) > kWidest || a->n_rows >= int64_t(1) << 31) return fail(HETA_ERR_UNSUPPORTED, "%s: too many rows, columns or classes", who);
+    if (!valid_dtype(a->dt)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    const size_t esz = dtype_size(a->dt);
+    const int64_t n = a->n_rows;
+    HETA_TRY(check_rows(who, "in", a->in, n, a->ld_in, a->d, esz));
+    HETA_TRY(check_rows(who, "W", a->W, 1, a->ld_w, a->n_classes, esz));
+    if (n > 0 && (!a->labels || !a->lse)) return fail(HETA_ERR_INVALID_ARG, "%s: null labels or lse", who);
+    if (reinterpret_cast<uintptr_t>(a->labels) & 7u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
+    for (const float *v : {a->bias, static_cast<const float *>(a->loss), static_cast<const float *>(a->lse), static_cast<const float *>(a->mean)})
+        if (reinterpret_cast<uintptr_t>(v) & 3u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
+    const RowRange outs[3] = {RowRange(a->loss, 1, n, n, 4), RowRange(a->lse, 1, n, n, 4), RowRange(a->mean, 1, 2, 2, 4)};
+    const RowRange ins[4] = {RowRange(a->in, n, a->ld_in, a->d, esz), RowRange(a->W, a->d, a->ld_w, a->n_classes, esz), RowRange(a->bias, 1, a->n_classes, a->n_classes, 4),
+                             RowRange(a->labels, 1, n, n, 8)};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (outs[i].overlaps(outs[j])) return fail(HETA_ERR_INVALID_ARG, "%s: two outputs overlap", who);
+        for (const RowRange &in : ins)
+            if (outs[i].overlaps(in)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand", who);
+    }
+    hipStream_t st = as_stream(hip_stream);
+    if (n == 0) {
+        if (a->mean) hipLaunchKernelGGL(xent_mean_kernel, dim3(1), dim3(256), 0, st, nullptr, 0, a->mean);
+        HETA_LAUNCH_CHECK("xent_mean_kernel");
+        return HETA_OK;
+    }
+    return a->dt == HETA_F32 ? xent_forward<float>(g, *a, st) : xent_forward<bf16_t>(g, *a, st);
+}
+
+extern "C" heta_status heta_linear_xent_bwd(heta_graph *g, const heta_linear_xent_bwd_args *a, void *hip_stream)
+{
+    const char *who = "heta_linear_xent_bwd";
+    if (!g || !a) return fail(HETA_ERR_INVALID_ARG, "%s: null arguments", who);
+    if (a->n_rows < 0 || a->d <= 0 || a->n_classes <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0, a width and classes", who);
+    if (std::max(a->d, a->n_classes) > kWidest || a->n_rows >= int64_t(1) << 31) return fail(HETA_ERR_UNSUPPORTED, "%s: too many rows, columns or classes", who);
+    if (!valid_dtype(a->dt) || (a->dW && !valid_dtype(a->dw_dt))) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (a->dt == HETA_F32 && a->dW && a->dw_dt != HETA_F32) return fail(HETA_ERR_UNSUPPORTED, "%s: fp32 operands have an fp32 weight gradient", who);
+    const size_t esz = dtype_size(a->dt);
+    const int64_t n = a->n_rows, V = a->n_classes;
+    HETA_TRY(check_rows(who, "in", a->in, n, a->ld_in, a->d, esz));
+    HETA_TRY(check_rows(who, "W", a->W, 1, a->ld_w, V, esz));
+    if (a->grad_in) HETA_TRY(check_rows(who, "grad_in", a->grad_in, n, a->ld_gi, a->d, esz));
+    if (a->dW) HETA_TRY(check_rows(who, "dW", a->dW, 1, a->ld_dw, V, dtype_size(a->dw_dt)));
+    if (n > 0 && (!a->labels || !a->lse)) return fail(HETA_ERR_INVALID_ARG, "%s: null labels or lse", who);
+    if (reinterpret_cast<uintptr_t>(a->labels) & 7u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
+    for (const float *v : {a->bias, a->lse, a->grad_loss, a->mean, static_cast<const float *>(a->dbias)})
+        if (reinterpret_cast<uintptr_t>(v) & 3u) return fail(HETA_ERR_INVALID_ARG, "%s: pointer not aligned to its element size", who);
+    if (a->dW && static_cast<int64_t>(a->d) * V > kFoldMost) return fail(HETA_ERR_UNSUPPORTED, "%s: weight gradient of too many elements", who);
+    const RowRange outs[3] = {RowRange(a->grad_in, n, a->ld_gi, a->d, esz), RowRange(a->dW, a->d, a->ld_dw, V, a->dW ? dtype_size(a->dw_dt) : 4), RowRange(a->dbias, 1, V, V, 4)};
+    const RowRange ins[7] = {RowRange(a->in, n, a->ld_in, a->d, esz), RowRange(a->W, a->d, a->ld_w, V, esz), RowRange(a->bias, 1, V, V, 4), RowRange(a->labels, 1, n, n, 8),
+                             RowRange(a->lse, 1, n, n, 4), RowRange(a->grad_loss, 1, n, n, 4), RowRange(a->mean, 1, 2, 2, 4)};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (outs[i].overlaps(outs[j])) return fail(HETA_ERR_INVALID_ARG, "%s: two outputs overlap", who);
+        for (const RowRange &in : ins)
+            if (outs[i].overlaps(in)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand", who);
+    }
+    hipStream_t st = as_stream(hip_stream);
+    if (n == 0) {
+        if (a->dbias) HETA_TRY(fold_partials(nullptr, 0, V, a->dbias, HETA_F32, a->n_classes, V, st));
+        if (a->dW) HETA_TRY(fold_partials(nullptr, 0, a->d * V, a->dW, a->dw_dt, a->n_classes, a->ld_dw, st));
+        return HETA_OK;
+    }
+    if (!a->grad_in && !a->dW && !a->dbias) return HETA_OK;
+    return a->dt == HETA_F32 ? xent_backward<float>(g, *a, st) : xent_backward<bf16_t>(g, *a, st);
+}

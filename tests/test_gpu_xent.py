@@ -1,0 +1,343 @@
+"""heta_linear_xent and heta_linear_xent_bwd against the definition in 64 bits.
+
+Tolerances, u = 2^-24 (one fp32 rounding; half a step of bf16 is 2^-8 of a value).
+  z: products added in fp32, a truncating accumulator loses 2 u an addition: (2 d + 16) u of sum |in||W| + |bias|; held as z log2(e): 4 u of |z| and |bias| more.
+  lse: a relative error of every exponential is one of their sum and an absolute one of its logarithm: the largest error of a z; exponentials (2 u and
+    u of their argument's size), sums of 16 and then one part after another: (8 |z| + V / 8 + 100) u.
+  loss: the errors of lse and of the label's z, and 4 u of both.
+  p = exp(z - lse): relative, the errors of z and of lse, 4 u of their sizes and 8 u, each by a factor of 1.1 for the exponential of an error below 0.1.
+  D = f (p - 1): f times p's error, 4 u of D; in the products D is rounded to the operands' type.
+  Products over the classes or rows: (2 k + 600) u of sum |a||b|, and D's error times the other operand; a result is rounded once to its type.
+"""
+import pytest
+import torch
+
+import paper_2408_09697_amd as heta
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+STEP = {F32: U, BF16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def handle():
+    g = heta.heta_graph_create([(1, 1, 0)], [])
+    yield g
+    g.destroy()
+
+
+def rows(n, d, dtype, seed, pad=0, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    buf = torch.full((n, d + pad), float("nan"), device="cuda").to(dtype)
+    buf[:, :d] = (torch.randn(n, d, generator=g, device="cuda") * scale).to(dtype)
+    return buf[:, :d]
+
+
+def labels_of(n, classes, seed, none=0.1):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    y = torch.randint(0, classes, (n,), generator=g, device="cuda")
+    u = torch.rand(n, generator=g, device="cuda")
+    y[u < none] = -1
+    y[u < none / 2] = classes  # outside on the other side
+    y[u < none / 4] = -(1 << 40)
+    return y
+
+
+def within(got, ref, bound, what):
+    off = (got.double() - ref).abs()
+    assert torch.isfinite(got.double()).all(), what
+    assert (off <= bound).all(), f"{what}: {float((off - bound).max()):.3e} over its bound, worst {float(off.max()):.3e}"
+
+
+class Problem:
+    def __init__(self, n, d, classes, dtype, pad=0, bias=True, seed=1, scale=2.0, none=0.1):
+        self.n, self.d, self.classes, self.dtype = n, d, classes, dtype
+        self.x, self.W = rows(n, d, dtype, seed, pad), rows(d, classes, dtype, seed + 1, pad, scale * d ** -0.5)
+        self.bias = rows(1, classes, F32, seed + 2)[0] if bias else None
+        self.y = labels_of(n, classes, seed + 3, none)
+        self.loss, self.lse, self.mean = torch.full((n,), float("nan"), device="cuda"), torch.full((n,), float("nan"), device="cuda"), torch.full((2,), float("nan"), device="cuda")
+
+    def forward(self, g, **kw):
+        heta.heta_linear_xent(g, self.x, self.W, self.y, self.loss, self.lse, bias=self.bias, mean=self.mean, **kw)
+
+    def outputs(self, pad=0, w_dtype=None):
+        self.gx, self.gW = rows(self.n, self.d, self.dtype, 8, pad), rows(self.d, self.classes, w_dtype or self.dtype, 9, pad)
+        self.gb = torch.full((self.classes,), float("nan"), device="cuda")
+
+    def backward(self, g, mean=True, grad_loss=None, scale=1.0, **kw):
+        heta.heta_linear_xent_bwd(g, self.x, self.W, self.y, self.lse, bias=self.bias, grad_loss=grad_loss, scale=scale, mean=self.mean if mean else None, grad_in=self.gx,
+                                  grad_W=self.gW, grad_bias=self.gb, **kw)
+
+    def reference(self, f=None):
+        x, W = self.x.double(), self.W.double()
+        b = self.bias.double() if self.bias is not None else torch.zeros(self.classes, device="cuda", dtype=torch.float64)
+        z = x @ W + b
+        self.ez = (2 * self.d + 16) * U * (x.abs() @ W.abs() + b.abs()) + 4 * U * (z.abs() + b.abs())
+        has = (self.y >= 0) & (self.y < self.classes)
+        lse = torch.logsumexp(z, 1)
+        at = torch.where(has, self.y, 0)[:, None]
+        self.e_lse = self.ez.amax(1) + (8 * z.abs().amax(1) + self.classes / 8 + 100) * U
+        zy = z.gather(1, at)[:, 0]
+        self.e_loss = torch.where(has, self.e_lse + self.ez.gather(1, at)[:, 0] + 4 * U * (lse.abs() + zy.abs()), 0.0)
+        self.r_loss, self.r_lse, self.has, self.z = torch.where(has, lse - zy, 0.0), lse, has, z
+        count = has.sum().clamp_min(1).double()
+        f = torch.where(has, 1 / count if f is None else f, 0.0)[:, None]
+        p = torch.exp(z - lse[:, None])
+        ep = 1.1 * p * (self.ez + self.e_lse[:, None] + 4 * U * (z.abs() + lse.abs()[:, None]) + 8 * U)
+        D = p.clone()
+        D.scatter_add_(1, at, -torch.ones_like(at, dtype=torch.float64))
+        self.D, self.eD = D * f, (ep + 4 * U * D.abs()) * f.abs()
+
+    def check_forward(self):
+        within(self.lse, self.r_lse, self.e_lse + U * self.r_lse.abs(), "lse")
+        within(self.loss, self.r_loss, self.e_loss, "loss")
+        assert (self.loss[~self.has] == 0).all()
+        count = int(self.has.sum())
+        assert float(self.mean[1]) == count
+        want = float(self.r_loss.sum()) / max(count, 1)
+        assert abs(float(self.mean[0]) - want) <= float(self.e_loss.sum()) / max(count, 1) + 2 * U * abs(want) + 1e-30
+
+    def check_backward(self):
+        x, W, D = self.x.double(), self.W.double(), self.D
+        e = self.eD + STEP[self.dtype] * (D.abs() + self.eD) * (self.dtype == BF16)
+        want = D @ W.t()
+        bound = e @ W.abs().t() + (2 * self.classes + 600) * U * ((D.abs() + e) @ W.abs().t())
+        within(self.gx, want, bound + STEP[self.dtype] * (want.abs() + bound), "grad_in")
+        want = x.t() @ D
+        bound = x.abs().t() @ e + (2 * self.n + 600) * U * (x.abs().t() @ (D.abs() + e))
+        within(self.gW, want, bound + STEP[self.gW.dtype] * (want.abs() + bound), "grad_W")
+        within(self.gb, D.sum(0), self.eD.sum(0) + (2 * self.n + 600) * U * D.abs().sum(0), "grad_bias")
+        assert (self.gx[~self.has] == 0).all()
+
+
+# one of each, tails of every tile dimension, several tiles, few rows and many classes, many rows and few classes
+SHAPES = [(1, 1, 1), (1, 7, 2), (3, 16, 5), (64, 256, 349), (65, 72, 130), (257, 128, 1000), (515, 300, 2983), (1000, 64, 8), (700, 789, 65), (4, 1024, 40000), (2049, 256, 4001),
+          (30000, 128, 153), (129, 1030, 264), (40, 8, 70001)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d,classes", SHAPES)
+def test_loss_and_gradients(handle, n, d, classes, dtype):
+    for pad, bias in ((0, True), (3, False)):
+        p = Problem(n, d, classes, dtype, pad, bias)
+        p.forward(handle)
+        p.outputs(pad)
+        p.backward(handle)
+        p.reference()
+        p.check_forward()
+        p.check_backward()
+
+
+@pytest.mark.parametrize("pad", [0, 1, 8])
+def test_fp32_weight_gradient_of_bf16_operands_and_outputs_that_are_not_asked_for(handle, pad):
+    p = Problem(600, 96, 1000, BF16, pad)
+    p.forward(handle)
+    p.outputs(pad, F32)
+    p.backward(handle)
+    p.reference()
+    p.check_backward()
+    whole = [t.clone() for t in (p.gx, p.gW, p.gb)]
+    for keep in range(3):
+        p.outputs(pad, F32)
+        outs = [t if i == keep else None for i, t in enumerate((p.gx, p.gW, p.gb))]
+        heta.heta_linear_xent_bwd(handle, p.x, p.W, p.y, p.lse, bias=p.bias, mean=p.mean, grad_in=outs[0], grad_W=outs[1], grad_bias=outs[2])
+        assert torch.equal(outs[keep], whole[keep])
+    lse = torch.empty_like(p.lse)
+    heta.heta_linear_xent(handle, p.x, p.W, p.y, None, lse, bias=p.bias)
+    assert torch.equal(lse, p.lse)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradients_of_each_row_and_a_scale(handle, dtype):
+    p = Problem(700, 64, 500, dtype, 8)
+    p.forward(handle)
+    p.outputs(8)
+    gl = rows(1, 700, F32, 20)[0]
+    gl[5] = 0
+    p.backward(handle, mean=False, grad_loss=gl, scale=0.25)
+    p.reference(gl.double() * 0.25)
+    p.check_backward()
+
+
+@pytest.mark.parametrize("dtype,n,d,classes", [(BF16, 3000, 40, 70001), (BF16, 12001, 72, 17000), (F32, 3000, 24, 33000), (F32, 9001, 16, 12000), (BF16, 600, 16, 300001)])
+def test_pieces_along_rows_and_classes(handle, dtype, n, d, classes):
+    p = Problem(n, d, classes, dtype)
+    p.forward(handle)
+    p.outputs()
+    p.backward(handle)
+    at = torch.arange(n, device="cuda")[:: max(1, n // 500)]
+    # rows are independent: the loss and grad_in of some of them; grad_W and grad_bias of the whole by pieces
+    x, W, b = p.x.double(), p.W.double(), p.bias.double()
+    count = float(((p.y >= 0) & (p.y < classes)).sum())
+    q = Problem.__new__(Problem)
+    q.__dict__.update(p.__dict__)
+    q.n, q.x, q.y, q.loss, q.lse, q.gx = len(at), p.x[at], p.y[at], p.loss[at], p.lse[at], p.gx[at]
+    q.reference(torch.full((len(at),), 1 / count, device="cuda", dtype=torch.float64))
+    within(q.lse, q.r_lse, q.e_lse + U * q.r_lse.abs(), "lse")
+    within(q.loss, q.r_loss, q.e_loss, "loss")
+    e = q.eD + STEP[dtype] * (q.D.abs() + q.eD) * (dtype == BF16)
+    want, bound = q.D @ W.t(), e @ W.abs().t() + (2 * classes + 600) * U * ((q.D.abs() + e) @ W.abs().t())
+    within(q.gx, want, bound + STEP[dtype] * (want.abs() + bound), "grad_in")
+    gW, gb = torch.zeros(d, classes, device="cuda", dtype=torch.float64), torch.zeros(classes, device="cuda", dtype=torch.float64)
+    for i in range(0, n, 500):
+        z = x[i:i + 500] @ W + b
+        D = torch.softmax(z, 1)
+        y = p.y[i:i + 500]
+        has = (y >= 0) & (y < classes)
+        D.scatter_add_(1, torch.where(has, y, 0)[:, None], -torch.ones(len(y), 1, device="cuda", dtype=torch.float64))
+        D *= (has / count)[:, None]
+        gW += x[i:i + 500].t() @ D
+        gb += D.sum(0)
+    # norms: D's roundings (2^-8, or the bounds above, below 2^-14) are independent of each other
+    assert float((p.gW.double() - gW).norm() / gW.norm()) <= (2 * STEP[BF16] if dtype == BF16 else 2.0 ** -14)
+    assert float((p.gb.double() - gb).norm() / gb.norm()) <= 2.0 ** -14
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_row_with_a_label(handle, dtype):
+    p = Problem(300, 40, 77, dtype)
+    p.y.fill_(-1)
+    p.x.fill_(float("nan"))
+    p.forward(handle)
+    p.outputs()
+    p.backward(handle)
+    assert (p.loss == 0).all() and (p.mean == 0).all()
+    for t in (p.gx, p.gW, p.gb):
+        assert (t == 0).all()
+
+
+def test_no_rows(handle):
+    p = Problem(0, 40, 77, F32)
+    p.forward(handle)
+    p.outputs()
+    p.backward(handle)
+    assert (p.mean == 0).all() and (p.gW == 0).all() and (p.gb == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,pad", [(200, 0), (200, 3), (700, 0), (700, 3), (20000, 0)])
+def test_what_a_row_without_a_label_holds_reaches_nothing(handle, dtype, n, pad):
+    p = Problem(n, 72, 333, dtype, pad)
+    p.forward(handle)
+    p.outputs(pad)
+    p.backward(handle)
+    p.reference()
+    p.check_forward()
+    p.check_backward()
+    clean = [t.clone() for t in (p.loss, p.mean, p.gx, p.gW, p.gb)]
+    none = torch.nonzero(~p.has)[:, 0]
+    assert len(none) >= 3
+    p.x[none[0]] = float("nan")
+    p.x[none[1], 5] = float("inf")
+    p.x[none[2]] = -float("inf")
+    for _ in range(2):
+        p.forward(handle)
+        p.outputs(pad)
+        p.backward(handle)
+        for got, want in zip((p.loss, p.mean, p.gx, p.gW, p.gb), clean):
+            assert torch.equal(got, want)
+
+
+def test_extreme_logits(handle):
+    """Logits of thousands, classes that a bias of -infinity rules out, a class of +infinity, one logit far above the others in one part of the classes."""
+    n, d, classes = 66, 16, 1000
+    x, W = torch.zeros(n, d, device="cuda"), torch.zeros(d, classes, device="cuda")
+    x[:, 0] = torch.linspace(-1, 1, n, device="cuda")
+    W[0] = torch.linspace(-5000, 5000, classes, device="cuda")
+    bias = torch.zeros(classes, device="cuda")
+    bias[::3] = -float("inf")
+    y = torch.arange(n, device="cuda") * 3 + 1
+    loss, lse, mean = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(2, device="cuda")
+    heta.heta_linear_xent(handle, x, W, y, loss, lse, bias=bias, mean=mean)
+    z = x.double() @ W.double() + bias.double()
+    want = torch.logsumexp(z, 1)
+    # z of up to 5,000: 16 additions and their conversion, (2 * 16 + 16 + 4 + 8) u of it
+    within(lse, want, 60 * U * 5000 + 300 * U, "lse")
+    within(loss, want - z.gather(1, y[:, None])[:, 0], 130 * U * 5000 + 300 * U, "loss")
+    gx, gW, gb = torch.empty_like(x), torch.empty_like(W), torch.empty(classes, device="cuda")
+    heta.heta_linear_xent_bwd(handle, x, W, y, lse, bias=bias, mean=mean, grad_in=gx, grad_W=gW, grad_bias=gb)
+    assert torch.isfinite(gx).all() and torch.isfinite(gW).all() and (gb[::3] == 0).all() and (gW[:, ::3] == 0).all()
+    bias.fill_(-float("inf"))
+    heta.heta_linear_xent(handle, x, W, y, loss, lse, bias=bias)
+    assert (lse == -float("inf")).all()
+    bias.fill_(-30000.0)
+    bias[777] = 1e5
+    heta.heta_linear_xent(handle, x, W, torch.full_like(y, 777), loss, lse, bias=bias)
+    assert (loss == 0).all() and ((lse.double() - (1e5 + (x.double() @ W.double())[:, 777])).abs() <= 1e5 * 8 * U + 60 * U * 5000).all()
+    bias.zero_()
+    bias[10] = float("inf")
+    heta.heta_linear_xent(handle, x, W, y, loss, lse, bias=bias)
+    assert (lse == float("inf")).all() and (loss[y != 10] == float("inf")).all() and torch.isnan(loss[y == 10]).all()  # infinity less itself
+    W[:, 10] = float("nan")
+    heta.heta_linear_xent(handle, x, W, y, loss, lse)
+    assert torch.isnan(lse).all() and torch.isnan(loss).all()
+
+
+@pytest.mark.parametrize("n,d,classes", [(50, 24, 37), (700, 40, 1100)])
+def test_gradients_against_differences(handle, n, d, classes):
+    """The directional derivative of the summed loss along a random direction v of all parameters, by a central difference of the 64-bit definition at
+    steps of 1e-4 (its own error, of third order, is below 1e-7 of the sizes involved), is the inner product of the gradients with v."""
+    p = Problem(n, d, classes, F32)
+    p.forward(handle)
+    p.outputs()
+    p.backward(handle, mean=False)
+    vx, vW, vb = rows(n, d, F32, 31).double(), rows(d, classes, F32, 32).double(), rows(1, classes, F32, 33)[0].double()
+    has = (p.y >= 0) & (p.y < classes)
+    at = torch.where(has, p.y, 0)[:, None]
+
+    def total(h):
+        z = (p.x.double() + h * vx) @ (p.W.double() + h * vW) + p.bias.double() + h * vb
+        return torch.where(has, torch.logsumexp(z, 1) - z.gather(1, at)[:, 0], 0.0).sum()
+
+    want = (total(1e-4) - total(-1e-4)) / 2e-4
+    parts = [(p.gx.double() * vx), (p.gW.double() * vW), (p.gb.double() * vb)]
+    got, size = sum(t.sum() for t in parts), sum(t.abs().sum() for t in parts)
+    assert abs(float(got - want)) <= 1e-6 * float(size)
+
+
+def test_same_bits_and_other_streams(handle):
+    a, b = Problem(900, 72, 3001, BF16), Problem(500, 128, 90, BF16, 1, seed=50)
+    for p in (a, b):
+        p.forward(handle)
+        p.outputs()
+        p.backward(handle)
+    kept = [[t.clone() for t in (p.loss, p.lse, p.mean, p.gx, p.gW, p.gb)] for p in (a, b)]
+    other = heta.heta_graph_create([(1, 1, 0)], [])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for p, g, s in ((a, handle, streams[0]), (b, other, streams[1])):  # at once, each on a handle and a stream of its own
+            p.forward(g, stream=s)
+            p.backward(g, stream=s)
+    torch.cuda.synchronize()
+    for p, want in zip((a, b), kept):
+        for got, w in zip((p.loss, p.lse, p.mean, p.gx, p.gW, p.gb), want):
+            assert torch.equal(got, w)
+    other.destroy()
+
+
+def test_captured_and_replayed(handle):
+    p = Problem(800, 72, 2000, BF16)
+    p.forward(handle)
+    p.outputs()
+    p.backward(handle)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.forward(handle)
+        p.backward(handle)
+    none = torch.nonzero((p.y < 0) | (p.y >= p.classes))[:, 0]
+    for k in range(4):
+        p.x.copy_(rows(p.n, p.d, BF16, 100 + k))
+        if k == 2:
+            p.x[none[0]] = float("nan")  # found by the replay itself
+        p.forward(handle)
+        p.backward(handle)
+        want = [t.clone() for t in (p.loss, p.mean, p.gx, p.gW, p.gb)]
+        p.outputs_cleared = [t.fill_(7) for t in (p.loss, p.mean, p.gx, p.gW, p.gb)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip((p.loss, p.mean, p.gx, p.gW, p.gb), want):
+            assert torch.equal(got, w), k
