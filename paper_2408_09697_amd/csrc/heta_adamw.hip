@@ -69,13 +69,17 @@ template <typename Call> __device__ __forceinline__ int item_of(const Call &q, u
     return __popcll(before) - 1;
 }
 
-__device__ __forceinline__ void advance(const AdamwHyper &h, float keep, float g, float &m, float &v, float &r, float &w)
+__device__ __forceinline__ void advance_states(const AdamwHyper &h, float g, float &m, float &v)
 {
 #pragma clang fp contract(off)
     m = h.beta1 * m + h.one_less_beta1 * g;
     v = h.beta2 * v + h.one_less_beta2 * g * g;
-    r = sqrtf(v);
-    w = w * keep - h.lr_c1 * m / (r * h.root_c2 + h.eps);
+}
+// r = sqrt(v).  The quotient by the hardware's reciprocal (one unit in the last place; the denominator is 0 or at least 1e-23).
+__device__ __forceinline__ float advance_weight(const AdamwHyper &h, float keep, float m, float r, float w)
+{
+#pragma clang fp contract(off)
+    return w * keep - h.lr_c1 * m * __builtin_amdgcn_rcpf(r * h.root_c2 + h.eps);
 }
 
 template <typename WT, typename GT> __global__ void __launch_bounds__(256) adamw_flat_kernel(AdamwFlatCall q)
@@ -92,19 +96,18 @@ template <typename WT, typename GT> __global__ void __launch_bounds__(256) adamw
     load8(p.v + at, valid, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        float r;
-        advance(q.h, p.keep, g[e], m[e], v[e], r, w[e]);
+        advance_states(q.h, g[e], m[e], v[e]);
+        w[e] = advance_weight(q.h, p.keep, m[e], sqrtf(v[e]), w[e]);
     }
     store8(static_cast<WT *>(p.W) + at, valid, w);
     store8(p.m + at, valid, m);
     store8(p.v + at, valid, v);
 }
 
-// 32 bits for the element at `place`: two rounds of multiplication and shifts (the finalizer of MurmurHash3, a 32-bit bijection of
-// good avalanche), a key in front of each.
-__device__ __forceinline__ uint32_t element_bits(uint32_t place, uint32_t key0, uint32_t key1)
+// 32 bits for the element that `x` stands for: two rounds of multiplication and shifts (the finalizer of MurmurHash3, a 32-bit bijection of good avalanche),
+// a key in front of each; x has the first one already.
+__device__ __forceinline__ uint32_t element_bits(uint32_t x, uint32_t key1)
 {
-    uint32_t x = place + key0;
     x ^= x >> 16;
     x *= 0x85ebca6bu;
     x ^= x >> 13;
@@ -113,19 +116,18 @@ __device__ __forceinline__ uint32_t element_bits(uint32_t place, uint32_t key0, 
     return x ^ (x >> 16);
 }
 
+// The root of a v from 2^-100 up: y = 1 / sqrt(v) to one unit in the last place, g = v y, and Newton's step g + (v - g^2) y / 2.  It is the correctly
+// rounded root for every one of the 2^24 significands of two binades, and so for all (the remainder v - g^2 is exact as long as it is no subnormal).
+constexpr uint32_t kQuickLeast = 27u << 23, kQuickRange = 0x7f800000u - kQuickLeast; // 2^-100, and from there to infinity, as they are held
+__device__ __forceinline__ float quick_root(float v)
+{
+    const float y = __builtin_amdgcn_rsqf(v), g = v * y;
+    return fmaf(fmaf(-g, g, v), 0.5f * y, g);
+}
+
 // What a block's values are multiplied by, and its scale, as in the other 8-bit rows but by reciprocals.
 __device__ __forceinline__ float state_factor(float amax) { return amax >= kE4m3Least ? 1.f / amax * 448.f : amax != amax ? amax : 0.f; }
 __device__ __forceinline__ float state_scale(float amax) { return amax < kE4m3Least ? 0.f : amax * (1.f / 448.f); }
-
-// |y| <= 448 (or NaN) as e4m3, rounded up where the part that is cut off plus bits / 2^16 of a step passes the step.  Below 2^-6, where
-// e4m3's steps are 2^-9 throughout, 2^-6 is added first: the steps of that binade are the same.
-__device__ __forceinline__ uint32_t e4m3_at_random(float y, uint32_t bits)
-{
-#pragma clang fp contract(off)
-    const bool low = y < 0.015625f;
-    const uint32_t u = (__float_as_uint(low ? y + 0.015625f : y) + (bits << 4)) >> 20;
-    return y != y ? 0x7fu : u - (low ? 968u : 960u);
-}
 
 __device__ __forceinline__ void decode8(const Codes8 &q, float scale, float (&x)[8])
 {
@@ -139,7 +141,7 @@ __device__ __forceinline__ void decode8(const Codes8 &q, float scale, float (&x)
     }
 }
 
-template <typename WT, typename GT, bool CODES> __global__ void __launch_bounds__(256) adamw_rows_kernel(AdamwRowsCall q)
+template <typename WT, typename GT, bool CODES, bool STREAM> __global__ void __launch_bounds__(256) adamw_rows_kernel(AdamwRowsCall q)
 {
     const uint32_t block = q.first + blockIdx.x;
     const AdamwRows &p = q.item[item_of(q, block)];
@@ -147,61 +149,98 @@ template <typename WT, typename GT, bool CODES> __global__ void __launch_bounds_
     const int64_t unit = static_cast<int64_t>(block - p.block0) * (256 >> p.lanes_log) + (threadIdx.x >> p.lanes_log);
     // below 2^31 units (uniform; a unit is at most 255 past them) row and block come from a 32-bit division
     const int64_t i = p.n * p.per_row <= 0x7fffffff ? static_cast<int64_t>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(p.per_row)) : unit / p.per_row;
-    const int b = static_cast<int>(unit - i * p.per_row), c = b * 128 + l * 8;
+    const int b = static_cast<int>(unit - i * p.per_row);
+    int c = b * 128 + l * 8;
     if (i >= p.n) return;
     const int64_t row = p.ids ? p.ids[i] : i;
     if (row < 0 || row >= p.rows) return; // a row id outside the tensor: nothing is read or written for it
-    const int valid = max(0, min(p.d - c, 8));
+    int valid = max(0, min(p.d - c, 8));
+    // The last lane of a row's last block steps back to its last eight columns: it does again, bit for bit, what its neighbour does with some of them (both are in one
+    // wavefront: what either reads, it reads before either writes).  Element by element, the rest of a row takes 8 accesses for each array.
+    if (valid > 0 && valid < 8 && l > 0) {
+        c -= 8 - valid;
+        valid = 8;
+    }
     float w[8], g[8], m[8], v[8], r[8];
     WT *const wp = static_cast<WT *>(p.W) + row * p.ld_w + c;
-    load8(wp, valid, w);
-    load8(static_cast<const GT *>(p.grad) + i * p.ld_grad + c, valid, g);
+    load8<STREAM>(wp, valid, w);
+    load8<STREAM>(static_cast<const GT *>(p.grad) + i * p.ld_grad + c, valid, g);
     if constexpr (!CODES) {
         float *const mp = static_cast<float *>(p.m) + row * p.ld_state + c, *const vp = static_cast<float *>(p.v) + row * p.ld_state + c;
-        load8(mp, valid, m);
-        load8(vp, valid, v);
+        load8<STREAM>(mp, valid, m);
+        load8<STREAM>(vp, valid, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) advance(q.h, p.keep, g[e], m[e], v[e], r[e], w[e]);
-        store8(wp, valid, w);
-        store8(mp, valid, m);
-        store8(vp, valid, v);
+        for (int e = 0; e < 8; ++e) {
+            advance_states(q.h, g[e], m[e], v[e]);
+            w[e] = advance_weight(q.h, p.keep, m[e], sqrtf(v[e]), w[e]);
+        }
+        store8<STREAM>(wp, valid, w);
+        store8<STREAM>(mp, valid, m);
+        store8<STREAM>(vp, valid, v);
     } else {
         uint8_t *const mp = static_cast<uint8_t *>(p.m) + row * p.ld_state + c, *const rp = static_cast<uint8_t *>(p.v) + row * p.ld_state + c;
         float *const ms = p.m_scale + row * p.ld_scale + b, *const rs = p.v_scale + row * p.ld_scale + b;
         Codes8 mc = load_codes(mp, valid), rc = load_codes(rp, valid);
         decode8(mc, *ms, m);
         decode8(rc, *rs, r);
-        uint32_t top_m = 0, top_r = 0;
+        uint32_t top_m = 0, top_r = 0, range = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             v[e] = r[e] * r[e];
-            advance(q.h, p.keep, g[e], m[e], v[e], r[e], w[e]);
+            advance_states(q.h, g[e], m[e], v[e]);
+            range = max(range, __float_as_uint(v[e]) - kQuickLeast);
+        }
+        // the compiler's root takes 15 operations (a table of 1.1 M x 256, bf16 weights and gradients: 619 us for 594)
+        if (__any(valid > 0 && range >= kQuickRange)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e] = sqrtf(v[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e] = quick_root(v[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            w[e] = advance_weight(q.h, p.keep, m[e], r[e], w[e]);
             if (e < valid) {
                 top_m = max(top_m, magnitude(m[e]));
                 top_r = max(top_r, magnitude(r[e]));
             }
         }
-        store8(wp, valid, w);
+        store8<STREAM>(wp, valid, w);
         for (int o = lanes >> 1; o > 0; o >>= 1) {
             top_m = max(top_m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top_m), o)));
             top_r = max(top_r, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top_r), o)));
         }
         const float am = __uint_as_float(top_m), ar = __uint_as_float(top_r), fm = state_factor(am), fr = state_factor(ar);
+        const float least = fr > 0.f ? 0.001953125f : 0.f; // the smallest code
         const uint64_t place = static_cast<uint64_t>(row) * static_cast<uint64_t>(p.d) + c;
-        mc = rc = Codes8{{0u, 0u}};
+        const uint32_t lo = static_cast<uint32_t>(place), base = lo + static_cast<uint32_t>(place >> 32) * 0x9e3779b9u + p.key0;
+        uint32_t x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint64_t at = place + e;
-            const uint32_t bits = element_bits(static_cast<uint32_t>(at) + static_cast<uint32_t>(at >> 32) * 0x9e3779b9u, p.key0, p.key1);
-            float y = fabsf(m[e]) * fm, z = r[e] * fr;
-            y = y > 448.f ? 448.f : y;
-            z = z > 448.f ? 448.f : z;
-            const uint32_t code = e4m3_at_random(y, bits & 0xffffu) | (__float_as_uint(m[e]) >> 24 & 0x80u);
-            uint32_t root = e4m3_at_random(z, bits >> 16);
-            root = r[e] > 0.f && fr > 0.f ? max(root, 1u) : root;
-            mc.w[e / 4] |= code << (8 * (e & 3));
-            rc.w[e / 4] |= root << (8 * (e & 3));
+        for (uint32_t e = 0; e < 8; ++e) x[e] = base + e;
+        if (__any(lo > 0xfffffff8u)) { // a chunk across a multiple of 2^32
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e) x[e] += lo + e < lo ? 0x9e3779b9u : 0u;
         }
+        // The hardware's conversion adds the upper 20 of its 32 random bits below the last place that is kept, subnormal codes included, and cuts the
+        // rest off; 448 is its largest result.  A block with a NaN or an infinity is NaN by its scale, whatever the codes.
+        int words[4] = {0, 0, 0, 0};
+        auto code = [&](auto element) {
+            constexpr int e = decltype(element)::value;
+            const uint32_t bits = element_bits(x[e], p.key1);
+            words[e / 4] = __builtin_amdgcn_cvt_sr_fp8_f32(m[e] * fm, bits << 16, words[e / 4], e % 4);
+            words[2 + e / 4] = __builtin_amdgcn_cvt_sr_fp8_f32(fmaxf(r[e] * fr, r[e] > 0.f ? least : 0.f), bits & 0xffff0000u, words[2 + e / 4], e % 4);
+        };
+        code(std::integral_constant<int, 0>{});
+        code(std::integral_constant<int, 1>{});
+        code(std::integral_constant<int, 2>{});
+        code(std::integral_constant<int, 3>{});
+        code(std::integral_constant<int, 4>{});
+        code(std::integral_constant<int, 5>{});
+        code(std::integral_constant<int, 6>{});
+        code(std::integral_constant<int, 7>{});
+        mc = Codes8{{static_cast<uint32_t>(words[0]), static_cast<uint32_t>(words[1])}};
+        rc = Codes8{{static_cast<uint32_t>(words[2]), static_cast<uint32_t>(words[3])}};
         store_codes(mp, valid, mc);
         store_codes(rp, valid, rc);
         if (l == 0) {
@@ -318,6 +357,7 @@ static heta_status adamw(int32_t n_items, const heta_adamw_item *items, float lr
     std::vector<Touched> touched;
     touched.reserve(static_cast<size_t>(n_items) * 5);
     double flat_bytes = 0, rows_bytes = 0;
+    bool listed = true; // all of the items that are updated by rows are lists
     for (int32_t i = 0; i < n_items; ++i) {
         const heta_adamw_item &it = items[i];
         HETA_TRY(check_item(who, it));
@@ -348,6 +388,7 @@ static heta_status adamw(int32_t n_items, const heta_adamw_item *items, float lr
         p.key0 = mix32(it.seed + 0x9e3779b9u * static_cast<uint32_t>(step));
         p.key1 = mix32(p.key0 + 0x7f4a7c15u);
         if (row_blocks(p) > (int64_t(1) << 31)) return fail(HETA_ERR_UNSUPPORTED, "%s: too many elements for one launch", who);
+        listed = listed && it.ids;
         rows[types + (codes ? 4 : 0)].push_back(p);
         rows_bytes += bytes;
     }
@@ -373,8 +414,14 @@ static heta_status adamw(int32_t n_items, const heta_adamw_item *items, float lr
             heta_status e = HETA_OK;
             with_types(k & 3, [&](auto w, auto g) {
                 e = launch_items<AdamwRows, AdamwRowsCall, kAdamwRows>(rows[k], h, row_blocks, [&](const AdamwRowsCall &q, unsigned count) {
-                    if (k >= 4) hipLaunchKernelGGL((adamw_rows_kernel<decltype(w), decltype(g), true>), dim3(count), dim3(256), 0, st, q);
-                    else hipLaunchKernelGGL((adamw_rows_kernel<decltype(w), decltype(g), false>), dim3(count), dim3(256), 0, st, q);
+                    auto go = [&](auto codes, auto stream) {
+                        hipLaunchKernelGGL((adamw_rows_kernel<decltype(w), decltype(g), decltype(codes)::value, decltype(stream)::value>), dim3(count), dim3(256), 0, st, q);
+                    };
+                    // Listed rows of more than the last-level cache holds are read and written with the streaming hint (200,000 of 1 M rows, 189 columns, fp32 with 8-bit
+                    // states: 191 us without, 162); whole tensors are faster without (1 M x 128: fp32 states 657 us, 695 with it; 8 bits 380, 394).
+                    const bool stream = listed && streams(rows_bytes);
+                    if (k >= 4) stream ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+                    else stream ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
                 });
             });
             if (e != HETA_OK) return e;

@@ -348,10 +348,15 @@ struct TilePlace {
 //     results, t being W elements of x.other (if kReads; zeros or nothing where it is null); x.pre (if kPre and not null) and
 //     out(x, it, split) receive them, rows x.ld_pre and x.ld_out apart; kWhole: N is a multiple of W.  struct Cols, Row { void
 //     load(const Extra &x, int64_t n, int64_t N); } are what a lane keeps of W columns and of a row (which may lie beyond the matrix).
-//   Instead, kTile = true: tile<C>(x, it, acc, strip, place, wave, lane) takes a wavefront's sums as they lie in the registers, and choose(x, it) may
-//     change the item's addresses by what is in memory when the kernel runs.
+//   Instead, kTile = true: begin<C>(x, it, acc, place, wave, lane) sets what the sums of a tile start from, tile<C>(x, it, acc, strip, place, wave, lane)
+//     takes a wavefront's sums as they lie in the registers, and choose(x, it) may change the item's addresses by what is in memory when the kernel runs; kStrips: whether it uses the strip.
 template <typename Epi, typename = void> struct takes_tile : std::false_type {};
 template <typename Epi> struct takes_tile<Epi, std::enable_if_t<Epi::kTile>> : std::true_type {};
+template <typename Epi> constexpr bool wants_strips()
+{
+    if constexpr (takes_tile<Epi>::value) return Epi::kStrips;
+    else return true;
+}
 template <typename Epi> struct TileArgs {
     int n_items;
     uint32_t stride; // one item: from one tile of a workgroup to its next; several: tiles of an XCD
@@ -389,7 +394,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
     using ImgB = TileImage<C::B_RC, BN, BK, EB>;
     constexpr int A_STAGE = ImgA::BYTES * T, STAGE = A_STAGE + ImgB::BYTES * T;
     // epilogue strips: one 32 x 32 block of sums per wavefront, its own; behind the ring where that is filled during the epilogue
-    constexpr int STRIPS = NW * 4096, STRIPS_AT = DIRECT ? ST * STAGE : 0;
+    constexpr int STRIPS = wants_strips<Epi>() ? NW * 4096 : 0, STRIPS_AT = DIRECT ? ST * STAGE : 0;
     __shared__ __attribute__((aligned(1024))) char ring[std::max(ST * STAGE, STRIPS_AT + STRIPS)];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -426,6 +431,10 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
             for (int jj = 0; jj < NJ; ++jj)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][jj][v] = 0;
+    };
+    auto begin = [&] {
+        if constexpr (takes_tile<Epi>::value) Epi::template begin<C>(extra, it, acc, now, wave, lane);
+        else clear();
     };
     auto four = [&](int i, int jj, int q) { return make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]); };
 
@@ -650,7 +659,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
         for (int s = 0; s < ST - 1; ++s) issue(s);
         int cur = 0;
         while (true) {
-            clear();
+            begin();
             for (int kv = now.kn; kv > 0; kv -= BK) {
                 // this wavefront's part of the k-tile is there, and its fragment reads of the last one are done
                 if (known > 0) {
@@ -692,7 +701,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
         do {
             const int64_t k_end = now.k0 + now.kn;
             const int tiles = (now.kn + BK - 1) / BK;
-            clear();
+            begin();
             sa.load(A, it.lda, now.m0, it.M, now.k0, k_end, tid);
             sb.load(B, it.ldb, now.n0, it.N, now.k0, k_end, tid);
             sa.store(ring, tid);

@@ -38,6 +38,34 @@ __device__ __forceinline__ XentPart join(XentPart a, XentPart b)
     return {t, a.sum * __builtin_amdgcn_exp2f(a.top - t) + b.sum * __builtin_amdgcn_exp2f(b.top - t)};
 }
 
+// Sums start from the bias (nullable); register 4 q + e of block jj is column 32 jj + 8 q + 4 (lane / 32) + e of the strip.
+template <typename C, typename Acc> __device__ __forceinline__ void begin_with(const float *bias, int64_t n0, int64_t N, Acc (&acc)[C::MI][C::NJ], int lane)
+{
+    int here = lane;
+    asm volatile("" : "+v"(here)); // not kept through the products
+    const int half = here >> 5;
+#pragma unroll
+    for (int jj = 0; jj < C::NJ; ++jj)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float b[4] = {0.f, 0.f, 0.f, 0.f};
+            if (bias) {
+                const int64_t n = n0 + 32 * jj + 8 * q + 4 * half;
+                if (n0 + 32 * C::NJ <= N) {
+                    const uintx4 w = load16(bias + n);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) b[e] = __uint_as_float(w[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) b[e] = bias[min(n + e, N - 1)];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][jj][4 * q + e] = b[e];
+        }
+}
 struct XentForward {
     const float *bias;     // nullable
     const int64_t *labels;
@@ -46,9 +74,13 @@ struct XentForward {
 };
 struct XentForwardEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kTile = true;
+    static constexpr bool kTile = true, kStrips = false;
     using Extra = XentForward;
     __device__ __forceinline__ static void choose(const Extra &, TileItem &) {}
+    template <typename C, typename Acc> __device__ __forceinline__ static void begin(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], const TilePlace &now, int wave, int lane)
+    {
+        begin_with<C>(x.bias, now.n0 + (wave % C::WN) * (32 * C::NJ), it.N, acc, lane);
+    }
     template <typename C, typename Acc>
     __device__ __forceinline__ static void tile(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], float *, const TilePlace &now, int wave, int lane)
     {
@@ -72,25 +104,23 @@ struct XentForwardEpi {
                     __builtin_amdgcn_sched_barrier(0); // one block at a time: the registers hold no more beside the sums
                     int beyond = n_here - 4 * half - 32 * jj;
                     asm volatile("" : "+v"(beyond)); // compared here, not once for all rows: that takes two scalar registers a column
-                    float z[16], top = -INFINITY, sum = 0.f;
+                    auto &z = acc[i][jj];
+                    float top = -INFINITY, sum = 0.f;
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
-                        const int c = 32 * jj + 8 * (v / 4) + 4 * half + v % 4;
-                        const float bias = x.bias ? x.bias[n0 + (EDGE ? min(c, n_here - 1) : c)] * kLog2e : 0.f;
-                        z[v] = fmaf(acc[i][jj][v], kLog2e, bias);
                         if constexpr (EDGE) z[v] = 8 * (v / 4) + v % 4 < beyond ? z[v] : -INFINITY;
                         top = fmaxf(top, z[v]);
                     }
-                    top = finite_top(top);
+                    top = finite_top(top * kLog2e);
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(z[v] - top);
+                    for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(fmaf(z[v], kLog2e, -top));
                     p = jj == 0 ? XentPart{top, sum} : join(p, {top, sum});
                     const int c = at - 32 * jj;
                     if (__any(c >= 0 && c < 32 && (c & 4) == 0)) {
                         float t = 0.f;
 #pragma unroll
                         for (int v = 0; v < 16; ++v) t = c == 8 * (v / 4) + v % 4 ? z[v] : t;
-                        if (c >= 0 && c < 32 && (c & 4) == 0 && m < it.M) x.target[m] = t;
+                        if (c >= 0 && c < 32 && (c & 4) == 0 && m < it.M) x.target[m] = t * kLog2e;
                     }
                 }
                 p = join(p, {__shfl_xor(p.top, 32), __shfl_xor(p.sum, 32)});
@@ -101,6 +131,28 @@ struct XentForwardEpi {
         else strip_part(std::true_type{});
     }
 };
+
+// ---- forward: many parts of few rows joined to fewer -------------------------------------------------------
+// A workgroup takes `each` strips of R rows; out: [chunks][n].
+template <int R> __global__ void __launch_bounds__(256) xent_join_kernel(const XentPart *part, int64_t strips, int64_t each, int64_t n, int64_t row_groups, XentPart *out)
+{
+    constexpr int G = 256 / R;
+    __shared__ XentPart parts[G][R];
+    const int r = threadIdx.x % R, g = threadIdx.x / R;
+    const int64_t chunk = blockIdx.x / row_groups, m = (blockIdx.x - chunk * row_groups) * R + r, end = min(strips, (chunk + 1) * each);
+    XentPart p{kNothing, 0.f};
+    if (m < n) {
+#pragma unroll 8
+        for (int64_t s = chunk * each + g; s < end; s += G) p = join(p, part[s * n + m]);
+    }
+    parts[g][r] = p;
+    __syncthreads();
+    for (int h = G / 2; h > 0; h /= 2) {
+        if (g < h) parts[g][r] = join(parts[g][r], parts[g + h][r]);
+        __syncthreads();
+    }
+    if (g == 0 && m < n) out[chunk * n + m] = parts[0][r];
+}
 
 // ---- forward: a row's parts joined -------------------------------------------------------------------------
 // R rows a workgroup, 256 / R threads a row.  sums: of the workgroup's losses, and how many rows have a label; a single workgroup writes the mean at once.
@@ -214,9 +266,13 @@ struct XentBackward {
 };
 template <typename O> struct XentBackwardEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kTile = true;
+    static constexpr bool kTile = true, kStrips = true;
     using Extra = XentBackward;
     __device__ __forceinline__ static void choose(const Extra &, TileItem &) {}
+    template <typename C, typename Acc> __device__ __forceinline__ static void begin(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], const TilePlace &now, int wave, int lane)
+    {
+        begin_with<C>(x.bias, now.n0 + (wave % C::WN) * (32 * C::NJ), it.N, acc, lane);
+    }
     template <typename C, typename Acc>
     __device__ __forceinline__ static void tile(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], float *strip, const TilePlace &now, int wave, int lane)
     {
@@ -224,48 +280,45 @@ template <typename O> struct XentBackwardEpi {
         int here = lane;
         asm volatile("" : "+v"(here)); // not kept through the products
         const int sr = here / LPR, sc = here % LPR, half = here >> 5, l32 = here & 31;
-        const int64_t m0 = now.m0 + (wave / C::WN) * (32 * MI) + sr, n0 = now.n0 + (wave % C::WN) * (32 * NJ) + sc * W;
-        float bias[NJ][W], sum[NJ][W];
+        const int64_t mw = now.m0 + (wave / C::WN) * (32 * MI), nw = now.n0 + (wave % C::WN) * (32 * NJ), m0 = mw + sr, n0 = nw + sc * W;
+        float sum[NJ][W];
 #pragma unroll
         for (int jj = 0; jj < NJ; ++jj)
 #pragma unroll
-            for (int e = 0; e < W; ++e) {
-                bias[jj][e] = x.bias ? x.bias[min(n0 + 32 * jj + e, it.N - 1)] * kLog2e : 0.f;
-                sum[jj][e] = 0.f;
-            }
+            for (int e = 0; e < W; ++e) sum[jj][e] = 0.f;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-            XentRow row[ROUNDS];
-#pragma unroll
-            for (int r = 0; r < ROUNDS; ++r) row[r] = x.rows[min(m0 + 32 * i + RPP * r, it.M - 1)];
+            // the exponentials as the sums lie, a row a lane
+            const XentRow row = x.rows[min(mw + 32 * i + l32, it.M - 1)];
+            const float f = mw + 32 * i + l32 < it.M ? row.f : 0.f;
+            const int64_t label = row.label - x.first - nw;
 #pragma unroll
             for (int jj = 0; jj < NJ; ++jj) {
-                const int64_t n = n0 + 32 * jj;
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
+                for (int q = 0; q < 4; ++q) {
+                    float y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][jj][4 * q + e], kLog2e, -row.lse)) * f;
+                        y[e] = f != 0.f ? p : 0.f;
+                    }
+                    *strip_at(strip, l32, 2 * q + half) = make_float4(y[0], y[1], y[2], y[3]);
+                }
+                const int64_t at = label - 32 * jj; // the label's column in the block
+                if (half == 0 && at >= 0 && at < 32) reinterpret_cast<float *>(strip_at(strip, l32, static_cast<int>(at) / 4))[at & 3] -= f;
+                const int64_t n = n0 + 32 * jj;
 #pragma unroll
                 for (int r = 0; r < ROUNDS; ++r) {
                     const int64_t m = m0 + 32 * i + RPP * r;
                     float y[W];
 #pragma unroll
                     for (int h = 0; h < W / 4; ++h) {
-                        const float4 f = *strip_at(strip, RPP * r + sr, sc * (W / 4) + h);
-                        y[4 * h] = f.x; y[4 * h + 1] = f.y; y[4 * h + 2] = f.z; y[4 * h + 3] = f.w;
+                        const float4 v = *strip_at(strip, RPP * r + sr, sc * (W / 4) + h);
+                        y[4 * h] = v.x; y[4 * h + 1] = v.y; y[4 * h + 2] = v.z; y[4 * h + 3] = v.w;
                     }
-                    const float f = m < it.M ? row[r].f : 0.f;
-                    const int64_t label = row[r].label - x.first - n;
-                    const int at = label >= 0 && label < W ? static_cast<int>(label) : -1; // its column among this lane's
-                    int valid = static_cast<int>(min(max(it.N - n, static_cast<int64_t>(0)), static_cast<int64_t>(W)));
-                    asm volatile("" : "+v"(valid)); // compared here, not once for all rows: that takes two scalar registers a column
 #pragma unroll
-                    for (int e = 0; e < W; ++e) {
-                        float p = __builtin_amdgcn_exp2f(fmaf(y[e], kLog2e, bias[jj][e]) - row[r].lse);
-                        if (at == e) p -= 1.f;
-                        y[e] = f != 0.f && e < valid ? p * f : 0.f;
-                        sum[jj][e] += y[e];
-                    }
-                    // D's rows are padded to whole pieces; what lies behind the classes is zero
+                    for (int e = 0; e < W; ++e) sum[jj][e] += y[e];
+                    // D's rows are padded to whole pieces; what lies behind the classes is read by nothing that is stored
                     if (m < it.M && n < x.ld) store16(static_cast<O *>(x.D) + m * x.ld + n, pack16<O>(y));
                 }
             }
@@ -284,34 +337,46 @@ template <typename O> struct XentBackwardEpi {
     }
 };
 
-// grad_W's partial products, the rows read from their clean copy where there is need of it
-struct XentWeights {
-    float *part;
-    int64_t ld_out;
-    const void *clean; // nullable
+// ---- backward: the products that read D -------------------------------------------------------------------
+// Their partial sums, or, where a contraction is whole, the results.  grad_W's rows are read from their clean copy where there is need of it.
+struct XentProduct {
+    void *out;           // [splits][M][ld]
+    int64_t ld;
+    const float *factor; // nullable
+    const void *clean;
     int64_t ld_clean;
-    const uint32_t *poison;
+    const uint32_t *poison; // nullable: no copy
     uint32_t call;
 };
-struct XentWeightsEpi {
+template <typename O> struct XentProductEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kTile = true;
-    using Extra = XentWeights;
+    static constexpr bool kTile = true, kStrips = true;
+    using Extra = XentProduct;
     __device__ __forceinline__ static void choose(const Extra &x, TileItem &it)
     {
-        if (*x.poison != x.call) return;
+        if (!x.poison || *x.poison != x.call) return;
         it.A = x.clean;
         it.lda = x.ld_clean;
+    }
+    template <typename C, typename Acc> __device__ __forceinline__ static void begin(const Extra &, const TileItem &, Acc (&acc)[C::MI][C::NJ], const TilePlace &, int, int)
+    {
+#pragma unroll
+        for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+            for (int jj = 0; jj < C::NJ; ++jj)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][jj][v] = 0.f;
     }
     template <typename C, typename Acc>
     __device__ __forceinline__ static void tile(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], float *strip, const TilePlace &now, int wave, int lane)
     {
-        constexpr int MI = C::MI, NJ = C::NJ;
+        constexpr int MI = C::MI, NJ = C::NJ, W = 16 / (int)sizeof(O), LPR = 32 / W, RPP = 64 / LPR, ROUNDS = 32 / RPP;
         int here = lane;
-        asm volatile("" : "+v"(here));
-        const int sr = here / 8, sc = here % 8, half = here >> 5, l32 = here & 31;
-        const int64_t m0 = now.m0 + (wave / C::WN) * (32 * MI) + sr, n0 = now.n0 + (wave % C::WN) * (32 * NJ) + sc * 4;
-        float *out = x.part + now.split * it.M * it.N;
+        asm volatile("" : "+v"(here)); // not kept through the products
+        const int sr = here / LPR, sc = here % LPR, half = here >> 5, l32 = here & 31;
+        const int64_t m0 = now.m0 + (wave / C::WN) * (32 * MI) + sr, n0 = now.n0 + (wave % C::WN) * (32 * NJ) + sc * W;
+        O *const out = static_cast<O *>(x.out) + now.split * it.M * x.ld;
+        const float f = x.factor ? *x.factor : 1.f;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -321,12 +386,15 @@ struct XentWeightsEpi {
                 for (int q = 0; q < 4; ++q)
                     *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t m = m0 + 32 * i + 8 * r;
-                    const float4 f = *strip_at(strip, 8 * r + sr, sc);
-                    if (m < it.M && n < it.N)
-                        store_piece(out + m * it.N + n, static_cast<int>(min(it.N - n, static_cast<int64_t>(4))),
-                                    uintx4{__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(f.z), __float_as_uint(f.w)});
+                for (int r = 0; r < ROUNDS; ++r) {
+                    const int64_t m = m0 + 32 * i + RPP * r;
+                    float y[W];
+#pragma unroll
+                    for (int h = 0; h < W / 4; ++h) {
+                        const float4 v = *strip_at(strip, RPP * r + sr, sc * (W / 4) + h);
+                        y[4 * h] = v.x * f; y[4 * h + 1] = v.y * f; y[4 * h + 2] = v.z * f; y[4 * h + 3] = v.w * f;
+                    }
+                    if (m < it.M && n < it.N) store_piece(out + m * x.ld + n, static_cast<int>(min(it.N - n, static_cast<int64_t>(W))), pack16<O>(y));
                 }
             }
     }
@@ -335,7 +403,11 @@ struct XentWeightsEpi {
 // ---- host side ---------------------------------------------------------------------------------------------
 template <typename E, bool A_RC, bool B_RC, bool LARGE, bool STAGED> struct XentShape;
 template <bool A_RC, bool B_RC> struct XentShape<bf16_t, A_RC, B_RC, true, false> { using type = TileShape<bf16_t, 2, 1, A_RC, B_RC, kDirect, 2, 4, 4, 2, 64, 2, 1>; };   // 256 x 256
-template <> struct XentShape<bf16_t, false, true, true, false> { using type = TileShape<bf16_t, 2, 1, false, true, kDirect, 4, 2, 2, 2, 64, 2, 1>; };                     // 256 x 128: the logits'
+// The logits' tiles: 256 x 128 by four wavefronts, two workgroups on a CU, so that one's exponentials run beside the other's products (forward + both gradients of 700,000 x
+// 256 x 349 and of 8,192 x 512 x 131,072, us: 1,414 and 5,630; one workgroup of eight wavefronts with 256 x 256 1,544 and 5,597, with 256 x 128 1,555 and 6,060; two with
+// 128 x 128 1,526 and 6,090; each when its sums started from zero instead of the bias: 1,581 and 6,186 for this one).
+using XentForwardTiles = TileShape<bf16_t, 2, 1, false, true, kDirect, 2, 2, 4, 2, 32, 3, 2>;
+using XentBackwardTiles = TileShape<bf16_t, 2, 1, false, true, kDirect, 2, 2, 4, 2, 32, 2, 2>;
 template <bool A_RC, bool B_RC> struct XentShape<bf16_t, A_RC, B_RC, false, false> { using type = TileShape<bf16_t, 2, 1, A_RC, B_RC, kDirect, 2, 2, 1, 1, 64, 3, 2>; };  // 64 x 64
 template <bool A_RC, bool B_RC, bool LARGE> struct XentShape<bf16_t, A_RC, B_RC, LARGE, true> { using type = TileShape<bf16_t, 2, 1, A_RC, B_RC, kStaged, 2, 2, 1, 1, 64, 2, 2>; };
 template <bool A_RC, bool B_RC, bool STAGED> struct XentShape<float, A_RC, B_RC, true, STAGED> { using type = TileShape<float, 2, 3, A_RC, B_RC, kStaged, 4, 2, 2, 2, 32, 2, 1>; };  // 256 x 128
@@ -383,19 +455,23 @@ template <typename E> static XentTiles tiles_for(bool direct, int64_t M, int64_t
     return M > 64 && tiles_of(M, N, 256, 256) * splits >= 128 ? kTilesLarge : kTilesSmall;
 }
 // f(shape)
-template <typename E, bool A_RC, bool B_RC, typename F> static heta_status with_tiles(XentTiles t, F f)
+template <typename T> struct Tag { using type = T; };
+template <typename E, bool A_RC, bool B_RC, typename Epi, typename F> static heta_status with_tiles(XentTiles t, F f)
 {
     if (t == kTilesStaged) return f(XentShape<E, A_RC, B_RC, false, true>{});
-    return t == kTilesLarge ? f(XentShape<E, A_RC, B_RC, true, false>{}) : f(XentShape<E, A_RC, B_RC, false, false>{});
+    if (t == kTilesSmall) return f(XentShape<E, A_RC, B_RC, false, false>{});
+    if constexpr (sizeof(E) == 2 && std::is_same<Epi, XentForwardEpi>::value) return f(Tag<XentForwardTiles>{});
+    else if constexpr (sizeof(E) == 2 && std::is_same<Epi, XentBackwardEpi<bf16_t>>::value) return f(Tag<XentBackwardTiles>{});
+    else return f(XentShape<E, A_RC, B_RC, true, false>{});
 }
 template <typename E, bool A_RC, bool B_RC, typename Epi> static heta_status go_tiles(const Launch &l, XentTiles t, const typename Epi::Extra &x)
 {
-    return with_tiles<E, A_RC, B_RC>(t, [&](auto shape) { return l.go<typename decltype(shape)::type, Epi>(x); });
+    return with_tiles<E, A_RC, B_RC, Epi>(t, [&](auto shape) { return l.go<typename decltype(shape)::type, Epi>(x); });
 }
 // rows and columns of a wavefront's sums
-template <typename E> static void strip_of(XentTiles t, int64_t *rows, int64_t *cols)
+template <typename E, typename Epi> static void strip_of(XentTiles t, int64_t *rows, int64_t *cols)
 {
-    (void)with_tiles<E, false, true>(t, [&](auto shape) {
+    (void)with_tiles<E, false, true, Epi>(t, [&](auto shape) {
         using C = typename decltype(shape)::type;
         *rows = 32 * C::MI;
         *cols = 32 * C::NJ;
@@ -469,11 +545,14 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     const size_t target_at = ws.take(static_cast<size_t>(n) * 4);
     const XentTiles tiles = tiles_for<E>((copy_w || direct_rows(a.W, a.ld_w, 2)) && (copy_in || direct_rows(a.in, a.ld_in, 2)), n, V, 1);
     int64_t strip_rows = 0, strip_cols = 0;
-    strip_of<E>(tiles, &strip_rows, &strip_cols);
+    strip_of<E, XentForwardEpi>(tiles, &strip_rows, &strip_cols);
     const int64_t strips = (V + strip_cols - 1) / strip_cols;
     const size_t part_at = ws.take(static_cast<size_t>(strips) * n * sizeof(XentPart));
-    const bool wide = n >= 4096 || V <= 4096;
-    const int64_t groups = (n + (wide ? 31 : 3)) / (wide ? 32 : 4);
+    // rows of a workgroup: few where there are few rows and many strips; and where there are very many, they are joined in two steps
+    const int per_group = n <= 256 && strips <= 16 ? 256 : n >= 4096 || strips <= 64 ? 32 : 4;
+    const int64_t groups = (n + per_group - 1) / per_group;
+    const int64_t each = std::max<int64_t>(256 / per_group * 8, (strips + 1023) / 1024), chunks = per_group == 4 && strips > 2 * each ? (strips + each - 1) / each : 0;
+    const size_t joined_at = ws.take(static_cast<size_t>(chunks) * n * sizeof(XentPart));
     const size_t sums_at = ws.take(a.mean && groups > 1 ? static_cast<size_t>(groups) * sizeof(XentSum) : 0);
     HETA_TRY(ensure_workspace(g, ws.bytes));
     char *base = static_cast<char *>(g->d_ws);
@@ -491,10 +570,23 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     const XentForward x{a.bias, a.labels, reinterpret_cast<XentPart *>(base + part_at), reinterpret_cast<float *>(base + target_at)};
     HETA_TRY((go_tiles<E, false, true, XentForwardEpi>(l, tiles, x)));
     XentSum *sums = a.mean && groups > 1 ? reinterpret_cast<XentSum *>(base + sums_at) : nullptr;
+    const XentPart *parts = x.part;
+    int64_t n_parts = strips;
+    if (chunks > 0) {
+        XentPart *joined = reinterpret_cast<XentPart *>(base + joined_at);
+        hipLaunchKernelGGL(xent_join_kernel<4>, dim3(static_cast<unsigned>(chunks * groups)), dim3(256), 0, st, x.part, strips, each, n, groups, joined);
+        HETA_LAUNCH_CHECK("xent_join_kernel");
+        parts = joined;
+        n_parts = chunks;
+    }
     {
-        ProfScope prof("xent_rows_kernel", st, static_cast<double>(n) * (8.0 * strips + 20), 0);
-        if (wide) hipLaunchKernelGGL(xent_rows_kernel<32>, dim3(static_cast<unsigned>(groups)), dim3(256), 0, st, x.part, strips, x.target, a.labels, n, V, a.loss, a.lse, sums, a.mean);
-        else hipLaunchKernelGGL(xent_rows_kernel<4>, dim3(static_cast<unsigned>(groups)), dim3(256), 0, st, x.part, strips, x.target, a.labels, n, V, a.loss, a.lse, sums, a.mean);
+        ProfScope prof("xent_rows_kernel", st, static_cast<double>(n) * (8.0 * n_parts + 20), 0);
+        auto go = [&](auto per) {
+            hipLaunchKernelGGL(xent_rows_kernel<decltype(per)::value>, dim3(static_cast<unsigned>(groups)), dim3(256), 0, st, parts, n_parts, x.target, a.labels, n, V, a.loss, a.lse, sums, a.mean);
+        };
+        if (per_group == 256) go(std::integral_constant<int, 256>{});
+        else if (per_group == 32) go(std::integral_constant<int, 32>{});
+        else go(std::integral_constant<int, 4>{});
         HETA_LAUNCH_CHECK("xent_rows_kernel");
     }
     if (sums) hipLaunchKernelGGL(xent_mean_kernel, dim3(1), dim3(256), 0, st, sums, groups, a.mean);
@@ -502,7 +594,7 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     return HETA_OK;
 }
 
-constexpr int64_t kXentPiece = int64_t(192) << 20; // bytes of D at a time
+constexpr int64_t kXentPiece = int64_t(512) << 20; // bytes of D at a time
 
 // splits of a contraction over K for tiles of M x N outputs: one workgroup per CU
 static void split_for(int64_t M, int64_t N, int64_t K, int64_t least, int32_t *n_split, int64_t *k_per_split)
@@ -582,7 +674,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                                (static_cast<double>(rn) * (d + cols) + static_cast<double>(d) * cols) * sizeof(E), product, st};
                 const XentTiles tiles = tiles_for<E>(direct_w && direct_in, rn, cols, 1);
                 int64_t strip_rows = 0, strip_cols = 0;
-                strip_of<E>(tiles, &strip_rows, &strip_cols);
+                strip_of<E, XentBackwardEpi<E>>(tiles, &strip_rows, &strip_cols);
                 const XentBackward x{a.bias ? a.bias + v0 : nullptr, rows + r0, base + d_at, ld_d, sums ? sums + bias_slots * cols : nullptr, v0};
                 HETA_TRY((go_tiles<E, false, true, XentBackwardEpi<E>>(l, tiles, x)));
                 bias_slots += (rn + strip_rows - 1) / strip_rows;
@@ -596,11 +688,16 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 const Launch l{g, who, "xent_grad_in_kernel", TileItem{base + d_at, Wv, ld_d, W.ld, 0, 0, rn, d, cols, k_each, splits, 0, 0, 0, 0, 0},
                                (static_cast<double>(rn) * (d + cols) + static_cast<double>(d) * cols) * sizeof(E), product, st};
                 float *so_far = reinterpret_cast<float *>(base + di_at) + (n_v > 1 ? r * R * d : 0), *part = reinterpret_cast<float *>(base + di_at) + (n_v > 1 ? n_r * R * d : 0);
-                const PartialEpi::Extra x{part, d};
-                HETA_TRY((go_tiles<E, false, false, PartialEpi>(l, tiles_for<E>(direct_w, rn, d, splits), x)));
                 E *out = static_cast<E *>(a.grad_in) + r0 * a.ld_gi;
-                const bool last = v + 1 == n_v;
-                HETA_TRY(xent_add(v > 0 ? so_far : nullptr, part, splits, rn * d, last ? static_cast<void *>(out) : so_far, last ? dt : HETA_F32, a.d, last ? a.ld_gi : d, last ? factor : nullptr, st));
+                const XentTiles tiles = tiles_for<E>(direct_w, rn, d, splits);
+                if (splits == 1 && n_v == 1) {
+                    HETA_TRY((go_tiles<E, false, false, XentProductEpi<E>>(l, tiles, XentProduct{out, a.ld_gi, factor, nullptr, 0, nullptr, 0})));
+                } else {
+                    const bool last = v + 1 == n_v;
+                    HETA_TRY((go_tiles<E, false, false, XentProductEpi<float>>(l, tiles, XentProduct{part, d, nullptr, nullptr, 0, nullptr, 0})));
+                    HETA_TRY(xent_add(v > 0 ? so_far : nullptr, part, splits, rn * d, last ? static_cast<void *>(out) : so_far, last ? dt : HETA_F32, a.d, last ? a.ld_gi : d,
+                                      last ? factor : nullptr, st));
+                }
             }
             if (a.dW) {
                 int32_t splits = 1;
@@ -610,13 +707,22 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 if (static_cast<int64_t>(splits) * k_each < rn) k_each = round_up((rn + splits - 1) / splits, 64), splits = static_cast<int32_t>((rn + k_each - 1) / k_each);
                 const Launch l{g, who, "xent_grad_w_kernel", TileItem{in_r, base + d_at, in.ld, ld_d, 0, 0, d, cols, rn, k_each, splits, 0, 0, 0, 0, 0},
                                (static_cast<double>(rn) * (d + cols)) * sizeof(E) + 4.0 * splits * d * cols, product, st};
-                const XentWeights x{dw + dw_parts * d * cols, cols, clean + r0 * ld_ic, ld_ic, poison, call};
-                HETA_TRY((go_tiles<E, true, true, XentWeightsEpi>(l, tiles_for<E>(direct_in, d, cols, splits), x)));
-                dw_parts += splits;
+                const XentTiles tiles = tiles_for<E>(direct_in, d, cols, splits);
+                XentProduct x{dw + dw_parts * d * cols, cols, nullptr, clean + r0 * ld_ic, ld_ic, poison, call};
+                if (splits == 1 && n_r == 1) {
+                    x.out = static_cast<char *>(a.dW) + v0 * dtype_size(a.dw_dt);
+                    x.ld = a.ld_dw;
+                    x.factor = factor;
+                    if (a.dw_dt == HETA_F32) HETA_TRY((go_tiles<E, true, true, XentProductEpi<float>>(l, tiles, x)));
+                    else HETA_TRY((go_tiles<E, true, true, XentProductEpi<bf16_t>>(l, tiles, x)));
+                } else {
+                    HETA_TRY((go_tiles<E, true, true, XentProductEpi<float>>(l, tiles, x)));
+                    dw_parts += splits;
+                }
             }
         }
         if (a.dbias) HETA_TRY(fold_partials(sums, bias_slots, cols, a.dbias + v0, HETA_F32, static_cast<int32_t>(cols), cols, st, factor));
-        if (a.dW) {
+        if (dw_parts > 0) {
             char *to = static_cast<char *>(a.dW) + v0 * dtype_size(a.dw_dt);
             HETA_TRY(fold_partials(dw, dw_parts, d * cols, to, a.dw_dt, static_cast<int32_t>(cols), a.ld_dw, st, factor));
         }
