@@ -646,7 +646,8 @@ heta_status heta_rms_norm_bwd(heta_graph *g, int64_t n_rows, int32_t d, const vo
  *   bias: device fp32 [d_out] or NULL; residual: out_dt [n_rows, ld_res] or NULL, may be out; pre (NULL: not stored) receives
  *   the pre-activation in out_dt, which heta_linear_bwd reads.
  * Infinite fp32 operands give what the definition gives (infinity times 0 is NaN).
- * g: handle whose workspace the call may use (and grow, by up to 4 MB). */
+ * g: handle whose workspace the call may use (and grow, by up to 4 MB; HETA_I8 by copies of up to 1 GiB of operands whose rows are not 16-byte aligned, where there
+ * is room). */
 typedef struct heta_linear_args {
     int64_t n_rows;
     int32_t d_in, d_out;

@@ -236,7 +236,7 @@ template <typename F> inline heta_status with_act(int a, F f)
 heta_status launch_linear_f32(const Launch &l, bool input_gradient, const LinearExtra &x);
 heta_status launch_linear_bf16(const Launch &l, bool input_gradient, heta_dtype out_dt, const LinearExtra &x);
 heta_status launch_linear_e4m3(const Launch &l, heta_dtype out_dt, bool coarse, const LinearExtra &x);
-heta_status launch_linear_i8(const Launch &l, heta_dtype out_dt, const LinearExtra &x);
+heta_status launch_linear_i8(Launch l, heta_dtype out_dt, const LinearExtra &x);
 heta_status launch_grad_w_f32(const Launch &l, float *part);
 // Bytes of the copies, in aligned rows, of the operands of a large weight gradient whose rows start anywhere (0: none are worth it), and
 // the copies themselves, `to` (256-byte aligned) that many bytes of the workspace.
