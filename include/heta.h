@@ -620,7 +620,7 @@ heta_status heta_sparse_adam_multi(int32_t n_items, const heta_adam_item *items,
  *   rstd: device fp32 [n_rows] (NULL: not stored).  sum may be x or residual (same rows).
  *   out: x_dt, or bf16, or HETA_E4M3: then scale (device fp32 [n_rows], otherwise NULL) receives
  *   max_j |out_ij| / 448 and out holds the nearest 8-bit values of out / scale (a row of zeros, or of nothing from 2^-119 on:
- *   zeros, scale 0; a row with a NaN among its outputs: NaN throughout, scale too).
+ *   zeros, scale 0; a row with a NaN among its outputs: NaN throughout, scale too); or HETA_I8: scale and out as heta_linear_rows_i8 makes them of the outputs.
  *   bf16 rows have no fp32 output.  Sums are fp32: with eps = 0 a row whose squares add up to 0 there has rstd 0 and zeros as outputs; one
  *   whose squares pass 3.4e38 has rstd 0, too. */
 heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, const void *residual, int64_t ld_res,
@@ -744,7 +744,7 @@ heta_status heta_linear_xent(heta_graph *g, const heta_linear_xent_args *args, v
  *   grad_in = D . W^T (dt);   dW = in^T . D (dw_dt: fp32, or bf16 for bf16 operands);   dbias[j] = sum_i D_ij (fp32)      each NULL: not computed
  * grad_loss: device fp32 [n_rows] or NULL; mean: what the forward wrote (gradients of the mean) or NULL (of the sum).  All outputs are overwritten; sums
  * are added in a fixed order.  The products read D rounded to dt.  The logits are formed again.
- * Uses the handle's workspace (may grow it: by 192 MB of D or D itself where that is less, a copy of the rows, partial sums of the gradients, and copies as
+ * Uses the handle's workspace (may grow it: by 512 MB of D or D itself where that is less, a copy of the rows, partial sums of the gradients, and copies as
  * above). */
 typedef struct heta_linear_xent_bwd_args {
     int64_t n_rows;

@@ -976,7 +976,7 @@ def heta_rms_norm(x: torch.Tensor, out: torch.Tensor, residual: Optional[torch.T
                   gamma: Optional[torch.Tensor] = None, eps: float = 1e-6, scale: Optional[torch.Tensor] = None,
                   rstd: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """sum = x + residual; out = sum * rstd * gamma with rstd = 1 / sqrt(mean(sum^2) + eps), per row.  out: x's type, bf16, or
-    torch.float8_e4m3fn with `scale` (one per row)."""
+    torch.float8_e4m3fn or torch.int8 with `scale` (one per row)."""
     t = x.dtype
     n, d = x.shape
     px, lx = _rows_of(x, "x", t, n, d)
@@ -1136,12 +1136,10 @@ class AdamwPlan:
 def _adamw_item(W, state, grad, weight_decay=0.0, ids=None, seed=0) -> bytes:
     as_rows = lambda t: t.unsqueeze(0) if t is not None and t.dim() == 1 else t  # noqa: E731
     W, grad = as_rows(W), as_rows(grad)
-    pw, lw, rows, d = _mat(W, "W", W.dtype)
-    pg, lg, n, dg = _mat(grad, "grad", grad.dtype)
-    if dg != d:
-        raise HetaError(HETA_ERR_SHAPE, f"grad must be {d} wide, got {dg}")
-    if ids is None and n != rows:
-        raise HetaError(HETA_ERR_SHAPE, f"grad must have {rows} rows without ids, got {n}")
+    rows, d = W.shape
+    n = rows if ids is None else grad.shape[0]
+    pw, lw = _rows_of(W, "W", W.dtype, rows, d)
+    pg, lg = _rows_of(grad, "grad", grad.dtype, n, d)
     pi = 0
     if ids is not None:
         pi, got = _vec(ids, "ids", torch.int64)

@@ -2,7 +2,7 @@
 // with a scale a row for products of 8-bit operands.
 //
 //     s = round(x + residual) (stored if asked for),  rstd = (sum_j s_j^2 / d + eps)^(-1/2),  out = s rstd gamma
-//     8-bit: scale = max_j |out_j| / 448,  q = e4m3(out / scale); a row of zeros has scale 0
+//     8-bit: scale = max_j |out_j| / 448,  q = e4m3(out / scale), or / 127 and whole numbers; a row of zeros has scale 0
 //     h = s rstd, w = grad_out gamma:  grad_x = rstd (w - h sum_j(w_j h_j) / d) + grad_sum,  grad_gamma = sum over rows of grad_out h
 //
 // HBM-bound: six to nine operations per element that is read.  One pass: a row lives in the registers of 8 to 64 lanes
@@ -11,6 +11,7 @@
 // grad_gamma: every lane adds up its columns over the rows it visits, a workgroup joins its groups of lanes through LDS in
 // order, and the workgroups' partial sums are added in a fixed order: no atomics.
 #include <algorithm>
+#include <type_traits>
 
 #include "heta_rows.h"
 
@@ -177,7 +178,23 @@ __device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d
     const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
 }
-template <int LANES, int NV, int P> __device__ __forceinline__ void store_row_e4m3(uint8_t *row, int d, int l, const float (&x)[NV][8], float f)
+// O of an 8-bit output: uint8_t for e4m3, int8_t for whole numbers
+template <typename O> __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d)
+{
+    if constexpr (std::is_same<O, int8_t>::value) return four_i8(a, b, c, d);
+    else return four_e4m3(a, b, c, d);
+}
+template <typename O> __device__ __forceinline__ float codes_factor(float amax)
+{
+    if constexpr (std::is_same<O, int8_t>::value) return i8_factor(amax);
+    else return e4m3_factor(amax);
+}
+template <typename O> __device__ __forceinline__ float codes_scale(float amax)
+{
+    if constexpr (std::is_same<O, int8_t>::value) return i8_scale(amax);
+    else return e4m3_scale(amax);
+}
+template <typename O, int LANES, int NV, int P> __device__ __forceinline__ void store_row_codes(uint8_t *row, int d, int l, const float (&x)[NV][8], float f)
 {
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -186,7 +203,7 @@ template <int LANES, int NV, int P> __device__ __forceinline__ void store_row_e4
             const int c = column<LANES, P>(v, h, l);
             uint32_t w[P / 4];
 #pragma unroll
-            for (int j = 0; j < P / 4; ++j) w[j] = four_e4m3(x[v][h + 4 * j] * f, x[v][h + 4 * j + 1] * f, x[v][h + 4 * j + 2] * f, x[v][h + 4 * j + 3] * f);
+            for (int j = 0; j < P / 4; ++j) w[j] = four_codes<O>(x[v][h + 4 * j] * f, x[v][h + 4 * j + 1] * f, x[v][h + 4 * j + 2] * f, x[v][h + 4 * j + 3] * f);
             if (c + P <= d) {
                 store_words<P / 4, false>(row + c, w);
             } else {
@@ -203,7 +220,7 @@ template <typename T> __device__ __forceinline__ float rounded(float v)
     else return v;
 }
 
-// T: type of x, residual and sum; O: of the output (uint8_t: e4m3)
+// T: type of x, residual and sum; O: of the output
 template <typename T, typename O, int LANES, int NV, int P, bool TAIL, bool STREAM> __global__ void __launch_bounds__(256) rms_norm_kernel(NormFwd p)
 {
     constexpr int GROUPS = 256 / LANES;
@@ -246,8 +263,8 @@ template <typename T, typename O, int LANES, int NV, int P, bool TAIL, bool STRE
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = max(top, magnitude(x[v][e]));
             const float amax = __uint_as_float(lanes_max<LANES>(top));
-            if (l == 0) p.scale[r] = e4m3_scale(amax);
-            store_row_e4m3<LANES, NV, P>(static_cast<uint8_t *>(p.out) + r * p.ld_out, p.d, l, x, e4m3_factor(amax));
+            if (l == 0) p.scale[r] = codes_scale<O>(amax);
+            store_row_codes<O, LANES, NV, P>(static_cast<uint8_t *>(p.out) + r * p.ld_out, p.d, l, x, codes_factor<O>(amax));
         } else {
             store_row<LANES, NV, P, TAIL, STREAM>(static_cast<O *>(p.out) + r * p.ld_out, p.d, l, x);
         }
@@ -299,11 +316,11 @@ template <typename T, typename O> __global__ void __launch_bounds__(256) rms_nor
             uint32_t top = 0;
             for (int c = threadIdx.x; c < p.d; c += 256) top = max(top, magnitude(value(c)));
             const float amax = group_max(top, lds);
-            if (threadIdx.x == 0) p.scale[r] = e4m3_scale(amax);
-            const float f = e4m3_factor(amax);
+            if (threadIdx.x == 0) p.scale[r] = codes_scale<O>(amax);
+            const float f = codes_factor<O>(amax);
             for (int c = threadIdx.x; c < p.d; c += 256) {
                 const float v = value(c) * f;
-                (static_cast<uint8_t *>(p.out) + r * p.ld_out)[c] = static_cast<uint8_t>(__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false) & 0xff);
+                (static_cast<uint8_t *>(p.out) + r * p.ld_out)[c] = static_cast<uint8_t>(four_codes<O>(v, 0.f, 0.f, 0.f) & 0xff);
             }
         } else {
             O *out = static_cast<O *>(p.out) + r * p.ld_out;
@@ -496,9 +513,9 @@ extern "C" heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, h
     const char *who = "heta_rms_norm";
     if (n_rows < 0 || d <= 0) return fail(HETA_ERR_SHAPE, "%s: need n_rows >= 0 and d > 0", who);
     if (d > kWidest) return fail(HETA_ERR_UNSUPPORTED, "%s: rows too wide", who);
-    if (!valid_dtype(x_dt) || (!valid_dtype(out_dt) && out_dt != HETA_E4M3)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (!valid_dtype(x_dt) || (!valid_dtype(out_dt) && out_dt != HETA_E4M3 && out_dt != HETA_I8)) return fail(HETA_ERR_INVALID_ARG, "%s: bad dtype", who);
     if (!(eps >= 0.f)) return fail(HETA_ERR_INVALID_ARG, "%s: need eps >= 0", who);
-    const bool q = out_dt == HETA_E4M3;
+    const bool q = out_dt == HETA_E4M3 || out_dt == HETA_I8;
     if (x_dt == HETA_BF16 && out_dt == HETA_F32) return fail(HETA_ERR_UNSUPPORTED, "%s: bf16 rows have a bf16 or an 8-bit output", who);
     if (q != (scale != nullptr) && !(q && n_rows == 0)) return fail(HETA_ERR_INVALID_ARG, "%s: scales belong to an 8-bit output, and that needs them", who);
     const size_t esz = dtype_size(x_dt), osz = q ? 1 : dtype_size(out_dt);
@@ -527,11 +544,13 @@ extern "C" heta_status heta_rms_norm(int64_t n_rows, int32_t d, const void *x, h
     const bool stream = streams(bytes);
     ProfScope prof("rms_norm_kernel", st, bytes, 6.0 * n_rows * d);
     if (x_dt == HETA_F32) {
-        if (q) launch_norm<float, uint8_t>(p, stream, st);
+        if (out_dt == HETA_I8) launch_norm<float, int8_t>(p, stream, st);
+        else if (q) launch_norm<float, uint8_t>(p, stream, st);
         else if (out_dt == HETA_F32) launch_norm<float, float>(p, stream, st);
         else launch_norm<float, bf16_t>(p, stream, st);
     } else {
-        if (q) launch_norm<bf16_t, uint8_t>(p, stream, st);
+        if (out_dt == HETA_I8) launch_norm<bf16_t, int8_t>(p, stream, st);
+        else if (q) launch_norm<bf16_t, uint8_t>(p, stream, st);
         else launch_norm<bf16_t, bf16_t>(p, stream, st);
     }
     HETA_LAUNCH_CHECK("rms_norm_kernel");

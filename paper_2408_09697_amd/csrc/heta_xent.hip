@@ -6,8 +6,9 @@
 // Forward: the product of heta_tiles.h with an epilogue that leaves, of a row's logits in a wavefront's columns, their largest and the sum of
 // the exponentials below it, 8 bytes for 64 logits; a second kernel joins a row's.  The label's logit is taken from the registers it is in.
 // Backward: the logits are formed again (2 d operations each; kept in 4 bytes they would cost as long to write and read at d = 1,024 and
-// longer below), their epilogue makes D of them, and two products read D.  D is made in pieces that the last-level cache holds:
-// Rows x Classes of about a square, since every further piece along the classes adds n d partial sums of grad_in, and every one along the rows d V of grad_W.
+// longer below), their epilogue makes D of them, and two products read D.  D is made in pieces of 512 MB, of about as many rows as classes,
+// since every further piece along the classes adds n d partial sums of grad_in, and every one along the rows d V of grad_W (192 MB, which the last-level cache holds: the products
+// read it a third faster, but there are more of them, split further; 8,192 x 512 x 131,072 5,823 us for 5,419; 256 MB 6,112, 768 MB 6,110).
 // D is stored in the operands' type: the matrix instruction reads 16 bits, and its rounding (2^-9 of each D, to and fro) is below that of a gradient
 // in 16 bits.  F, which all rows share (scale, over the number of labelled rows), multiplies the sums: in D, its rounding would be the same for all labels' elements
 // (8,192 x 512 x 131,072: gradients 3.7e-3 of their norm off, 1.7e-3 this way, their own rounding).  grad_bias is added up from the unrounded D in the epilogue's registers.
@@ -132,6 +133,20 @@ struct XentForwardEpi {
     }
 };
 
+// Row m's parts of every G-th strip from `first` on, eight loads in flight.
+template <int G> __device__ __forceinline__ XentPart join_strips(const XentPart *part, int64_t first, int64_t end, int64_t n, int64_t m)
+{
+    XentPart p{kNothing, 0.f};
+    for (int64_t s = first; s < end; s += 8 * G) {
+        XentPart q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) q[u] = s + u * G < end ? part[(s + u * G) * n + m] : XentPart{kNothing, 0.f};
+#pragma unroll
+        for (int u = 0; u < 8; ++u) p = join(p, q[u]);
+    }
+    return p;
+}
+
 // ---- forward: many parts of few rows joined to fewer -------------------------------------------------------
 // A workgroup takes `each` strips of R rows; out: [chunks][n].
 template <int R> __global__ void __launch_bounds__(256) xent_join_kernel(const XentPart *part, int64_t strips, int64_t each, int64_t n, int64_t row_groups, XentPart *out)
@@ -141,10 +156,7 @@ template <int R> __global__ void __launch_bounds__(256) xent_join_kernel(const X
     const int r = threadIdx.x % R, g = threadIdx.x / R;
     const int64_t chunk = blockIdx.x / row_groups, m = (blockIdx.x - chunk * row_groups) * R + r, end = min(strips, (chunk + 1) * each);
     XentPart p{kNothing, 0.f};
-    if (m < n) {
-#pragma unroll 8
-        for (int64_t s = chunk * each + g; s < end; s += G) p = join(p, part[s * n + m]);
-    }
+    if (m < n) p = join_strips<G>(part, chunk * each + g, end, n, m);
     parts[g][r] = p;
     __syncthreads();
     for (int h = G / 2; h > 0; h /= 2) {
@@ -173,10 +185,7 @@ template <int R> __global__ void __launch_bounds__(256) xent_rows_kernel(const X
     const int r = threadIdx.x % R, g = threadIdx.x / R;
     const int64_t m = static_cast<int64_t>(blockIdx.x) * R + r;
     XentPart p{kNothing, 0.f};
-    if (m < n) {
-#pragma unroll 4
-        for (int64_t s = g; s < strips; s += G) p = join(p, part[s * n + m]);
-    }
+    if (m < n) p = join_strips<G>(part, g, strips, n, m);
     parts[g][r] = p;
     __syncthreads();
     for (int h = G / 2; h > 0; h /= 2) {
@@ -402,7 +411,11 @@ template <typename O> struct XentProductEpi {
 
 // ---- host side ---------------------------------------------------------------------------------------------
 template <typename E, bool A_RC, bool B_RC, bool LARGE, bool STAGED> struct XentShape;
-template <bool A_RC, bool B_RC> struct XentShape<bf16_t, A_RC, B_RC, true, false> { using type = TileShape<bf16_t, 2, 1, A_RC, B_RC, kDirect, 2, 4, 4, 2, 64, 2, 1>; };   // 256 x 256
+// grad_in's 256 x 256 (8,192 x 512 x 32,768 and 700,000 x 256 x 349, us: 337 and 282; 256 x 128 by two workgroups a CU 387 and 348, 256 x 128 by one 460 and 377, four wavefronts with
+// 128 x 128 each 313 and 326) and grad_W's, whose operands are both read transposed, 256 x 128 by two workgroups a CU, a wavefront 64 x 128 (261 and 219; 256 x 256 320 and 248, 64
+// columns a wavefront 331 and 256).
+template <> struct XentShape<bf16_t, false, false, true, false> { using type = TileShape<bf16_t, 2, 1, false, false, kDirect, 2, 4, 4, 2, 64, 2, 1>; };
+template <> struct XentShape<bf16_t, true, true, true, false> { using type = TileShape<bf16_t, 2, 1, true, true, kDirect, 4, 1, 2, 4, 32, 2, 2>; };
 // The logits' tiles: 256 x 128 by four wavefronts, two workgroups on a CU, so that one's exponentials run beside the other's products (forward + both gradients of 700,000 x
 // 256 x 349 and of 8,192 x 512 x 131,072, us: 1,414 and 5,630; one workgroup of eight wavefronts with 256 x 256 1,544 and 5,597, with 256 x 128 1,555 and 6,060; two with
 // 128 x 128 1,526 and 6,090; each when its sums started from zero instead of the bias: 1,581 and 6,186 for this one).
@@ -521,6 +534,22 @@ template <typename O> __global__ void __launch_bounds__(256) xent_add_kernel(con
         }
     }
 }
+// Sums of D's columns over the strips of rows: where there are many, first over `each` of them at a time.  part: [slots][cols], out: [chunks][cols].
+__global__ void __launch_bounds__(256) xent_column_sums_kernel(const float *part, int64_t slots, int64_t each, int64_t cols, int64_t column_groups, float *out)
+{
+    const int64_t chunk = blockIdx.x / column_groups, c = (blockIdx.x - chunk * column_groups) * 256 + threadIdx.x, end = min(slots, (chunk + 1) * each);
+    if (c >= cols) return;
+    float y = 0.f;
+    for (int64_t s = chunk * each; s < end; s += 8) {
+        float q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) q[u] = s + u < end ? part[(s + u) * cols + c] : 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) y += q[u];
+    }
+    out[chunk * cols + c] = y;
+}
+
 static heta_status xent_add(const float *so_far, const float *part, int splits, int64_t total, void *out, heta_dtype dt, int32_t width, int64_t ld, const float *factor, hipStream_t st)
 {
     const int64_t blocks = (total + 1023) / 1024;
@@ -549,7 +578,7 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     const int64_t strips = (V + strip_cols - 1) / strip_cols;
     const size_t part_at = ws.take(static_cast<size_t>(strips) * n * sizeof(XentPart));
     // rows of a workgroup: few where there are few rows and many strips; and where there are very many, they are joined in two steps
-    const int per_group = n <= 256 && strips <= 16 ? 256 : n >= 4096 || strips <= 64 ? 32 : 4;
+    const int per_group = strips <= 16 ? 256 : n >= 4096 || strips <= 64 ? 32 : 4;
     const int64_t groups = (n + per_group - 1) / per_group;
     const int64_t each = std::max<int64_t>(256 / per_group * 8, (strips + 1023) / 1024), chunks = per_group == 4 && strips > 2 * each ? (strips + each - 1) / each : 0;
     const size_t joined_at = ws.take(static_cast<size_t>(chunks) * n * sizeof(XentPart));
@@ -621,7 +650,9 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
         R = std::min(R, n);
         Vc = std::min(Vc, V);
     }
-    const int64_t n_r = (n + R - 1) / R, n_v = (V + Vc - 1) / Vc, ld_d = round_up(Vc, 8);
+    const int64_t n_r = (n + R - 1) / R, n_v = (V + Vc - 1) / Vc;
+    // rows of D an odd number of 128 bytes apart (8,192 x 512 x 130,072: 5,760 us at 65,536 bytes, 5,515)
+    const int64_t ld_d = round_up(Vc, 8) + (round_up(Vc, 8) * static_cast<int64_t>(sizeof(E)) % 1024 == 0 ? 64 : 0);
     const bool copy_w = bf16 && copies_pay(n) && !direct_rows(a.W, a.ld_w, 2), copy_in = bf16 && copies_pay(n) && !direct_rows(a.in, a.ld_in, 2);
     const int64_t ld_wc = round_up(V, 8), ld_ic = round_up(d, 8);
     int32_t in_splits = 1, w_splits = 1;
@@ -634,6 +665,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
     const size_t w_at = ws.take(copy_w ? static_cast<size_t>(d) * ld_wc * 2 : 0), in_at = ws.take(a.dW ? static_cast<size_t>(n) * ld_ic * sizeof(E) : copy_in ? static_cast<size_t>(n) * ld_ic * 2 : 0);
     const size_t d_at = ws.take(static_cast<size_t>(R) * ld_d * sizeof(E));
     const size_t sums_at = ws.take(a.dbias ? static_cast<size_t>((R + 31) / 32 * n_r) * Vc * 4 : 0);
+    const size_t joined_at = ws.take(a.dbias ? static_cast<size_t>(64) * Vc * 4 : 0);
     const size_t dw_at = ws.take(a.dW ? static_cast<size_t>(w_splits) * n_r * d * Vc * 4 : 0);
     // grad_in's sums over the classes so far, and in front of each piece's partial products
     const size_t di_at = ws.take(a.grad_in ? static_cast<size_t>(in_splits + (n_v > 1 ? n_r : 0)) * R * d * 4 : 0);
@@ -721,7 +753,17 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 }
             }
         }
-        if (a.dbias) HETA_TRY(fold_partials(sums, bias_slots, cols, a.dbias + v0, HETA_F32, static_cast<int32_t>(cols), cols, st, factor));
+        const float *bias_parts = sums;
+        if (a.dbias && bias_slots > 256) { // 5,469 strips of 349 columns: 27 us in one step, few workgroups of which have columns
+            const int64_t each = (bias_slots + 63) / 64, groups = (cols + 255) / 256;
+            float *joined = reinterpret_cast<float *>(base + joined_at);
+            const int64_t all_slots = bias_slots;
+            bias_slots = (bias_slots + each - 1) / each;
+            hipLaunchKernelGGL(xent_column_sums_kernel, dim3(static_cast<unsigned>(bias_slots * groups)), dim3(256), 0, st, sums, all_slots, each, cols, groups, joined);
+            HETA_LAUNCH_CHECK("xent_column_sums_kernel");
+            bias_parts = joined;
+        }
+        if (a.dbias) HETA_TRY(fold_partials(bias_parts, bias_slots, cols, a.dbias + v0, HETA_F32, static_cast<int32_t>(cols), cols, st, factor));
         if (dw_parts > 0) {
             char *to = static_cast<char *>(a.dW) + v0 * dtype_size(a.dw_dt);
             HETA_TRY(fold_partials(dw, dw_parts, d * cols, to, a.dw_dt, static_cast<int32_t>(cols), a.ld_dw, st, factor));

@@ -4,7 +4,7 @@
 
 `agg` is what a layer's relation aggregation yields for the type (RafLayer.H[t], Eq. 1 of the paper), x the embeddings that it
 adds to: with such blocks behind its layers a model of this library can be made deep.  The block trains with heta_muon_multi
-on its two matrices (`update`), and for inference its first product can run on 8-bit operands.  This module allocates
+on its two matrices (`update`) and heta_adamw_multi on its vectors (`vector_items`), and for inference its first product can run on 8-bit operands.  This module allocates
 buffers and orders calls on torch's current stream (the buffers' own: none is given back while a call may still read it); all
 arithmetic is in libheta.
 """
@@ -26,6 +26,7 @@ class FeedForwardBlock:
         if W1.shape != W2.shape[::-1]:
             raise ValueError("W1 is [d, d_hidden] and W2 [d_hidden, d]")
         self.g, self.W1, self.W2, self.gamma, self.b1, self.b2, self.act, self.eps = g, W1, W2, gamma, b1, b2, act, eps
+        self.vector_states: Optional[List] = None
         self.m = [torch.zeros(w.shape, dtype=torch.float32, device=w.device) for w in (W1, W2)]
         self.saved: Optional[Dict[str, torch.Tensor]] = None
         self.grads: Dict[str, Optional[torch.Tensor]] = {}
@@ -63,21 +64,28 @@ class FeedForwardBlock:
         """This block's part of a heta_muon_multi call (a model's blocks and relation matrices take one call together)."""
         return [(self.W1, self.m[0], self.grads["W1"]), (self.W2, self.m[1], self.grads["W2"])]
 
+    def vector_items(self) -> List[tuple]:
+        """This block's part of a heta_adamw_multi call: gamma, b1 and b2, without weight decay, with the last backward pass's gradients."""
+        vectors = [("gamma", self.gamma), ("b1", self.b1), ("b2", self.b2)]
+        if self.vector_states is None:
+            self.vector_states = [None if v is None else hb.heta_adamw_state(v) for _, v in vectors]
+        return [(v, s, self.grads[name]) for (name, v), s in zip(vectors, self.vector_states) if v is not None]
+
     def update(self, lr: float = 0.02, momentum: float = 0.95, weight_decay: float = 0.0) -> None:
         """Orthogonalised momentum on W1 and W2 with the last backward pass's gradients."""
         hb.heta_muon_multi(self.g, self.muon_items(), lr=lr, momentum=momentum, weight_decay=weight_decay)
 
-    def pack(self) -> Tuple[torch.Tensor, torch.Tensor]:
-        """W1 as it is now, in 8 bits with a scale per column, for `infer`; to be packed again by whoever changes W1."""
+    def pack(self, dtype: torch.dtype = torch.float8_e4m3fn) -> Tuple[torch.Tensor, torch.Tensor]:
+        """W1 as it is now, in 8 bits (torch.float8_e4m3fn or torch.int8) with a scale per column, for `infer`; to be packed again by whoever changes W1."""
         d, d_hidden = self.W1.shape
-        packed, scale = torch.empty((d_hidden, d), dtype=torch.float8_e4m3fn, device=self.W1.device), torch.empty(d_hidden, device=self.W1.device)
-        hb.heta_linear_pack_e4m3(self.W1, packed, scale)
+        packed, scale = torch.empty((d_hidden, d), dtype=dtype, device=self.W1.device), torch.empty(d_hidden, device=self.W1.device)
+        (hb.heta_linear_pack_i8 if dtype is torch.int8 else hb.heta_linear_pack_e4m3)(self.W1, packed, scale)
         return packed, scale
 
     def infer(self, x: torch.Tensor, agg: Optional[torch.Tensor] = None, packed: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
               coarse_sums: bool = False) -> torch.Tensor:
         """The output alone.  With `packed` (what `pack` gave; bf16 embeddings) the norm writes its rows in 8 bits and the first product
-        reads them and the weights that way; with `coarse_sums` the 8-bit matrix instruction adds, at up to twice the rate (heta_linear)."""
+        reads them and the weights that way: whole numbers at twice the rate of bf16, e4m3 as well with `coarse_sums` (heta_linear)."""
         n, d = x.shape
         dev, t, d_hidden = x.device, x.dtype, self.W1.shape[1]
         h = x if agg is None else torch.empty_like(x)
@@ -86,10 +94,10 @@ class FeedForwardBlock:
         if packed is None:
             normed, scales, w, w_scale = torch.empty((n, d), dtype=t, device=dev), None, self.W1, None
         else:
-            normed, scales = torch.empty((n, d), dtype=torch.float8_e4m3fn, device=dev), torch.empty(n, device=dev)
             w, w_scale = packed
+            normed, scales = torch.empty((n, d), dtype=w.dtype, device=dev), torch.empty(n, device=dev)
         hb.heta_rms_norm(x, normed, residual=agg, sum=sum_, gamma=self.gamma, eps=self.eps, scale=scales)
         hb.heta_linear(self.g, normed, w, hidden, bias=self.b1, act=self.act, in_scale=scales, w_scale=w_scale,
-                       coarse_sums=coarse_sums and packed is not None)
+                       coarse_sums=coarse_sums and packed is not None and w.dtype is torch.float8_e4m3fn)
         hb.heta_linear(self.g, hidden, self.W2, out, bias=self.b2, residual=h)
         return out

@@ -26,11 +26,13 @@ class MiniBatchTrainer:
     tables[t] : device [N_t, d_t] feature / embedding tables (fp32 or bf16), updated in place when learnable
     W[l][r]   : device [d_in(l, r), d_hidden] weights of layer l (0 = outermost), updated in place
     fanouts   : outermost hop first, e.g. [25, 20]
+    state_bits, weight_decay: 8 keeps the optimizer states of weights and tables in 8 bits (heta_adamw_state), and either that or a weight decay
+                (of the weights; tables have none) makes the update heta_adamw_multi's instead of heta_sparse_adam_multi's
     """
 
     def __init__(self, base: hb.Graph, tables: Sequence[torch.Tensor], W: Sequence[Sequence[torch.Tensor]],
                  fanouts: Sequence[int], d_hidden: int, op: int, seed_type: int, lr: float = 1e-3,
-                 beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, seed: int = 0):
+                 beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, seed: int = 0, state_bits: int = 32, weight_decay: float = 0.0):
         if len(W) != len(fanouts):
             raise ValueError("one weight list per layer")
         self.base, self.tables, self.W = base, list(tables), [list(w) for w in W]
@@ -39,11 +41,16 @@ class MiniBatchTrainer:
         self.T = len(base.ntypes)
         f32 = torch.float32
         self.learnable = [t for t in range(self.T) if base.ntypes[t][2]]
+        self.weight_decay, self.adamw = weight_decay, state_bits != 32 or weight_decay != 0.0
+        if self.adamw:
+            self.sW = [[hb.heta_adamw_state(w, state_bits) for w in ws] for ws in self.W]
+            self.sT = {t: hb.heta_adamw_state(self.tables[t], state_bits) for t in self.learnable}
         # Adam moments: one pair per weight matrix, one pair per learnable table (fp32, the table's shape)
-        self.mW = [[torch.zeros(w.shape, dtype=f32, device=w.device) for w in ws] for ws in self.W]
-        self.vW = [[torch.zeros(w.shape, dtype=f32, device=w.device) for w in ws] for ws in self.W]
-        self.mT = {t: torch.zeros(self.tables[t].shape, dtype=f32, device=self.tables[t].device) for t in self.learnable}
-        self.vT = {t: torch.zeros(self.tables[t].shape, dtype=f32, device=self.tables[t].device) for t in self.learnable}
+        else:
+            self.mW = [[torch.zeros(w.shape, dtype=f32, device=w.device) for w in ws] for ws in self.W]
+            self.vW = [[torch.zeros(w.shape, dtype=f32, device=w.device) for w in ws] for ws in self.W]
+            self.mT = {t: torch.zeros(self.tables[t].shape, dtype=f32, device=self.tables[t].device) for t in self.learnable}
+            self.vT = {t: torch.zeros(self.tables[t].shape, dtype=f32, device=self.tables[t].device) for t in self.learnable}
         self.t = 0
         self.last_blocks: Optional[List[hs.DeviceBlock]] = None
         self.last_layers: Optional[List[RafLayer]] = None
@@ -73,7 +80,7 @@ class MiniBatchTrainer:
     def step(self, seeds: torch.Tensor, loss_grad: Callable[[torch.Tensor], torch.Tensor], stream=None,
              keep_blocks: bool = False) -> torch.Tensor:
         """One iteration on the mini-batch `seeds` (device int64, distinct).  `loss_grad(H)` returns dL/dH
-        for the seeds' embeddings H [n_seeds, d_hidden] (fp32).  Returns H.
+        for the seeds' embeddings H [n_seeds, d_hidden] (fp32); ClassifierHead.loss_grad(labels) is one.  Returns H.
 
         The whole iteration - sampling, the buffers torch allocates for it, forward, backward, updates and
         `loss_grad` - runs on ONE stream: torch's current stream, or `stream` (a torch stream or a raw
@@ -102,12 +109,18 @@ class MiniBatchTrainer:
                         G[t] = torch.zeros_like(h)
         # parameter update: dense Adam on the weights, sparse Adam on the touched rows of learnable tables
         # (every update of the iteration in one call: up to 16 tables share a launch)
-        updates = [(self.W[l][r], self.mW[l][r], self.vW[l][r], layer.dW[r], None) for l, layer in enumerate(layers) for r in layer.rels]
         first = layers[0]
-        for t in self.learnable:
-            if t in first.dH0 and blocks[0].src_ids[t].numel() > 0:
-                updates.append((self.tables[t], self.mT[t], self.vT[t], first.dH0[t], blocks[0].src_ids[t]))
-        hb.heta_sparse_adam_multi(updates, lr=self.lr, beta1=self.beta1, beta2=self.beta2, eps=self.eps, step=self.t, stream=stream)
+        weights = [(l, r, layer.dW[r]) for l, layer in enumerate(layers) for r in layer.rels]
+        tables = [(t, first.dH0[t], blocks[0].src_ids[t]) for t in self.learnable if t in first.dH0 and blocks[0].src_ids[t].numel() > 0]
+        if self.adamw:  # every tensor's random bits are its own: seeds count the weights, then the tables
+            place = {(l, r): i for i, (l, r) in enumerate((l, r) for l, ws in enumerate(self.W) for r in range(len(ws)))}
+            items = [(self.W[l][r], self.sW[l][r], dW, self.weight_decay, None, self.seed + place[l, r]) for l, r, dW in weights]
+            items += [(self.tables[t], self.sT[t], dT, 0.0, ids, self.seed + len(place) + t) for t, dT, ids in tables]
+            hb.heta_adamw_multi(items, lr=self.lr, beta1=self.beta1, beta2=self.beta2, eps=self.eps, step=self.t, stream=stream)
+        else:
+            updates = [(self.W[l][r], self.mW[l][r], self.vW[l][r], dW, None) for l, r, dW in weights]
+            updates += [(self.tables[t], self.mT[t], self.vT[t], dT, ids) for t, dT, ids in tables]
+            hb.heta_sparse_adam_multi(updates, lr=self.lr, beta1=self.beta1, beta2=self.beta2, eps=self.eps, step=self.t, stream=stream)
         if keep_blocks:
             self.last_blocks, self.last_layers = blocks, layers
         else:

@@ -160,7 +160,8 @@ def test_gradients_of_each_row_and_a_scale(handle, dtype):
     p.check_backward()
 
 
-@pytest.mark.parametrize("dtype,n,d,classes", [(BF16, 3000, 40, 70001), (BF16, 12001, 72, 17000), (F32, 3000, 24, 33000), (F32, 9001, 16, 12000), (BF16, 600, 16, 300001)])
+@pytest.mark.parametrize("dtype,n,d,classes", [(BF16, 3000, 40, 70001), (BF16, 12001, 72, 17000), (F32, 3000, 24, 33000), (F32, 9001, 16, 12000), (BF16, 600, 16, 300001),
+                                                     (BF16, 20001, 24, 30011), (BF16, 40003, 16, 9001), (BF16, 4096, 16, 131072), (F32, 20001, 8, 15001)])
 def test_pieces_along_rows_and_classes(handle, dtype, n, d, classes):
     p = Problem(n, d, classes, dtype)
     p.forward(handle)
