@@ -252,7 +252,7 @@ def _ld(t: torch.Tensor) -> int:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:  # torch's current stream on the current device, without building a Stream object (3 us a call)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -946,6 +946,8 @@ def _rows_of(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, rows: int
     """(address, leading dimension) of a device matrix of exactly rows x cols elements; (0, cols) for None."""
     if t is None:
         return 0, cols
+    if t.is_contiguous() and t.is_cuda and t.dtype is dtype and t.shape == (rows, cols):
+        return t.data_ptr(), cols
     p, ld, r, c = _mat(t, name, dtype)
     if r != rows or c != cols:
         raise HetaError(HETA_ERR_SHAPE, f"{name} must be [{rows}, {cols}], got [{r}, {c}]")
