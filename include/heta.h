@@ -22,7 +22,8 @@
  *   - Matrices are row-major with a leading dimension `ld` counted in ELEMENTS.
  *   - Every compute call is asynchronous on the given HIP stream (`hip_stream` is a
  *     hipStream_t passed as void*, NULL = the default stream) and performs no hidden
- *     synchronisation, except where a call says it may grow the handle's workspace.
+ *     synchronisation, except where a call says it may grow the handle's workspace (under graph capture it must not have to: run the
+ *     largest call once before).  A captured graph holds the workspace's address: it may be replayed as long as no later call made the workspace grow.
  *   - Every call returns a heta_status.  Arguments are validated on the host before any
  *     kernel is launched; on failure nothing is launched, output buffers are untouched and
  *     heta_last_error() describes the reason.  No exception or abort crosses this boundary.
@@ -721,7 +722,8 @@ heta_status heta_linear_pack_i8(const void *W, heta_dtype w_dt, int64_t ld_w, in
  * heta_linear_xent: softmax cross entropy of n_rows rows over n_classes classes,
  *   z = in . W + bias;  lse_i = log sum_j exp z_ij;  loss_i = lse_i - z_i,labels[i]
  * in, W: fp32 or bf16, [n_rows, d] and [d, n_classes]; bias: device fp32 [n_classes] or NULL; labels: device int64 [n_rows].  A row whose label is outside
- * [0, n_classes) (-1 by custom) has none: its loss is 0, its gradients are zeros, and nothing else depends on what the row holds, NaN included.
+ * [0, n_classes) (-1 by custom) has none: its loss is 0, its gradients are zeros (with finite weights), and nothing else depends on what the row holds, NaN
+ * included.  A bias of -infinity rules a class out.
  * loss (NULL: not stored), lse: device fp32 [n_rows].  mean (device fp32 [2], NULL: not computed): the mean of the losses of the rows with a label (0
  * without any) and how many these are.  Logits are fp32 sums; they are at no time in memory.
  * Uses the handle's workspace (may grow it: by 8 bytes for 32 to 64 logits, and, from 512 rows on, by copies of bf16 operands whose rows are not

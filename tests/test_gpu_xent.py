@@ -342,3 +342,39 @@ def test_captured_and_replayed(handle):
         torch.cuda.synchronize()
         for got, w in zip((p.loss, p.mean, p.gx, p.gW, p.gb), want):
             assert torch.equal(got, w), k
+
+
+def test_a_workspace_that_cannot_grow(handle):
+    """Without room both calls fail before their first launch, outputs as they were; and work when there is room again."""
+    g = heta.heta_graph_create([(1, 1, 0)], [])
+    p = Problem(500, 64, 3000, BF16)
+    p.outputs()
+    from paper_2408_09697_amd import binding as hb
+    hb.heta_workspace_limit(4096)
+    try:
+        for call in (p.forward, p.backward):
+            with pytest.raises(heta.HetaError) as e:
+                call(g)
+            assert e.value.status == heta.HETA_ERR_OOM
+    finally:
+        hb.heta_workspace_limit(0)
+    torch.cuda.synchronize()
+    assert torch.isnan(p.lse).all() and torch.isnan(p.loss).all() and torch.isnan(p.mean).all() and torch.isnan(p.gb).all()
+    p.forward(g)
+    p.backward(g)
+    p.reference()
+    p.check_forward()
+    p.check_backward()
+    g.destroy()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d,classes", [(5000, 512, 8), (40000, 40, 64), (40000, 264, 65), (128, 40, 20000)])
+def test_few_classes_or_few_rows_of_many(handle, n, d, classes, dtype):
+    p = Problem(n, d, classes, dtype)
+    p.forward(handle)
+    p.outputs()
+    p.backward(handle)
+    p.reference()
+    p.check_forward()
+    p.check_backward()
