@@ -181,7 +181,7 @@ template <int R> __global__ void __launch_bounds__(256) xent_rows_kernel(const X
 {
     constexpr int G = 256 / R;
     __shared__ XentPart parts[G][R];
-    __shared__ XentSum rows[R];
+    __shared__ XentSum waves[4];
     const int r = threadIdx.x % R, g = threadIdx.x / R;
     const int64_t m = static_cast<int64_t>(blockIdx.x) * R + r;
     XentPart p{kNothing, 0.f};
@@ -192,24 +192,25 @@ template <int R> __global__ void __launch_bounds__(256) xent_rows_kernel(const X
         if (g < h) parts[g][r] = join(parts[g][r], parts[g + h][r]);
         __syncthreads();
     }
-    if (g == 0) {
-        XentSum s{0., 0.};
-        if (m < n) {
-            p = parts[0][r];
-            const float l2 = p.top + __builtin_amdgcn_logf(p.sum);
-            const int64_t label = labels[m];
-            const bool has = label >= 0 && label < n_classes;
-            const float mine = has ? (l2 - target[m]) * kLn2 : 0.f;
-            lse[m] = l2 * kLn2;
-            if (loss) loss[m] = mine;
-            s = {mine, has ? 1. : 0.};
-        }
-        rows[r] = s;
+    XentSum s{0., 0.};
+    if (g == 0 && m < n) {
+        p = parts[0][r];
+        const float l2 = p.top + __builtin_amdgcn_logf(p.sum);
+        const int64_t label = labels[m];
+        const bool has = label >= 0 && label < n_classes;
+        const float mine = has ? (l2 - target[m]) * kLn2 : 0.f;
+        lse[m] = l2 * kLn2;
+        if (loss) loss[m] = mine;
+        s = {mine, has ? 1. : 0.};
     }
+    if (!mean) return;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s = {s.loss + __shfl_xor(s.loss, o), s.rows + __shfl_xor(s.rows, o)};
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0 && (sums || mean)) {
-        XentSum s{0., 0.};
-        for (int i = 0; i < R; ++i) s = {s.loss + rows[i].loss, s.rows + rows[i].rows};
+    if (threadIdx.x == 0) {
+        s = waves[0];
+        for (int i = 1; i < 4; ++i) s = {s.loss + waves[i].loss, s.rows + waves[i].rows};
         if (sums) sums[blockIdx.x] = s;
         else mean_of(s, mean);
     }
@@ -439,6 +440,10 @@ template <typename E, bool A_RC, bool B_RC, bool LARGE, bool STAGED> struct Xent
 // columns a wavefront 331 and 256).
 template <> struct XentShape<bf16_t, false, false, true, false> { using type = TileShape<bf16_t, 2, 1, false, false, kDirect, 2, 4, 4, 2, 64, 2, 1>; };
 template <> struct XentShape<bf16_t, true, true, true, false> { using type = TileShape<bf16_t, 2, 1, true, true, kDirect, 4, 1, 2, 4, 32, 2, 2>; };
+// Logits of up to 32 rows: the weights are read once, 512 consecutive bytes at a time (4 x 1,024 x 1,100,000, forward, us: 380, 5.9 TB/s; 64 x 64 463, 32 x 128 398, 64 x 128 391, deeper
+// rings by one workgroup a CU 389 to 405; 16 x 256 x 4,096 11.2, 64 x 64 21.3).
+using XentSkinnyForwardTiles = TileShape<bf16_t, 2, 1, false, true, kDirect, 1, 4, 1, 2, 64, 2, 2>; // 32 x 256
+using XentSkinnyBackwardTiles = TileShape<bf16_t, 2, 1, false, true, kDirect, 1, 4, 1, 2, 64, 2, 1>;
 // The logits' tiles: 256 x 128 by four wavefronts, two workgroups on a CU, so that one's exponentials run beside the other's products (forward + both gradients of 700,000 x
 // 256 x 349 and of 8,192 x 512 x 131,072, us: 1,414 and 5,630; one workgroup of eight wavefronts with 256 x 256 1,544 and 5,597, with 256 x 128 1,555 and 6,060; two with
 // 128 x 128 1,526 and 6,090; each when its sums started from zero instead of the bias: 1,581 and 6,186 for this one).
@@ -482,7 +487,7 @@ template <typename E> __global__ void __launch_bounds__(256) xent_align_kernel(c
 }
 static unsigned walk(int64_t items) { return static_cast<unsigned>(std::min<int64_t>((items + 255) / 256, 16384)); }
 
-enum XentTiles { kTilesLarge, kTilesSmall, kTilesStaged };
+enum XentTiles { kTilesLarge, kTilesSmall, kTilesSkinny, kTilesStaged };
 // The tiles of a product M x N of `splits` parts: staged where bf16 rows are not aligned, large where they give every second CU one and are not mostly
 // beyond the last row or column.
 template <typename E> static XentTiles tiles_for(bool direct, int64_t M, int64_t N, int64_t splits)
@@ -490,14 +495,21 @@ template <typename E> static XentTiles tiles_for(bool direct, int64_t M, int64_t
     if (sizeof(E) == 2 && !direct) return kTilesStaged;
     return M > 64 && N > 64 && tiles_of(M, N, 256, 256) * splits >= 128 ? kTilesLarge : kTilesSmall;
 }
+// Those of the logits: a tile for few rows too.
+template <typename E> static XentTiles logit_tiles_for(bool direct, int64_t M, int64_t N) { return sizeof(E) == 2 && direct && M <= 32 ? kTilesSkinny : tiles_for<E>(direct, M, N, 1); }
 // f(shape)
 template <typename T> struct Tag { using type = T; };
 template <typename E, bool A_RC, bool B_RC, typename Epi, typename F> static heta_status with_tiles(XentTiles t, F f)
 {
     if (t == kTilesStaged) return f(XentShape<E, A_RC, B_RC, false, true>{});
+    constexpr bool FORWARD = sizeof(E) == 2 && std::is_same<Epi, XentForwardEpi>::value, BACKWARD = sizeof(E) == 2 && std::is_same<Epi, XentBackwardEpi<bf16_t>>::value;
+    if constexpr (FORWARD)
+        if (t == kTilesSkinny) return f(Tag<XentSkinnyForwardTiles>{});
+    if constexpr (BACKWARD)
+        if (t == kTilesSkinny) return f(Tag<XentSkinnyBackwardTiles>{});
     if (t == kTilesSmall) return f(XentShape<E, A_RC, B_RC, false, false>{});
-    if constexpr (sizeof(E) == 2 && std::is_same<Epi, XentForwardEpi>::value) return f(Tag<XentForwardTiles>{});
-    else if constexpr (sizeof(E) == 2 && std::is_same<Epi, XentBackwardEpi<bf16_t>>::value) return f(Tag<XentBackwardTiles>{});
+    if constexpr (FORWARD) return f(Tag<XentForwardTiles>{});
+    else if constexpr (BACKWARD) return f(Tag<XentBackwardTiles>{});
     else return f(XentShape<E, A_RC, B_RC, true, false>{});
 }
 template <typename E, bool A_RC, bool B_RC, typename Epi> static heta_status go_tiles(const Launch &l, XentTiles t, const typename Epi::Extra &x)
@@ -594,7 +606,7 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     const int64_t ld_wc = round_up(V, 8), ld_ic = round_up(d, 8);
     const size_t w_at = ws.take(copy_w ? static_cast<size_t>(d) * ld_wc * 2 : 0), in_at = ws.take(copy_in ? static_cast<size_t>(n) * ld_ic * 2 : 0);
     const size_t target_at = ws.take(static_cast<size_t>(n) * 4);
-    const XentTiles tiles = tiles_for<E>((copy_w || direct_rows(a.W, a.ld_w, 2)) && (copy_in || direct_rows(a.in, a.ld_in, 2)), n, V, 1);
+    const XentTiles tiles = logit_tiles_for<E>((copy_w || direct_rows(a.W, a.ld_w, 2)) && (copy_in || direct_rows(a.in, a.ld_in, 2)), n, V);
     int64_t strip_rows = 0, strip_cols = 0;
     strip_of<E, XentForwardEpi>(tiles, &strip_rows, &strip_cols);
     const int64_t strips = (V + strip_cols - 1) / strip_cols;
@@ -736,7 +748,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
             {
                 const Launch l{g, who, "xent_logit_grad_kernel", TileItem{in_r, Wv, in.ld, W.ld, 0, 0, rn, cols, d, d, 1, 0, 0, 0, 0, 0},
                                (static_cast<double>(rn) * (d + cols) + static_cast<double>(d) * cols) * sizeof(E), product, st};
-                const XentTiles tiles = tiles_for<E>(direct_w && direct_in, rn, cols, 1);
+                const XentTiles tiles = logit_tiles_for<E>(direct_w && direct_in, rn, cols);
                 int64_t strip_rows = 0, strip_cols = 0;
                 strip_of<E, XentBackwardEpi<E>>(tiles, &strip_rows, &strip_cols);
                 const XentBackward x{a.bias ? a.bias + v0 : nullptr, rows + r0, base + d_at, ld_d, sums ? sums + bias_slots * cols : nullptr, v0};
