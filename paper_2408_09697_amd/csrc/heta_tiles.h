@@ -295,6 +295,7 @@ struct TileItem { // M, N, K > 0
     int32_t mt, nt;            // tiles
     int32_t symmetric;         // C is: the tiles below the diagonal are not formed (several items, one tile size along both sides)
     uint32_t block0, places;   // one item: its tiles, places of them (a multiple of 8); several: the tiles before it, its tiles
+    int32_t group = 0;         // one item that is not split: row blocks that are walked together, column by column (0, 1: each by itself)
 };
 
 // An output tile and the part of the contraction that goes into it.
@@ -322,8 +323,14 @@ struct TilePlace {
             const uint32_t tile = at % 8 * each + at / 8;
             if (tile >= it.block0) continue;
             const uint32_t outer = tile / inner, in = tile - outer * inner;
-            if (splits) set(it, in / it.nt, in % it.nt, static_cast<int>(outer), bm, bn);
-            else set(it, outer, in, 0, bm, bn);
+            if (splits) {
+                set(it, in / it.nt, in % it.nt, static_cast<int>(outer), bm, bn);
+            } else if (it.group > 1) {
+                const uint32_t first = outer / it.group * it.group, rows = min(static_cast<uint32_t>(it.mt) - first, static_cast<uint32_t>(it.group)), place = tile - first * inner;
+                set(it, first + place % rows, place / rows, 0, bm, bn);
+            } else {
+                set(it, outer, in, 0, bm, bn);
+            }
             return true;
         }
         return false;

@@ -629,7 +629,10 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
         in = {base + in_at, ld_ic};
     }
     HETA_LAUNCH_CHECK("xent_align_kernel");
-    const Launch l{g, who, "xent_kernel", TileItem{in.p, W.p, in.ld, W.ld, 0, 0, n, V, d, d, 1, 0, 0, 0, 0, 0}, (static_cast<double>(n) * d + static_cast<double>(d) * V) * sizeof(E), flops, st};
+    // Weights that an XCD's L2 does not hold are read by four row blocks at a time (8,192 x 512 x 131,072: 1,250 us one by one, 1,187; eight 1,188, sixteen 1,228).  D's tiles, which
+    // write their rows, lose by it (433 us for a quarter of the classes, 474), and so do weights that fit (700,000 x 256 x 349: 231, 238).
+    const int32_t group = d * V * static_cast<int64_t>(sizeof(E)) > int64_t(4) << 20 ? 4 : 0;
+    const Launch l{g, who, "xent_kernel", TileItem{in.p, W.p, in.ld, W.ld, 0, 0, n, V, d, d, 1, 0, 0, 0, 0, 0, group}, (static_cast<double>(n) * d + static_cast<double>(d) * V) * sizeof(E), flops, st};
     const XentForward x{a.bias, a.labels, reinterpret_cast<XentPart *>(base + part_at), reinterpret_cast<float *>(base + target_at)};
     HETA_TRY((go_tiles<E, false, true, XentForwardEpi>(l, tiles, x)));
     XentSum *sums = a.mean && groups > 1 ? reinterpret_cast<XentSum *>(base + sums_at) : nullptr;
@@ -746,7 +749,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
             const E *in_r = static_cast<const E *>(in.p) + r0 * in.ld;
             const double product = 2.0 * rn * d * cols;
             {
-                const Launch l{g, who, "xent_logit_grad_kernel", TileItem{in_r, Wv, in.ld, W.ld, 0, 0, rn, cols, d, d, 1, 0, 0, 0, 0, 0},
+                const Launch l{g, who, "xent_logit_grad_kernel", TileItem{in_r, Wv, in.ld, W.ld, 0, 0, rn, cols, d, d, 1, 0, 0, 0, 0, 0, 0},
                                (static_cast<double>(rn) * (d + cols) + static_cast<double>(d) * cols) * sizeof(E), product, st};
                 const XentTiles tiles = logit_tiles_for<E>(direct_w && direct_in, rn, cols);
                 int64_t strip_rows = 0, strip_cols = 0;
@@ -781,7 +784,8 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 split_for(d, cols, rn, 256, &splits, &k_each);
                 splits = std::min(splits, w_splits);
                 if (static_cast<int64_t>(splits) * k_each < rn) k_each = round_up((rn + splits - 1) / splits, 64), splits = static_cast<int32_t>((rn + k_each - 1) / k_each);
-                const Launch l{g, who, "xent_grad_w_kernel", TileItem{in_r, base + d_at, in.ld, ld_d, 0, 0, d, cols, rn, k_each, splits, 0, 0, 0, 0, 0},
+                // a column's row blocks one after the other: they share its part of D
+                const Launch l{g, who, "xent_grad_w_kernel", TileItem{in_r, base + d_at, in.ld, ld_d, 0, 0, d, cols, rn, k_each, splits, 0, 0, 0, 0, 0, 64},
                                (static_cast<double>(rn) * (d + cols)) * sizeof(E) + 4.0 * splits * d * cols, product, st};
                 const XentTiles tiles = tiles_for<E>(direct_in, d, cols, splits);
                 XentProduct x{dw + dw_parts * d * cols, cols, nullptr, clean + r0 * ld_ic, ld_ic, poison, call};
