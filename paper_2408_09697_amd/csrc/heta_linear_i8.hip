@@ -13,7 +13,10 @@ template <int WM, int WN, int MI, int NJ, int LOAD, int ST, int OCC> using Shape
 // 256 x 256 and 256 x 128 by eight wavefronts as for e4m3 (200,000 x 1,024 x 4,096, us: 1,200; two workgroups of four wavefronts a CU, 256 x 128: 1,364, 128 x 128: 1,520; LDS is read
 // and written for as long as the matrix pipe works, and smaller tiles read more of it)
 using Large = Shape<2, 4, 4, 2, kDirect, 2, 1>;       // 256 x 256
-using Half = Shape<4, 2, 2, 2, kDirect, 2, 1>;        // 256 x 128: for epilogues that read or take any width
+using Ragged = Shape<4, 2, 2, 2, kDirect, 2, 1>;      // 256 x 128: for epilogues of any width
+// 128 x 128 by four wavefronts, two workgroups a CU, for epilogues that read: they wait for it while the other multiplies (200,000 x 1,024 x 4,096 with a residual 1,901 -> 1,716 us, 100,000 x
+// 4,096 x 1,024 823 -> 748)
+using Reading = Shape<2, 2, 2, 2, kDirect, 2, 2>;
 using Small = Shape<2, 2, 1, 1, kDirect, 3, 2>;       // 64 x 64
 using StagedLarge = Shape<4, 2, 2, 2, kStaged, 2, 1>; // 256 x 128
 using StagedSmall = Shape<2, 2, 1, 1, kStaged, 2, 2>; // 64 x 64
@@ -66,8 +69,8 @@ static heta_status align_operands(Launch &l)
 heta_status launch_linear_i8(Launch l, heta_dtype out_dt, const LinearExtra &x)
 {
     HETA_TRY(align_operands(l));
-    if (out_dt == HETA_F32) return launch_linear<Large, Half, Half, Small, StagedLarge, StagedSmall, float, false>(l, 1, x);
-    return launch_linear<Large, Half, Half, Small, StagedLarge, StagedSmall, bf16_t, false>(l, 1, x);
+    if (out_dt == HETA_F32) return launch_linear<Large, Reading, Ragged, Small, StagedLarge, StagedSmall, float, false>(l, 1, x);
+    return launch_linear<Large, Reading, Ragged, Small, StagedLarge, StagedSmall, bf16_t, false>(l, 1, x);
 }
 
 // ---- rows ----------------------------------------------------------------------------------------------

@@ -296,6 +296,7 @@ struct XentBackward {
     int64_t ld;
     float *sums;         // [strips of rows][N]: D's sums over them; nullable
     int64_t first;       // the piece's first class
+    const float *factor; // of the sums (a single strip's are the result); nullable
 };
 template <typename O> struct XentBackwardEpi {
     static constexpr int kItems = 1;
@@ -358,6 +359,7 @@ template <typename O> struct XentBackwardEpi {
         }
         if (!x.sums || now.m0 + (wave / C::WN) * (32 * MI) >= it.M) return;
         const int64_t slot = now.m0 / (32 * MI) + wave / C::WN;
+        const float factor = x.factor ? *x.factor : 1.f;
 #pragma unroll
         for (int jj = 0; jj < NJ; ++jj)
 #pragma unroll
@@ -365,7 +367,7 @@ template <typename O> struct XentBackwardEpi {
                 float s = sum[jj][e];
 #pragma unroll
                 for (int o = LPR; o < 64; o <<= 1) s += __shfl_xor(s, o);
-                if (sr == 0 && n0 + 32 * jj + e < it.N) x.sums[slot * it.N + n0 + 32 * jj + e] = s;
+                if (sr == 0 && n0 + 32 * jj + e < it.N) x.sums[slot * it.N + n0 + 32 * jj + e] = s * factor;
             }
     }
 };
@@ -754,9 +756,11 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 const XentTiles tiles = logit_tiles_for<E>(direct_w && direct_in, rn, cols);
                 int64_t strip_rows = 0, strip_cols = 0;
                 strip_of<E, XentBackwardEpi<E>>(tiles, &strip_rows, &strip_cols);
-                const XentBackward x{a.bias ? a.bias + v0 : nullptr, rows + r0, base + d_at, ld_d, sums ? sums + bias_slots * cols : nullptr, v0};
+                const bool single = sums && n_r == 1 && rn <= strip_rows;
+                const XentBackward x{a.bias ? a.bias + v0 : nullptr, rows + r0, base + d_at, ld_d, single ? a.dbias + v0 : sums ? sums + bias_slots * cols : nullptr, v0,
+                                     single ? factor : nullptr};
                 HETA_TRY((go_tiles<E, false, true, XentBackwardEpi<E>>(l, tiles, x)));
-                bias_slots += (rn + strip_rows - 1) / strip_rows;
+                if (sums && !single) bias_slots += (rn + strip_rows - 1) / strip_rows; // none without dbias: nothing is added up below
             }
             if (a.grad_in) {
                 int32_t splits = 1;
@@ -802,7 +806,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
             }
         }
         const float *bias_parts = sums;
-        if (a.dbias && bias_slots > 256) { // 5,469 strips of 349 columns: 27 us in one step, few workgroups of which have columns
+        if (bias_slots > 256) { // 5,469 strips of 349 columns: 27 us in one step, few workgroups of which have columns
             const int64_t each = (bias_slots + 63) / 64, groups = (cols + 255) / 256;
             float *joined = reinterpret_cast<float *>(base + joined_at);
             const int64_t all_slots = bias_slots;
@@ -811,7 +815,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
             HETA_LAUNCH_CHECK("xent_column_sums_kernel");
             bias_parts = joined;
         }
-        if (a.dbias) HETA_TRY(fold_partials(bias_parts, bias_slots, cols, a.dbias + v0, HETA_F32, static_cast<int32_t>(cols), cols, st, factor));
+        if (bias_slots > 0) HETA_TRY(fold_partials(bias_parts, bias_slots, cols, a.dbias + v0, HETA_F32, static_cast<int32_t>(cols), cols, st, factor));
         if (dw_parts > 0) {
             char *to = static_cast<char *>(a.dW) + v0 * dtype_size(a.dw_dt);
             HETA_TRY(fold_partials(dw, dw_parts, d * cols, to, a.dw_dt, static_cast<int32_t>(cols), a.ld_dw, st, factor));
