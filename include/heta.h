@@ -723,10 +723,10 @@ heta_status heta_linear_pack_i8(const void *W, heta_dtype w_dt, int64_t ld_w, in
  *   z = in . W + bias;  lse_i = log sum_j exp z_ij;  loss_i = lse_i - z_i,labels[i]
  * in, W: fp32 or bf16, [n_rows, d] and [d, n_classes]; bias: device fp32 [n_classes] or NULL; labels: device int64 [n_rows].  A row whose label is outside
  * [0, n_classes) (-1 by custom) has none: its loss is 0, its gradients are zeros (with finite weights), and nothing else depends on what the row holds, NaN
- * included.  A bias of -infinity rules a class out.
+ * included.  A bias of -infinity (or the lowest number) rules a class out; logits beyond 6.9e29 either way count as infinite.
  * loss (NULL: not stored), lse: device fp32 [n_rows].  mean (device fp32 [2], NULL: not computed): the mean of the losses of the rows with a label (0
  * without any) and how many these are.  Logits are fp32 sums; they are at no time in memory.
- * Uses the handle's workspace (may grow it: by 8 bytes for 32 to 64 logits, and, from 512 rows on, by copies of bf16 operands whose rows are not
+ * Uses the handle's workspace (may grow it: by 8 bytes for 32 to 64 logits, of as many rows at a time as make 512 MB of them, and, from 512 rows on, by copies of bf16 operands whose rows are not
  * 16-byte aligned). */
 typedef struct heta_linear_xent_args {
     int64_t n_rows;

@@ -597,11 +597,12 @@ static heta_status xent_add(const float *so_far, const float *part, int splits, 
     return HETA_OK;
 }
 
+constexpr int64_t kXentPiece = int64_t(512) << 20; // bytes at a time: of D, and of a forward pass's parts
+
 template <typename E> static heta_status xent_forward(heta_graph *g, const heta_linear_xent_args &a, hipStream_t st)
 {
     const char *who = "heta_linear_xent";
     const int64_t n = a.n_rows, d = a.d, V = a.n_classes;
-    const double flops = 2.0 * n * d * V;
     Regions ws;
     const bool bf16 = sizeof(E) == 2;
     const bool copy_w = bf16 && copies_pay(n) && !direct_rows(a.W, a.ld_w, 2), copy_in = bf16 && copies_pay(n) && !direct_rows(a.in, a.ld_in, 2);
@@ -612,12 +613,14 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     int64_t strip_rows = 0, strip_cols = 0;
     strip_of<E, XentForwardEpi>(tiles, &strip_rows, &strip_cols);
     const int64_t strips = (V + strip_cols - 1) / strip_cols;
-    const size_t part_at = ws.take(static_cast<size_t>(strips) * n * sizeof(XentPart));
+    // rows at a time: all of them, or as many as leave kXentPiece bytes of parts
+    const int64_t most = std::max<int64_t>(256, kXentPiece / static_cast<int64_t>(sizeof(XentPart)) / strips / 256 * 256), R = std::min(n, most);
+    const size_t part_at = ws.take(static_cast<size_t>(strips) * R * sizeof(XentPart));
     // rows of a workgroup: few where there are few rows and many strips; and where there are very many, they are joined in two steps
-    const int per_group = strips <= 16 ? 256 : n >= 4096 || strips <= 64 ? 32 : 4;
+    const int per_group = strips <= 16 ? 256 : R >= 4096 || strips <= 64 ? 32 : 4;
     const int64_t groups = (n + per_group - 1) / per_group;
     const int64_t each = std::max<int64_t>(256 / per_group * 8, (strips + 1023) / 1024), chunks = per_group == 4 && strips > 2 * each ? (strips + each - 1) / each : 0;
-    const size_t joined_at = ws.take(static_cast<size_t>(chunks) * n * sizeof(XentPart));
+    const size_t joined_at = ws.take(static_cast<size_t>(chunks) * R * sizeof(XentPart));
     const size_t sums_at = ws.take(a.mean && groups > 1 ? static_cast<size_t>(groups) * sizeof(XentSum) : 0);
     HETA_TRY(ensure_workspace(g, ws.bytes));
     char *base = static_cast<char *>(g->d_ws);
@@ -634,23 +637,26 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     // Weights that an XCD's L2 does not hold are read by four row blocks at a time (8,192 x 512 x 131,072: 1,250 us one by one, 1,187; eight 1,188, sixteen 1,228).  D's tiles, which
     // write their rows, lose by it (433 us for a quarter of the classes, 474), and so do weights that fit (700,000 x 256 x 349: 231, 238).
     const int32_t group = d * V * static_cast<int64_t>(sizeof(E)) > int64_t(4) << 20 ? 4 : 0;
-    const Launch l{g, who, "xent_kernel", TileItem{in.p, W.p, in.ld, W.ld, 0, 0, n, V, d, d, 1, 0, 0, 0, 0, 0, group}, (static_cast<double>(n) * d + static_cast<double>(d) * V) * sizeof(E), flops, st};
-    const XentForward x{a.bias, a.labels, reinterpret_cast<XentPart *>(base + part_at), reinterpret_cast<float *>(base + target_at)};
-    HETA_TRY((go_tiles<E, false, true, XentForwardEpi>(l, tiles, x)));
     XentSum *sums = a.mean && groups > 1 ? reinterpret_cast<XentSum *>(base + sums_at) : nullptr;
-    const XentPart *parts = x.part;
-    int64_t n_parts = strips;
-    if (chunks > 0) {
-        XentPart *joined = reinterpret_cast<XentPart *>(base + joined_at);
-        hipLaunchKernelGGL(xent_join_kernel<4>, dim3(static_cast<unsigned>(chunks * groups)), dim3(256), 0, st, x.part, strips, each, n, groups, joined);
-        HETA_LAUNCH_CHECK("xent_join_kernel");
-        parts = joined;
-        n_parts = chunks;
-    }
-    {
-        ProfScope prof("xent_rows_kernel", st, static_cast<double>(n) * (8.0 * n_parts + 20), 0);
+    for (int64_t r0 = 0; r0 < n; r0 += R) { // a piece starts at a multiple of 256 rows, and so at a workgroup's first of xent_rows_kernel
+        const int64_t rn = std::min(R, n - r0), here = (rn + per_group - 1) / per_group;
+        const Launch l{g, who, "xent_kernel", TileItem{static_cast<const E *>(in.p) + r0 * in.ld, W.p, in.ld, W.ld, 0, 0, rn, V, d, d, 1, 0, 0, 0, 0, 0, group},
+                       (static_cast<double>(rn) * d + static_cast<double>(d) * V) * sizeof(E), 2.0 * rn * d * V, st};
+        const XentForward x{a.bias, a.labels + r0, reinterpret_cast<XentPart *>(base + part_at), reinterpret_cast<float *>(base + target_at) + r0};
+        HETA_TRY((go_tiles<E, false, true, XentForwardEpi>(l, tiles, x)));
+        const XentPart *parts = x.part;
+        int64_t n_parts = strips;
+        if (chunks > 0) {
+            XentPart *joined = reinterpret_cast<XentPart *>(base + joined_at);
+            hipLaunchKernelGGL(xent_join_kernel<4>, dim3(static_cast<unsigned>(chunks * here)), dim3(256), 0, st, x.part, strips, each, rn, here, joined);
+            HETA_LAUNCH_CHECK("xent_join_kernel");
+            parts = joined;
+            n_parts = chunks;
+        }
+        ProfScope prof("xent_rows_kernel", st, static_cast<double>(rn) * (8.0 * n_parts + 20), 0);
         auto go = [&](auto per) {
-            hipLaunchKernelGGL(xent_rows_kernel<decltype(per)::value>, dim3(static_cast<unsigned>(groups)), dim3(256), 0, st, parts, n_parts, x.target, a.labels, n, V, a.loss, a.lse, sums, a.mean);
+            hipLaunchKernelGGL(xent_rows_kernel<decltype(per)::value>, dim3(static_cast<unsigned>(here)), dim3(256), 0, st, parts, n_parts, x.target, x.labels, rn, V,
+                               a.loss ? a.loss + r0 : nullptr, a.lse + r0, sums ? sums + r0 / per_group : nullptr, a.mean);
         };
         if (per_group == 256) go(std::integral_constant<int, 256>{});
         else if (per_group == 32) go(std::integral_constant<int, 32>{});
@@ -661,8 +667,6 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     HETA_LAUNCH_CHECK("xent_mean_kernel");
     return HETA_OK;
 }
-
-constexpr int64_t kXentPiece = int64_t(512) << 20; // bytes of D at a time
 
 // splits of a contraction over K for tiles of M x N outputs: one workgroup per CU
 static void split_for(int64_t M, int64_t N, int64_t K, int64_t least, int32_t *n_split, int64_t *k_per_split)
@@ -705,9 +709,9 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
     const size_t d_at = ws.take(static_cast<size_t>(R) * ld_d * sizeof(E));
     const size_t sums_at = ws.take(a.dbias ? static_cast<size_t>((R + 31) / 32 * n_r) * Vc * 4 : 0);
     const size_t joined_at = ws.take(a.dbias ? static_cast<size_t>(64) * Vc * 4 : 0);
-    const size_t dw_at = ws.take(a.dW ? static_cast<size_t>(w_splits) * n_r * d * Vc * 4 : 0);
+    const size_t dw_at = ws.take(a.dW && (w_splits > 1 || n_r > 1) ? static_cast<size_t>(w_splits) * n_r * d * Vc * 4 : 0);
     // grad_in's sums over the classes so far, and in front of each piece's partial products
-    const size_t di_at = ws.take(a.grad_in ? static_cast<size_t>(in_splits + (n_v > 1 ? n_r : 0)) * R * d * 4 : 0);
+    const size_t di_at = ws.take(a.grad_in && (in_splits > 1 || n_v > 1) ? static_cast<size_t>(in_splits + (n_v > 1 ? n_r : 0)) * R * d * 4 : 0);
     if (a.grad_in && (n_v > 1 || in_splits > 1) && R * d > max_blocks(256) * 1024) return fail(HETA_ERR_UNSUPPORTED, "%s: input gradient too large for one launch", who);
     HETA_TRY(ensure_workspace(g, ws.bytes));
     char *base = static_cast<char *>(g->d_ws);

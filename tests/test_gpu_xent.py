@@ -378,3 +378,75 @@ def test_few_classes_or_few_rows_of_many(handle, n, d, classes, dtype):
     p.reference()
     p.check_forward()
     p.check_backward()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_forward_in_pieces_of_rows(handle, dtype):
+    """1,876 strips of classes: 35,584 rows at a time."""
+    n, d, classes = 40300, 16, 120001
+    p = Problem(n, d, classes, dtype)
+    p.forward(handle)
+    count, total, room = 0, 0.0, 0.0
+    for i in range(0, n, 500):
+        q = Problem.__new__(Problem)
+        q.__dict__.update(p.__dict__)
+        q.x, q.y, q.loss, q.lse = p.x[i:i + 500], p.y[i:i + 500], p.loss[i:i + 500], p.lse[i:i + 500]
+        q.n = len(q.y)
+        q.reference()
+        within(q.lse, q.r_lse, q.e_lse + U * q.r_lse.abs(), "lse")
+        within(q.loss, q.r_loss, q.e_loss, "loss")
+        count, total, room = count + int(q.has.sum()), total + float(q.r_loss.sum()), room + float(q.e_loss.sum())
+    assert float(p.mean[1]) == count
+    assert abs(float(p.mean[0]) - total / count) <= room / count + 2 * U * total / count
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_classes_ruled_out_by_the_lowest_number(handle, dtype):
+    """As by minus infinity, to the bit; whole strips of classes among them."""
+    results = []
+    for low in (-float("inf"), torch.finfo(F32).min):
+        p = Problem(300, 40, 1000, dtype)
+        p.bias[::3] = low
+        p.bias[256:600] = low
+        p.y[(p.y % 3 == 0) | ((p.y >= 256) & (p.y < 600))] = 601
+        p.forward(handle)
+        p.outputs()
+        p.backward(handle)
+        results.append([p.loss, p.lse, p.mean, p.gx, p.gW, p.gb])
+        assert all(torch.isfinite(t.float()).all() for t in results[-1])
+        assert (p.gb[::3] == 0).all() and (p.gb[256:600] == 0).all() and (p.gW[:, 256:600] == 0).all()
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_two_captured_graphs_of_many_rows_on_one_handle(handle):
+    """Rows that are looked for by the replay: with something to clear in some replays of one graph and none in the other's."""
+    problems = [Problem(70000, 72, 50, BF16, seed=1), Problem(60000, 80, 70, BF16, seed=20)]
+    graphs = []
+    for p in problems:
+        p.outputs()
+        p.forward(handle)
+        p.backward(handle)
+    torch.cuda.synchronize()
+    for p in problems:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            p.forward(handle)
+            p.backward(handle)
+    for k in range(6):
+        p, graph = problems[k % 2], graphs[k % 2]
+        none = torch.nonzero((p.y < 0) | (p.y >= p.classes))[:, 0]
+        p.x.copy_(rows(p.n, p.d, BF16, 100 + k))
+        if k in (0, 3):
+            p.x[none[:50]] = float("nan")
+        p.forward(handle)
+        p.backward(handle)
+        want = [t.clone() for t in (p.loss, p.mean, p.gx, p.gW, p.gb)]
+        assert all(torch.isfinite(t.float()).all() for t in want)
+        for t in (p.loss, p.mean, p.gx, p.gW, p.gb):
+            t.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip((p.loss, p.mean, p.gx, p.gW, p.gb), want):
+            assert torch.equal(got, w), k
