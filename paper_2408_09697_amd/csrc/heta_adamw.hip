@@ -104,8 +104,8 @@ template <typename WT, typename GT> __global__ void __launch_bounds__(256) adamw
     store8(p.v + at, valid, v);
 }
 
-// 32 bits for the element that `x` stands for: two rounds of multiplication and shifts (the finalizer of MurmurHash3, a 32-bit bijection of good avalanche),
-// a key in front of each; x has the first one already.
+// 32 bits for the element that `x` stands for: two rounds of multiplication and shifts (the 32-bit finalizer that Appleby published in 2011, a bijection in which every
+// bit of the input changes about half of the output's), a key in front of each; x has the first one already.
 __device__ __forceinline__ uint32_t element_bits(uint32_t x, uint32_t key1)
 {
     x ^= x >> 16;
