@@ -156,8 +156,13 @@ struct PartialEpi {
     __device__ __forceinline__ static void second(const Extra &, float (&)[4], const float (&)[4]) {}
 };
 
+// The same of integer products, as integers.
+struct PartialBitsEpi : PartialEpi {
+    static constexpr bool kBits = true;
+};
+
 // The rest of a product whose contraction was split: the partial products of 16 bytes of outputs added in order, and the epilogue.
-template <typename O, bool SCALED> __global__ void __launch_bounds__(256) linear_finish_kernel(LinearExtra x, const float *part, int n_split, int64_t M, int64_t N)
+template <typename O, bool SCALED, bool INT> __global__ void __launch_bounds__(256) linear_finish_kernel(LinearExtra x, const float *part, int n_split, int64_t M, int64_t N)
 {
     using Epi = LinearEpi<O, SCALED>;
     constexpr int W = Epi::W;
@@ -168,17 +173,24 @@ template <typename O, bool SCALED> __global__ void __launch_bounds__(256) linear
     typename Epi::Row row;
     cols.load(x, n, N);
     row.load(x, m, M);
+    using Sum = std::conditional_t<INT, int, float>;
+    Sum sum[W];
     float y[W], t[W];
 #pragma unroll
-    for (int e = 0; e < W; ++e) y[e] = 0.f;
+    for (int e = 0; e < W; ++e) sum[e] = 0;
 #pragma unroll 4
     for (int s = 0; s < n_split; ++s)
 #pragma unroll
         for (int h = 0; h < W; h += 4) {
             const uintx4 q = load_piece(part + (s * M + m) * N + n + h, valid - h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[h + e] += __uint_as_float(q[e]);
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (INT) sum[h + e] += static_cast<int>(q[e]);
+                else sum[h + e] += __uint_as_float(q[e]);
+            }
         }
+#pragma unroll
+    for (int e = 0; e < W; ++e) y[e] = sum[e];
     unpack16<O>(x.other ? load_piece(static_cast<const O *>(x.other) + m * x.ld_other + n, valid) : uintx4{0u, 0u, 0u, 0u}, t);
     Epi::first(cols, row, y);
     if (x.pre) store_piece(static_cast<O *>(x.pre) + m * x.ld_pre + n, valid, pack16<O>(y));
@@ -261,11 +273,12 @@ inline heta_status launch_linear(const Launch &l, size_t elt, const LinearExtra 
             HETA_TRY(ensure_workspace(l.g, split.bytes));
             float *ws = static_cast<float *>(l.g->d_ws);
             const PartialEpi::Extra px{ws, l.it.N};
-            HETA_TRY((direct ? part.go<Small, PartialEpi>(px) : part.go<StagedSmall, PartialEpi>(px)));
+            using Partial = std::conditional_t<Small::INT, PartialBitsEpi, PartialEpi>;
+            HETA_TRY((direct ? part.go<Small, Partial>(px) : part.go<StagedSmall, Partial>(px)));
             constexpr int W = 16 / (int)sizeof(O);
             const int64_t blocks = (l.it.M * ((l.it.N + W - 1) / W) + 255) / 256;
             ProfScope prof("linear_finish_kernel", l.st, static_cast<double>(l.it.M) * l.it.N * (4.0 * part.it.n_split + sizeof(O)), 0);
-            hipLaunchKernelGGL((linear_finish_kernel<O, SCALED>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, l.st, x, ws, part.it.n_split, l.it.M, l.it.N);
+            hipLaunchKernelGGL((linear_finish_kernel<O, SCALED, Small::INT>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, l.st, x, ws, part.it.n_split, l.it.M, l.it.N);
             HETA_LAUNCH_CHECK("linear_finish_kernel");
             return HETA_OK;
         }

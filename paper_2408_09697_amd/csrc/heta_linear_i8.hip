@@ -22,13 +22,21 @@ using StagedLarge = Shape<4, 2, 2, 2, kStaged, 2, 1>; // 256 x 128
 using StagedSmall = Shape<2, 2, 1, 1, kStaged, 2, 2>; // 64 x 64
 
 // Rows of 8-bit values, `chunks` pieces of 16 bytes each, the last one filled up with zeros.
-static __global__ void __launch_bounds__(256) align_codes_kernel(const uint8_t *src, int64_t ld, int64_t rows, int32_t d, int32_t chunks, uint8_t *dst)
+// Two operands in one launch (no rows of one that needs no copy), at most 2^26 pieces.
+struct CodeRows {
+    const uint8_t *p;
+    uint8_t *to;
+    int64_t ld;
+    uint32_t rows;
+};
+static __global__ void __launch_bounds__(256) align_codes_kernel(CodeRows a, CodeRows b, int32_t d, uint32_t chunks)
 {
-    const int64_t total = rows * chunks;
-    for (int64_t q = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; q < total; q += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t r = q / chunks;
+    const uint32_t first = a.rows * chunks, total = first + b.rows * chunks;
+    for (uint32_t at = blockIdx.x * 256 + threadIdx.x; at < total; at += gridDim.x * 256) {
+        const CodeRows &x = at < first ? a : b;
+        const uint32_t q = at < first ? at : at - first, r = q / chunks;
         const int c = static_cast<int>(q - r * chunks) * 16;
-        const uint8_t *from = src + r * ld + c;
+        const uint8_t *from = x.p + r * x.ld + c;
         uintx4 v = {0u, 0u, 0u, 0u};
         if (c + 16 <= d) {
             v = load16(from);
@@ -37,7 +45,7 @@ static __global__ void __launch_bounds__(256) align_codes_kernel(const uint8_t *
             for (int e = 0; e < 16; ++e)
                 if (c + e < d) v[e / 4] |= static_cast<uint32_t>(from[e]) << (8 * (e & 3));
         }
-        store16(dst + q * 16, v);
+        store16(x.to + static_cast<int64_t>(q) * 16, v);
     }
 }
 
@@ -53,15 +61,13 @@ static heta_status align_operands(Launch &l)
     if ((l.g->ws_refused > 0 && bytes >= l.g->ws_refused) || ensure_workspace(l.g, bytes) != HETA_OK) return HETA_OK;
     char *to = static_cast<char *>(l.g->d_ws);
     ProfScope prof("align_codes_kernel", l.st, 2.0 * bytes, 0);
-    auto copy = [&](const void *&p, int64_t &ld_p, int64_t rows, char *dst) {
-        const int64_t blocks = std::min<int64_t>((rows * (ld / 16) + 255) / 256, 16384);
-        hipLaunchKernelGGL(align_codes_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, l.st, static_cast<const uint8_t *>(p), ld_p, rows, static_cast<int32_t>(it.K),
-                           static_cast<int32_t>(ld / 16), reinterpret_cast<uint8_t *>(dst));
-        p = dst;
-        ld_p = ld;
-    };
-    if (!a_in) copy(it.A, it.lda, it.M, to);
-    if (!b_in) copy(it.B, it.ldb, it.N, to + (a_bytes + 255) / 256 * 256);
+    char *const to_b = to + (a_bytes + 255) / 256 * 256;
+    const CodeRows a{static_cast<const uint8_t *>(it.A), reinterpret_cast<uint8_t *>(to), it.lda, a_in ? 0u : static_cast<uint32_t>(it.M)},
+        b{static_cast<const uint8_t *>(it.B), reinterpret_cast<uint8_t *>(to_b), it.ldb, b_in ? 0u : static_cast<uint32_t>(it.N)};
+    const uint32_t chunks = static_cast<uint32_t>(ld / 16);
+    hipLaunchKernelGGL(align_codes_kernel, dim3(std::min(((a.rows + b.rows) * chunks + 255) / 256, 16384u)), dim3(256), 0, l.st, a, b, static_cast<int32_t>(it.K), chunks);
+    if (!a_in) it.A = to, it.lda = ld;
+    if (!b_in) it.B = to_b, it.ldb = ld;
     HETA_LAUNCH_CHECK("align_codes_kernel");
     return HETA_OK;
 }
@@ -69,8 +75,16 @@ static heta_status align_operands(Launch &l)
 heta_status launch_linear_i8(Launch l, heta_dtype out_dt, const LinearExtra &x)
 {
     HETA_TRY(align_operands(l));
-    if (out_dt == HETA_F32) return launch_linear<Large, Reading, Ragged, Small, StagedLarge, StagedSmall, float, false>(l, 1, x);
-    return launch_linear<Large, Reading, Ragged, Small, StagedLarge, StagedSmall, bf16_t, false>(l, 1, x);
+    // a quarter of 256 columns a tile or more would be beyond the last (100,000 x 800 x 320 and x 384, 20,000 x 4,096 x 384, 100,000 x 256 x 384, us: 74.3, 74.5, 55.8 and 35.6 by
+    // 256 x 256, 64.4, 68.3, 36.5 and 29.3 by 128 x 128; a sixth, x 640: 96.6 and 98.4)
+    const int64_t columns = (l.it.N + 255) / 256 * 256;
+    const bool narrow = (columns - l.it.N) * 4 >= columns;
+    auto go = [&](auto o) {
+        using O = decltype(o);
+        return narrow ? launch_linear<Reading, Reading, Ragged, Small, StagedLarge, StagedSmall, O, false>(l, 1, x)
+                      : launch_linear<Large, Reading, Ragged, Small, StagedLarge, StagedSmall, O, false>(l, 1, x);
+    };
+    return out_dt == HETA_F32 ? go(float{}) : go(bf16_t{});
 }
 
 // ---- rows ----------------------------------------------------------------------------------------------

@@ -364,6 +364,9 @@ template <typename Epi> constexpr bool wants_strips()
     if constexpr (takes_tile<Epi>::value) return Epi::kStrips;
     else return true;
 }
+// kBits = true: 32-bit integer sums reach a block epilogue as they are held, not rounded to fp32.
+template <typename Epi, typename = void> struct takes_bits : std::false_type {};
+template <typename Epi> struct takes_bits<Epi, std::enable_if_t<Epi::kBits>> : std::true_type {};
 template <typename Epi> struct TileArgs {
     int n_items;
     uint32_t stride; // one item: from one tile of a workgroup to its next; several: tiles of an XCD
@@ -378,7 +381,7 @@ template <typename Epi> struct TileArgs {
 // but aligns its products to the largest with about 14 bits below (sums of 1,024 products of random values: 1.5e-5 off
 // relative to the result, against 2e-7).
 // INT: the 8-bit values are whole numbers, their products are added as 32-bit integers, at the 8-bit rate and exactly (|sum| < 2^31: fewer than 2^17
-// products), and rounded to fp32 in front of the epilogue.
+// products), and rounded to fp32 in front of the epilogue (kBits: not there).
 template <typename S_, int EB_, int T_, bool A_RC_, bool B_RC_, int LOAD_, int WM_, int WN_, int MI_, int NJ_, int BK_, int ST_, int OCC_, bool WIDEN_ = false, bool INT_ = false> struct TileShape {
     using S = S_;
     static constexpr int EB = EB_, T = T_, LOAD = LOAD_, WM = WM_, WN = WN_, MI = MI_, NJ = NJ_, BK = BK_, ST = LOAD_ == kDirect ? ST_ : 2, OCC = OCC_;
@@ -443,7 +446,11 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
         if constexpr (takes_tile<Epi>::value) Epi::template begin<C>(extra, it, acc, now, wave, lane);
         else clear();
     };
-    auto four = [&](int i, int jj, int q) { return make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]); };
+    auto four = [&](int i, int jj, int q) {
+        const auto &a = acc[i][jj];
+        if constexpr (C::INT && takes_bits<Epi>::value) return make_float4(__int_as_float(a[4 * q]), __int_as_float(a[4 * q + 1]), __int_as_float(a[4 * q + 2]), __int_as_float(a[4 * q + 3]));
+        else return make_float4(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]);
+    };
 
     // One k-tile.  The fragments of a step are read before the products of the step in front of it, and scheduling barriers
     // keep them there: left to itself the compiler reads a fragment just before its first product, and every step waits for LDS.

@@ -173,3 +173,14 @@ def test_captured_together(handle):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+# contractions that are split over workgroups, large products by tiles of every width, rows that are copied first (one operand or both)
+@pytest.mark.parametrize("pad_in,pad_w", [(0, 0), (0, 3), (5, 0), (1, 1)])
+@pytest.mark.parametrize("n,k,m", [(3, 131071, 2), (64, 5008, 40), (1, 20000, 16), (700, 1024, 320), (40000, 304, 100), (3000, 500, 700), (5000, 3200, 384), (20000, 789, 349)])
+def test_sums_are_exact_however_they_are_formed(handle, n, k, m, pad_in, pad_w):
+    """With scales of 1 the result is the exact sum, rounded to fp32 once."""
+    q, W = whole(n, k, 1, pad_in, 60), whole(m, k, 2, pad_w, 60)  # values of one sign: sums beyond 2^24
+    out = torch.empty(n, m, device="cuda")
+    heta.heta_linear(handle, q, W, out, in_scale=torch.ones(n, device="cuda"), w_scale=torch.ones(m, device="cuda"))
+    assert torch.equal(out, (q.double() @ W.double().t()).float())
