@@ -282,7 +282,7 @@ template <int EB, int T, int MI, int NJ, bool INT> struct Fragments { // of one 
 };
 
 // four columns (chunk 0..7) of a row of a 32 x 32 fp32 strip
-__device__ __forceinline__ float4 *strip_at(float *strip, int row, int chunk) { return reinterpret_cast<float4 *>(strip + row * 32 + ((chunk ^ (row & 7)) * 4)); }
+template <int COLS = 32> __device__ __forceinline__ float4 *strip_at(float *strip, int row, int chunk) { return reinterpret_cast<float4 *>(strip + row * COLS + ((chunk ^ (row & 7)) * 4)); }
 
 // ---- items of a launch ------------------------------------------------------------------------------
 struct TileItem { // M, N, K > 0
@@ -356,13 +356,13 @@ struct TilePlace {
 //     out(x, it, split) receive them, rows x.ld_pre and x.ld_out apart; kWhole: N is a multiple of W.  struct Cols, Row { void
 //     load(const Extra &x, int64_t n, int64_t N); } are what a lane keeps of W columns and of a row (which may lie beyond the matrix).
 //   Instead, kTile = true: begin<C>(x, it, acc, place, wave, lane) sets what the sums of a tile start from, tile<C>(x, it, acc, strip, place, wave, lane)
-//     takes a wavefront's sums as they lie in the registers, and choose(x, it) may change the item's addresses by what is in memory when the kernel runs; kStrips: whether it uses the strip.
+//     takes a wavefront's sums as they lie in the registers, and choose(x, it) may change the item's addresses by what is in memory when the kernel runs; kStrip<C>: bytes of its strip.
 template <typename Epi, typename = void> struct takes_tile : std::false_type {};
 template <typename Epi> struct takes_tile<Epi, std::enable_if_t<Epi::kTile>> : std::true_type {};
-template <typename Epi> constexpr bool wants_strips()
+template <typename C, typename Epi> constexpr int strip_bytes() // a 32 x 32 block of fp32, unless the epilogue says otherwise
 {
-    if constexpr (takes_tile<Epi>::value) return Epi::kStrips;
-    else return true;
+    if constexpr (takes_tile<Epi>::value) return Epi::template kStrip<C>;
+    else return 4096;
 }
 // kBits = true: 32-bit integer sums reach a block epilogue as they are held, not rounded to fp32.
 template <typename Epi, typename = void> struct takes_bits : std::false_type {};
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
     using ImgB = TileImage<C::B_RC, BN, BK, EB>;
     constexpr int A_STAGE = ImgA::BYTES * T, STAGE = A_STAGE + ImgB::BYTES * T;
     // epilogue strips: one 32 x 32 block of sums per wavefront, its own; behind the ring where that is filled during the epilogue
-    constexpr int STRIPS = wants_strips<Epi>() ? NW * 4096 : 0, STRIPS_AT = DIRECT ? ST * STAGE : 0;
+    constexpr int STRIPS = NW * strip_bytes<C, Epi>(), STRIPS_AT = DIRECT ? ST * STAGE : 0;
     __shared__ __attribute__((aligned(1024))) char ring[std::max(ST * STAGE, STRIPS_AT + STRIPS)];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -544,7 +544,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_gemm_kernel(TileArgs<Epi> 
     // register 4 q + e of block (i, jj) is column 8 q + 4 (lane / 32) + e of row lane % 32
     auto epilogue = [&] {
         if constexpr (takes_tile<Epi>::value) {
-            Epi::template tile<C>(extra, it, acc, reinterpret_cast<float *>(ring + STRIPS_AT + wave * 4096), now, wave, lane);
+            Epi::template tile<C>(extra, it, acc, reinterpret_cast<float *>(ring + STRIPS_AT + wave * strip_bytes<C, Epi>()), now, wave, lane);
         } else if constexpr (Epi::kBlocks) {
             const int half = lane >> 5, l32 = lane & 31;
             float *strip = reinterpret_cast<float *>(ring + STRIPS_AT + wave * 4096);

@@ -75,7 +75,8 @@ struct XentForward {
 };
 struct XentForwardEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kTile = true, kStrips = false;
+    static constexpr bool kTile = true;
+    template <typename C> static constexpr int kStrip = 0;
     using Extra = XentForward;
     __device__ __forceinline__ static void choose(const Extra &, TileItem &) {}
     template <typename C, typename Acc> __device__ __forceinline__ static void begin(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], const TilePlace &now, int wave, int lane)
@@ -300,7 +301,9 @@ struct XentBackward {
 };
 template <typename O> struct XentBackwardEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kTile = true, kStrips = true;
+    static constexpr bool kTile = true;
+    // a wavefront's columns side by side: 64 columns of 16 bits are stored as whole lines (a quarter of 8,192 x 512 x 131,072 448 us by 32 columns, 420; 700,000 x 256 x 349 365, 325)
+    template <typename C> static constexpr int kStrip = 4096 * C::NJ;
     using Extra = XentBackward;
     __device__ __forceinline__ static void choose(const Extra &, TileItem &) {}
     template <typename C, typename Acc> __device__ __forceinline__ static void begin(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], const TilePlace &now, int wave, int lane)
@@ -310,65 +313,65 @@ template <typename O> struct XentBackwardEpi {
     template <typename C, typename Acc>
     __device__ __forceinline__ static void tile(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], float *strip, const TilePlace &now, int wave, int lane)
     {
-        constexpr int MI = C::MI, NJ = C::NJ, W = 16 / (int)sizeof(O), LPR = 32 / W, RPP = 64 / LPR, ROUNDS = 32 / RPP;
+        constexpr int MI = C::MI, NJ = C::NJ, COLS = 32 * NJ, W = 16 / (int)sizeof(O), LPR = COLS / W, RPP = 64 / LPR, ROUNDS = 32 / RPP;
         int here = lane;
         asm volatile("" : "+v"(here)); // not kept through the products
         const int sr = here / LPR, sc = here % LPR, half = here >> 5, l32 = here & 31;
         const int64_t mw = now.m0 + (wave / C::WN) * (32 * MI), nw = now.n0 + (wave % C::WN) * (32 * NJ), m0 = mw + sr, n0 = nw + sc * W;
-        float sum[NJ][W];
+        float sum[W];
 #pragma unroll
-        for (int jj = 0; jj < NJ; ++jj)
-#pragma unroll
-            for (int e = 0; e < W; ++e) sum[jj][e] = 0.f;
+        for (int e = 0; e < W; ++e) sum[e] = 0.f;
+        // a row a lane, as the sums lie; all of them here: a load behind the stores below waits for them
+        float lse[MI], factor[MI];
+        int at[MI]; // the label's column
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-            // the exponentials as the sums lie, a row a lane
             const XentRow row = x.rows[min(mw + 32 * i + l32, it.M - 1)];
-            const float f = mw + 32 * i + l32 < it.M ? row.f : 0.f;
             const int64_t label = row.label - x.first - nw;
+            lse[i] = row.lse;
+            factor[i] = mw + 32 * i + l32 < it.M ? row.f : 0.f;
+            at[i] = label >= 0 && label < 32 * NJ ? static_cast<int>(label) : -64;
+        }
 #pragma unroll
-            for (int jj = 0; jj < NJ; ++jj) {
+        for (int i = 0; i < MI; ++i) {
+            const float f = factor[i];
+#pragma unroll
+            for (int jj = 0; jj < NJ; ++jj)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     float y[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][jj][4 * q + e], kLog2e, -row.lse)) * f;
+                        const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][jj][4 * q + e], kLog2e, -lse[i])) * f;
                         y[e] = f != 0.f ? p : 0.f;
                     }
-                    *strip_at(strip, l32, 2 * q + half) = make_float4(y[0], y[1], y[2], y[3]);
+                    *strip_at<COLS>(strip, l32, 8 * jj + 2 * q + half) = make_float4(y[0], y[1], y[2], y[3]);
                 }
-                const int64_t at = label - 32 * jj; // the label's column in the block
-                if (half == 0 && at >= 0 && at < 32) reinterpret_cast<float *>(strip_at(strip, l32, static_cast<int>(at) / 4))[at & 3] -= f;
-                const int64_t n = n0 + 32 * jj;
+            if (half == 0 && at[i] >= 0) reinterpret_cast<float *>(strip_at<COLS>(strip, l32, at[i] / 4))[at[i] & 3] -= f;
 #pragma unroll
-                for (int r = 0; r < ROUNDS; ++r) {
-                    const int64_t m = m0 + 32 * i + RPP * r;
-                    float y[W];
+            for (int r = 0; r < ROUNDS; ++r) {
+                const int64_t m = m0 + 32 * i + RPP * r;
+                float y[W];
 #pragma unroll
-                    for (int h = 0; h < W / 4; ++h) {
-                        const float4 v = *strip_at(strip, RPP * r + sr, sc * (W / 4) + h);
-                        y[4 * h] = v.x; y[4 * h + 1] = v.y; y[4 * h + 2] = v.z; y[4 * h + 3] = v.w;
-                    }
-#pragma unroll
-                    for (int e = 0; e < W; ++e) sum[jj][e] += y[e];
-                    // D's rows are padded to whole pieces; what lies behind the classes is read by nothing that is stored
-                    if (m < it.M && n < x.ld) store16(static_cast<O *>(x.D) + m * x.ld + n, pack16<O>(y));
+                for (int h = 0; h < W / 4; ++h) {
+                    const float4 v = *strip_at<COLS>(strip, RPP * r + sr, sc * (W / 4) + h);
+                    y[4 * h] = v.x; y[4 * h + 1] = v.y; y[4 * h + 2] = v.z; y[4 * h + 3] = v.w;
                 }
+#pragma unroll
+                for (int e = 0; e < W; ++e) sum[e] += y[e];
+                // D's rows are padded to whole pieces; what lies behind the classes is read by nothing that is stored
+                if (m < it.M && n0 < x.ld) store16(static_cast<O *>(x.D) + m * x.ld + n0, pack16<O>(y));
             }
         }
-        if (!x.sums || now.m0 + (wave / C::WN) * (32 * MI) >= it.M) return;
-        const int64_t slot = now.m0 / (32 * MI) + wave / C::WN;
-        const float factor = x.factor ? *x.factor : 1.f;
+        if (!x.sums || mw >= it.M) return;
+        const float whole = x.factor ? *x.factor : 1.f;
 #pragma unroll
-        for (int jj = 0; jj < NJ; ++jj)
+        for (int e = 0; e < W; ++e) {
+            float s = sum[e];
 #pragma unroll
-            for (int e = 0; e < W; ++e) {
-                float s = sum[jj][e];
-#pragma unroll
-                for (int o = LPR; o < 64; o <<= 1) s += __shfl_xor(s, o);
-                if (sr == 0 && n0 + 32 * jj + e < it.N) x.sums[slot * it.N + n0 + 32 * jj + e] = s * factor;
-            }
+            for (int o = LPR; o < 64; o <<= 1) s += __shfl_xor(s, o);
+            if (sr == 0 && n0 + e < it.N) x.sums[mw / (32 * MI) * it.N + n0 + e] = s * whole;
+        }
     }
 };
 
@@ -383,9 +386,12 @@ struct XentProduct {
     const uint32_t *poison; // nullable: no copy
     uint32_t call;
 };
+typedef uint32_t StripWords2 __attribute__((ext_vector_type(2), may_alias));
+typedef uint32_t StripWords4 __attribute__((ext_vector_type(4), may_alias));
 template <typename O> struct XentProductEpi {
     static constexpr int kItems = 1;
-    static constexpr bool kTile = true, kStrips = true;
+    static constexpr bool kTile = true;
+    template <typename C> static constexpr int kStrip = 4096;
     using Extra = XentProduct;
     __device__ __forceinline__ static void choose(const Extra &x, TileItem &it)
     {
@@ -402,10 +408,19 @@ template <typename O> struct XentProductEpi {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][jj][v] = 0.f;
     }
+    // Four columns from 4 c on of a row of 32 P columns.  fp32: as strip_at.  16 bits: pieces of 16 bytes, 4 P of them a row, so placed that rows whose
+    // pieces would begin in the same bank do not.
+    template <int P> __device__ __forceinline__ static char *strip_four(float *strip, int row, int c)
+    {
+        if constexpr (sizeof(O) == 4) return reinterpret_cast<char *>(strip_at<32 * P>(strip, row, c));
+        else return reinterpret_cast<char *>(strip) + row * (64 * P) + ((c / 2) ^ (P == 2 ? row & 7 : (row >> 1) & 3)) * 16 + (c & 1) * 8;
+    }
     template <typename C, typename Acc>
     __device__ __forceinline__ static void tile(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], float *strip, const TilePlace &now, int wave, int lane)
     {
-        constexpr int MI = C::MI, NJ = C::NJ, W = 16 / (int)sizeof(O), LPR = 32 / W, RPP = 64 / LPR, ROUNDS = 32 / RPP;
+        // Blocks side by side in the strip, in the output's type: a row of 64 columns of 16 bits is a whole line.  Rounded in front of the strip, not behind it (grad_in of 700,000 x 256 x
+        // 349 288 us with 32 columns of fp32 in the strip, 239; partial sums of a quarter of 8,192 x 512 x 131,072, multiplied in front of it, 338, 264).
+        constexpr int MI = C::MI, NJ = C::NJ, P = sizeof(O) == 2 && NJ % 2 == 0 ? 2 : 1, W = 16 / (int)sizeof(O), LPR = 32 * P / W, RPP = 64 / LPR, ROUNDS = 32 / RPP;
         int here = lane;
         asm volatile("" : "+v"(here)); // not kept through the products
         const int sr = here / LPR, sc = here % LPR, half = here >> 5, l32 = here & 31;
@@ -415,21 +430,23 @@ template <typename O> struct XentProductEpi {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int jj = 0; jj < NJ; ++jj) {
+            for (int jj = 0; jj < NJ; jj += P) {
                 const int64_t n = n0 + 32 * jj;
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const auto &a = acc[i][jj + p];
+                        char *const to = strip_four<P>(strip, l32, 8 * p + 2 * q + half);
+                        if constexpr (sizeof(O) == 4)
+                            *reinterpret_cast<StripWords4 *>(to) = StripWords4{__float_as_uint(a[4 * q] * f), __float_as_uint(a[4 * q + 1] * f), __float_as_uint(a[4 * q + 2] * f), __float_as_uint(a[4 * q + 3] * f)};
+                        else *reinterpret_cast<StripWords2 *>(to) = StripWords2{pack2_bf16(a[4 * q] * f, a[4 * q + 1] * f), pack2_bf16(a[4 * q + 2] * f, a[4 * q + 3] * f)};
+                    }
 #pragma unroll
                 for (int r = 0; r < ROUNDS; ++r) {
                     const int64_t m = m0 + 32 * i + RPP * r;
-                    float y[W];
-#pragma unroll
-                    for (int h = 0; h < W / 4; ++h) {
-                        const float4 v = *strip_at(strip, RPP * r + sr, sc * (W / 4) + h);
-                        y[4 * h] = v.x * f; y[4 * h + 1] = v.y * f; y[4 * h + 2] = v.z * f; y[4 * h + 3] = v.w * f;
-                    }
-                    if (m < it.M && n < it.N) store_piece(out + m * x.ld + n, static_cast<int>(min(it.N - n, static_cast<int64_t>(W))), pack16<O>(y));
+                    const uintx4 w = *reinterpret_cast<const StripWords4 *>(strip_four<P>(strip, RPP * r + sr, sc * (W / 4)));
+                    if (m < it.M && n < it.N) store_piece(out + m * x.ld + n, static_cast<int>(min(it.N - n, static_cast<int64_t>(W))), w);
                 }
             }
     }
@@ -437,7 +454,7 @@ template <typename O> struct XentProductEpi {
 
 // ---- host side ---------------------------------------------------------------------------------------------
 template <typename E, bool A_RC, bool B_RC, bool LARGE, bool STAGED> struct XentShape;
-// grad_in's 256 x 256 (8,192 x 512 x 32,768 and 700,000 x 256 x 349, us: 337 and 282; 256 x 128 by two workgroups a CU 387 and 348, 256 x 128 by one 460 and 377, four wavefronts with
+// grad_in's 256 x 256 (8,192 x 512 x 32,768 and 700,000 x 256 x 349, us, before their epilogue took a fifth less: 337 and 282; 256 x 128 by two workgroups a CU 387 and 348, 256 x 128 by one 460 and 377, four wavefronts with
 // 128 x 128 each 313 and 326) and grad_W's, whose operands are both read transposed, 256 x 128 by two workgroups a CU, a wavefront 64 x 128 (261 and 219; 256 x 256 320 and 248, 64
 // columns a wavefront 331 and 256).
 template <> struct XentShape<bf16_t, false, false, true, false> { using type = TileShape<bf16_t, 2, 1, false, false, kDirect, 2, 4, 4, 2, 64, 2, 1>; };
@@ -695,7 +712,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
     }
     const int64_t n_r = (n + R - 1) / R, n_v = (V + Vc - 1) / Vc;
     // rows of D an odd number of 128 bytes apart (8,192 x 512 x 130,072: 5,760 us at 65,536 bytes, 5,515)
-    const int64_t ld_d = round_up(Vc, 8) + (round_up(Vc, 8) * static_cast<int64_t>(sizeof(E)) % 1024 == 0 ? 64 : 0);
+        const int64_t ld_d = round_up(Vc, 8) + (round_up(Vc, 8) * static_cast<int64_t>(sizeof(E)) % 1024 == 0 ? 64 : 0);
     const bool copy_w = bf16 && copies_pay(n) && !direct_rows(a.W, a.ld_w, 2), copy_in = bf16 && copies_pay(n) && !direct_rows(a.in, a.ld_in, 2);
     const int64_t ld_wc = round_up(V, 8), ld_ic = round_up(d, 8);
     int32_t in_splits = 1, w_splits = 1;
