@@ -114,12 +114,15 @@ template <typename O> __device__ __forceinline__ uintx4 load_piece(const O *p, i
     constexpr int W = 16 / (int)sizeof(O);
     if (valid >= W) return load16(p);
     uintx4 w = {0u, 0u, 0u, 0u};
+    if (valid <= 0) return w;
+    O v[W - 1]; // the last one there is in the place of those that are not: loads under a branch each would be awaited one by one
 #pragma unroll
-    for (int e = 0; e < W; ++e)
-        if (e < valid) {
-            if constexpr (sizeof(O) == 2) w[e / 2] |= static_cast<uint32_t>(p[e]) << (16 * (e & 1));
-            else w[e] = __float_as_uint(p[e]);
-        }
+    for (int e = 0; e < W - 1; ++e) v[e] = p[min(e, valid - 1)];
+#pragma unroll
+    for (int e = 0; e < W - 1; ++e) {
+        if constexpr (sizeof(O) == 2) w[e / 2] |= e < valid ? static_cast<uint32_t>(v[e]) << (16 * (e & 1)) : 0u;
+        else w[e] = e < valid ? __float_as_uint(v[e]) : 0u;
+    }
     return w;
 }
 
