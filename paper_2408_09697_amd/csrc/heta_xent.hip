@@ -7,8 +7,8 @@
 // the exponentials below it, 8 bytes for 64 logits; a second kernel joins a row's.  The label's logit is taken from the registers it is in.
 // Backward: the logits are formed again (2 d operations each; kept in 4 bytes they would cost as long to write and read at d = 1,024 and
 // longer below), their epilogue makes D of them, and two products read D.  D is made in pieces of 512 MB, of about as many rows as classes,
-// since every further piece along the classes adds n d partial sums of grad_in, and every one along the rows d V of grad_W (192 MB, which the last-level cache holds: the products
-// read it a third faster, but there are more of them, split further; 8,192 x 512 x 131,072 5,823 us for 5,419; 256 MB 6,112, 768 MB 6,110).
+// since every further piece along the classes adds n d partial sums of grad_in, and every one along the rows d V of grad_W (8,192 x 512 x 131,072, us:
+// 5,044; 192 MB, which the last-level cache holds, but with more products, split further, 5,602; 256 MB 5,507, 1 GB 5,103, all at once 5,277).
 // D is stored in the operands' type: the matrix instruction reads 16 bits, and its rounding (2^-9 of each D, to and fro) is below that of a gradient
 // in 16 bits.  F, which all rows share (scale, over the number of labelled rows), multiplies the sums: in D, its rounding would be the same for all labels' elements
 // (8,192 x 512 x 131,072: gradients 3.7e-3 of their norm off, 1.7e-3 this way, their own rounding).  grad_bias is added up from the unrounded D in the epilogue's registers.
@@ -302,7 +302,7 @@ struct XentBackward {
 template <typename O> struct XentBackwardEpi {
     static constexpr int kItems = 1;
     static constexpr bool kTile = true;
-    // a wavefront's columns side by side: 64 columns of 16 bits are stored as whole lines (a quarter of 8,192 x 512 x 131,072 448 us by 32 columns, 420; 700,000 x 256 x 349 365, 325)
+    // a wavefront's columns side by side: 64 columns of 16 bits are stored as whole lines (a quarter of 8,192 x 512 x 131,072 441 us by 32 columns, 420; 700,000 x 256 x 349 353, 325)
     template <typename C> static constexpr int kStrip = 4096 * C::NJ;
     using Extra = XentBackward;
     __device__ __forceinline__ static void choose(const Extra &, TileItem &) {}
@@ -386,8 +386,6 @@ struct XentProduct {
     const uint32_t *poison; // nullable: no copy
     uint32_t call;
 };
-typedef uint32_t StripWords2 __attribute__((ext_vector_type(2), may_alias));
-typedef uint32_t StripWords4 __attribute__((ext_vector_type(4), may_alias));
 template <typename O> struct XentProductEpi {
     static constexpr int kItems = 1;
     static constexpr bool kTile = true;
@@ -408,45 +406,37 @@ template <typename O> struct XentProductEpi {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][jj][v] = 0.f;
     }
-    // Four columns from 4 c on of a row of 32 P columns.  fp32: as strip_at.  16 bits: pieces of 16 bytes, 4 P of them a row, so placed that rows whose
-    // pieces would begin in the same bank do not.
-    template <int P> __device__ __forceinline__ static char *strip_four(float *strip, int row, int c)
-    {
-        if constexpr (sizeof(O) == 4) return reinterpret_cast<char *>(strip_at<32 * P>(strip, row, c));
-        else return reinterpret_cast<char *>(strip) + row * (64 * P) + ((c / 2) ^ (P == 2 ? row & 7 : (row >> 1) & 3)) * 16 + (c & 1) * 8;
-    }
     template <typename C, typename Acc>
     __device__ __forceinline__ static void tile(const Extra &x, const TileItem &it, Acc (&acc)[C::MI][C::NJ], float *strip, const TilePlace &now, int wave, int lane)
     {
-        // Blocks side by side in the strip, in the output's type: a row of 64 columns of 16 bits is a whole line.  Rounded in front of the strip, not behind it (grad_in of 700,000 x 256 x
-        // 349 288 us with 32 columns of fp32 in the strip, 239; partial sums of a quarter of 8,192 x 512 x 131,072, multiplied in front of it, 338, 264).
-        constexpr int MI = C::MI, NJ = C::NJ, P = sizeof(O) == 2 && NJ % 2 == 0 ? 2 : 1, W = 16 / (int)sizeof(O), LPR = 32 * P / W, RPP = 64 / LPR, ROUNDS = 32 / RPP;
+        constexpr int MI = C::MI, NJ = C::NJ, W = 16 / (int)sizeof(O), LPR = 32 / W, RPP = 64 / LPR, ROUNDS = 32 / RPP;
         int here = lane;
         asm volatile("" : "+v"(here)); // not kept through the products
         const int sr = here / LPR, sc = here % LPR, half = here >> 5, l32 = here & 31;
         const int64_t m0 = now.m0 + (wave / C::WN) * (32 * MI) + sr, n0 = now.n0 + (wave % C::WN) * (32 * NJ) + sc * W;
         O *const out = static_cast<O *>(x.out) + now.split * it.M * x.ld;
-        const float f = x.factor ? *x.factor : 1.f;
+        // awaited here: left to the branches below, a load is awaited behind every store so far at each of its uses (grad_in of 700,000 x 256 x 349 288 us that way, 249 this way; partial
+        // sums of a quarter of 8,192 x 512 x 131,072 338 and 267)
+        float f = x.factor ? *x.factor : 1.f;
+        asm volatile("" : "+v"(f));
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int jj = 0; jj < NJ; jj += P) {
+            for (int jj = 0; jj < NJ; ++jj) {
                 const int64_t n = n0 + 32 * jj;
 #pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const auto &a = acc[i][jj + p];
-                        char *const to = strip_four<P>(strip, l32, 8 * p + 2 * q + half);
-                        if constexpr (sizeof(O) == 4)
-                            *reinterpret_cast<StripWords4 *>(to) = StripWords4{__float_as_uint(a[4 * q] * f), __float_as_uint(a[4 * q + 1] * f), __float_as_uint(a[4 * q + 2] * f), __float_as_uint(a[4 * q + 3] * f)};
-                        else *reinterpret_cast<StripWords2 *>(to) = StripWords2{pack2_bf16(a[4 * q] * f, a[4 * q + 1] * f), pack2_bf16(a[4 * q + 2] * f, a[4 * q + 3] * f)};
-                    }
+                for (int q = 0; q < 4; ++q)
+                    *strip_at(strip, l32, 2 * q + half) = make_float4(acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]);
 #pragma unroll
                 for (int r = 0; r < ROUNDS; ++r) {
                     const int64_t m = m0 + 32 * i + RPP * r;
-                    const uintx4 w = *reinterpret_cast<const StripWords4 *>(strip_four<P>(strip, RPP * r + sr, sc * (W / 4)));
-                    if (m < it.M && n < it.N) store_piece(out + m * x.ld + n, static_cast<int>(min(it.N - n, static_cast<int64_t>(W))), w);
+                    float y[W];
+#pragma unroll
+                    for (int h = 0; h < W / 4; ++h) {
+                        const float4 v = *strip_at(strip, RPP * r + sr, sc * (W / 4) + h);
+                        y[4 * h] = v.x * f; y[4 * h + 1] = v.y * f; y[4 * h + 2] = v.z * f; y[4 * h + 3] = v.w * f;
+                    }
+                    if (m < it.M && n < it.N) store_piece(out + m * x.ld + n, static_cast<int>(min(it.N - n, static_cast<int64_t>(W))), pack16<O>(y));
                 }
             }
     }
