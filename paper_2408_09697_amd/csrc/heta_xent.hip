@@ -458,6 +458,9 @@ using XentSkinnyBackwardTiles = TileShape<bf16_t, 2, 1, false, true, kDirect, 1,
 // 128 x 128 1,526 and 6,090; each when its sums started from zero instead of the bias: 1,581 and 6,186 for this one).
 using XentForwardTiles = TileShape<bf16_t, 2, 1, false, true, kDirect, 2, 2, 4, 2, 32, 3, 2>;
 using XentBackwardTiles = TileShape<bf16_t, 2, 1, false, true, kDirect, 2, 2, 4, 2, 32, 2, 2>;
+// grad_W's where 256 x 128 would have more beyond its rows
+template <typename E> struct XentTurned { using type = TileShape<float, 2, 3, true, true, kStaged, 2, 4, 2, 2, 32, 2, 1>; };                 // 128 x 256
+template <> struct XentTurned<bf16_t> { using type = TileShape<bf16_t, 2, 1, true, true, kDirect, 1, 4, 4, 2, 32, 2, 2>; };
 template <bool A_RC, bool B_RC> struct XentShape<bf16_t, A_RC, B_RC, false, false> { using type = TileShape<bf16_t, 2, 1, A_RC, B_RC, kDirect, 2, 2, 1, 1, 64, 3, 2>; };  // 64 x 64
 template <bool A_RC, bool B_RC, bool LARGE> struct XentShape<bf16_t, A_RC, B_RC, LARGE, true> { using type = TileShape<bf16_t, 2, 1, A_RC, B_RC, kStaged, 2, 2, 1, 1, 64, 2, 2>; };
 template <bool A_RC, bool B_RC, bool STAGED> struct XentShape<float, A_RC, B_RC, true, STAGED> { using type = TileShape<float, 2, 3, A_RC, B_RC, kStaged, 4, 2, 2, 2, 32, 2, 1>; };  // 256 x 128
@@ -496,16 +499,15 @@ template <typename E> __global__ void __launch_bounds__(256) xent_align_kernel(c
 }
 static unsigned walk(int64_t items) { return static_cast<unsigned>(std::min<int64_t>((items + 255) / 256, 16384)); }
 
-enum XentTiles { kTilesLarge, kTilesSmall, kTilesSkinny, kTilesStaged };
-// The tiles of a product M x N of `splits` parts: staged where bf16 rows are not aligned, large where they give every second CU one and are not mostly
-// beyond the last row or column.
-template <typename E> static XentTiles tiles_for(bool direct, int64_t M, int64_t N, int64_t splits)
+enum XentTiles { kTilesLarge, kTilesTurned, kTilesSmall, kTilesSkinny, kTilesStaged };
+// The tiles of a product: staged where bf16 rows are not aligned, large where they give every second CU one and are not mostly beyond the last row or column.
+// Those of the logits: a tile for few rows too.
+template <typename E> static XentTiles logit_tiles_for(bool direct, int64_t M, int64_t N)
 {
     if (sizeof(E) == 2 && !direct) return kTilesStaged;
-    return M > 64 && N > 64 && tiles_of(M, N, 256, 256) * splits >= 128 ? kTilesLarge : kTilesSmall;
+    if (sizeof(E) == 2 && M <= 32) return kTilesSkinny;
+    return M > 64 && N > 64 && tiles_of(M, N, 256, 256) >= 128 ? kTilesLarge : kTilesSmall;
 }
-// Those of the logits: a tile for few rows too.
-template <typename E> static XentTiles logit_tiles_for(bool direct, int64_t M, int64_t N) { return sizeof(E) == 2 && direct && M <= 32 ? kTilesSkinny : tiles_for<E>(direct, M, N, 1); }
 // f(shape)
 template <typename T> struct Tag { using type = T; };
 template <typename E, bool A_RC, bool B_RC, typename Epi, typename F> static heta_status with_tiles(XentTiles t, F f)
@@ -517,6 +519,8 @@ template <typename E, bool A_RC, bool B_RC, typename Epi, typename F> static het
     if constexpr (BACKWARD)
         if (t == kTilesSkinny) return f(Tag<XentSkinnyBackwardTiles>{});
     if (t == kTilesSmall) return f(XentShape<E, A_RC, B_RC, false, false>{});
+    if constexpr (A_RC && B_RC)
+        if (t == kTilesTurned) return f(XentTurned<E>{});
     if constexpr (FORWARD) return f(Tag<XentForwardTiles>{});
     else if constexpr (BACKWARD) return f(Tag<XentBackwardTiles>{});
     else return f(XentShape<E, A_RC, B_RC, true, false>{});
@@ -675,12 +679,37 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     return HETA_OK;
 }
 
-// splits of a contraction over K for tiles of M x N outputs: one workgroup per CU
-static void split_for(int64_t M, int64_t N, int64_t K, int64_t least, int32_t *n_split, int64_t *k_per_split)
+// A product whose contraction over K may be split: as many parts as fill the chip once, counted in the tiles that are used (forward and both gradients, us: fp32 5,003 x 300 x 2,983 378
+// where 256 x 256 were counted for all and grad_W had 256 x 128 only, 338; 3,000 x 100 x 5,000 187, 163; bf16 700,000 x 256 x 349 1,024, 998; 200,000 x 512 x 100 296, 306).
+struct SplitProduct {
+    XentTiles tiles;
+    int32_t splits;
+    int64_t k_each;
+};
+// bm x bn: the large tiles, `slots` of which the chip holds at a time
+template <typename E> static SplitProduct split_product(bool direct, int64_t M, int64_t N, int64_t K, int64_t least, XentTiles large, int bm, int bn, int64_t slots, int32_t at_most)
 {
-    const int64_t tiles = tiles_of(M, N, 256, 256), most = std::max<int64_t>(1, 256 / tiles);
-    *k_per_split = round_up(std::max((K + most - 1) / most, least), 64);
-    *n_split = static_cast<int32_t>((K + *k_per_split - 1) / *k_per_split);
+    const int64_t tiles = tiles_of(M, N, bm, bn), most = std::max<int64_t>(1, slots / tiles);
+    SplitProduct p;
+    p.k_each = round_up(std::max((K + most - 1) / most, least), 64);
+    p.splits = static_cast<int32_t>((K + p.k_each - 1) / p.k_each);
+    if (p.splits > at_most) {
+        p.k_each = round_up((K + at_most - 1) / at_most, 64);
+        p.splits = static_cast<int32_t>((K + p.k_each - 1) / p.k_each);
+    }
+    p.tiles = sizeof(E) == 2 && !direct ? kTilesStaged : M > 64 && N > 64 && tiles * p.splits * 2 >= slots ? large : kTilesSmall;
+    return p;
+}
+template <typename E> static SplitProduct grad_in_product(bool direct, int64_t n, int64_t d, int64_t V, int32_t at_most)
+{
+    return split_product<E>(direct, n, d, V, 512, kTilesLarge, 256, sizeof(E) == 2 ? 256 : 128, 256, at_most);
+}
+// 256 x 128 tiles or 128 x 256, whichever have less beyond the result
+template <typename E> static SplitProduct grad_w_product(bool direct, int64_t n, int64_t d, int64_t V, int32_t at_most)
+{
+    const int64_t slots = sizeof(E) == 2 ? 512 : 256;
+    if (round_up(d, 128) * round_up(V, 256) < round_up(d, 256) * round_up(V, 128)) return split_product<E>(direct, d, V, n, 256, kTilesTurned, 128, 256, slots, at_most);
+    return split_product<E>(direct, d, V, n, 256, kTilesLarge, 256, 128, slots, at_most);
 }
 
 template <typename E> static heta_status xent_backward(heta_graph *g, const heta_linear_xent_bwd_args &a, hipStream_t st)
@@ -705,11 +734,8 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
         const int64_t ld_d = round_up(Vc, 8) + (round_up(Vc, 8) * static_cast<int64_t>(sizeof(E)) % 1024 == 0 ? 64 : 0);
     const bool copy_w = bf16 && copies_pay(n) && !direct_rows(a.W, a.ld_w, 2), copy_in = bf16 && copies_pay(n) && !direct_rows(a.in, a.ld_in, 2);
     const int64_t ld_wc = round_up(V, 8), ld_ic = round_up(d, 8);
-    int32_t in_splits = 1, w_splits = 1;
-    int64_t in_k = Vc, w_k = R;
-    split_for(R, d, Vc, 512, &in_splits, &in_k);
-    split_for(d, Vc, R, 256, &w_splits, &w_k);
     const bool direct_w = copy_w || direct_rows(a.W, a.ld_w, 2), direct_in = copy_in || direct_rows(a.in, a.ld_in, 2);
+    const int32_t in_splits = grad_in_product<E>(direct_w, R, d, Vc, INT32_MAX).splits, w_splits = grad_w_product<E>(direct_in, R, d, Vc, INT32_MAX).splits;
     Regions ws;
     const size_t poison_at = ws.take(8), rows_at = ws.take(static_cast<size_t>(n) * sizeof(XentRow));
     const size_t w_at = ws.take(copy_w ? static_cast<size_t>(d) * ld_wc * 2 : 0), in_at = ws.take(a.dW ? static_cast<size_t>(n) * ld_ic * sizeof(E) : copy_in ? static_cast<size_t>(n) * ld_ic * 2 : 0);
@@ -774,16 +800,11 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 if (sums && !single) bias_slots += (rn + strip_rows - 1) / strip_rows; // none without dbias: nothing is added up below
             }
             if (a.grad_in) {
-                int32_t splits = 1;
-                int64_t k_each = cols;
-                split_for(rn, d, cols, 512, &splits, &k_each);
-                splits = std::min(splits, in_splits);
-                if (static_cast<int64_t>(splits) * k_each < cols) k_each = round_up((cols + splits - 1) / splits, 64), splits = static_cast<int32_t>((cols + k_each - 1) / k_each);
+                const auto [tiles, splits, k_each] = grad_in_product<E>(direct_w, rn, d, cols, in_splits);
                 const Launch l{g, who, "xent_grad_in_kernel", TileItem{base + d_at, Wv, ld_d, W.ld, 0, 0, rn, d, cols, k_each, splits, 0, 0, 0, 0, 0},
                                (static_cast<double>(rn) * (d + cols) + static_cast<double>(d) * cols) * sizeof(E), product, st};
                 float *so_far = reinterpret_cast<float *>(base + di_at) + (n_v > 1 ? r * R * d : 0), *part = reinterpret_cast<float *>(base + di_at) + (n_v > 1 ? n_r * R * d : 0);
                 E *out = static_cast<E *>(a.grad_in) + r0 * a.ld_gi;
-                const XentTiles tiles = tiles_for<E>(direct_w, rn, d, splits);
                 if (splits == 1 && n_v == 1) {
                     HETA_TRY((go_tiles<E, false, false, XentProductEpi<E>>(l, tiles, XentProduct{out, a.ld_gi, factor, nullptr, 0, nullptr, 0})));
                 } else {
@@ -794,15 +815,10 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 }
             }
             if (a.dW) {
-                int32_t splits = 1;
-                int64_t k_each = rn;
-                split_for(d, cols, rn, 256, &splits, &k_each);
-                splits = std::min(splits, w_splits);
-                if (static_cast<int64_t>(splits) * k_each < rn) k_each = round_up((rn + splits - 1) / splits, 64), splits = static_cast<int32_t>((rn + k_each - 1) / k_each);
+                const auto [tiles, splits, k_each] = grad_w_product<E>(direct_in, rn, d, cols, w_splits);
                 // a column's row blocks one after the other: they share its part of D
                 const Launch l{g, who, "xent_grad_w_kernel", TileItem{in_r, base + d_at, in.ld, ld_d, 0, 0, d, cols, rn, k_each, splits, 0, 0, 0, 0, 0, 64},
                                (static_cast<double>(rn) * (d + cols)) * sizeof(E) + 4.0 * splits * d * cols, product, st};
-                const XentTiles tiles = tiles_for<E>(direct_in, d, cols, splits);
                 XentProduct x{dw + dw_parts * d * cols, cols, nullptr, clean + r0 * ld_ic, ld_ic, poison, call};
                 if (splits == 1 && n_r == 1) {
                     x.out = static_cast<char *>(a.dW) + v0 * dtype_size(a.dw_dt);

@@ -450,3 +450,9 @@ def test_two_captured_graphs_of_many_rows_on_one_handle(handle):
         torch.cuda.synchronize()
         for got, w in zip((p.loss, p.mean, p.gx, p.gW, p.gb), want):
             assert torch.equal(got, w), k
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d,classes", [(5003, 300, 2983), (9001, 100, 1500), (6000, 65, 4100), (7003, 389, 700)])
+def test_weight_gradient_tiles_of_fewer_rows_than_columns(handle, n, d, classes, dtype):
+    test_loss_and_gradients(handle, n, d, classes, dtype)
