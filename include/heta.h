@@ -747,7 +747,7 @@ heta_status heta_linear_xent(heta_graph *g, const heta_linear_xent_args *args, v
  * grad_loss: device fp32 [n_rows] or NULL; mean: what the forward wrote (gradients of the mean) or NULL (of the sum).  All outputs are overwritten; sums
  * are added in a fixed order.  The products read D rounded to dt.  The logits are formed again.
  * Uses the handle's workspace (may grow it: by 512 MB of D or D itself where that is less, a copy of the rows, partial sums of the gradients, and copies as
- * above). */
+ * above, of weights also where a row has 16 MB and more; a copy of weights holds as many classes as the piece of D). */
 typedef struct heta_linear_xent_bwd_args {
     int64_t n_rows;
     int32_t d, n_classes;

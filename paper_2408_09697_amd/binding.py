@@ -42,7 +42,7 @@ EXPORTS = ["heta_graph_create", "heta_graph_create_batch", "heta_graph_destroy",
            "heta_graph_index_bytes", "heta_rms_norm", "heta_rms_norm_bwd", "heta_linear", "heta_linear_bwd", "heta_linear_pack_e4m3", "heta_muon_multi",
            "heta_linear_rows_i8", "heta_linear_pack_i8", "heta_linear_xent", "heta_linear_xent_bwd", "heta_adamw_multi"]
 # process-wide switches for tests and measurements, declared in csrc/heta_test_hooks.h (not in the public header)
-TEST_HOOKS = ["heta_projection_force_staged", "heta_ingest_force", "heta_projection_f32_native", "heta_workspace_limit"]
+TEST_HOOKS = ["heta_projection_force_staged", "heta_ingest_force", "heta_projection_f32_native", "heta_workspace_limit", "heta_xent_reads"]
 HETA_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 
@@ -1885,6 +1885,16 @@ def heta_projection_f32_native(on: bool) -> None:
     L = load_library()
     L.heta_projection_f32_native.argtypes = [ctypes.c_int32]
     _check(L.heta_projection_f32_native(1 if on else 0))
+
+
+def heta_xent_reads(n_rows: int, d: int, n_classes: int, backward: bool, inp: int = 0, ld_in: int = 0, W: int = 0, ld_w: int = 0) -> dict:
+    """How heta_linear_xent(_bwd) reads bf16 operands at the addresses inp and W (csrc/heta_test_hooks.h)."""
+    L = load_library()
+    L.heta_xent_reads.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p]
+    args = _XentBwdArgs(n_rows=n_rows, d=d, n_classes=n_classes, inp=inp, ld_in=ld_in or d, W=W, ld_w=ld_w or n_classes)
+    out = (ctypes.c_int64 * 8)()
+    _check(L.heta_xent_reads(ctypes.byref(args), int(backward), out))
+    return dict(zip(("copy_w", "copy_in", "logits", "grad_in", "grad_w", "classes", "reach_w", "reach_in"), out))
 
 
 def heta_workspace_limit(n_bytes: int) -> None:

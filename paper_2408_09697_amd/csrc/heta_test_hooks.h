@@ -29,6 +29,11 @@ heta_status heta_projection_f32_native(int32_t on);
  * holds already stays usable.  0 (the default): no limit. */
 heta_status heta_workspace_limit(int64_t bytes);
 
+/* How heta_linear_xent (backward = 0) and heta_linear_xent_bwd read bf16 operands at these addresses, of the arguments' sizes; no device call.  out, int64 [8]: 1 where W and where
+ * in are copied to aligned rows first; 1 where the operands of the logits, of grad_in and of grad_W go straight into LDS; the classes of a piece, which a copy of W holds;
+ * and the largest offset in bytes that such loads make from a tile's first row, of W and of in, which have 32 bits for it. */
+heta_status heta_xent_reads(const heta_linear_xent_bwd_args *args, int32_t backward, int64_t *out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,6 +20,7 @@
 #include <cmath>
 
 #include "heta_linear.h"
+#include "heta_test_hooks.h"
 
 namespace heta {
 
@@ -485,6 +486,38 @@ struct Operand {
     int64_t ld;
 };
 
+// How the products of bf16 operands read them (those of fp32 go through registers, their addresses are 64 bits wide).  Straight into LDS goes what lies in rows that start at 16 bytes
+// and whose offsets from a tile's first row stay below 2^32 bytes: kTileRows rows where a row's consecutive elements are contracted over (both operands of the logits but W, and W for
+// grad_in), kTileDepth of them where a row is one k-value (W for the logits; in and D for grad_W).  D's offsets do, being within a piece.
+constexpr int64_t kTileRows = 256, kTileDepth = 64;
+static bool aligned_rows(const void *p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
+static bool offsets_fit(int64_t rows, int64_t ld) { return rows * ld * 2 < (int64_t(1) << 32); }
+// Whether the products are worth aligned copies of their operands: where the weights are read by several tiles.
+static bool copies_pay(int64_t n) { return n >= 512; }
+struct XentReads {
+    bool copy_w = false, copy_in = false;                 // to aligned rows first: of W, as many classes as a piece has
+    bool logits = false, grad_in = false, grad_w = false; // products whose operands go straight into LDS
+    int64_t ld_w = 0, ld_in = 0;                          // of what the products read
+};
+// `classes`: those of a piece, which a copy of W holds at a time.  A forward pass reads W for the logits alone.
+static XentReads xent_reads(int64_t n, int64_t d, int64_t classes, const void *in, int64_t ld_in, const void *W, int64_t ld_w, bool backward)
+{
+    XentReads r;
+    const int64_t ld_wc = round_up(classes, 8), ld_ic = round_up(d, 8), w_rows = backward ? kTileRows : kTileDepth;
+    const bool w = aligned_rows(W, ld_w), x = aligned_rows(in, ld_in) && offsets_fit(kTileRows, ld_in);
+    r.copy_w = copies_pay(n) && !(w && offsets_fit(w_rows, ld_w)) && offsets_fit(w_rows, ld_wc);
+    r.copy_in = copies_pay(n) && !x && offsets_fit(kTileRows, ld_ic);
+    r.ld_w = r.copy_w ? ld_wc : ld_w;
+    r.ld_in = r.copy_in ? ld_ic : ld_in;
+    r.grad_w = x || r.copy_in;
+    // rows of 8 MB and more, forward + input gradient of n x 256 x 5,000,000, us, straight into LDS / through registers: 4 rows 461 + 1,140 / 601 + 1,251, 32 504 + 1,227 / 629 + 1,306,
+    // 64 790 + 2,095 / 684 + 1,681, 128 1,003 + 2,252 / 1,132 + 2,817, 511 2,085 + 5,232 / 4,340 + 10,114
+    const bool registers = n > 32 && n <= 64 && !offsets_fit(512, r.ld_w);
+    r.logits = r.grad_w && (w || r.copy_w) && offsets_fit(kTileDepth, r.ld_w) && !registers;
+    r.grad_in = (w || r.copy_w) && offsets_fit(kTileRows, r.ld_w) && !registers;
+    return r;
+}
+
 template <typename E> __global__ void __launch_bounds__(256) xent_align_kernel(const E *in, int64_t ld, int64_t n, int32_t d, E *out, int64_t ld_out)
 {
     const int chunks = static_cast<int>(ld_out / 8);
@@ -498,6 +531,8 @@ template <typename E> __global__ void __launch_bounds__(256) xent_align_kernel(c
     }
 }
 static unsigned walk(int64_t items) { return static_cast<unsigned>(std::min<int64_t>((items + 255) / 256, 16384)); }
+
+template <typename C> constexpr bool offsets_as_ruled() { return C::LOAD != kDirect || (C::BK <= kTileDepth && C::BM <= kTileRows && C::BN <= kTileRows); }
 
 enum XentTiles { kTilesLarge, kTilesTurned, kTilesSmall, kTilesSkinny, kTilesStaged };
 // The tiles of a product: staged where bf16 rows are not aligned, large where they give every second CU one and are not mostly beyond the last row or column.
@@ -527,7 +562,11 @@ template <typename E, bool A_RC, bool B_RC, typename Epi, typename F> static het
 }
 template <typename E, bool A_RC, bool B_RC, typename Epi> static heta_status go_tiles(const Launch &l, XentTiles t, const typename Epi::Extra &x)
 {
-    return with_tiles<E, A_RC, B_RC, Epi>(t, [&](auto shape) { return l.go<typename decltype(shape)::type, Epi>(x); });
+    return with_tiles<E, A_RC, B_RC, Epi>(t, [&](auto shape) {
+        using C = typename decltype(shape)::type;
+        static_assert(offsets_as_ruled<C>(), "xent_reads() knows tiles of kTileRows and kTileDepth");
+        return l.go<C, Epi>(x);
+    });
 }
 // rows and columns of a wavefront's sums
 template <typename E, typename Epi> static void strip_of(XentTiles t, int64_t *rows, int64_t *cols)
@@ -539,9 +578,6 @@ template <typename E, typename Epi> static void strip_of(XentTiles t, int64_t *r
         return HETA_OK;
     });
 }
-
-// Whether the product is worth aligned copies of its operands: where the weights are read by several tiles.
-static bool copies_pay(int64_t n) { return n >= 512; }
 
 // Sums over the parts of a contraction, after those of earlier pieces (nullable): out[i / width][i % width] for i < total, in a fixed order.
 template <typename O> __global__ void __launch_bounds__(256) xent_add_kernel(const float *so_far, const float *part, int splits, int64_t total, O *out, int32_t width, int64_t ld, const float *factor)
@@ -616,11 +652,10 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     const int64_t n = a.n_rows, d = a.d, V = a.n_classes;
     Regions ws;
     const bool bf16 = sizeof(E) == 2;
-    const bool copy_w = bf16 && copies_pay(n) && !direct_rows(a.W, a.ld_w, 2), copy_in = bf16 && copies_pay(n) && !direct_rows(a.in, a.ld_in, 2);
-    const int64_t ld_wc = round_up(V, 8), ld_ic = round_up(d, 8);
-    const size_t w_at = ws.take(copy_w ? static_cast<size_t>(d) * ld_wc * 2 : 0), in_at = ws.take(copy_in ? static_cast<size_t>(n) * ld_ic * 2 : 0);
+    const XentReads reads = bf16 ? xent_reads(n, d, V, a.in, a.ld_in, a.W, a.ld_w, false) : XentReads{};
+    const size_t w_at = ws.take(reads.copy_w ? static_cast<size_t>(d) * reads.ld_w * 2 : 0), in_at = ws.take(reads.copy_in ? static_cast<size_t>(n) * reads.ld_in * 2 : 0);
     const size_t target_at = ws.take(static_cast<size_t>(n) * 4);
-    const XentTiles tiles = logit_tiles_for<E>((copy_w || direct_rows(a.W, a.ld_w, 2)) && (copy_in || direct_rows(a.in, a.ld_in, 2)), n, V);
+    const XentTiles tiles = logit_tiles_for<E>(reads.logits, n, V);
     int64_t strip_rows = 0, strip_cols = 0;
     strip_of<E, XentForwardEpi>(tiles, &strip_rows, &strip_cols);
     const int64_t strips = (V + strip_cols - 1) / strip_cols;
@@ -636,13 +671,15 @@ template <typename E> static heta_status xent_forward(heta_graph *g, const heta_
     HETA_TRY(ensure_workspace(g, ws.bytes));
     char *base = static_cast<char *>(g->d_ws);
     Operand W{a.W, a.ld_w}, in{a.in, a.ld_in};
-    if (copy_w) {
-        hipLaunchKernelGGL(xent_align_kernel<bf16_t>, dim3(walk(d * ld_wc / 8)), dim3(256), 0, st, static_cast<const bf16_t *>(a.W), a.ld_w, d, a.n_classes, reinterpret_cast<bf16_t *>(base + w_at), ld_wc);
-        W = {base + w_at, ld_wc};
+    if (reads.copy_w) {
+        hipLaunchKernelGGL(xent_align_kernel<bf16_t>, dim3(walk(d * reads.ld_w / 8)), dim3(256), 0, st, static_cast<const bf16_t *>(a.W), a.ld_w, d, a.n_classes, reinterpret_cast<bf16_t *>(base + w_at),
+                           reads.ld_w);
+        W = {base + w_at, reads.ld_w};
     }
-    if (copy_in) {
-        hipLaunchKernelGGL(xent_align_kernel<bf16_t>, dim3(walk(n * ld_ic / 8)), dim3(256), 0, st, static_cast<const bf16_t *>(a.in), a.ld_in, n, a.d, reinterpret_cast<bf16_t *>(base + in_at), ld_ic);
-        in = {base + in_at, ld_ic};
+    if (reads.copy_in) {
+        hipLaunchKernelGGL(xent_align_kernel<bf16_t>, dim3(walk(n * reads.ld_in / 8)), dim3(256), 0, st, static_cast<const bf16_t *>(a.in), a.ld_in, n, a.d, reinterpret_cast<bf16_t *>(base + in_at),
+                           reads.ld_in);
+        in = {base + in_at, reads.ld_in};
     }
     HETA_LAUNCH_CHECK("xent_align_kernel");
     // Weights that an XCD's L2 does not hold are read by four row blocks at a time (8,192 x 512 x 131,072: 1,250 us one by one, 1,187; eight 1,188, sixteen 1,228).  D's tiles, which
@@ -712,14 +749,14 @@ template <typename E> static SplitProduct grad_w_product(bool direct, int64_t n,
     return split_product<E>(direct, d, V, n, 256, kTilesLarge, 256, 128, slots, at_most);
 }
 
-template <typename E> static heta_status xent_backward(heta_graph *g, const heta_linear_xent_bwd_args &a, hipStream_t st)
+// Rows and classes of a piece of D: all of them, or kXentPiece bytes of pieces of one size.
+struct PieceOfD {
+    int64_t rows, classes;
+};
+static PieceOfD piece_of_d(int64_t n, int64_t V, size_t elt)
 {
-    const char *who = "heta_linear_xent_bwd";
-    const int64_t n = a.n_rows, d = a.d, V = a.n_classes;
-    const bool bf16 = sizeof(E) == 2;
-    const heta_dtype dt = bf16 ? HETA_BF16 : HETA_F32;
-    const int64_t room = kXentPiece / static_cast<int64_t>(sizeof(E));
-    int64_t R = n, Vc = V; // a piece of D
+    const int64_t room = kXentPiece / static_cast<int64_t>(elt);
+    int64_t R = n, Vc = V;
     if (n * round_up(V, 8) > room) {
         const int64_t side = static_cast<int64_t>(std::sqrt(static_cast<double>(room)));
         R = std::min(n, std::max(side, room / round_up(V, 8)));
@@ -729,16 +766,25 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
         R = std::min(R, n);
         Vc = std::min(Vc, V);
     }
+    return {R, Vc};
+}
+
+template <typename E> static heta_status xent_backward(heta_graph *g, const heta_linear_xent_bwd_args &a, hipStream_t st)
+{
+    const char *who = "heta_linear_xent_bwd";
+    const int64_t n = a.n_rows, d = a.d, V = a.n_classes;
+    const bool bf16 = sizeof(E) == 2;
+    const heta_dtype dt = bf16 ? HETA_BF16 : HETA_F32;
+    const auto [R, Vc] = piece_of_d(n, V, sizeof(E));
     const int64_t n_r = (n + R - 1) / R, n_v = (V + Vc - 1) / Vc;
     // rows of D an odd number of 128 bytes apart (8,192 x 512 x 130,072: 5,760 us at 65,536 bytes, 5,515)
-        const int64_t ld_d = round_up(Vc, 8) + (round_up(Vc, 8) * static_cast<int64_t>(sizeof(E)) % 1024 == 0 ? 64 : 0);
-    const bool copy_w = bf16 && copies_pay(n) && !direct_rows(a.W, a.ld_w, 2), copy_in = bf16 && copies_pay(n) && !direct_rows(a.in, a.ld_in, 2);
-    const int64_t ld_wc = round_up(V, 8), ld_ic = round_up(d, 8);
-    const bool direct_w = copy_w || direct_rows(a.W, a.ld_w, 2), direct_in = copy_in || direct_rows(a.in, a.ld_in, 2);
-    const int32_t in_splits = grad_in_product<E>(direct_w, R, d, Vc, INT32_MAX).splits, w_splits = grad_w_product<E>(direct_in, R, d, Vc, INT32_MAX).splits;
+    const int64_t ld_d = round_up(Vc, 8) + (round_up(Vc, 8) * static_cast<int64_t>(sizeof(E)) % 1024 == 0 ? 64 : 0);
+    const XentReads reads = bf16 ? xent_reads(n, d, Vc, a.in, a.ld_in, a.W, a.ld_w, true) : XentReads{};
+    const int64_t ld_ic = round_up(d, 8);
+    const int32_t in_splits = grad_in_product<E>(reads.grad_in, R, d, Vc, INT32_MAX).splits, w_splits = grad_w_product<E>(reads.grad_w, R, d, Vc, INT32_MAX).splits;
     Regions ws;
     const size_t poison_at = ws.take(8), rows_at = ws.take(static_cast<size_t>(n) * sizeof(XentRow));
-    const size_t w_at = ws.take(copy_w ? static_cast<size_t>(d) * ld_wc * 2 : 0), in_at = ws.take(a.dW ? static_cast<size_t>(n) * ld_ic * sizeof(E) : copy_in ? static_cast<size_t>(n) * ld_ic * 2 : 0);
+    const size_t w_at = ws.take(reads.copy_w ? static_cast<size_t>(d) * reads.ld_w * 2 : 0), in_at = ws.take(a.dW || reads.copy_in ? static_cast<size_t>(n) * ld_ic * sizeof(E) : 0);
     const size_t d_at = ws.take(static_cast<size_t>(R) * ld_d * sizeof(E));
     const size_t sums_at = ws.take(a.dbias ? static_cast<size_t>((R + 31) / 32 * n_r) * Vc * 4 : 0);
     const size_t joined_at = ws.take(a.dbias ? static_cast<size_t>(64) * Vc * 4 : 0);
@@ -754,7 +800,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
     const uint32_t call = ++g->xent_calls;
     E *clean = reinterpret_cast<E *>(base + in_at);
     // few rows: their copy is made at once, and taken whatever they hold (a launch less: 11 x 47 x 3, forward and gradients, 37.7 us for 35.0)
-    const bool at_once = (a.dW || copy_in) && n * ld_ic * static_cast<int64_t>(sizeof(E)) <= int64_t(8) << 20;
+    const bool at_once = (a.dW || reads.copy_in) && n * ld_ic * static_cast<int64_t>(sizeof(E)) <= int64_t(8) << 20;
     {
         ProfScope prof("xent_prepare_kernel", st, 32.0 * n, 0);
         if (at_once && d >= 128)
@@ -767,20 +813,23 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
             hipLaunchKernelGGL(xent_prepare_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, a.labels, a.lse, a.grad_loss, a.mean, a.scale, n, V, rows, factor, poison, call);
         HETA_LAUNCH_CHECK("xent_prepare_kernel");
     }
-    Operand W{a.W, a.ld_w}, in{a.in, a.ld_in};
-    if (copy_w) {
-        hipLaunchKernelGGL(xent_align_kernel<bf16_t>, dim3(walk(d * ld_wc / 8)), dim3(256), 0, st, static_cast<const bf16_t *>(a.W), a.ld_w, d, a.n_classes, reinterpret_cast<bf16_t *>(base + w_at), ld_wc);
-        W = {base + w_at, ld_wc};
-    }
-    if ((copy_in || a.dW) && !at_once)
-        hipLaunchKernelGGL(xent_clean_kernel<E>, dim3(walk(n * ld_ic / 8)), dim3(256), 0, st, static_cast<const E *>(a.in), a.ld_in, n, a.d, rows, clean, ld_ic, copy_in, poison, call);
-    if (copy_in) in = {clean, ld_ic};
-    HETA_LAUNCH_CHECK("xent_align_kernel");
+    Operand in{a.in, a.ld_in};
+    if ((reads.copy_in || a.dW) && !at_once)
+        hipLaunchKernelGGL(xent_clean_kernel<E>, dim3(walk(n * ld_ic / 8)), dim3(256), 0, st, static_cast<const E *>(a.in), a.ld_in, n, a.d, rows, clean, ld_ic, reads.copy_in, poison, call);
+    if (reads.copy_in) in = {clean, ld_ic};
+    HETA_LAUNCH_CHECK("xent_clean_kernel");
 
     float *sums = a.dbias ? reinterpret_cast<float *>(base + sums_at) : nullptr;
     for (int64_t v = 0; v < n_v; ++v) {
         const int64_t v0 = v * Vc, cols = std::min(Vc, V - v0);
-        const E *Wv = static_cast<const E *>(W.p) + v0;
+        const E *Wv = static_cast<const E *>(a.W) + v0;
+        const int64_t ld_w = reads.copy_w ? reads.ld_w : a.ld_w;
+        if (reads.copy_w) { // of this piece's classes: rows of any length are short ones here
+            bf16_t *const copy = reinterpret_cast<bf16_t *>(base + w_at);
+            hipLaunchKernelGGL(xent_align_kernel<bf16_t>, dim3(walk(d * ld_w / 8)), dim3(256), 0, st, reinterpret_cast<const bf16_t *>(Wv), a.ld_w, d, static_cast<int32_t>(cols), copy, ld_w);
+            HETA_LAUNCH_CHECK("xent_align_kernel");
+            Wv = reinterpret_cast<const E *>(copy);
+        }
         float *dw = reinterpret_cast<float *>(base + dw_at);
         int64_t bias_slots = 0, dw_parts = 0;
         for (int64_t r = 0; r < n_r; ++r) {
@@ -788,9 +837,9 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
             const E *in_r = static_cast<const E *>(in.p) + r0 * in.ld;
             const double product = 2.0 * rn * d * cols;
             {
-                const Launch l{g, who, "xent_logit_grad_kernel", TileItem{in_r, Wv, in.ld, W.ld, 0, 0, rn, cols, d, d, 1, 0, 0, 0, 0, 0, 0},
+                const Launch l{g, who, "xent_logit_grad_kernel", TileItem{in_r, Wv, in.ld, ld_w, 0, 0, rn, cols, d, d, 1, 0, 0, 0, 0, 0, 0},
                                (static_cast<double>(rn) * (d + cols) + static_cast<double>(d) * cols) * sizeof(E), product, st};
-                const XentTiles tiles = logit_tiles_for<E>(direct_w && direct_in, rn, cols);
+                const XentTiles tiles = logit_tiles_for<E>(reads.logits, rn, cols);
                 int64_t strip_rows = 0, strip_cols = 0;
                 strip_of<E, XentBackwardEpi<E>>(tiles, &strip_rows, &strip_cols);
                 const bool single = sums && n_r == 1 && rn <= strip_rows;
@@ -800,8 +849,8 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 if (sums && !single) bias_slots += (rn + strip_rows - 1) / strip_rows; // none without dbias: nothing is added up below
             }
             if (a.grad_in) {
-                const auto [tiles, splits, k_each] = grad_in_product<E>(direct_w, rn, d, cols, in_splits);
-                const Launch l{g, who, "xent_grad_in_kernel", TileItem{base + d_at, Wv, ld_d, W.ld, 0, 0, rn, d, cols, k_each, splits, 0, 0, 0, 0, 0},
+                const auto [tiles, splits, k_each] = grad_in_product<E>(reads.grad_in, rn, d, cols, in_splits);
+                const Launch l{g, who, "xent_grad_in_kernel", TileItem{base + d_at, Wv, ld_d, ld_w, 0, 0, rn, d, cols, k_each, splits, 0, 0, 0, 0, 0},
                                (static_cast<double>(rn) * (d + cols) + static_cast<double>(d) * cols) * sizeof(E), product, st};
                 float *so_far = reinterpret_cast<float *>(base + di_at) + (n_v > 1 ? r * R * d : 0), *part = reinterpret_cast<float *>(base + di_at) + (n_v > 1 ? n_r * R * d : 0);
                 E *out = static_cast<E *>(a.grad_in) + r0 * a.ld_gi;
@@ -815,7 +864,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 }
             }
             if (a.dW) {
-                const auto [tiles, splits, k_each] = grad_w_product<E>(direct_in, rn, d, cols, w_splits);
+                const auto [tiles, splits, k_each] = grad_w_product<E>(reads.grad_w, rn, d, cols, w_splits);
                 // a column's row blocks one after the other: they share its part of D
                 const Launch l{g, who, "xent_grad_w_kernel", TileItem{in_r, base + d_at, in.ld, ld_d, 0, 0, d, cols, rn, k_each, splits, 0, 0, 0, 0, 0, 64},
                                (static_cast<double>(rn) * (d + cols)) * sizeof(E) + 4.0 * splits * d * cols, product, st};
@@ -924,4 +973,22 @@ extern "C" heta_status heta_linear_xent_bwd(heta_graph *g, const heta_linear_xen
     }
     if (!a->grad_in && !a->dW && !a->dbias) return HETA_OK;
     return a->dt == HETA_F32 ? xent_backward<float>(g, *a, st) : xent_backward<bf16_t>(g, *a, st);
+}
+
+extern "C" heta_status heta_xent_reads(const heta_linear_xent_bwd_args *a, int32_t backward, int64_t *out)
+{
+    if (!a || !out) return fail(HETA_ERR_INVALID_ARG, "heta_xent_reads: null arguments");
+    const int64_t classes = backward ? piece_of_d(a->n_rows, a->n_classes, 2).classes : a->n_classes;
+    const XentReads r = xent_reads(a->n_rows, a->d, classes, a->in, a->ld_in, a->W, a->ld_w, backward != 0);
+    // bytes from the first row to behind the last one of a tile of so many, `there` of which exist
+    auto reach = [](bool direct, int64_t rows, int64_t there, int64_t ld) { return direct ? std::min(rows, there) * ld * 2 : 0; };
+    out[0] = r.copy_w;
+    out[1] = r.copy_in;
+    out[2] = r.logits;
+    out[3] = backward ? r.grad_in : 0;
+    out[4] = backward ? r.grad_w : 0;
+    out[5] = classes;
+    out[6] = std::max(reach(r.logits, kTileDepth, a->d, r.ld_w), reach(out[3] != 0, kTileRows, a->d, r.ld_w));
+    out[7] = std::max(reach(r.logits, kTileRows, a->n_rows, r.ld_in), reach(out[4] != 0, kTileDepth, a->n_rows, r.ld_in));
+    return HETA_OK;
 }

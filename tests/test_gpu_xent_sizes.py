@@ -1,0 +1,72 @@
+"""Cross entropy over millions of classes, whose rows of W are longer than 32-bit offsets of a tile reach, against the definition in 64 bits.
+
+Tolerances as for fewer classes, u = 2^-24, but for the two sums over all classes.  lse: 64 exponentials a part, and fewer than 40 joins of parts one after another (eight
+at a time by 64 threads in two steps, and two trees of six), five roundings each: (64 * 2 + 40 * 5 + 100) u < 500 u, where it is V / 8 + 100 by one addition after another.  grad_in: pieces of
+2^19 classes or fewer, or a whole of 4.3 M, split into parts of at most 20,000, of which there are at most 256, and 17 pieces: (2 * 20,000 + 300) u.
+"""
+import pytest
+import torch
+
+import paper_2408_09697_amd as heta
+from tests.test_gpu_xent import BF16, F32, STEP, U, Problem, within
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def handle():
+    g = heta.heta_graph_create([(1, 1, 0)], [])
+    yield g
+    g.destroy()
+    torch.cuda.empty_cache()
+
+
+# rows of 16.9 MB in pieces, unaligned ones, aligned ones of 8.5 MB, few rows: the logits straight into LDS, grad_in through registers
+@pytest.mark.parametrize("n,d,classes,pad", [(512, 256, 8_500_000, 0), (600, 64, 4_300_001, 0), (515, 72, 4_300_000, 0), (40, 64, 4_300_000, 0), (600, 24, 8_600_000, 3)])
+def test_millions_of_classes(handle, n, d, classes, pad):
+    p = Problem(n, d, classes, BF16, pad, scale=4.0)
+    p.forward(handle)
+    p.outputs(0, F32)
+    p.backward(handle)
+    x, W, b, y = p.x.double(), p.W.double(), p.bias.double(), p.y
+    Wa = W.abs()
+    has = (y >= 0) & (y < classes)
+    at = torch.where(has, y, 0)
+    f = torch.where(has, 1 / has.sum().double(), 0.0)
+    lse, e_lse, shown = [], [], torch.unique(torch.tensor([0, 1, n // 2, n - 1]))
+    for i in range(0, n, 16):
+        z = x[i:i + 16] @ W + b
+        ez = (2 * d + 16) * U * (x[i:i + 16].abs() @ Wa + b.abs()) + 4 * U * (z.abs() + b.abs())
+        lse.append(torch.logsumexp(z, 1))
+        e_lse.append(ez.amax(1) + (8 * z.abs().amax(1) + 500) * U)
+        zy, ezy = z.gather(1, at[i:i + 16, None])[:, 0], ez.gather(1, at[i:i + 16, None])[:, 0]
+        want = torch.where(has[i:i + 16], lse[-1] - zy, 0.0)
+        within(p.loss[i:i + 16], want, torch.where(has[i:i + 16], e_lse[-1] + ezy + 4 * U * (lse[-1].abs() + zy.abs()), 0.0), "loss")
+        for r in shown.tolist():
+            if i <= r < i + 16:  # this row's gradient
+                k = r - i
+                prob = torch.exp(z[k] - lse[-1][k])
+                D = prob.clone()
+                D[at[r]] -= 1
+                e = 1.1 * prob * (ez[k] + e_lse[-1][k] + 4 * U * (z[k].abs() + lse[-1][k].abs()) + 8 * U) + 4 * U * D.abs()
+                D, e = D * f[r], e * f[r]
+                e = e + STEP[BF16] * (D.abs() + e)
+                want = W @ D
+                bound = Wa @ e + (2 * 20000 + 300) * U * (Wa @ (D.abs() + e))
+                within(p.gx[r], want, bound + STEP[BF16] * (want.abs() + bound), "grad_in")
+    lse, e_lse = torch.cat(lse), torch.cat(e_lse)
+    within(p.lse, lse, e_lse + U * lse.abs(), "lse")
+    assert (p.gx[~has] == 0).all() and torch.isfinite(p.gW).all() and torch.isfinite(p.gb).all()
+    # the weights' and the bias's gradient of some classes, the rows' labels and the borders of pieces among them
+    cols = torch.unique(torch.cat([torch.linspace(0, classes - 1, 300, device="cuda", dtype=torch.float64).long(), at, torch.arange(1, classes // 2 ** 18, device="cuda") * 2 ** 18]))
+    Wc, bc = W[:, cols], b[cols]
+    z = x @ Wc + bc
+    ez = (2 * d + 16) * U * (x.abs() @ Wc.abs() + bc.abs()) + 4 * U * (z.abs() + bc.abs())
+    prob = torch.exp(z - lse[:, None])
+    D = prob - (cols[None, :] == at[:, None]).double()
+    e = (1.1 * prob * (ez + e_lse[:, None] + 4 * U * (z.abs() + lse.abs()[:, None]) + 8 * U) + 4 * U * D.abs()) * f[:, None]
+    D = D * f[:, None]
+    within(p.gb[cols], D.sum(0), e.sum(0) + (2 * n + 600) * U * D.abs().sum(0), "grad_bias")
+    e = e + STEP[BF16] * (D.abs() + e)
+    want, bound = x.t() @ D, x.abs().t() @ e
+    within(p.gW[:, cols], want, bound + (2 * n + 600) * U * (x.abs().t() @ (D.abs() + e)) + U * want.abs(), "grad_W")
