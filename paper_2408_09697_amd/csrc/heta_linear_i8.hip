@@ -122,12 +122,13 @@ template <typename T, int LANES, int NV> __global__ void __launch_bounds__(256) 
 template <typename T> __global__ void __launch_bounds__(256) rows_i8_wide_kernel(const T *x, int64_t ld_x, int64_t n_rows, int32_t d, int8_t *out, int64_t ld_out, float *scale)
 {
     __shared__ uint32_t tops[4];
+    const uint32_t width = static_cast<uint32_t>(d); // unsigned: a step past the widest row, of 2^31 - 1,024, is still ahead
     for (int64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
         const T *row = x + r * ld_x;
         uint32_t top = 0;
-        for (int c = threadIdx.x * 8; c < d; c += 2048) {
+        for (uint32_t c = threadIdx.x * 8; c < width; c += 2048) {
             float v[8];
-            load8(row + c, d - c, v);
+            load8(row + c, static_cast<int>(width - c), v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
         }
@@ -138,10 +139,10 @@ template <typename T> __global__ void __launch_bounds__(256) rows_i8_wide_kernel
         __syncthreads();
         const float amax = __uint_as_float(max(max(tops[0], tops[1]), max(tops[2], tops[3]))), f = i8_factor(amax);
         if (threadIdx.x == 0) scale[r] = i8_scale(amax);
-        for (int c = threadIdx.x * 8; c < d; c += 2048) {
+        for (uint32_t c = threadIdx.x * 8; c < width; c += 2048) {
             float v[8];
-            load8(row + c, d - c, v);
-            store_codes(reinterpret_cast<uint8_t *>(out) + r * ld_out + c, d - c, Codes8{{four_i8(v[0] * f, v[1] * f, v[2] * f, v[3] * f), four_i8(v[4] * f, v[5] * f, v[6] * f, v[7] * f)}});
+            load8(row + c, static_cast<int>(width - c), v);
+            store_codes(reinterpret_cast<uint8_t *>(out) + r * ld_out + c, static_cast<int>(width - c), Codes8{{four_i8(v[0] * f, v[1] * f, v[2] * f, v[3] * f), four_i8(v[4] * f, v[5] * f, v[6] * f, v[7] * f)}});
         }
     }
 }
