@@ -9,19 +9,24 @@ buffers and orders calls on torch's current stream; all arithmetic is in libheta
 """
 from __future__ import annotations
 
+import itertools
 from typing import Callable, Dict, List, Optional, Tuple
 
 import torch
 
 from . import binding as hb
 
+# Seeds of heads that are given none: one each, and far from those of trainers, which count their tensors from their own seed on (0 unless told otherwise).
+_SEEDS = itertools.count(1 << 31)
+
 
 class ClassifierHead:
     """g: any handle whose workspace the calls may use, one for each stream that runs them.  W [d, n_classes] of the embeddings' type (fp32 or bf16),
-    bias fp32 [n_classes] or None; state_bits, weight_decay: the update's (the bias has 32-bit states and no decay)."""
+    bias fp32 [n_classes] or None; state_bits, weight_decay: the update's (the bias has 32-bit states and no decay); seed: of W's 8-bit states, another one for
+    each tensor that has such (None: this head's own, 2^31 and one more for each head of the process)."""
 
-    def __init__(self, g: hb.Graph, W: torch.Tensor, bias: Optional[torch.Tensor] = None, state_bits: int = 32, weight_decay: float = 0.0, seed: int = 0):
-        self.g, self.W, self.bias, self.weight_decay, self.seed = g, W, bias, weight_decay, seed
+    def __init__(self, g: hb.Graph, W: torch.Tensor, bias: Optional[torch.Tensor] = None, state_bits: int = 32, weight_decay: float = 0.0, seed: Optional[int] = None):
+        self.g, self.W, self.bias, self.weight_decay, self.seed = g, W, bias, weight_decay, next(_SEEDS) if seed is None else seed
         self.states = [hb.heta_adamw_state(W, state_bits)] + ([] if bias is None else [hb.heta_adamw_state(bias)])
         self.saved: Optional[Dict[str, torch.Tensor]] = None
         self.grads: Dict[str, Optional[torch.Tensor]] = {}

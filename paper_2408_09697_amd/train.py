@@ -28,6 +28,7 @@ class MiniBatchTrainer:
     fanouts   : outermost hop first, e.g. [25, 20]
     state_bits, weight_decay: 8 keeps the optimizer states of weights and tables in 8 bits (heta_adamw_state), and either that or a weight decay
                 (of the weights; tables have none) makes the update heta_adamw_multi's instead of heta_sparse_adam_multi's
+    seed      : of the sampling; 8-bit states round by seed + the tensor's place among the weights and tables
     """
 
     def __init__(self, base: hb.Graph, tables: Sequence[torch.Tensor], W: Sequence[Sequence[torch.Tensor]],
