@@ -746,8 +746,9 @@ heta_status heta_linear_xent(heta_graph *g, const heta_linear_xent_args *args, v
  *   grad_in = D . W^T (dt);   dW = in^T . D (dw_dt: fp32, or bf16 for bf16 operands);   dbias[j] = sum_i D_ij (fp32)      each NULL: not computed
  * grad_loss: device fp32 [n_rows] or NULL; mean: what the forward wrote (gradients of the mean) or NULL (of the sum).  All outputs are overwritten; sums
  * are added in a fixed order.  The products read D rounded to dt.  The logits are formed again.
- * Uses the handle's workspace (may grow it: by 512 MB of D or D itself where that is less, a copy of the rows, partial sums of the gradients, and copies as
- * above, of weights also where a row has 16 MB and more; a copy of weights holds as many classes as the piece of D). */
+ * Uses the handle's workspace (may grow it: by 512 MB of D or D itself where that is less, a copy of the rows, partial sums of grad_W (512 MB and a sum, or those of
+ * one piece of D) and of dbias (64 MB likewise), 64 MB of partial sums of grad_in and, where the classes take several pieces, sums of all of it in fp32, and copies as above, of
+ * weights also where a row has 16 MB and more; a copy of weights holds as many classes as the piece of D). */
 typedef struct heta_linear_xent_bwd_args {
     int64_t n_rows;
     int32_t d, n_classes;

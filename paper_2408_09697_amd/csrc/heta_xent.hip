@@ -749,6 +749,39 @@ template <typename E> static SplitProduct grad_w_product(bool direct, int64_t n,
     return split_product<E>(direct, d, V, n, 256, kTilesLarge, 256, 128, slots, at_most);
 }
 
+// Partial sums that pieces of rows leave, one after another, until there is no room for more (if `bounded`): then they are added up into the first place, in order.
+struct Partials {
+    float *at; // [most, and one place in front of them if bounded][total]
+    int64_t total, most;
+    int32_t width; // a divisor of total
+    bool bounded;
+    float *joined; // [64][total], for sums of many parts of few columns; nullable
+    int64_t parts = 0, in_joined = 0;
+    bool added = false; // the first place holds a sum
+    float *next() const { return at + (bounded + parts) * total; }
+    heta_status make_room(int64_t n, hipStream_t st)
+    {
+        if (parts + n <= most) return HETA_OK;
+        HETA_TRY(join(st));
+        HETA_TRY(xent_add(nullptr, first(), static_cast<int>(count()), total, at, HETA_F32, width, width, nullptr, st));
+        parts = in_joined = 0;
+        added = true;
+        return HETA_OK;
+    }
+    // Many parts are first added up 64 ways: 5,469 strips of 349 columns take 27 us in one step, few workgroups of which have columns.
+    heta_status join(hipStream_t st)
+    {
+        if (!joined || count() <= 256) return HETA_OK;
+        const int64_t slots = count(), each = (slots + 63) / 64, groups = (total + 255) / 256, chunks = (slots + each - 1) / each;
+        hipLaunchKernelGGL(xent_column_sums_kernel, dim3(static_cast<unsigned>(chunks * groups)), dim3(256), 0, st, first(), slots, each, total, groups, joined);
+        HETA_LAUNCH_CHECK("xent_column_sums_kernel");
+        in_joined = chunks;
+        return HETA_OK;
+    }
+    const float *first() const { return in_joined > 0 ? joined : added ? at : at + bounded * total; }
+    int64_t count() const { return in_joined > 0 ? in_joined : parts + added; }
+};
+
 // Rows and classes of a piece of D: all of them, or kXentPiece bytes of pieces of one size.
 struct PieceOfD {
     int64_t rows, classes;
@@ -786,9 +819,12 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
     const size_t poison_at = ws.take(8), rows_at = ws.take(static_cast<size_t>(n) * sizeof(XentRow));
     const size_t w_at = ws.take(reads.copy_w ? static_cast<size_t>(d) * reads.ld_w * 2 : 0), in_at = ws.take(a.dW || reads.copy_in ? static_cast<size_t>(n) * ld_ic * sizeof(E) : 0);
     const size_t d_at = ws.take(static_cast<size_t>(R) * ld_d * sizeof(E));
-    const size_t sums_at = ws.take(a.dbias ? static_cast<size_t>((R + 31) / 32 * n_r) * Vc * 4 : 0);
+    // partial sums of one piece of rows at least, of all of them at most, between these 64 MB of D's columns' and 512 MB of grad_W's
+    const int64_t strips = (R + 31) / 32, all_sums = strips * n_r, most_sums = std::min(all_sums, std::max(strips, kXentPiece / 8 / (Vc * 4)));
+    const int64_t all_dw = w_splits * n_r, most_dw = std::min(all_dw, std::max<int64_t>(w_splits, kXentPiece / (d * Vc * 4)));
+    const size_t sums_at = ws.take(a.dbias ? static_cast<size_t>(most_sums + (most_sums < all_sums)) * Vc * 4 : 0);
     const size_t joined_at = ws.take(a.dbias ? static_cast<size_t>(64) * Vc * 4 : 0);
-    const size_t dw_at = ws.take(a.dW && (w_splits > 1 || n_r > 1) ? static_cast<size_t>(w_splits) * n_r * d * Vc * 4 : 0);
+    const size_t dw_at = ws.take(a.dW && (w_splits > 1 || n_r > 1) ? static_cast<size_t>(most_dw + (most_dw < all_dw)) * d * Vc * 4 : 0);
     // grad_in's sums over the classes so far, and in front of each piece's partial products
     const size_t di_at = ws.take(a.grad_in && (in_splits > 1 || n_v > 1) ? static_cast<size_t>(in_splits + (n_v > 1 ? n_r : 0)) * R * d * 4 : 0);
     if (a.grad_in && (n_v > 1 || in_splits > 1) && R * d > max_blocks(256) * 1024) return fail(HETA_ERR_UNSUPPORTED, "%s: input gradient too large for one launch", who);
@@ -819,7 +855,6 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
     if (reads.copy_in) in = {clean, ld_ic};
     HETA_LAUNCH_CHECK("xent_clean_kernel");
 
-    float *sums = a.dbias ? reinterpret_cast<float *>(base + sums_at) : nullptr;
     for (int64_t v = 0; v < n_v; ++v) {
         const int64_t v0 = v * Vc, cols = std::min(Vc, V - v0);
         const E *Wv = static_cast<const E *>(a.W) + v0;
@@ -830,8 +865,8 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
             HETA_LAUNCH_CHECK("xent_align_kernel");
             Wv = reinterpret_cast<const E *>(copy);
         }
-        float *dw = reinterpret_cast<float *>(base + dw_at);
-        int64_t bias_slots = 0, dw_parts = 0;
+        Partials sums{reinterpret_cast<float *>(base + sums_at), cols, most_sums, static_cast<int32_t>(cols), most_sums < all_sums, reinterpret_cast<float *>(base + joined_at)};
+        Partials dw{reinterpret_cast<float *>(base + dw_at), d * cols, most_dw, static_cast<int32_t>(cols), most_dw < all_dw, nullptr};
         for (int64_t r = 0; r < n_r; ++r) {
             const int64_t r0 = r * R, rn = std::min(R, n - r0);
             const E *in_r = static_cast<const E *>(in.p) + r0 * in.ld;
@@ -842,11 +877,13 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 const XentTiles tiles = logit_tiles_for<E>(reads.logits, rn, cols);
                 int64_t strip_rows = 0, strip_cols = 0;
                 strip_of<E, XentBackwardEpi<E>>(tiles, &strip_rows, &strip_cols);
-                const bool single = sums && n_r == 1 && rn <= strip_rows;
-                const XentBackward x{a.bias ? a.bias + v0 : nullptr, rows + r0, base + d_at, ld_d, single ? a.dbias + v0 : sums ? sums + bias_slots * cols : nullptr, v0,
+                const int64_t strips_here = (rn + strip_rows - 1) / strip_rows;
+                const bool single = a.dbias && n_r == 1 && strips_here == 1;
+                if (a.dbias && !single) HETA_TRY(sums.make_room(strips_here, st));
+                const XentBackward x{a.bias ? a.bias + v0 : nullptr, rows + r0, base + d_at, ld_d, single ? a.dbias + v0 : a.dbias ? sums.next() : nullptr, v0,
                                      single ? factor : nullptr};
                 HETA_TRY((go_tiles<E, false, true, XentBackwardEpi<E>>(l, tiles, x)));
-                if (sums && !single) bias_slots += (rn + strip_rows - 1) / strip_rows; // none without dbias: nothing is added up below
+                if (a.dbias && !single) sums.parts += strips_here; // none without dbias: nothing is added up below
             }
             if (a.grad_in) {
                 const auto [tiles, splits, k_each] = grad_in_product<E>(reads.grad_in, rn, d, cols, in_splits);
@@ -868,7 +905,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                 // a column's row blocks one after the other: they share its part of D
                 const Launch l{g, who, "xent_grad_w_kernel", TileItem{in_r, base + d_at, in.ld, ld_d, 0, 0, d, cols, rn, k_each, splits, 0, 0, 0, 0, 0, 64},
                                (static_cast<double>(rn) * (d + cols)) * sizeof(E) + 4.0 * splits * d * cols, product, st};
-                XentProduct x{dw + dw_parts * d * cols, cols, nullptr, clean + r0 * ld_ic, ld_ic, poison, call};
+                XentProduct x{nullptr, cols, nullptr, clean + r0 * ld_ic, ld_ic, poison, call};
                 if (splits == 1 && n_r == 1) {
                     x.out = static_cast<char *>(a.dW) + v0 * dtype_size(a.dw_dt);
                     x.ld = a.ld_dw;
@@ -876,25 +913,18 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
                     if (a.dw_dt == HETA_F32) HETA_TRY((go_tiles<E, true, true, XentProductEpi<float>>(l, tiles, x)));
                     else HETA_TRY((go_tiles<E, true, true, XentProductEpi<bf16_t>>(l, tiles, x)));
                 } else {
+                    HETA_TRY(dw.make_room(splits, st));
+                    x.out = dw.next();
                     HETA_TRY((go_tiles<E, true, true, XentProductEpi<float>>(l, tiles, x)));
-                    dw_parts += splits;
+                    dw.parts += splits;
                 }
             }
         }
-        const float *bias_parts = sums;
-        if (bias_slots > 256) { // 5,469 strips of 349 columns: 27 us in one step, few workgroups of which have columns
-            const int64_t each = (bias_slots + 63) / 64, groups = (cols + 255) / 256;
-            float *joined = reinterpret_cast<float *>(base + joined_at);
-            const int64_t all_slots = bias_slots;
-            bias_slots = (bias_slots + each - 1) / each;
-            hipLaunchKernelGGL(xent_column_sums_kernel, dim3(static_cast<unsigned>(bias_slots * groups)), dim3(256), 0, st, sums, all_slots, each, cols, groups, joined);
-            HETA_LAUNCH_CHECK("xent_column_sums_kernel");
-            bias_parts = joined;
-        }
-        if (bias_slots > 0) HETA_TRY(fold_partials(bias_parts, bias_slots, cols, a.dbias + v0, HETA_F32, static_cast<int32_t>(cols), cols, st, factor));
-        if (dw_parts > 0) {
+        HETA_TRY(sums.join(st));
+        if (sums.count() > 0) HETA_TRY(fold_partials(sums.first(), sums.count(), cols, a.dbias + v0, HETA_F32, static_cast<int32_t>(cols), cols, st, factor));
+        if (dw.count() > 0) {
             char *to = static_cast<char *>(a.dW) + v0 * dtype_size(a.dw_dt);
-            HETA_TRY(fold_partials(dw, dw_parts, d * cols, to, a.dw_dt, static_cast<int32_t>(cols), a.ld_dw, st, factor));
+            HETA_TRY(fold_partials(dw.first(), dw.count(), d * cols, to, a.dw_dt, static_cast<int32_t>(cols), a.ld_dw, st, factor));
         }
     }
     return HETA_OK;

@@ -70,3 +70,35 @@ def test_millions_of_classes(handle, n, d, classes, pad):
     e = e + STEP[BF16] * (D.abs() + e)
     want, bound = x.t() @ D, x.abs().t() @ e
     within(p.gW[:, cols], want, bound + (2 * n + 600) * U * (x.abs().t() @ (D.abs() + e)) + U * want.abs(), "grad_W")
+
+
+@pytest.mark.parametrize("dtype,n,d,classes,room", [(BF16, 300_000, 512, 20_000, 2100), (BF16, 300_000, 64, 20_000, 1200), (F32, 150_000, 64, 20_000, 860)])
+def test_partial_sums_of_many_rows_have_bounded_room(handle, dtype, n, d, classes, room):
+    """19 (13) pieces of rows, whose parts of grad_W (512: 57 parts of 21 MB) and of the column sums are more than 512 and 64 MB: `room` MB are what the header names, and less than with all
+    parts.  Norms as for fewer pieces: D's roundings (2^-8, or the bounds of fp32, below 2^-14) are independent of each other; a missing part of 57 would be 0.1 of it."""
+    g = heta.heta_graph_create([(1, 1, 0)], [])
+    p = Problem(n, d, classes, dtype)
+    heta.binding.heta_workspace_limit(room << 20)
+    try:
+        p.forward(g)
+        p.outputs()
+        p.backward(g)
+    finally:
+        heta.binding.heta_workspace_limit(0)
+    W, b = p.W.double(), p.bias.double()
+    has = (p.y >= 0) & (p.y < classes)
+    at, f = torch.where(has, p.y, 0)[:, None], has.double()[:, None] / has.sum()
+    gW, gb = torch.zeros(d, classes, device="cuda", dtype=torch.float64), torch.zeros(classes, device="cuda", dtype=torch.float64)
+    for i in range(0, n, 5000):
+        x = p.x[i:i + 5000].double()
+        D = torch.softmax(x @ W + b, 1)
+        D.scatter_add_(1, at[i:i + 5000], -torch.ones(len(x), 1, device="cuda", dtype=torch.float64))
+        D *= f[i:i + 5000]
+        gW += x.t() @ D
+        gb += D.sum(0)
+        want = D[:3] @ W.t()
+        assert float((p.gx[i:i + 3].double() - want).norm()) <= (2 * STEP[BF16] if dtype == BF16 else 2.0 ** -14) * float(want.norm())
+    assert float((p.gW.double() - gW).norm() / gW.norm()) <= (2 * STEP[BF16] if dtype == BF16 else 2.0 ** -14)
+    assert float((p.gb.double() - gb).norm() / gb.norm()) <= 2.0 ** -14
+    g.destroy()
+    torch.cuda.empty_cache()
