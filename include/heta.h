@@ -709,8 +709,8 @@ heta_status heta_linear_bwd(heta_graph *g, const heta_linear_bwd_args *args, voi
 heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int64_t ld_w, int32_t d_in, int32_t d_out, void *packed, int64_t ld_packed,
                                   float *scale, void *hip_stream);
 
-/* Rows in 8-bit whole numbers, for heta_linear: out_ij = the nearest whole number (ties to even) to 127 x_ij / max_j |x_ij|, scale_i = max_j |x_ij| / 127
- * (device fp32 [n_rows]); rows of nothing from 2^-119 on are zeros with scale 0, those with a NaN or an infinity have it as their scale.  x: fp32 or bf16
+/* Rows in 8-bit whole numbers, for heta_linear: out_ij = the nearest whole number (ties to even) to x_ij (127 (1 / max_j |x_ij|)) as fp32 forms it, each of the three
+ * rounded (what is within 3.1e-5 of half way may go to the other neighbour of the exact quotient), scale_i = max_j |x_ij| / 127, by the fp32 number next to 1 / 127 (device fp32 [n_rows]); rows of nothing from 2^-119 on are zeros with scale 0, those with a NaN or an infinity have it as their scale.  x: fp32 or bf16
  * [n_rows, ld_x]; out: device [n_rows, ld_out] of HETA_I8. */
 heta_status heta_linear_rows_i8(int64_t n_rows, int32_t d, const void *x, heta_dtype x_dt, int64_t ld_x, void *out, int64_t ld_out, float *scale, void *hip_stream);
 /* Weights W [d_in, d_out] (fp32 or bf16) as such rows: packed [d_out, ld_packed >= d_in] of HETA_I8, scale [d_out] = max_k |W[k, j]| / 127.  Once per set
@@ -780,6 +780,8 @@ heta_status heta_linear_xent_bwd(heta_graph *g, const heta_linear_xent_bwd_args 
  *   and a value goes to one of its two neighbours among the codes, up with probability (value - lower) / (upper - lower), by 16 bits that are a function of
  *   seed, step and the element's place alone; a sqrt(v) above 0 keeps a code above 0.  Zeros (codes and scales) are the state before the first step.  A NaN or
  *   an infinity among a block's new values makes the block NaN.  W's step is taken from the new values before they are rounded.
+ * step and what follows from it (the two corrections, the random bits) are taken when the call is made: a replay of a captured call is that same step once more, and rounds by the
+ * same bits.  Successive steps are calls of their own, not replays.
  * seed: of its own for each tensor with 8-bit states.  weight_decay: per item (0 for gains and biases, by custom).
  * All arrays are device memory, items a HOST array; no array that is written may overlap another one of the call.  All items are checked before the first
  * launch.  Items share launches: up to 64 that are contiguous with fp32 states, up to 24 others of the same types.  n_items = 0 is a no-op. */

@@ -1173,7 +1173,7 @@ def heta_adamw_plan(items: Sequence[Sequence]) -> AdamwPlan:
 
 
 def heta_adamw_multi(items, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 1, stream=None) -> None:
-    """One AdamW step (step = 1, 2, ...) on several tensors, in place; items: a heta_adamw_plan, or what makes one."""
+    """One AdamW step (step = 1, 2, ...) on several tensors, in place; items: a heta_adamw_plan, or what makes one.  A captured call repeats its step when it is replayed."""
     plan = items if isinstance(items, AdamwPlan) else AdamwPlan(items)
     _check(load_library().heta_adamw_multi(len(plan.items), plan.packed, lr, beta1, beta2, eps, int(step), _stream(stream)))
 

@@ -104,7 +104,7 @@ template <typename WT, typename GT> __global__ void __launch_bounds__(256) adamw
     store8(p.v + at, valid, v);
 }
 
-// 32 bits for the element that `x` stands for: two rounds of multiplication and shifts (the 32-bit finalizer that Appleby published in 2011, a bijection in which every
+// 32 bits for the element that `x` stands for: two rounds of multiplication and shifts (the 32-bit finalizer of MurmurHash3, which Appleby published in 2011, a bijection in which every
 // bit of the input changes about half of the output's), a key in front of each; x has the first one already.
 __device__ __forceinline__ uint32_t element_bits(uint32_t x, uint32_t key1)
 {
@@ -418,7 +418,7 @@ static heta_status adamw(int32_t n_items, const heta_adamw_item *items, float lr
                         hipLaunchKernelGGL((adamw_rows_kernel<decltype(w), decltype(g), decltype(codes)::value, decltype(stream)::value>), dim3(count), dim3(256), 0, st, q);
                     };
                     // Listed rows of more than the last-level cache holds are read and written with the streaming hint (200,000 of 1 M rows, 189 columns, fp32 with 8-bit
-                    // states: 191 us without, 162); whole tensors are faster without (1 M x 128: fp32 states 657 us, 695 with it; 8 bits 380, 394).
+                    // states: 191 us without, 179); whole tensors are faster without (1 M x 128: fp32 states 657 us, 695 with it; 8 bits 380, 394).
                     const bool stream = listed && streams(rows_bytes);
                     if (k >= 4) stream ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
                     else stream ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});

@@ -492,7 +492,10 @@ struct Operand {
 constexpr int64_t kTileRows = 256, kTileDepth = 64;
 static bool aligned_rows(const void *p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
 static bool offsets_fit(int64_t rows, int64_t ld) { return rows * ld * 2 < (int64_t(1) << 32); }
-// Whether the products are worth aligned copies of their operands: where the weights are read by several tiles.
+// Whether the products are worth aligned copies of operands whose rows start anywhere: a copy of the weights is a pass over them, tiles that read them through registers take longer the more of
+// them there are.  Forward + gradients, us, with copies / without: 256 x 30,011 by 256 rows 31 + 75 / 24 + 70, 384 28 + 97 / 31 + 107, 512 29 + 100 / 34 + 117, 4,096 97 + 318 / 178 +
+// 579; 512 x 300,001 by 128 rows 218 + 484 / 138 + 488, 256 239 + 587 / 238 + 813, 512 314 + 876 / 435 + 1,391; 256 x 349 by 512 rows 18 + 30 / 16 + 30.  In between, down to
+// some 300 rows over many classes, copies would already pay.
 static bool copies_pay(int64_t n) { return n >= 512; }
 struct XentReads {
     bool copy_w = false, copy_in = false;                 // to aligned rows first: of W, as many classes as a piece has
@@ -810,7 +813,7 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
     const heta_dtype dt = bf16 ? HETA_BF16 : HETA_F32;
     const auto [R, Vc] = piece_of_d(n, V, sizeof(E));
     const int64_t n_r = (n + R - 1) / R, n_v = (V + Vc - 1) / Vc;
-    // rows of D an odd number of 128 bytes apart (8,192 x 512 x 130,072: 5,760 us at 65,536 bytes, 5,515)
+    // rows of D are not multiples of 1,024 bytes apart (8,192 x 512 x 130,072: 5,760 us at 65,536 bytes, 5,515 with 128 bytes more)
     const int64_t ld_d = round_up(Vc, 8) + (round_up(Vc, 8) * static_cast<int64_t>(sizeof(E)) % 1024 == 0 ? 64 : 0);
     const XentReads reads = bf16 ? xent_reads(n, d, Vc, a.in, a.ld_in, a.W, a.ld_w, true) : XentReads{};
     const int64_t ld_ic = round_up(d, 8);
@@ -902,7 +905,8 @@ template <typename E> static heta_status xent_backward(heta_graph *g, const heta
             }
             if (a.dW) {
                 const auto [tiles, splits, k_each] = grad_w_product<E>(reads.grad_w, rn, d, cols, w_splits);
-                // a column's row blocks one after the other: they share its part of D
+                // a column's row blocks one after the other, where the contraction is whole: they share its part of D (all gradients of 8,192 x 512 x 131,072: 3,783 us row block by
+                // row block, 3,741 this way; of 700,000 x 256 x 349, which is split, the same)
                 const Launch l{g, who, "xent_grad_w_kernel", TileItem{in_r, base + d_at, in.ld, ld_d, 0, 0, d, cols, rn, k_each, splits, 0, 0, 0, 0, 0, 64},
                                (static_cast<double>(rn) * (d + cols)) * sizeof(E) + 4.0 * splits * d * cols, product, st};
                 XentProduct x{nullptr, cols, nullptr, clean + r0 * ld_ic, ld_ic, poison, call};

@@ -67,7 +67,7 @@ class ClassifierHead:
         return items
 
     def update(self, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8) -> None:
-        """One AdamW step with the last backward pass's gradients."""
+        """One AdamW step with the last backward pass's gradients.  Captured into a graph it stays that step: replays do not count (heta_adamw_multi)."""
         self.step += 1
         hb.heta_adamw_multi(self.adamw_items(), lr=lr, beta1=beta1, beta2=beta2, eps=eps, step=self.step)
 
