@@ -61,6 +61,8 @@ class ClassifierHead:
 
     def adamw_items(self) -> List[tuple]:
         """This head's part of a heta_adamw_multi call (a model's blocks and heads take one call together)."""
+        if not self.grads:
+            raise RuntimeError("backward has not run")
         items = [(self.W, self.states[0], self.grads["W"], self.weight_decay, None, self.seed)]
         if self.bias is not None:
             items.append((self.bias, self.states[1], self.grads["bias"]))
@@ -68,8 +70,8 @@ class ClassifierHead:
 
     def update(self, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8) -> None:
         """One AdamW step with the last backward pass's gradients.  Captured into a graph it stays that step: replays do not count (heta_adamw_multi)."""
+        hb.heta_adamw_multi(self.adamw_items(), lr=lr, beta1=beta1, beta2=beta2, eps=eps, step=self.step + 1)
         self.step += 1
-        hb.heta_adamw_multi(self.adamw_items(), lr=lr, beta1=beta1, beta2=beta2, eps=eps, step=self.step)
 
     def pack(self) -> Tuple[torch.Tensor, torch.Tensor]:
         """W as it is now in 8-bit whole numbers with a scale per class, for `scores`; to be packed again by whoever changes W."""
