@@ -102,3 +102,36 @@ def test_partial_sums_of_many_rows_have_bounded_room(handle, dtype, n, d, classe
     assert float((p.gb.double() - gb).norm() / gb.norm()) <= 2.0 ** -14
     g.destroy()
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_tens_of_millions_of_rows(handle, dtype):
+    """More rows than a forward pass takes at a time (2^26 of one strip of classes), and three pieces of D; the rows' own results, and the gradients' sums by their norms (D's roundings, 2^-8 or
+    below 2^-14, are independent; fp32 sums of 140,000 additions and fewer, 512 times: below 2^-14 for random signs)."""
+    n, d, classes = 70_000_003, 3, 5
+    p = Problem(n, d, classes, dtype)
+    p.forward(handle)
+    p.outputs()
+    p.backward(handle)
+    has = (p.y >= 0) & (p.y < classes)
+    count = float(has.sum())
+    gW, gb, total = 0, 0, 0.0
+    for i in range(0, n, 5_000_000):
+        q = Problem.__new__(Problem)
+        q.__dict__.update(p.__dict__)
+        at = slice(i, min(n, i + 5_000_000))
+        q.x, q.y, q.loss, q.lse = p.x[at], p.y[at], p.loss[at], p.lse[at]
+        q.n = len(q.y)
+        q.reference(torch.full((q.n,), 1 / count, device="cuda", dtype=torch.float64))
+        within(q.lse, q.r_lse, q.e_lse + U * q.r_lse.abs(), "lse")
+        within(q.loss, q.r_loss, q.e_loss, "loss")
+        e = q.eD + STEP[dtype] * (q.D.abs() + q.eD) * (dtype == BF16)
+        W = p.W.double()
+        want, bound = q.D @ W.t(), e @ W.abs().t() + (2 * classes + 600) * U * ((q.D.abs() + e) @ W.abs().t())
+        within(p.gx[at], want, bound + STEP[dtype] * (want.abs() + bound), "grad_in")
+        gW, gb, total = gW + q.x.double().t() @ q.D, gb + q.D.sum(0), total + float(q.r_loss.sum())
+    assert abs(float(p.mean[1]) - count) <= U * count and abs(float(p.mean[0]) - total / count) <= 1e-6 * total / count
+    room = 2 * STEP[BF16] if dtype == BF16 else 2.0 ** -14
+    assert float((p.gW.double() - gW).norm() / gW.norm()) <= room and float((p.gb.double() - gb).norm() / gb.norm()) <= 2.0 ** -12
+    del p, q
+    torch.cuda.empty_cache()
