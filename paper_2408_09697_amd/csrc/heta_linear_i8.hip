@@ -149,9 +149,9 @@ template <typename T> __global__ void __launch_bounds__(256) rows_i8_wide_kernel
 
 // ---- weights -------------------------------------------------------------------------------------------
 // Column j of W [d_in, d_out] becomes row j of the packed matrix.  Once per set of weights: one wavefront per column.
-template <typename T> __global__ void __launch_bounds__(256) pack_i8_kernel(const T *W, int64_t ld_w, int32_t d_in, int32_t d_out, int8_t *out, int64_t ld_out, float *scale)
+template <typename T> __global__ void __launch_bounds__(256) pack_i8_kernel(const T *W, int64_t ld_w, int32_t d_in, int32_t d_out, int8_t *out, int64_t ld_out, float *scale, unsigned first)
 {
-    const int64_t j = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t j = (static_cast<int64_t>(blockIdx.x) + first) * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (j >= d_out) return;
     uint32_t top = 0;
@@ -217,10 +217,11 @@ extern "C" heta_status heta_linear_pack_i8(const void *W, heta_dtype w_dt, int64
     if (o.overlaps(w) || s.overlaps(w) || s.overlaps(o)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);
     hipStream_t st = as_stream(hip_stream);
     ProfScope prof("pack_i8_kernel", st, static_cast<double>(d_in) * d_out * (2.0 * dtype_size(w_dt) + 1.0), 0);
-    if (w_dt == HETA_F32)
-        hipLaunchKernelGGL(pack_i8_kernel<float>, dim3((d_out + 3) / 4), dim3(256), 0, st, static_cast<const float *>(W), ld_w, d_in, d_out, static_cast<int8_t *>(packed), ld_packed, scale);
-    else
-        hipLaunchKernelGGL(pack_i8_kernel<bf16_t>, dim3((d_out + 3) / 4), dim3(256), 0, st, static_cast<const bf16_t *>(W), ld_w, d_in, d_out, static_cast<int8_t *>(packed), ld_packed, scale);
+    launch_pieces((d_out + 3) / 4, 256, [&](unsigned first, unsigned count) {
+        int8_t *const to = static_cast<int8_t *>(packed);
+        if (w_dt == HETA_F32) hipLaunchKernelGGL(pack_i8_kernel<float>, dim3(count), dim3(256), 0, st, static_cast<const float *>(W), ld_w, d_in, d_out, to, ld_packed, scale, first);
+        else hipLaunchKernelGGL(pack_i8_kernel<bf16_t>, dim3(count), dim3(256), 0, st, static_cast<const bf16_t *>(W), ld_w, d_in, d_out, to, ld_packed, scale, first);
+    });
     HETA_LAUNCH_CHECK("pack_i8_kernel");
     return HETA_OK;
 }
