@@ -157,9 +157,9 @@ template <typename E, int ACT, bool STREAM> __global__ void __launch_bounds__(25
 // ---- weights in 8 bits -------------------------------------------------------------------------------
 // Column j of W [d_in, d_out] becomes row j of the packed matrix [d_out, d_in], e4m3 with the scale max|W[:, j]| / 448.  Once per
 // set of weights: one wavefront per column.
-template <typename E> __global__ void __launch_bounds__(256) pack_e4m3_kernel(const E *W, int64_t ld_w, int32_t d_in, int32_t d_out, uint8_t *out, int64_t ld_out, float *scale)
+template <typename E> __global__ void __launch_bounds__(256) pack_e4m3_kernel(const E *W, int64_t ld_w, int32_t d_in, int32_t d_out, uint8_t *out, int64_t ld_out, float *scale, unsigned first)
 {
-    const int64_t j = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t j = (static_cast<int64_t>(blockIdx.x) + first) * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (j >= d_out) return;
     uint32_t top = 0;
@@ -347,12 +347,11 @@ extern "C" heta_status heta_linear_pack_e4m3(const void *W, heta_dtype w_dt, int
     if (o.overlaps(w) || s.overlaps(w) || s.overlaps(o)) return fail(HETA_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", who);
     hipStream_t st = as_stream(hip_stream);
     ProfScope prof("pack_e4m3_kernel", st, static_cast<double>(d_in) * d_out * (2.0 * dtype_size(w_dt) + 1.0), 0);
-    if (w_dt == HETA_F32)
-        hipLaunchKernelGGL(pack_e4m3_kernel<float>, dim3((d_out + 3) / 4), dim3(256), 0, st, static_cast<const float *>(W), ld_w, d_in, d_out,
-                           static_cast<uint8_t *>(packed), ld_packed, scale);
-    else
-        hipLaunchKernelGGL(pack_e4m3_kernel<bf16_t>, dim3((d_out + 3) / 4), dim3(256), 0, st, static_cast<const bf16_t *>(W), ld_w, d_in, d_out,
-                           static_cast<uint8_t *>(packed), ld_packed, scale);
+    launch_pieces((d_out + 3) / 4, 256, [&](unsigned first, unsigned count) {
+        uint8_t *const to = static_cast<uint8_t *>(packed);
+        if (w_dt == HETA_F32) hipLaunchKernelGGL(pack_e4m3_kernel<float>, dim3(count), dim3(256), 0, st, static_cast<const float *>(W), ld_w, d_in, d_out, to, ld_packed, scale, first);
+        else hipLaunchKernelGGL(pack_e4m3_kernel<bf16_t>, dim3(count), dim3(256), 0, st, static_cast<const bf16_t *>(W), ld_w, d_in, d_out, to, ld_packed, scale, first);
+    });
     HETA_LAUNCH_CHECK("pack_e4m3_kernel");
     return HETA_OK;
 }

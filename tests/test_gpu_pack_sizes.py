@@ -5,7 +5,7 @@ import torch
 import paper_2408_09697_amd as heta
 
 pytestmark = pytest.mark.gpu
-PACK = {torch.int8: (heta.binding.heta_linear_pack_i8, 127.0)}
+PACK = {torch.int8: (heta.binding.heta_linear_pack_i8, 127.0), torch.float8_e4m3fn: (heta.binding.heta_linear_pack_e4m3, 448.0)}
 
 
 @pytest.mark.parametrize("dtype", list(PACK))
